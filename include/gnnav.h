@@ -472,6 +472,102 @@ gnnav_status gnnav_weight_grad(const float *self_dev, int64_t ld_self, const flo
                                int64_t ld_agg, int64_t m, int64_t d_in, const float *dz_dev,
                                int64_t ld_dz, int64_t d_out, float *dw_dev, void *stream);
 
+/* ------------------------------------------------------- trained tables ---
+ * A table of trained rows (node embeddings), n_rows x d on the device, in the
+ * place of fixed features: its lookup for a frontier and the gradient of that
+ * lookup.  dt = F32 or BF16; all rows on 16-byte boundaries.
+ *
+ * gnnav_embedding: out row i = scale * table row ids_dev[i], in fp32, rounded once;
+ * an id outside [0, n_rows) gives a zero row.  The columns of out from d up to
+ * the next 16-byte boundary are written with zeros.  n_ids_dev (may be NULL): a
+ * device int32 read when the work runs; only the first min(n_ids, *n_ids_dev)
+ * rows are then written.
+ *
+ * gnnav_embedding_backward: dtable row v = scale * sum over the i with
+ * ids_dev[i] = v of dout row i, summed in fp32 in a fixed order that depends on
+ * the ids alone (no floating-point atomics: repeated calls give identical bits)
+ * and rounded once.  accumulate = 0: every row of dtable is written, with zeros
+ * where no id names it; otherwise the sums are added to dtable's rows and the rows
+ * that no id names stay as they are.  Ids outside [0, n_rows) are left out.
+ * n_ids_dev as above.  workspace_dev: device memory of at least
+ * gnnav_embedding_backward_workspace bytes (0 for few ids; -1 for bad
+ * arguments; host only) on a 256-byte boundary, used until the work has run; its
+ * contents do not matter.  No call allocates; calls that use different
+ * workspaces may overlap.
+ * Errors: E_INVALID (null pointers, sizes, strides, alignment, workspace),
+ * E_CAPACITY (a size beyond int32), E_DEVICE.  Asynchronous.               */
+gnnav_status gnnav_embedding(const void *table_dev, int64_t n_rows, int64_t ld_table, int64_t d,
+                             gnnav_dtype dt, const int32_t *ids_dev, const int32_t *n_ids_dev,
+                             int64_t n_ids, float scale, void *out_dev, int64_t ld_out, void *stream);
+int64_t gnnav_embedding_backward_workspace(int64_t n_ids, int64_t n_rows, int64_t d, gnnav_dtype dt);
+gnnav_status gnnav_embedding_backward(const void *dout_dev, int64_t ld_dout, const int32_t *ids_dev,
+                                      const int32_t *n_ids_dev, int64_t n_ids, int64_t d, gnnav_dtype dt,
+                                      float scale, int32_t accumulate, void *dtable_dev, int64_t n_rows,
+                                      int64_t ld_table, void *workspace_dev, int64_t workspace_bytes,
+                                      void *stream);
+
+/* ----------------------------------------------- cross entropy, many classes ---
+ * Softmax cross entropy of m rows h against n_classes rows w (one per class, e.g.
+ * a table of trained rows), both with d columns, without the m x n_classes
+ * logits: with z_iv = h_i . w_v and lse_i = log sum_v exp z_iv,
+ *   row_loss[i] = lse_i - z_i,y(i),  y = labels_dev (device int32[m]);
+ *   loss_dev[0] = mean of row_loss over the rows that count;
+ *   dh_i = (1/N) (sum_v p_iv w_v - w_y),  dw_v = (1/N) sum_i (p_iv - [v = y_i]) h_i,
+ *   p_iv = exp(z_iv - lse_i), N = the rows that count.
+ * Rows whose label is ignore_label do not count: row_loss 0, zero gradients, and
+ * their h is not used (it may hold anything).  No rows that count: loss 0,
+ * zero gradients.  Any other label outside [0, n_classes) makes its row's
+ * loss NaN (so the mean is NaN) and its gradients zero; it counts.  n_classes
+ * may be anything from 1; m = 0 is allowed.
+ * dt = F32: fp32-accurate products (six bf16 part products; an infinite entry
+ * of a row that counts or of w makes its logits NaN).  dt = BF16: bf16
+ * operands, fp32 accumulation and statistics; p - [v = y] is rounded to bf16
+ * before the gradients' products, the gradients once to bf16.  exp of less than
+ * 2^-126 counts as 0.  row_loss_dev,
+ * dh_dev, dw_dev may be NULL; dh and dw are of type dt, every row written, the
+ * columns from d up to the next 16-byte boundary with zeros.  Results do not
+ * depend on the run (no atomics).  workspace_dev: at least
+ * gnnav_linear_xent_workspace bytes (grads: whether dh or dw is asked for; -1
+ * for bad arguments; host only) on a 256-byte boundary.  Its size grows with m, d and
+ * n_classes / 256, not with their product.  No call allocates.
+ * Errors: E_INVALID (null pointers, sizes, strides, alignment, workspace),
+ * E_CAPACITY (a size beyond int32), E_DEVICE.  Asynchronous.               */
+int64_t gnnav_linear_xent_workspace(int64_t m, int64_t n_classes, int64_t d, gnnav_dtype dt, int32_t grads);
+gnnav_status gnnav_linear_xent(const void *h_dev, int64_t ld_h, int64_t m, const void *w_dev, int64_t ld_w,
+                               int64_t n_classes, int64_t d, gnnav_dtype dt, const int32_t *labels_dev,
+                               int32_t ignore_label, float *loss_dev, float *row_loss_dev, void *dh_dev,
+                               int64_t ld_dh, void *dw_dev, int64_t ld_dw, void *workspace_dev,
+                               int64_t workspace_bytes, void *stream);
+
+/* ------------------------------------------------------ gradient clipping ---
+ * Over n_tensors device tensors of one type (host arrays of device pointers and
+ * element counts, read before the call returns; contiguous, aligned to their
+ * element; counts may be 0):
+ *   norm = sqrt(sum of all squares), summed in 64 bits in a fixed order, written
+ *   to norm_dev[0] in fp32;  c = 1 if norm <= max_norm, else max_norm / norm.
+ * gnnav_grad_norm: the norm alone.
+ * gnnav_clip_grads: out[k] = c * grads[k]; out may name the gradients
+ * themselves (in place).
+ * gnnav_sgd_clip_step: weights[k] -= (lr * c) * grads[k], in place.
+ * All in fp32, rounded once to dt.  An infinite norm gives c = 0 (NaN where the
+ * gradient is infinite), a NaN one c = NaN.  Tensors of one call must not overlap
+ * unless out[k] is grads[k].  workspace_dev: at least gnnav_clip_workspace bytes (host only)
+ * on a 256-byte boundary.  No call allocates.
+ * Errors: E_INVALID (null pointers, negative counts, misaligned tensors,
+ * max_norm negative or NaN, lr not finite, workspace), E_CAPACITY (more than
+ * 2^45 elements), E_DEVICE.  Asynchronous.                                 */
+int64_t gnnav_clip_workspace(int32_t n_tensors);
+gnnav_status gnnav_grad_norm(int32_t n_tensors, const void *const *grads, const int64_t *counts,
+                             gnnav_dtype dt, float *norm_dev, void *workspace_dev,
+                             int64_t workspace_bytes, void *stream);
+gnnav_status gnnav_clip_grads(int32_t n_tensors, const void *const *grads, const int64_t *counts,
+                              gnnav_dtype dt, float max_norm, void *const *out, float *norm_dev,
+                              void *workspace_dev, int64_t workspace_bytes, void *stream);
+gnnav_status gnnav_sgd_clip_step(int32_t n_tensors, void *const *weights, const void *const *grads,
+                                 const int64_t *counts, gnnav_dtype dt, float lr, float max_norm,
+                                 float *norm_dev, void *workspace_dev, int64_t workspace_bytes,
+                                 void *stream);
+
 /* -------------------------------------------------- locality-biased sampler ---
  * gnnav_sample with the neighbour-selection probability made a function of
  * data locality, p(eta) (Section 3.2, the sampler abstraction that

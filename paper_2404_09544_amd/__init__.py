@@ -44,6 +44,9 @@ EXPORTS = [
     "gnnav_profile_stop", "gnnav_profile_count", "gnnav_profile_get", "gnnav_profile_samples",
     "gnnav_sync", "gnnav_debug_set_spin_limit", "gnnav_debug_fail_allocations", "gnnav_gather_noalloc",
     "gnnav_stream_create", "gnnav_stream_destroy",
+    "gnnav_embedding", "gnnav_embedding_backward", "gnnav_embedding_backward_workspace",
+    "gnnav_linear_xent", "gnnav_linear_xent_workspace",
+    "gnnav_grad_norm", "gnnav_clip_grads", "gnnav_sgd_clip_step", "gnnav_clip_workspace",
 ]
 
 
@@ -105,6 +108,15 @@ _sig = {
     "gnnav_gather_noalloc": ([P, P, i64, P, i64, P, P], i32),
     "gnnav_stream_create": ([i32, i32, P], i32),
     "gnnav_stream_destroy": ([P], i32),
+    "gnnav_embedding": ([P, i64, i64, i64, i32, P, P, i64, C.c_float, P, i64, P], i32),
+    "gnnav_embedding_backward": ([P, i64, P, P, i64, i64, i32, C.c_float, i32, P, i64, i64, P, i64, P], i32),
+    "gnnav_embedding_backward_workspace": ([i64, i64, i64, i32], i64),
+    "gnnav_linear_xent": ([P, i64, i64, P, i64, i64, i64, i32, P, i32, P, P, P, i64, P, i64, P, i64, P], i32),
+    "gnnav_linear_xent_workspace": ([i64, i64, i64, i32, i32], i64),
+    "gnnav_grad_norm": ([i32, P, P, i32, P, P, i64, P], i32),
+    "gnnav_clip_grads": ([i32, P, P, i32, C.c_float, P, P, P, i64, P], i32),
+    "gnnav_sgd_clip_step": ([i32, P, P, P, i32, C.c_float, C.c_float, P, P, i64, P], i32),
+    "gnnav_clip_workspace": ([i32], i64),
 }
 for _name, (_args, _res) in _sig.items():
     _f = getattr(_lib, _name)
@@ -475,6 +487,192 @@ def sage_forward(blocks: Blocks, x, weights, dims, dtype: str, logits, stream=No
     _check(_lib.gnnav_sage_forward(blocks._h, _dev_ptr(x), x.stride(0), wp, _np_ptr(dm), L,
                                    dtype_code(dtype), _dev_ptr(logits), logits.stride(0),
                                    _stream(stream)))
+
+
+# ------------------------------------- trained tables and large class sets
+_TORCH_CODE = {torch.float32: F32, torch.bfloat16: BF16}
+
+
+def _rows(t, what: str, d: int = None, dtype=None):
+    """Checks a device matrix argument with contiguous columns (rows of any stride)."""
+    if t.dim() != 2 or not t.is_cuda or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError(f"{what} must be a device matrix with contiguous columns")
+    if t.dtype not in _TORCH_CODE or (dtype is not None and t.dtype != dtype):
+        raise ValueError(f"{what} must be {dtype or 'float32 or bfloat16'}")
+    if d is not None and t.shape[1] != d:
+        raise ValueError(f"{what} must have {d} columns")
+    _here(t, what)
+    return t
+
+
+def _here(t, what: str):
+    if t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{what} is not on the current device")
+
+
+def _vector(t, what: str, dtype, n: int = None):
+    if not t.is_cuda or t.dtype != dtype or not t.is_contiguous() or (n is not None and t.numel() < n):
+        raise ValueError(f"{what} must be a contiguous device {dtype} tensor" + (f" of {n}" if n is not None else ""))
+    _here(t, what)
+    return t
+
+
+def _workspace(given, need: int, stream):
+    """(pointer, bytes, tensor that holds them) of a call's workspace; one that is not given comes
+    from torch's allocator, in the pool of the stream the call runs on."""
+    if given is not None:
+        _vector(given, "workspace", torch.uint8)
+        return given.data_ptr(), given.numel(), given
+    if need == 0:
+        return None, 0, None
+    if stream is None:
+        t = torch.empty(need, dtype=torch.uint8, device="cuda")
+    else:
+        st = stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(int(stream))
+        with torch.cuda.stream(st):
+            t = torch.empty(need, dtype=torch.uint8, device="cuda")
+    return t.data_ptr(), need, t
+
+
+def embedding(table, ids, out, scale: float = 1.0, n_ids_dev=None, stream=None):
+    """gnnav_embedding: out[i] = scale * table[ids[i]] for the table's type (fp32 or
+    bf16); an id outside the table gives a zero row.  ids: device int32;
+    n_ids_dev: optional device int32 tensor with the count of ids to take."""
+    d = _rows(table, "table").shape[1]
+    _rows(out, "out", d, table.dtype)
+    n = _vector(ids, "ids", torch.int32).numel()
+    if out.shape[0] < n:
+        raise ValueError("out has fewer rows than ids")
+    _check(_lib.gnnav_embedding(_dev_ptr(table), table.shape[0], table.stride(0), d, _TORCH_CODE[table.dtype],
+                                _dev_ptr(ids), _count_ptr(n_ids_dev), n, float(scale), _dev_ptr(out), out.stride(0),
+                                _stream(stream)))
+
+
+def _count_ptr(t):
+    return None if t is None else _vector(t, "n_ids_dev", torch.int32, 1).data_ptr()
+
+
+def embedding_backward_workspace(n_ids: int, n_rows: int, d: int, dtype: str) -> int:
+    """Bytes of workspace that embedding_backward needs."""
+    return _workspace_bytes(_lib.gnnav_embedding_backward_workspace(int(n_ids), int(n_rows), int(d), dtype_code(dtype)))
+
+
+def _workspace_bytes(n: int) -> int:
+    if n < 0:
+        raise GnnavError(1, "bad workspace arguments")
+    return int(n)
+
+
+def embedding_backward(dout, ids, dtable, scale: float = 1.0, accumulate: bool = False, n_ids_dev=None,
+                       workspace=None, stream=None):
+    """gnnav_embedding_backward: dtable[v] (+)= scale * the sum of the rows of dout whose id is v."""
+    d = _rows(dout, "dout").shape[1]
+    _rows(dtable, "dtable", d, dout.dtype)
+    n = _vector(ids, "ids", torch.int32).numel()
+    if dout.shape[0] < n:
+        raise ValueError("dout has fewer rows than ids")
+    code = _TORCH_CODE[dout.dtype]
+    need = 0 if workspace is not None else _workspace_bytes(
+        _lib.gnnav_embedding_backward_workspace(n, dtable.shape[0], d, code))
+    ws, ws_bytes, _hold = _workspace(workspace, need, stream)
+    _check(_lib.gnnav_embedding_backward(_dev_ptr(dout), dout.stride(0), _dev_ptr(ids), _count_ptr(n_ids_dev), n, d,
+                                         code, float(scale), int(bool(accumulate)), _dev_ptr(dtable),
+                                         dtable.shape[0], dtable.stride(0), ws, ws_bytes, _stream(stream)))
+
+
+def linear_xent_workspace(m: int, n_classes: int, d: int, dtype: str, grads: bool = True) -> int:
+    """Bytes of workspace that linear_xent needs (grads: whether dh or dw is asked for)."""
+    return _workspace_bytes(_lib.gnnav_linear_xent_workspace(int(m), int(n_classes), int(d), dtype_code(dtype),
+                                                             int(bool(grads))))
+
+
+def linear_xent(h, w, labels, loss, row_loss=None, dh=None, dw=None, ignore_label: int = -1, workspace=None,
+                stream=None):
+    """gnnav_linear_xent: softmax cross entropy of h [m, d] against the classes' rows w
+    [n_classes, d] without the logits.  loss: float32[1], the mean over the rows
+    whose label is not ignore_label; row_loss (float32[m]), dh [m, d] and dw
+    [n_classes, d] are written where given."""
+    m, d = _rows(h, "h").shape
+    _rows(w, "w", d, h.dtype)
+    _vector(labels, "labels", torch.int32, m)
+    _vector(loss, "loss", torch.float32, 1)
+    if row_loss is not None:
+        _vector(row_loss, "row_loss", torch.float32, m)
+    if dh is not None and _rows(dh, "dh", d, h.dtype).shape[0] < m:
+        raise ValueError("dh has fewer rows than h")
+    if dw is not None and _rows(dw, "dw", d, h.dtype).shape[0] < w.shape[0]:
+        raise ValueError("dw has fewer rows than w")
+    code = _TORCH_CODE[h.dtype]
+    need = 0 if workspace is not None else _workspace_bytes(
+        _lib.gnnav_linear_xent_workspace(m, w.shape[0], d, code, int(dh is not None or dw is not None)))
+    ws, ws_bytes, _hold = _workspace(workspace, need, stream)
+    _check(_lib.gnnav_linear_xent(_dev_ptr(h), h.stride(0), m, _dev_ptr(w), w.stride(0), w.shape[0], d, code,
+                                  _dev_ptr(labels), int(ignore_label), _dev_ptr(loss), _dev_ptr(row_loss),
+                                  _dev_ptr(dh), dh.stride(0) if dh is not None else 0, _dev_ptr(dw),
+                                  dw.stride(0) if dw is not None else 0, ws, ws_bytes, _stream(stream)))
+
+
+class TensorList:
+    """Contiguous device tensors of one type, with the pointer and count arrays
+    that the calls over many tensors take.  Holds the tensors."""
+
+    def __init__(self, tensors):
+        self.tensors = list(tensors)
+        types = {t.dtype for t in self.tensors} or {torch.float32}
+        if len(types) > 1 or next(iter(types)) not in _TORCH_CODE:
+            raise ValueError("tensors must be all float32 or all bfloat16")
+        for t in self.tensors:
+            if not t.is_cuda or not t.is_contiguous():
+                raise ValueError("tensors must be contiguous device tensors")
+            _here(t, "a tensor")
+        self.code = _TORCH_CODE[next(iter(types))]
+        self.n = len(self.tensors)
+        self.shapes = [t.numel() for t in self.tensors]
+        self.ptrs = (P * max(self.n, 1))(*[t.data_ptr() for t in self.tensors])
+        self.counts = (i64 * max(self.n, 1))(*self.shapes)
+
+
+def _tensor_list(x) -> TensorList:
+    return x if isinstance(x, TensorList) else TensorList(x)
+
+
+def _same(a: TensorList, b: TensorList, what: str):
+    if a.shapes != b.shapes or (a.n and a.code != b.code):
+        raise ValueError(f"{what} must match the gradients in number, sizes and type")
+    return b
+
+
+def clip_workspace(grads) -> int:
+    """Bytes of workspace that grad_norm, clip_grads and sgd_clip_step need."""
+    return int(_lib.gnnav_clip_workspace(_tensor_list(grads).n))
+
+
+def grad_norm(grads, norm, workspace=None, stream=None):
+    """gnnav_grad_norm: norm[0] = the global 2-norm of the tensors (a list or a TensorList)."""
+    g = _tensor_list(grads)
+    _vector(norm, "norm", torch.float32, 1)
+    ws, ws_bytes, _hold = _workspace(workspace, clip_workspace(g), stream)
+    _check(_lib.gnnav_grad_norm(g.n, g.ptrs, g.counts, g.code, _dev_ptr(norm), ws, ws_bytes, _stream(stream)))
+
+
+def clip_grads(grads, max_norm: float, norm, out=None, workspace=None, stream=None):
+    """gnnav_clip_grads: the tensors times min(1, max_norm / norm), in place or into `out`."""
+    g = _tensor_list(grads)
+    o = g if out is None else _same(g, _tensor_list(out), "out")
+    _vector(norm, "norm", torch.float32, 1)
+    ws, ws_bytes, _hold = _workspace(workspace, clip_workspace(g), stream)
+    _check(_lib.gnnav_clip_grads(g.n, g.ptrs, g.counts, g.code, float(max_norm), o.ptrs, _dev_ptr(norm), ws, ws_bytes,
+                                 _stream(stream)))
+
+
+def sgd_clip_step(weights, grads, lr: float, max_norm: float, norm, workspace=None, stream=None):
+    """gnnav_sgd_clip_step: weights -= lr * min(1, max_norm / norm) * grads, in place."""
+    g = _tensor_list(grads)
+    w = _same(g, _tensor_list(weights), "weights")
+    _vector(norm, "norm", torch.float32, 1)
+    ws, ws_bytes, _hold = _workspace(workspace, clip_workspace(g), stream)
+    _check(_lib.gnnav_sgd_clip_step(g.n, w.ptrs, g.ptrs, g.counts, g.code, float(lr), float(max_norm), _dev_ptr(norm),
+                                    ws, ws_bytes, _stream(stream)))
 
 
 # -------------------------------------------------------------- profiling

@@ -1575,3 +1575,151 @@ extern "C" gnnav_status gnnav_weight_grad(const float *self_dev, int64_t ld_self
         });
     });
 }
+
+// ------------------------------------------- trained tables and large class sets
+namespace {
+// Rows of a matrix argument: present, on 16-byte boundaries, not narrower than d.
+void check_rows(const void *p, int64_t ld, int64_t d, int64_t elt, const char *what) {
+    GNNAV_CHECK(p, GNNAV_E_INVALID, std::string("NULL ") + what);
+    GNNAV_CHECK(ld >= d && (ld * elt) % 16 == 0 && aligned16(p), GNNAV_E_INVALID,
+                std::string(what) + " rows must be 16-byte aligned with a stride of at least d");
+}
+void check_workspace(const void *ws, int64_t bytes, size_t need) {
+    GNNAV_CHECK(bytes >= (int64_t)need, GNNAV_E_INVALID,
+                "workspace of " + std::to_string(bytes) + " bytes, " + std::to_string(need) + " needed");
+    GNNAV_CHECK(need == 0 || (ws && ((uintptr_t)ws & 255u) == 0), GNNAV_E_INVALID,
+                "workspace must be on a 256-byte boundary");
+}
+bool dtype_ok(gnnav_dtype dt) { return dt == GNNAV_F32 || dt == GNNAV_BF16; }
+}  // namespace
+
+extern "C" gnnav_status gnnav_embedding(const void *table_dev, int64_t n_rows, int64_t ld_table, int64_t d,
+                                        gnnav_dtype dt, const int32_t *ids_dev, const int32_t *n_ids_dev,
+                                        int64_t n_ids, float scale, void *out_dev, int64_t ld_out, void *stream) {
+    return guarded([&] {
+        GNNAV_CHECK(dtype_ok(dt), GNNAV_E_INVALID, "bad dtype");
+        GNNAV_CHECK(n_rows >= 0 && n_ids >= 0 && d > 0, GNNAV_E_INVALID, "negative size or d <= 0");
+        GNNAV_CHECK(n_rows <= INT32_MAX && n_ids <= INT32_MAX && d <= INT32_MAX, GNNAV_E_CAPACITY, "sizes beyond int32");
+        if (n_ids == 0) return;
+        const int64_t elt = dt == GNNAV_BF16 ? 2 : 4;
+        GNNAV_CHECK(ids_dev, GNNAV_E_INVALID, "NULL ids");
+        if (n_rows > 0) check_rows(table_dev, ld_table, d, elt, "table");
+        check_rows(out_dev, ld_out, d, elt, "out");
+        launch_embedding(table_dev, n_rows, ld_table * elt, d, dt == GNNAV_BF16, ids_dev, n_ids_dev, n_ids, scale,
+                         out_dev, ld_out * elt, (hipStream_t)stream);
+    });
+}
+
+extern "C" int64_t gnnav_embedding_backward_workspace(int64_t n_ids, int64_t n_rows, int64_t d, gnnav_dtype dt) {
+    if (!dtype_ok(dt) || n_ids < 0 || n_rows < 0 || d <= 0 || n_ids > INT32_MAX || n_rows > INT32_MAX || d > INT32_MAX)
+        return -1;
+    return (int64_t)embedding_backward_workspace(n_ids, n_rows, d, dt == GNNAV_BF16);
+}
+
+extern "C" gnnav_status gnnav_embedding_backward(const void *dout_dev, int64_t ld_dout, const int32_t *ids_dev,
+                                                 const int32_t *n_ids_dev, int64_t n_ids, int64_t d, gnnav_dtype dt,
+                                                 float scale, int32_t accumulate, void *dtable_dev, int64_t n_rows,
+                                                 int64_t ld_table, void *workspace_dev, int64_t workspace_bytes,
+                                                 void *stream) {
+    return guarded([&] {
+        GNNAV_CHECK(dtype_ok(dt), GNNAV_E_INVALID, "bad dtype");
+        GNNAV_CHECK(n_rows >= 0 && n_ids >= 0 && d > 0, GNNAV_E_INVALID, "negative size or d <= 0");
+        GNNAV_CHECK(n_rows <= INT32_MAX && n_ids <= INT32_MAX && d <= INT32_MAX, GNNAV_E_CAPACITY, "sizes beyond int32");
+        if (n_rows == 0 || (n_ids == 0 && accumulate)) return;
+        const int64_t elt = dt == GNNAV_BF16 ? 2 : 4;
+        check_rows(dtable_dev, ld_table, d, elt, "dtable");
+        if (n_ids > 0) {
+            GNNAV_CHECK(ids_dev, GNNAV_E_INVALID, "NULL ids");
+            check_rows(dout_dev, ld_dout, d, elt, "dout");
+        }
+        check_workspace(workspace_dev, workspace_bytes, embedding_backward_workspace(n_ids, n_rows, d, dt == GNNAV_BF16));
+        launch_embedding_backward(dout_dev, ld_dout * elt, ids_dev, n_ids_dev, n_ids, d, dt == GNNAV_BF16, scale,
+                                  accumulate != 0, dtable_dev, n_rows, ld_table * elt, workspace_dev,
+                                  (hipStream_t)stream);
+    });
+}
+
+extern "C" int64_t gnnav_linear_xent_workspace(int64_t m, int64_t n_classes, int64_t d, gnnav_dtype dt, int32_t grads) {
+    if (!dtype_ok(dt) || m < 0 || n_classes <= 0 || d <= 0 || m > INT32_MAX || n_classes > INT32_MAX || d > INT32_MAX)
+        return -1;
+    return (int64_t)linear_xent_workspace(m, n_classes, d, dt == GNNAV_BF16, grads != 0);
+}
+
+extern "C" gnnav_status gnnav_linear_xent(const void *h_dev, int64_t ld_h, int64_t m, const void *w_dev, int64_t ld_w,
+                                          int64_t n_classes, int64_t d, gnnav_dtype dt, const int32_t *labels_dev,
+                                          int32_t ignore_label, float *loss_dev, float *row_loss_dev, void *dh_dev,
+                                          int64_t ld_dh, void *dw_dev, int64_t ld_dw, void *workspace_dev,
+                                          int64_t workspace_bytes, void *stream) {
+    return guarded([&] {
+        GNNAV_CHECK(dtype_ok(dt), GNNAV_E_INVALID, "bad dtype");
+        GNNAV_CHECK(m >= 0 && n_classes > 0 && d > 0, GNNAV_E_INVALID, "m < 0, or n_classes or d <= 0");
+        GNNAV_CHECK(m <= INT32_MAX && n_classes <= INT32_MAX && d <= INT32_MAX, GNNAV_E_CAPACITY, "sizes beyond int32");
+        GNNAV_CHECK(loss_dev, GNNAV_E_INVALID, "NULL loss");
+        const int64_t elt = dt == GNNAV_BF16 ? 2 : 4;
+        check_rows(w_dev, ld_w, d, elt, "w");
+        if (m > 0) {
+            GNNAV_CHECK(labels_dev, GNNAV_E_INVALID, "NULL labels");
+            check_rows(h_dev, ld_h, d, elt, "h");
+        }
+        if (dh_dev) check_rows(dh_dev, ld_dh, d, elt, "dh");
+        if (dw_dev) check_rows(dw_dev, ld_dw, d, elt, "dw");
+        check_workspace(workspace_dev, workspace_bytes,
+                        linear_xent_workspace(m, n_classes, d, dt == GNNAV_BF16, dh_dev || dw_dev));
+        LinearXentArgs x = {h_dev, ld_h, m, w_dev, ld_w, n_classes, d, dt == GNNAV_BF16, labels_dev, ignore_label,
+                            loss_dev, row_loss_dev, dh_dev, ld_dh, dw_dev, ld_dw, workspace_dev};
+        launch_linear_xent(x, (hipStream_t)stream);
+    });
+}
+
+extern "C" int64_t gnnav_clip_workspace(int32_t n_tensors) {
+    return n_tensors < 0 ? -1 : (int64_t)clip_workspace(n_tensors);
+}
+
+static void check_tensors(int32_t n_tensors, const void *const *a, const void *const *b, const int64_t *counts,
+                          gnnav_dtype dt, const float *norm, const void *ws, int64_t ws_bytes) {
+    GNNAV_CHECK(dtype_ok(dt), GNNAV_E_INVALID, "bad dtype");
+    GNNAV_CHECK(n_tensors >= 0, GNNAV_E_INVALID, "n_tensors < 0");
+    GNNAV_CHECK(n_tensors == 0 || (a && b && counts), GNNAV_E_INVALID, "NULL tensor list");
+    const uintptr_t elt = dt == GNNAV_BF16 ? 2 : 4;
+    for (int32_t k = 0; k < n_tensors; ++k) {
+        GNNAV_CHECK(counts[k] >= 0, GNNAV_E_INVALID, "negative count");
+        GNNAV_CHECK(counts[k] == 0 || (a[k] && b[k]), GNNAV_E_INVALID, "NULL tensor");
+        GNNAV_CHECK((uintptr_t)a[k] % elt == 0 && (uintptr_t)b[k] % elt == 0, GNNAV_E_INVALID, "misaligned tensor");
+    }
+    GNNAV_CHECK(norm, GNNAV_E_INVALID, "NULL norm");
+    check_workspace(ws, ws_bytes, clip_workspace(n_tensors));
+}
+
+extern "C" gnnav_status gnnav_grad_norm(int32_t n_tensors, const void *const *grads, const int64_t *counts,
+                                        gnnav_dtype dt, float *norm_dev, void *workspace_dev, int64_t workspace_bytes,
+                                        void *stream) {
+    return guarded([&] {
+        check_tensors(n_tensors, grads, grads, counts, dt, norm_dev, workspace_dev, workspace_bytes);
+        launch_clip(n_tensors, grads, counts, dt == GNNAV_BF16, 0.0, nullptr, false, 0.f, norm_dev, workspace_dev,
+                    (hipStream_t)stream);
+    });
+}
+
+extern "C" gnnav_status gnnav_clip_grads(int32_t n_tensors, const void *const *grads, const int64_t *counts,
+                                         gnnav_dtype dt, float max_norm, void *const *out, float *norm_dev,
+                                         void *workspace_dev, int64_t workspace_bytes, void *stream) {
+    return guarded([&] {
+        GNNAV_CHECK(max_norm >= 0.f, GNNAV_E_INVALID, "max_norm is negative or NaN");
+        check_tensors(n_tensors, grads, out, counts, dt, norm_dev, workspace_dev, workspace_bytes);
+        launch_clip(n_tensors, grads, counts, dt == GNNAV_BF16, max_norm, out, false, 0.f, norm_dev, workspace_dev,
+                    (hipStream_t)stream);
+    });
+}
+
+extern "C" gnnav_status gnnav_sgd_clip_step(int32_t n_tensors, void *const *weights, const void *const *grads,
+                                            const int64_t *counts, gnnav_dtype dt, float lr, float max_norm,
+                                            float *norm_dev, void *workspace_dev, int64_t workspace_bytes,
+                                            void *stream) {
+    return guarded([&] {
+        GNNAV_CHECK(std::isfinite(lr), GNNAV_E_INVALID, "lr is not finite");
+        GNNAV_CHECK(max_norm >= 0.f, GNNAV_E_INVALID, "max_norm is negative or NaN");
+        check_tensors(n_tensors, grads, weights, counts, dt, norm_dev, workspace_dev, workspace_bytes);
+        launch_clip(n_tensors, grads, counts, dt == GNNAV_BF16, max_norm, weights, true, lr, norm_dev, workspace_dev,
+                    (hipStream_t)stream);
+    });
+}

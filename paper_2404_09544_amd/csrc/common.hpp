@@ -340,4 +340,38 @@ void launch_combine(const void *self, int64_t ld_self, const void *agg, int64_t 
                     bool out_bf16, void *out, int64_t ld_out, hipStream_t s,
                     const char *label = "combine_gemm", bool six_products = false);
 
+// embedding.hip: lookup in a trained table, and its gradient.  n_dev: device
+// count (nullable; at most n).  Ids outside [0, n_rows): a zero row, no gradient.
+void launch_embedding(const void *table, int64_t n_rows, int64_t ld_bytes, int64_t d, bool bf16, const int32_t *ids,
+                      const int32_t *n_dev, int64_t n, float scale, void *out, int64_t out_ld_bytes, hipStream_t s);
+size_t embedding_backward_workspace(int64_t n, int64_t n_rows, int64_t d, bool bf16);
+void launch_embedding_backward(const void *dout, int64_t ld_bytes, const int32_t *ids, const int32_t *n_dev,
+                               int64_t n, int64_t d, bool bf16, float scale, bool accumulate, void *dtable,
+                               int64_t n_rows, int64_t table_ld_bytes, void *ws, hipStream_t s);
+
+// linear_xent.hip: softmax cross entropy over many classes without the logits
+struct LinearXentArgs {
+    const void *h;
+    int64_t ld_h, m;
+    const void *w;
+    int64_t ld_w, n_classes, d;
+    bool bf16;
+    const int32_t *labels;
+    int32_t ignore;
+    float *loss, *row_loss;   // row_loss nullable
+    void *dh;                 // nullable
+    int64_t ld_dh;
+    void *dw;                 // nullable
+    int64_t ld_dw;
+    void *workspace;
+};
+size_t linear_xent_workspace(int64_t m, int64_t n_classes, int64_t d, bool bf16, bool grads);
+void launch_linear_xent(const LinearXentArgs &x, hipStream_t s);
+
+// clip.hip: out nullptr: the norm alone; step: out holds weights, which take
+// -lr * c * g; otherwise out = c * g
+size_t clip_workspace(int64_t n_tensors);
+void launch_clip(int32_t n_tensors, const void *const *grads, const int64_t *counts, bool bf16, double max_norm,
+                 void *const *out, bool step, float lr, float *norm, void *ws, hipStream_t s);
+
 }  // namespace gnnav

@@ -1,0 +1,737 @@
+// Lookup in a trained table and its gradient.
+//
+//   lookup     out[i] = scale * table[ids[i]]: one lane group per row, 16-byte
+//              units, several rows in flight
+//   gradient   dtable[v] = scale * sum of dout[i] over the i with ids[i] = v, in
+//              fp32.  The (id, position) pairs are sorted by id with a stable
+//              radix sort, so equal ids lie side by side in order of position;
+//              the sorted list is cut into stretches of equal length, each
+//              summed by one lane group, and an id's part sums of several
+//              stretches are joined in order afterwards.  Every lane group
+//              reads the same number of rows however popular an id is, and
+//              there are no floating-point atomics, so the bits are the same
+//              on every run.  Rows of ids that do not occur are filled with
+//              zeros by the same launch.  A few ids need no sort: each
+//              position looks for its id among the others itself.
+#include <algorithm>
+
+#include "common.hpp"
+
+namespace gnnav {
+
+namespace {
+
+typedef float f32x4e __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4e __attribute__((ext_vector_type(4)));
+
+// A 16-byte unit of a row as fp32 values: 4 of fp32, 8 of bf16.
+template <bool BF>
+struct Unit {
+    static constexpr int N = BF ? 8 : 4;
+    float v[N];
+    __device__ __forceinline__ void zero() {
+#pragma unroll
+        for (int e = 0; e < N; ++e) v[e] = 0.f;
+    }
+    __device__ __forceinline__ void from(u32x4e u) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            if constexpr (BF) {
+                v[2 * q] = __uint_as_float(u[q] << 16);
+                v[2 * q + 1] = __uint_as_float(u[q] & 0xffff0000u);
+            } else {
+                v[q] = __uint_as_float(u[q]);
+            }
+        }
+    }
+    __device__ __forceinline__ void add(u32x4e u) {
+        Unit x;
+        x.from(u);
+#pragma unroll
+        for (int e = 0; e < N; ++e) v[e] += x.v[e];
+    }
+    // rounded once to the row's type; zeros from column d on (first: the unit's first column)
+    __device__ __forceinline__ u32x4e to(int64_t first, int64_t d) const {
+        u32x4e u;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            if constexpr (BF) {
+                const uint32_t lo = first + 2 * q < d ? bf16_rne(v[2 * q]) : 0u;
+                const uint32_t hi = first + 2 * q + 1 < d ? bf16_rne(v[2 * q + 1]) : 0u;
+                u[q] = lo | (hi << 16);
+            } else {
+                u[q] = first + q < d ? __float_as_uint(v[q]) : 0u;
+            }
+        }
+        return u;
+    }
+};
+
+int lane_group(int64_t units) {   // lanes per row: the power of two that covers it, at most a wavefront
+    int g = 1;
+    while (g < units && g < kWave) g <<= 1;
+    return g;
+}
+
+}  // namespace
+
+// ---------------------------------------------------------------- lookup
+// G lanes per row, R rows of a lane group in flight, each with the first Q
+// units of a lane loaded before any is stored; longer rows loop over slabs.
+template <int G, int R, bool BF>
+__global__ void __launch_bounds__(256) k_embedding(const u32x4e *__restrict__ table, int64_t n_rows, int64_t ld16,
+                                                   int32_t units, int64_t d, const int32_t *__restrict__ ids,
+                                                   const int32_t *__restrict__ n_dev, int64_t n, float scale,
+                                                   u32x4e *__restrict__ out, int64_t out_ld16) {
+    constexpr int RPW = kWave / G;
+    const int lane = lane_id(), sub = lane / G, c0 = lane % G;
+    if (n_dev) n = std::min<int64_t>(n, std::max<int32_t>(*n_dev, 0));
+    const int64_t groups = ((int64_t)gridDim.x * blockDim.x) / kWave * RPW;
+    const int64_t first = (((int64_t)blockIdx.x * blockDim.x + threadIdx.x) / kWave) * RPW + sub;
+    for (int64_t i0 = first; i0 < n; i0 += R * groups) {
+        int32_t id[R];
+#pragma unroll
+        for (int r = 0; r < R; ++r) id[r] = i0 + r * groups < n ? ids[i0 + r * groups] : -1;
+        for (int32_t c = c0; c < units; c += G) {
+            u32x4e x[R];
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                x[r] = u32x4e{0, 0, 0, 0};
+                if (id[r] >= 0 && id[r] < n_rows) x[r] = table[(int64_t)id[r] * ld16 + c];
+            }
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                if (i0 + r * groups >= n) continue;
+                Unit<BF> v;
+                v.from(x[r]);
+#pragma unroll
+                for (int e = 0; e < Unit<BF>::N; ++e) v.v[e] *= scale;
+                if (id[r] < 0 || id[r] >= n_rows) v.zero();
+                out[(i0 + r * groups) * out_ld16 + c] = v.to((int64_t)c * Unit<BF>::N, d);
+            }
+        }
+    }
+}
+
+void launch_embedding(const void *table, int64_t n_rows, int64_t ld_bytes, int64_t d, bool bf16, const int32_t *ids,
+                      const int32_t *n_dev, int64_t n, float scale, void *out, int64_t out_ld_bytes, hipStream_t s) {
+    if (n <= 0) return;
+    const int32_t units = (int32_t)((d * (bf16 ? 2 : 4) + 15) / 16);
+    const int g = lane_group(units);
+    KernelTimer t("embedding", s);
+    const unsigned grid = grid_for(n, 256 / g * 4, 4096);
+#define GNNAV_L(GV)                                                                                                 \
+    case GV:                                                                                                        \
+        if (bf16)                                                                                                   \
+            hipLaunchKernelGGL((k_embedding<GV, 4, true>), dim3(grid), dim3(256), 0, s, (const u32x4e *)table,      \
+                               n_rows, ld_bytes / 16, units, d, ids, n_dev, n, scale, (u32x4e *)out,                \
+                               out_ld_bytes / 16);                                                                  \
+        else                                                                                                        \
+            hipLaunchKernelGGL((k_embedding<GV, 4, false>), dim3(grid), dim3(256), 0, s, (const u32x4e *)table,     \
+                               n_rows, ld_bytes / 16, units, d, ids, n_dev, n, scale, (u32x4e *)out,                \
+                               out_ld_bytes / 16);                                                                  \
+        break
+    switch (g) {
+        GNNAV_L(1);
+        GNNAV_L(2);
+        GNNAV_L(4);
+        GNNAV_L(8);
+        GNNAV_L(16);
+        GNNAV_L(32);
+        GNNAV_L(64);
+        default: fail(GNNAV_E_INVALID, "bad row width");
+    }
+#undef GNNAV_L
+    GNNAV_HIP(hipGetLastError());
+}
+
+// ------------------------------------------------- gradient: few positions
+// One workgroup per position: it lists the positions of its id, in order, and
+// leaves if one of them lies before it; otherwise its lane groups add up the
+// rows in turn and their sums are joined in a fixed order.  Workgroups past the
+// positions fill the rows of ids that do not occur (one stretch of rows each,
+// the ids that occur in it marked in LDS).
+constexpr int64_t kFewIds = 4096;
+constexpr int kZeroRows = 64;      // rows of the table per zero-filling workgroup at least
+constexpr int kMarkWords = 1024;   // marks of at most 32,768 rows
+
+template <int G, bool BF>
+__global__ void __launch_bounds__(256) k_embedding_grad_few(const u32x4e *__restrict__ dout, int64_t ld16,
+                                                            int32_t units, int64_t d, const int32_t *__restrict__ ids,
+                                                            const int32_t *__restrict__ n_dev, int32_t n, float scale,
+                                                            bool accumulate, u32x4e *__restrict__ dtable,
+                                                            int64_t n_rows, int64_t table_ld16, int32_t positions,
+                                                            int32_t zero_rows) {
+    constexpr int RPW = kWave / G, PAR = 4 * RPW, N = Unit<BF>::N;
+    __shared__ union {
+        struct {
+            int32_t list[kFewIds];
+            int32_t counts[4];
+        } p;
+        uint32_t marks[kMarkWords];
+    } sh;
+    __shared__ float part[4][kWave][N];
+    const int tid = threadIdx.x, lane = lane_id(), wid = tid / kWave;
+    if (n_dev) n = std::min(n, std::max(*n_dev, 0));
+    if ((int32_t)blockIdx.x >= positions) {
+        const int64_t lo = (int64_t)(blockIdx.x - positions) * zero_rows;
+        const int64_t hi = std::min<int64_t>(lo + zero_rows, n_rows);
+        for (int32_t w = tid; w < (zero_rows + 31) / 32; w += 256) sh.marks[w] = 0;
+        __syncthreads();
+        for (int32_t i = tid; i < n; i += 256) {
+            const int64_t v = ids[i];
+            if (v >= lo && v < hi) atomicOr(&sh.marks[(v - lo) >> 5], 1u << ((v - lo) & 31));
+        }
+        __syncthreads();
+        for (int64_t r = lo + wid * RPW + lane / G; r < hi; r += 4 * RPW) {
+            if ((sh.marks[(r - lo) >> 5] >> ((r - lo) & 31)) & 1) continue;
+            for (int32_t c = lane % G; c < units; c += G) dtable[r * table_ld16 + c] = u32x4e{0, 0, 0, 0};
+        }
+        return;
+    }
+    const int32_t p = blockIdx.x;
+    if (p >= n) return;
+    const int32_t id = ids[p];
+    if (id < 0 || id >= n_rows) return;
+    // positions of the id: each wavefront scans a quarter of the list, twice
+    const int32_t quarter = ((n + 3) / 4 + kWave - 1) / kWave * kWave;
+    const int32_t b = std::min(wid * quarter, n), e = std::min(b + quarter, n);
+    int32_t mine = 0;
+    bool earlier = false;
+    for (int32_t i = b; i < e; i += kWave) {
+        const bool hit = i + lane < e && ids[i + lane] == id;
+        earlier = earlier || (hit && i + lane < p);
+        mine += __popcll(__ballot(hit));
+    }
+    if (lane == 0) sh.p.counts[wid] = mine;
+    if (__syncthreads_or(earlier)) return;
+    int32_t at = 0, total = 0;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+        at += w < wid ? sh.p.counts[w] : 0;
+        total += sh.p.counts[w];
+    }
+    for (int32_t i = b; i < e && mine > 0; i += kWave) {
+        const bool hit = i + lane < e && ids[i + lane] == id;
+        const uint64_t m = __ballot(hit);
+        if (hit) sh.p.list[at + __popcll(m & ((1ull << lane) - 1ull))] = i + lane;
+        at += __popcll(m);
+    }
+    __syncthreads();
+    const int sub = wid * RPW + lane / G;
+    for (int32_t slab = 0; slab < units; slab += G) {
+        const int32_t c = slab + lane % G;
+        Unit<BF> acc;
+        acc.zero();
+        if (c < units) {
+            int32_t k = sub;
+            for (; k + 3 * PAR < total; k += 4 * PAR) {
+                u32x4e x[4];
+#pragma unroll
+                for (int q = 0; q < 4; ++q) x[q] = dout[(int64_t)sh.p.list[k + q * PAR] * ld16 + c];
+#pragma unroll
+                for (int q = 0; q < 4; ++q) acc.add(x[q]);
+            }
+            for (; k < total; k += PAR) acc.add(dout[(int64_t)sh.p.list[k] * ld16 + c]);
+        }
+#pragma unroll
+        for (int o = G; o < kWave; o <<= 1)
+#pragma unroll
+            for (int q = 0; q < N; ++q) acc.v[q] += __shfl_xor(acc.v[q], o, kWave);
+        __syncthreads();
+#pragma unroll
+        for (int q = 0; q < N; ++q) part[wid][lane][q] = acc.v[q];
+        __syncthreads();
+        if (wid == 0 && lane < G && c < units) {
+            Unit<BF> old;
+            u32x4e *to = dtable + (int64_t)id * table_ld16 + c;
+            old.zero();
+            if (accumulate) old.from(*to);
+#pragma unroll
+            for (int q = 0; q < N; ++q)
+                acc.v[q] = old.v[q] + scale * ((part[0][lane][q] + part[1][lane][q]) + (part[2][lane][q] + part[3][lane][q]));
+            *to = acc.to((int64_t)c * N, d);
+        }
+    }
+}
+
+// ------------------------------------------------------- gradient: the sort
+// Stable radix sort of (id, position), digits of at most 10 bits, least
+// significant first.  A tile is kSortThreads * iters pairs; there are at most
+// kSortTiles tiles, so every scatter workgroup adds up all tiles' digit counts by
+// itself and a pass is one launch: it also counts the next pass's digits by
+// output tile.  Ids outside [0, n_rows) become n_rows and sort to the end.
+namespace {
+
+constexpr int kIdThreads = 1024;
+constexpr int kIdWaves = kIdThreads / kWave;
+constexpr int64_t kIdTiles = 256;
+constexpr int kMaxBits = 10;
+
+struct IdSortPlan {
+    int passes, bits, iters;
+    int64_t tiles;
+    IdSortPlan(int64_t n, int64_t n_rows) {
+        int all = 1;
+        while (all < 32 && (int64_t(1) << all) <= n_rows) ++all;   // values 0 .. n_rows
+        passes = (all + kMaxBits - 1) / kMaxBits;
+        bits = (all + passes - 1) / passes;
+        // four rounds of 1,024 pairs a tile (a round is a few barriers), more only past 256 tiles
+        iters = 4;
+        while ((n + (int64_t)kIdThreads * iters - 1) / ((int64_t)kIdThreads * iters) > kIdTiles) iters *= 2;
+        tiles = std::max<int64_t>(1, (n + (int64_t)kIdThreads * iters - 1) / ((int64_t)kIdThreads * iters));
+    }
+    int64_t digits() const { return int64_t(1) << bits; }
+};
+
+__device__ __forceinline__ uint32_t sort_key(int32_t id, int64_t n_rows) {
+    return id < 0 || id >= n_rows ? (uint32_t)n_rows : (uint32_t)id;
+}
+
+}  // namespace
+
+__global__ void __launch_bounds__(kIdThreads) k_id_first(const int32_t *__restrict__ ids,
+                                                         const int32_t *__restrict__ n_dev, int64_t n, int64_t n_rows,
+                                                         int bits, int iters, int32_t *__restrict__ hist,
+                                                         int64_t tiles, int64_t zeros, uint32_t *__restrict__ flags,
+                                                         int64_t flag_words) {
+    __shared__ int32_t h[1 << kMaxBits];
+    if (n_dev) n = std::min<int64_t>(n, std::max<int32_t>(*n_dev, 0));
+    const int64_t digits = int64_t(1) << bits;
+    if (blockIdx.x < tiles) {
+        h[threadIdx.x] = 0;
+        __syncthreads();
+        for (int it = 0; it < iters; ++it) {
+            const int64_t e = ((int64_t)blockIdx.x * iters + it) * kIdThreads + threadIdx.x;
+            if (e < n) atomicAdd(&h[sort_key(ids[e], n_rows) & (digits - 1)], 1);
+        }
+        __syncthreads();
+        if (threadIdx.x < digits) hist[blockIdx.x * digits + threadIdx.x] = h[threadIdx.x];
+        return;
+    }
+    const int64_t stride = (int64_t)(gridDim.x - tiles) * kIdThreads;
+    const int64_t first = (int64_t)(blockIdx.x - tiles) * kIdThreads + threadIdx.x;
+    for (int64_t i = first; i < zeros; i += stride) hist[tiles * digits + i] = 0;
+    for (int64_t i = first; i < flag_words; i += stride) flags[i] = 0;
+}
+
+// flags (first pass only, nullable): a byte per row of the table, set where its id occurs.
+template <bool FIRST>
+__global__ void __launch_bounds__(kIdThreads) k_id_scatter(const int32_t *__restrict__ keys_in,
+                                                           const int32_t *__restrict__ vals_in,
+                                                           const int32_t *__restrict__ n_dev, int64_t n,
+                                                           int64_t n_rows, int shift, int bits, int iters,
+                                                           const int32_t *__restrict__ hist, int64_t tiles,
+                                                           int32_t *__restrict__ keys_out,
+                                                           int32_t *__restrict__ vals_out,
+                                                           int32_t *__restrict__ hist_next,
+                                                           uint8_t *__restrict__ flags) {
+    __shared__ int32_t run[1 << kMaxBits];
+    __shared__ int32_t cnt[kIdWaves][1 << kMaxBits];
+    __shared__ int32_t scratch[kIdWaves];
+    if (n_dev) n = std::min<int64_t>(n, std::max<int32_t>(*n_dev, 0));
+    const int tile_bits = 31 - __builtin_clz(kIdThreads * iters);   // iters is a power of two
+    const int64_t base = (int64_t)blockIdx.x << tile_bits;
+    if (base >= n) return;
+    const int lane = lane_id(), wid = threadIdx.x / kWave, digits = 1 << bits;
+    int32_t all = 0, before = 0;
+    if ((int)threadIdx.x < digits) {
+#pragma unroll 8
+        for (int t = 0; t < (int)tiles; ++t) {
+            const int32_t c = hist[t * digits + threadIdx.x];
+            all += c;
+            before += t < (int)blockIdx.x ? c : 0;
+        }
+#pragma unroll
+        for (int w = 0; w < kIdWaves; ++w) cnt[w][threadIdx.x] = 0;
+    }
+    int32_t total;
+    const int32_t off = block_exclusive_sum<int32_t, kIdThreads>(all, scratch, total) + before;
+    if ((int)threadIdx.x < digits) run[threadIdx.x] = off;
+    __syncthreads();
+    const uint64_t below = (1ull << lane) - 1ull;
+    for (int it = 0; it < iters; ++it) {
+        const int64_t e = base + (int64_t)it * kIdThreads + threadIdx.x;
+        if (base + (int64_t)it * kIdThreads >= n) break;
+        const bool valid = e < n;
+        uint32_t key = 0;
+        int32_t val = 0;
+        if (valid) {
+            if constexpr (FIRST) {
+                key = sort_key(keys_in[e], n_rows);
+                val = (int32_t)e;
+                if (flags && key < (uint32_t)n_rows) flags[key] = 1;
+            } else {
+                key = (uint32_t)keys_in[e];
+                val = vals_in[e];
+            }
+        }
+        const int dg = (int)(key >> shift) & (digits - 1);
+        uint64_t m = __ballot(valid);
+        for (int bit = 0; bit < bits; ++bit) {
+            const uint64_t ones = __ballot((dg >> bit) & 1);
+            m &= ((dg >> bit) & 1) ? ones : ~ones;
+        }
+        const int rank = __popcll(m & below);
+        if (valid && rank == 0) cnt[wid][dg] = __popcll(m);
+        __syncthreads();
+        if ((int)threadIdx.x < digits) {   // exclusive sums over the wavefronts, from the digit's place
+            int32_t at = run[threadIdx.x];
+#pragma unroll
+            for (int w = 0; w < kIdWaves; ++w) {
+                const int32_t c = cnt[w][threadIdx.x];
+                cnt[w][threadIdx.x] = at;
+                at += c;
+            }
+            run[threadIdx.x] = at;
+        }
+        __syncthreads();
+        if (valid) {
+            const int32_t pos = cnt[wid][dg] + rank;
+            keys_out[pos] = (int32_t)key;
+            vals_out[pos] = val;
+            if (hist_next) {   // one addition for the lanes that share an output tile and a next digit
+                const int next = (int)(key >> (shift + bits)) & (digits - 1);
+                const int32_t slot = (pos >> tile_bits) * digits + next;
+                // lanes of one digit go to consecutive places: at most two tiles, many next digits
+                atomicAdd(&hist_next[slot], 1);
+            }
+        }
+        __syncthreads();
+        if ((int)threadIdx.x < digits)
+#pragma unroll
+            for (int w = 0; w < kIdWaves; ++w) cnt[w][threadIdx.x] = 0;
+        __syncthreads();
+    }
+}
+
+// ------------------------------------------------ gradient: stretches of ids
+// A lane group takes kStretch sorted pairs and adds up the rows of equal ids.
+// An id that lies inside the stretch is written at once; the part of one that
+// began earlier goes to part[2 * stretch], of one that begins here and goes on to
+// part[2 * stretch + 1].  Workgroups past the stretches fill the rows of ids that
+// do not occur.  Q units of a row per lane, wider rows in slabs (blockIdx.y).
+constexpr int kStretch = 64;
+
+template <int G, int Q, bool BF>
+__global__ void __launch_bounds__(256) k_embedding_grad(const u32x4e *__restrict__ dout, int64_t ld16, int32_t units,
+                                                        int64_t d, const int32_t *__restrict__ keys,
+                                                        const int32_t *__restrict__ vals,
+                                                        const int32_t *__restrict__ n_dev, int64_t n, float scale,
+                                                        bool accumulate, u32x4e *__restrict__ dtable, int64_t n_rows,
+                                                        int64_t table_ld16, float *__restrict__ part,
+                                                        const uint8_t *__restrict__ flags, int64_t blocks) {
+    constexpr int RPW = kWave / G, N = Unit<BF>::N;
+    const int lane = lane_id(), sub = lane / G, cl = lane % G;
+    if (n_dev) n = std::min<int64_t>(n, std::max<int32_t>(*n_dev, 0));
+    const int32_t c0 = (int32_t)blockIdx.y * (G * Q) + cl;
+    if ((int64_t)blockIdx.x >= blocks) {
+        const int64_t waves = (int64_t)(gridDim.x - blocks) * 4;
+        const int64_t w0 = (int64_t)(blockIdx.x - blocks) * 4 + threadIdx.x / kWave;
+        for (int64_t r0 = w0 * kWave; r0 < n_rows; r0 += waves * kWave) {
+            const bool mine = r0 + lane < n_rows && flags[r0 + lane] == 0;
+            uint64_t m = __ballot(mine);
+            while (m) {   // RPW rows at a time
+                uint64_t left = m;
+                int row = -1;
+#pragma unroll
+                for (int k = 0; k < RPW; ++k) {
+                    const int at = left ? __builtin_ctzll(left) : -1;
+                    if (k == sub) row = at;
+                    left = left ? left & (left - 1) : 0;
+                }
+                m = left;
+                if (row >= 0)
+#pragma unroll
+                    for (int q = 0; q < Q; ++q)
+                        if (c0 + q * G < units) dtable[(r0 + row) * table_ld16 + c0 + q * G] = u32x4e{0, 0, 0, 0};
+            }
+        }
+        return;
+    }
+    const int64_t st = ((int64_t)blockIdx.x * 4 + threadIdx.x / kWave) * RPW + sub;
+    const int64_t b = st * kStretch, e = std::min<int64_t>(b + kStretch, n);
+    const int64_t padded = (int64_t)units * N;
+    const int32_t before = b > 0 && b < n ? keys[b - 1] : -1, after = e < n && b < n ? keys[e] : -1;
+    Unit<BF> acc[Q];
+#pragma unroll
+    for (int q = 0; q < Q; ++q) acc[q].zero();
+    auto flush = [&](int32_t id, bool began, bool ended) {
+        if (id >= n_rows) return;
+        if (began && ended) {
+#pragma unroll
+            for (int q = 0; q < Q; ++q) {
+                const int32_t c = c0 + q * G;
+                if (c >= units) continue;
+                u32x4e *to = dtable + (int64_t)id * table_ld16 + c;
+                Unit<BF> o;
+                o.zero();
+                if (accumulate) o.from(*to);
+#pragma unroll
+                for (int x = 0; x < N; ++x) o.v[x] += scale * acc[q].v[x];
+                *to = o.to((int64_t)c * N, d);
+            }
+        } else {
+            float *to = part + (2 * st + (began ? 1 : 0)) * padded;
+#pragma unroll
+            for (int q = 0; q < Q; ++q) {
+                const int32_t c = c0 + q * G;
+                if (c >= units) continue;
+#pragma unroll
+                for (int x = 0; x < N; x += 4)
+                    *(f32x4e *)(to + (int64_t)c * N + x) = f32x4e{acc[q].v[x], acc[q].v[x + 1], acc[q].v[x + 2], acc[q].v[x + 3]};
+            }
+        }
+    };
+    constexpr int U = 4;
+    int32_t cur = b < n ? keys[b] : -1;
+    bool began = b < n && cur != before;
+    // the loop's trip count is the same for all lane groups of a wavefront
+    for (int i0 = 0; i0 < kStretch; i0 += U) {
+        int32_t key[U];
+        u32x4e x[U][Q];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int64_t p = b + i0 + u;
+            key[u] = p < e ? keys[p] : -1;
+            const int64_t row = p < e ? vals[p] : 0;
+#pragma unroll
+            for (int q = 0; q < Q; ++q) {
+                x[u][q] = u32x4e{0, 0, 0, 0};
+                if (p < e && key[u] < n_rows && c0 + q * G < units) x[u][q] = dout[row * ld16 + c0 + q * G];
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (key[u] < 0) continue;
+            if (key[u] != cur) {
+                flush(cur, began, true);
+                cur = key[u];
+                began = true;
+#pragma unroll
+                for (int q = 0; q < Q; ++q) acc[q].zero();
+            }
+#pragma unroll
+            for (int q = 0; q < Q; ++q) acc[q].add(x[u][q]);
+        }
+    }
+    if (b < n) flush(cur, began, cur != after);
+}
+
+// Joins the parts of ids that span stretches: the workgroup of the stretch where
+// such an id begins adds that part and those of the stretches up to its last one,
+// in order, a quarter of them per wavefront.
+template <bool BF>
+__global__ void __launch_bounds__(256) k_embedding_grad_join(const int32_t *__restrict__ keys,
+                                                             const int32_t *__restrict__ n_dev, int64_t n,
+                                                             int32_t units, int64_t d, float scale, bool accumulate,
+                                                             u32x4e *__restrict__ dtable, int64_t n_rows,
+                                                             int64_t table_ld16, const float *__restrict__ part) {
+    constexpr int N = Unit<BF>::N;
+    __shared__ float sums[4][kWave][N];
+    if (n_dev) n = std::min<int64_t>(n, std::max<int32_t>(*n_dev, 0));
+    const int lane = lane_id(), wid = threadIdx.x / kWave;
+    const int64_t padded = (int64_t)units * N;
+    for (int64_t st = blockIdx.x; (st + 1) * kStretch < n; st += gridDim.x) {
+        const int64_t b = st * kStretch, e = b + kStretch;
+        const int32_t id = keys[e - 1];
+        if (id >= n_rows || keys[e] != id) continue;                  // ends here
+        if (keys[b] == id && b > 0 && keys[b - 1] == id) continue;    // began earlier
+        int64_t lo = e, hi = n;                                       // first pair past the id
+        while (lo < hi) {
+            const int64_t mid = (lo + hi) >> 1;
+            if (keys[mid] <= id) lo = mid + 1;
+            else hi = mid;
+        }
+        const int64_t rest = (lo - 1) / kStretch - st;                // stretches after this one
+        const int64_t quarter = (rest + 3) / 4;
+        const int64_t k0 = std::min(wid * quarter, rest), k1 = std::min(k0 + quarter, rest);
+        for (int32_t slab = 0; slab < units; slab += kWave) {
+            const int32_t c = slab + lane;
+            float acc[N];
+#pragma unroll
+            for (int x = 0; x < N; ++x) acc[x] = 0.f;
+            if (c < units) {
+                const float *at = part + (int64_t)c * N;
+                if (wid == 0) {
+#pragma unroll
+                    for (int x = 0; x < N; ++x) acc[x] = at[(2 * st + 1) * padded + x];
+                }
+                int64_t k = k0;
+                for (; k + 8 <= k1; k += 8) {
+                    f32x4e v[8][N / 4];
+#pragma unroll
+                    for (int u = 0; u < 8; ++u)
+#pragma unroll
+                        for (int x = 0; x < N / 4; ++x) v[u][x] = *(const f32x4e *)(at + 2 * (st + 1 + k + u) * padded + 4 * x);
+#pragma unroll
+                    for (int u = 0; u < 8; ++u)
+#pragma unroll
+                        for (int x = 0; x < N; ++x) acc[x] += v[u][x / 4][x % 4];
+                }
+                for (; k < k1; ++k)
+#pragma unroll
+                    for (int x = 0; x < N; ++x) acc[x] += at[2 * (st + 1 + k) * padded + x];
+            }
+            __syncthreads();
+#pragma unroll
+            for (int x = 0; x < N; ++x) sums[wid][lane][x] = acc[x];
+            __syncthreads();
+            if (wid == 0 && c < units) {
+                u32x4e *to = dtable + (int64_t)id * table_ld16 + c;
+                Unit<BF> o;
+                o.zero();
+                if (accumulate) o.from(*to);
+#pragma unroll
+                for (int x = 0; x < N; ++x)
+                    o.v[x] += scale * ((sums[0][lane][x] + sums[1][lane][x]) + (sums[2][lane][x] + sums[3][lane][x]));
+                *to = o.to((int64_t)c * N, d);
+            }
+        }
+    }
+}
+
+namespace {
+// Workspace of the gradient: two (id, position) lists, the digit counts of every
+// pass, a byte per table row, the part sums.
+struct GradWorkspace {
+    size_t keys[2], vals[2], hist, flags, part, total;
+    GradWorkspace(int64_t n, int64_t n_rows, int64_t d, bool bf16) {
+        const IdSortPlan p(n, n_rows);
+        const int64_t units = (d * (bf16 ? 2 : 4) + 15) / 16, padded = units * (bf16 ? 8 : 4);
+        size_t at = 0;
+        auto take = [&](size_t bytes) {
+            const size_t here = at;
+            at += (bytes + 255) / 256 * 256;
+            return here;
+        };
+        for (int k = 0; k < 2; ++k) {
+            keys[k] = take((size_t)n * 4);
+            vals[k] = take((size_t)n * 4);
+        }
+        hist = take((size_t)(p.passes * p.tiles * p.digits()) * 4);
+        flags = take((size_t)n_rows);
+        part = take((size_t)(2 * ((n + kStretch - 1) / kStretch) * padded) * 4);
+        total = at;
+    }
+};
+}  // namespace
+
+size_t embedding_backward_workspace(int64_t n, int64_t n_rows, int64_t d, bool bf16) {
+    return n <= kFewIds ? 0 : GradWorkspace(n, n_rows, d, bf16).total;
+}
+
+void launch_embedding_backward(const void *dout, int64_t ld_bytes, const int32_t *ids, const int32_t *n_dev,
+                               int64_t n, int64_t d, bool bf16, float scale, bool accumulate, void *dtable,
+                               int64_t n_rows, int64_t table_ld_bytes, void *ws, hipStream_t s) {
+    if (n_rows <= 0 || (n <= 0 && accumulate)) return;
+    const int32_t units = (int32_t)((d * (bf16 ? 2 : 4) + 15) / 16);
+    const int g = lane_group(units);
+    const u32x4e *in = (const u32x4e *)dout;
+    u32x4e *out = (u32x4e *)dtable;
+    const int64_t ld16 = ld_bytes / 16, tld16 = table_ld_bytes / 16;
+    if (n <= kFewIds) {
+        KernelTimer t("embedding_grad_few", s);
+        int64_t zero_rows = (n_rows + 511) / 512;   // two workgroups per compute unit fill zeros
+        zero_rows = std::max<int64_t>(kZeroRows, std::min<int64_t>(zero_rows, kMarkWords * 32));
+        const int64_t zeros = accumulate ? 0 : (n_rows + zero_rows - 1) / zero_rows;
+#define GNNAV_L(GV)                                                                                                   \
+    case GV:                                                                                                          \
+        if (bf16)                                                                                                     \
+            hipLaunchKernelGGL((k_embedding_grad_few<GV, true>), dim3((unsigned)(n + zeros)), dim3(256), 0, s, in,    \
+                               ld16, units, d, ids, n_dev, (int32_t)n, scale, accumulate, out, n_rows, tld16,         \
+                               (int32_t)n, (int32_t)zero_rows);                                                       \
+        else                                                                                                          \
+            hipLaunchKernelGGL((k_embedding_grad_few<GV, false>), dim3((unsigned)(n + zeros)), dim3(256), 0, s, in,   \
+                               ld16, units, d, ids, n_dev, (int32_t)n, scale, accumulate, out, n_rows, tld16,         \
+                               (int32_t)n, (int32_t)zero_rows);                                                       \
+        break
+        switch (g) {
+            GNNAV_L(1);
+            GNNAV_L(2);
+            GNNAV_L(4);
+            GNNAV_L(8);
+            GNNAV_L(16);
+            GNNAV_L(32);
+            default: GNNAV_L(64);
+        }
+#undef GNNAV_L
+        GNNAV_HIP(hipGetLastError());
+        return;
+    }
+    const GradWorkspace w(n, n_rows, d, bf16);
+    const IdSortPlan p(n, n_rows);
+    char *base = (char *)ws;
+    auto i32 = [&](size_t at) { return (int32_t *)(base + at); };
+    int32_t *hist = i32(w.hist);
+    uint8_t *flags = accumulate ? nullptr : (uint8_t *)(base + w.flags);
+    const int32_t *kin = ids, *vin = nullptr;
+    {
+        KernelTimer t("embedding_sort", s);
+        const int64_t zeros = (p.passes - 1) * p.tiles * p.digits(), words = accumulate ? 0 : (n_rows + 3) / 4;
+        hipLaunchKernelGGL(k_id_first, dim3((unsigned)p.tiles + grid_for(std::max(zeros, words), kIdThreads, 256)),
+                           dim3(kIdThreads), 0, s, ids, n_dev, n, n_rows, p.bits, p.iters, hist, p.tiles, zeros,
+                           (uint32_t *)flags, words);
+        for (int k = 0; k < p.passes; ++k) {
+            int32_t *kout = i32(w.keys[k & 1]), *vout = i32(w.vals[k & 1]);
+            const int32_t *h = hist + k * p.tiles * p.digits();
+            int32_t *next = k + 1 < p.passes ? hist + (k + 1) * p.tiles * p.digits() : nullptr;
+            if (k == 0)
+                hipLaunchKernelGGL(k_id_scatter<true>, dim3((unsigned)p.tiles), dim3(kIdThreads), 0, s, kin, vin,
+                                   n_dev, n, n_rows, 0, p.bits, p.iters, h, p.tiles, kout, vout, next, flags);
+            else
+                hipLaunchKernelGGL(k_id_scatter<false>, dim3((unsigned)p.tiles), dim3(kIdThreads), 0, s, kin, vin,
+                                   n_dev, n, n_rows, k * p.bits, p.bits, p.iters, h, p.tiles, kout, vout, next,
+                                   nullptr);
+            kin = kout;
+            vin = vout;
+        }
+    }
+    float *part = (float *)(base + w.part);
+    {
+        KernelTimer t("embedding_grad", s);
+        const int64_t stretches = (n + kStretch - 1) / kStretch;
+        const int64_t blocks = (stretches + 4 * (kWave / g) - 1) / (4 * (kWave / g));
+        const unsigned zeros = accumulate ? 0u : grid_for(n_rows, 256, 1024);
+        const unsigned slabs = (unsigned)((units + 3 * kWave - 1) / (3 * kWave));
+        const int q = (int)((units + g * slabs - 1) / (g * slabs));
+#define GNNAV_L(GV, QV)                                                                                               \
+    do {                                                                                                              \
+        if (bf16)                                                                                                     \
+            hipLaunchKernelGGL((k_embedding_grad<GV, QV, true>), dim3((unsigned)blocks + zeros, slabs), dim3(256), 0, \
+                               s, in, ld16, units, d, kin, vin, n_dev, n, scale, accumulate, out, n_rows, tld16,      \
+                               part, flags, blocks);                                                                  \
+        else                                                                                                          \
+            hipLaunchKernelGGL((k_embedding_grad<GV, QV, false>), dim3((unsigned)blocks + zeros, slabs), dim3(256),   \
+                               0, s, in, ld16, units, d, kin, vin, n_dev, n, scale, accumulate, out, n_rows, tld16,   \
+                               part, flags, blocks);                                                                  \
+    } while (0)
+        switch (g) {
+            case 1: GNNAV_L(1, 1); break;
+            case 2: GNNAV_L(2, 1); break;
+            case 4: GNNAV_L(4, 1); break;
+            case 8: GNNAV_L(8, 1); break;
+            case 16: GNNAV_L(16, 1); break;
+            case 32: GNNAV_L(32, 1); break;
+            default:
+                if (q == 1) GNNAV_L(64, 1);
+                else if (q == 2) GNNAV_L(64, 2);
+                else GNNAV_L(64, 3);
+        }
+#undef GNNAV_L
+        GNNAV_HIP(hipGetLastError());
+    }
+    {
+        KernelTimer t("embedding_grad_join", s);
+        const unsigned grid = grid_for((n + kStretch - 1) / kStretch, 1, 8192);
+        if (bf16)
+            hipLaunchKernelGGL(k_embedding_grad_join<true>, dim3(grid), dim3(256), 0, s, kin, n_dev, n, units, d,
+                               scale, accumulate, out, n_rows, tld16, part);
+        else
+            hipLaunchKernelGGL(k_embedding_grad_join<false>, dim3(grid), dim3(256), 0, s, kin, n_dev, n, units, d,
+                               scale, accumulate, out, n_rows, tld16, part);
+    }
+    GNNAV_HIP(hipGetLastError());
+}
+
+}  // namespace gnnav

@@ -1,0 +1,736 @@
+// Softmax cross entropy of rows against a large set of classes, and its
+// gradients, without the logits:
+//
+//   z_iv = h_i . w_v,  lse_i = log sum_v exp z_iv,  loss_i = lse_i - z_i,y(i)
+//   p_iv = exp(z_iv - lse_i) - [v = y(i)]
+//   dh_i = (1/N) sum_v p_iv w_v,   dw_v = (1/N) sum_i p_iv h_i
+//
+// The classes are taken in pieces.  A first pass over the pieces multiplies and
+// keeps, per row and tile of classes, the largest logit and the sum of
+// exponentials (the logits stay in registers); one launch joins them to lse.  A
+// second pass multiplies a piece again, writes its p, in the matrix cores' 16-bit
+// type, to a buffer the size of a piece, and two products take the piece's dw and
+// its part of dh from that buffer.
+//
+// Operands are packed first: chunk-major, 16-byte chunks of 8 consecutive
+// columns, the chunks of one column group side by side for all rows
+// (x[c / 8][row][c % 8]), padded with zeros to whole tiles.  This one layout
+// serves as an operand whose columns are summed over (a fragment is 8 columns of
+// a row: one chunk) and as one whose rows are (the transposing LDS reads
+// of gfx950 take 4 rows of 16 columns); copies to LDS are contiguous and need
+// no bounds.  fp32 operands are packed as three bf16 planes and multiplied with
+// the six part products of bf16split.hpp; bf16 ones as they are.
+//
+// All three products are one kernel: M (MFMA rows) is the class of the logits and
+// the feature of the gradients, N (MFMA columns) the row of h, or the class for dw.
+#include <algorithm>
+#include <cmath>
+
+#include "bf16split.hpp"
+#include "common.hpp"
+#include "dma.hpp"
+
+namespace gnnav {
+
+namespace {
+
+typedef float f32x16x __attribute__((ext_vector_type(16)));
+typedef float f32x4x __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4x __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2x __attribute__((ext_vector_type(2)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+
+constexpr int kVTile = 256;              // classes of a logit tile
+constexpr float kLog2e = 1.44269504088896340736f;
+
+// What a row does: counted rows carry their lse, the others +inf, which makes
+// every p of theirs zero.
+__device__ __forceinline__ bool row_counts(float lse) { return lse < INFINITY || lse != lse; }
+
+}  // namespace
+
+// ------------------------------------------------------------------ packing
+// rows x d (row-major, 16-byte aligned rows) -> PL planes of chunks
+// [chunk][R rows], zeros past rows and d, and in rows whose label is `ignore` or
+// outside [0, n_classes) (labels nullable).  One workgroup: 64 rows x 64 columns
+// through LDS.
+template <bool BF>
+__global__ void __launch_bounds__(256) k_xent_pack(const void *__restrict__ src, int64_t ld, int64_t rows, int64_t d,
+                                                   const int32_t *__restrict__ labels, int32_t ignore,
+                                                   int64_t n_classes, int64_t R, int64_t chunks,
+                                                   u32x4x *__restrict__ out) {
+    constexpr int PL = BF ? 1 : 3;
+    __shared__ u32x4x tile[PL][8][65];
+    const int tid = threadIdx.x;
+    const int64_t r0 = (int64_t)blockIdx.x * 64, c0 = (int64_t)blockIdx.y * 8;
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        const int lr = tid / 8 + 32 * k, lc = tid % 8;
+        const int64_t r = r0 + lr, col = (c0 + lc) * 8;
+        bool live = r < rows && col < d;
+        if (live && labels) {
+            const int32_t y = labels[r];
+            live = y != ignore && y >= 0 && y < n_classes;
+        }
+        if constexpr (BF) {
+            u32x4x x = {0, 0, 0, 0};
+            if (live) {
+                x = *(const u32x4x *)((const uint16_t *)src + r * ld + col);
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    if (col + 2 * q + 1 >= d) x[q] &= 0xffffu;
+                    if (col + 2 * q >= d) x[q] = 0;
+                }
+            }
+            tile[0][lc][lr] = x;
+        } else {
+            float x[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] = 0.f;
+            if (live) {
+                const float *p = (const float *)src + r * ld + col;
+                const f32x4x a = *(const f32x4x *)p;
+                f32x4x b = {0.f, 0.f, 0.f, 0.f};
+                if (col + 4 < d) b = *(const f32x4x *)(p + 4);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    x[e] = col + e < d ? a[e] : 0.f;
+                    x[4 + e] = col + 4 + e < d ? b[e] : 0.f;
+                }
+            }
+            bf16x8 p1, p2, p3;
+            split3(x, p1, p2, p3);
+            tile[0][lc][lr] = __builtin_bit_cast(u32x4x, p1);
+            tile[PL - 2][lc][lr] = __builtin_bit_cast(u32x4x, p2);
+            tile[PL - 1][lc][lr] = __builtin_bit_cast(u32x4x, p3);
+        }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < 2 * PL; ++k) {
+        const int lc = (tid / 64) + 4 * (k & 1), lr = tid % 64, p = k >> 1;
+        if (c0 + lc < chunks && r0 + lr < R) out[(p * chunks + c0 + lc) * R + r0 + lr] = tile[p][lc][lr];
+    }
+}
+
+// ------------------------------------------------------------------ products
+enum { kStats, kProb, kDh, kDw };
+
+struct XentArgs {
+    const u32x4x *A, *B;       // packed operands
+    int64_t a_rows, b_rows;    // rows of their chunks
+    int64_t a_plane, b_plane;  // chunks of a plane
+    int64_t k;                 // summed length, a multiple of the step
+    int32_t m_tiles, n_tiles;
+    int32_t split_steps;       // kDh: steps of one split
+    // kStats, kProb
+    int64_t v0, n_classes;     // first class of the piece, classes in all
+    int64_t rows;              // packed rows of h
+    const int32_t *labels;
+    int64_t m;                 // rows of h
+    float2 *stats;             // [tile of classes][rows]
+    float *label_logit;        // [rows]
+    const float *lse;          // [rows]
+    u32x4x *p;                 // planes [class chunk][rows]
+    int64_t p_plane;
+    // kDh
+    f32x4x *part;
+    int64_t split_stride;      // float4s of a split's parts
+    bool first;
+    // kDw
+    void *dw;
+    int64_t ld_dw, d;
+    const float *inv_count;
+    bool dw_bf16;
+};
+
+// Wave grid WGM x WGN, each wavefront WMF x WNF MFMA blocks of 32 x 32; BK summed
+// elements per stage, ST stages in LDS.  AT, BT: the operand's rows are summed over.
+template <int PL, int WMF, int WNF, int WGM, int WGN, int BK, int ST, bool AT, bool BT, int EPI>
+__global__ void __launch_bounds__(64 * WGM * WGN, 2) k_xent(const XentArgs a) {
+    constexpr int NW = WGM * WGN, BM = 32 * WMF * WGM, BN = 32 * WNF * WGN;
+    constexpr int APC = BM * BK / 8, BPC = BN * BK / 8;      // chunks of a plane of a stage
+    constexpr int STAGE = PL * (APC + BPC);
+    constexpr int INSTR = STAGE / 64, IN = (INSTR + NW - 1) / NW;
+    static_assert(APC % 64 == 0 && BPC % 64 == 0, "whole wavefront copies");
+    __shared__ u32x4x S[ST * STAGE];
+    __shared__ float2 red[EPI == kStats ? WGM * BN : 1];
+    const int tid = threadIdx.x, lane = tid & 63, wid = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wm = wid / WGN, wn = wid % WGN, h = lane >> 5, lr = lane & 31;
+    const int32_t mt = blockIdx.x % a.m_tiles, nt = blockIdx.x / a.m_tiles;
+    const int64_t m0 = (int64_t)mt * BM, n0 = (int64_t)nt * BN;
+    const int32_t all_steps = (int32_t)(a.k / BK);
+    int32_t s0 = 0, T = all_steps;
+    if constexpr (EPI == kDh) {
+        s0 = blockIdx.y * a.split_steps;
+        T = std::min(a.split_steps, all_steps - s0);
+    }
+
+    // this wavefront's copies of a stage: source of the next step, its advance
+    const char *src[IN];
+    int64_t inc[IN];
+    int dst[IN];
+#pragma unroll
+    for (int u = 0; u < IN; ++u) {
+        const int q = std::min(wid * IN + u, INSTR - 1);   // the last wavefront may repeat the last copy
+        const int slot = q * 64;
+        const bool isB = slot >= PL * APC;
+        const int rel = slot - (isB ? PL * APC : 0), pc = isB ? BPC : APC;
+        const int plane = rel / pc, s = rel % pc + lane;
+        const u32x4x *base = (isB ? a.B + plane * a.b_plane : a.A + plane * a.a_plane);
+        const int64_t R = isB ? a.b_rows : a.a_rows, x0 = isB ? n0 : m0;
+        const bool tr = isB ? BT : AT;
+        if (tr) {
+            const int mc = s / BK, kk = (s % BK) ^ ((mc & 1) * 4);
+            src[u] = (const char *)(base + (x0 / 8 + mc) * R + (int64_t)s0 * BK + kk);
+            inc[u] = (int64_t)BK * 16;
+        } else {
+            const int tile = isB ? BN : BM, c = s / tile, r = s % tile;
+            src[u] = (const char *)(base + ((int64_t)s0 * (BK / 8) + c) * R + x0 + r);
+            inc[u] = (int64_t)(BK / 8) * R * 16;
+        }
+        dst[u] = slot;
+    }
+    auto issue = [&](int stage) {
+#pragma unroll
+        for (int u = 0; u < IN; ++u) {
+            dma16(src[u], &S[stage * STAGE + dst[u]]);
+            src[u] += inc[u];
+        }
+    };
+
+    f32x16x acc[WMF][WNF];
+#pragma unroll
+    for (int i = 0; i < WMF; ++i)
+#pragma unroll
+        for (int j = 0; j < WNF; ++j)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
+
+    // lane parts of the fragments' LDS addresses
+    const int tr_mc = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1), tr_k = 8 * h + ((lane & 15) >> 2);
+    const int tr_swz = (tr_mc & 1) * 4;
+    auto frag = [&](const u32x4x *plane, auto tr_, int tile, int x, int kk) -> bf16x8 {
+        if constexpr (decltype(tr_)::value) {
+            typedef __attribute__((address_space(3))) s16x4 lds4;
+            const char *p0 = (const char *)(plane + (x / 8 + tr_mc) * BK + ((kk * 16 + tr_k) ^ tr_swz)) + 8 * (lane & 1);
+            const char *p1 = (const char *)(plane + (x / 8 + tr_mc) * BK + ((kk * 16 + tr_k + 4) ^ tr_swz)) + 8 * (lane & 1);
+            const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4 *)p0);
+            const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4 *)p1);
+            typedef short s16x8 __attribute__((ext_vector_type(8)));
+            return __builtin_bit_cast(bf16x8, s16x8{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]});
+        } else {
+            return __builtin_bit_cast(bf16x8, plane[(2 * kk + h) * tile + x + lr]);
+        }
+    };
+    auto compute = [&](int stage) {
+        const u32x4x *sa = &S[stage * STAGE], *sb = sa + PL * APC;
+#pragma unroll
+        for (int kk = 0; kk < BK / 16; ++kk) {
+            bf16x8 fa[WMF][PL], fb[WNF][PL];
+#pragma unroll
+            for (int i = 0; i < WMF; ++i)
+#pragma unroll
+                for (int p = 0; p < PL; ++p)
+                    fa[i][p] = frag(sa + p * APC, std::integral_constant<bool, AT>(), BM, wm * (32 * WMF) + 32 * i, kk);
+#pragma unroll
+            for (int j = 0; j < WNF; ++j)
+#pragma unroll
+                for (int p = 0; p < PL; ++p)
+                    fb[j][p] = frag(sb + p * BPC, std::integral_constant<bool, BT>(), BN, wn * (32 * WNF) + 32 * j, kk);
+#pragma unroll
+            for (int i = 0; i < WMF; ++i)
+#pragma unroll
+                for (int j = 0; j < WNF; ++j) {
+                    if constexpr (PL == 1)
+                        acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa[i][0], fb[j][0], acc[i][j], 0, 0, 0);
+                    else
+                        acc[i][j] = mfma_split6(fa[i][0], fa[i][PL - 2], fa[i][PL - 1], fb[j][0], fb[j][PL - 2],
+                                                fb[j][PL - 1], acc[i][j]);
+                }
+        }
+    };
+
+#pragma unroll
+    for (int s = 0; s < ST - 1; ++s)
+        if (s < T) issue(s);
+    int stage = 0;
+    for (int32_t t = 0; t < T; ++t) {
+        if (ST > 2 && t + ST - 1 <= T) wait_vm<IN *(ST - 2)>();
+        else wait_vm<0>();
+        lds_barrier();   // stage t visible, everyone done with the one before it
+        if (t + ST - 1 < T) issue(stage == 0 ? ST - 1 : stage - 1);
+        compute(stage);
+        stage = stage + 1 == ST ? 0 : stage + 1;
+    }
+
+    // block (i, j), register r of a lane: M index 32 i + 8 (r / 4) + 4 h + r % 4, N index 32 j + lane % 32
+    const int64_t mw = m0 + wm * (32 * WMF), nw = n0 + wn * (32 * WNF);
+    // a row's label among this wavefront's classes, -1 if it is none of them
+    auto label_place = [&](int64_t n) {
+        const int64_t y = (n < a.m ? a.labels[n] : -1) - (a.v0 + mw);
+        return y >= 0 && y < 32 * WMF ? (int)y : -1;
+    };
+    if constexpr (EPI == kStats) {
+        const bool tail = a.v0 + m0 + BM > a.n_classes;
+        float2 mine[WNF];
+#pragma unroll
+        for (int j = 0; j < WNF; ++j) {
+            const int64_t n = nw + 32 * j + lr;
+            const int y = label_place(n);
+            float mx = -INFINITY;
+#pragma unroll
+            for (int i = 0; i < WMF; ++i)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    const int m = 32 * i + 8 * (r / 4) + 4 * h + r % 4;
+                    if (tail && a.v0 + mw + m >= a.n_classes) acc[i][j][r] = -INFINITY;
+                    mx = fmaxf(mx, acc[i][j][r]);
+                }
+            if (y >= 0) {
+#pragma unroll
+                for (int i = 0; i < WMF; ++i)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r)
+                        if (y == 32 * i + 8 * (r / 4) + 4 * h + r % 4) a.label_logit[n] = acc[i][j][r];
+            }
+            mx = fmaxf(mx, __shfl_xor(mx, 32, kWave));
+            // a row whose classes here are all -inf has the sum 0: any finite reference does
+            const float ref = mx == -INFINITY ? 0.f : mx;
+            float s = 0.f;
+#pragma unroll
+            for (int i = 0; i < WMF; ++i)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    if constexpr (PL == 1) s += __builtin_amdgcn_exp2f((acc[i][j][r] - ref) * kLog2e);
+                    else s += expf(acc[i][j][r] - ref);
+                }
+            s += __shfl_xor(s, 32, kWave);
+            mine[j] = make_float2(mx, s);
+        }
+#pragma unroll
+        for (int j = 0; j < WNF; ++j)
+            if (h == 0) red[wm * BN + wn * (32 * WNF) + 32 * j + lr] = mine[j];
+        __syncthreads();
+        for (int c = tid; c < BN; c += 64 * NW) {
+            float mx = red[c].x;
+#pragma unroll
+            for (int w = 1; w < WGM; ++w) mx = fmaxf(mx, red[w * BN + c].x);
+            float s = 0.f;
+#pragma unroll
+            for (int w = 0; w < WGM; ++w) {
+                const float2 o = red[w * BN + c];
+                s += o.x == -INFINITY ? o.y : o.y * expf(o.x - mx);
+            }
+            a.stats[(a.v0 / kVTile + mt) * a.rows + n0 + c] = make_float2(mx, s);
+        }
+    } else if constexpr (EPI == kProb) {
+        const bool tail = a.v0 + m0 + BM > a.n_classes;
+#pragma unroll
+        for (int j = 0; j < WNF; ++j) {
+            const int64_t n = nw + 32 * j + lr;
+            const float lse = a.lse[n];
+            const bool counts = row_counts(lse);
+            const int y = label_place(n);
+#pragma unroll
+            for (int i = 0; i < WMF; ++i) {
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    const int m = 32 * i + 8 * (r / 4) + 4 * h + r % 4;
+                    float p;
+                    if constexpr (PL == 1) p = __builtin_amdgcn_exp2f((acc[i][j][r] - lse) * kLog2e);
+                    else p = expf(acc[i][j][r] - lse);
+                    if (y == m) p -= 1.f;
+                    acc[i][j][r] = counts && !(tail && a.v0 + mw + m >= a.n_classes) ? p : 0.f;
+                }
+                // two groups of 4 classes of the lane and of lane ^ 32 make two chunks of 8, one for each
+#pragma unroll
+                for (int pl = 0; pl < PL; ++pl)
+#pragma unroll
+                    for (int g = 0; g < 4; g += 2) {
+                        uint32_t w[2][2];
+#pragma unroll
+                        for (int x = 0; x < 2; ++x)
+#pragma unroll
+                            for (int y2 = 0; y2 < 2; ++y2) {
+                                const float f0 = acc[i][j][4 * (g + x) + 2 * y2], f1 = acc[i][j][4 * (g + x) + 2 * y2 + 1];
+                                if constexpr (PL == 1) {
+                                    // rounded to the operands' type: half a step, 2^-9 of each p, is what
+                                    // rounding the gradients themselves costs
+                                    w[x][y2] = (uint32_t)bf16_rne(f0) | ((uint32_t)bf16_rne(f1) << 16);
+                                } else {
+                                    uint16_t q0[3], q1[3];
+                                    split3_bits(f0, q0[0], q0[1], q0[2]);
+                                    split3_bits(f1, q1[0], q1[1], q1[2]);
+                                    w[x][y2] = (uint32_t)q0[pl] | ((uint32_t)q1[pl] << 16);
+                                }
+                            }
+                        const auto lo = __builtin_amdgcn_permlane32_swap(w[0][0], w[1][0], false, false);
+                        const auto hi = __builtin_amdgcn_permlane32_swap(w[0][1], w[1][1], false, false);
+                        const int64_t chunk = (mw + 32 * i) / 8 + g + h;
+                        a.p[pl * a.p_plane + chunk * a.rows + n] = u32x4x{lo[0], hi[0], lo[1], hi[1]};
+                    }
+            }
+        }
+    } else if constexpr (EPI == kDh) {
+        f32x4x *to = a.part + blockIdx.y * a.split_stride +
+                     ((int64_t)blockIdx.x * NW + wid) * (WMF * WNF * 4 * 64) + lane;
+#pragma unroll
+        for (int i = 0; i < WMF; ++i)
+#pragma unroll
+            for (int j = 0; j < WNF; ++j)
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    f32x4x *at = to + ((i * WNF + j) * 4 + g) * 64;
+                    f32x4x v = {acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]};
+                    if (!a.first) v += *at;
+                    *at = v;
+                }
+    } else {
+        const float inv = a.inv_count[0];
+#pragma unroll
+        for (int j = 0; j < WNF; ++j) {
+            const int64_t v = a.v0 + nw + 32 * j + lr;
+            if (v >= a.n_classes) continue;
+#pragma unroll
+            for (int i = 0; i < WMF; ++i)
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    const int64_t c = mw + 32 * i + 8 * g + 4 * h;
+                    float x[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) x[e] = c + e < a.d ? acc[i][j][4 * g + e] * inv : 0.f;
+                    if (a.dw_bf16) {
+                        if (c < (a.d + 7) / 8 * 8)
+                            *(u32x2x *)((uint16_t *)a.dw + v * a.ld_dw + c) =
+                                u32x2x{(uint32_t)bf16_rne(x[0]) | ((uint32_t)bf16_rne(x[1]) << 16),
+                                       (uint32_t)bf16_rne(x[2]) | ((uint32_t)bf16_rne(x[3]) << 16)};
+                    } else if (c < (a.d + 3) / 4 * 4) {
+                        *(f32x4x *)((float *)a.dw + v * a.ld_dw + c) = f32x4x{x[0], x[1], x[2], x[3]};
+                    }
+                }
+        }
+    }
+}
+
+// ------------------------------------------------------------- rows and loss
+// Joins a row's tiles: lse (+inf for a row that does not count), the row's
+// loss.  32 rows a workgroup, the tiles dealt to 8 threads of each.
+__global__ void __launch_bounds__(256) k_xent_rows(const float2 *__restrict__ stats, int64_t tiles, int64_t rows,
+                                                   int64_t m, const int32_t *__restrict__ labels, int32_t ignore,
+                                                   int64_t n_classes, const float *__restrict__ label_logit,
+                                                   float *__restrict__ lse, float *__restrict__ losses,
+                                                   float *__restrict__ row_loss) {
+    __shared__ float2 part[8][32];
+    const int tid = threadIdx.x, c = tid & 31, k = tid >> 5;
+    const int64_t n = (int64_t)blockIdx.x * 32 + c;
+    float mx = -INFINITY, s = 0.f;
+    auto join = [&](float2 o) {
+        const float top = fmaxf(mx, o.x);
+        const float ref = top == -INFINITY ? 0.f : top;
+        s = s * expf(mx - ref) + (o.x == -INFINITY ? o.y : o.y * expf(o.x - ref));
+        mx = top;
+    };
+#pragma unroll 4
+    for (int64_t t = k; t < tiles; t += 8) join(stats[t * rows + n]);
+    part[k][c] = make_float2(mx, s);
+    __syncthreads();
+    if (k > 0) return;
+    for (int w = 1; w < 8; ++w) join(part[w][c]);
+    const int32_t y = n < m ? labels[n] : ignore;
+    const bool out = n >= m || y == ignore, bad = !out && (y < 0 || y >= n_classes);
+    const float top = mx + logf(s);
+    lse[n] = out || bad ? INFINITY : top;
+    const float loss = out ? 0.f : bad ? NAN : logf(s) + (mx - label_logit[n]);
+    losses[n] = loss;
+    if (row_loss && n < m) row_loss[n] = loss;
+}
+
+// The mean over the rows that count, in 64 bits and a fixed order, and its weight.
+__global__ void __launch_bounds__(256) k_xent_loss(const float *__restrict__ losses, int64_t m,
+                                                   const int32_t *__restrict__ labels, int32_t ignore,
+                                                   float *__restrict__ loss, float *__restrict__ inv_count) {
+    __shared__ double part[256];
+    __shared__ int64_t count[256];
+    double s = 0.0;
+    int64_t k = 0;
+    for (int64_t i = threadIdx.x; i < m; i += 256) {
+        s += (double)losses[i];
+        k += labels[i] != ignore;
+    }
+    part[threadIdx.x] = s;
+    count[threadIdx.x] = k;
+    __syncthreads();
+    for (int w = 128; w > 0; w >>= 1) {
+        if ((int)threadIdx.x < w) {
+            part[threadIdx.x] += part[threadIdx.x + w];
+            count[threadIdx.x] += count[threadIdx.x + w];
+        }
+        __syncthreads();
+    }
+    if (threadIdx.x == 0) {
+        loss[0] = count[0] > 0 ? (float)(part[0] / (double)count[0]) : 0.f;
+        inv_count[0] = count[0] > 0 ? (float)(1.0 / (double)count[0]) : 0.f;
+    }
+}
+
+// dh from the splits' parts, in the order the products kept them in.
+template <int WMF, int WNF, int WGM, int WGN>
+__global__ void __launch_bounds__(256) k_xent_dh(const f32x4x *__restrict__ part, int64_t total, int32_t splits,
+                                                 int64_t split_stride, int32_t m_tiles, int64_t m, int64_t d,
+                                                 const float *__restrict__ lse, const float *__restrict__ inv_count,
+                                                 void *__restrict__ dh, int64_t ld, bool bf16) {
+    const float inv = inv_count[0];
+    const int64_t stride = (int64_t)gridDim.x * 256;
+    for (int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x; at < total; at += stride) {
+        int64_t x = at;
+        const int lane = x & 63;
+        x >>= 6;
+        const int g = x & 3;
+        x >>= 2;
+        const int j = x % WNF;
+        x /= WNF;
+        const int i = x % WMF;
+        x /= WMF;
+        const int wid = x % (WGM * WGN);
+        x /= WGM * WGN;
+        const int64_t c = (x % m_tiles) * (32 * WMF * WGM) + (wid / WGN) * (32 * WMF) + 32 * i + 8 * g + 4 * (lane >> 5);
+        const int64_t n = (x / m_tiles) * (32 * WNF * WGN) + (wid % WGN) * (32 * WNF) + 32 * j + (lane & 31);
+        const int64_t width = bf16 ? (d + 7) / 8 * 8 : (d + 3) / 4 * 4;
+        if (n >= m || c >= width) continue;
+        f32x4x v = {0.f, 0.f, 0.f, 0.f};
+        if (row_counts(lse[n]))
+            for (int32_t s = 0; s < splits; ++s) v += part[s * split_stride + at];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = c + e < d ? v[e] * inv : 0.f;
+        if (bf16)
+            *(u32x2x *)((uint16_t *)dh + n * ld + c) = u32x2x{(uint32_t)bf16_rne(v[0]) | ((uint32_t)bf16_rne(v[1]) << 16),
+                                                              (uint32_t)bf16_rne(v[2]) | ((uint32_t)bf16_rne(v[3]) << 16)};
+        else
+            *(f32x4x *)((float *)dh + n * ld + c) = v;
+    }
+}
+
+// ------------------------------------------------------------------ the plan
+namespace {
+
+constexpr int64_t kPBytes = int64_t(192) << 20;   // p of a piece, at most (or one tile of classes)
+constexpr int64_t kWBytes = int64_t(512) << 20;   // packed weights of a piece, at most (or one tile)
+
+int64_t up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
+
+struct XentPlan {
+    int pl;                         // planes
+    int64_t rows, rn, bk;           // packed rows of h, rows of a tile, summed elements per step
+    int64_t bm, width, chunks;      // features of a gradient tile, packed columns, their chunks
+    int64_t piece, tiles;           // classes of a piece, logit tiles in all
+    int32_t splits, split_steps;    // of dh's sum over a piece
+    size_t h, w, p, part, stats, label_logit, lse, losses, inv, total;
+
+    XentPlan(int64_t m, int64_t n_classes, int64_t d, bool bf16, bool grads, bool dh) {
+        pl = bf16 ? 1 : 3;
+        bk = bf16 ? 32 : 16;
+        rn = m <= 32 ? 32 : 128;
+        rows = up(std::max<int64_t>(m, 1), rn);
+        if (d <= 64) bm = 64;
+        else bm = bf16 && up(d, 256) * 10 <= up(d, 128) * 11 ? 256 : 128;
+        width = up(d, grads ? bm : 64);
+        chunks = width / 8;
+        const int64_t all = up(n_classes, kVTile);
+        tiles = all / kVTile;
+        piece = std::max<int64_t>(kVTile, kWBytes / (width * 2 * pl) / kVTile * kVTile);
+        if (grads) piece = std::min(piece, std::max<int64_t>(kVTile, kPBytes / (rows * 2 * pl) / kVTile * kVTile));
+        piece = std::min(piece, all);
+        const int64_t pieces = (all + piece - 1) / piece;
+        piece = up((all + pieces - 1) / pieces, kVTile);   // equal ones
+        splits = 1;
+        split_steps = 0;
+        if (dh) {
+            const int64_t t = width / bm * (rows / rn), steps = piece / bk;
+            splits = (int32_t)std::max<int64_t>(1, std::min(512 / t, steps / 8));
+            split_steps = (int32_t)((steps + splits - 1) / splits);
+            splits = (int32_t)((steps + split_steps - 1) / split_steps);
+        }
+        size_t at = 0;
+        auto take = [&](int64_t bytes) {
+            const size_t here = at;
+            at += (size_t)up(bytes, 256);
+            return here;
+        };
+        h = take(rows * width * 2 * pl);
+        w = take(piece * width * 2 * pl);
+        p = take(grads ? rows * piece * 2 * pl : 0);
+        part = take(dh ? splits * rows * width * 4 : 0);
+        stats = take(tiles * rows * 8);
+        label_logit = take(rows * 4);
+        lse = take(rows * 4);
+        losses = take(rows * 4);
+        inv = take(4);
+        total = at;
+    }
+};
+
+template <int PL, int WMF, int WNF, int WGM, int WGN, bool AT, bool BT, int EPI>
+void run_xent(XentArgs &a, int64_t mdim, int64_t ndim, int32_t splits, const char *label, hipStream_t s) {
+    constexpr int BK = PL == 1 ? 32 : 16, ST = 3;
+    a.m_tiles = (int32_t)(mdim / (32 * WMF * WGM));
+    a.n_tiles = (int32_t)(ndim / (32 * WNF * WGN));
+    KernelTimer t(label, s);
+    hipLaunchKernelGGL((k_xent<PL, WMF, WNF, WGM, WGN, BK, ST, AT, BT, EPI>),
+                       dim3((unsigned)a.m_tiles * (unsigned)a.n_tiles, (unsigned)splits), dim3(64 * WGM * WGN), 0, s, a);
+}
+
+// tile shapes: M x N = 256 x 128 (or x 32), for gradients 128 x 128 and 64 x 128 too
+template <int PL, bool AT, bool BT, int EPI>
+void run_shape(XentArgs &a, int64_t bm, int64_t bn, int64_t mdim, int64_t ndim, int32_t splits, const char *label,
+               hipStream_t s) {
+    constexpr bool kLogits = EPI == kStats || EPI == kProb;
+    if (bn == 32) {
+        if constexpr (EPI != kDw) {
+            if (bm == 256) return run_xent<PL, 2, 1, 4, 1, AT, BT, EPI>(a, mdim, ndim, splits, label, s);
+            if constexpr (!kLogits) {
+                if (bm == 128) return run_xent<PL, 1, 1, 4, 1, AT, BT, EPI>(a, mdim, ndim, splits, label, s);
+                return run_xent<PL, 1, 1, 2, 1, AT, BT, EPI>(a, mdim, ndim, splits, label, s);
+            }
+        }
+    } else {
+        if (bm == 256) {
+            if constexpr (PL == 1) return run_xent<PL, 4, 2, 2, 2, AT, BT, EPI>(a, mdim, ndim, splits, label, s);
+            else if constexpr (kLogits) return run_xent<PL, 2, 2, 4, 2, AT, BT, EPI>(a, mdim, ndim, splits, label, s);
+        }
+        if constexpr (!kLogits) {
+            if (bm == 128) return run_xent<PL, 2, 2, 2, 2, AT, BT, EPI>(a, mdim, ndim, splits, label, s);
+            return run_xent<PL, 1, 2, 2, 2, AT, BT, EPI>(a, mdim, ndim, splits, label, s);
+        }
+    }
+    fail(GNNAV_E_DEVICE, "no such tile");
+}
+
+template <int PL>
+void xent(const XentPlan &p, const LinearXentArgs &x, hipStream_t s) {
+    constexpr bool BF = PL == 1;
+    char *ws = (char *)x.workspace;
+    u32x4x *H = (u32x4x *)(ws + p.h), *W = (u32x4x *)(ws + p.w), *Pb = (u32x4x *)(ws + p.p);
+    float *lse = (float *)(ws + p.lse), *inv = (float *)(ws + p.inv), *losses = (float *)(ws + p.losses);
+    const int64_t esize = BF ? 2 : 4, k1 = up(x.d, p.bk);
+    auto pack_w = [&](int64_t v0, int64_t vp) {
+        KernelTimer t("xent_pack", s);
+        hipLaunchKernelGGL(k_xent_pack<BF>, dim3((unsigned)(vp / 64), (unsigned)((p.chunks + 7) / 8)), dim3(256), 0, s,
+                           (const char *)x.w + v0 * x.ld_w * esize, x.ld_w, std::min(vp, x.n_classes - v0), x.d,
+                           nullptr, 0, 0, vp, p.chunks, W);
+    };
+    {
+        KernelTimer t("xent_pack", s);
+        hipLaunchKernelGGL(k_xent_pack<BF>, dim3((unsigned)((p.rows + 63) / 64), (unsigned)((p.chunks + 7) / 8)),
+                           dim3(256), 0, s, x.h, x.ld_h, x.m, x.d, x.labels, x.ignore, x.n_classes, p.rows, p.chunks, H);
+    }
+    XentArgs a = {};
+    a.n_classes = x.n_classes;
+    a.rows = p.rows;
+    a.labels = x.labels;
+    a.m = x.m;
+    a.stats = (float2 *)(ws + p.stats);
+    a.label_logit = (float *)(ws + p.label_logit);
+    a.lse = lse;
+    a.inv_count = inv;
+    auto logits = [&](int64_t v0, int64_t vp) {
+        a.v0 = v0;
+        a.A = W;
+        a.a_rows = vp;
+        a.a_plane = p.chunks * vp;
+        a.B = H;
+        a.b_rows = p.rows;
+        a.b_plane = p.chunks * p.rows;
+        a.k = k1;
+    };
+    const int64_t all = p.tiles * kVTile;
+    bool packed = false;   // one piece: packed once for both passes
+    for (int64_t v0 = 0; v0 < all; v0 += p.piece) {
+        const int64_t vp = std::min(p.piece, all - v0);
+        pack_w(v0, vp);
+        packed = vp == all;
+        logits(v0, vp);
+        run_shape<PL, false, false, kStats>(a, 256, p.rn, vp, p.rows, 1, "xent_stats", s);
+    }
+    {
+        KernelTimer t("xent_rows", s);
+        hipLaunchKernelGGL(k_xent_rows, dim3((unsigned)(p.rows / 32)), dim3(256), 0, s, a.stats, p.tiles, p.rows, x.m,
+                           x.labels, x.ignore, x.n_classes, a.label_logit, lse, losses, x.row_loss);
+        hipLaunchKernelGGL(k_xent_loss, dim3(1), dim3(256), 0, s, losses, x.m, x.labels, x.ignore, x.loss, inv);
+    }
+    if (x.dh || x.dw) {
+        for (int64_t v0 = 0; v0 < all; v0 += p.piece) {
+            const int64_t vp = std::min(p.piece, all - v0);
+            if (!packed) pack_w(v0, vp);
+            logits(v0, vp);
+            a.p = Pb;
+            a.p_plane = vp / 8 * p.rows;
+            run_shape<PL, false, false, kProb>(a, 256, p.rn, vp, p.rows, 1, "xent_prob", s);
+            if (x.dw) {
+                a.A = H;
+                a.a_rows = p.rows;
+                a.a_plane = p.chunks * p.rows;
+                a.B = Pb;
+                a.b_rows = p.rows;
+                a.b_plane = a.p_plane;
+                a.k = p.rows;
+                a.dw = x.dw;
+                a.ld_dw = x.ld_dw;
+                a.d = x.d;
+                a.dw_bf16 = BF;
+                run_shape<PL, true, true, kDw>(a, p.bm, 128, p.width, vp, 1, "xent_dw", s);
+            }
+            if (x.dh) {
+                a.A = W;
+                a.a_rows = vp;
+                a.a_plane = p.chunks * vp;
+                a.B = Pb;
+                a.b_rows = p.rows;
+                a.b_plane = a.p_plane;
+                a.k = vp;
+                a.part = (f32x4x *)(ws + p.part);
+                a.split_stride = p.rows * p.width / 4;
+                a.split_steps = p.split_steps;
+                a.first = v0 == 0;
+                run_shape<PL, true, false, kDh>(a, p.bm, p.rn, p.width, p.rows, p.splits, "xent_dh", s);
+            }
+        }
+        if (x.dh) {
+            KernelTimer t("xent_dh_join", s);
+            const int64_t total = p.rows * p.width / 4;
+            const f32x4x *part = (const f32x4x *)(ws + p.part);
+            const int32_t mt = (int32_t)(p.width / p.bm);
+            const unsigned grid = grid_for(total, 256, 4096);
+#define GNNAV_L(A, B, C, D)                                                                                          \
+    hipLaunchKernelGGL((k_xent_dh<A, B, C, D>), dim3(grid), dim3(256), 0, s, part, total, p.splits, total, mt, x.m,   \
+                       x.d, lse, inv, x.dh, x.ld_dh, BF)
+            if (p.rn == 32) {
+                if (p.bm == 256) GNNAV_L(2, 1, 4, 1);
+                else if (p.bm == 128) GNNAV_L(1, 1, 4, 1);
+                else GNNAV_L(1, 1, 2, 1);
+            } else if (p.bm == 256) {
+                GNNAV_L(4, 2, 2, 2);
+            } else if (p.bm == 128) {
+                GNNAV_L(2, 2, 2, 2);
+            } else {
+                GNNAV_L(1, 2, 2, 2);
+            }
+#undef GNNAV_L
+        }
+    }
+    GNNAV_HIP(hipGetLastError());
+}
+
+}  // namespace
+
+size_t linear_xent_workspace(int64_t m, int64_t n_classes, int64_t d, bool bf16, bool grads) {
+    return XentPlan(m, n_classes, d, bf16, grads, grads).total;
+}
+
+void launch_linear_xent(const LinearXentArgs &x, hipStream_t s) {
+    const XentPlan p(x.m, x.n_classes, x.d, x.bf16, x.dh || x.dw, x.dh != nullptr);
+    if (x.bf16) xent<1>(p, x, s);
+    else xent<3>(p, x, s);
+}
+
+}  // namespace gnnav
