@@ -43,6 +43,13 @@ typedef short s16x4 __attribute__((ext_vector_type(4)));
 constexpr int kVTile = 256;              // classes of a logit tile
 constexpr float kLog2e = 1.44269504088896340736f;
 
+// Two values rounded to bf16, nearest even.
+__device__ __forceinline__ uint32_t bf16_pair(float lo, float hi) {
+    typedef float f32x2 __attribute__((ext_vector_type(2)));
+    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{lo, hi}, bf16x2));
+}
+
 // What a row does: counted rows carry their lse, the others +inf, which makes
 // every p of theirs zero.
 __device__ __forceinline__ bool row_counts(float lse) { return lse < INFINITY || lse != lse; }
@@ -121,7 +128,7 @@ struct XentArgs {
     int64_t a_rows, b_rows;    // rows of their chunks
     int64_t a_plane, b_plane;  // chunks of a plane
     int64_t k;                 // summed length, a multiple of the step
-    int32_t m_tiles, n_tiles;
+    int32_t m_tiles, n_tiles, splits;
     int32_t split_steps;       // kDh: steps of one split
     // kStats, kProb
     int64_t v0, n_classes;     // first class of the piece, classes in all
@@ -145,24 +152,49 @@ struct XentArgs {
 };
 
 // Wave grid WGM x WGN, each wavefront WMF x WNF MFMA blocks of 32 x 32; BK summed
-// elements per stage, ST stages in LDS.  AT, BT: the operand's rows are summed over.
-template <int PL, int WMF, int WNF, int WGM, int WGN, int BK, int ST, bool AT, bool BT, int EPI>
-__global__ void __launch_bounds__(64 * WGM * WGN, 2) k_xent(const XentArgs a) {
-    constexpr int NW = WGM * WGN, BM = 32 * WMF * WGM, BN = 32 * WNF * WGN;
-    constexpr int APC = BM * BK / 8, BPC = BN * BK / 8;      // chunks of a plane of a stage
-    constexpr int STAGE = PL * (APC + BPC);
-    constexpr int INSTR = STAGE / 64, IN = (INSTR + NW - 1) / NW;
+// elements per stage, ST stages in LDS.
+template <int PL, int WMF, int WNF, int WGM, int WGN>
+struct Tile {
+    static constexpr int BK = PL == 1 ? 32 : 16;
+    static constexpr int NW = WGM * WGN, BM = 32 * WMF * WGM, BN = 32 * WNF * WGN;
+    static constexpr int APC = BM * BK / 8, BPC = BN * BK / 8;   // chunks of a plane of a stage
+    static constexpr int STAGE = PL * (APC + BPC);
+    static constexpr int ST = WGN == 4 && WNF == 2 ? 4 : 3, LDS = ST * STAGE;   // stages: two workgroups a unit, or one
     static_assert(APC % 64 == 0 && BPC % 64 == 0, "whole wavefront copies");
-    __shared__ u32x4x S[ST * STAGE];
-    __shared__ float2 red[EPI == kStats ? WGM * BN : 1];
+};
+
+// Tile of workgroup `id` of those of one product.  Workgroups go to the eight
+// XCDs in turn; each XCD gets a contiguous run of the tiles, in groups of
+// kGroup along M, so that the tiles it works on together share operands in its L2.
+constexpr int kGroup = 8;
+__device__ __forceinline__ bool tile_of(const XentArgs &a, int32_t id, int32_t &split, int32_t &mt, int32_t &nt) {
+    const int32_t plane = a.m_tiles * a.n_tiles, total = plane * a.splits;
+    const int32_t per = total / 8, extra = total % 8, x = id & 7, k = id >> 3;
+    if (k >= per + (x < extra ? 1 : 0)) return false;
+    const int32_t lin = x * per + std::min(x, extra) + k;
+    split = lin / plane;
+    const int32_t t = lin - split * plane, g = t / (kGroup * a.n_tiles), r = t - g * (kGroup * a.n_tiles);
+    const int32_t wide = std::min(kGroup, a.m_tiles - g * kGroup);
+    nt = r / wide;
+    mt = g * kGroup + r - nt * wide;
+    return true;
+}
+
+// AT, BT: the operand's rows are summed over.
+template <int PL, int WMF, int WNF, int WGM, int WGN, bool AT, bool BT, int EPI>
+__device__ __forceinline__ void xent_tile(const XentArgs &a, int32_t id, u32x4x *S, float2 *red) {
+    using C = Tile<PL, WMF, WNF, WGM, WGN>;
+    constexpr int BK = C::BK, ST = C::ST, NW = C::NW, BM = C::BM, BN = C::BN, APC = C::APC, BPC = C::BPC;
+    constexpr int STAGE = C::STAGE, INSTR = STAGE / 64, IN = (INSTR + NW - 1) / NW;
     const int tid = threadIdx.x, lane = tid & 63, wid = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wm = wid / WGN, wn = wid % WGN, h = lane >> 5, lr = lane & 31;
-    const int32_t mt = blockIdx.x % a.m_tiles, nt = blockIdx.x / a.m_tiles;
+    int32_t split, mt, nt;
+    if (!tile_of(a, id, split, mt, nt)) return;
     const int64_t m0 = (int64_t)mt * BM, n0 = (int64_t)nt * BN;
     const int32_t all_steps = (int32_t)(a.k / BK);
     int32_t s0 = 0, T = all_steps;
     if constexpr (EPI == kDh) {
-        s0 = blockIdx.y * a.split_steps;
+        s0 = split * a.split_steps;
         T = std::min(a.split_steps, all_steps - s0);
     }
 
@@ -181,7 +213,7 @@ __global__ void __launch_bounds__(64 * WGM * WGN, 2) k_xent(const XentArgs a) {
         const int64_t R = isB ? a.b_rows : a.a_rows, x0 = isB ? n0 : m0;
         const bool tr = isB ? BT : AT;
         if (tr) {
-            const int mc = s / BK, kk = (s % BK) ^ ((mc & 1) * 4);
+            const int mc = s / BK, kk = (s % BK) ^ ((mc & 3) * 4);
             src[u] = (const char *)(base + (x0 / 8 + mc) * R + (int64_t)s0 * BK + kk);
             inc[u] = (int64_t)BK * 16;
         } else {
@@ -191,12 +223,9 @@ __global__ void __launch_bounds__(64 * WGM * WGN, 2) k_xent(const XentArgs a) {
         }
         dst[u] = slot;
     }
-    auto issue = [&](int stage) {
-#pragma unroll
-        for (int u = 0; u < IN; ++u) {
-            dma16(src[u], &S[stage * STAGE + dst[u]]);
-            src[u] += inc[u];
-        }
+    auto issue = [&](int stage, int u) {
+        dma16(src[u], &S[stage * STAGE + dst[u]]);
+        src[u] += inc[u];
     };
 
     f32x16x acc[WMF][WNF];
@@ -209,7 +238,7 @@ __global__ void __launch_bounds__(64 * WGM * WGN, 2) k_xent(const XentArgs a) {
 
     // lane parts of the fragments' LDS addresses
     const int tr_mc = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1), tr_k = 8 * h + ((lane & 15) >> 2);
-    const int tr_swz = (tr_mc & 1) * 4;
+    const int tr_swz = tr_mc * 4;   // of the lane's chunk, its number mod 4: 32 lanes read from 256 bytes of distinct banks
     auto frag = [&](const u32x4x *plane, auto tr_, int tile, int x, int kk) -> bf16x8 {
         if constexpr (decltype(tr_)::value) {
             typedef __attribute__((address_space(3))) s16x4 lds4;
@@ -223,45 +252,90 @@ __global__ void __launch_bounds__(64 * WGM * WGN, 2) k_xent(const XentArgs a) {
             return __builtin_bit_cast(bf16x8, plane[(2 * kk + h) * tile + x + lr]);
         }
     };
-    auto compute = [&](int stage) {
+    struct Frags {
+        bf16x8 a[WMF][PL], b[WNF][PL];
+    };
+    // fragment k of a step: B's, then A's, as the products need them
+    constexpr int NF = (WMF + WNF) * PL;
+    auto read = [&](Frags &f, int stage, int kk, int k) {
         const u32x4x *sa = &S[stage * STAGE], *sb = sa + PL * APC;
+        const int x = k / PL, p = k % PL;
+        if (x < WNF) f.b[x][p] = frag(sb + p * BPC, std::integral_constant<bool, BT>(), BN, wn * (32 * WNF) + 32 * x, kk);
+        else f.a[x - WNF][p] = frag(sa + p * APC, std::integral_constant<bool, AT>(), BM, wm * (32 * WMF) + 32 * (x - WNF), kk);
+    };
+    // The products of one fragment set.  Between them go, one at a time, the reads of the next set (first half) and
+    // copies [c0, c1) of a stage to come (second half): in one burst behind the barrier they queue
+    // up, and the wavefront's products wait with them.  Past the last stage the reads are idle ones.
+    auto multiply = [&](const Frags &f, Frags &nxt, int from, int kk, bool more, int into, auto c0_, auto c1_) {
+        constexpr int SLOTS = WMF * WNF, HALF = (SLOTS + 1) / 2, C0 = decltype(c0_)::value, C1 = decltype(c1_)::value;
+        constexpr int REST = SLOTS > HALF ? SLOTS - HALF : 1, CUT = SLOTS > HALF ? HALF : 0;
 #pragma unroll
-        for (int kk = 0; kk < BK / 16; ++kk) {
-            bf16x8 fa[WMF][PL], fb[WNF][PL];
+        for (int k = 0; k < SLOTS; ++k) {
+            const int i = k / WNF, j = k % WNF;
+            if constexpr (PL == 1)
+                acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f.a[i][0], f.b[j][0], acc[i][j], 0, 0, 0);
+            else
+                acc[i][j] = mfma_split6(f.a[i][0], f.a[i][PL - 2], f.a[i][PL - 1], f.b[j][0], f.b[j][PL - 2],
+                                        f.b[j][PL - 1], acc[i][j]);
+            __builtin_amdgcn_sched_barrier(0);
+            if (k < HALF)
 #pragma unroll
-            for (int i = 0; i < WMF; ++i)
+                for (int q = NF * k / HALF; q < NF * (k + 1) / HALF; ++q) read(nxt, from, kk, q);
+            if (k >= CUT && more)
 #pragma unroll
-                for (int p = 0; p < PL; ++p)
-                    fa[i][p] = frag(sa + p * APC, std::integral_constant<bool, AT>(), BM, wm * (32 * WMF) + 32 * i, kk);
-#pragma unroll
-            for (int j = 0; j < WNF; ++j)
-#pragma unroll
-                for (int p = 0; p < PL; ++p)
-                    fb[j][p] = frag(sb + p * BPC, std::integral_constant<bool, BT>(), BN, wn * (32 * WNF) + 32 * j, kk);
-#pragma unroll
-            for (int i = 0; i < WMF; ++i)
-#pragma unroll
-                for (int j = 0; j < WNF; ++j) {
-                    if constexpr (PL == 1)
-                        acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa[i][0], fb[j][0], acc[i][j], 0, 0, 0);
-                    else
-                        acc[i][j] = mfma_split6(fa[i][0], fa[i][PL - 2], fa[i][PL - 1], fb[j][0], fb[j][PL - 2],
-                                                fb[j][PL - 1], acc[i][j]);
-                }
+                for (int q = C0 + (C1 - C0) * (k - CUT) / REST; q < C0 + (C1 - C0) * (k - CUT + 1) / REST; ++q) issue(into, q);
+            __builtin_amdgcn_sched_barrier(0);
         }
     };
-
-#pragma unroll
-    for (int s = 0; s < ST - 1; ++s)
-        if (s < T) issue(s);
-    int stage = 0;
-    for (int32_t t = 0; t < T; ++t) {
-        if (ST > 2 && t + ST - 1 <= T) wait_vm<IN *(ST - 2)>();
+    // Makes stage t readable: its copies, of those of up to ST - 2 later stages, are done, everywhere.
+    auto advance = [&](int32_t t) {
+        const int32_t later = T - 1 - t;
+        if (later >= ST - 2) wait_vm<IN *(ST - 2)>();
+        else if (ST > 3 && later == 1) wait_vm<IN>();
         else wait_vm<0>();
-        lds_barrier();   // stage t visible, everyone done with the one before it
-        if (t + ST - 1 < T) issue(stage == 0 ? ST - 1 : stage - 1);
-        compute(stage);
-        stage = stage + 1 == ST ? 0 : stage + 1;
+        lds_barrier();
+    };
+    static_assert((ST == 3 || ST == 4) && (BK == 16 || BK == 32), "loop below");
+    auto next = [](int stage) { return stage + 1 == ST ? 0 : stage + 1; };
+    // One fragment set is multiplied while the next one is read, across the barrier between two stages.  Once
+    // stage t is readable, stage t + ST - 1 is copied into the one read before it, over the products up to the next barrier.
+    constexpr int FIRST = BK == 32 ? IN / 2 : IN;   // copies before a stage's second fragment set is read
+    constexpr std::integral_constant<int, 0> kBegin{};
+    constexpr std::integral_constant<int, FIRST> kMiddle{};
+    constexpr std::integral_constant<int, IN> kEnd{};
+    Frags f0, f1;
+    int ready = 0, fill = BK == 32 ? ST - 1 : 0;
+    if (T > 0) {
+#pragma unroll
+        for (int k = 0; k < ST - 1; ++k)
+            if (k < T)
+#pragma unroll
+                for (int u = 0; u < IN; ++u) issue(k, u);
+        advance(0);
+        if (ST - 1 < T)
+#pragma unroll
+            for (int u = 0; u < FIRST; ++u) issue(ST - 1, u);
+#pragma unroll
+        for (int q = 0; q < NF; ++q) read(f0, 0, 0, q);
+    }
+    for (int32_t t = 0; t < T;) {
+        if constexpr (BK == 32) {
+            multiply(f0, f1, ready, 1, t + ST - 1 < T, fill, kMiddle, kEnd);
+            fill = next(fill);
+            ready = next(ready);
+            if (++t < T) advance(t);
+            multiply(f1, f0, ready, 0, t + ST - 1 < T, fill, kBegin, kMiddle);
+        } else {
+            ready = next(ready);
+            if (++t < T) advance(t);
+            multiply(f0, f1, ready, 0, t + ST - 1 < T, fill, kBegin, kEnd);
+            fill = next(fill);
+            if (t >= T) break;
+            ready = next(ready);
+            if (++t < T) advance(t);
+            multiply(f1, f0, ready, 0, t + ST - 1 < T, fill, kBegin, kEnd);
+            fill = next(fill);
+        }
     }
 
     // block (i, j), register r of a lane: M index 32 i + 8 (r / 4) + 4 h + r % 4, N index 32 j + lane % 32
@@ -278,15 +352,17 @@ __global__ void __launch_bounds__(64 * WGM * WGN, 2) k_xent(const XentArgs a) {
         for (int j = 0; j < WNF; ++j) {
             const int64_t n = nw + 32 * j + lr;
             const int y = label_place(n);
+            if (tail)
+#pragma unroll
+                for (int i = 0; i < WMF; ++i)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r)
+                        if (a.v0 + mw + 32 * i + 8 * (r / 4) + 4 * h + r % 4 >= a.n_classes) acc[i][j][r] = -INFINITY;
             float mx = -INFINITY;
 #pragma unroll
             for (int i = 0; i < WMF; ++i)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    const int m = 32 * i + 8 * (r / 4) + 4 * h + r % 4;
-                    if (tail && a.v0 + mw + m >= a.n_classes) acc[i][j][r] = -INFINITY;
-                    mx = fmaxf(mx, acc[i][j][r]);
-                }
+                for (int r = 0; r < 16; ++r) mx = fmaxf(mx, acc[i][j][r]);
             if (y >= 0) {
 #pragma unroll
                 for (int i = 0; i < WMF; ++i)
@@ -302,6 +378,7 @@ __global__ void __launch_bounds__(64 * WGM * WGN, 2) k_xent(const XentArgs a) {
             for (int i = 0; i < WMF; ++i)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
+                    // (the difference first: of huge logits a product's rounding alone would overflow)
                     if constexpr (PL == 1) s += __builtin_amdgcn_exp2f((acc[i][j][r] - ref) * kLog2e);
                     else s += expf(acc[i][j][r] - ref);
                 }
@@ -330,19 +407,27 @@ __global__ void __launch_bounds__(64 * WGM * WGN, 2) k_xent(const XentArgs a) {
         for (int j = 0; j < WNF; ++j) {
             const int64_t n = nw + 32 * j + lr;
             const float lse = a.lse[n];
-            const bool counts = row_counts(lse);
             const int y = label_place(n);
 #pragma unroll
-            for (int i = 0; i < WMF; ++i) {
+            for (int i = 0; i < WMF; ++i)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
-                    const int m = 32 * i + 8 * (r / 4) + 4 * h + r % 4;
-                    float p;
-                    if constexpr (PL == 1) p = __builtin_amdgcn_exp2f((acc[i][j][r] - lse) * kLog2e);
-                    else p = expf(acc[i][j][r] - lse);
-                    if (y == m) p -= 1.f;
-                    acc[i][j][r] = counts && !(tail && a.v0 + mw + m >= a.n_classes) ? p : 0.f;
+                    if constexpr (PL == 1) acc[i][j][r] = __builtin_amdgcn_exp2f((acc[i][j][r] - lse) * kLog2e);
+                    else acc[i][j][r] = expf(acc[i][j][r] - lse);
                 }
+            const bool dead = !row_counts(lse);
+            if (__any(y >= 0 || dead) || tail) {   // labels here, rows or classes that are none
+#pragma unroll
+                for (int i = 0; i < WMF; ++i)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) {
+                        const int m = 32 * i + 8 * (r / 4) + 4 * h + r % 4;
+                        if (y == m) acc[i][j][r] -= 1.f;
+                        if (dead || (tail && a.v0 + mw + m >= a.n_classes)) acc[i][j][r] = 0.f;
+                    }
+            }
+#pragma unroll
+            for (int i = 0; i < WMF; ++i) {
                 // two groups of 4 classes of the lane and of lane ^ 32 make two chunks of 8, one for each
 #pragma unroll
                 for (int pl = 0; pl < PL; ++pl)
@@ -357,7 +442,7 @@ __global__ void __launch_bounds__(64 * WGM * WGN, 2) k_xent(const XentArgs a) {
                                 if constexpr (PL == 1) {
                                     // rounded to the operands' type: half a step, 2^-9 of each p, is what
                                     // rounding the gradients themselves costs
-                                    w[x][y2] = (uint32_t)bf16_rne(f0) | ((uint32_t)bf16_rne(f1) << 16);
+                                    w[x][y2] = bf16_pair(f0, f1);
                                 } else {
                                     uint16_t q0[3], q1[3];
                                     split3_bits(f0, q0[0], q0[1], q0[2]);
@@ -373,8 +458,8 @@ __global__ void __launch_bounds__(64 * WGM * WGN, 2) k_xent(const XentArgs a) {
             }
         }
     } else if constexpr (EPI == kDh) {
-        f32x4x *to = a.part + blockIdx.y * a.split_stride +
-                     ((int64_t)blockIdx.x * NW + wid) * (WMF * WNF * 4 * 64) + lane;
+        f32x4x *to = a.part + split * a.split_stride +
+                     ((int64_t)(nt * a.m_tiles + mt) * NW + wid) * (WMF * WNF * 4 * 64) + lane;
 #pragma unroll
         for (int i = 0; i < WMF; ++i)
 #pragma unroll
@@ -403,14 +488,33 @@ __global__ void __launch_bounds__(64 * WGM * WGN, 2) k_xent(const XentArgs a) {
                     if (a.dw_bf16) {
                         if (c < (a.d + 7) / 8 * 8)
                             *(u32x2x *)((uint16_t *)a.dw + v * a.ld_dw + c) =
-                                u32x2x{(uint32_t)bf16_rne(x[0]) | ((uint32_t)bf16_rne(x[1]) << 16),
-                                       (uint32_t)bf16_rne(x[2]) | ((uint32_t)bf16_rne(x[3]) << 16)};
+                                u32x2x{bf16_pair(x[0], x[1]), bf16_pair(x[2], x[3])};
                     } else if (c < (a.d + 3) / 4 * 4) {
                         *(f32x4x *)((float *)a.dw + v * a.ld_dw + c) = f32x4x{x[0], x[1], x[2], x[3]};
                     }
                 }
         }
     }
+}
+
+template <int PL, int WMF, int WNF, int WGM, int WGN, int EPI>
+__global__ void __launch_bounds__(64 * WGM * WGN, 2) k_xent_logits(const XentArgs a) {
+    using C = Tile<PL, WMF, WNF, WGM, WGN>;
+    __shared__ u32x4x S[C::LDS];
+    __shared__ float2 red[EPI == kStats ? WGM * C::BN : 1];
+    xent_tile<PL, WMF, WNF, WGM, WGN, false, false, EPI>(a, blockIdx.x, S, red);
+}
+
+// A piece's dw and dh in one launch: the workgroups of dw (of the first `dw_ids`), then those of dh, fill
+// the units together.  dw's tiles are 32 x WMF x WGM by 32 x WNW x WGN, dh's 32 x WMF x WGM by 32 x WNH x WGN.
+template <int PL, int WMF, int WNW, int WNH, int WGM, int WGN, int WGMH, int WMFH>
+__global__ void __launch_bounds__(64 * WGM * WGN, 2) k_xent_grads(const XentArgs w, const XentArgs h, int32_t dw_ids) {
+    constexpr int WGNH = WGM * WGN / WGMH;
+    using CW = Tile<PL, WMF, WNW, WGM, WGN>;
+    using CH = Tile<PL, WMFH, WNH, WGMH, WGNH>;
+    __shared__ u32x4x S[CW::LDS > CH::LDS ? CW::LDS : CH::LDS];
+    if ((int32_t)blockIdx.x < dw_ids) xent_tile<PL, WMF, WNW, WGM, WGN, true, true, kDw>(w, blockIdx.x, S, nullptr);
+    else xent_tile<PL, WMFH, WNH, WGMH, WGNH, true, false, kDh>(h, blockIdx.x - dw_ids, S, nullptr);
 }
 
 // ------------------------------------------------------------- rows and loss
@@ -500,12 +604,12 @@ __global__ void __launch_bounds__(256) k_xent_dh(const f32x4x *__restrict__ part
         if (n >= m || c >= width) continue;
         f32x4x v = {0.f, 0.f, 0.f, 0.f};
         if (row_counts(lse[n]))
+#pragma unroll 8
             for (int32_t s = 0; s < splits; ++s) v += part[s * split_stride + at];
 #pragma unroll
         for (int e = 0; e < 4; ++e) v[e] = c + e < d ? v[e] * inv : 0.f;
         if (bf16)
-            *(u32x2x *)((uint16_t *)dh + n * ld + c) = u32x2x{(uint32_t)bf16_rne(v[0]) | ((uint32_t)bf16_rne(v[1]) << 16),
-                                                              (uint32_t)bf16_rne(v[2]) | ((uint32_t)bf16_rne(v[3]) << 16)};
+            *(u32x2x *)((uint16_t *)dh + n * ld + c) = u32x2x{bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3])};
         else
             *(f32x4x *)((float *)dh + n * ld + c) = v;
     }
@@ -514,14 +618,15 @@ __global__ void __launch_bounds__(256) k_xent_dh(const f32x4x *__restrict__ part
 // ------------------------------------------------------------------ the plan
 namespace {
 
-constexpr int64_t kPBytes = int64_t(192) << 20;   // p of a piece, at most (or one tile of classes)
+constexpr int64_t kPBytes = int64_t(1) << 30;     // p of a piece, at most (or one tile of classes)
 constexpr int64_t kWBytes = int64_t(512) << 20;   // packed weights of a piece, at most (or one tile)
 
 int64_t up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
 
 struct XentPlan {
     int pl;                         // planes
-    int64_t rows, rn, bk;           // packed rows of h, rows of a tile, summed elements per step
+    int64_t rows, bk;               // packed rows of h, summed elements per step
+    int64_t ln, rn;                 // rows of a logit tile, of a dh tile (and classes of a dw tile, at least 128)
     int64_t bm, width, chunks;      // features of a gradient tile, packed columns, their chunks
     int64_t piece, tiles;           // classes of a piece, logit tiles in all
     int32_t splits, split_steps;    // of dh's sum over a piece
@@ -530,10 +635,14 @@ struct XentPlan {
     XentPlan(int64_t m, int64_t n_classes, int64_t d, bool bf16, bool grads, bool dh) {
         pl = bf16 ? 1 : 3;
         bk = bf16 ? 32 : 16;
-        rn = m <= 32 ? 32 : 128;
-        rows = up(std::max<int64_t>(m, 1), rn);
-        if (d <= 64) bm = 64;
+        if (d <= 64 && m > 32) bm = 64;
         else bm = bf16 && up(d, 256) * 10 <= up(d, 128) * 11 ? 256 : 128;
+        ln = rn = m <= 32 ? 32 : 128;
+        if (bf16 && bm == 256 && m > 128) {
+            rn = 256;
+            if (d >= 512) ln = 256;
+        }
+        rows = up(std::max<int64_t>(m, 1), grads ? rn : ln);
         width = up(d, grads ? bm : 64);
         chunks = width / 8;
         const int64_t all = up(n_classes, kVTile);
@@ -547,7 +656,7 @@ struct XentPlan {
         split_steps = 0;
         if (dh) {
             const int64_t t = width / bm * (rows / rn), steps = piece / bk;
-            splits = (int32_t)std::max<int64_t>(1, std::min(512 / t, steps / 8));
+            splits = (int32_t)std::max<int64_t>(1, std::min((rn == 256 ? 256 : 512) / t, steps / 8));
             split_steps = (int32_t)((steps + splits - 1) / splits);
             splits = (int32_t)((steps + split_steps - 1) / split_steps);
         }
@@ -570,40 +679,53 @@ struct XentPlan {
     }
 };
 
-template <int PL, int WMF, int WNF, int WGM, int WGN, bool AT, bool BT, int EPI>
-void run_xent(XentArgs &a, int64_t mdim, int64_t ndim, int32_t splits, const char *label, hipStream_t s) {
-    constexpr int BK = PL == 1 ? 32 : 16, ST = 3;
-    a.m_tiles = (int32_t)(mdim / (32 * WMF * WGM));
-    a.n_tiles = (int32_t)(ndim / (32 * WNF * WGN));
-    KernelTimer t(label, s);
-    hipLaunchKernelGGL((k_xent<PL, WMF, WNF, WGM, WGN, BK, ST, AT, BT, EPI>),
-                       dim3((unsigned)a.m_tiles * (unsigned)a.n_tiles, (unsigned)splits), dim3(64 * WGM * WGN), 0, s, a);
+unsigned ids_of(const XentArgs &a) {   // workgroups of a product, whole rounds over the XCDs
+    return (unsigned)up((int64_t)a.m_tiles * a.n_tiles * a.splits, 8);
 }
 
-// tile shapes: M x N = 256 x 128 (or x 32), for gradients 128 x 128 and 64 x 128 too
-template <int PL, bool AT, bool BT, int EPI>
-void run_shape(XentArgs &a, int64_t bm, int64_t bn, int64_t mdim, int64_t ndim, int32_t splits, const char *label,
-               hipStream_t s) {
-    constexpr bool kLogits = EPI == kStats || EPI == kProb;
-    if (bn == 32) {
-        if constexpr (EPI != kDw) {
-            if (bm == 256) return run_xent<PL, 2, 1, 4, 1, AT, BT, EPI>(a, mdim, ndim, splits, label, s);
-            if constexpr (!kLogits) {
-                if (bm == 128) return run_xent<PL, 1, 1, 4, 1, AT, BT, EPI>(a, mdim, ndim, splits, label, s);
-                return run_xent<PL, 1, 1, 2, 1, AT, BT, EPI>(a, mdim, ndim, splits, label, s);
-            }
-        }
-    } else {
+// Logit tiles: 256 classes x 128 rows (or 32); fp32 in 8 wavefronts where bf16 takes 4.
+template <int PL, int EPI>
+void run_logits(XentArgs &a, int64_t rn, int64_t vdim, const char *label, hipStream_t s) {
+    a.m_tiles = (int32_t)(vdim / kVTile);
+    a.n_tiles = (int32_t)(a.rows / rn);
+    a.splits = 1;
+    KernelTimer t(label, s);
+    if (rn == 32)
+        hipLaunchKernelGGL((k_xent_logits<PL, 2, 1, 4, 1, EPI>), dim3(ids_of(a)), dim3(256), 0, s, a);
+    else if constexpr (PL == 1) {
+        if (rn == 256)
+            hipLaunchKernelGGL((k_xent_logits<PL, 4, 2, 2, 4, EPI>), dim3(ids_of(a)), dim3(512), 0, s, a);
+        else
+            hipLaunchKernelGGL((k_xent_logits<PL, 4, 2, 2, 2, EPI>), dim3(ids_of(a)), dim3(256), 0, s, a);
+    } else
+        hipLaunchKernelGGL((k_xent_logits<PL, 2, 2, 4, 2, EPI>), dim3(ids_of(a)), dim3(512), 0, s, a);
+}
+
+// Gradient tiles: bm features x 128 classes for dw, bm x rn rows for dh.  Either product may be absent (no tiles).
+template <int PL>
+void run_grads(const XentArgs &w, const XentArgs &h, int64_t bm, int64_t rn, hipStream_t s) {
+    KernelTimer t("xent_grads", s);
+    const unsigned nw = w.m_tiles > 0 ? ids_of(w) : 0, nh = h.m_tiles > 0 ? ids_of(h) : 0;
+#define GNNAV_L(WMF, WNW, WNH, WGM, WGN, WGMH, WMFH)                                                                  \
+    hipLaunchKernelGGL((k_xent_grads<PL, WMF, WNW, WNH, WGM, WGN, WGMH, WMFH>), dim3(nw + nh),                           \
+                       dim3(64 * WGM * WGN), 0, s, w, h,                                                              \
+                       (int32_t)nw)
+    if (rn == 32) {
         if (bm == 256) {
-            if constexpr (PL == 1) return run_xent<PL, 4, 2, 2, 2, AT, BT, EPI>(a, mdim, ndim, splits, label, s);
-            else if constexpr (kLogits) return run_xent<PL, 2, 2, 4, 2, AT, BT, EPI>(a, mdim, ndim, splits, label, s);
+            if constexpr (PL == 1) GNNAV_L(4, 2, 1, 2, 2, 4, 2);
+        } else {
+            GNNAV_L(2, 2, 1, 2, 2, 4, 1);
         }
-        if constexpr (!kLogits) {
-            if (bm == 128) return run_xent<PL, 2, 2, 2, 2, AT, BT, EPI>(a, mdim, ndim, splits, label, s);
-            return run_xent<PL, 1, 2, 2, 2, AT, BT, EPI>(a, mdim, ndim, splits, label, s);
-        }
+    } else if (rn == 256) {
+        if constexpr (PL == 1) GNNAV_L(4, 2, 2, 2, 4, 2, 4);
+    } else if (bm == 256) {
+        if constexpr (PL == 1) GNNAV_L(4, 2, 2, 2, 2, 2, 4);
+    } else if (bm == 128) {
+        GNNAV_L(2, 2, 2, 2, 2, 2, 2);
+    } else {
+        GNNAV_L(1, 2, 2, 2, 2, 2, 1);
     }
-    fail(GNNAV_E_DEVICE, "no such tile");
+#undef GNNAV_L
 }
 
 template <int PL>
@@ -650,7 +772,7 @@ void xent(const XentPlan &p, const LinearXentArgs &x, hipStream_t s) {
         pack_w(v0, vp);
         packed = vp == all;
         logits(v0, vp);
-        run_shape<PL, false, false, kStats>(a, 256, p.rn, vp, p.rows, 1, "xent_stats", s);
+        run_logits<PL, kStats>(a, p.ln, vp, "xent_stats", s);
     }
     {
         KernelTimer t("xent_rows", s);
@@ -665,35 +787,30 @@ void xent(const XentPlan &p, const LinearXentArgs &x, hipStream_t s) {
             logits(v0, vp);
             a.p = Pb;
             a.p_plane = vp / 8 * p.rows;
-            run_shape<PL, false, false, kProb>(a, 256, p.rn, vp, p.rows, 1, "xent_prob", s);
-            if (x.dw) {
-                a.A = H;
-                a.a_rows = p.rows;
-                a.a_plane = p.chunks * p.rows;
-                a.B = Pb;
-                a.b_rows = p.rows;
-                a.b_plane = a.p_plane;
-                a.k = p.rows;
-                a.dw = x.dw;
-                a.ld_dw = x.ld_dw;
-                a.d = x.d;
-                a.dw_bf16 = BF;
-                run_shape<PL, true, true, kDw>(a, p.bm, 128, p.width, vp, 1, "xent_dw", s);
-            }
-            if (x.dh) {
-                a.A = W;
-                a.a_rows = vp;
-                a.a_plane = p.chunks * vp;
-                a.B = Pb;
-                a.b_rows = p.rows;
-                a.b_plane = a.p_plane;
-                a.k = vp;
-                a.part = (f32x4x *)(ws + p.part);
-                a.split_stride = p.rows * p.width / 4;
-                a.split_steps = p.split_steps;
-                a.first = v0 == 0;
-                run_shape<PL, true, false, kDh>(a, p.bm, p.rn, p.width, p.rows, p.splits, "xent_dh", s);
-            }
+            run_logits<PL, kProb>(a, p.ln, vp, "xent_prob", s);
+            XentArgs w = a, h = a;
+            w.B = h.B = Pb;
+            w.b_rows = h.b_rows = p.rows;
+            w.b_plane = h.b_plane = a.p_plane;
+            w.A = H;
+            w.a_rows = p.rows;
+            w.a_plane = p.chunks * p.rows;
+            w.k = p.rows;
+            w.dw = x.dw;
+            w.ld_dw = x.ld_dw;
+            w.d = x.d;
+            w.dw_bf16 = BF;
+            w.m_tiles = x.dw ? (int32_t)(p.width / p.bm) : 0;
+            w.n_tiles = (int32_t)(vp / std::max<int64_t>(p.rn, 128));
+            h.k = vp;
+            h.part = (f32x4x *)(ws + p.part);
+            h.split_stride = p.rows * p.width / 4;
+            h.split_steps = p.split_steps;
+            h.splits = p.splits;
+            h.first = v0 == 0;
+            h.m_tiles = x.dh ? (int32_t)(p.width / p.bm) : 0;
+            h.n_tiles = (int32_t)(p.rows / p.rn);
+            run_grads<PL>(w, h, p.bm, p.rn, s);
         }
         if (x.dh) {
             KernelTimer t("xent_dh_join", s);
@@ -706,8 +823,9 @@ void xent(const XentPlan &p, const LinearXentArgs &x, hipStream_t s) {
                        x.d, lse, inv, x.dh, x.ld_dh, BF)
             if (p.rn == 32) {
                 if (p.bm == 256) GNNAV_L(2, 1, 4, 1);
-                else if (p.bm == 128) GNNAV_L(1, 1, 4, 1);
-                else GNNAV_L(1, 1, 2, 1);
+                else GNNAV_L(1, 1, 4, 1);
+            } else if (p.rn == 256) {
+                GNNAV_L(4, 2, 2, 4);
             } else if (p.bm == 256) {
                 GNNAV_L(4, 2, 2, 2);
             } else if (p.bm == 128) {
