@@ -193,14 +193,18 @@ __global__ void __launch_bounds__(256) k_embedding_grad_few(const u32x4e *__rest
     if (p >= n) return;
     const int32_t id = ids[p];
     if (id < 0 || id >= n_rows) return;
-    // positions of the id: each wavefront scans a quarter of the list, twice
-    const int32_t quarter = ((n + 3) / 4 + kWave - 1) / kWave * kWave;
-    const int32_t b = std::min(wid * quarter, n), e = std::min(b + quarter, n);
+    // positions of the id: each wavefront looks through a quarter of the list
+    constexpr int PER = kFewIds / 4 / kWave;
+    int32_t seen[PER];
+    const int32_t b = wid * (kFewIds / 4);
+#pragma unroll
+    for (int k = 0; k < PER; ++k) seen[k] = b + k * kWave + lane < n ? ids[b + k * kWave + lane] : -1;
     int32_t mine = 0;
     bool earlier = false;
-    for (int32_t i = b; i < e; i += kWave) {
-        const bool hit = i + lane < e && ids[i + lane] == id;
-        earlier = earlier || (hit && i + lane < p);
+#pragma unroll
+    for (int k = 0; k < PER; ++k) {
+        const bool hit = seen[k] == id;
+        earlier = earlier || (hit && b + k * kWave + lane < p);
         mine += __popcll(__ballot(hit));
     }
     if (lane == 0) sh.p.counts[wid] = mine;
@@ -211,12 +215,14 @@ __global__ void __launch_bounds__(256) k_embedding_grad_few(const u32x4e *__rest
         at += w < wid ? sh.p.counts[w] : 0;
         total += sh.p.counts[w];
     }
-    for (int32_t i = b; i < e && mine > 0; i += kWave) {
-        const bool hit = i + lane < e && ids[i + lane] == id;
-        const uint64_t m = __ballot(hit);
-        if (hit) sh.p.list[at + __popcll(m & ((1ull << lane) - 1ull))] = i + lane;
-        at += __popcll(m);
-    }
+    if (mine > 0)
+#pragma unroll
+        for (int k = 0; k < PER; ++k) {
+            const bool hit = seen[k] == id;
+            const uint64_t m = __ballot(hit);
+            if (hit) sh.p.list[at + __popcll(m & ((1ull << lane) - 1ull))] = b + k * kWave + lane;
+            at += __popcll(m);
+        }
     __syncthreads();
     const int sub = wid * RPW + lane / G;
     for (int32_t slab = 0; slab < units; slab += G) {
@@ -259,8 +265,8 @@ __global__ void __launch_bounds__(256) k_embedding_grad_few(const u32x4e *__rest
 // Stable radix sort of (id, position), digits of at most 10 bits, least
 // significant first.  A tile is kSortThreads * iters pairs; there are at most
 // kSortTiles tiles, so every scatter workgroup adds up all tiles' digit counts by
-// itself and a pass is one launch: it also counts the next pass's digits by
-// output tile.  Ids outside [0, n_rows) become n_rows and sort to the end.
+// itself: a pass is two launches.  (Counting the next pass's digits from the scatter, with global additions, is one
+// launch less, but popular ids meet at a few counters: 55 us where the two launches take 25.)  Ids outside [0, n_rows) become n_rows and sort to the end.
 namespace {
 
 constexpr int kIdThreads = 1024;
@@ -290,10 +296,12 @@ __device__ __forceinline__ uint32_t sort_key(int32_t id, int64_t n_rows) {
 
 }  // namespace
 
-__global__ void __launch_bounds__(kIdThreads) k_id_first(const int32_t *__restrict__ ids,
+// Digit counts of a pass; in the first one (ids as given), workgroups past the tiles clear the flags.
+template <bool FIRST>
+__global__ void __launch_bounds__(kIdThreads) k_id_count(const int32_t *__restrict__ keys,
                                                          const int32_t *__restrict__ n_dev, int64_t n, int64_t n_rows,
-                                                         int bits, int iters, int32_t *__restrict__ hist,
-                                                         int64_t tiles, int64_t zeros, uint32_t *__restrict__ flags,
+                                                         int shift, int bits, int iters, int32_t *__restrict__ hist,
+                                                         int64_t tiles, uint32_t *__restrict__ flags,
                                                          int64_t flag_words) {
     __shared__ int32_t h[1 << kMaxBits];
     if (n_dev) n = std::min<int64_t>(n, std::max<int32_t>(*n_dev, 0));
@@ -301,18 +309,17 @@ __global__ void __launch_bounds__(kIdThreads) k_id_first(const int32_t *__restri
     if (blockIdx.x < tiles) {
         h[threadIdx.x] = 0;
         __syncthreads();
+#pragma unroll 4
         for (int it = 0; it < iters; ++it) {
             const int64_t e = ((int64_t)blockIdx.x * iters + it) * kIdThreads + threadIdx.x;
-            if (e < n) atomicAdd(&h[sort_key(ids[e], n_rows) & (digits - 1)], 1);
+            if (e < n) atomicAdd(&h[((FIRST ? sort_key(keys[e], n_rows) : (uint32_t)keys[e]) >> shift) & (digits - 1)], 1);
         }
         __syncthreads();
         if (threadIdx.x < digits) hist[blockIdx.x * digits + threadIdx.x] = h[threadIdx.x];
         return;
     }
     const int64_t stride = (int64_t)(gridDim.x - tiles) * kIdThreads;
-    const int64_t first = (int64_t)(blockIdx.x - tiles) * kIdThreads + threadIdx.x;
-    for (int64_t i = first; i < zeros; i += stride) hist[tiles * digits + i] = 0;
-    for (int64_t i = first; i < flag_words; i += stride) flags[i] = 0;
+    for (int64_t i = (int64_t)(blockIdx.x - tiles) * kIdThreads + threadIdx.x; i < flag_words; i += stride) flags[i] = 0;
 }
 
 // flags (first pass only, nullable): a byte per row of the table, set where its id occurs.
@@ -324,26 +331,37 @@ __global__ void __launch_bounds__(kIdThreads) k_id_scatter(const int32_t *__rest
                                                            const int32_t *__restrict__ hist, int64_t tiles,
                                                            int32_t *__restrict__ keys_out,
                                                            int32_t *__restrict__ vals_out,
-                                                           int32_t *__restrict__ hist_next,
                                                            uint8_t *__restrict__ flags) {
     __shared__ int32_t run[1 << kMaxBits];
     __shared__ int32_t cnt[kIdWaves][1 << kMaxBits];
     __shared__ int32_t scratch[kIdWaves];
     if (n_dev) n = std::min<int64_t>(n, std::max<int32_t>(*n_dev, 0));
-    const int tile_bits = 31 - __builtin_clz(kIdThreads * iters);   // iters is a power of two
-    const int64_t base = (int64_t)blockIdx.x << tile_bits;
+    const int64_t base = (int64_t)blockIdx.x * kIdThreads * iters;
     if (base >= n) return;
     const int lane = lane_id(), wid = threadIdx.x / kWave, digits = 1 << bits;
+    // a digit's count in all tiles and in those before this one: the tiles dealt to the threads that share a digit
     int32_t all = 0, before = 0;
-    if ((int)threadIdx.x < digits) {
-#pragma unroll 8
-        for (int t = 0; t < (int)tiles; ++t) {
-            const int32_t c = hist[t * digits + threadIdx.x];
+    {
+        const int dgt = threadIdx.x & (digits - 1), first = threadIdx.x >> bits, step = kIdThreads >> bits;
+#pragma unroll 16
+        for (int t = first; t < (int)tiles; t += step) {
+            const int32_t c = hist[t * digits + dgt];
             all += c;
             before += t < (int)blockIdx.x ? c : 0;
         }
+        int32_t *sum = &cnt[0][0];
+        sum[2 * threadIdx.x] = all;
+        sum[2 * threadIdx.x + 1] = before;
+        __syncthreads();
+        for (int q = 1; q < step && (int)threadIdx.x < digits; ++q) {
+            all += sum[2 * (threadIdx.x + q * digits)];
+            before += sum[2 * (threadIdx.x + q * digits) + 1];
+        }
+        if ((int)threadIdx.x >= digits) all = before = 0;
+        __syncthreads();
+        if ((int)threadIdx.x < digits)
 #pragma unroll
-        for (int w = 0; w < kIdWaves; ++w) cnt[w][threadIdx.x] = 0;
+            for (int w = 0; w < kIdWaves; ++w) cnt[w][threadIdx.x] = 0;
     }
     int32_t total;
     const int32_t off = block_exclusive_sum<int32_t, kIdThreads>(all, scratch, total) + before;
@@ -390,12 +408,6 @@ __global__ void __launch_bounds__(kIdThreads) k_id_scatter(const int32_t *__rest
             const int32_t pos = cnt[wid][dg] + rank;
             keys_out[pos] = (int32_t)key;
             vals_out[pos] = val;
-            if (hist_next) {   // one addition for the lanes that share an output tile and a next digit
-                const int next = (int)(key >> (shift + bits)) & (digits - 1);
-                const int32_t slot = (pos >> tile_bits) * digits + next;
-                // lanes of one digit go to consecutive places: at most two tiles, many next digits
-                atomicAdd(&hist_next[slot], 1);
-            }
         }
         __syncthreads();
         if ((int)threadIdx.x < digits)
@@ -483,30 +495,39 @@ __global__ void __launch_bounds__(256) k_embedding_grad(const u32x4e *__restrict
             }
         }
     };
-    constexpr int U = 4;
+    constexpr int U = Q == 1 ? 8 : 4;   // rows in flight; their ids are read one round ahead
     int32_t cur = b < n ? keys[b] : -1;
     bool began = b < n && cur != before;
-    // the loop's trip count is the same for all lane groups of a wavefront
-    for (int i0 = 0; i0 < kStretch; i0 += U) {
-        int32_t key[U];
-        u32x4e x[U][Q];
+    int32_t key[U], row[U];
+    auto ids = [&](int i0) {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int64_t p = b + i0 + u;
             key[u] = p < e ? keys[p] : -1;
-            const int64_t row = p < e ? vals[p] : 0;
+            row[u] = p < e ? vals[p] : 0;
+        }
+    };
+    ids(0);
+    // the loop's trip count is the same for all lane groups of a wavefront
+    for (int i0 = 0; i0 < kStretch; i0 += U) {
+        u32x4e x[U][Q];
+        int32_t now[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            now[u] = key[u];
 #pragma unroll
             for (int q = 0; q < Q; ++q) {
                 x[u][q] = u32x4e{0, 0, 0, 0};
-                if (p < e && key[u] < n_rows && c0 + q * G < units) x[u][q] = dout[row * ld16 + c0 + q * G];
+                if (key[u] >= 0 && key[u] < n_rows && c0 + q * G < units) x[u][q] = dout[(int64_t)row[u] * ld16 + c0 + q * G];
             }
         }
+        if (i0 + U < kStretch) ids(i0 + U);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            if (key[u] < 0) continue;
-            if (key[u] != cur) {
+            if (now[u] < 0) continue;
+            if (now[u] != cur) {
                 flush(cur, began, true);
-                cur = key[u];
+                cur = now[u];
                 began = true;
 #pragma unroll
                 for (int q = 0; q < Q; ++q) acc[q].zero();
@@ -518,81 +539,109 @@ __global__ void __launch_bounds__(256) k_embedding_grad(const u32x4e *__restrict
     if (b < n) flush(cur, began, cur != after);
 }
 
-// Joins the parts of ids that span stretches: the workgroup of the stretch where
-// such an id begins adds that part and those of the stretches up to its last one,
-// in order, a quarter of them per wavefront.
+// Joins the parts of ids that span stretches: the part of the stretch where such
+// an id begins and those of the stretches up to its last one, in order.  A
+// wavefront takes a stretch; what goes on over more than kJoinLong others is left
+// to the whole workgroup, a sixteenth of the parts per wavefront.
+constexpr int kJoinWaves = 16, kJoinLong = 16;
+
 template <bool BF>
-__global__ void __launch_bounds__(256) k_embedding_grad_join(const int32_t *__restrict__ keys,
-                                                             const int32_t *__restrict__ n_dev, int64_t n,
-                                                             int32_t units, int64_t d, float scale, bool accumulate,
-                                                             u32x4e *__restrict__ dtable, int64_t n_rows,
-                                                             int64_t table_ld16, const float *__restrict__ part) {
+__global__ void __launch_bounds__(64 * kJoinWaves) k_embedding_grad_join(const int32_t *__restrict__ keys,
+                                                                         const int32_t *__restrict__ n_dev, int64_t n,
+                                                                         int32_t units, int64_t d, float scale,
+                                                                         bool accumulate, u32x4e *__restrict__ dtable,
+                                                                         int64_t n_rows, int64_t table_ld16,
+                                                                         const float *__restrict__ part) {
     constexpr int N = Unit<BF>::N;
-    __shared__ float sums[4][kWave][N];
+    __shared__ float sums[kJoinWaves][kWave][N];
+    __shared__ int32_t s_rest[kJoinWaves];
     if (n_dev) n = std::min<int64_t>(n, std::max<int32_t>(*n_dev, 0));
     const int lane = lane_id(), wid = threadIdx.x / kWave;
     const int64_t padded = (int64_t)units * N;
-    for (int64_t st = blockIdx.x; (st + 1) * kStretch < n; st += gridDim.x) {
-        const int64_t b = st * kStretch, e = b + kStretch;
-        const int32_t id = keys[e - 1];
-        if (id >= n_rows || keys[e] != id) continue;                  // ends here
-        if (keys[b] == id && b > 0 && keys[b - 1] == id) continue;    // began earlier
-        int64_t lo = e, hi = n;                                       // first pair past the id
-        while (lo < hi) {
-            const int64_t mid = (lo + hi) >> 1;
-            if (keys[mid] <= id) lo = mid + 1;
-            else hi = mid;
+    // parts [k0, k1) of those after stretch st, unit c; the stretch's own first if `first`
+    auto add = [&](float (&acc)[N], int64_t st, int64_t k0, int64_t k1, int32_t c, bool first) {
+        const float *at = part + (int64_t)c * N;
+#pragma unroll
+        for (int x = 0; x < N; ++x) acc[x] = first ? at[(2 * st + 1) * padded + x] : 0.f;
+        int64_t k = k0;
+        for (; k + 4 <= k1; k += 4) {
+            f32x4e v[4][N / 4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+#pragma unroll
+                for (int x = 0; x < N / 4; ++x) v[u][x] = *(const f32x4e *)(at + 2 * (st + 1 + k + u) * padded + 4 * x);
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+#pragma unroll
+                for (int x = 0; x < N; ++x) acc[x] += v[u][x / 4][x % 4];
         }
-        const int64_t rest = (lo - 1) / kStretch - st;                // stretches after this one
-        const int64_t quarter = (rest + 3) / 4;
-        const int64_t k0 = std::min(wid * quarter, rest), k1 = std::min(k0 + quarter, rest);
-        for (int32_t slab = 0; slab < units; slab += kWave) {
-            const int32_t c = slab + lane;
-            float acc[N];
+        for (; k < k1; ++k)
 #pragma unroll
-            for (int x = 0; x < N; ++x) acc[x] = 0.f;
-            if (c < units) {
-                const float *at = part + (int64_t)c * N;
-                if (wid == 0) {
+            for (int x = 0; x < N; ++x) acc[x] += at[2 * (st + 1 + k) * padded + x];
+    };
+    auto put = [&](const float (&acc)[N], int32_t id, int32_t c) {
+        u32x4e *to = dtable + (int64_t)id * table_ld16 + c;
+        Unit<BF> o;
+        o.zero();
+        if (accumulate) o.from(*to);
 #pragma unroll
-                    for (int x = 0; x < N; ++x) acc[x] = at[(2 * st + 1) * padded + x];
+        for (int x = 0; x < N; ++x) o.v[x] += scale * acc[x];
+        *to = o.to((int64_t)c * N, d);
+    };
+    for (int64_t base = (int64_t)blockIdx.x * kJoinWaves; (base + 1) * kStretch < n; base += (int64_t)gridDim.x * kJoinWaves) {
+        const int64_t st = base + wid, b = st * kStretch, e = b + kStretch;
+        int32_t rest = 0;   // stretches after this one that the id goes on in
+        if (e < n) {
+            const int32_t id = keys[e - 1];
+            const bool begins = !(keys[b] == id && b > 0 && keys[b - 1] == id);
+            if (id < n_rows && begins && keys[e] == id)
+                for (;;) {
+                    const int64_t p = (st + 1 + rest + lane) * kStretch;
+                    const uint64_t on = __ballot(p < n && keys[p < n ? p : n - 1] == id);
+                    if (on != ~0ull) {
+                        rest += __builtin_ctzll(~on);
+                        break;
+                    }
+                    rest += kWave;
                 }
-                int64_t k = k0;
-                for (; k + 8 <= k1; k += 8) {
-                    f32x4e v[8][N / 4];
-#pragma unroll
-                    for (int u = 0; u < 8; ++u)
-#pragma unroll
-                        for (int x = 0; x < N / 4; ++x) v[u][x] = *(const f32x4e *)(at + 2 * (st + 1 + k + u) * padded + 4 * x);
-#pragma unroll
-                    for (int u = 0; u < 8; ++u)
-#pragma unroll
-                        for (int x = 0; x < N; ++x) acc[x] += v[u][x / 4][x % 4];
-                }
-                for (; k < k1; ++k)
-#pragma unroll
-                    for (int x = 0; x < N; ++x) acc[x] += at[2 * (st + 1 + k) * padded + x];
+        }
+        if (lane == 0) s_rest[wid] = rest > kJoinLong ? rest : 0;
+        if (rest > 0 && rest <= kJoinLong)
+            for (int32_t c = lane; c < units; c += kWave) {
+                float acc[N];
+                add(acc, st, 0, rest, c, true);
+                put(acc, keys[e - 1], c);
             }
-            __syncthreads();
+        __syncthreads();
+        for (int w = 0; w < kJoinWaves; ++w) {
+            const int32_t all = s_rest[w];
+            if (all == 0) continue;
+            const int64_t from = base + w, share = (all + kJoinWaves - 1) / kJoinWaves;
+            const int64_t k0 = std::min<int64_t>(wid * share, all), k1 = std::min<int64_t>(k0 + share, all);
+            for (int32_t slab = 0; slab < units; slab += kWave) {
+                const int32_t c = slab + lane;
+                float acc[N];
+                if (c < units) {
+                    add(acc, from, k0, k1, c, wid == 0);
 #pragma unroll
-            for (int x = 0; x < N; ++x) sums[wid][lane][x] = acc[x];
-            __syncthreads();
-            if (wid == 0 && c < units) {
-                u32x4e *to = dtable + (int64_t)id * table_ld16 + c;
-                Unit<BF> o;
-                o.zero();
-                if (accumulate) o.from(*to);
+                    for (int x = 0; x < N; ++x) sums[wid][lane][x] = acc[x];
+                }
+                __syncthreads();
+                if (wid == 0 && c < units) {
+                    for (int v = 1; v < kJoinWaves; ++v)
 #pragma unroll
-                for (int x = 0; x < N; ++x)
-                    o.v[x] += scale * ((sums[0][lane][x] + sums[1][lane][x]) + (sums[2][lane][x] + sums[3][lane][x]));
-                *to = o.to((int64_t)c * N, d);
+                        for (int x = 0; x < N; ++x) acc[x] += sums[v][lane][x];
+                    put(acc, keys[(from + 1) * kStretch - 1], c);
+                }
+                __syncthreads();
             }
         }
+        __syncthreads();
     }
 }
 
 namespace {
-// Workspace of the gradient: two (id, position) lists, the digit counts of every
+// Workspace of the gradient: two (id, position) lists, the digit counts of a
 // pass, a byte per table row, the part sums.
 struct GradWorkspace {
     size_t keys[2], vals[2], hist, flags, part, total;
@@ -609,7 +658,7 @@ struct GradWorkspace {
             keys[k] = take((size_t)n * 4);
             vals[k] = take((size_t)n * 4);
         }
-        hist = take((size_t)(p.passes * p.tiles * p.digits()) * 4);
+        hist = take((size_t)(p.tiles * p.digits()) * 4);
         flags = take((size_t)n_rows);
         part = take((size_t)(2 * ((n + kStretch - 1) / kStretch) * padded) * 4);
         total = at;
@@ -668,21 +717,22 @@ void launch_embedding_backward(const void *dout, int64_t ld_bytes, const int32_t
     const int32_t *kin = ids, *vin = nullptr;
     {
         KernelTimer t("embedding_sort", s);
-        const int64_t zeros = (p.passes - 1) * p.tiles * p.digits(), words = accumulate ? 0 : (n_rows + 3) / 4;
-        hipLaunchKernelGGL(k_id_first, dim3((unsigned)p.tiles + grid_for(std::max(zeros, words), kIdThreads, 256)),
-                           dim3(kIdThreads), 0, s, ids, n_dev, n, n_rows, p.bits, p.iters, hist, p.tiles, zeros,
-                           (uint32_t *)flags, words);
+        const int64_t words = accumulate ? 0 : (n_rows + 3) / 4;
         for (int k = 0; k < p.passes; ++k) {
             int32_t *kout = i32(w.keys[k & 1]), *vout = i32(w.vals[k & 1]);
-            const int32_t *h = hist + k * p.tiles * p.digits();
-            int32_t *next = k + 1 < p.passes ? hist + (k + 1) * p.tiles * p.digits() : nullptr;
-            if (k == 0)
-                hipLaunchKernelGGL(k_id_scatter<true>, dim3((unsigned)p.tiles), dim3(kIdThreads), 0, s, kin, vin,
-                                   n_dev, n, n_rows, 0, p.bits, p.iters, h, p.tiles, kout, vout, next, flags);
-            else
-                hipLaunchKernelGGL(k_id_scatter<false>, dim3((unsigned)p.tiles), dim3(kIdThreads), 0, s, kin, vin,
-                                   n_dev, n, n_rows, k * p.bits, p.bits, p.iters, h, p.tiles, kout, vout, next,
-                                   nullptr);
+            const int shift = k * p.bits;
+            if (k == 0) {
+                hipLaunchKernelGGL(k_id_count<true>, dim3((unsigned)p.tiles + (words ? grid_for(words, kIdThreads, 256) : 0)),
+                                   dim3(kIdThreads), 0, s, kin, n_dev, n, n_rows, shift, p.bits, p.iters, hist, p.tiles,
+                                   (uint32_t *)flags, words);
+                hipLaunchKernelGGL(k_id_scatter<true>, dim3((unsigned)p.tiles), dim3(kIdThreads), 0, s, kin, vin, n_dev,
+                                   n, n_rows, shift, p.bits, p.iters, hist, p.tiles, kout, vout, flags);
+            } else {
+                hipLaunchKernelGGL(k_id_count<false>, dim3((unsigned)p.tiles), dim3(kIdThreads), 0, s, kin, n_dev, n,
+                                   n_rows, shift, p.bits, p.iters, hist, p.tiles, nullptr, 0);
+                hipLaunchKernelGGL(k_id_scatter<false>, dim3((unsigned)p.tiles), dim3(kIdThreads), 0, s, kin, vin, n_dev,
+                                   n, n_rows, shift, p.bits, p.iters, hist, p.tiles, kout, vout, nullptr);
+            }
             kin = kout;
             vin = vout;
         }
@@ -723,12 +773,12 @@ void launch_embedding_backward(const void *dout, int64_t ld_bytes, const int32_t
     }
     {
         KernelTimer t("embedding_grad_join", s);
-        const unsigned grid = grid_for((n + kStretch - 1) / kStretch, 1, 8192);
+        const unsigned grid = grid_for((n + kStretch - 1) / kStretch, kJoinWaves, 2048);
         if (bf16)
-            hipLaunchKernelGGL(k_embedding_grad_join<true>, dim3(grid), dim3(256), 0, s, kin, n_dev, n, units, d,
+            hipLaunchKernelGGL(k_embedding_grad_join<true>, dim3(grid), dim3(64 * kJoinWaves), 0, s, kin, n_dev, n, units, d,
                                scale, accumulate, out, n_rows, tld16, part);
         else
-            hipLaunchKernelGGL(k_embedding_grad_join<false>, dim3(grid), dim3(256), 0, s, kin, n_dev, n, units, d,
+            hipLaunchKernelGGL(k_embedding_grad_join<false>, dim3(grid), dim3(64 * kJoinWaves), 0, s, kin, n_dev, n, units, d,
                                scale, accumulate, out, n_rows, tld16, part);
     }
     GNNAV_HIP(hipGetLastError());

@@ -40,7 +40,8 @@ typedef uint32_t u32x4x __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2x __attribute__((ext_vector_type(2)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 
-constexpr int kVTile = 256;              // classes of a logit tile
+constexpr int kVTile = 128;    // classes of a logit tile
+constexpr int kPiece = 256;    // pieces of the classes are multiples of this, a whole number of any product's tiles
 constexpr float kLog2e = 1.44269504088896340736f;
 
 // Two values rounded to bf16, nearest even.
@@ -178,6 +179,80 @@ __device__ __forceinline__ bool tile_of(const XentArgs &a, int32_t id, int32_t &
     nt = r / wide;
     mt = g * kGroup + r - nt * wide;
     return true;
+}
+
+// Block (i, j), register r of a lane of a product: M index 32 i + 8 (r / 4) + 4 (lane / 32) + r % 4, N index 32 j + lane % 32.
+
+// A row's label among the 32 WMF classes from mw of the piece on, -1 if it is none of them.
+template <int WMF>
+__device__ __forceinline__ int label_place(const XentArgs &a, int64_t n, int64_t mw) {
+    const int64_t y = (n < a.m ? a.labels[n] : -1) - (a.v0 + mw);
+    return y >= 0 && y < 32 * WMF ? (int)y : -1;
+}
+
+// Largest logit and sum of exponentials of the workgroup's classes, for each of its rows.
+template <int PL, int WMF, int WNF, int WGM, int WGN>
+__device__ __forceinline__ void stats_of(const XentArgs &a, f32x16x (&acc)[WMF][WNF], int64_t mt, int64_t n0, float2 *red) {
+    constexpr int BM = 32 * WMF * WGM, BN = 32 * WNF * WGN;
+    static_assert(BM == kVTile, "one entry per tile of classes");
+    const int tid = threadIdx.x, lane = tid & 63, wid = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wm = wid / WGN, wn = wid % WGN, h = lane >> 5, lr = lane & 31;
+    const int64_t m0 = mt * BM, mw = m0 + wm * (32 * WMF), nw = n0 + wn * (32 * WNF);
+    const bool tail = a.v0 + m0 + BM > a.n_classes;
+    float2 mine[WNF];
+#pragma unroll
+    for (int j = 0; j < WNF; ++j) {
+        const int64_t n = nw + 32 * j + lr;
+        const int y = label_place<WMF>(a, n, mw);
+        if (tail)
+#pragma unroll
+            for (int i = 0; i < WMF; ++i)
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    if (a.v0 + mw + 32 * i + 8 * (r / 4) + 4 * h + r % 4 >= a.n_classes) acc[i][j][r] = -INFINITY;
+        float mx = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < WMF; ++i)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) mx = fmaxf(mx, acc[i][j][r]);
+        if (y >= 0) {
+#pragma unroll
+            for (int i = 0; i < WMF; ++i)
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    if (y == 32 * i + 8 * (r / 4) + 4 * h + r % 4) a.label_logit[n] = acc[i][j][r];
+        }
+        mx = fmaxf(mx, __shfl_xor(mx, 32, kWave));
+        // a row whose classes here are all -inf has the sum 0: any finite reference does
+        const float ref = mx == -INFINITY ? 0.f : mx;
+        float s = 0.f;
+#pragma unroll
+        for (int i = 0; i < WMF; ++i)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                // (the difference first: of huge logits a product's rounding alone would overflow)
+                if constexpr (PL == 1) s += __builtin_amdgcn_exp2f((acc[i][j][r] - ref) * kLog2e);
+                else s += expf(acc[i][j][r] - ref);
+            }
+        s += __shfl_xor(s, 32, kWave);
+        mine[j] = make_float2(mx, s);
+    }
+#pragma unroll
+    for (int j = 0; j < WNF; ++j)
+        if (h == 0) red[wm * BN + wn * (32 * WNF) + 32 * j + lr] = mine[j];
+    __syncthreads();
+    for (int c = tid; c < BN; c += 64 * WGM * WGN) {
+        float mx = red[c].x;
+#pragma unroll
+        for (int w = 1; w < WGM; ++w) mx = fmaxf(mx, red[w * BN + c].x);
+        float s = 0.f;
+#pragma unroll
+        for (int w = 0; w < WGM; ++w) {
+            const float2 o = red[w * BN + c];
+            s += o.x == -INFINITY ? o.y : o.y * expf(o.x - mx);
+        }
+        a.stats[(a.v0 / kVTile + mt) * a.rows + n0 + c] = make_float2(mx, s);
+    }
 }
 
 // AT, BT: the operand's rows are summed over.
@@ -338,76 +413,16 @@ __device__ __forceinline__ void xent_tile(const XentArgs &a, int32_t id, u32x4x 
         }
     }
 
-    // block (i, j), register r of a lane: M index 32 i + 8 (r / 4) + 4 h + r % 4, N index 32 j + lane % 32
     const int64_t mw = m0 + wm * (32 * WMF), nw = n0 + wn * (32 * WNF);
-    // a row's label among this wavefront's classes, -1 if it is none of them
-    auto label_place = [&](int64_t n) {
-        const int64_t y = (n < a.m ? a.labels[n] : -1) - (a.v0 + mw);
-        return y >= 0 && y < 32 * WMF ? (int)y : -1;
-    };
     if constexpr (EPI == kStats) {
-        const bool tail = a.v0 + m0 + BM > a.n_classes;
-        float2 mine[WNF];
-#pragma unroll
-        for (int j = 0; j < WNF; ++j) {
-            const int64_t n = nw + 32 * j + lr;
-            const int y = label_place(n);
-            if (tail)
-#pragma unroll
-                for (int i = 0; i < WMF; ++i)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r)
-                        if (a.v0 + mw + 32 * i + 8 * (r / 4) + 4 * h + r % 4 >= a.n_classes) acc[i][j][r] = -INFINITY;
-            float mx = -INFINITY;
-#pragma unroll
-            for (int i = 0; i < WMF; ++i)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) mx = fmaxf(mx, acc[i][j][r]);
-            if (y >= 0) {
-#pragma unroll
-                for (int i = 0; i < WMF; ++i)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r)
-                        if (y == 32 * i + 8 * (r / 4) + 4 * h + r % 4) a.label_logit[n] = acc[i][j][r];
-            }
-            mx = fmaxf(mx, __shfl_xor(mx, 32, kWave));
-            // a row whose classes here are all -inf has the sum 0: any finite reference does
-            const float ref = mx == -INFINITY ? 0.f : mx;
-            float s = 0.f;
-#pragma unroll
-            for (int i = 0; i < WMF; ++i)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    // (the difference first: of huge logits a product's rounding alone would overflow)
-                    if constexpr (PL == 1) s += __builtin_amdgcn_exp2f((acc[i][j][r] - ref) * kLog2e);
-                    else s += expf(acc[i][j][r] - ref);
-                }
-            s += __shfl_xor(s, 32, kWave);
-            mine[j] = make_float2(mx, s);
-        }
-#pragma unroll
-        for (int j = 0; j < WNF; ++j)
-            if (h == 0) red[wm * BN + wn * (32 * WNF) + 32 * j + lr] = mine[j];
-        __syncthreads();
-        for (int c = tid; c < BN; c += 64 * NW) {
-            float mx = red[c].x;
-#pragma unroll
-            for (int w = 1; w < WGM; ++w) mx = fmaxf(mx, red[w * BN + c].x);
-            float s = 0.f;
-#pragma unroll
-            for (int w = 0; w < WGM; ++w) {
-                const float2 o = red[w * BN + c];
-                s += o.x == -INFINITY ? o.y : o.y * expf(o.x - mx);
-            }
-            a.stats[(a.v0 / kVTile + mt) * a.rows + n0 + c] = make_float2(mx, s);
-        }
+        stats_of<PL, WMF, WNF, WGM, WGN>(a, acc, mt, n0, red);
     } else if constexpr (EPI == kProb) {
         const bool tail = a.v0 + m0 + BM > a.n_classes;
 #pragma unroll
         for (int j = 0; j < WNF; ++j) {
             const int64_t n = nw + 32 * j + lr;
             const float lse = a.lse[n];
-            const int y = label_place(n);
+            const int y = label_place<WMF>(a, n, mw);
 #pragma unroll
             for (int i = 0; i < WMF; ++i)
 #pragma unroll
@@ -505,6 +520,67 @@ __global__ void __launch_bounds__(64 * WGM * WGN, 2) k_xent_logits(const XentArg
     xent_tile<PL, WMF, WNF, WGM, WGN, false, false, EPI>(a, blockIdx.x, S, red);
 }
 
+// The statistics for at most 32 rows: bound by reading w once, so it is read as it lies (row-major, into the
+// fragments), without the packing that the tiles above need.  A wavefront takes 32 classes.
+template <int PL>
+__global__ void __launch_bounds__(256) k_xent_score(const XentArgs a, const void *__restrict__ W, int64_t ld, int64_t d) {
+    __shared__ float2 red[4 * 32];
+    const int lane = threadIdx.x & 63, wid = threadIdx.x >> 6, h = lane >> 5, lr = lane & 31;
+    const int64_t v = std::min<int64_t>((int64_t)blockIdx.x * kVTile + 32 * wid + lr, a.n_classes - 1);
+    const uint16_t *w16 = (const uint16_t *)W + v * ld;
+    const float *w32 = (const float *)W + v * ld;
+    f32x16x acc[1][1];
+#pragma unroll
+    for (int r = 0; r < 16; ++r) acc[0][0][r] = 0.f;
+    // 16 columns a step, 8 of them this lane's; past d they count as zeros
+    constexpr int U = PL == 1 ? 8 : 4;   // steps in flight
+    for (int64_t k0 = 0; k0 < d; k0 += 16 * U) {
+        u32x4x x[U][PL == 1 ? 1 : 2], b[U][PL];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int64_t k = k0 + 16 * u + 8 * h, c = (k0 + 16 * u) / 8 + h;
+            const u32x4x zero = {0, 0, 0, 0};
+            if constexpr (PL == 1) {
+                x[u][0] = zero;
+                if (k < d) x[u][0] = *(const u32x4x *)(w16 + k);
+            } else {
+                x[u][0] = x[u][PL == 1 ? 0 : 1] = zero;
+                if (k < d) x[u][0] = *(const u32x4x *)(w32 + k);
+                if (k + 4 < d) x[u][PL == 1 ? 0 : 1] = *(const u32x4x *)(w32 + k + 4);
+            }
+#pragma unroll
+            for (int p = 0; p < PL; ++p) {
+                b[u][p] = zero;
+                if (k < d) b[u][p] = a.B[p * a.b_plane + c * a.b_rows + lr];
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int64_t k = k0 + 16 * u + 8 * h;
+            bf16x8 f[PL];
+            if constexpr (PL == 1) {
+                if (k + 8 > d)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        if (k + 2 * q + 1 >= d) x[u][0][q] &= 0xffffu;
+                        if (k + 2 * q >= d) x[u][0][q] = 0;
+                    }
+                f[0] = __builtin_bit_cast(bf16x8, x[u][0]);
+                acc[0][0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[0], __builtin_bit_cast(bf16x8, b[u][0]), acc[0][0], 0, 0, 0);
+            } else {
+                float y[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) y[e] = k + e < d ? __uint_as_float(x[u][PL == 1 ? 0 : e / 4][e % 4]) : 0.f;
+                split3(y, f[0], f[PL - 2], f[PL - 1]);
+                acc[0][0] = mfma_split6(f[0], f[PL - 2], f[PL - 1], __builtin_bit_cast(bf16x8, b[u][0]),
+                                        __builtin_bit_cast(bf16x8, b[u][PL - 2]), __builtin_bit_cast(bf16x8, b[u][PL - 1]),
+                                        acc[0][0]);
+            }
+        }
+    }
+    stats_of<PL, 1, 1, 4, 1>(a, acc, blockIdx.x, 0, red);
+}
+
 // A piece's dw and dh in one launch: the workgroups of dw (of the first `dw_ids`), then those of dh, fill
 // the units together.  dw's tiles are 32 x WMF x WGM by 32 x WNW x WGN, dh's 32 x WMF x WGM by 32 x WNH x WGN.
 template <int PL, int WMF, int WNW, int WNH, int WGM, int WGN, int WGMH, int WMFH>
@@ -518,64 +594,101 @@ __global__ void __launch_bounds__(64 * WGM * WGN, 2) k_xent_grads(const XentArgs
 }
 
 // ------------------------------------------------------------- rows and loss
-// Joins a row's tiles: lse (+inf for a row that does not count), the row's
-// loss.  32 rows a workgroup, the tiles dealt to 8 threads of each.
-__global__ void __launch_bounds__(256) k_xent_rows(const float2 *__restrict__ stats, int64_t tiles, int64_t rows,
-                                                   int64_t m, const int32_t *__restrict__ labels, int32_t ignore,
-                                                   int64_t n_classes, const float *__restrict__ label_logit,
-                                                   float *__restrict__ lse, float *__restrict__ losses,
-                                                   float *__restrict__ row_loss) {
-    __shared__ float2 part[8][32];
-    const int tid = threadIdx.x, c = tid & 31, k = tid >> 5;
-    const int64_t n = (int64_t)blockIdx.x * 32 + c;
-    float mx = -INFINITY, s = 0.f;
-    auto join = [&](float2 o) {
-        const float top = fmaxf(mx, o.x);
-        const float ref = top == -INFINITY ? 0.f : top;
-        s = s * expf(mx - ref) + (o.x == -INFINITY ? o.y : o.y * expf(o.x - ref));
-        mx = top;
-    };
-#pragma unroll 4
-    for (int64_t t = k; t < tiles; t += 8) join(stats[t * rows + n]);
-    part[k][c] = make_float2(mx, s);
-    __syncthreads();
-    if (k > 0) return;
-    for (int w = 1; w < 8; ++w) join(part[w][c]);
-    const int32_t y = n < m ? labels[n] : ignore;
-    const bool out = n >= m || y == ignore, bad = !out && (y < 0 || y >= n_classes);
-    const float top = mx + logf(s);
-    lse[n] = out || bad ? INFINITY : top;
-    const float loss = out ? 0.f : bad ? NAN : logf(s) + (mx - label_logit[n]);
-    losses[n] = loss;
-    if (row_loss && n < m) row_loss[n] = loss;
-}
-
-// The mean over the rows that count, in 64 bits and a fixed order, and its weight.
-__global__ void __launch_bounds__(256) k_xent_loss(const float *__restrict__ losses, int64_t m,
-                                                   const int32_t *__restrict__ labels, int32_t ignore,
-                                                   float *__restrict__ loss, float *__restrict__ inv_count) {
-    __shared__ double part[256];
-    __shared__ int64_t count[256];
+// The mean over the rows that count, in 64 bits and a fixed order, and its weight.  Run by one workgroup.
+template <int THREADS>
+__device__ __forceinline__ void xent_loss(const float *losses, int64_t m, const int32_t *labels, int32_t ignore,
+                                          float *loss, float *inv_count) {
+    __shared__ double part[THREADS / kWave];
+    __shared__ int32_t count[THREADS / kWave];
     double s = 0.0;
-    int64_t k = 0;
-    for (int64_t i = threadIdx.x; i < m; i += 256) {
+    int32_t k = 0;
+#pragma unroll 4
+    for (int64_t i = threadIdx.x; i < m; i += THREADS) {
         s += (double)losses[i];
         k += labels[i] != ignore;
     }
-    part[threadIdx.x] = s;
-    count[threadIdx.x] = k;
+#pragma unroll
+    for (int o = kWave / 2; o > 0; o >>= 1) {
+        s += __shfl_xor(s, o, kWave);
+        k += __shfl_xor(k, o, kWave);
+    }
+    if (lane_id() == 0) {
+        part[threadIdx.x / kWave] = s;
+        count[threadIdx.x / kWave] = k;
+    }
     __syncthreads();
-    for (int w = 128; w > 0; w >>= 1) {
-        if ((int)threadIdx.x < w) {
-            part[threadIdx.x] += part[threadIdx.x + w];
-            count[threadIdx.x] += count[threadIdx.x + w];
+    if (threadIdx.x == 0) {
+        for (int w = 1; w < THREADS / kWave; ++w) {
+            s += part[w];
+            k += count[w];
+        }
+        loss[0] = k > 0 ? (float)(s / (double)k) : 0.f;
+        inv_count[0] = k > 0 ? (float)(1.0 / (double)k) : 0.f;
+    }
+}
+
+// Joins a row's tiles: lse (+inf for a row that does not count), the row's
+// loss.  ROWS rows a workgroup, the tiles dealt to SLICES threads of each.  LOSS: there is
+// one workgroup, which takes the mean too.
+template <int ROWS, int SLICES, bool LOSS>
+__global__ void __launch_bounds__(ROWS * SLICES) k_xent_rows(const float2 *__restrict__ stats, int64_t tiles, int64_t rows,
+                                                             int64_t m, const int32_t *__restrict__ labels,
+                                                             int32_t ignore, int64_t n_classes,
+                                                             const float *__restrict__ label_logit,
+                                                             float *__restrict__ lse, float *losses,
+                                                             float *__restrict__ row_loss, float *loss,
+                                                             float *inv_count) {
+    __shared__ float2 part[SLICES][ROWS];
+    const int tid = threadIdx.x, c = tid % ROWS, k = tid / ROWS;
+    const int64_t n = (int64_t)blockIdx.x * ROWS + c;
+    float mx = -INFINITY, s = 0.f;
+    // (a tile whose logits are all -inf has the sum 0, or NaN, with no reference)
+    auto join = [&](const float2 *o, int count) {
+        float top = mx;
+        for (int q = 0; q < count; ++q) top = fmaxf(top, o[q].x);
+        const float ref = top == -INFINITY ? 0.f : top;
+        s *= expf(mx - ref);
+        for (int q = 0; q < count; ++q) s += o[q].x == -INFINITY ? o[q].y : o[q].y * expf(o[q].x - ref);
+        mx = top;
+    };
+    int64_t t = k;
+    for (; t + 7 * SLICES < tiles; t += 8 * SLICES) {
+        float2 o[8];
+#pragma unroll
+        for (int q = 0; q < 8; ++q) o[q] = stats[(t + q * SLICES) * rows + n];
+        join(o, 8);
+    }
+    for (; t < tiles; t += SLICES) {
+        const float2 o = stats[t * rows + n];
+        join(&o, 1);
+    }
+    part[k][c] = make_float2(mx, s);
+    __syncthreads();
+    for (int w = SLICES / 2; w > 0; w >>= 1) {
+        if (k < w) {
+            join(&part[k + w][c], 1);
+            part[k][c] = make_float2(mx, s);
         }
         __syncthreads();
     }
-    if (threadIdx.x == 0) {
-        loss[0] = count[0] > 0 ? (float)(part[0] / (double)count[0]) : 0.f;
-        inv_count[0] = count[0] > 0 ? (float)(1.0 / (double)count[0]) : 0.f;
+    if (k == 0) {
+        const int32_t y = n < m ? labels[n] : ignore;
+        const bool out = n >= m || y == ignore, bad = !out && (y < 0 || y >= n_classes);
+        lse[n] = out || bad ? INFINITY : mx + logf(s);
+        const float one = out ? 0.f : bad ? NAN : logf(s) + (mx - label_logit[n]);
+        losses[n] = one;
+        if (row_loss && n < m) row_loss[n] = one;
     }
+    if constexpr (LOSS) {
+        __syncthreads();
+        xent_loss<ROWS * SLICES>(losses, m, labels, ignore, loss, inv_count);
+    }
+}
+
+__global__ void __launch_bounds__(1024) k_xent_loss(const float *__restrict__ losses, int64_t m,
+                                                    const int32_t *__restrict__ labels, int32_t ignore,
+                                                    float *__restrict__ loss, float *__restrict__ inv_count) {
+    xent_loss<1024>(losses, m, labels, ignore, loss, inv_count);
 }
 
 // dh from the splits' parts, in the order the products kept them in.
@@ -635,23 +748,22 @@ struct XentPlan {
     XentPlan(int64_t m, int64_t n_classes, int64_t d, bool bf16, bool grads, bool dh) {
         pl = bf16 ? 1 : 3;
         bk = bf16 ? 32 : 16;
-        if (d <= 64 && m > 32) bm = 64;
-        else bm = bf16 && up(d, 256) * 10 <= up(d, 128) * 11 ? 256 : 128;
-        ln = rn = m <= 32 ? 32 : 128;
-        if (bf16 && bm == 256 && m > 128) {
-            rn = 256;
-            if (d >= 512) ln = 256;
-        }
+        // Gradient tiles of 256 x 256 where the columns fill them: 4,093 x 169,000 x 256 bf16 2,093 us in all (256 x 128: 2,178,
+        // 128 x 128: 2,303), 8,192 x 65,536 x 1,024 4,105 (4,200, 4,435).
+        const bool big = bf16 && m > 128 && d > 128 && up(d, 256) * 10 <= up(d, 128) * 11;
+        ln = m <= 32 ? 32 : 128;
+        rn = big ? 256 : ln;
+        bm = big ? 256 : d <= 64 && rn == 128 ? 64 : 128;
         rows = up(std::max<int64_t>(m, 1), grads ? rn : ln);
         width = up(d, grads ? bm : 64);
         chunks = width / 8;
-        const int64_t all = up(n_classes, kVTile);
+        const int64_t all = up(n_classes, kPiece);
         tiles = all / kVTile;
-        piece = std::max<int64_t>(kVTile, kWBytes / (width * 2 * pl) / kVTile * kVTile);
-        if (grads) piece = std::min(piece, std::max<int64_t>(kVTile, kPBytes / (rows * 2 * pl) / kVTile * kVTile));
+        piece = std::max<int64_t>(kPiece, kWBytes / (width * 2 * pl) / kPiece * kPiece);
+        if (grads) piece = std::min(piece, std::max<int64_t>(kPiece, kPBytes / (rows * 2 * pl) / kPiece * kPiece));
         piece = std::min(piece, all);
         const int64_t pieces = (all + piece - 1) / piece;
-        piece = up((all + pieces - 1) / pieces, kVTile);   // equal ones
+        piece = up((all + pieces - 1) / pieces, kPiece);   // equal ones
         splits = 1;
         split_steps = 0;
         if (dh) {
@@ -683,43 +795,36 @@ unsigned ids_of(const XentArgs &a) {   // workgroups of a product, whole rounds 
     return (unsigned)up((int64_t)a.m_tiles * a.n_tiles * a.splits, 8);
 }
 
-// Logit tiles: 256 classes x 128 rows (or 32); fp32 in 8 wavefronts where bf16 takes 4.
+// Logit tiles: 128 classes x 128 rows (or 32).  256 x 128 and, in 8 wavefronts, 256 x 256 tiles move less to LDS
+// but have fewer workgroups on a unit to fill each other's gaps (4,093 x 169,000 x 256 bf16: both
+// passes 609 us, 128 x 128 595; x 1,024 columns 2,118 and 2,145; fp32 1,024 rows 1,342 and 1,256).
 template <int PL, int EPI>
-void run_logits(XentArgs &a, int64_t rn, int64_t vdim, const char *label, hipStream_t s) {
+void run_logits(XentArgs &a, int64_t ln, int64_t vdim, const char *label, hipStream_t s) {
     a.m_tiles = (int32_t)(vdim / kVTile);
-    a.n_tiles = (int32_t)(a.rows / rn);
+    a.n_tiles = (int32_t)(a.rows / ln);
     a.splits = 1;
     KernelTimer t(label, s);
-    if (rn == 32)
-        hipLaunchKernelGGL((k_xent_logits<PL, 2, 1, 4, 1, EPI>), dim3(ids_of(a)), dim3(256), 0, s, a);
-    else if constexpr (PL == 1) {
-        if (rn == 256)
-            hipLaunchKernelGGL((k_xent_logits<PL, 4, 2, 2, 4, EPI>), dim3(ids_of(a)), dim3(512), 0, s, a);
-        else
-            hipLaunchKernelGGL((k_xent_logits<PL, 4, 2, 2, 2, EPI>), dim3(ids_of(a)), dim3(256), 0, s, a);
-    } else
-        hipLaunchKernelGGL((k_xent_logits<PL, 2, 2, 4, 2, EPI>), dim3(ids_of(a)), dim3(512), 0, s, a);
+    if constexpr (EPI == kProb)
+        if (ln == 32) {
+            hipLaunchKernelGGL((k_xent_logits<PL, 1, 1, 4, 1, EPI>), dim3(ids_of(a)), dim3(256), 0, s, a);
+            return;
+        }
+    hipLaunchKernelGGL((k_xent_logits<PL, 2, 2, 2, 2, EPI>), dim3(ids_of(a)), dim3(256), 0, s, a);
 }
 
-// Gradient tiles: bm features x 128 classes for dw, bm x rn rows for dh.  Either product may be absent (no tiles).
+// Gradient tiles: bm features x 128 classes for dw, bm x rn rows for dh (rn = 256: 256 x 256 both).  Either product
+// may be absent (no tiles).
 template <int PL>
 void run_grads(const XentArgs &w, const XentArgs &h, int64_t bm, int64_t rn, hipStream_t s) {
     KernelTimer t("xent_grads", s);
     const unsigned nw = w.m_tiles > 0 ? ids_of(w) : 0, nh = h.m_tiles > 0 ? ids_of(h) : 0;
 #define GNNAV_L(WMF, WNW, WNH, WGM, WGN, WGMH, WMFH)                                                                  \
-    hipLaunchKernelGGL((k_xent_grads<PL, WMF, WNW, WNH, WGM, WGN, WGMH, WMFH>), dim3(nw + nh),                           \
-                       dim3(64 * WGM * WGN), 0, s, w, h,                                                              \
-                       (int32_t)nw)
+    hipLaunchKernelGGL((k_xent_grads<PL, WMF, WNW, WNH, WGM, WGN, WGMH, WMFH>), dim3(nw + nh),                        \
+                       dim3(64 * WGM * WGN), 0, s, w, h, (int32_t)nw)
     if (rn == 32) {
-        if (bm == 256) {
-            if constexpr (PL == 1) GNNAV_L(4, 2, 1, 2, 2, 4, 2);
-        } else {
-            GNNAV_L(2, 2, 1, 2, 2, 4, 1);
-        }
+        GNNAV_L(2, 2, 1, 2, 2, 4, 1);
     } else if (rn == 256) {
         if constexpr (PL == 1) GNNAV_L(4, 2, 2, 2, 4, 2, 4);
-    } else if (bm == 256) {
-        if constexpr (PL == 1) GNNAV_L(4, 2, 2, 2, 2, 2, 4);
     } else if (bm == 128) {
         GNNAV_L(2, 2, 2, 2, 2, 2, 2);
     } else {
@@ -767,7 +872,14 @@ void xent(const XentPlan &p, const LinearXentArgs &x, hipStream_t s) {
     };
     const int64_t all = p.tiles * kVTile;
     bool packed = false;   // one piece: packed once for both passes
-    for (int64_t v0 = 0; v0 < all; v0 += p.piece) {
+    if (p.ln == 32) {
+        a.B = H;
+        a.b_rows = p.rows;
+        a.b_plane = p.chunks * p.rows;
+        KernelTimer t("xent_stats", s);
+        hipLaunchKernelGGL(k_xent_score<PL>, dim3((unsigned)p.tiles), dim3(256), 0, s, a, x.w, x.ld_w, x.d);
+    }
+    for (int64_t v0 = 0; v0 < all && p.ln > 32; v0 += p.piece) {
         const int64_t vp = std::min(p.piece, all - v0);
         pack_w(v0, vp);
         packed = vp == all;
@@ -776,9 +888,15 @@ void xent(const XentPlan &p, const LinearXentArgs &x, hipStream_t s) {
     }
     {
         KernelTimer t("xent_rows", s);
-        hipLaunchKernelGGL(k_xent_rows, dim3((unsigned)(p.rows / 32)), dim3(256), 0, s, a.stats, p.tiles, p.rows, x.m,
-                           x.labels, x.ignore, x.n_classes, a.label_logit, lse, losses, x.row_loss);
-        hipLaunchKernelGGL(k_xent_loss, dim3(1), dim3(256), 0, s, losses, x.m, x.labels, x.ignore, x.loss, inv);
+        if (p.rows == 32) {
+            hipLaunchKernelGGL((k_xent_rows<32, 32, true>), dim3(1), dim3(1024), 0, s, a.stats, p.tiles, p.rows, x.m,
+                               x.labels, x.ignore, x.n_classes, a.label_logit, lse, losses, x.row_loss, x.loss, inv);
+        } else {
+            hipLaunchKernelGGL((k_xent_rows<16, 16, false>), dim3((unsigned)(p.rows / 16)), dim3(256), 0, s, a.stats,
+                               p.tiles, p.rows, x.m, x.labels, x.ignore, x.n_classes, a.label_logit, lse, losses,
+                               x.row_loss, nullptr, nullptr);
+            hipLaunchKernelGGL(k_xent_loss, dim3(1), dim3(1024), 0, s, losses, x.m, x.labels, x.ignore, x.loss, inv);
+        }
     }
     if (x.dh || x.dw) {
         for (int64_t v0 = 0; v0 < all; v0 += p.piece) {
@@ -821,18 +939,10 @@ void xent(const XentPlan &p, const LinearXentArgs &x, hipStream_t s) {
 #define GNNAV_L(A, B, C, D)                                                                                          \
     hipLaunchKernelGGL((k_xent_dh<A, B, C, D>), dim3(grid), dim3(256), 0, s, part, total, p.splits, total, mt, x.m,   \
                        x.d, lse, inv, x.dh, x.ld_dh, BF)
-            if (p.rn == 32) {
-                if (p.bm == 256) GNNAV_L(2, 1, 4, 1);
-                else GNNAV_L(1, 1, 4, 1);
-            } else if (p.rn == 256) {
-                GNNAV_L(4, 2, 2, 4);
-            } else if (p.bm == 256) {
-                GNNAV_L(4, 2, 2, 2);
-            } else if (p.bm == 128) {
-                GNNAV_L(2, 2, 2, 2);
-            } else {
-                GNNAV_L(1, 2, 2, 2);
-            }
+            if (p.rn == 32) GNNAV_L(1, 1, 4, 1);
+            else if (p.rn == 256) GNNAV_L(4, 2, 2, 4);
+            else if (p.bm == 128) GNNAV_L(2, 2, 2, 2);
+            else GNNAV_L(1, 2, 2, 2);
 #undef GNNAV_L
         }
     }
