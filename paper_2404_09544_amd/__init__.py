@@ -493,36 +493,44 @@ def sage_forward(blocks: Blocks, x, weights, dims, dtype: str, logits, stream=No
 _TORCH_CODE = {torch.float32: F32, torch.bfloat16: BF16}
 
 
-def _rows(t, what: str, d: int = None, dtype=None):
-    """Checks a device matrix argument with contiguous columns (rows of any stride)."""
-    if t.dim() != 2 or not t.is_cuda or (t.shape[1] > 1 and t.stride(1) != 1):
-        raise ValueError(f"{what} must be a device matrix with contiguous columns")
-    if t.dtype not in _TORCH_CODE or (dtype is not None and t.dtype != dtype):
-        raise ValueError(f"{what} must be {dtype or 'float32 or bfloat16'}")
-    if d is not None and t.shape[1] != d:
-        raise ValueError(f"{what} must have {d} columns")
-    _here(t, what)
-    return t
+def _here() -> int:
+    """Index of the current device (a host tensor's is -1; before torch's first use of a device there are no others)."""
+    return torch._C._cuda_getDevice() if torch.cuda.is_initialized() else 0
 
 
-def _here(t, what: str):
-    if t.device.index != torch.cuda.current_device():
+def _on(stream, device: int) -> int:
+    """The call's stream as an address: the current stream of the device unless one is given."""
+    return torch._C._cuda_getCurrentRawStream(device) if stream is None else _stream(stream)
+
+
+def _rows(t, what: str, device: int, d=None, dtype=None):
+    """Checks a device matrix with contiguous columns (rows at any stride); its (rows, columns, stride)."""
+    if t.get_device() != device:
         raise ValueError(f"{what} is not on the current device")
+    shape, stride = t.shape, t.stride()
+    if len(shape) != 2 or (stride[1] != 1 and shape[1] > 1):
+        raise ValueError(f"{what} must be a matrix with contiguous columns")
+    if t.dtype is not dtype and (dtype is not None or t.dtype not in _TORCH_CODE):
+        raise ValueError(f"{what} must be {dtype or 'float32 or bfloat16'}")
+    if d is not None and shape[1] != d:
+        raise ValueError(f"{what} must have {d} columns")
+    return shape[0], shape[1], stride[0]
 
 
-def _vector(t, what: str, dtype, n: int = None):
-    if not t.is_cuda or t.dtype != dtype or not t.is_contiguous() or (n is not None and t.numel() < n):
-        raise ValueError(f"{what} must be a contiguous device {dtype} tensor" + (f" of {n}" if n is not None else ""))
-    _here(t, what)
-    return t
+def _vector(t, what: str, device: int, dtype, n: int = 0):
+    """Checks a contiguous device tensor of at least n elements; its address."""
+    if t.get_device() != device:
+        raise ValueError(f"{what} is not on the current device")
+    if t.dtype is not dtype or not t.is_contiguous() or t.numel() < n:
+        raise ValueError(f"{what} must be a contiguous {dtype} tensor of at least {n} elements")
+    return t.data_ptr()
 
 
-def _workspace(given, need: int, stream):
-    """(pointer, bytes, tensor that holds them) of a call's workspace; one that is not given comes
-    from torch's allocator, in the pool of the stream the call runs on."""
+def _workspace(given, need: int, device: int, stream):
+    """(address, bytes, tensor that holds them) of a call's workspace; one that is not given comes
+    from torch's allocator, in the pool of the stream that the call runs on."""
     if given is not None:
-        _vector(given, "workspace", torch.uint8)
-        return given.data_ptr(), given.numel(), given
+        return _vector(given, "workspace", device, torch.uint8), given.numel(), given
     if need == 0:
         return None, 0, None
     if stream is None:
@@ -534,22 +542,25 @@ def _workspace(given, need: int, stream):
     return t.data_ptr(), need, t
 
 
+def _workspace_bytes(n: int) -> int:
+    if n < 0:
+        raise GnnavError(1, "bad workspace arguments")
+    return int(n)
+
+
 def embedding(table, ids, out, scale: float = 1.0, n_ids_dev=None, stream=None):
-    """gnnav_embedding: out[i] = scale * table[ids[i]] for the table's type (fp32 or
+    """gnnav_embedding: out[i] = scale * table[ids[i]] in the table's type (fp32 or
     bf16); an id outside the table gives a zero row.  ids: device int32;
     n_ids_dev: optional device int32 tensor with the count of ids to take."""
-    d = _rows(table, "table").shape[1]
-    _rows(out, "out", d, table.dtype)
-    n = _vector(ids, "ids", torch.int32).numel()
-    if out.shape[0] < n:
+    dev, dt = _here(), table.dtype
+    rows, d, ld = _rows(table, "table", dev)
+    n_out, _, ld_out = _rows(out, "out", dev, d, dt)
+    n, ids_ptr = ids.numel(), _vector(ids, "ids", dev, torch.int32)
+    if n_out < n:
         raise ValueError("out has fewer rows than ids")
-    _check(_lib.gnnav_embedding(_dev_ptr(table), table.shape[0], table.stride(0), d, _TORCH_CODE[table.dtype],
-                                _dev_ptr(ids), _count_ptr(n_ids_dev), n, float(scale), _dev_ptr(out), out.stride(0),
-                                _stream(stream)))
-
-
-def _count_ptr(t):
-    return None if t is None else _vector(t, "n_ids_dev", torch.int32, 1).data_ptr()
+    count = None if n_ids_dev is None else _vector(n_ids_dev, "n_ids_dev", dev, torch.int32, 1)
+    _check(_lib.gnnav_embedding(table.data_ptr(), rows, ld, d, _TORCH_CODE[dt], ids_ptr, count, n, scale,
+                                out.data_ptr(), ld_out, _on(stream, dev)))
 
 
 def embedding_backward_workspace(n_ids: int, n_rows: int, d: int, dtype: str) -> int:
@@ -557,27 +568,20 @@ def embedding_backward_workspace(n_ids: int, n_rows: int, d: int, dtype: str) ->
     return _workspace_bytes(_lib.gnnav_embedding_backward_workspace(int(n_ids), int(n_rows), int(d), dtype_code(dtype)))
 
 
-def _workspace_bytes(n: int) -> int:
-    if n < 0:
-        raise GnnavError(1, "bad workspace arguments")
-    return int(n)
-
-
 def embedding_backward(dout, ids, dtable, scale: float = 1.0, accumulate: bool = False, n_ids_dev=None,
                        workspace=None, stream=None):
     """gnnav_embedding_backward: dtable[v] (+)= scale * the sum of the rows of dout whose id is v."""
-    d = _rows(dout, "dout").shape[1]
-    _rows(dtable, "dtable", d, dout.dtype)
-    n = _vector(ids, "ids", torch.int32).numel()
-    if dout.shape[0] < n:
+    dev, dt = _here(), dout.dtype
+    n_in, d, ld = _rows(dout, "dout", dev)
+    rows, _, ld_table = _rows(dtable, "dtable", dev, d, dt)
+    n, ids_ptr, code = ids.numel(), _vector(ids, "ids", dev, torch.int32), _TORCH_CODE[dt]
+    if n_in < n:
         raise ValueError("dout has fewer rows than ids")
-    code = _TORCH_CODE[dout.dtype]
-    need = 0 if workspace is not None else _workspace_bytes(
-        _lib.gnnav_embedding_backward_workspace(n, dtable.shape[0], d, code))
-    ws, ws_bytes, _hold = _workspace(workspace, need, stream)
-    _check(_lib.gnnav_embedding_backward(_dev_ptr(dout), dout.stride(0), _dev_ptr(ids), _count_ptr(n_ids_dev), n, d,
-                                         code, float(scale), int(bool(accumulate)), _dev_ptr(dtable),
-                                         dtable.shape[0], dtable.stride(0), ws, ws_bytes, _stream(stream)))
+    count = None if n_ids_dev is None else _vector(n_ids_dev, "n_ids_dev", dev, torch.int32, 1)
+    need = 0 if workspace is not None else _workspace_bytes(_lib.gnnav_embedding_backward_workspace(n, rows, d, code))
+    ws, ws_bytes, _hold = _workspace(workspace, need, dev, stream)
+    _check(_lib.gnnav_embedding_backward(dout.data_ptr(), ld, ids_ptr, count, n, d, code, scale, bool(accumulate),
+                                         dtable.data_ptr(), rows, ld_table, ws, ws_bytes, _on(stream, dev)))
 
 
 def linear_xent_workspace(m: int, n_classes: int, d: int, dtype: str, grads: bool = True) -> int:
@@ -592,28 +596,34 @@ def linear_xent(h, w, labels, loss, row_loss=None, dh=None, dw=None, ignore_labe
     [n_classes, d] without the logits.  loss: float32[1], the mean over the rows
     whose label is not ignore_label; row_loss (float32[m]), dh [m, d] and dw
     [n_classes, d] are written where given."""
-    m, d = _rows(h, "h").shape
-    _rows(w, "w", d, h.dtype)
-    _vector(labels, "labels", torch.int32, m)
-    _vector(loss, "loss", torch.float32, 1)
-    if row_loss is not None:
-        _vector(row_loss, "row_loss", torch.float32, m)
-    if dh is not None and _rows(dh, "dh", d, h.dtype).shape[0] < m:
-        raise ValueError("dh has fewer rows than h")
-    if dw is not None and _rows(dw, "dw", d, h.dtype).shape[0] < w.shape[0]:
-        raise ValueError("dw has fewer rows than w")
-    code = _TORCH_CODE[h.dtype]
+    dev, dt = _here(), h.dtype
+    m, d, ld_h = _rows(h, "h", dev)
+    v, _, ld_w = _rows(w, "w", dev, d, dt)
+    labels_ptr = _vector(labels, "labels", dev, torch.int32, m)
+    loss_ptr = _vector(loss, "loss", dev, torch.float32, 1)
+    row_ptr = None if row_loss is None else _vector(row_loss, "row_loss", dev, torch.float32, m)
+    dh_ptr = dw_ptr = None
+    ld_dh = ld_dw = 0
+    if dh is not None:
+        n, _, ld_dh = _rows(dh, "dh", dev, d, dt)
+        dh_ptr = dh.data_ptr()
+        if n < m:
+            raise ValueError("dh has fewer rows than h")
+    if dw is not None:
+        n, _, ld_dw = _rows(dw, "dw", dev, d, dt)
+        dw_ptr = dw.data_ptr()
+        if n < v:
+            raise ValueError("dw has fewer rows than w")
+    code = _TORCH_CODE[dt]
     need = 0 if workspace is not None else _workspace_bytes(
-        _lib.gnnav_linear_xent_workspace(m, w.shape[0], d, code, int(dh is not None or dw is not None)))
-    ws, ws_bytes, _hold = _workspace(workspace, need, stream)
-    _check(_lib.gnnav_linear_xent(_dev_ptr(h), h.stride(0), m, _dev_ptr(w), w.stride(0), w.shape[0], d, code,
-                                  _dev_ptr(labels), int(ignore_label), _dev_ptr(loss), _dev_ptr(row_loss),
-                                  _dev_ptr(dh), dh.stride(0) if dh is not None else 0, _dev_ptr(dw),
-                                  dw.stride(0) if dw is not None else 0, ws, ws_bytes, _stream(stream)))
+        _lib.gnnav_linear_xent_workspace(m, v, d, code, dh is not None or dw is not None))
+    ws, ws_bytes, _hold = _workspace(workspace, need, dev, stream)
+    _check(_lib.gnnav_linear_xent(h.data_ptr(), ld_h, m, w.data_ptr(), ld_w, v, d, code, labels_ptr, ignore_label,
+                                  loss_ptr, row_ptr, dh_ptr, ld_dh, dw_ptr, ld_dw, ws, ws_bytes, _on(stream, dev)))
 
 
 class TensorList:
-    """Contiguous device tensors of one type, with the pointer and count arrays
+    """Contiguous device tensors of one type, with the address and count arrays
     that the calls over many tensors take.  Holds the tensors."""
 
     def __init__(self, tensors):
@@ -621,58 +631,62 @@ class TensorList:
         types = {t.dtype for t in self.tensors} or {torch.float32}
         if len(types) > 1 or next(iter(types)) not in _TORCH_CODE:
             raise ValueError("tensors must be all float32 or all bfloat16")
+        self.device = self.tensors[0].get_device() if self.tensors else None
         for t in self.tensors:
-            if not t.is_cuda or not t.is_contiguous():
-                raise ValueError("tensors must be contiguous device tensors")
-            _here(t, "a tensor")
+            if t.get_device() < 0 or t.get_device() != self.device or not t.is_contiguous():
+                raise ValueError("tensors must be contiguous tensors of one device")
         self.code = _TORCH_CODE[next(iter(types))]
         self.n = len(self.tensors)
-        self.shapes = [t.numel() for t in self.tensors]
+        self.sizes = [t.numel() for t in self.tensors]
         self.ptrs = (P * max(self.n, 1))(*[t.data_ptr() for t in self.tensors])
-        self.counts = (i64 * max(self.n, 1))(*self.shapes)
+        self.counts = (i64 * max(self.n, 1))(*self.sizes)
 
 
-def _tensor_list(x) -> TensorList:
-    return x if isinstance(x, TensorList) else TensorList(x)
+def _tensor_list(x, device: int) -> TensorList:
+    x = x if isinstance(x, TensorList) else TensorList(x)
+    if x.device is not None and x.device != device:
+        raise ValueError("the tensors are not on the current device")
+    return x
 
 
 def _same(a: TensorList, b: TensorList, what: str):
-    if a.shapes != b.shapes or (a.n and a.code != b.code):
+    if a.sizes != b.sizes or (a.n and a.code != b.code):
         raise ValueError(f"{what} must match the gradients in number, sizes and type")
     return b
 
 
 def clip_workspace(grads) -> int:
-    """Bytes of workspace that grad_norm, clip_grads and sgd_clip_step need."""
-    return int(_lib.gnnav_clip_workspace(_tensor_list(grads).n))
+    """Bytes of workspace that grad_norm, clip_grads and sgd_clip_step need for these tensors."""
+    return int(_lib.gnnav_clip_workspace(grads.n if isinstance(grads, TensorList) else len(grads)))
+
+
+def _clip_args(grads, norm, workspace, stream):
+    dev = _here()
+    g = _tensor_list(grads, dev)
+    norm_ptr = _vector(norm, "norm", dev, torch.float32, 1)
+    return dev, g, norm_ptr, _workspace(workspace, 0 if workspace is not None else clip_workspace(g), dev, stream)
 
 
 def grad_norm(grads, norm, workspace=None, stream=None):
     """gnnav_grad_norm: norm[0] = the global 2-norm of the tensors (a list or a TensorList)."""
-    g = _tensor_list(grads)
-    _vector(norm, "norm", torch.float32, 1)
-    ws, ws_bytes, _hold = _workspace(workspace, clip_workspace(g), stream)
-    _check(_lib.gnnav_grad_norm(g.n, g.ptrs, g.counts, g.code, _dev_ptr(norm), ws, ws_bytes, _stream(stream)))
+    dev, g, norm_ptr, (ws, ws_bytes, _hold) = _clip_args(grads, norm, workspace, stream)
+    _check(_lib.gnnav_grad_norm(g.n, g.ptrs, g.counts, g.code, norm_ptr, ws, ws_bytes, _on(stream, dev)))
 
 
 def clip_grads(grads, max_norm: float, norm, out=None, workspace=None, stream=None):
     """gnnav_clip_grads: the tensors times min(1, max_norm / norm), in place or into `out`."""
-    g = _tensor_list(grads)
-    o = g if out is None else _same(g, _tensor_list(out), "out")
-    _vector(norm, "norm", torch.float32, 1)
-    ws, ws_bytes, _hold = _workspace(workspace, clip_workspace(g), stream)
-    _check(_lib.gnnav_clip_grads(g.n, g.ptrs, g.counts, g.code, float(max_norm), o.ptrs, _dev_ptr(norm), ws, ws_bytes,
-                                 _stream(stream)))
+    dev, g, norm_ptr, (ws, ws_bytes, _hold) = _clip_args(grads, norm, workspace, stream)
+    o = g if out is None else _same(g, _tensor_list(out, dev), "out")
+    _check(_lib.gnnav_clip_grads(g.n, g.ptrs, g.counts, g.code, max_norm, o.ptrs, norm_ptr, ws, ws_bytes,
+                                 _on(stream, dev)))
 
 
 def sgd_clip_step(weights, grads, lr: float, max_norm: float, norm, workspace=None, stream=None):
     """gnnav_sgd_clip_step: weights -= lr * min(1, max_norm / norm) * grads, in place."""
-    g = _tensor_list(grads)
-    w = _same(g, _tensor_list(weights), "weights")
-    _vector(norm, "norm", torch.float32, 1)
-    ws, ws_bytes, _hold = _workspace(workspace, clip_workspace(g), stream)
-    _check(_lib.gnnav_sgd_clip_step(g.n, w.ptrs, g.ptrs, g.counts, g.code, float(lr), float(max_norm), _dev_ptr(norm),
-                                    ws, ws_bytes, _stream(stream)))
+    dev, g, norm_ptr, (ws, ws_bytes, _hold) = _clip_args(grads, norm, workspace, stream)
+    w = _same(g, _tensor_list(weights, dev), "weights")
+    _check(_lib.gnnav_sgd_clip_step(g.n, w.ptrs, g.ptrs, g.counts, g.code, lr, max_norm, norm_ptr, ws, ws_bytes,
+                                    _on(stream, dev)))
 
 
 # -------------------------------------------------------------- profiling

@@ -542,8 +542,8 @@ __global__ void __launch_bounds__(256) k_embedding_grad(const u32x4e *__restrict
 // Joins the parts of ids that span stretches: the part of the stretch where such
 // an id begins and those of the stretches up to its last one, in order.  A
 // wavefront takes a stretch; what goes on over more than kJoinLong others is left
-// to the whole workgroup, a sixteenth of the parts per wavefront.
-constexpr int kJoinWaves = 16, kJoinLong = 16;
+// to the whole workgroup, an eighth of the parts per wavefront.
+constexpr int kJoinWaves = 8, kJoinLong = 16;
 
 template <bool BF>
 __global__ void __launch_bounds__(64 * kJoinWaves) k_embedding_grad_join(const int32_t *__restrict__ keys,
