@@ -165,7 +165,7 @@ __global__ void __launch_bounds__(256) k_embedding_grad_few(const u32x4e *__rest
     constexpr int RPW = kWave / G, PAR = 4 * RPW, N = Unit<BF>::N;
     __shared__ union {
         struct {
-            int32_t list[kFewIds];
+            uint16_t list[kFewIds];
             int32_t counts[4];
         } p;
         uint32_t marks[kMarkWords];
@@ -215,12 +215,29 @@ __global__ void __launch_bounds__(256) k_embedding_grad_few(const u32x4e *__rest
         at += w < wid ? sh.p.counts[w] : 0;
         total += sh.p.counts[w];
     }
+    auto put = [&](Unit<BF> &sum, int32_t c) {
+        Unit<BF> old;
+        u32x4e *to = dtable + (int64_t)id * table_ld16 + c;
+        old.zero();
+        if (accumulate) old.from(*to);
+#pragma unroll
+        for (int q = 0; q < N; ++q) sum.v[q] = old.v[q] + scale * sum.v[q];
+        *to = sum.to((int64_t)c * N, d);
+    };
+    if (total == 1) {   // most ids of a frontier
+        for (int32_t c = tid; c < units; c += 256) {
+            Unit<BF> x;
+            x.from(dout[(int64_t)p * ld16 + c]);
+            put(x, c);
+        }
+        return;
+    }
     if (mine > 0)
 #pragma unroll
         for (int k = 0; k < PER; ++k) {
             const bool hit = seen[k] == id;
             const uint64_t m = __ballot(hit);
-            if (hit) sh.p.list[at + __popcll(m & ((1ull << lane) - 1ull))] = b + k * kWave + lane;
+            if (hit) sh.p.list[at + __popcll(m & ((1ull << lane) - 1ull))] = (uint16_t)(b + k * kWave + lane);
             at += __popcll(m);
         }
     __syncthreads();
@@ -249,14 +266,10 @@ __global__ void __launch_bounds__(256) k_embedding_grad_few(const u32x4e *__rest
         for (int q = 0; q < N; ++q) part[wid][lane][q] = acc.v[q];
         __syncthreads();
         if (wid == 0 && lane < G && c < units) {
-            Unit<BF> old;
-            u32x4e *to = dtable + (int64_t)id * table_ld16 + c;
-            old.zero();
-            if (accumulate) old.from(*to);
 #pragma unroll
             for (int q = 0; q < N; ++q)
-                acc.v[q] = old.v[q] + scale * ((part[0][lane][q] + part[1][lane][q]) + (part[2][lane][q] + part[3][lane][q]));
-            *to = acc.to((int64_t)c * N, d);
+                acc.v[q] = (part[0][lane][q] + part[1][lane][q]) + (part[2][lane][q] + part[3][lane][q]);
+            put(acc, c);
         }
     }
 }
