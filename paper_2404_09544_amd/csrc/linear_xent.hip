@@ -43,12 +43,23 @@ typedef short s16x4 __attribute__((ext_vector_type(4)));
 constexpr int kVTile = 128;    // classes of a logit tile
 constexpr int kPiece = 256;    // pieces of the classes are multiples of this, a whole number of any product's tiles
 constexpr float kLog2e = 1.44269504088896340736f;
+// exp2(x log2e - r log2e) as one multiply-add errs by the rounding of r log2e, less than that of a logit of r's size;
+// past this the error would leave the exponent's range, and the difference is taken first.
+constexpr float kFmaRange = 65536.f;
 
 // Two values rounded to bf16, nearest even.
 __device__ __forceinline__ uint32_t bf16_pair(float lo, float hi) {
     typedef float f32x2 __attribute__((ext_vector_type(2)));
     typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
     return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{lo, hi}, bf16x2));
+}
+
+// Two groups of 4 values (as bf16 pairs) of a lane, of its row's classes c .. c + 3 and c + 8 .. c + 11, with those of
+// lane ^ 32, c + 4 .. and c + 12 ..: the chunk of 8 from c for the lower lanes, from c + 8 for the upper ones.
+__device__ __forceinline__ u32x4x join_chunk(uint32_t a0, uint32_t a1, uint32_t b0, uint32_t b1) {
+    const auto lo = __builtin_amdgcn_permlane32_swap(a0, b0, false, false);
+    const auto hi = __builtin_amdgcn_permlane32_swap(a1, b1, false, false);
+    return u32x4x{lo[0], hi[0], lo[1], hi[1]};
 }
 
 // What a row does: counted rows carry their lse, the others +inf, which makes
@@ -130,7 +141,8 @@ struct XentArgs {
     int64_t a_plane, b_plane;  // chunks of a plane
     int64_t k;                 // summed length, a multiple of the step
     int32_t m_tiles, n_tiles, splits;
-    int32_t split_steps;       // kDh: steps of one split
+    int32_t split_steps;       // kDh: steps of one split; k_xent_strip: tiles of a strip
+    int32_t strip0;            // k_xent_strip: the piece's first strip
     // kStats, kProb
     int64_t v0, n_classes;     // first class of the piece, classes in all
     int64_t rows;              // packed rows of h
@@ -183,11 +195,20 @@ __device__ __forceinline__ bool tile_of(const XentArgs &a, int32_t id, int32_t &
 
 // Block (i, j), register r of a lane of a product: M index 32 i + 8 (r / 4) + 4 (lane / 32) + r % 4, N index 32 j + lane % 32.
 
-// A row's label among the 32 WMF classes from mw of the piece on, -1 if it is none of them.
+// Less the lane's 4 (lane / 32): the same for every lane, so that what is compared with it is kept per lane and not these.
+__device__ __forceinline__ constexpr int place(int i, int r) { return 32 * i + 8 * (r / 4) + r % 4; }
+
+// The place of a row's label among the 32 WMF classes from mw of the piece on, below -4 if it is none of them.
 template <int WMF>
-__device__ __forceinline__ int label_place(const XentArgs &a, int64_t n, int64_t mw) {
+__device__ __forceinline__ int label_place(const XentArgs &a, int64_t n, int64_t mw, int h) {
     const int64_t y = (n < a.m ? a.labels[n] : -1) - (a.v0 + mw);
-    return y >= 0 && y < 32 * WMF ? (int)y : -1;
+    return y >= 0 && y < 32 * WMF ? (int)y - 4 * h : -64;
+}
+
+// The place past the last class, of 32 WMF ones from mw of the piece on.
+template <int WMF>
+__device__ __forceinline__ int live_classes(const XentArgs &a, int64_t mw, int h) {
+    return (int)std::max<int64_t>(std::min<int64_t>(a.n_classes - a.v0 - mw, 32 * WMF), 0) - 4 * h;
 }
 
 // Largest logit and sum of exponentials of the workgroup's classes, for each of its rows.
@@ -198,28 +219,29 @@ __device__ __forceinline__ void stats_of(const XentArgs &a, f32x16x (&acc)[WMF][
     const int wm = wid / WGN, wn = wid % WGN, h = lane >> 5, lr = lane & 31;
     const int64_t m0 = mt * BM, mw = m0 + wm * (32 * WMF), nw = n0 + wn * (32 * WNF);
     const bool tail = a.v0 + m0 + BM > a.n_classes;
+    const int live = live_classes<WMF>(a, mw, h);
     float2 mine[WNF];
 #pragma unroll
     for (int j = 0; j < WNF; ++j) {
         const int64_t n = nw + 32 * j + lr;
-        const int y = label_place<WMF>(a, n, mw);
+        const int y = label_place<WMF>(a, n, mw, h);
         if (tail)
 #pragma unroll
             for (int i = 0; i < WMF; ++i)
 #pragma unroll
                 for (int r = 0; r < 16; ++r)
-                    if (a.v0 + mw + 32 * i + 8 * (r / 4) + 4 * h + r % 4 >= a.n_classes) acc[i][j][r] = -INFINITY;
+                    if (place(i, r) >= live) acc[i][j][r] = -INFINITY;
         float mx = -INFINITY;
 #pragma unroll
         for (int i = 0; i < WMF; ++i)
 #pragma unroll
             for (int r = 0; r < 16; ++r) mx = fmaxf(mx, acc[i][j][r]);
-        if (y >= 0) {
+        if (y > -64) {
 #pragma unroll
             for (int i = 0; i < WMF; ++i)
 #pragma unroll
                 for (int r = 0; r < 16; ++r)
-                    if (y == 32 * i + 8 * (r / 4) + 4 * h + r % 4) a.label_logit[n] = acc[i][j][r];
+                    if (y == place(i, r)) a.label_logit[n] = acc[i][j][r];
         }
         mx = fmaxf(mx, __shfl_xor(mx, 32, kWave));
         // a row whose classes here are all -inf has the sum 0: any finite reference does
@@ -416,12 +438,14 @@ __device__ __forceinline__ void xent_tile(const XentArgs &a, int32_t id, u32x4x 
     if constexpr (EPI == kStats) {
         stats_of<PL, WMF, WNF, WGM, WGN>(a, acc, mt, n0, red);
     } else if constexpr (EPI == kProb) {
+        // (a row that does not count has the lse +inf, so its p is 0 where its logits, those of zeros, are finite)
         const bool tail = a.v0 + m0 + BM > a.n_classes;
+        const int live = live_classes<WMF>(a, mw, h);
 #pragma unroll
         for (int j = 0; j < WNF; ++j) {
             const int64_t n = nw + 32 * j + lr;
             const float lse = a.lse[n];
-            const int y = label_place<WMF>(a, n, mw);
+            const int y = label_place<WMF>(a, n, mw, h);
 #pragma unroll
             for (int i = 0; i < WMF; ++i)
 #pragma unroll
@@ -429,20 +453,18 @@ __device__ __forceinline__ void xent_tile(const XentArgs &a, int32_t id, u32x4x 
                     if constexpr (PL == 1) acc[i][j][r] = __builtin_amdgcn_exp2f((acc[i][j][r] - lse) * kLog2e);
                     else acc[i][j][r] = expf(acc[i][j][r] - lse);
                 }
-            const bool dead = !row_counts(lse);
-            if (__any(y >= 0 || dead) || tail) {   // labels here, rows or classes that are none
+            if (__any(y > -64) || tail) {   // labels here, or classes that are none
+                const float one = lse == INFINITY ? 0.f : 1.f;
 #pragma unroll
                 for (int i = 0; i < WMF; ++i)
 #pragma unroll
                     for (int r = 0; r < 16; ++r) {
-                        const int m = 32 * i + 8 * (r / 4) + 4 * h + r % 4;
-                        if (y == m) acc[i][j][r] -= 1.f;
-                        if (dead || (tail && a.v0 + mw + m >= a.n_classes)) acc[i][j][r] = 0.f;
+                        if (y == place(i, r)) acc[i][j][r] -= one;
+                        if (place(i, r) >= live) acc[i][j][r] = 0.f;
                     }
             }
 #pragma unroll
             for (int i = 0; i < WMF; ++i) {
-                // two groups of 4 classes of the lane and of lane ^ 32 make two chunks of 8, one for each
 #pragma unroll
                 for (int pl = 0; pl < PL; ++pl)
 #pragma unroll
@@ -464,10 +486,8 @@ __device__ __forceinline__ void xent_tile(const XentArgs &a, int32_t id, u32x4x 
                                     w[x][y2] = (uint32_t)q0[pl] | ((uint32_t)q1[pl] << 16);
                                 }
                             }
-                        const auto lo = __builtin_amdgcn_permlane32_swap(w[0][0], w[1][0], false, false);
-                        const auto hi = __builtin_amdgcn_permlane32_swap(w[0][1], w[1][1], false, false);
                         const int64_t chunk = (mw + 32 * i) / 8 + g + h;
-                        a.p[pl * a.p_plane + chunk * a.rows + n] = u32x4x{lo[0], hi[0], lo[1], hi[1]};
+                        a.p[pl * a.p_plane + chunk * a.rows + n] = join_chunk(w[0][0], w[0][1], w[1][0], w[1][1]);
                     }
             }
         }
@@ -517,6 +537,170 @@ __global__ void __launch_bounds__(64 * WGM * WGN, 2) k_xent_logits(const XentArg
     __shared__ u32x4x S[C::LDS];
     __shared__ float2 red[EPI == kStats ? WGM * C::BN : 1];
     xent_tile<PL, WMF, WNF, WGM, WGN, false, false, EPI>(a, blockIdx.x, S, red);
+}
+
+// The logits of bf16 rows of at most 256 columns.  The tiles above copy 128 KB to LDS per 128 x 128 of them, and
+// those copies' rate (some 25 bytes a clock and unit) is their bound at so few columns: here a wavefront keeps its 32 WNF
+// rows of h in registers for good (KS steps of 16 columns) and only the classes stream through LDS, 64 at a
+// time, two buffers and one barrier a tile.  A workgroup's four wavefronts hold 128 WNF rows and take a strip
+// of the piece's classes; two workgroups a unit, so that one's exponentials run beside the other's products.
+// A lane's running maximum and sum stay in registers over the strip.
+constexpr int kStrip = 64;   // classes of a tile
+
+template <int KS, int WNF, int EPI>
+__global__ void __launch_bounds__(256, 2) k_xent_strip(const XentArgs a) {
+    constexpr int TILE = 2 * KS * kStrip;            // chunks
+    constexpr int IN = 2 * KS / 4;                   // copies of a wavefront per tile
+    static_assert(KS % 2 == 0, "whole copies");
+    __shared__ u32x4x S[2 * TILE];
+    const int lane = threadIdx.x & 63, wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5, lr = lane & 31;
+    int32_t split, rb, strip;   // row blocks along M, strips along N
+    if (!tile_of(a, blockIdx.x, split, rb, strip)) return;
+    const int32_t all = (int32_t)(a.a_rows / kStrip), t0 = strip * a.split_steps, T = std::min(a.split_steps, all - t0);
+    const int64_t n0 = (int64_t)rb * (128 * WNF) + wid * (32 * WNF);
+
+    const char *src = (const char *)(a.A + (int64_t)(IN * wid) * a.a_rows + (int64_t)t0 * kStrip + lane);
+    auto issue = [&](int buf, int u) { dma16(src + (int64_t)u * a.a_rows * 16, &S[buf * TILE + (IN * wid + u) * kStrip]); };
+    if (T > 0)
+#pragma unroll
+        for (int u = 0; u < IN; ++u) issue(0, u);
+    src += kStrip * 16;
+    bf16x8 b[KS][WNF];
+    float lse[WNF], mx[WNF], sum[WNF];
+    int32_t y[WNF];   // the label's place in the piece (negative or past it: elsewhere)
+#pragma unroll
+    for (int j = 0; j < WNF; ++j) {
+        const int64_t n = n0 + 32 * j + lr;
+#pragma unroll
+        for (int k = 0; k < KS; ++k) b[k][j] = __builtin_bit_cast(bf16x8, a.B[(2 * k + h) * a.b_rows + n]);
+        y[j] = n < a.m && a.labels[n] >= 0 ? a.labels[n] - (int32_t)a.v0 : -1;
+        lse[j] = EPI == kProb ? a.lse[n] : 0.f;
+        mx[j] = -INFINITY;
+        sum[j] = 0.f;
+    }
+    for (int32_t t = 0; t < T; ++t) {
+        const u32x4x *tile = &S[(t & 1) * TILE];
+        // this tile's copies are done; the stores of the tile before it (the newest of all) may not be
+        if (EPI == kProb && t > 0) wait_vm<4 * WNF>();
+        else wait_vm<0>();
+        lds_barrier();
+        const bool more = t + 1 < T;
+        f32x16x acc[2][WNF];
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int j = 0; j < WNF; ++j)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
+        bf16x8 f[2][2];
+        auto read = [&](int k) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i) f[k & 1][i] = __builtin_bit_cast(bf16x8, tile[(2 * k + h) * kStrip + 32 * i + lr]);
+        };
+        read(0);
+#pragma unroll
+        for (int k = 0; k < KS; ++k) {
+            if (k + 1 < KS) read(k + 1);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int j = 0; j < WNF; ++j)
+                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[k & 1][i], b[k][j], acc[i][j], 0, 0, 0);
+            if (more)
+#pragma unroll
+                for (int u = IN * k / KS; u < IN * (k + 1) / KS; ++u) issue((t + 1) & 1, u);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        src += kStrip * 16;
+        const int64_t m0 = (int64_t)(t0 + t) * kStrip;                        // the tile's first class in the piece
+        const bool tail = a.v0 + m0 + kStrip > a.n_classes;
+        const int live = (int)std::max<int64_t>(std::min<int64_t>(a.n_classes - a.v0 - m0, kStrip), 0) - 4 * h;   // classes that are any
+#pragma unroll
+        for (int j = 0; j < WNF; ++j) {
+            const int64_t n = n0 + 32 * j + lr;
+            const uint32_t off = (uint32_t)y[j] - (uint32_t)m0;
+            const int at = off < (uint32_t)kStrip ? (int)off - 4 * h : -64;   // (less 4 h, as the places below)
+            if constexpr (EPI == kStats) {
+                if (tail)
+#pragma unroll
+                    for (int i = 0; i < 2; ++i)
+#pragma unroll
+                        for (int r = 0; r < 16; ++r)
+                            if (place(i, r) >= live) acc[i][j][r] = -INFINITY;
+                if (__any(at > -64))
+#pragma unroll
+                    for (int i = 0; i < 2; ++i)
+#pragma unroll
+                        for (int r = 0; r < 16; ++r)
+                            if (at == place(i, r)) a.label_logit[n] = acc[i][j][r];
+                float top = mx[j];
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) top = fmaxf(top, acc[i][j][r]);
+                const float ref = top == -INFINITY ? 0.f : top;
+                float part[2] = {sum[j] * __builtin_amdgcn_exp2f((mx[j] - ref) * kLog2e), 0.f};
+                if (__any(!(fabsf(ref) < kFmaRange))) {
+#pragma unroll
+                    for (int i = 0; i < 2; ++i)
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) part[i] += __builtin_amdgcn_exp2f((acc[i][j][r] - ref) * kLog2e);
+                } else {
+                    const float shift = -ref * kLog2e;
+#pragma unroll
+                    for (int i = 0; i < 2; ++i)
+#pragma unroll
+                        for (int r = 0; r < 16; ++r)
+                            part[i] += __builtin_amdgcn_exp2f(__builtin_fmaf(acc[i][j][r], kLog2e, shift));
+                }
+                sum[j] = part[0] + part[1];
+                mx[j] = top;
+            } else {
+                if (__any(!(fabsf(lse[j]) < kFmaRange || lse[j] == INFINITY))) {
+#pragma unroll
+                    for (int i = 0; i < 2; ++i)
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) acc[i][j][r] = __builtin_amdgcn_exp2f((acc[i][j][r] - lse[j]) * kLog2e);
+                } else {
+                    const float shift = -lse[j] * kLog2e;
+#pragma unroll
+                    for (int i = 0; i < 2; ++i)
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) acc[i][j][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(acc[i][j][r], kLog2e, shift));
+                }
+                if (__any(at > -64) || tail) {
+                    const float one = lse[j] == INFINITY ? 0.f : 1.f;
+#pragma unroll
+                    for (int i = 0; i < 2; ++i)
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) {
+                            if (at == place(i, r)) acc[i][j][r] -= one;
+                            if (place(i, r) >= live) acc[i][j][r] = 0.f;
+                        }
+                }
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int g = 0; g < 4; g += 2) {
+                        const f32x16x &p = acc[i][j];
+                        a.p[(m0 / 8 + 4 * i + g + h) * a.rows + n] =
+                            join_chunk(bf16_pair(p[4 * g], p[4 * g + 1]), bf16_pair(p[4 * g + 2], p[4 * g + 3]),
+                                       bf16_pair(p[4 * g + 4], p[4 * g + 5]), bf16_pair(p[4 * g + 6], p[4 * g + 7]));
+                    }
+            }
+        }
+    }
+    if constexpr (EPI == kStats) {
+#pragma unroll
+        for (int j = 0; j < WNF; ++j) {
+            const float om = __shfl_xor(mx[j], 32, kWave), os = __shfl_xor(sum[j], 32, kWave);
+            const float top = fmaxf(mx[j], om), ref = top == -INFINITY ? 0.f : top;
+            // (a lane whose logits are all -inf has the sum 0, or NaN, with no reference)
+            const float s = (mx[j] == -INFINITY ? sum[j] : sum[j] * expf(mx[j] - ref)) + (om == -INFINITY ? os : os * expf(om - ref));
+            if (h == 0) a.stats[((int64_t)a.strip0 + strip) * a.rows + n0 + 32 * j + lr] = make_float2(top, s);
+        }
+    }
 }
 
 // The statistics for at most 32 rows: bound by reading w once, so w and h are read as they lie (row-major, into the
@@ -753,7 +937,8 @@ struct XentPlan {
     int64_t rows, bk;               // packed rows of h, summed elements per step
     int64_t ln, rn;                 // rows of a logit tile, of a dh tile (and classes of a dw tile, at least 128)
     int64_t bm, width, chunks;      // features of a gradient tile, packed columns, their chunks
-    int64_t piece, tiles;           // classes of a piece, logit tiles in all
+    int32_t strips, strip_tiles;    // k_xent_strip: strips of a piece, their tiles (0: the other kernels)
+    int64_t piece, tiles;           // classes of a piece, entries of the rows' statistics
     int32_t splits, split_steps;    // of dh's sum over a piece
     size_t h, w, p, part, stats, label_logit, lse, losses, inv, total;
 
@@ -766,8 +951,11 @@ struct XentPlan {
         ln = m <= 32 ? 32 : 128;
         rn = big ? 256 : ln;
         bm = big ? 256 : d <= 64 && rn == 128 ? 64 : 128;
-        rows = up(std::max<int64_t>(m, 1), grads ? rn : ln);
+        if (bf16 && m > 32 && d <= 256) ln = m > 128 ? 256 : 128;   // held in registers
+        rows = up(std::max<int64_t>(m, 1), grads ? std::max(rn, ln) : ln);
         width = up(d, grads ? bm : 64);
+        if (bf16 && m > 32 && d > 128 && d <= 256) width = 256;
+        if (bf16 && m > 32 && d > 64 && d <= 128) width = 128;
         chunks = width / 8;
         const int64_t all = up(n_classes, kPiece);
         tiles = all / (ln == 32 ? kFewTile : kVTile);
@@ -776,6 +964,13 @@ struct XentPlan {
         piece = std::min(piece, all);
         const int64_t pieces = (all + piece - 1) / piece;
         piece = up((all + pieces - 1) / pieces, kPiece);   // equal ones
+        strips = strip_tiles = 0;
+        if (bf16 && m > 32 && d <= 256) {   // two workgroups a unit
+            const int64_t t = piece / kStrip, s = std::min(t, std::max<int64_t>(1, 512 / (rows / ln)));
+            strip_tiles = (int32_t)((t + s - 1) / s);
+            strips = (int32_t)((t + strip_tiles - 1) / strip_tiles);
+            tiles = pieces * strips;
+        }
         splits = 1;
         split_steps = 0;
         if (dh) {
@@ -811,7 +1006,27 @@ unsigned ids_of(const XentArgs &a) {   // workgroups of a product, whole rounds 
 // but have fewer workgroups on a unit to fill each other's gaps (4,093 x 169,000 x 256 bf16: both
 // passes 609 us, 128 x 128 595; x 1,024 columns 2,118 and 2,145; fp32 1,024 rows 1,342 and 1,256).
 template <int PL, int EPI>
-void run_logits(XentArgs &a, int64_t ln, int64_t vdim, const char *label, hipStream_t s) {
+void run_logits(XentArgs &a, const XentPlan &plan, int64_t d, int64_t vdim, const char *label, hipStream_t s) {
+    const int64_t ln = plan.ln;
+    if constexpr (PL == 1)
+        if (plan.strips > 0) {
+            a.m_tiles = (int32_t)(a.rows / ln);
+            a.n_tiles = plan.strips;
+            a.splits = 1;
+            a.split_steps = plan.strip_tiles;
+            a.strip0 = (int32_t)(a.v0 / plan.piece) * plan.strips;
+            KernelTimer t(label, s);
+#define GNNAV_L(KS)                                                                                                   \
+    do {                                                                                                              \
+        if (ln == 256) hipLaunchKernelGGL((k_xent_strip<KS, 2, EPI>), dim3(ids_of(a)), dim3(256), 0, s, a);           \
+        else hipLaunchKernelGGL((k_xent_strip<KS, 1, EPI>), dim3(ids_of(a)), dim3(256), 0, s, a);                     \
+    } while (0)
+            if (d <= 64) GNNAV_L(4);
+            else if (d <= 128) GNNAV_L(8);
+            else GNNAV_L(16);
+#undef GNNAV_L
+            return;
+        }
     a.m_tiles = (int32_t)(vdim / kVTile);
     a.n_tiles = (int32_t)(a.rows / ln);
     a.splits = 1;
@@ -894,7 +1109,7 @@ void xent(const XentPlan &p, const LinearXentArgs &x, hipStream_t s) {
         pack_w(v0, vp);
         packed = vp == all;
         logits(v0, vp);
-        run_logits<PL, kStats>(a, p.ln, vp, "xent_stats", s);
+        run_logits<PL, kStats>(a, p, x.d, vp, "xent_stats", s);
     }
     {
         KernelTimer t("xent_rows", s);
@@ -915,7 +1130,7 @@ void xent(const XentPlan &p, const LinearXentArgs &x, hipStream_t s) {
             logits(v0, vp);
             a.p = Pb;
             a.p_plane = vp / 8 * p.rows;
-            run_logits<PL, kProb>(a, p.ln, vp, "xent_prob", s);
+            run_logits<PL, kProb>(a, p, x.d, vp, "xent_prob", s);
             XentArgs w = a, h = a;
             w.B = h.B = Pb;
             w.b_rows = h.b_rows = p.rows;
