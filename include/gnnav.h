@@ -528,8 +528,9 @@ gnnav_status gnnav_embedding_backward(const void *dout_dev, int64_t ld_dout, con
  * columns from d up to the next 16-byte boundary with zeros.  Results do not
  * depend on the run (no atomics).  workspace_dev: at least
  * gnnav_linear_xent_workspace bytes (grads: whether dh or dw is asked for; -1
- * for bad arguments; host only) on a 256-byte boundary.  Its size grows with m, d and
- * n_classes / 256, not with their product.  No call allocates.
+ * for bad arguments; host only) on a 256-byte boundary.  It holds h and one
+ * piece of the classes: some multiples of m x d, and less than 2 GiB for the
+ * piece, however many classes there are (m <= 32: n_classes bytes more).  No call allocates.
  * Errors: E_INVALID (null pointers, sizes, strides, alignment, workspace),
  * E_CAPACITY (a size beyond int32), E_DEVICE.  Asynchronous.               */
 int64_t gnnav_linear_xent_workspace(int64_t m, int64_t n_classes, int64_t d, gnnav_dtype dt, int32_t grads);

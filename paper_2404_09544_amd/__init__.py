@@ -548,19 +548,35 @@ def _workspace_bytes(n: int) -> int:
     return int(n)
 
 
-def embedding(table, ids, out, scale: float = 1.0, n_ids_dev=None, stream=None):
+def _ids(ids, n_ids, device: int):
+    """(address, count) of an id list: a device int32 tensor, or an address such as Blocks.nodes_ptr() with its count."""
+    if isinstance(ids, int):
+        if n_ids is None:
+            raise ValueError("an address of ids needs n_ids")
+        return ids, n_ids
+    n = ids.numel() if n_ids is None else n_ids
+    return _vector(ids, "ids", device, torch.int32, n), n
+
+
+def _count(n_ids_dev, device: int):
+    if n_ids_dev is None or isinstance(n_ids_dev, int):
+        return n_ids_dev
+    return _vector(n_ids_dev, "n_ids_dev", device, torch.int32, 1)
+
+
+def embedding(table, ids, out, scale: float = 1.0, n_ids=None, n_ids_dev=None, stream=None):
     """gnnav_embedding: out[i] = scale * table[ids[i]] in the table's type (fp32 or
-    bf16); an id outside the table gives a zero row.  ids: device int32;
-    n_ids_dev: optional device int32 tensor with the count of ids to take."""
+    bf16); an id outside the table gives a zero row.  ids: device int32 tensor,
+    or the address of n_ids of them (a frontier's Blocks.nodes_ptr());
+    n_ids_dev: device int32 (tensor or address) with the count of ids to take."""
     dev, dt = _here(), table.dtype
     rows, d, ld = _rows(table, "table", dev)
     n_out, _, ld_out = _rows(out, "out", dev, d, dt)
-    n, ids_ptr = ids.numel(), _vector(ids, "ids", dev, torch.int32)
+    ids_ptr, n = _ids(ids, n_ids, dev)
     if n_out < n:
         raise ValueError("out has fewer rows than ids")
-    count = None if n_ids_dev is None else _vector(n_ids_dev, "n_ids_dev", dev, torch.int32, 1)
-    _check(_lib.gnnav_embedding(table.data_ptr(), rows, ld, d, _TORCH_CODE[dt], ids_ptr, count, n, scale,
-                                out.data_ptr(), ld_out, _on(stream, dev)))
+    _check(_lib.gnnav_embedding(table.data_ptr(), rows, ld, d, _TORCH_CODE[dt], ids_ptr, _count(n_ids_dev, dev), n,
+                                scale, out.data_ptr(), ld_out, _on(stream, dev)))
 
 
 def embedding_backward_workspace(n_ids: int, n_rows: int, d: int, dtype: str) -> int:
@@ -568,19 +584,19 @@ def embedding_backward_workspace(n_ids: int, n_rows: int, d: int, dtype: str) ->
     return _workspace_bytes(_lib.gnnav_embedding_backward_workspace(int(n_ids), int(n_rows), int(d), dtype_code(dtype)))
 
 
-def embedding_backward(dout, ids, dtable, scale: float = 1.0, accumulate: bool = False, n_ids_dev=None,
+def embedding_backward(dout, ids, dtable, scale: float = 1.0, accumulate: bool = False, n_ids=None, n_ids_dev=None,
                        workspace=None, stream=None):
-    """gnnav_embedding_backward: dtable[v] (+)= scale * the sum of the rows of dout whose id is v."""
+    """gnnav_embedding_backward: dtable[v] (+)= scale * the sum of the rows of dout whose id is v.
+    ids, n_ids and n_ids_dev as for embedding."""
     dev, dt = _here(), dout.dtype
     n_in, d, ld = _rows(dout, "dout", dev)
     rows, _, ld_table = _rows(dtable, "dtable", dev, d, dt)
-    n, ids_ptr, code = ids.numel(), _vector(ids, "ids", dev, torch.int32), _TORCH_CODE[dt]
+    (ids_ptr, n), code = _ids(ids, n_ids, dev), _TORCH_CODE[dt]
     if n_in < n:
         raise ValueError("dout has fewer rows than ids")
-    count = None if n_ids_dev is None else _vector(n_ids_dev, "n_ids_dev", dev, torch.int32, 1)
     need = 0 if workspace is not None else _workspace_bytes(_lib.gnnav_embedding_backward_workspace(n, rows, d, code))
     ws, ws_bytes, _hold = _workspace(workspace, need, dev, stream)
-    _check(_lib.gnnav_embedding_backward(dout.data_ptr(), ld, ids_ptr, count, n, d, code, scale, bool(accumulate),
+    _check(_lib.gnnav_embedding_backward(dout.data_ptr(), ld, ids_ptr, _count(n_ids_dev, dev), n, d, code, scale, bool(accumulate),
                                          dtable.data_ptr(), rows, ld_table, ws, ws_bytes, _on(stream, dev)))
 
 

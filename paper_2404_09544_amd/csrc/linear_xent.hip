@@ -142,13 +142,12 @@ struct XentArgs {
     int64_t k;                 // summed length, a multiple of the step
     int32_t m_tiles, n_tiles, splits;
     int32_t split_steps;       // kDh: steps of one split; k_xent_strip: tiles of a strip
-    int32_t strip0;            // k_xent_strip: the piece's first strip
     // kStats, kProb
     int64_t v0, n_classes;     // first class of the piece, classes in all
     int64_t rows;              // packed rows of h
     const int32_t *labels;
     int64_t m;                 // rows of h
-    float2 *stats;             // [tile of classes][rows]
+    float2 *stats;             // [1 + tile or strip of the piece's classes][rows]; the first: of earlier pieces
     float *label_logit;        // [rows]
     const float *lse;          // [rows]
     u32x4x *p;                 // planes [class chunk][rows]
@@ -272,7 +271,7 @@ __device__ __forceinline__ void stats_of(const XentArgs &a, f32x16x (&acc)[WMF][
             const float2 o = red[w * BN + c];
             s += o.x == -INFINITY ? o.y : o.y * expf(o.x - mx);
         }
-        a.stats[(a.v0 / BM + mt) * a.rows + n0 + c] = make_float2(mx, s);
+        a.stats[(1 + mt) * a.rows + n0 + c] = make_float2(mx, s);
     }
 }
 
@@ -698,7 +697,7 @@ __global__ void __launch_bounds__(256, 2) k_xent_strip(const XentArgs a) {
             const float top = fmaxf(mx[j], om), ref = top == -INFINITY ? 0.f : top;
             // (a lane whose logits are all -inf has the sum 0, or NaN, with no reference)
             const float s = (mx[j] == -INFINITY ? sum[j] : sum[j] * expf(mx[j] - ref)) + (om == -INFINITY ? os : os * expf(om - ref));
-            if (h == 0) a.stats[((int64_t)a.strip0 + strip) * a.rows + n0 + 32 * j + lr] = make_float2(top, s);
+            if (h == 0) a.stats[((int64_t)1 + strip) * a.rows + n0 + 32 * j + lr] = make_float2(top, s);
         }
     }
 }
@@ -777,16 +776,16 @@ __global__ void __launch_bounds__(256) k_xent_score(const XentArgs a, const void
     stats_of<PL, kFew, 1, 4, 1>(a, acc, blockIdx.x, 0, red);
 }
 
-// A piece's dw and dh in one launch: the workgroups of dw (of the first `dw_ids`), then those of dh, fill
+// A piece's dh and dw in one launch: the workgroups of dh (the first `dh_ids`), then those of dw, fill
 // the units together.  dw's tiles are 32 x WMF x WGM by 32 x WNW x WGN, dh's 32 x WMF x WGM by 32 x WNH x WGN.
 template <int PL, int WMF, int WNW, int WNH, int WGM, int WGN, int WGMH, int WMFH>
-__global__ void __launch_bounds__(64 * WGM * WGN, 2) k_xent_grads(const XentArgs w, const XentArgs h, int32_t dw_ids) {
+__global__ void __launch_bounds__(64 * WGM * WGN, 2) k_xent_grads(const XentArgs w, const XentArgs h, int32_t dh_ids) {
     constexpr int WGNH = WGM * WGN / WGMH;
     using CW = Tile<PL, WMF, WNW, WGM, WGN>;
     using CH = Tile<PL, WMFH, WNH, WGMH, WGNH>;
     __shared__ u32x4x S[CW::LDS > CH::LDS ? CW::LDS : CH::LDS];
-    if ((int32_t)blockIdx.x < dw_ids) xent_tile<PL, WMF, WNW, WGM, WGN, true, true, kDw>(w, blockIdx.x, S, nullptr);
-    else xent_tile<PL, WMFH, WNH, WGMH, WGNH, true, false, kDh>(h, blockIdx.x - dw_ids, S, nullptr);
+    if ((int32_t)blockIdx.x < dh_ids) xent_tile<PL, WMFH, WNH, WGMH, WGNH, true, false, kDh>(h, blockIdx.x, S, nullptr);
+    else xent_tile<PL, WMF, WNW, WGM, WGN, true, true, kDw>(w, blockIdx.x - dh_ids, S, nullptr);
 }
 
 // ------------------------------------------------------------- rows and loss
@@ -823,11 +822,12 @@ __device__ __forceinline__ void xent_loss(const float *losses, int64_t m, const 
     }
 }
 
-// Joins a row's tiles: lse (+inf for a row that does not count), the row's
-// loss.  ROWS rows a workgroup, the tiles dealt to SLICES threads of each.  LOSS: there is
-// one workgroup, which takes the mean too.
-template <int ROWS, int SLICES, bool LOSS>
-__global__ void __launch_bounds__(ROWS * SLICES) k_xent_rows(const float2 *__restrict__ stats, int64_t tiles, int64_t rows,
+// Joins a row's entries [from, tiles]: before the last piece to entry 0 (kFold), then to lse (+inf for a row that
+// does not count) and the row's loss.  ROWS rows a workgroup, the entries dealt to SLICES threads of each.
+// kLoss: there is one workgroup, which takes the mean too.
+enum { kFold, kLse, kLoss };
+template <int ROWS, int SLICES, int MODE>
+__global__ void __launch_bounds__(ROWS * SLICES) k_xent_rows(float2 *stats, int64_t from, int64_t tiles, int64_t rows,
                                                              int64_t m, const int32_t *__restrict__ labels,
                                                              int32_t ignore, int64_t n_classes,
                                                              const float *__restrict__ label_logit,
@@ -847,14 +847,14 @@ __global__ void __launch_bounds__(ROWS * SLICES) k_xent_rows(const float2 *__res
         for (int q = 0; q < count; ++q) s += o[q].x == -INFINITY ? o[q].y : o[q].y * expf(o[q].x - ref);
         mx = top;
     };
-    int64_t t = k;
-    for (; t + 7 * SLICES < tiles; t += 8 * SLICES) {
+    int64_t t = from + k;
+    for (; t + 7 * SLICES <= tiles; t += 8 * SLICES) {
         float2 o[8];
 #pragma unroll
         for (int q = 0; q < 8; ++q) o[q] = stats[(t + q * SLICES) * rows + n];
         join(o, 8);
     }
-    for (; t < tiles; t += SLICES) {
+    for (; t <= tiles; t += SLICES) {
         const float2 o = stats[t * rows + n];
         join(&o, 1);
     }
@@ -867,6 +867,10 @@ __global__ void __launch_bounds__(ROWS * SLICES) k_xent_rows(const float2 *__res
         }
         __syncthreads();
     }
+    if constexpr (MODE == kFold) {   // (every entry has been read)
+        if (k == 0) stats[n] = make_float2(mx, s);
+        return;
+    }
     if (k == 0) {
         const int32_t y = n < m ? labels[n] : ignore;
         const bool out = n >= m || y == ignore, bad = !out && (y < 0 || y >= n_classes);
@@ -875,7 +879,7 @@ __global__ void __launch_bounds__(ROWS * SLICES) k_xent_rows(const float2 *__res
         losses[n] = one;
         if (row_loss && n < m) row_loss[n] = one;
     }
-    if constexpr (LOSS) {
+    if constexpr (MODE == kLoss) {
         __syncthreads();
         xent_loss<ROWS * SLICES>(losses, m, labels, ignore, loss, inv_count);
     }
@@ -928,6 +932,7 @@ __global__ void __launch_bounds__(256) k_xent_dh(const f32x4x *__restrict__ part
 namespace {
 
 constexpr int64_t kPBytes = int64_t(1) << 30;     // p of a piece, at most (or one tile of classes)
+constexpr int64_t kLogits = int64_t(1) << 32;     // logits of a piece whose p is not kept, at most: its statistics are a 64th of their size
 constexpr int64_t kWBytes = int64_t(512) << 20;   // packed weights of a piece, at most (or one tile)
 
 int64_t up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
@@ -938,9 +943,44 @@ struct XentPlan {
     int64_t ln, rn;                 // rows of a logit tile, of a dh tile (and classes of a dw tile, at least 128)
     int64_t bm, width, chunks;      // features of a gradient tile, packed columns, their chunks
     int32_t strips, strip_tiles;    // k_xent_strip: strips of a piece, their tiles (0: the other kernels)
-    int64_t piece, tiles;           // classes of a piece, entries of the rows' statistics
+    int64_t piece;                  // classes of a piece
     int32_t splits, split_steps;    // of dh's sum over a piece
     size_t h, w, p, part, stats, label_logit, lse, losses, inv, total;
+
+    // In how many parts dh's sum over a piece is taken: `tiles` workgroups of `steps` steps each are cut into so many,
+    // and `dw` workgroups of `dw_steps` follow them on the device's places.  The makespan of that, and the time of
+    // moving a part's sums (`part_bytes`), decide: 4,093 x 169,000 x 256 bf16 takes 16 tiles of 2,646 steps and 331 of
+    // 128 on 256 places, 420 us a piece in 16 parts.
+    int32_t dh_splits(int64_t tiles, int64_t steps, int64_t dw, int64_t dw_steps, int64_t part_bytes) const {
+        const int64_t places = rn == 256 ? 256 : 512;   // a 256 x 256 tile has a unit to itself
+        // seconds of a step of one workgroup at the rate that the products reach
+        const double step = 2.0 * bm * std::max<int64_t>(rn, 128) * bk * (pl == 3 ? 6 : 1) * places / 1.1e15;
+        double best = 0;
+        int32_t best_s = 0;
+        for (int64_t s = 1; s <= 128 && s <= std::max<int64_t>(1, steps / 8); s += s < 16 ? 1 : s < 32 ? 2 : 8) {
+            const int64_t len = (steps + s - 1) / s, jobs = tiles * s, full = jobs / places, late = jobs % places;
+            // `late` places are free after full + 1 jobs, the others after full
+            auto done = [&](int64_t t) {
+                const int64_t x = t - full * len, y = x - len;
+                return (places - late) * (x > 0 ? x / dw_steps : 0) + late * (y > 0 ? y / dw_steps : 0);
+            };
+            int64_t end = full * len + (late ? len : 0);
+            if (dw > 0) {
+                int64_t k = dw / places;   // rounds of dw on the earlier places at least, on the later ones one fewer
+                k = std::max<int64_t>(0, k - (len + dw_steps - 1) / dw_steps - 1);
+                int64_t t = full * len + k * dw_steps, u = full * len + len + std::max<int64_t>(0, k - len / dw_steps - 1) * dw_steps;
+                while (done(t) < dw) t += dw_steps;
+                while (done(u) < dw) u += dw_steps;
+                end = std::max(end, std::min(t, u));
+            }
+            const double cost = end * step + (double)s * part_bytes / 4e12;
+            if (best_s == 0 || cost < best) {
+                best = cost;
+                best_s = (int32_t)s;
+            }
+        }
+        return best_s;
+    }
 
     XentPlan(int64_t m, int64_t n_classes, int64_t d, bool bf16, bool grads, bool dh) {
         pl = bf16 ? 1 : 3;
@@ -958,9 +998,9 @@ struct XentPlan {
         if (bf16 && m > 32 && d > 64 && d <= 128) width = 128;
         chunks = width / 8;
         const int64_t all = up(n_classes, kPiece);
-        tiles = all / (ln == 32 ? kFewTile : kVTile);
         piece = std::max<int64_t>(kPiece, kWBytes / (width * 2 * pl) / kPiece * kPiece);
-        if (grads) piece = std::min(piece, std::max<int64_t>(kPiece, kPBytes / (rows * 2 * pl) / kPiece * kPiece));
+        const int64_t most = grads ? kPBytes / (2 * pl) : kLogits;
+        piece = std::min(piece, std::max<int64_t>(kPiece, most / rows / kPiece * kPiece));
         piece = std::min(piece, all);
         const int64_t pieces = (all + piece - 1) / piece;
         piece = up((all + pieces - 1) / pieces, kPiece);   // equal ones
@@ -969,13 +1009,12 @@ struct XentPlan {
             const int64_t t = piece / kStrip, s = std::min(t, std::max<int64_t>(1, 512 / (rows / ln)));
             strip_tiles = (int32_t)((t + s - 1) / s);
             strips = (int32_t)((t + strip_tiles - 1) / strip_tiles);
-            tiles = pieces * strips;
         }
         splits = 1;
         split_steps = 0;
         if (dh) {
-            const int64_t t = width / bm * (rows / rn), steps = piece / bk;
-            splits = (int32_t)std::max<int64_t>(1, std::min((rn == 256 ? 256 : 512) / t, steps / 8));
+            const int64_t steps = piece / bk, dw = width / bm * (piece / std::max<int64_t>(rn, 128));
+            splits = dh_splits(width / bm * (rows / rn), steps, dw, rows / bk, rows * width * 4 * (pieces + 1));
             split_steps = (int32_t)((steps + splits - 1) / splits);
             splits = (int32_t)((steps + split_steps - 1) / split_steps);
         }
@@ -986,10 +1025,10 @@ struct XentPlan {
             return here;
         };
         h = take(rows * width * 2 * pl);
-        w = take(piece * width * 2 * pl);
+        w = take(ln > 32 || grads ? piece * width * 2 * pl : 0);
         p = take(grads ? rows * piece * 2 * pl : 0);
         part = take(dh ? splits * rows * width * 4 : 0);
-        stats = take(tiles * rows * 8);
+        stats = take((1 + (ln == 32 ? all / kFewTile : strips > 0 ? strips : piece / kVTile)) * rows * 8);
         label_logit = take(rows * 4);
         lse = take(rows * 4);
         losses = take(rows * 4);
@@ -1014,7 +1053,6 @@ void run_logits(XentArgs &a, const XentPlan &plan, int64_t d, int64_t vdim, cons
             a.n_tiles = plan.strips;
             a.splits = 1;
             a.split_steps = plan.strip_tiles;
-            a.strip0 = (int32_t)(a.v0 / plan.piece) * plan.strips;
             KernelTimer t(label, s);
 #define GNNAV_L(KS)                                                                                                   \
     do {                                                                                                              \
@@ -1047,7 +1085,7 @@ void run_grads(const XentArgs &w, const XentArgs &h, int64_t bm, int64_t rn, hip
     const unsigned nw = w.m_tiles > 0 ? ids_of(w) : 0, nh = h.m_tiles > 0 ? ids_of(h) : 0;
 #define GNNAV_L(WMF, WNW, WNH, WGM, WGN, WGMH, WMFH)                                                                  \
     hipLaunchKernelGGL((k_xent_grads<PL, WMF, WNW, WNH, WGM, WGN, WGMH, WMFH>), dim3(nw + nh),                        \
-                       dim3(64 * WGM * WGN), 0, s, w, h, (int32_t)nw)
+                       dim3(64 * WGM * WGN), 0, s, w, h, (int32_t)nh)
     if (rn == 32) {
         GNNAV_L(2, 2, 1, 2, 2, 4, 1);
     } else if (rn == 256) {
@@ -1099,26 +1137,38 @@ void xent(const XentPlan &p, const LinearXentArgs &x, hipStream_t s) {
     };
     const int64_t all = up(x.n_classes, kPiece);
     bool packed = false;   // one piece: packed once for both passes
+    bool several = false;  // entry 0 of the statistics holds earlier pieces'
+    int64_t entries = 0;   // of the piece
     if (p.ln == 32) {
         KernelTimer t("xent_stats", s);
-        hipLaunchKernelGGL(k_xent_score<PL>, dim3((unsigned)p.tiles), dim3(256), 0, s, a, x.w, x.ld_w, x.h, x.ld_h,
+        entries = all / kFewTile;
+        hipLaunchKernelGGL(k_xent_score<PL>, dim3((unsigned)entries), dim3(256), 0, s, a, x.w, x.ld_w, x.h, x.ld_h,
                            x.ignore, x.d);
     }
     for (int64_t v0 = 0; v0 < all && p.ln > 32; v0 += p.piece) {
         const int64_t vp = std::min(p.piece, all - v0);
+        if (v0 > 0) {
+            KernelTimer t("xent_rows", s);
+            hipLaunchKernelGGL((k_xent_rows<16, 16, kFold>), dim3((unsigned)(p.rows / 16)), dim3(256), 0, s, a.stats,
+                               several ? 0 : 1, entries, p.rows, x.m, x.labels, x.ignore, x.n_classes, a.label_logit,
+                               lse, losses, nullptr, nullptr, nullptr);
+            several = true;
+        }
         pack_w(v0, vp);
         packed = vp == all;
         logits(v0, vp);
         run_logits<PL, kStats>(a, p, x.d, vp, "xent_stats", s);
+        entries = p.strips > 0 ? p.strips : vp / kVTile;
     }
     {
         KernelTimer t("xent_rows", s);
+        const int64_t from = several ? 0 : 1;
         if (p.rows == 32) {
-            hipLaunchKernelGGL((k_xent_rows<32, 32, true>), dim3(1), dim3(1024), 0, s, a.stats, p.tiles, p.rows, x.m,
-                               x.labels, x.ignore, x.n_classes, a.label_logit, lse, losses, x.row_loss, x.loss, inv);
+            hipLaunchKernelGGL((k_xent_rows<32, 32, kLoss>), dim3(1), dim3(1024), 0, s, a.stats, from, entries, p.rows,
+                               x.m, x.labels, x.ignore, x.n_classes, a.label_logit, lse, losses, x.row_loss, x.loss, inv);
         } else {
-            hipLaunchKernelGGL((k_xent_rows<16, 16, false>), dim3((unsigned)(p.rows / 16)), dim3(256), 0, s, a.stats,
-                               p.tiles, p.rows, x.m, x.labels, x.ignore, x.n_classes, a.label_logit, lse, losses,
+            hipLaunchKernelGGL((k_xent_rows<16, 16, kLse>), dim3((unsigned)(p.rows / 16)), dim3(256), 0, s, a.stats,
+                               from, entries, p.rows, x.m, x.labels, x.ignore, x.n_classes, a.label_logit, lse, losses,
                                x.row_loss, nullptr, nullptr);
             hipLaunchKernelGGL(k_xent_loss, dim3(1), dim3(1024), 0, s, losses, x.m, x.labels, x.ignore, x.loss, inv);
         }

@@ -12,6 +12,9 @@ logits.  Buffers are sized once from the Eq. 12 capacity bounds.
 and gather, then gnnav_sage_train_step (forward, softmax cross-entropy over
 F_0, backward, SGD on the step's weights in place).
 
+With ``clip_norm`` the update is that of the gradients clipped by their global
+norm (gnnav_sgd_clip_step), which lands in the step's ``grad_norm``.
+
 ``Pipeline`` runs consecutive batches on alternating streams, each with its
 own step (blocks, gathered rows, logits), so batch b+1's sampling and
 host-link gather overlap batch b's aggregation and combine: the overlap
@@ -30,8 +33,8 @@ import atexit
 import numpy as np
 import torch
 
-from . import (Blocks, Cache, Graph, gather, gather_n, sage_forward, sage_train_step, sample, sample_async,
-               sample_biased, stream_create, stream_destroy, sync)
+from . import (Blocks, Cache, Graph, clip_workspace, gather, gather_n, sage_forward, sage_train_step, sample,
+               sample_async, sample_biased, sgd_clip_step, stream_create, stream_destroy, sync)
 
 
 def to_device_weights(ws, dtype: str):
@@ -61,6 +64,8 @@ class MiniBatchStep:
         self.logits = torch.empty((0, self.dims[-1]), dtype=torch.float32, device="cuda")
         self.counts = torch.zeros(3, dtype=torch.int64, device="cuda")
         self.loss = torch.zeros(1, dtype=torch.float32, device="cuda")
+        self.grad_norm = torch.zeros(1, dtype=torch.float32, device="cuda")
+        self._clip = None                        # gradients and workspace of a clipped update
         self.gathered = torch.cuda.Event()       # recorded after each gather
         self.sizes = None
         self._seeds = None
@@ -133,13 +138,25 @@ class MiniBatchStep:
             self._grow(sizes[-1], sizes[0])
             gather(self.cache, nodes_ptr, sizes[-1], self.h0, self.counts, st)
 
-    def _train_tail(self, labels_dev, lr: float, grads, st):
-        sage_train_step(self.blocks, self.h0, self.weights, self.dims, labels_dev, lr, self.logits, self.loss,
-                        grads, st)
+    def _train_tail(self, labels_dev, lr: float, grads, st, clip_norm=None):
+        if clip_norm is None:
+            sage_train_step(self.blocks, self.h0, self.weights, self.dims, labels_dev, lr, self.logits, self.loss,
+                            grads, st)
+            return
+        if self._clip is None:
+            self._clip = ([torch.empty_like(w) for w in self.weights],
+                          torch.empty(clip_workspace(self.weights), dtype=torch.uint8, device="cuda"))
+            torch.cuda.current_stream().synchronize()      # the buffers are used on other streams too
+        own, ws = self._clip
+        grads = own if grads is None else grads
+        sage_train_step(self.blocks, self.h0, self.weights, self.dims, labels_dev, 0.0, self.logits, self.loss, grads, st)
+        sgd_clip_step(self.weights, grads, lr, clip_norm, self.grad_norm, workspace=ws, stream=st)
 
     def train(self, seeds_dev, rng_seed: int, labels_dev, lr: float, grads=None, async_mode: bool = False,
-              stream=None):
+              stream=None, clip_norm=None):
         """One training iteration; labels_dev: device int32 label of every vertex.
+        clip_norm: largest global norm of the gradients that the update takes
+        (``grads`` receives them as they were); the norm lands in ``self.grad_norm``.
 
         Sync mode returns the logits view [|F_0|, classes]; async mode
         returns None (call ``finish`` for the view).  The loss lands in
@@ -149,7 +166,7 @@ class MiniBatchStep:
             raise ValueError("training runs in fp32")
         st = stream if stream is not None else torch.cuda.current_stream()
         self._inputs(seeds_dev, rng_seed, async_mode, st)
-        self._train_tail(labels_dev, lr, grads, st)
+        self._train_tail(labels_dev, lr, grads, st, clip_norm)
         return None if async_mode else self.logits[:self.sizes[0]]
 
     def finish(self):
@@ -234,10 +251,11 @@ class Pipeline:
         self.count += 1
         return self.slots[k]
 
-    def enqueue_train(self, seeds_dev, rng_seed: int, labels_dev, lr: float):
+    def enqueue_train(self, seeds_dev, rng_seed: int, labels_dev, lr: float, clip_norm=None):
         """Enqueue the next training iteration.  Its sampling and gather may
         run alongside the previous batch; its forward waits for the previous
-        batch's weight update (the weights are shared)."""
+        batch's weight update (the weights are shared).  clip_norm: as of
+        MiniBatchStep.train."""
         k = self.count % self.depth
         slot, st = self.slots[k], self.streams[k]
         if slot.dtype != "f32":
@@ -246,7 +264,7 @@ class Pipeline:
         slot._inputs(seeds_dev, rng_seed, True, st, gather_after=self._previous_gather())
         if self._updated is not None:
             st.wait_event(self._updated)
-        slot._train_tail(labels_dev, lr, None, st)
+        slot._train_tail(labels_dev, lr, None, st, clip_norm)
         self._updated = torch.cuda.Event()
         self._updated.record(st)
         self.count += 1

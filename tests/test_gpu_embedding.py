@@ -119,7 +119,7 @@ GRADS = [("uniform", 1, 1, 1), ("uniform", 1, 9, 8), ("uniform", 300, 1000, 17),
          ("uniform", 4097, 3000, 64), ("same", 4097, 1, 8), ("same", 10_007, 9, 100), ("few", 9000, 3, 602),
          ("bad", 6000, 1000, 5), ("bad", 5000, 1, 12), ("runs", 6400, 110, 32), ("skew", 50_000, 20_000, 128),
          ("skew", 70_000, 300, 1030), ("uniform", 30_000, 1_500_000, 8), ("uniform", 20_001, 1025, 48),
-         ("uniform", 8000, 1023, 260), ("uniform", 8000, 1024, 20)]
+         ("uniform", 8000, 1023, 260), ("uniform", 8000, 1024, 20), ("skew", 1_200_000, 5000, 4)]
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])

@@ -211,7 +211,8 @@ def test_infinite_and_nan_inputs(G, dtype):
     assert torch.isnan(dh[5]).all() and torch.isfinite(dh[:5]).all() and torch.isfinite(dh[6:]).all()
 
 
-@pytest.mark.parametrize("dtype,m,v,d", [("f32", 1000, 70_001, 16), ("bf16", 2100, 90_001, 24)])
+@pytest.mark.parametrize("dtype,m,v,d", [("f32", 4000, 70_001, 16), ("bf16", 8100, 90_001, 24), ("bf16", 8000, 80_001, 264),
+                                         ("f32", 70_001, 300, 40), ("bf16", 70_001, 300, 40)])
 def test_several_pieces_of_classes(G, dtype, m, v, d):
     """More classes than a piece holds, the last piece ragged; in 64 bits on the device."""
     import torch

@@ -89,7 +89,11 @@ def test_workspace_sizes():
     for dtype, elt in (("f32", 4), ("bf16", 2)):
         m, v, d = 8192, 10_000_000, 256
         logits = m * v * 4
-        assert G.linear_xent_workspace(m, v, d, dtype, True) < logits // 50
+        assert G.linear_xent_workspace(m, v, d, dtype, True) < logits // 100
+        for rows in (1, 32, 33, 200, 8192, 300_000):     # a piece is a piece
+            for grads in (False, True):
+                one, ten = (G.linear_xent_workspace(rows, k * v, d, dtype, grads) for k in (1, 10))
+                assert ten < 1.1 * one + (10 * v if rows <= 32 else 0) + (1 << 20), (rows, grads, one, ten)
         # growing only with what it is made of
         sizes = [G.linear_xent_workspace(m, v, d, dtype, g) for m in (1, 33, 1000) for v in (10, 10_000, 1_000_000)
                  for d in (3, 100) for g in (False, True)]
