@@ -67,6 +67,14 @@ struct Unit {
     }
 };
 
+// Results larger than this are stored past the caches, which the tables and gradients being read then have for
+// themselves: 800,000 rows of 256 bytes 89 us, 79 so; the gradient of 524,288 skewed ids x 256 bf16 159 and 145.
+constexpr int64_t kStreamBytes = int64_t(64) << 20;
+__device__ __forceinline__ void store(u32x4e *to, u32x4e v, bool streamed) {
+    if (streamed) __builtin_nontemporal_store(v, to);
+    else *to = v;
+}
+
 int lane_group(int64_t units) {   // lanes per row: the power of two that covers it, at most a wavefront
     int g = 1;
     while (g < units && g < kWave) g <<= 1;
@@ -82,7 +90,7 @@ template <int G, int R, bool BF>
 __global__ void __launch_bounds__(256) k_embedding(const u32x4e *__restrict__ table, int64_t n_rows, int64_t ld16,
                                                    int32_t units, int64_t d, const int32_t *__restrict__ ids,
                                                    const int32_t *__restrict__ n_dev, int64_t n, float scale,
-                                                   u32x4e *__restrict__ out, int64_t out_ld16) {
+                                                   u32x4e *__restrict__ out, int64_t out_ld16, bool streamed) {
     constexpr int RPW = kWave / G;
     const int lane = lane_id(), sub = lane / G, c0 = lane % G;
     if (n_dev) n = std::min<int64_t>(n, std::max<int32_t>(*n_dev, 0));
@@ -107,7 +115,7 @@ __global__ void __launch_bounds__(256) k_embedding(const u32x4e *__restrict__ ta
 #pragma unroll
                 for (int e = 0; e < Unit<BF>::N; ++e) v.v[e] *= scale;
                 if (id[r] < 0 || id[r] >= n_rows) v.zero();
-                out[(i0 + r * groups) * out_ld16 + c] = v.to((int64_t)c * Unit<BF>::N, d);
+                store(&out[(i0 + r * groups) * out_ld16 + c], v.to((int64_t)c * Unit<BF>::N, d), streamed);
             }
         }
     }
@@ -120,16 +128,17 @@ void launch_embedding(const void *table, int64_t n_rows, int64_t ld_bytes, int64
     const int g = lane_group(units);
     KernelTimer t("embedding", s);
     const unsigned grid = grid_for(n, 256 / g * 4, 4096);
+    const bool streamed = n * units * 16 > kStreamBytes;
 #define GNNAV_L(GV)                                                                                                 \
     case GV:                                                                                                        \
         if (bf16)                                                                                                   \
             hipLaunchKernelGGL((k_embedding<GV, 4, true>), dim3(grid), dim3(256), 0, s, (const u32x4e *)table,      \
                                n_rows, ld_bytes / 16, units, d, ids, n_dev, n, scale, (u32x4e *)out,                \
-                               out_ld_bytes / 16);                                                                  \
+                               out_ld_bytes / 16, streamed);                                                        \
         else                                                                                                        \
             hipLaunchKernelGGL((k_embedding<GV, 4, false>), dim3(grid), dim3(256), 0, s, (const u32x4e *)table,     \
                                n_rows, ld_bytes / 16, units, d, ids, n_dev, n, scale, (u32x4e *)out,                \
-                               out_ld_bytes / 16);                                                                  \
+                               out_ld_bytes / 16, streamed);                                                        \
         break
     switch (g) {
         GNNAV_L(1);
@@ -276,29 +285,29 @@ __global__ void __launch_bounds__(256) k_embedding_grad_few(const u32x4e *__rest
 
 // ------------------------------------------------------- gradient: the sort
 // Stable radix sort of (id, position), digits of at most 10 bits, least
-// significant first.  A tile is kSortThreads * iters pairs; there are at most
-// kSortTiles tiles, so every scatter workgroup adds up all tiles' digit counts by
+// significant first.  A tile is a number of rounds of 4,096 pairs (one round up to
+// a million); there are at most kIdTiles tiles, so every scatter workgroup adds up all tiles' digit counts by
 // itself: a pass is two launches.  (Counting the next pass's digits from the scatter, with global additions, is one
 // launch less, but popular ids meet at a few counters: 55 us where the two launches take 25.)  Ids outside [0, n_rows) become n_rows and sort to the end.
 namespace {
 
 constexpr int kIdThreads = 1024;
 constexpr int kIdWaves = kIdThreads / kWave;
+constexpr int kIdIters = 4;
+constexpr int64_t kIdRound = kIdThreads * kIdIters;
 constexpr int64_t kIdTiles = 256;
 constexpr int kMaxBits = 10;
 
 struct IdSortPlan {
-    int passes, bits, iters;
+    int passes, bits, rounds;
     int64_t tiles;
     IdSortPlan(int64_t n, int64_t n_rows) {
         int all = 1;
         while (all < 32 && (int64_t(1) << all) <= n_rows) ++all;   // values 0 .. n_rows
         passes = (all + kMaxBits - 1) / kMaxBits;
-        bits = (all + passes - 1) / passes;
-        // four rounds of 1,024 pairs a tile (a round is a few barriers), more only past 256 tiles
-        iters = 4;
-        while ((n + (int64_t)kIdThreads * iters - 1) / ((int64_t)kIdThreads * iters) > kIdTiles) iters *= 2;
-        tiles = std::max<int64_t>(1, (n + (int64_t)kIdThreads * iters - 1) / ((int64_t)kIdThreads * iters));
+        bits = std::max(2, (all + passes - 1) / passes);
+        rounds = (int)std::max<int64_t>(1, (n + kIdTiles * kIdRound - 1) / (kIdTiles * kIdRound));
+        tiles = std::max<int64_t>(1, (n + kIdRound * rounds - 1) / (kIdRound * rounds));
     }
     int64_t digits() const { return int64_t(1) << bits; }
 };
@@ -311,9 +320,9 @@ __device__ __forceinline__ uint32_t sort_key(int32_t id, int64_t n_rows) {
 
 // Digit counts of a pass; in the first one (ids as given), workgroups past the tiles clear the flags.
 template <bool FIRST>
-__global__ void __launch_bounds__(kIdThreads) k_id_count(const int32_t *__restrict__ keys,
+__global__ void __launch_bounds__(kIdThreads) k_id_count(const void *__restrict__ in,
                                                          const int32_t *__restrict__ n_dev, int64_t n, int64_t n_rows,
-                                                         int shift, int bits, int iters, int32_t *__restrict__ hist,
+                                                         int shift, int bits, int rounds, int32_t *__restrict__ hist,
                                                          int64_t tiles, uint32_t *__restrict__ flags,
                                                          int64_t flag_words) {
     __shared__ int32_t h[1 << kMaxBits];
@@ -322,10 +331,12 @@ __global__ void __launch_bounds__(kIdThreads) k_id_count(const int32_t *__restri
     if (blockIdx.x < tiles) {
         h[threadIdx.x] = 0;
         __syncthreads();
-#pragma unroll 4
-        for (int it = 0; it < iters; ++it) {
-            const int64_t e = ((int64_t)blockIdx.x * iters + it) * kIdThreads + threadIdx.x;
-            if (e < n) atomicAdd(&h[((FIRST ? sort_key(keys[e], n_rows) : (uint32_t)keys[e]) >> shift) & (digits - 1)], 1);
+#pragma unroll 8
+        for (int it = 0; it < kIdIters * rounds; ++it) {
+            const int64_t e = ((int64_t)blockIdx.x * kIdIters * rounds + it) * kIdThreads + threadIdx.x;
+            if (e >= n) continue;
+            const uint32_t key = FIRST ? sort_key(((const int32_t *)in)[e], n_rows) : (uint32_t)((const int2 *)in)[e].x;
+            atomicAdd(&h[(key >> shift) & (digits - 1)], 1);
         }
         __syncthreads();
         if (threadIdx.x < digits) hist[blockIdx.x * digits + threadIdx.x] = h[threadIdx.x];
@@ -337,40 +348,40 @@ __global__ void __launch_bounds__(kIdThreads) k_id_count(const int32_t *__restri
 
 // flags (first pass only, nullable): a byte per row of the table, set where its id occurs.
 template <bool FIRST>
-__global__ void __launch_bounds__(kIdThreads) k_id_scatter(const int32_t *__restrict__ keys_in,
-                                                           const int32_t *__restrict__ vals_in,
+__global__ void __launch_bounds__(kIdThreads) k_id_scatter(const void *__restrict__ in,
                                                            const int32_t *__restrict__ n_dev, int64_t n,
-                                                           int64_t n_rows, int shift, int bits, int iters,
+                                                           int64_t n_rows, int shift, int bits, int rounds,
                                                            const int32_t *__restrict__ hist, int64_t tiles,
-                                                           int32_t *__restrict__ keys_out,
-                                                           int32_t *__restrict__ vals_out,
+                                                           int2 *__restrict__ out,
                                                            uint8_t *__restrict__ flags) {
     __shared__ int32_t run[1 << kMaxBits];
-    __shared__ int32_t cnt[kIdWaves][1 << kMaxBits];
+    __shared__ __align__(16) int32_t cnt[kIdWaves][1 << kMaxBits];
     __shared__ int32_t scratch[kIdWaves];
     if (n_dev) n = std::min<int64_t>(n, std::max<int32_t>(*n_dev, 0));
-    const int64_t base = (int64_t)blockIdx.x * kIdThreads * iters;
+    const int64_t base = (int64_t)blockIdx.x * kIdRound * rounds;
     if (base >= n) return;
     const int lane = lane_id(), wid = threadIdx.x / kWave, digits = 1 << bits;
-    // a digit's count in all tiles and in those before this one: the tiles dealt to the threads that share a digit
+    // a digit's count in all tiles and in those before this one: four digits a thread, the tiles dealt to the threads that
+    // share them
     int32_t all = 0, before = 0;
     {
-        const int dgt = threadIdx.x & (digits - 1), first = threadIdx.x >> bits, step = kIdThreads >> bits;
+        typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
+        const int quads = digits / 4, quad = threadIdx.x & (quads - 1), first = threadIdx.x / quads, step = kIdThreads / quads;
+        i32x4 a = {0, 0, 0, 0}, b = {0, 0, 0, 0};
 #pragma unroll 16
         for (int t = first; t < (int)tiles; t += step) {
-            const int32_t c = hist[t * digits + dgt];
-            all += c;
-            before += t < (int)blockIdx.x ? c : 0;
+            const i32x4 c = ((const i32x4 *)hist)[t * quads + quad];
+            a += c;
+            if (t < (int)blockIdx.x) b += c;
         }
-        int32_t *sum = &cnt[0][0];
-        sum[2 * threadIdx.x] = all;
-        sum[2 * threadIdx.x + 1] = before;
+        int32_t *sum = &cnt[0][0];   // [step][digits] twice, 4 * kIdThreads each
+        ((i32x4 *)sum)[threadIdx.x] = a;
+        ((i32x4 *)sum)[kIdThreads + threadIdx.x] = b;
         __syncthreads();
-        for (int q = 1; q < step && (int)threadIdx.x < digits; ++q) {
-            all += sum[2 * (threadIdx.x + q * digits)];
-            before += sum[2 * (threadIdx.x + q * digits) + 1];
+        for (int q = 0; q < step && (int)threadIdx.x < digits; ++q) {
+            all += sum[q * digits + threadIdx.x];
+            before += sum[4 * kIdThreads + q * digits + threadIdx.x];
         }
-        if ((int)threadIdx.x >= digits) all = before = 0;
         __syncthreads();
         if ((int)threadIdx.x < digits)
 #pragma unroll
@@ -381,47 +392,60 @@ __global__ void __launch_bounds__(kIdThreads) k_id_scatter(const int32_t *__rest
     if ((int)threadIdx.x < digits) run[threadIdx.x] = off;
     __syncthreads();
     const uint64_t below = (1ull << lane) - 1ull;
-    for (int it = 0; it < iters; ++it) {
-        const int64_t e = base + (int64_t)it * kIdThreads + threadIdx.x;
-        if (base + (int64_t)it * kIdThreads >= n) break;
-        const bool valid = e < n;
-        uint32_t key = 0;
-        int32_t val = 0;
-        if (valid) {
-            if constexpr (FIRST) {
-                key = sort_key(keys_in[e], n_rows);
-                val = (int32_t)e;
-                if (flags && key < (uint32_t)n_rows) flags[key] = 1;
-            } else {
-                key = (uint32_t)keys_in[e];
-                val = vals_in[e];
+    for (int r = 0; r < rounds; ++r) {
+        const int64_t at = base + (int64_t)r * kIdRound;
+        if (at >= n) break;
+        // a wavefront's run of the round: each pair's place among the wavefront's of its digit
+        uint32_t key[kIdIters];
+        int32_t val[kIdIters], place[kIdIters];
+#pragma unroll
+        for (int it = 0; it < kIdIters; ++it) {
+            const int64_t e = at + (wid * kIdIters + it) * kWave + lane;
+            key[it] = 0;
+            val[it] = (int32_t)e;
+            if (e < n) {
+                if constexpr (FIRST) {
+                    key[it] = sort_key(((const int32_t *)in)[e], n_rows);
+                } else {
+                    const int2 p = ((const int2 *)in)[e];
+                    key[it] = (uint32_t)p.x;
+                    val[it] = p.y;
+                }
             }
         }
-        const int dg = (int)(key >> shift) & (digits - 1);
-        uint64_t m = __ballot(valid);
-        for (int bit = 0; bit < bits; ++bit) {
-            const uint64_t ones = __ballot((dg >> bit) & 1);
-            m &= ((dg >> bit) & 1) ? ones : ~ones;
+#pragma unroll
+        for (int it = 0; it < kIdIters; ++it) {
+            const bool valid = at + (wid * kIdIters + it) * kWave + lane < n;
+            if (FIRST && flags && valid && key[it] < (uint32_t)n_rows) flags[key[it]] = 1;
+            const int dg = (int)(key[it] >> shift) & (digits - 1);
+            uint64_t m = __ballot(valid);
+            for (int bit = 0; bit < bits; ++bit) {
+                const uint64_t ones = __ballot((dg >> bit) & 1);
+                m &= ((dg >> bit) & 1) ? ones : ~ones;
+            }
+            const int rank = __popcll(m & below);
+            const int32_t earlier = valid ? cnt[wid][dg] : 0;
+            if (valid && rank == 0) cnt[wid][dg] = earlier + __popcll(m);
+            place[it] = earlier + rank;
         }
-        const int rank = __popcll(m & below);
-        if (valid && rank == 0) cnt[wid][dg] = __popcll(m);
         __syncthreads();
         if ((int)threadIdx.x < digits) {   // exclusive sums over the wavefronts, from the digit's place
-            int32_t at = run[threadIdx.x];
+            int32_t to = run[threadIdx.x];
 #pragma unroll
             for (int w = 0; w < kIdWaves; ++w) {
                 const int32_t c = cnt[w][threadIdx.x];
-                cnt[w][threadIdx.x] = at;
-                at += c;
+                cnt[w][threadIdx.x] = to;
+                to += c;
             }
-            run[threadIdx.x] = at;
+            run[threadIdx.x] = to;
         }
         __syncthreads();
-        if (valid) {
-            const int32_t pos = cnt[wid][dg] + rank;
-            keys_out[pos] = (int32_t)key;
-            vals_out[pos] = val;
-        }
+#pragma unroll
+        for (int it = 0; it < kIdIters; ++it)
+            if (at + (wid * kIdIters + it) * kWave + lane < n) {
+                const int32_t pos = cnt[wid][(key[it] >> shift) & (digits - 1)] + place[it];
+                out[pos] = make_int2((int32_t)key[it], val[it]);
+            }
         __syncthreads();
         if ((int)threadIdx.x < digits)
 #pragma unroll
@@ -440,12 +464,11 @@ constexpr int kStretch = 64;
 
 template <int G, int Q, bool BF>
 __global__ void __launch_bounds__(256) k_embedding_grad(const u32x4e *__restrict__ dout, int64_t ld16, int32_t units,
-                                                        int64_t d, const int32_t *__restrict__ keys,
-                                                        const int32_t *__restrict__ vals,
+                                                        int64_t d, const int2 *__restrict__ pairs,
                                                         const int32_t *__restrict__ n_dev, int64_t n, float scale,
                                                         bool accumulate, u32x4e *__restrict__ dtable, int64_t n_rows,
                                                         int64_t table_ld16, float *__restrict__ part,
-                                                        const uint8_t *__restrict__ flags, int64_t blocks) {
+                                                        const uint8_t *__restrict__ flags, int64_t blocks, bool streamed) {
     constexpr int RPW = kWave / G, N = Unit<BF>::N;
     const int lane = lane_id(), sub = lane / G, cl = lane % G;
     if (n_dev) n = std::min<int64_t>(n, std::max<int32_t>(*n_dev, 0));
@@ -469,7 +492,7 @@ __global__ void __launch_bounds__(256) k_embedding_grad(const u32x4e *__restrict
                 if (row >= 0)
 #pragma unroll
                     for (int q = 0; q < Q; ++q)
-                        if (c0 + q * G < units) dtable[(r0 + row) * table_ld16 + c0 + q * G] = u32x4e{0, 0, 0, 0};
+                        if (c0 + q * G < units) store(&dtable[(r0 + row) * table_ld16 + c0 + q * G], u32x4e{0, 0, 0, 0}, streamed);
             }
         }
         return;
@@ -477,7 +500,7 @@ __global__ void __launch_bounds__(256) k_embedding_grad(const u32x4e *__restrict
     const int64_t st = ((int64_t)blockIdx.x * 4 + threadIdx.x / kWave) * RPW + sub;
     const int64_t b = st * kStretch, e = std::min<int64_t>(b + kStretch, n);
     const int64_t padded = (int64_t)units * N;
-    const int32_t before = b > 0 && b < n ? keys[b - 1] : -1, after = e < n && b < n ? keys[e] : -1;
+    const int32_t before = b > 0 && b < n ? pairs[b - 1].x : -1, after = e < n && b < n ? pairs[e].x : -1;
     Unit<BF> acc[Q];
 #pragma unroll
     for (int q = 0; q < Q; ++q) acc[q].zero();
@@ -494,7 +517,7 @@ __global__ void __launch_bounds__(256) k_embedding_grad(const u32x4e *__restrict
                 if (accumulate) o.from(*to);
 #pragma unroll
                 for (int x = 0; x < N; ++x) o.v[x] += scale * acc[q].v[x];
-                *to = o.to((int64_t)c * N, d);
+                store(to, o.to((int64_t)c * N, d), streamed);
             }
         } else {
             float *to = part + (2 * st + (began ? 1 : 0)) * padded;
@@ -509,15 +532,16 @@ __global__ void __launch_bounds__(256) k_embedding_grad(const u32x4e *__restrict
         }
     };
     constexpr int U = Q == 1 ? 8 : 4;   // rows in flight; their ids are read one round ahead
-    int32_t cur = b < n ? keys[b] : -1;
+    int32_t cur = b < n ? pairs[b].x : -1;
     bool began = b < n && cur != before;
     int32_t key[U], row[U];
     auto ids = [&](int i0) {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int64_t p = b + i0 + u;
-            key[u] = p < e ? keys[p] : -1;
-            row[u] = p < e ? vals[p] : 0;
+            const int2 pair = p < e ? pairs[p] : make_int2(-1, 0);
+            key[u] = pair.x;
+            row[u] = pair.y;
         }
     };
     ids(0);
@@ -559,7 +583,7 @@ __global__ void __launch_bounds__(256) k_embedding_grad(const u32x4e *__restrict
 constexpr int kJoinWaves = 8, kJoinLong = 16;
 
 template <bool BF>
-__global__ void __launch_bounds__(64 * kJoinWaves) k_embedding_grad_join(const int32_t *__restrict__ keys,
+__global__ void __launch_bounds__(64 * kJoinWaves) k_embedding_grad_join(const int2 *__restrict__ pairs,
                                                                          const int32_t *__restrict__ n_dev, int64_t n,
                                                                          int32_t units, int64_t d, float scale,
                                                                          bool accumulate, u32x4e *__restrict__ dtable,
@@ -605,12 +629,12 @@ __global__ void __launch_bounds__(64 * kJoinWaves) k_embedding_grad_join(const i
         const int64_t st = base + wid, b = st * kStretch, e = b + kStretch;
         int32_t rest = 0;   // stretches after this one that the id goes on in
         if (e < n) {
-            const int32_t id = keys[e - 1];
-            const bool begins = !(keys[b] == id && b > 0 && keys[b - 1] == id);
-            if (id < n_rows && begins && keys[e] == id)
+            const int32_t id = pairs[e - 1].x;
+            const bool begins = !(pairs[b].x == id && b > 0 && pairs[b - 1].x == id);
+            if (id < n_rows && begins && pairs[e].x == id)
                 for (;;) {
                     const int64_t p = (st + 1 + rest + lane) * kStretch;
-                    const uint64_t on = __ballot(p < n && keys[p < n ? p : n - 1] == id);
+                    const uint64_t on = __ballot(p < n && pairs[p < n ? p : n - 1].x == id);
                     if (on != ~0ull) {
                         rest += __builtin_ctzll(~on);
                         break;
@@ -623,7 +647,7 @@ __global__ void __launch_bounds__(64 * kJoinWaves) k_embedding_grad_join(const i
             for (int32_t c = lane; c < units; c += kWave) {
                 float acc[N];
                 add(acc, st, 0, rest, c, true);
-                put(acc, keys[e - 1], c);
+                put(acc, pairs[e - 1].x, c);
             }
         __syncthreads();
         for (int w = 0; w < kJoinWaves; ++w) {
@@ -644,7 +668,7 @@ __global__ void __launch_bounds__(64 * kJoinWaves) k_embedding_grad_join(const i
                     for (int v = 1; v < kJoinWaves; ++v)
 #pragma unroll
                         for (int x = 0; x < N; ++x) acc[x] += sums[v][lane][x];
-                    put(acc, keys[(from + 1) * kStretch - 1], c);
+                    put(acc, pairs[(from + 1) * kStretch - 1].x, c);
                 }
                 __syncthreads();
             }
@@ -654,10 +678,10 @@ __global__ void __launch_bounds__(64 * kJoinWaves) k_embedding_grad_join(const i
 }
 
 namespace {
-// Workspace of the gradient: two (id, position) lists, the digit counts of a
+// Workspace of the gradient: two lists of (id, position), the digit counts of a
 // pass, a byte per table row, the part sums.
 struct GradWorkspace {
-    size_t keys[2], vals[2], hist, flags, part, total;
+    size_t pairs[2], hist, flags, part, total;
     GradWorkspace(int64_t n, int64_t n_rows, int64_t d, bool bf16) {
         const IdSortPlan p(n, n_rows);
         const int64_t units = (d * (bf16 ? 2 : 4) + 15) / 16, padded = units * (bf16 ? 8 : 4);
@@ -667,10 +691,7 @@ struct GradWorkspace {
             at += (bytes + 255) / 256 * 256;
             return here;
         };
-        for (int k = 0; k < 2; ++k) {
-            keys[k] = take((size_t)n * 4);
-            vals[k] = take((size_t)n * 4);
-        }
+        for (int k = 0; k < 2; ++k) pairs[k] = take((size_t)n * 8);
         hist = take((size_t)(p.tiles * p.digits()) * 4);
         flags = take((size_t)n_rows);
         part = take((size_t)(2 * ((n + kStretch - 1) / kStretch) * padded) * 4);
@@ -727,47 +748,48 @@ void launch_embedding_backward(const void *dout, int64_t ld_bytes, const int32_t
     auto i32 = [&](size_t at) { return (int32_t *)(base + at); };
     int32_t *hist = i32(w.hist);
     uint8_t *flags = accumulate ? nullptr : (uint8_t *)(base + w.flags);
-    const int32_t *kin = ids, *vin = nullptr;
+    const void *in_ids = ids;   // the list to sort, then what the last pass wrote
     {
         KernelTimer t("embedding_sort", s);
         const int64_t words = accumulate ? 0 : (n_rows + 3) / 4;
         for (int k = 0; k < p.passes; ++k) {
-            int32_t *kout = i32(w.keys[k & 1]), *vout = i32(w.vals[k & 1]);
+            int2 *to = (int2 *)(base + w.pairs[k & 1]);
             const int shift = k * p.bits;
             if (k == 0) {
                 hipLaunchKernelGGL(k_id_count<true>, dim3((unsigned)p.tiles + (words ? grid_for(words, kIdThreads, 256) : 0)),
-                                   dim3(kIdThreads), 0, s, kin, n_dev, n, n_rows, shift, p.bits, p.iters, hist, p.tiles,
+                                   dim3(kIdThreads), 0, s, in_ids, n_dev, n, n_rows, shift, p.bits, p.rounds, hist, p.tiles,
                                    (uint32_t *)flags, words);
-                hipLaunchKernelGGL(k_id_scatter<true>, dim3((unsigned)p.tiles), dim3(kIdThreads), 0, s, kin, vin, n_dev,
-                                   n, n_rows, shift, p.bits, p.iters, hist, p.tiles, kout, vout, flags);
+                hipLaunchKernelGGL(k_id_scatter<true>, dim3((unsigned)p.tiles), dim3(kIdThreads), 0, s, in_ids, n_dev,
+                                   n, n_rows, shift, p.bits, p.rounds, hist, p.tiles, to, flags);
             } else {
-                hipLaunchKernelGGL(k_id_count<false>, dim3((unsigned)p.tiles), dim3(kIdThreads), 0, s, kin, n_dev, n,
-                                   n_rows, shift, p.bits, p.iters, hist, p.tiles, nullptr, 0);
-                hipLaunchKernelGGL(k_id_scatter<false>, dim3((unsigned)p.tiles), dim3(kIdThreads), 0, s, kin, vin, n_dev,
-                                   n, n_rows, shift, p.bits, p.iters, hist, p.tiles, kout, vout, nullptr);
+                hipLaunchKernelGGL(k_id_count<false>, dim3((unsigned)p.tiles), dim3(kIdThreads), 0, s, in_ids, n_dev, n,
+                                   n_rows, shift, p.bits, p.rounds, hist, p.tiles, nullptr, 0);
+                hipLaunchKernelGGL(k_id_scatter<false>, dim3((unsigned)p.tiles), dim3(kIdThreads), 0, s, in_ids, n_dev,
+                                   n, n_rows, shift, p.bits, p.rounds, hist, p.tiles, to, nullptr);
             }
-            kin = kout;
-            vin = vout;
+            in_ids = to;
         }
     }
     float *part = (float *)(base + w.part);
+    const int2 *pairs = (const int2 *)in_ids;
     {
         KernelTimer t("embedding_grad", s);
         const int64_t stretches = (n + kStretch - 1) / kStretch;
         const int64_t blocks = (stretches + 4 * (kWave / g) - 1) / (4 * (kWave / g));
         const unsigned zeros = accumulate ? 0u : grid_for(n_rows, 256, 1024);
+        const bool streamed = n_rows * units * 16 > kStreamBytes;
         const unsigned slabs = (unsigned)((units + 3 * kWave - 1) / (3 * kWave));
         const int q = (int)((units + g * slabs - 1) / (g * slabs));
 #define GNNAV_L(GV, QV)                                                                                               \
     do {                                                                                                              \
         if (bf16)                                                                                                     \
             hipLaunchKernelGGL((k_embedding_grad<GV, QV, true>), dim3((unsigned)blocks + zeros, slabs), dim3(256), 0, \
-                               s, in, ld16, units, d, kin, vin, n_dev, n, scale, accumulate, out, n_rows, tld16,      \
-                               part, flags, blocks);                                                                  \
+                               s, in, ld16, units, d, pairs, n_dev, n, scale, accumulate, out, n_rows, tld16,      \
+                               part, flags, blocks, streamed);                                                                  \
         else                                                                                                          \
             hipLaunchKernelGGL((k_embedding_grad<GV, QV, false>), dim3((unsigned)blocks + zeros, slabs), dim3(256),   \
-                               0, s, in, ld16, units, d, kin, vin, n_dev, n, scale, accumulate, out, n_rows, tld16,   \
-                               part, flags, blocks);                                                                  \
+                               0, s, in, ld16, units, d, pairs, n_dev, n, scale, accumulate, out, n_rows, tld16,   \
+                               part, flags, blocks, streamed);                                                                  \
     } while (0)
         switch (g) {
             case 1: GNNAV_L(1, 1); break;
@@ -788,10 +810,10 @@ void launch_embedding_backward(const void *dout, int64_t ld_bytes, const int32_t
         KernelTimer t("embedding_grad_join", s);
         const unsigned grid = grid_for((n + kStretch - 1) / kStretch, kJoinWaves, 2048);
         if (bf16)
-            hipLaunchKernelGGL(k_embedding_grad_join<true>, dim3(grid), dim3(64 * kJoinWaves), 0, s, kin, n_dev, n, units, d,
+            hipLaunchKernelGGL(k_embedding_grad_join<true>, dim3(grid), dim3(64 * kJoinWaves), 0, s, pairs, n_dev, n, units, d,
                                scale, accumulate, out, n_rows, tld16, part);
         else
-            hipLaunchKernelGGL(k_embedding_grad_join<false>, dim3(grid), dim3(64 * kJoinWaves), 0, s, kin, n_dev, n, units, d,
+            hipLaunchKernelGGL(k_embedding_grad_join<false>, dim3(grid), dim3(64 * kJoinWaves), 0, s, pairs, n_dev, n, units, d,
                                scale, accumulate, out, n_rows, tld16, part);
     }
     GNNAV_HIP(hipGetLastError());
