@@ -495,7 +495,7 @@ gnnav_status gnnav_weight_grad(const float *self_dev, int64_t ld_self, const flo
  * contents do not matter.  No call allocates; calls that use different
  * workspaces may overlap.
  * Errors: E_INVALID (null pointers, sizes, strides, alignment, workspace),
- * E_CAPACITY (a size beyond int32), E_DEVICE.  Asynchronous.               */
+ * E_CAPACITY (a size beyond int32, d beyond 2^20), E_DEVICE.  Asynchronous. */
 gnnav_status gnnav_embedding(const void *table_dev, int64_t n_rows, int64_t ld_table, int64_t d,
                              gnnav_dtype dt, const int32_t *ids_dev, const int32_t *n_ids_dev,
                              int64_t n_ids, float scale, void *out_dev, int64_t ld_out, void *stream);
@@ -532,7 +532,7 @@ gnnav_status gnnav_embedding_backward(const void *dout_dev, int64_t ld_dout, con
  * piece of the classes: some multiples of m x d, and less than 2 GiB for the
  * piece, however many classes there are (m <= 32: n_classes bytes more).  No call allocates.
  * Errors: E_INVALID (null pointers, sizes, strides, alignment, workspace),
- * E_CAPACITY (a size beyond int32), E_DEVICE.  Asynchronous.               */
+ * E_CAPACITY (a size beyond int32, d beyond 2^20), E_DEVICE.  Asynchronous. */
 int64_t gnnav_linear_xent_workspace(int64_t m, int64_t n_classes, int64_t d, gnnav_dtype dt, int32_t grads);
 gnnav_status gnnav_linear_xent(const void *h_dev, int64_t ld_h, int64_t m, const void *w_dev, int64_t ld_w,
                                int64_t n_classes, int64_t d, gnnav_dtype dt, const int32_t *labels_dev,

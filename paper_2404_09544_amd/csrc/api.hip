@@ -1591,6 +1591,7 @@ void check_workspace(const void *ws, int64_t bytes, size_t need) {
                 "workspace must be on a 256-byte boundary");
 }
 bool dtype_ok(gnnav_dtype dt) { return dt == GNNAV_F32 || dt == GNNAV_BF16; }
+constexpr int64_t kMaxWidth = int64_t(1) << 20;   // columns of a row: the grids' second dimension covers them
 }  // namespace
 
 extern "C" gnnav_status gnnav_embedding(const void *table_dev, int64_t n_rows, int64_t ld_table, int64_t d,
@@ -1599,7 +1600,8 @@ extern "C" gnnav_status gnnav_embedding(const void *table_dev, int64_t n_rows, i
     return guarded([&] {
         GNNAV_CHECK(dtype_ok(dt), GNNAV_E_INVALID, "bad dtype");
         GNNAV_CHECK(n_rows >= 0 && n_ids >= 0 && d > 0, GNNAV_E_INVALID, "negative size or d <= 0");
-        GNNAV_CHECK(n_rows <= INT32_MAX && n_ids <= INT32_MAX && d <= INT32_MAX, GNNAV_E_CAPACITY, "sizes beyond int32");
+        GNNAV_CHECK(n_rows <= INT32_MAX && n_ids <= INT32_MAX && d <= kMaxWidth, GNNAV_E_CAPACITY,
+                    "sizes beyond int32, or rows wider than 2^20");
         if (n_ids == 0) return;
         const int64_t elt = dt == GNNAV_BF16 ? 2 : 4;
         GNNAV_CHECK(ids_dev, GNNAV_E_INVALID, "NULL ids");
@@ -1611,7 +1613,7 @@ extern "C" gnnav_status gnnav_embedding(const void *table_dev, int64_t n_rows, i
 }
 
 extern "C" int64_t gnnav_embedding_backward_workspace(int64_t n_ids, int64_t n_rows, int64_t d, gnnav_dtype dt) {
-    if (!dtype_ok(dt) || n_ids < 0 || n_rows < 0 || d <= 0 || n_ids > INT32_MAX || n_rows > INT32_MAX || d > INT32_MAX)
+    if (!dtype_ok(dt) || n_ids < 0 || n_rows < 0 || d <= 0 || n_ids > INT32_MAX || n_rows > INT32_MAX || d > kMaxWidth)
         return -1;
     return (int64_t)embedding_backward_workspace(n_ids, n_rows, d, dt == GNNAV_BF16);
 }
@@ -1624,7 +1626,8 @@ extern "C" gnnav_status gnnav_embedding_backward(const void *dout_dev, int64_t l
     return guarded([&] {
         GNNAV_CHECK(dtype_ok(dt), GNNAV_E_INVALID, "bad dtype");
         GNNAV_CHECK(n_rows >= 0 && n_ids >= 0 && d > 0, GNNAV_E_INVALID, "negative size or d <= 0");
-        GNNAV_CHECK(n_rows <= INT32_MAX && n_ids <= INT32_MAX && d <= INT32_MAX, GNNAV_E_CAPACITY, "sizes beyond int32");
+        GNNAV_CHECK(n_rows <= INT32_MAX && n_ids <= INT32_MAX && d <= kMaxWidth, GNNAV_E_CAPACITY,
+                    "sizes beyond int32, or rows wider than 2^20");
         if (n_rows == 0 || (n_ids == 0 && accumulate)) return;
         const int64_t elt = dt == GNNAV_BF16 ? 2 : 4;
         check_rows(dtable_dev, ld_table, d, elt, "dtable");
@@ -1640,7 +1643,7 @@ extern "C" gnnav_status gnnav_embedding_backward(const void *dout_dev, int64_t l
 }
 
 extern "C" int64_t gnnav_linear_xent_workspace(int64_t m, int64_t n_classes, int64_t d, gnnav_dtype dt, int32_t grads) {
-    if (!dtype_ok(dt) || m < 0 || n_classes <= 0 || d <= 0 || m > INT32_MAX || n_classes > INT32_MAX || d > INT32_MAX)
+    if (!dtype_ok(dt) || m < 0 || n_classes <= 0 || d <= 0 || m > INT32_MAX || n_classes > INT32_MAX || d > kMaxWidth)
         return -1;
     return (int64_t)linear_xent_workspace(m, n_classes, d, dt == GNNAV_BF16, grads != 0);
 }
@@ -1653,7 +1656,8 @@ extern "C" gnnav_status gnnav_linear_xent(const void *h_dev, int64_t ld_h, int64
     return guarded([&] {
         GNNAV_CHECK(dtype_ok(dt), GNNAV_E_INVALID, "bad dtype");
         GNNAV_CHECK(m >= 0 && n_classes > 0 && d > 0, GNNAV_E_INVALID, "m < 0, or n_classes or d <= 0");
-        GNNAV_CHECK(m <= INT32_MAX && n_classes <= INT32_MAX && d <= INT32_MAX, GNNAV_E_CAPACITY, "sizes beyond int32");
+        GNNAV_CHECK(m <= INT32_MAX && n_classes <= INT32_MAX && d <= kMaxWidth, GNNAV_E_CAPACITY,
+                    "sizes beyond int32, or rows wider than 2^20");
         GNNAV_CHECK(loss_dev, GNNAV_E_INVALID, "NULL loss");
         const int64_t elt = dt == GNNAV_BF16 ? 2 : 4;
         check_rows(w_dev, ld_w, d, elt, "w");

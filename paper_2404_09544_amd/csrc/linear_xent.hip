@@ -72,16 +72,25 @@ __device__ __forceinline__ bool row_counts(float lse) { return lse < INFINITY ||
 // rows x d (row-major, 16-byte aligned rows) -> PL planes of chunks
 // [chunk][R rows], zeros past rows and d, and in rows whose label is `ignore` or
 // outside [0, n_classes) (labels nullable).  One workgroup: 64 rows x 64 columns
-// through LDS.
+// through LDS.  A launch takes two matrices (the first has `blocks` workgroups of rows).
+struct PackArgs {
+    const void *src;
+    int64_t ld, rows, R;
+    const int32_t *labels;
+    u32x4x *out;
+};
 template <bool BF>
-__global__ void __launch_bounds__(256) k_xent_pack(const void *__restrict__ src, int64_t ld, int64_t rows, int64_t d,
-                                                   const int32_t *__restrict__ labels, int32_t ignore,
-                                                   int64_t n_classes, int64_t R, int64_t chunks,
-                                                   u32x4x *__restrict__ out) {
+__global__ void __launch_bounds__(256) k_xent_pack(const PackArgs first, const PackArgs second, int32_t blocks, int64_t d,
+                                                   int32_t ignore, int64_t n_classes, int64_t chunks) {
+    const bool one = (int32_t)blockIdx.x < blocks;
+    const void *__restrict__ src = one ? first.src : second.src;
+    const int64_t ld = one ? first.ld : second.ld, rows = one ? first.rows : second.rows, R = one ? first.R : second.R;
+    const int32_t *__restrict__ labels = one ? first.labels : second.labels;
+    u32x4x *__restrict__ out = one ? first.out : second.out;
     constexpr int PL = BF ? 1 : 3;
     __shared__ u32x4x tile[PL][8][65];
     const int tid = threadIdx.x;
-    const int64_t r0 = (int64_t)blockIdx.x * 64, c0 = (int64_t)blockIdx.y * 8;
+    const int64_t r0 = (int64_t)(blockIdx.x - (one ? 0 : blocks)) * 64, c0 = (int64_t)blockIdx.y * 8;
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
         const int lr = tid / 8 + 32 * k, lc = tid % 8;
@@ -159,8 +168,13 @@ struct XentArgs {
     // kDw
     void *dw;
     int64_t ld_dw, d;
-    const float *inv_count;
+    float *inv_count;
     bool dw_bf16;
+    // the mean loss, taken by a workgroup of its own of the first kProb launch (-1: none)
+    int32_t loss_block;
+    const float *losses;
+    int32_t ignore;
+    float *loss;
 };
 
 // Wave grid WGM x WGN, each wavefront WMF x WNF MFMA blocks of 32 x 32; BK summed
@@ -530,11 +544,48 @@ __device__ __forceinline__ void xent_tile(const XentArgs &a, int32_t id, u32x4x 
     }
 }
 
+// The mean over the rows that count, in 64 bits and a fixed order, and its weight.  Run by one workgroup.
+template <int THREADS>
+__device__ __forceinline__ void xent_loss(const float *losses, int64_t m, const int32_t *labels, int32_t ignore,
+                                          float *loss, float *inv_count) {
+    __shared__ double part[THREADS / kWave];
+    __shared__ int32_t count[THREADS / kWave];
+    double s = 0.0;
+    int32_t k = 0;
+#pragma unroll 4
+    for (int64_t i = threadIdx.x; i < m; i += THREADS) {
+        s += (double)losses[i];
+        k += labels[i] != ignore;
+    }
+#pragma unroll
+    for (int o = kWave / 2; o > 0; o >>= 1) {
+        s += __shfl_xor(s, o, kWave);
+        k += __shfl_xor(k, o, kWave);
+    }
+    if (lane_id() == 0) {
+        part[threadIdx.x / kWave] = s;
+        count[threadIdx.x / kWave] = k;
+    }
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        for (int w = 1; w < THREADS / kWave; ++w) {
+            s += part[w];
+            k += count[w];
+        }
+        loss[0] = k > 0 ? (float)(s / (double)k) : 0.f;
+        inv_count[0] = k > 0 ? (float)(1.0 / (double)k) : 0.f;
+    }
+}
+
 template <int PL, int WMF, int WNF, int WGM, int WGN, int EPI>
 __global__ void __launch_bounds__(64 * WGM * WGN, 2) k_xent_logits(const XentArgs a) {
     using C = Tile<PL, WMF, WNF, WGM, WGN>;
     __shared__ u32x4x S[C::LDS];
     __shared__ float2 red[EPI == kStats ? WGM * C::BN : 1];
+    if (EPI == kProb && (int32_t)blockIdx.x == a.loss_block) {
+        xent_loss<64 * WGM * WGN>(a.losses, a.m, a.labels, a.ignore, a.loss, a.inv_count);
+        return;
+    }
     xent_tile<PL, WMF, WNF, WGM, WGN, false, false, EPI>(a, blockIdx.x, S, red);
 }
 
@@ -553,6 +604,10 @@ __global__ void __launch_bounds__(256, 2) k_xent_strip(const XentArgs a) {
     static_assert(KS % 2 == 0, "whole copies");
     __shared__ u32x4x S[2 * TILE];
     const int lane = threadIdx.x & 63, wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5, lr = lane & 31;
+    if (EPI == kProb && (int32_t)blockIdx.x == a.loss_block) {
+        xent_loss<256>(a.losses, a.m, a.labels, a.ignore, a.loss, a.inv_count);
+        return;
+    }
     int32_t split, rb, strip;   // row blocks along M, strips along N
     if (!tile_of(a, blockIdx.x, split, rb, strip)) return;
     const int32_t all = (int32_t)(a.a_rows / kStrip), t0 = strip * a.split_steps, T = std::min(a.split_steps, all - t0);
@@ -789,39 +844,6 @@ __global__ void __launch_bounds__(64 * WGM * WGN, 2) k_xent_grads(const XentArgs
 }
 
 // ------------------------------------------------------------- rows and loss
-// The mean over the rows that count, in 64 bits and a fixed order, and its weight.  Run by one workgroup.
-template <int THREADS>
-__device__ __forceinline__ void xent_loss(const float *losses, int64_t m, const int32_t *labels, int32_t ignore,
-                                          float *loss, float *inv_count) {
-    __shared__ double part[THREADS / kWave];
-    __shared__ int32_t count[THREADS / kWave];
-    double s = 0.0;
-    int32_t k = 0;
-#pragma unroll 4
-    for (int64_t i = threadIdx.x; i < m; i += THREADS) {
-        s += (double)losses[i];
-        k += labels[i] != ignore;
-    }
-#pragma unroll
-    for (int o = kWave / 2; o > 0; o >>= 1) {
-        s += __shfl_xor(s, o, kWave);
-        k += __shfl_xor(k, o, kWave);
-    }
-    if (lane_id() == 0) {
-        part[threadIdx.x / kWave] = s;
-        count[threadIdx.x / kWave] = k;
-    }
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        for (int w = 1; w < THREADS / kWave; ++w) {
-            s += part[w];
-            k += count[w];
-        }
-        loss[0] = k > 0 ? (float)(s / (double)k) : 0.f;
-        inv_count[0] = k > 0 ? (float)(1.0 / (double)k) : 0.f;
-    }
-}
-
 // Joins a row's entries [from, tiles]: before the last piece to entry 0 (kFold), then to lse (+inf for a row that
 // does not count) and the row's loss.  ROWS rows a workgroup, the entries dealt to SLICES threads of each.
 // kLoss: there is one workgroup, which takes the mean too.
@@ -1045,7 +1067,8 @@ unsigned ids_of(const XentArgs &a) {   // workgroups of a product, whole rounds 
 // but have fewer workgroups on a unit to fill each other's gaps (4,093 x 169,000 x 256 bf16: both
 // passes 609 us, 128 x 128 595; x 1,024 columns 2,118 and 2,145; fp32 1,024 rows 1,342 and 1,256).
 template <int PL, int EPI>
-void run_logits(XentArgs &a, const XentPlan &plan, int64_t d, int64_t vdim, const char *label, hipStream_t s) {
+void run_logits(XentArgs &a, const XentPlan &plan, int64_t d, int64_t vdim, bool with_loss, const char *label,
+                hipStream_t s) {
     const int64_t ln = plan.ln;
     if constexpr (PL == 1)
         if (plan.strips > 0) {
@@ -1054,10 +1077,12 @@ void run_logits(XentArgs &a, const XentPlan &plan, int64_t d, int64_t vdim, cons
             a.splits = 1;
             a.split_steps = plan.strip_tiles;
             KernelTimer t(label, s);
+            a.loss_block = with_loss ? (int32_t)ids_of(a) : -1;
+            const unsigned grid = ids_of(a) + (with_loss ? 1 : 0);
 #define GNNAV_L(KS)                                                                                                   \
     do {                                                                                                              \
-        if (ln == 256) hipLaunchKernelGGL((k_xent_strip<KS, 2, EPI>), dim3(ids_of(a)), dim3(256), 0, s, a);           \
-        else hipLaunchKernelGGL((k_xent_strip<KS, 1, EPI>), dim3(ids_of(a)), dim3(256), 0, s, a);                     \
+        if (ln == 256) hipLaunchKernelGGL((k_xent_strip<KS, 2, EPI>), dim3(grid), dim3(256), 0, s, a);                \
+        else hipLaunchKernelGGL((k_xent_strip<KS, 1, EPI>), dim3(grid), dim3(256), 0, s, a);                          \
     } while (0)
             if (d <= 64) GNNAV_L(4);
             else if (d <= 128) GNNAV_L(8);
@@ -1068,13 +1093,15 @@ void run_logits(XentArgs &a, const XentPlan &plan, int64_t d, int64_t vdim, cons
     a.m_tiles = (int32_t)(vdim / kVTile);
     a.n_tiles = (int32_t)(a.rows / ln);
     a.splits = 1;
+    a.loss_block = with_loss ? (int32_t)ids_of(a) : -1;
+    const unsigned grid = ids_of(a) + (with_loss ? 1 : 0);
     KernelTimer t(label, s);
     if constexpr (EPI == kProb)
         if (ln == 32) {
-            hipLaunchKernelGGL((k_xent_logits<PL, 1, 1, 4, 1, EPI>), dim3(ids_of(a)), dim3(256), 0, s, a);
+            hipLaunchKernelGGL((k_xent_logits<PL, 1, 1, 4, 1, EPI>), dim3(grid), dim3(256), 0, s, a);
             return;
         }
-    hipLaunchKernelGGL((k_xent_logits<PL, 2, 2, 2, 2, EPI>), dim3(ids_of(a)), dim3(256), 0, s, a);
+    hipLaunchKernelGGL((k_xent_logits<PL, 2, 2, 2, 2, EPI>), dim3(grid), dim3(256), 0, s, a);
 }
 
 // Gradient tiles: bm features x 128 classes for dw, bm x rn rows for dh (rn = 256: 256 x 256 both).  Either product
@@ -1105,17 +1132,17 @@ void xent(const XentPlan &p, const LinearXentArgs &x, hipStream_t s) {
     u32x4x *H = (u32x4x *)(ws + p.h), *W = (u32x4x *)(ws + p.w), *Pb = (u32x4x *)(ws + p.p);
     float *lse = (float *)(ws + p.lse), *inv = (float *)(ws + p.inv), *losses = (float *)(ws + p.losses);
     const int64_t esize = BF ? 2 : 4, k1 = up(x.d, p.bk);
+    // h, with the first piece of w that is packed
+    bool h_packed = false;
     auto pack_w = [&](int64_t v0, int64_t vp) {
         KernelTimer t("xent_pack", s);
-        hipLaunchKernelGGL(k_xent_pack<BF>, dim3((unsigned)(vp / 64), (unsigned)((p.chunks + 7) / 8)), dim3(256), 0, s,
-                           (const char *)x.w + v0 * x.ld_w * esize, x.ld_w, std::min(vp, x.n_classes - v0), x.d,
-                           nullptr, 0, 0, vp, p.chunks, W);
+        const PackArgs rows = {x.h, x.ld_h, x.m, p.rows, x.labels, H};
+        const PackArgs classes = {(const char *)x.w + v0 * x.ld_w * esize, x.ld_w, std::min(vp, x.n_classes - v0), vp, nullptr, W};
+        const unsigned blocks = h_packed ? 0 : (unsigned)((p.rows + 63) / 64);
+        hipLaunchKernelGGL(k_xent_pack<BF>, dim3(blocks + (unsigned)(vp / 64), (unsigned)((p.chunks + 7) / 8)), dim3(256),
+                           0, s, rows, classes, (int32_t)blocks, x.d, x.ignore, x.n_classes, p.chunks);
+        h_packed = true;
     };
-    if (p.ln > 32 || x.dh || x.dw) {
-        KernelTimer t("xent_pack", s);
-        hipLaunchKernelGGL(k_xent_pack<BF>, dim3((unsigned)((p.rows + 63) / 64), (unsigned)((p.chunks + 7) / 8)),
-                           dim3(256), 0, s, x.h, x.ld_h, x.m, x.d, x.labels, x.ignore, x.n_classes, p.rows, p.chunks, H);
-    }
     XentArgs a = {};
     a.n_classes = x.n_classes;
     a.rows = p.rows;
@@ -1125,6 +1152,10 @@ void xent(const XentPlan &p, const LinearXentArgs &x, hipStream_t s) {
     a.label_logit = (float *)(ws + p.label_logit);
     a.lse = lse;
     a.inv_count = inv;
+    a.losses = losses;
+    a.ignore = x.ignore;
+    a.loss = x.loss;
+    a.loss_block = -1;
     auto logits = [&](int64_t v0, int64_t vp) {
         a.v0 = v0;
         a.A = W;
@@ -1157,7 +1188,7 @@ void xent(const XentPlan &p, const LinearXentArgs &x, hipStream_t s) {
         pack_w(v0, vp);
         packed = vp == all;
         logits(v0, vp);
-        run_logits<PL, kStats>(a, p, x.d, vp, "xent_stats", s);
+        run_logits<PL, kStats>(a, p, x.d, vp, false, "xent_stats", s);
         entries = p.strips > 0 ? p.strips : vp / kVTile;
     }
     {
@@ -1170,7 +1201,8 @@ void xent(const XentPlan &p, const LinearXentArgs &x, hipStream_t s) {
             hipLaunchKernelGGL((k_xent_rows<16, 16, kLse>), dim3((unsigned)(p.rows / 16)), dim3(256), 0, s, a.stats,
                                from, entries, p.rows, x.m, x.labels, x.ignore, x.n_classes, a.label_logit, lse, losses,
                                x.row_loss, nullptr, nullptr);
-            hipLaunchKernelGGL(k_xent_loss, dim3(1), dim3(1024), 0, s, losses, x.m, x.labels, x.ignore, x.loss, inv);
+            if (!(x.dh || x.dw))   // otherwise it rides with the first probabilities
+                hipLaunchKernelGGL(k_xent_loss, dim3(1), dim3(1024), 0, s, losses, x.m, x.labels, x.ignore, x.loss, inv);
         }
     }
     if (x.dh || x.dw) {
@@ -1180,7 +1212,7 @@ void xent(const XentPlan &p, const LinearXentArgs &x, hipStream_t s) {
             logits(v0, vp);
             a.p = Pb;
             a.p_plane = vp / 8 * p.rows;
-            run_logits<PL, kProb>(a, p, x.d, vp, "xent_prob", s);
+            run_logits<PL, kProb>(a, p, x.d, vp, v0 == 0 && p.rows > 32, "xent_prob", s);
             XentArgs w = a, h = a;
             w.B = h.B = Pb;
             w.b_rows = h.b_rows = p.rows;
