@@ -493,7 +493,7 @@ gnnav_status gnnav_weight_grad(const float *self_dev, int64_t ld_self, const flo
  * gnnav_embedding_backward_workspace bytes (0 for few ids; -1 for bad
  * arguments; host only) on a 256-byte boundary, used until the work has run; its
  * contents do not matter.  No call allocates; calls that use different
- * workspaces may overlap.
+ * workspaces may overlap.  Outputs must not overlap inputs.
  * Errors: E_INVALID (null pointers, sizes, strides, alignment, workspace),
  * E_CAPACITY (a size beyond int32, d beyond 2^20), E_DEVICE.  Asynchronous. */
 gnnav_status gnnav_embedding(const void *table_dev, int64_t n_rows, int64_t ld_table, int64_t d,
@@ -531,6 +531,7 @@ gnnav_status gnnav_embedding_backward(const void *dout_dev, int64_t ld_dout, con
  * for bad arguments; host only) on a 256-byte boundary.  It holds h and one
  * piece of the classes: some multiples of m x d, and less than 2 GiB for the
  * piece, however many classes there are (m <= 32: n_classes bytes more).  No call allocates.
+ * Outputs must not overlap inputs or each other.
  * Errors: E_INVALID (null pointers, sizes, strides, alignment, workspace),
  * E_CAPACITY (a size beyond int32, d beyond 2^20), E_DEVICE.  Asynchronous. */
 int64_t gnnav_linear_xent_workspace(int64_t m, int64_t n_classes, int64_t d, gnnav_dtype dt, int32_t grads);

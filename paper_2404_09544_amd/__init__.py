@@ -536,7 +536,9 @@ def _workspace(given, need: int, device: int, stream):
     if stream is None:
         t = torch.empty(need, dtype=torch.uint8, device="cuda")
     else:
-        st = stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(int(stream))
+        address = _stream(stream)
+        st = (stream if hasattr(stream, "cuda_stream") else
+              torch.cuda.ExternalStream(address) if address else torch.cuda.default_stream())
         with torch.cuda.stream(st):
             t = torch.empty(need, dtype=torch.uint8, device="cuda")
     return t.data_ptr(), need, t

@@ -10,6 +10,9 @@
 // order, and goes over the tensors again, last element first: what the first
 // pass read last is still in the last-level cache.  The tensors' table travels
 // as a kernel argument, kClipTensors tensors a launch.
+//
+// Bound by HBM, read twice and written once: 400 million bf16 gradients 2.4 GB in
+// 500 us, 4.8 TB/s; two small tensors by their two launches, 9 us.
 #include <algorithm>
 
 #include "common.hpp"
@@ -25,7 +28,7 @@ constexpr int kClipTensors = 96;       // of a launch: the table stays below 4 K
 constexpr int64_t kClipChunk = 16384;  // elements a workgroup takes at a time
 constexpr int64_t kClipParts = 4096;   // part sums, at most (or one per launch)
 // Results larger than this are stored past the caches, which then hold more of the gradients for the second
-// pass: 400 million bf16 gradients 493 us, 461 so (before the second pass went backwards over the launches, 506).
+// pass: 400 million bf16 gradients over and over 493 us, 461 so; over three sets of buffers in turn 506 and 500.
 constexpr int64_t kStreamBytes = int64_t(128) << 20;
 
 struct ClipTable {

@@ -21,8 +21,15 @@
 // no bounds.  fp32 operands are packed as three bf16 planes and multiplied with
 // the six part products of bf16split.hpp; bf16 ones as they are.
 //
-// All three products are one kernel: M (MFMA rows) is the class of the logits and
+// The products are one tile function: M (MFMA rows) is the class of the logits and
 // the feature of the gradients, N (MFMA columns) the row of h, or the class for dw.
+// Narrow bf16 rows have a logit kernel of their own (k_xent_strip), few rows
+// another (k_xent_score).
+//
+// Operations: 2 m V d for each of the two logit passes, dh and dw: 8 m V d, where
+// kept logits would take 6.  8,192 x 65,536 x 1,024 bf16: 4.06 ms, 1,083 TFLOP/s of the
+// 1,307 that a library product of 8,192^3 reaches; 4,093 x 169,000 x 256 bf16 1.53 ms
+// (925); 1,024 x 169,000 x 256 fp32 2.05 ms (1,037 of bf16 part products).
 #include <algorithm>
 #include <cmath>
 
@@ -73,6 +80,7 @@ __device__ __forceinline__ bool row_counts(float lse) { return lse < INFINITY ||
 // [chunk][R rows], zeros past rows and d, and in rows whose label is `ignore` or
 // outside [0, n_classes) (labels nullable).  One workgroup: 64 rows x 64 columns
 // through LDS.  A launch takes two matrices (the first has `blocks` workgroups of rows).
+// Bound by memory: 4,096 + 84,736 bf16 rows of 256 columns 18 us, 5.0 TB/s.
 struct PackArgs {
     const void *src;
     int64_t ld, rows, R;
@@ -289,6 +297,11 @@ __device__ __forceinline__ void stats_of(const XentArgs &a, f32x16x (&acc)[WMF][
     }
 }
 
+// One tile of a product, from packed operands by way of LDS, and what becomes of it.  Bound by the matrix cores at the clock
+// that their power leaves (the same launch on zeros is 1.3 times as fast): 128 x 128 x 1,024 logit tiles 1,037
+// TFLOP/s, 256 x 256 gradient tiles 1,120-1,210, a library product of the same shapes 1,140-1,265.  Fragments that
+// are read and copies that are issued in one burst behind the barrier: 10% slower; higher priority for the
+// products, a fourth stage for 128 x 128 tiles, groups of 4 or 16 tiles: nothing or slower.
 // AT, BT: the operand's rows are summed over.
 template <int PL, int WMF, int WNF, int WGM, int WGN, bool AT, bool BT, int EPI>
 __device__ __forceinline__ void xent_tile(const XentArgs &a, int32_t id, u32x4x *S, float2 *red) {
@@ -489,8 +502,8 @@ __device__ __forceinline__ void xent_tile(const XentArgs &a, int32_t id, u32x4x 
                             for (int y2 = 0; y2 < 2; ++y2) {
                                 const float f0 = acc[i][j][4 * (g + x) + 2 * y2], f1 = acc[i][j][4 * (g + x) + 2 * y2 + 1];
                                 if constexpr (PL == 1) {
-                                    // rounded to the operands' type: half a step, 2^-9 of each p, is what
-                                    // rounding the gradients themselves costs
+                                    // rounded to the operands' type: at most 2^-8 of each p, as the rounding
+                                    // of the gradients themselves costs
                                     w[x][y2] = bf16_pair(f0, f1);
                                 } else {
                                     uint16_t q0[3], q1[3];
@@ -594,7 +607,8 @@ __global__ void __launch_bounds__(64 * WGM * WGN, 2) k_xent_logits(const XentArg
 // rows of h in registers for good (KS steps of 16 columns) and only the classes stream through LDS, 64 at a
 // time, two buffers and one barrier a tile.  A workgroup's four wavefronts hold 128 WNF rows and take a strip
 // of the piece's classes; two workgroups a unit, so that one's exponentials run beside the other's products.
-// A lane's running maximum and sum stay in registers over the strip.
+// A lane's running maximum and sum stay in registers over the strip.  4,096 x 84,736 x 256: statistics 230 us
+// with the tiles above, 167 so (1,063 TFLOP/s); probabilities 345 and 210 (the 694 MB of p go out at 3.3 TB/s).
 constexpr int kStrip = 64;   // classes of a tile
 
 template <int KS, int WNF, int EPI>
@@ -759,7 +773,7 @@ __global__ void __launch_bounds__(256, 2) k_xent_strip(const XentArgs a) {
 
 // The statistics for at most 32 rows: bound by reading w once, so w and h are read as they lie (row-major, into the
 // fragments), without the packing that the tiles above need.  A wavefront takes kFew x 32 classes.  169,000 x 256 bf16, one
-// row: 22 us, 3.9 TB/s.
+// row: 23 us, 3.8 TB/s (a launch of its own to pack h: 3 us more).
 constexpr int kFew = 2, kFewTile = 4 * 32 * kFew;
 
 template <int PL>
@@ -913,7 +927,8 @@ __global__ void __launch_bounds__(1024) k_xent_loss(const float *__restrict__ lo
     xent_loss<1024>(losses, m, labels, ignore, loss, inv_count);
 }
 
-// dh from the splits' parts, in the order the products kept them in.
+// dh from the splits' parts, in the order the products kept them in (each lane's registers side by side, so that
+// parts are written, added to and read in whole lines).
 template <int WMF, int WNF, int WGM, int WGN>
 __global__ void __launch_bounds__(256) k_xent_dh(const f32x4x *__restrict__ part, int64_t total, int32_t splits,
                                                  int64_t split_stride, int32_t m_tiles, int64_t m, int64_t d,
@@ -955,7 +970,7 @@ namespace {
 
 constexpr int64_t kPBytes = int64_t(1) << 30;     // p of a piece, at most (or one tile of classes)
 constexpr int64_t kLogits = int64_t(1) << 32;     // logits of a piece whose p is not kept, at most: its statistics are a 64th of their size
-constexpr int64_t kWBytes = int64_t(512) << 20;   // packed weights of a piece, at most (or one tile)
+constexpr int64_t kWBytes = int64_t(512) << 20;   // packed weights, at most (or one tile): of all pieces, else of one
 
 int64_t up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
 
@@ -966,6 +981,7 @@ struct XentPlan {
     int64_t bm, width, chunks;      // features of a gradient tile, packed columns, their chunks
     int32_t strips, strip_tiles;    // k_xent_strip: strips of a piece, their tiles (0: the other kernels)
     int64_t piece;                  // classes of a piece
+    bool whole;                     // the packed weights of all pieces are kept between the passes
     int32_t splits, split_steps;    // of dh's sum over a piece
     size_t h, w, p, part, stats, label_logit, lse, losses, inv, total;
 
@@ -1047,7 +1063,8 @@ struct XentPlan {
             return here;
         };
         h = take(rows * width * 2 * pl);
-        w = take(ln > 32 || grads ? piece * width * 2 * pl : 0);
+        whole = ln > 32 && all * width * 2 * pl <= kWBytes;
+        w = take(ln > 32 || grads ? (whole ? all : piece) * width * 2 * pl : 0);
         p = take(grads ? rows * piece * 2 * pl : 0);
         part = take(dh ? splits * rows * width * 4 : 0);
         stats = take((1 + (ln == 32 ? all / kFewTile : strips > 0 ? strips : piece / kVTile)) * rows * 8);
@@ -1134,10 +1151,11 @@ void xent(const XentPlan &p, const LinearXentArgs &x, hipStream_t s) {
     const int64_t esize = BF ? 2 : 4, k1 = up(x.d, p.bk);
     // h, with the first piece of w that is packed
     bool h_packed = false;
+    auto weights = [&](int64_t v0) { return W + (p.whole ? v0 * p.chunks * PL : 0); };
     auto pack_w = [&](int64_t v0, int64_t vp) {
         KernelTimer t("xent_pack", s);
         const PackArgs rows = {x.h, x.ld_h, x.m, p.rows, x.labels, H};
-        const PackArgs classes = {(const char *)x.w + v0 * x.ld_w * esize, x.ld_w, std::min(vp, x.n_classes - v0), vp, nullptr, W};
+        const PackArgs classes = {(const char *)x.w + v0 * x.ld_w * esize, x.ld_w, std::min(vp, x.n_classes - v0), vp, nullptr, weights(v0)};
         const unsigned blocks = h_packed ? 0 : (unsigned)((p.rows + 63) / 64);
         hipLaunchKernelGGL(k_xent_pack<BF>, dim3(blocks + (unsigned)(vp / 64), (unsigned)((p.chunks + 7) / 8)), dim3(256),
                            0, s, rows, classes, (int32_t)blocks, x.d, x.ignore, x.n_classes, p.chunks);
@@ -1158,7 +1176,7 @@ void xent(const XentPlan &p, const LinearXentArgs &x, hipStream_t s) {
     a.loss_block = -1;
     auto logits = [&](int64_t v0, int64_t vp) {
         a.v0 = v0;
-        a.A = W;
+        a.A = weights(v0);
         a.a_rows = vp;
         a.a_plane = p.chunks * vp;
         a.B = H;
@@ -1167,7 +1185,6 @@ void xent(const XentPlan &p, const LinearXentArgs &x, hipStream_t s) {
         a.k = k1;
     };
     const int64_t all = up(x.n_classes, kPiece);
-    bool packed = false;   // one piece: packed once for both passes
     bool several = false;  // entry 0 of the statistics holds earlier pieces'
     int64_t entries = 0;   // of the piece
     if (p.ln == 32) {
@@ -1186,7 +1203,6 @@ void xent(const XentPlan &p, const LinearXentArgs &x, hipStream_t s) {
             several = true;
         }
         pack_w(v0, vp);
-        packed = vp == all;
         logits(v0, vp);
         run_logits<PL, kStats>(a, p, x.d, vp, false, "xent_stats", s);
         entries = p.strips > 0 ? p.strips : vp / kVTile;
@@ -1208,7 +1224,7 @@ void xent(const XentPlan &p, const LinearXentArgs &x, hipStream_t s) {
     if (x.dh || x.dw) {
         for (int64_t v0 = 0; v0 < all; v0 += p.piece) {
             const int64_t vp = std::min(p.piece, all - v0);
-            if (!packed) pack_w(v0, vp);
+            if (!p.whole && !(p.piece == all && p.ln > 32)) pack_w(v0, vp);   // otherwise the first pass packed it
             logits(v0, vp);
             a.p = Pb;
             a.p_plane = vp / 8 * p.rows;

@@ -164,6 +164,19 @@ def test_on_several_streams_at_once(G, dtype):
         G.stream_destroy(st)
 
 
+def test_streams_by_address(G):
+    """A stream given as an address, the null stream's among them; workspaces come from torch either way."""
+    import torch
+    a, b, c = (chain_state("f32", 5000, 900, 16, 3) for _ in range(3))
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for s, st in ((a, None), (b, 0), (c, side.cuda_stream)):
+        chain(G, s, stream=st)
+    torch.cuda.synchronize()
+    for k in OUT:
+        assert torch.equal(a[k], b[k]) and torch.equal(a[k], c[k]), k
+
+
 def test_nothing_is_allocated(G):
     """With workspaces given, the library allocates nothing (its allocation hook armed)."""
     import torch
