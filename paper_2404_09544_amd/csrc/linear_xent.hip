@@ -47,7 +47,6 @@ typedef uint32_t u32x4x __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2x __attribute__((ext_vector_type(2)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 
-constexpr int kVTile = 128;    // classes of a logit tile
 constexpr int kPiece = 256;    // pieces of the classes are multiples of this, a whole number of any product's tiles
 constexpr float kLog2e = 1.44269504088896340736f;
 // exp2(x log2e - r log2e) as one multiply-add errs by the rounding of r log2e, less than that of a logit of r's size;
@@ -193,7 +192,7 @@ struct Tile {
     static constexpr int NW = WGM * WGN, BM = 32 * WMF * WGM, BN = 32 * WNF * WGN;
     static constexpr int APC = BM * BK / 8, BPC = BN * BK / 8;   // chunks of a plane of a stage
     static constexpr int STAGE = PL * (APC + BPC);
-    static constexpr int ST = WGN == 4 && WNF == 2 ? 4 : 3, LDS = ST * STAGE;   // stages: two workgroups a unit, or one
+    static constexpr int ST = 3, LDS = ST * STAGE;   // stages
     static_assert(APC % 64 == 0 && BPC % 64 == 0, "whole wavefront copies");
 };
 
@@ -301,7 +300,7 @@ __device__ __forceinline__ void stats_of(const XentArgs &a, f32x16x (&acc)[WMF][
 // that their power leaves (the same launch on zeros is 1.3 times as fast): 128 x 128 x 1,024 logit tiles 1,037
 // TFLOP/s, 256 x 256 gradient tiles 1,120-1,210, a library product of the same shapes 1,140-1,265.  Fragments that
 // are read and copies that are issued in one burst behind the barrier: 10% slower; higher priority for the
-// products, a fourth stage for 128 x 128 tiles, groups of 4 or 16 tiles: nothing or slower.
+// products, a fourth stage, 128 x 128 blocks per wavefront, groups of 4 or 16 tiles: nothing or slower.
 // AT, BT: the operand's rows are summed over.
 template <int PL, int WMF, int WNF, int WGM, int WGN, bool AT, bool BT, int EPI>
 __device__ __forceinline__ void xent_tile(const XentArgs &a, int32_t id, u32x4x *S, float2 *red) {
@@ -409,15 +408,13 @@ __device__ __forceinline__ void xent_tile(const XentArgs &a, int32_t id, u32x4x 
             __builtin_amdgcn_sched_barrier(0);
         }
     };
-    // Makes stage t readable: its copies, of those of up to ST - 2 later stages, are done, everywhere.
+    // Makes stage t readable: its copies are done, everywhere; those of the stage after it may not be.
     auto advance = [&](int32_t t) {
-        const int32_t later = T - 1 - t;
-        if (later >= ST - 2) wait_vm<IN *(ST - 2)>();
-        else if (ST > 3 && later == 1) wait_vm<IN>();
+        if (t + 1 < T) wait_vm<IN *(ST - 2)>();
         else wait_vm<0>();
         lds_barrier();
     };
-    static_assert((ST == 3 || ST == 4) && (BK == 16 || BK == 32), "loop below");
+    static_assert(ST == 3 && (BK == 16 || BK == 32), "loop below");
     auto next = [](int stage) { return stage + 1 == ST ? 0 : stage + 1; };
     // One fragment set is multiplied while the next one is read, across the barrier between two stages.  Once
     // stage t is readable, stage t + ST - 1 is copied into the one read before it, over the products up to the next barrier.
@@ -773,7 +770,7 @@ __global__ void __launch_bounds__(256, 2) k_xent_strip(const XentArgs a) {
 
 // The statistics for at most 32 rows: bound by reading w once, so w and h are read as they lie (row-major, into the
 // fragments), without the packing that the tiles above need.  A wavefront takes kFew x 32 classes.  169,000 x 256 bf16, one
-// row: 23 us, 3.8 TB/s (a launch of its own to pack h: 3 us more).
+// row: 22 us, 3.9 TB/s (a launch of its own to pack h: 3 us more).
 constexpr int kFew = 2, kFewTile = 4 * 32 * kFew;
 
 template <int PL>
@@ -798,7 +795,7 @@ __global__ void __launch_bounds__(256) k_xent_score(const XentArgs a, const void
 #pragma unroll
         for (int r = 0; r < 16; ++r) acc[f][0][r] = 0.f;
     // 16 columns a step, 8 of them this lane's; past d they count as zeros
-    constexpr int U = PL == 1 ? 8 : 4;   // steps in flight
+    constexpr int U = 4;   // steps in flight (8: 2 us more, fewer wavefronts fit)
     for (int64_t k0 = 0; k0 < d; k0 += 16 * U) {
         u32x4x x[U][kFew + 1][X];
 #pragma unroll
@@ -980,7 +977,7 @@ struct XentPlan {
     int64_t ln, rn;                 // rows of a logit tile, of a dh tile (and classes of a dw tile, at least 128)
     int64_t bm, width, chunks;      // features of a gradient tile, packed columns, their chunks
     int32_t strips, strip_tiles;    // k_xent_strip: strips of a piece, their tiles (0: the other kernels)
-    int64_t piece;                  // classes of a piece
+    int64_t piece, vt;              // classes of a piece, of a logit tile
     bool whole;                     // the packed weights of all pieces are kept between the passes
     int32_t splits, split_steps;    // of dh's sum over a piece
     size_t h, w, p, part, stats, label_logit, lse, losses, inv, total;
@@ -1042,6 +1039,9 @@ struct XentPlan {
         piece = std::min(piece, all);
         const int64_t pieces = (all + piece - 1) / piece;
         piece = up((all + pieces - 1) / pieces, kPiece);   // equal ones
+        // fp32 with fewer 128 x 128 tiles than places for them: 64 x 64 (256 x 10,000 x 64 47 -> 41 us, 128 x 5,000 x 256 59 ->
+        // 44; bf16 tiles are too short for it to matter)
+        vt = !bf16 && ln > 32 && piece / 128 * (rows / 128) < 512 ? 64 : 128;
         strips = strip_tiles = 0;
         if (bf16 && m > 32 && d <= 256) {   // two workgroups a unit
             const int64_t t = piece / kStrip, s = std::min(t, std::max<int64_t>(1, 512 / (rows / ln)));
@@ -1067,7 +1067,7 @@ struct XentPlan {
         w = take(ln > 32 || grads ? (whole ? all : piece) * width * 2 * pl : 0);
         p = take(grads ? rows * piece * 2 * pl : 0);
         part = take(dh ? splits * rows * width * 4 : 0);
-        stats = take((1 + (ln == 32 ? all / kFewTile : strips > 0 ? strips : piece / kVTile)) * rows * 8);
+        stats = take((1 + (ln == 32 ? all / kFewTile : strips > 0 ? strips : piece / vt)) * rows * 8);
         label_logit = take(rows * 4);
         lse = take(rows * 4);
         losses = take(rows * 4);
@@ -1107,8 +1107,9 @@ void run_logits(XentArgs &a, const XentPlan &plan, int64_t d, int64_t vdim, bool
 #undef GNNAV_L
             return;
         }
-    a.m_tiles = (int32_t)(vdim / kVTile);
-    a.n_tiles = (int32_t)(a.rows / ln);
+    const bool small = PL == 3 && plan.vt == 64;
+    a.m_tiles = (int32_t)(vdim / plan.vt);
+    a.n_tiles = (int32_t)(a.rows / (small ? 64 : ln));
     a.splits = 1;
     a.loss_block = with_loss ? (int32_t)ids_of(a) : -1;
     const unsigned grid = ids_of(a) + (with_loss ? 1 : 0);
@@ -1116,6 +1117,11 @@ void run_logits(XentArgs &a, const XentPlan &plan, int64_t d, int64_t vdim, bool
     if constexpr (EPI == kProb)
         if (ln == 32) {
             hipLaunchKernelGGL((k_xent_logits<PL, 1, 1, 4, 1, EPI>), dim3(grid), dim3(256), 0, s, a);
+            return;
+        }
+    if constexpr (PL == 3)
+        if (small) {
+            hipLaunchKernelGGL((k_xent_logits<PL, 1, 1, 2, 2, EPI>), dim3(grid), dim3(256), 0, s, a);
             return;
         }
     hipLaunchKernelGGL((k_xent_logits<PL, 2, 2, 2, 2, EPI>), dim3(grid), dim3(256), 0, s, a);
@@ -1205,7 +1211,7 @@ void xent(const XentPlan &p, const LinearXentArgs &x, hipStream_t s) {
         pack_w(v0, vp);
         logits(v0, vp);
         run_logits<PL, kStats>(a, p, x.d, vp, false, "xent_stats", s);
-        entries = p.strips > 0 ? p.strips : vp / kVTile;
+        entries = p.strips > 0 ? p.strips : vp / p.vt;
     }
     {
         KernelTimer t("xent_rows", s);
