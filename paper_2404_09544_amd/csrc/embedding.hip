@@ -457,14 +457,26 @@ __global__ void __launch_bounds__(kIdThreads) k_id_scatter(const void *__restric
 }
 
 // ------------------------------------------------ gradient: stretches of ids
-// A lane group takes kStretch sorted pairs and adds up the rows of equal ids.
+// A lane group takes a stretch of sorted pairs and adds up the rows of equal ids.
 // An id that lies inside the stretch is written at once; the part of one that
 // began earlier goes to part[2 * stretch], of one that begins here and goes on to
 // part[2 * stretch + 1].  Workgroups past the stretches fill the rows of ids that
 // do not occur.  Q units of a row per lane, wider rows in slabs (blockIdx.y).  Bound by HBM: 260,003 rows of
 // 602 fp32 into 233,000, 277 us, 4.3 TB/s; 524,288 skewed ones of 256 bf16 91 us, 3.9 TB/s.  Stretches of 32 ids join
-// more parts (skewed 151 -> 158 us in all), of 128 leave units idle (168).
-constexpr int kStretch = 64;
+// more parts (skewed 151 -> 158 us in all), of 128 leave units idle (168).  Where stretches of 64 are fewer than
+// kFullWaves wavefronts their loads are too few to hide each other: they are halved, to 8 at the least (7,124 ids of
+// 272 bf16 73 -> 37 us in all, 43,847 skewed ones of 100 83 -> 51; kFullWaves of 4,096: 218,815 skewed ones of 584 fp32
+// 158 -> 172).
+constexpr int kStretch = 64, kShortStretch = 8, kFullWaves = 1024;
+
+namespace {
+int stretch_of(int64_t n, int32_t units) {
+    const int64_t per = kWave / lane_group(units);
+    int len = kStretch;
+    while (len > kShortStretch && (n + len * per - 1) / (len * per) < kFullWaves) len /= 2;
+    return len;
+}
+}  // namespace
 
 template <int G, int Q, bool BF>
 __global__ void __launch_bounds__(256) k_embedding_grad(const u32x4e *__restrict__ dout, int64_t ld16, int32_t units,
@@ -472,7 +484,8 @@ __global__ void __launch_bounds__(256) k_embedding_grad(const u32x4e *__restrict
                                                         const int32_t *__restrict__ n_dev, int64_t n, float scale,
                                                         bool accumulate, u32x4e *__restrict__ dtable, int64_t n_rows,
                                                         int64_t table_ld16, float *__restrict__ part,
-                                                        const uint8_t *__restrict__ flags, int64_t blocks, bool streamed) {
+                                                        const uint8_t *__restrict__ flags, int64_t blocks, int32_t stretch,
+                                                        bool streamed) {
     constexpr int RPW = kWave / G, N = Unit<BF>::N;
     const int lane = lane_id(), sub = lane / G, cl = lane % G;
     if (n_dev) n = std::min<int64_t>(n, std::max<int32_t>(*n_dev, 0));
@@ -502,7 +515,7 @@ __global__ void __launch_bounds__(256) k_embedding_grad(const u32x4e *__restrict
         return;
     }
     const int64_t st = ((int64_t)blockIdx.x * 4 + threadIdx.x / kWave) * RPW + sub;
-    const int64_t b = st * kStretch, e = std::min<int64_t>(b + kStretch, n);
+    const int64_t b = st * stretch, e = std::min<int64_t>(b + stretch, n);
     const int64_t padded = (int64_t)units * N;
     const int32_t before = b > 0 && b < n ? pairs[b - 1].x : -1, after = e < n && b < n ? pairs[e].x : -1;
     Unit<BF> acc[Q];
@@ -550,7 +563,7 @@ __global__ void __launch_bounds__(256) k_embedding_grad(const u32x4e *__restrict
     };
     ids(0);
     // the loop's trip count is the same for all lane groups of a wavefront
-    for (int i0 = 0; i0 < kStretch; i0 += U) {
+    for (int i0 = 0; i0 < stretch; i0 += U) {
         u32x4e x[U][Q];
         int32_t now[U];
 #pragma unroll
@@ -562,7 +575,7 @@ __global__ void __launch_bounds__(256) k_embedding_grad(const u32x4e *__restrict
                 if (key[u] >= 0 && key[u] < n_rows && c0 + q * G < units) x[u][q] = dout[(int64_t)row[u] * ld16 + c0 + q * G];
             }
         }
-        if (i0 + U < kStretch) ids(i0 + U);
+        if (i0 + U < stretch) ids(i0 + U);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             if (now[u] < 0) continue;
@@ -592,7 +605,8 @@ __global__ void __launch_bounds__(64 * kJoinWaves) k_embedding_grad_join(const i
                                                                          int32_t units, int64_t d, float scale,
                                                                          bool accumulate, u32x4e *__restrict__ dtable,
                                                                          int64_t n_rows, int64_t table_ld16,
-                                                                         const float *__restrict__ part) {
+                                                                         const float *__restrict__ part,
+                                                                         int32_t stretch) {
     constexpr int N = Unit<BF>::N;
     __shared__ float sums[kJoinWaves][kWave][N];
     __shared__ int32_t s_rest[kJoinWaves];
@@ -628,15 +642,15 @@ __global__ void __launch_bounds__(64 * kJoinWaves) k_embedding_grad_join(const i
         for (int x = 0; x < N; ++x) o.v[x] += scale * acc[x];
         *to = o.to((int64_t)c * N, d);
     };
-    for (int64_t base = (int64_t)blockIdx.x * kJoinWaves; (base + 1) * kStretch < n; base += (int64_t)gridDim.x * kJoinWaves) {
-        const int64_t st = base + wid, b = st * kStretch, e = b + kStretch;
+    for (int64_t base = (int64_t)blockIdx.x * kJoinWaves; (base + 1) * stretch < n; base += (int64_t)gridDim.x * kJoinWaves) {
+        const int64_t st = base + wid, b = st * stretch, e = b + stretch;
         int32_t rest = 0;   // stretches after this one that the id goes on in
         if (e < n) {
             const int32_t id = pairs[e - 1].x;
             const bool begins = !(pairs[b].x == id && b > 0 && pairs[b - 1].x == id);
             if (id < n_rows && begins && pairs[e].x == id)
                 for (;;) {
-                    const int64_t p = (st + 1 + rest + lane) * kStretch;
+                    const int64_t p = (st + 1 + rest + lane) * stretch;
                     const uint64_t on = __ballot(p < n && pairs[p < n ? p : n - 1].x == id);
                     if (on != ~0ull) {
                         rest += __builtin_ctzll(~on);
@@ -671,7 +685,7 @@ __global__ void __launch_bounds__(64 * kJoinWaves) k_embedding_grad_join(const i
                     for (int v = 1; v < kJoinWaves; ++v)
 #pragma unroll
                         for (int x = 0; x < N; ++x) acc[x] += sums[v][lane][x];
-                    put(acc, pairs[(from + 1) * kStretch - 1].x, c);
+                    put(acc, pairs[(from + 1) * stretch - 1].x, c);
                 }
                 __syncthreads();
             }
@@ -688,6 +702,7 @@ struct GradWorkspace {
     GradWorkspace(int64_t n, int64_t n_rows, int64_t d, bool bf16) {
         const IdSortPlan p(n, n_rows);
         const int64_t units = (d * (bf16 ? 2 : 4) + 15) / 16, padded = units * (bf16 ? 8 : 4);
+        const int64_t stretch = stretch_of(n, (int32_t)units);
         size_t at = 0;
         auto take = [&](size_t bytes) {
             const size_t here = at;
@@ -697,7 +712,7 @@ struct GradWorkspace {
         for (int k = 0; k < 2; ++k) pairs[k] = take((size_t)n * 8);
         hist = take((size_t)(p.tiles * p.digits()) * 4);
         flags = take((size_t)n_rows);
-        part = take((size_t)(2 * ((n + kStretch - 1) / kStretch) * padded) * 4);
+        part = take((size_t)(2 * ((n + stretch - 1) / stretch) * padded) * 4);
         total = at;
     }
 };
@@ -775,9 +790,10 @@ void launch_embedding_backward(const void *dout, int64_t ld_bytes, const int32_t
     }
     float *part = (float *)(base + w.part);
     const int2 *pairs = (const int2 *)in_ids;
+    const int32_t stretch = stretch_of(n, units);
     {
         KernelTimer t("embedding_grad", s);
-        const int64_t stretches = (n + kStretch - 1) / kStretch;
+        const int64_t stretches = (n + stretch - 1) / stretch;
         const int64_t blocks = (stretches + 4 * (kWave / g) - 1) / (4 * (kWave / g));
         const unsigned zeros = accumulate ? 0u : grid_for(n_rows, 256, 1024);
         const bool streamed = n_rows * units * 16 > kStreamBytes;
@@ -788,11 +804,11 @@ void launch_embedding_backward(const void *dout, int64_t ld_bytes, const int32_t
         if (bf16)                                                                                                     \
             hipLaunchKernelGGL((k_embedding_grad<GV, QV, true>), dim3((unsigned)blocks + zeros, slabs), dim3(256), 0, \
                                s, in, ld16, units, d, pairs, n_dev, n, scale, accumulate, out, n_rows, tld16,      \
-                               part, flags, blocks, streamed);                                                                  \
+                               part, flags, blocks, stretch, streamed);                                                                  \
         else                                                                                                          \
             hipLaunchKernelGGL((k_embedding_grad<GV, QV, false>), dim3((unsigned)blocks + zeros, slabs), dim3(256),   \
                                0, s, in, ld16, units, d, pairs, n_dev, n, scale, accumulate, out, n_rows, tld16,   \
-                               part, flags, blocks, streamed);                                                                  \
+                               part, flags, blocks, stretch, streamed);                                                                  \
     } while (0)
         switch (g) {
             case 1: GNNAV_L(1, 1); break;
@@ -811,13 +827,13 @@ void launch_embedding_backward(const void *dout, int64_t ld_bytes, const int32_t
     }
     {
         KernelTimer t("embedding_grad_join", s);
-        const unsigned grid = grid_for((n + kStretch - 1) / kStretch, kJoinWaves, 2048);
+        const unsigned grid = grid_for((n + stretch - 1) / stretch, kJoinWaves, 2048);
         if (bf16)
             hipLaunchKernelGGL(k_embedding_grad_join<true>, dim3(grid), dim3(64 * kJoinWaves), 0, s, pairs, n_dev, n, units, d,
-                               scale, accumulate, out, n_rows, tld16, part);
+                               scale, accumulate, out, n_rows, tld16, part, stretch);
         else
             hipLaunchKernelGGL(k_embedding_grad_join<false>, dim3(grid), dim3(64 * kJoinWaves), 0, s, pairs, n_dev, n, units, d,
-                               scale, accumulate, out, n_rows, tld16, part);
+                               scale, accumulate, out, n_rows, tld16, part, stretch);
     }
     GNNAV_HIP(hipGetLastError());
 }
