@@ -1021,11 +1021,14 @@ struct XentPlan {
         pl = bf16 ? 1 : 3;
         bk = bf16 ? 32 : 16;
         // Gradient tiles of 256 x 256 where the columns fill them: 4,093 x 169,000 x 256 bf16 2,093 us in all (256 x 128: 2,178,
-        // 128 x 128: 2,303), 8,192 x 65,536 x 1,024 4,105 (4,200, 4,435).
-        const bool big = bf16 && m > 128 && d > 128 && up(d, 256) * 10 <= up(d, 128) * 11;
-        ln = m <= 32 ? 32 : 128;
+        // 128 x 128: 2,303), 8,192 x 65,536 x 1,024 4,105 (4,200, 4,435), and where dw has some half a round of them:
+        // 1,000 x 40,000 x 256 (157) 120 us, 128 x 128 126; 1,000 x 20,000 (79) 93 and 86.
+        const bool big = bf16 && m > 128 && d > 128 && up(d, 256) * 10 <= up(d, 128) * 11 &&
+                         up(d, 256) / 256 * (up(n_classes, 256) / 256) >= 128;
+        // (fp32, 57 x 25,820 x 602: 158 us with 128 rows of which half are none, 115 with 64)
+        ln = m <= 32 ? 32 : !bf16 && m <= 64 ? 64 : 128;
         rn = big ? 256 : ln;
-        bm = big ? 256 : d <= 64 && rn == 128 ? 64 : 128;
+        bm = big ? 256 : d <= 64 && rn >= 64 ? 64 : 128;
         if (bf16 && m > 32 && d <= 256) ln = m > 128 ? 256 : 128;   // held in registers
         rows = up(std::max<int64_t>(m, 1), grads ? std::max(rn, ln) : ln);
         width = up(d, grads ? bm : 64);
@@ -1041,7 +1044,7 @@ struct XentPlan {
         piece = up((all + pieces - 1) / pieces, kPiece);   // equal ones
         // fp32 with fewer 128 x 128 tiles than places for them: 64 x 64 (256 x 10,000 x 64 47 -> 41 us, 128 x 5,000 x 256 59 ->
         // 44; bf16 tiles are too short for it to matter)
-        vt = !bf16 && ln > 32 && piece / 128 * (rows / 128) < 512 ? 64 : 128;
+        vt = !bf16 && (ln == 64 || (ln == 128 && piece / 128 * (rows / 128) < 512)) ? 64 : 128;
         strips = strip_tiles = 0;
         if (bf16 && m > 32 && d <= 256) {   // two workgroups a unit
             const int64_t t = piece / kStrip, s = std::min(t, std::max<int64_t>(1, 512 / (rows / ln)));
@@ -1127,7 +1130,7 @@ void run_logits(XentArgs &a, const XentPlan &plan, int64_t d, int64_t vdim, bool
     hipLaunchKernelGGL((k_xent_logits<PL, 2, 2, 2, 2, EPI>), dim3(grid), dim3(256), 0, s, a);
 }
 
-// Gradient tiles: bm features x 128 classes for dw, bm x rn rows for dh (rn = 256: 256 x 256 both).  Either product
+// Gradient tiles: bm features x 128 classes for dw, bm x rn rows for dh (rn = 256: 256 x 256 both; 64: fp32 only).  Either product
 // may be absent (no tiles).
 template <int PL>
 void run_grads(const XentArgs &w, const XentArgs &h, int64_t bm, int64_t rn, hipStream_t s) {
@@ -1140,6 +1143,11 @@ void run_grads(const XentArgs &w, const XentArgs &h, int64_t bm, int64_t rn, hip
         GNNAV_L(2, 2, 1, 2, 2, 4, 1);
     } else if (rn == 256) {
         if constexpr (PL == 1) GNNAV_L(4, 2, 2, 2, 4, 2, 4);
+    } else if (rn == 64) {
+        if constexpr (PL == 3) {
+            if (bm == 128) GNNAV_L(2, 2, 1, 2, 2, 2, 2);
+            else GNNAV_L(1, 2, 1, 2, 2, 2, 1);
+        }
     } else if (bm == 128) {
         GNNAV_L(2, 2, 2, 2, 2, 2, 2);
     } else {
@@ -1270,6 +1278,8 @@ void xent(const XentPlan &p, const LinearXentArgs &x, hipStream_t s) {
                        x.d, lse, inv, x.dh, x.ld_dh, BF)
             if (p.rn == 32) GNNAV_L(1, 1, 4, 1);
             else if (p.rn == 256) GNNAV_L(4, 2, 2, 4);
+            else if (p.rn == 64 && p.bm == 128) GNNAV_L(2, 1, 2, 2);
+            else if (p.rn == 64) GNNAV_L(1, 1, 2, 2);
             else if (p.bm == 128) GNNAV_L(2, 2, 2, 2);
             else GNNAV_L(1, 2, 2, 2);
 #undef GNNAV_L

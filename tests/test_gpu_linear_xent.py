@@ -115,6 +115,18 @@ def test_loss_and_gradients(G, m, v, d, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("m,v,d", [(150, 33_001, 200), (300, 17_000, 400), (60, 33_001, 70)])
+def test_loss_and_gradients_of_many_classes(G, m, v, d, dtype):
+    """Enough classes for the products' largest tiles."""
+    say("xent many classes", m, v, d, dtype)
+    rng = np.random.default_rng(m + v + d)
+    h, w = matrix(m, d, dtype, m + 1, extra=1), matrix(v, d, dtype, v + 2, extra=1)
+    y = rng.integers(0, v, m)
+    y[rng.random(m) < 0.2] = -1
+    check(G, h, w, y, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("what", [(), ("row",), ("dh",), ("dw",), ("row", "dw")], ids=str)
 def test_what_is_asked_for(G, what, dtype):
     say("xent outputs", what, dtype)
