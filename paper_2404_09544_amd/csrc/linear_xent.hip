@@ -24,7 +24,7 @@
 // The products are one tile function: M (MFMA rows) is the class of the logits and
 // the feature of the gradients, N (MFMA columns) the row of h, or the class for dw.
 // Narrow bf16 rows have a logit kernel of their own (k_xent_strip), few rows
-// another (k_xent_score).
+// two, for the statistics and for the gradients (k_xent_score, k_xent_few).
 //
 // Operations: 2 m V d for each of the two logit passes, dh and dw: 8 m V d, where
 // kept logits would take 6.  8,192 x 65,536 x 1,024 bf16: 4.06 ms, 1,083 TFLOP/s of the
@@ -182,6 +182,9 @@ struct XentArgs {
     const float *losses;
     int32_t ignore;
     float *loss;
+    // few rows: the logits of four classes at a time, [class / 4][few] (nullable)
+    f32x4x *z;
+    int32_t few;               // rows of z, a power of two
 };
 
 // Wave grid WGM x WGN, each wavefront WMF x WNF MFMA blocks of 32 x 32; BK summed
@@ -769,77 +772,301 @@ __global__ void __launch_bounds__(256, 2) k_xent_strip(const XentArgs a) {
 }
 
 // The statistics for at most 32 rows: bound by reading w once, so w and h are read as they lie (row-major, into the
-// fragments), without the packing that the tiles above need.  A wavefront takes kFew x 32 classes.  169,000 x 256 bf16, one
-// row: 22 us, 3.9 TB/s (a launch of its own to pack h: 3 us more).
-constexpr int kFew = 2, kFewTile = 4 * 32 * kFew;
-
-template <int PL>
+// fragments), without the packing that the tiles above need.  A wavefront takes F x 32 classes: two blocks where its rows
+// are short (30 x 200,000 x 64 bf16 24 -> 18 us), else one, so that there are more of them (1 x 169,000 x 256 31 -> 27;
+// with the columns dealt to the four wavefronts of a workgroup 32).  169,000 x 256 bf16, one row: 19 us, 4.6 TB/s.
+template <int PL, int F>
 __global__ void __launch_bounds__(256) k_xent_score(const XentArgs a, const void *__restrict__ W, int64_t ld_w,
                                                     const void *__restrict__ H, int64_t ld_h, int32_t ignore,
-                                                    int64_t d) {
-    constexpr int X = PL == 1 ? 1 : 2;   // 16-byte units of 8 columns
+                                                    int32_t d) {
+    constexpr int X = PL == 1 ? 1 : 2;                 // 16-byte units of 8 columns
+    constexpr int U = 4;                 // steps of 16 columns in flight
     __shared__ float2 red[4 * 32];
-    const int lane = threadIdx.x & 63, wid = threadIdx.x >> 6, h = lane >> 5, lr = lane & 31;
+    const int lane = threadIdx.x & 63, wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5, lr = lane & 31;
     const int elt = PL == 1 ? 2 : 4;
-    const char *src[kFew + 1];   // this lane's rows of w, and of h
-    for (int f = 0; f < kFew; ++f) {
-        const int64_t v = std::min<int64_t>((int64_t)blockIdx.x * kFewTile + 32 * (kFew * wid + f) + lr, a.n_classes - 1);
+    const char *src[F + 1];   // this lane's rows of w, and of h
+#pragma unroll
+    for (int f = 0; f < F; ++f) {
+        const int64_t v = std::min<int64_t>((int64_t)blockIdx.x * (4 * 32 * F) + 32 * (F * wid + f) + lr, a.n_classes - 1);
         src[f] = (const char *)W + v * ld_w * elt;
     }
     const int32_t y = lr < a.m ? a.labels[lr] : -1;
     const bool live = lr < a.m && y != ignore && y >= 0 && y < a.n_classes;
-    src[kFew] = (const char *)H + (live ? lr : 0) * ld_h * elt;
-    f32x16x acc[kFew][1];
+    src[F] = (const char *)H + (live ? lr : 0) * ld_h * elt;
+    f32x16x acc[F][1];
 #pragma unroll
-    for (int f = 0; f < kFew; ++f)
+    for (int f = 0; f < F; ++f)
 #pragma unroll
         for (int r = 0; r < 16; ++r) acc[f][0][r] = 0.f;
-    // 16 columns a step, 8 of them this lane's; past d they count as zeros
-    constexpr int U = 4;   // steps in flight (8: 2 us more, fewer wavefronts fit)
-    for (int64_t k0 = 0; k0 < d; k0 += 16 * U) {
-        u32x4x x[U][kFew + 1][X];
+    // 16 columns a step, 8 of them this lane's; past the end they count as zeros
+    for (int32_t k0 = 0; k0 < d; k0 += 16 * U) {
+        u32x4x x[U][F + 1][X];
 #pragma unroll
         for (int u = 0; u < U; ++u)
 #pragma unroll
-            for (int f = 0; f <= kFew; ++f)
+            for (int f = 0; f <= F; ++f)
 #pragma unroll
                 for (int q = 0; q < X; ++q) {
-                    const int64_t k = k0 + 16 * u + 8 * h + q * 4;
+                    const int32_t k = k0 + 16 * u + 8 * h + q * 4;
                     x[u][f][q] = u32x4x{0, 0, 0, 0};
-                    if (k < d && (f < kFew || live)) x[u][f][q] = *(const u32x4x *)(src[f] + k * elt);
+                    if (k < d && (f < F || live)) x[u][f][q] = *(const u32x4x *)(src[f] + k * elt);
                 }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int64_t k = k0 + 16 * u + 8 * h;
-            bf16x8 p[kFew + 1][PL];
+            const int32_t left = d - (k0 + 16 * u + 8 * h);
+            bf16x8 p[F + 1][PL];
+            if (left < 8)
 #pragma unroll
-            for (int f = 0; f <= kFew; ++f) {
+                for (int f = 0; f <= F; ++f)
+#pragma unroll
+                    for (int q = 0; q < 4 * X; ++q) {
+                        const uint32_t unit = x[u][f][q / 4][q % 4];
+                        if constexpr (PL == 1) x[u][f][0][q] = 2 * q >= left ? 0u : 2 * q + 1 >= left ? unit & 0xffffu : unit;
+                        else x[u][f][q / 4][q % 4] = q >= left ? 0u : unit;
+                    }
+#pragma unroll
+            for (int f = 0; f <= F; ++f) {
                 if constexpr (PL == 1) {
-                    if (k + 8 > d)
-#pragma unroll
-                        for (int q = 0; q < 4; ++q) {
-                            if (k + 2 * q + 1 >= d) x[u][f][0][q] &= 0xffffu;
-                            if (k + 2 * q >= d) x[u][f][0][q] = 0;
-                        }
                     p[f][0] = __builtin_bit_cast(bf16x8, x[u][f][0]);
                 } else {
                     float z[8];
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) z[e] = k + e < d ? __uint_as_float(x[u][f][e / 4 * (X - 1)][e % 4]) : 0.f;
+                    for (int e = 0; e < 8; ++e) z[e] = __uint_as_float(x[u][f][e / 4 * (X - 1)][e % 4]);
                     split3(z, p[f][0], p[f][PL - 2], p[f][PL - 1]);
                 }
             }
 #pragma unroll
-            for (int f = 0; f < kFew; ++f) {
-                if constexpr (PL == 1)
-                    acc[f][0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(p[f][0], p[kFew][0], acc[f][0], 0, 0, 0);
-                else
-                    acc[f][0] = mfma_split6(p[f][0], p[f][PL - 2], p[f][PL - 1], p[kFew][0], p[kFew][PL - 2],
-                                            p[kFew][PL - 1], acc[f][0]);
+            for (int f = 0; f < F; ++f) {
+                if constexpr (PL == 1) acc[f][0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(p[f][0], p[F][0], acc[f][0], 0, 0, 0);
+                else acc[f][0] = mfma_split6(p[f][0], p[f][PL - 2], p[f][PL - 1], p[F][0], p[F][PL - 2], p[F][PL - 1], acc[f][0]);
             }
         }
     }
-    stats_of<PL, kFew, 1, 4, 1>(a, acc, blockIdx.x, 0, red);
+    if (a.z && lr < a.few)
+#pragma unroll
+        for (int f = 0; f < F; ++f)
+#pragma unroll
+            for (int g = 0; g < 4; ++g)
+                a.z[((int64_t)blockIdx.x * (32 * F) + 8 * (F * wid + f) + 2 * g + h) * a.few + lr] =
+                    f32x4x{acc[f][0][4 * g], acc[f][0][4 * g + 1], acc[f][0][4 * g + 2], acc[f][0][4 * g + 3]};
+    stats_of<PL, F, 1, 4, 1>(a, acc, blockIdx.x, 0, red);
+}
+
+// The gradients of at most 32 rows: bound by reading w and writing dw once, so they too take w and h as they lie, and the
+// logits that the statistics kept (4 bytes a class and row, where a second product would read all of w again).
+// A workgroup takes CW columns of every splits-th block of CB classes: w's block goes through LDS, where both its
+// classes (dh) and, of p, the rows (dw) can be summed over; the next block's loads are in flight meanwhile.  One row x
+// 169,000 x 256 bf16, in all: 61 us, through packed operands and the tiles 126; 4 x 39,124 x 373 fp32 138 -> 58.  Blocks
+// of 128 classes need more registers than three workgroups leave (2 x 244,200 x 100 bf16 36 us against 20).
+constexpr int kFewClasses = 64;
+
+template <int PL, int CW, int CB>
+__global__ void __launch_bounds__(256, 3) k_xent_few(const XentArgs a, const void *__restrict__ W, int64_t ld_w,
+                                                     const void *__restrict__ H, int64_t ld_h, int32_t blocks,
+                                                     float *__restrict__ part, int64_t width) {
+    constexpr int FB = CW / 32, HALVES = 4 / FB;       // wavefronts along the columns, along the classes
+    constexpr int C8 = CW / 8, UW = CB * C8 / 256, X = PL == 1 ? 1 : 2, ZN = CB / 4 * 32 / 256;
+    __shared__ u32x4x sw[PL][C8 * CB], sp[PL][CB / 8 * 32], sh[PL][C8 * 32];
+    const int tid = threadIdx.x, lane = tid & 63, wid = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5, lr = lane & 31;
+    const int fb = wid % FB, half = wid / FB, elt = PL == 1 ? 2 : 4;
+    const int64_t c0 = (int64_t)blockIdx.y * CW;
+    const bool want_dh = part != nullptr, want_dw = a.dw != nullptr;
+    // 8 columns from `col` on as the matrix cores take them, zeros past d
+    auto fetch = [&](u32x4x (&x)[X], const void *base, int64_t row, int64_t ld, int64_t col, bool live) {
+#pragma unroll
+        for (int q = 0; q < X; ++q) {
+            x[q] = u32x4x{0, 0, 0, 0};
+            if (live && col + 4 * q < a.d) x[q] = *(const u32x4x *)((const char *)base + (row * ld + col + 4 * q) * elt);
+        }
+    };
+    auto put = [&](u32x4x (&x)[X], int64_t col, u32x4x *to, int plane) {
+        if constexpr (PL == 1) {
+            if (col + 8 > a.d)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    if (col + 2 * q + 1 >= a.d) x[0][q] &= 0xffffu;
+                    if (col + 2 * q >= a.d) x[0][q] = 0;
+                }
+            to[0] = x[0];
+        } else {
+            float v[8];
+            bf16x8 p[3];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = col + e < a.d ? __uint_as_float(x[e / 4 * (X - 1)][e % 4]) : 0.f;
+            split3(v, p[0], p[1], p[2]);
+#pragma unroll
+            for (int pl = 0; pl < PL; ++pl) to[pl * plane] = __builtin_bit_cast(u32x4x, p[pl]);
+        }
+    };
+    for (int q = tid; q < C8 * 32; q += 256) {
+        const int lc = q % C8, r = q / C8;
+        const int32_t y = r < a.m ? a.labels[r] : -1;
+        u32x4x x[X];
+        fetch(x, H, r, ld_h, c0 + 8 * lc, r < a.m && y != a.ignore && y >= 0 && y < a.n_classes);
+        put(x, c0 + 8 * lc, &sh[0][lc * 32 + (r ^ ((lc & 3) * 4))], C8 * 32);
+    }
+    for (int q = tid; q < PL * (CB / 8) * 32; q += 256) (&sp[0][0])[q] = u32x4x{0, 0, 0, 0};
+    // p of four classes of a row, per thread and entry: the row is the same for all of a thread's entries
+    const int quads = CB / 4 * a.few, row = tid & (a.few - 1), log = __builtin_ctz(a.few);
+    const float lse = row < a.m ? a.lse[row] : INFINITY;
+    const int32_t label = row < a.m ? a.labels[row] : -1;
+    u32x4x x[UW][X];
+    f32x4x z[ZN];
+    auto load = [&](int32_t b) {
+        if (want_dh)
+#pragma unroll
+            for (int u = 0; u < UW; ++u) {
+                const int q = tid + 256 * u;
+                const int64_t v = (int64_t)b * CB + q / C8;
+                fetch(x[u], W, v, ld_w, c0 + 8 * (q % C8), v < a.n_classes);
+            }
+#pragma unroll
+        for (int u = 0; u < ZN; ++u)
+            if (tid + 256 * u < quads) z[u] = a.z[(int64_t)b * quads + tid + 256 * u];
+    };
+    const int tr_mc = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1), tr_k = 8 * h + ((lane & 15) >> 2), tr_swz = tr_mc * 4;
+    auto across = [&](const u32x4x *plane, auto rows_, int x0, int kk) -> bf16x8 {   // 16 rows of 32 columns from x0 on
+        constexpr int R = decltype(rows_)::value;
+        typedef __attribute__((address_space(3))) s16x4 lds4;
+        const char *p0 = (const char *)(plane + (x0 / 8 + tr_mc) * R + ((kk * 16 + tr_k) ^ tr_swz)) + 8 * (lane & 1);
+        const char *p1 = (const char *)(plane + (x0 / 8 + tr_mc) * R + ((kk * 16 + tr_k + 4) ^ tr_swz)) + 8 * (lane & 1);
+        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4 *)p0);
+        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4 *)p1);
+        typedef short s16x8 __attribute__((ext_vector_type(8)));
+        return __builtin_bit_cast(bf16x8, s16x8{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]});
+    };
+    auto multiply = [&](const bf16x8 (&p)[PL], const bf16x8 (&q)[PL], f32x16x c) -> f32x16x {
+        if constexpr (PL == 1) return __builtin_amdgcn_mfma_f32_32x32x16_bf16(p[0], q[0], c, 0, 0, 0);
+        else return mfma_split6(p[0], p[PL - 2], p[PL - 1], q[0], q[PL - 2], q[PL - 1], c);
+    };
+    f32x16x dh;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) dh[r] = 0.f;
+    const float inv = want_dw ? a.inv_count[0] : 0.f;
+    load(blockIdx.x);
+    __syncthreads();
+    bf16x8 fh[2][PL];
+#pragma unroll
+    for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+        for (int pl = 0; pl < PL; ++pl) fh[kk][pl] = across(sh[pl], std::integral_constant<int, 32>(), 32 * fb, kk);
+    for (int32_t b = blockIdx.x; b < blocks; b += gridDim.x) {
+        if (want_dh)
+#pragma unroll
+            for (int u = 0; u < UW; ++u) {
+                const int q = tid + 256 * u, lc = q % C8, r = q / C8;
+                put(x[u], c0 + 8 * lc, &sw[0][lc * CB + (r ^ ((lc & 3) * 4))], C8 * CB);
+            }
+#pragma unroll
+        for (int u = 0; u < ZN; ++u) {
+            const int q = tid + 256 * u;
+            if (q >= quads) break;
+            const int c4 = q >> log;
+            const int64_t v = (int64_t)b * CB + 4 * c4;
+            float p[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                if constexpr (PL == 1) p[e] = __builtin_amdgcn_exp2f((z[u][e] - lse) * kLog2e);
+                else p[e] = expf(z[u][e] - lse);
+                if (label == v + e) p[e] -= 1.f;
+                if (lse == INFINITY || v + e >= a.n_classes) p[e] = 0.f;
+            }
+            const int at = c4 / 2 * 32 + (row ^ ((c4 / 2 & 3) * 4));
+            if constexpr (PL == 1) {   // (rounded as in the tiles above)
+                ((u32x2x *)&sp[0][at])[c4 & 1] = u32x2x{bf16_pair(p[0], p[1]), bf16_pair(p[2], p[3])};
+            } else {
+                uint16_t s[4][3];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) split3_bits(p[e], s[e][0], s[e][1], s[e][2]);
+#pragma unroll
+                for (int pl = 0; pl < PL; ++pl)
+                    ((u32x2x *)&sp[pl][at])[c4 & 1] =
+                        u32x2x{(uint32_t)s[0][pl] | ((uint32_t)s[1][pl] << 16), (uint32_t)s[2][pl] | ((uint32_t)s[3][pl] << 16)};
+            }
+        }
+        __syncthreads();
+        if (b + (int32_t)gridDim.x < blocks) load(b + gridDim.x);
+        if (want_dh)
+#pragma unroll
+            for (int k = 0; k < CB / 16 / HALVES; ++k) {
+                const int kk = half * (CB / 16 / HALVES) + k, c8 = 2 * kk + h;
+                bf16x8 f[PL], g[PL];
+#pragma unroll
+                for (int pl = 0; pl < PL; ++pl) {
+                    f[pl] = across(sw[pl], std::integral_constant<int, CB>(), 32 * fb, kk);
+                    g[pl] = __builtin_bit_cast(bf16x8, sp[pl][c8 * 32 + (lr ^ ((c8 & 3) * 4))]);
+                }
+                dh = multiply(f, g, dh);
+            }
+        if (want_dw)
+#pragma unroll
+            for (int k = 0; k < CB / 32 / HALVES; ++k) {
+                const int cb = half * (CB / 32 / HALVES) + k;
+                f32x16x acc;
+#pragma unroll
+                for (int r = 0; r < 16; ++r) acc[r] = 0.f;
+#pragma unroll
+                for (int kk = 0; kk < 2; ++kk) {
+                    bf16x8 g[PL];
+#pragma unroll
+                    for (int pl = 0; pl < PL; ++pl) g[pl] = across(sp[pl], std::integral_constant<int, 32>(), 32 * cb, kk);
+                    acc = multiply(fh[kk], g, acc);
+                }
+                const int64_t v = (int64_t)b * CB + 32 * cb + lr, c = c0 + 32 * fb;
+                if constexpr (PL == 1) {
+#pragma unroll
+                    for (int g = 0; g < 4; g += 2) {
+                        float o[8];
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) o[e] = c + 8 * (g + e / 4) + 4 * h + e % 4 < a.d ? acc[4 * g + e] * inv : 0.f;
+                        const u32x4x w = join_chunk(bf16_pair(o[0], o[1]), bf16_pair(o[2], o[3]), bf16_pair(o[4], o[5]), bf16_pair(o[6], o[7]));
+                        if (v < a.n_classes && c + 8 * (g + h) < a.d) *(u32x4x *)((uint16_t *)a.dw + v * a.ld_dw + c + 8 * (g + h)) = w;
+                    }
+                } else {
+#pragma unroll
+                    for (int g = 0; g < 4; ++g) {
+                        f32x4x o;
+                        const int64_t at = c + 8 * g + 4 * h;
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) o[e] = at + e < a.d ? acc[4 * g + e] * inv : 0.f;
+                        if (v < a.n_classes && at < a.d) *(f32x4x *)((float *)a.dw + v * a.ld_dw + at) = o;
+                    }
+                }
+            }
+        __syncthreads();
+    }
+    if (want_dh && lr < a.few)
+#pragma unroll
+        for (int g = 0; g < 4; ++g)
+            *(f32x4x *)(part + (((int64_t)blockIdx.x * HALVES + half) * a.few + lr) * width + c0 + 32 * fb + 8 * g + 4 * h) =
+                f32x4x{dh[4 * g], dh[4 * g + 1], dh[4 * g + 2], dh[4 * g + 3]};
+}
+
+// dh of few rows from its parts: 8 units of four columns a workgroup, the parts dealt to 32 threads of each.
+__global__ void __launch_bounds__(256) k_xent_few_dh(const f32x4x *__restrict__ part, int32_t parts, int32_t few,
+                                                     int64_t width, int64_t d, const float *__restrict__ lse,
+                                                     const float *__restrict__ inv_count, void *__restrict__ dh, int64_t ld,
+                                                     bool bf16) {
+    __shared__ f32x4x sums[4][8];
+    const int tid = threadIdx.x, unit = tid & 7;
+    const int64_t c = ((int64_t)blockIdx.x * 8 + unit) * 4, n = blockIdx.y, units = width / 4;
+    f32x4x v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 8
+    for (int32_t s = tid >> 3; s < parts; s += 32) v += part[((int64_t)s * few + n) * units + c / 4];
+#pragma unroll
+    for (int o = 8; o < kWave; o <<= 1)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] += __shfl_xor(v[e], o, kWave);
+    if ((tid & 63) < 8) sums[tid / 64][unit] = v;
+    __syncthreads();
+    if (tid >= 8 || c >= (bf16 ? (d + 7) / 8 * 8 : (d + 3) / 4 * 4)) return;
+    v = (sums[0][unit] + sums[1][unit]) + (sums[2][unit] + sums[3][unit]);
+    const bool counts = row_counts(lse[n]);
+    const float inv = inv_count[0];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = counts && c + e < d ? v[e] * inv : 0.f;
+    if (bf16) *(u32x2x *)((uint16_t *)dh + n * ld + c) = u32x2x{bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3])};
+    else *(f32x4x *)((float *)dh + n * ld + c) = v;
 }
 
 // A piece's dh and dw in one launch: the workgroups of dh (the first `dh_ids`), then those of dw, fill
@@ -978,9 +1205,11 @@ struct XentPlan {
     int64_t bm, width, chunks;      // features of a gradient tile, packed columns, their chunks
     int32_t strips, strip_tiles;    // k_xent_strip: strips of a piece, their tiles (0: the other kernels)
     int64_t piece, vt;              // classes of a piece, of a logit tile
+    int32_t few;                    // rows of the kept logits, of the kernels for at most 32 rows (0: the other kernels)
+    int32_t few_blocks, few_splits; // k_xent_few: blocks of classes, workgroups along them
     bool whole;                     // the packed weights of all pieces are kept between the passes
     int32_t splits, split_steps;    // of dh's sum over a piece
-    size_t h, w, p, part, stats, label_logit, lse, losses, inv, total;
+    size_t z, h, w, p, part, stats, label_logit, lse, losses, inv, total;
 
     // In how many parts dh's sum over a piece is taken: `tiles` workgroups of `steps` steps each are cut into so many,
     // and `dw` workgroups of `dw_steps` follow them on the device's places.  The makespan of that, and the time of
@@ -1017,6 +1246,33 @@ struct XentPlan {
         return best_s;
     }
 
+    // Columns and classes of a block of k_xent_few: 256 bytes of a row, half where that is all.
+    static int few_columns(int64_t d, bool bf16) { return bf16 && d > 64 ? 128 : 64; }
+    
+
+    void few_plan(int64_t n_classes, int64_t d, bool bf16, bool grads, bool dh) {
+        const int64_t all = up(n_classes, kPiece), cw = few_columns(d, bf16);
+        width = up(d, cw);
+        few_blocks = (int32_t)((n_classes + kFewClasses - 1) / kFewClasses);
+        // two workgroups a unit (three: 32 x 169,000 x 256 fp32 167 -> 172 us, 1 row 121 -> 126), of as many blocks each
+        const int64_t most = std::max<int64_t>(1, 512 / (width / cw)), each = (few_blocks + most - 1) / most;
+        few_splits = (int32_t)((few_blocks + each - 1) / each);
+        size_t at = 0;
+        auto take = [&](int64_t bytes) {
+            const size_t here = at;
+            at += (size_t)up(bytes, 256);
+            return here;
+        };
+        z = take(grads ? all * few * 4 : 0);
+        part = take(dh ? few_splits * (128 / cw) * few * width * 4 : 0);
+        stats = take((1 + all / 128) * rows * 8);
+        label_logit = take(rows * 4);
+        lse = take(rows * 4);
+        losses = take(rows * 4);
+        inv = take(4);
+        total = at;
+    }
+
     XentPlan(int64_t m, int64_t n_classes, int64_t d, bool bf16, bool grads, bool dh) {
         pl = bf16 ? 1 : 3;
         bk = bf16 ? 32 : 16;
@@ -1026,14 +1282,22 @@ struct XentPlan {
         const bool big = bf16 && m > 128 && d > 128 && up(d, 256) * 10 <= up(d, 128) * 11 &&
                          up(d, 256) / 256 * (up(n_classes, 256) / 256) >= 128;
         // (fp32, 57 x 25,820 x 602: 158 us with 128 rows of which half are none, 115 with 64)
-        ln = m <= 32 ? 32 : !bf16 && m <= 64 ? 64 : 128;
+        few = 1;
+        while (few < m) few *= 2;
+        // kept logits past the limit of p (32 rows of 8 million classes): the tiles, in pieces
+        if (m > 32 || (grads && up(n_classes, kPiece) * few * 4 > kPBytes)) few = 0;
+        ln = few > 0 ? 32 : !bf16 && m <= 64 ? 64 : 128;
         rn = big ? 256 : ln;
         bm = big ? 256 : d <= 64 && rn >= 64 ? 64 : 128;
-        if (bf16 && m > 32 && d <= 256) ln = m > 128 ? 256 : 128;   // held in registers
+        if (bf16 && few == 0 && d <= 256) ln = m > 128 ? 256 : 128;   // held in registers
         rows = up(std::max<int64_t>(m, 1), grads ? std::max(rn, ln) : ln);
         width = up(d, grads ? bm : 64);
-        if (bf16 && m > 32 && d > 128 && d <= 256) width = 256;
-        if (bf16 && m > 32 && d > 64 && d <= 128) width = 128;
+        if (bf16 && few == 0 && d > 128 && d <= 256) width = 256;
+        if (bf16 && few == 0 && d > 64 && d <= 128) width = 128;
+        if (few > 0) {
+            few_plan(n_classes, d, bf16, grads, dh);
+            return;
+        }
         chunks = width / 8;
         const int64_t all = up(n_classes, kPiece);
         piece = std::max<int64_t>(kPiece, kWBytes / (width * 2 * pl) / kPiece * kPiece);
@@ -1046,7 +1310,7 @@ struct XentPlan {
         // 44; bf16 tiles are too short for it to matter)
         vt = !bf16 && (ln == 64 || (ln == 128 && piece / 128 * (rows / 128) < 512)) ? 64 : 128;
         strips = strip_tiles = 0;
-        if (bf16 && m > 32 && d <= 256) {   // two workgroups a unit
+        if (bf16 && d <= 256) {   // two workgroups a unit
             const int64_t t = piece / kStrip, s = std::min(t, std::max<int64_t>(1, 512 / (rows / ln)));
             strip_tiles = (int32_t)((t + s - 1) / s);
             strips = (int32_t)((t + strip_tiles - 1) / strip_tiles);
@@ -1066,11 +1330,11 @@ struct XentPlan {
             return here;
         };
         h = take(rows * width * 2 * pl);
-        whole = ln > 32 && all * width * 2 * pl <= kWBytes;
-        w = take(ln > 32 || grads ? (whole ? all : piece) * width * 2 * pl : 0);
+        whole = all * width * 2 * pl <= kWBytes;
+        w = take((whole ? all : piece) * width * 2 * pl);
         p = take(grads ? rows * piece * 2 * pl : 0);
         part = take(dh ? splits * rows * width * 4 : 0);
-        stats = take((1 + (ln == 32 ? all / kFewTile : strips > 0 ? strips : piece / vt)) * rows * 8);
+        stats = take((1 + (strips > 0 ? strips : piece / vt)) * rows * 8);
         label_logit = take(rows * 4);
         lse = take(rows * 4);
         losses = take(rows * 4);
@@ -1083,7 +1347,7 @@ unsigned ids_of(const XentArgs &a) {   // workgroups of a product, whole rounds 
     return (unsigned)up((int64_t)a.m_tiles * a.n_tiles * a.splits, 8);
 }
 
-// Logit tiles: 128 classes x 128 rows (or 32).  256 x 128 and, in 8 wavefronts, 256 x 256 tiles move less to LDS
+// Logit tiles: 128 classes x 128 rows.  256 x 128 and, in 8 wavefronts, 256 x 256 tiles move less to LDS
 // but have fewer workgroups on a unit to fill each other's gaps (4,093 x 169,000 x 256 bf16: both
 // passes 609 us, 128 x 128 595; x 1,024 columns 2,118 and 2,145; fp32 1,024 rows 1,342 and 1,256).
 template <int PL, int EPI>
@@ -1117,11 +1381,6 @@ void run_logits(XentArgs &a, const XentPlan &plan, int64_t d, int64_t vdim, bool
     a.loss_block = with_loss ? (int32_t)ids_of(a) : -1;
     const unsigned grid = ids_of(a) + (with_loss ? 1 : 0);
     KernelTimer t(label, s);
-    if constexpr (EPI == kProb)
-        if (ln == 32) {
-            hipLaunchKernelGGL((k_xent_logits<PL, 1, 1, 4, 1, EPI>), dim3(grid), dim3(256), 0, s, a);
-            return;
-        }
     if constexpr (PL == 3)
         if (small) {
             hipLaunchKernelGGL((k_xent_logits<PL, 1, 1, 2, 2, EPI>), dim3(grid), dim3(256), 0, s, a);
@@ -1139,9 +1398,7 @@ void run_grads(const XentArgs &w, const XentArgs &h, int64_t bm, int64_t rn, hip
 #define GNNAV_L(WMF, WNW, WNH, WGM, WGN, WGMH, WMFH)                                                                  \
     hipLaunchKernelGGL((k_xent_grads<PL, WMF, WNW, WNH, WGM, WGN, WGMH, WMFH>), dim3(nw + nh),                        \
                        dim3(64 * WGM * WGN), 0, s, w, h, (int32_t)nh)
-    if (rn == 32) {
-        GNNAV_L(2, 2, 1, 2, 2, 4, 1);
-    } else if (rn == 256) {
+    if (rn == 256) {
         if constexpr (PL == 1) GNNAV_L(4, 2, 2, 2, 4, 2, 4);
     } else if (rn == 64) {
         if constexpr (PL == 3) {
@@ -1157,7 +1414,67 @@ void run_grads(const XentArgs &w, const XentArgs &h, int64_t bm, int64_t rn, hip
 }
 
 template <int PL>
+void xent_few(const XentPlan &p, const LinearXentArgs &x, hipStream_t s) {
+    constexpr bool BF = PL == 1;
+    char *ws = (char *)x.workspace;
+    float *lse = (float *)(ws + p.lse), *inv = (float *)(ws + p.inv), *losses = (float *)(ws + p.losses);
+    XentArgs a = {};
+    a.n_classes = x.n_classes;
+    a.rows = p.rows;
+    a.labels = x.labels;
+    a.m = x.m;
+    a.d = x.d;
+    a.stats = (float2 *)(ws + p.stats);
+    a.label_logit = (float *)(ws + p.label_logit);
+    a.lse = lse;
+    a.inv_count = inv;
+    a.ignore = x.ignore;
+    a.few = p.few;
+    a.z = x.dh || x.dw ? (f32x4x *)(ws + p.z) : nullptr;
+    a.dw = x.dw;
+    a.ld_dw = x.ld_dw;
+    int64_t entries;
+    {
+        KernelTimer t("xent_stats", s);
+#define GNNAV_L(F)                                                                                                       \
+    do {                                                                                                                 \
+        entries = up(x.n_classes, kPiece) / (4 * 32 * F);                                                                \
+        hipLaunchKernelGGL((k_xent_score<PL, F>), dim3((unsigned)entries), dim3(256), 0, s, a, x.w, x.ld_w, x.h, x.ld_h, \
+                           x.ignore, (int32_t)x.d);                                                                      \
+    } while (0)
+        if (x.d <= 64) GNNAV_L(2);
+        else GNNAV_L(1);
+#undef GNNAV_L
+    }
+    {
+        KernelTimer t("xent_rows", s);
+#define GNNAV_L(ROWS)                                                                                                    \
+    hipLaunchKernelGGL((k_xent_rows<ROWS, 1024 / ROWS, kLoss>), dim3(1), dim3(1024), 0, s, a.stats, (int64_t)1, entries, p.rows, \
+                       x.m, x.labels, x.ignore, x.n_classes, a.label_logit, lse, losses, x.row_loss, x.loss, inv)
+        if (p.few <= 4) GNNAV_L(4);
+        else GNNAV_L(32);
+#undef GNNAV_L
+    }
+    if (x.dh || x.dw) {
+        KernelTimer t("xent_grads", s);
+        float *part = x.dh ? (float *)(ws + p.part) : nullptr;
+        const int cw = p.few_columns(x.d, BF);
+        const dim3 grid((unsigned)p.few_splits, (unsigned)(p.width / cw));
+        if constexpr (BF)
+            if (cw == 128)
+                hipLaunchKernelGGL((k_xent_few<PL, 128, kFewClasses>), grid, dim3(256), 0, s, a, x.w, x.ld_w, x.h, x.ld_h, p.few_blocks, part, p.width);
+        if (cw == 64)
+            hipLaunchKernelGGL((k_xent_few<PL, 64, kFewClasses>), grid, dim3(256), 0, s, a, x.w, x.ld_w, x.h, x.ld_h, p.few_blocks, part, p.width);
+        if (x.dh && x.m > 0)
+            hipLaunchKernelGGL(k_xent_few_dh, dim3((unsigned)(p.width / 32), (unsigned)x.m), dim3(256), 0, s, (const f32x4x *)part,
+                               p.few_splits * (128 / cw), p.few, p.width, x.d, lse, inv, x.dh, x.ld_dh, BF);
+    }
+    GNNAV_HIP(hipGetLastError());
+}
+
+template <int PL>
 void xent(const XentPlan &p, const LinearXentArgs &x, hipStream_t s) {
+    if (p.few > 0) return xent_few<PL>(p, x, s);
     constexpr bool BF = PL == 1;
     char *ws = (char *)x.workspace;
     u32x4x *H = (u32x4x *)(ws + p.h), *W = (u32x4x *)(ws + p.w), *Pb = (u32x4x *)(ws + p.p);
@@ -1201,13 +1518,7 @@ void xent(const XentPlan &p, const LinearXentArgs &x, hipStream_t s) {
     const int64_t all = up(x.n_classes, kPiece);
     bool several = false;  // entry 0 of the statistics holds earlier pieces'
     int64_t entries = 0;   // of the piece
-    if (p.ln == 32) {
-        KernelTimer t("xent_stats", s);
-        entries = all / kFewTile;
-        hipLaunchKernelGGL(k_xent_score<PL>, dim3((unsigned)entries), dim3(256), 0, s, a, x.w, x.ld_w, x.h, x.ld_h,
-                           x.ignore, x.d);
-    }
-    for (int64_t v0 = 0; v0 < all && p.ln > 32; v0 += p.piece) {
+    for (int64_t v0 = 0; v0 < all; v0 += p.piece) {
         const int64_t vp = std::min(p.piece, all - v0);
         if (v0 > 0) {
             KernelTimer t("xent_rows", s);
@@ -1224,25 +1535,20 @@ void xent(const XentPlan &p, const LinearXentArgs &x, hipStream_t s) {
     {
         KernelTimer t("xent_rows", s);
         const int64_t from = several ? 0 : 1;
-        if (p.rows == 32) {
-            hipLaunchKernelGGL((k_xent_rows<32, 32, kLoss>), dim3(1), dim3(1024), 0, s, a.stats, from, entries, p.rows,
-                               x.m, x.labels, x.ignore, x.n_classes, a.label_logit, lse, losses, x.row_loss, x.loss, inv);
-        } else {
-            hipLaunchKernelGGL((k_xent_rows<16, 16, kLse>), dim3((unsigned)(p.rows / 16)), dim3(256), 0, s, a.stats,
-                               from, entries, p.rows, x.m, x.labels, x.ignore, x.n_classes, a.label_logit, lse, losses,
-                               x.row_loss, nullptr, nullptr);
-            if (!(x.dh || x.dw))   // otherwise it rides with the first probabilities
-                hipLaunchKernelGGL(k_xent_loss, dim3(1), dim3(1024), 0, s, losses, x.m, x.labels, x.ignore, x.loss, inv);
-        }
+        hipLaunchKernelGGL((k_xent_rows<16, 16, kLse>), dim3((unsigned)(p.rows / 16)), dim3(256), 0, s, a.stats, from,
+                           entries, p.rows, x.m, x.labels, x.ignore, x.n_classes, a.label_logit, lse, losses, x.row_loss,
+                           nullptr, nullptr);
+        if (!(x.dh || x.dw))   // otherwise it rides with the first probabilities
+            hipLaunchKernelGGL(k_xent_loss, dim3(1), dim3(1024), 0, s, losses, x.m, x.labels, x.ignore, x.loss, inv);
     }
     if (x.dh || x.dw) {
         for (int64_t v0 = 0; v0 < all; v0 += p.piece) {
             const int64_t vp = std::min(p.piece, all - v0);
-            if (!p.whole && !(p.piece == all && p.ln > 32)) pack_w(v0, vp);   // otherwise the first pass packed it
+            if (!p.whole && p.piece < all) pack_w(v0, vp);   // otherwise the first pass packed it
             logits(v0, vp);
             a.p = Pb;
             a.p_plane = vp / 8 * p.rows;
-            run_logits<PL, kProb>(a, p, x.d, vp, v0 == 0 && p.rows > 32, "xent_prob", s);
+            run_logits<PL, kProb>(a, p, x.d, vp, v0 == 0, "xent_prob", s);
             XentArgs w = a, h = a;
             w.B = h.B = Pb;
             w.b_rows = h.b_rows = p.rows;
@@ -1276,8 +1582,7 @@ void xent(const XentPlan &p, const LinearXentArgs &x, hipStream_t s) {
 #define GNNAV_L(A, B, C, D)                                                                                          \
     hipLaunchKernelGGL((k_xent_dh<A, B, C, D>), dim3(grid), dim3(256), 0, s, part, total, p.splits, total, mt, x.m,   \
                        x.d, lse, inv, x.dh, x.ld_dh, BF)
-            if (p.rn == 32) GNNAV_L(1, 1, 4, 1);
-            else if (p.rn == 256) GNNAV_L(4, 2, 2, 4);
+            if (p.rn == 256) GNNAV_L(4, 2, 2, 4);
             else if (p.rn == 64 && p.bm == 128) GNNAV_L(2, 1, 2, 2);
             else if (p.rn == 64) GNNAV_L(1, 1, 2, 2);
             else if (p.bm == 128) GNNAV_L(2, 2, 2, 2);
