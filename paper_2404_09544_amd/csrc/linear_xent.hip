@@ -163,7 +163,7 @@ struct XentArgs {
     int64_t rows;              // packed rows of h
     const int32_t *labels;
     int64_t m;                 // rows of h
-    float2 *stats;             // [1 + tile or strip of the piece's classes][rows]; the first: of earlier pieces
+    float2 *stats;             // [1 + tile or strip of the piece's classes][rows]; the first: of earlier pieces (k_xent_score: nullable)
     float *label_logit;        // [rows]
     const float *lse;          // [rows]
     u32x4x *p;                 // planes [class chunk][rows]
@@ -775,19 +775,20 @@ __global__ void __launch_bounds__(256, 2) k_xent_strip(const XentArgs a) {
 // fragments), without the packing that the tiles above need.  A wavefront takes F x 32 classes: two blocks where its rows
 // are short (30 x 200,000 x 64 bf16 24 -> 18 us), else one, so that there are more of them (1 x 169,000 x 256 31 -> 27;
 // with the columns dealt to the four wavefronts of a workgroup 32).  169,000 x 256 bf16, one row: 19 us, 4.6 TB/s.
-template <int PL, int F>
-__global__ void __launch_bounds__(256) k_xent_score(const XentArgs a, const void *__restrict__ W, int64_t ld_w,
+template <int PL, int F, int WAVES>
+__global__ void __launch_bounds__(64 * WAVES) k_xent_score(const XentArgs a, const void *__restrict__ W, int64_t ld_w,
                                                     const void *__restrict__ H, int64_t ld_h, int32_t ignore,
                                                     int32_t d) {
     constexpr int X = PL == 1 ? 1 : 2;                 // 16-byte units of 8 columns
     constexpr int U = 4;                 // steps of 16 columns in flight
-    __shared__ float2 red[4 * 32];
+    constexpr int TILE = 32 * F * WAVES;   // classes of a workgroup
+    __shared__ float2 red[WAVES * 32];
     const int lane = threadIdx.x & 63, wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5, lr = lane & 31;
     const int elt = PL == 1 ? 2 : 4;
     const char *src[F + 1];   // this lane's rows of w, and of h
 #pragma unroll
     for (int f = 0; f < F; ++f) {
-        const int64_t v = std::min<int64_t>((int64_t)blockIdx.x * (4 * 32 * F) + 32 * (F * wid + f) + lr, a.n_classes - 1);
+        const int64_t v = std::min<int64_t>(a.v0 + (int64_t)blockIdx.x * TILE + 32 * (F * wid + f) + lr, a.n_classes - 1);
         src[f] = (const char *)W + v * ld_w * elt;
     }
     const int32_t y = lr < a.m ? a.labels[lr] : -1;
@@ -847,9 +848,9 @@ __global__ void __launch_bounds__(256) k_xent_score(const XentArgs a, const void
         for (int f = 0; f < F; ++f)
 #pragma unroll
             for (int g = 0; g < 4; ++g)
-                a.z[((int64_t)blockIdx.x * (32 * F) + 8 * (F * wid + f) + 2 * g + h) * a.few + lr] =
+                a.z[((int64_t)blockIdx.x * (TILE / 4) + 8 * (F * wid + f) + 2 * g + h) * a.few + lr] =
                     f32x4x{acc[f][0][4 * g], acc[f][0][4 * g + 1], acc[f][0][4 * g + 2], acc[f][0][4 * g + 3]};
-    stats_of<PL, F, 1, 4, 1>(a, acc, blockIdx.x, 0, red);
+    if (a.stats) stats_of<PL, F, 1, WAVES, 1>(a, acc, blockIdx.x, 0, red);
 }
 
 // The gradients of at most 32 rows: bound by reading w and writing dw once, so they too take w and h as they lie, and the
@@ -917,7 +918,7 @@ __global__ void __launch_bounds__(256, 3) k_xent_few(const XentArgs a, const voi
 #pragma unroll
             for (int u = 0; u < UW; ++u) {
                 const int q = tid + 256 * u;
-                const int64_t v = (int64_t)b * CB + q / C8;
+                const int64_t v = a.v0 + (int64_t)b * CB + q / C8;
                 fetch(x[u], W, v, ld_w, c0 + 8 * (q % C8), v < a.n_classes);
             }
 #pragma unroll
@@ -943,7 +944,7 @@ __global__ void __launch_bounds__(256, 3) k_xent_few(const XentArgs a, const voi
 #pragma unroll
     for (int r = 0; r < 16; ++r) dh[r] = 0.f;
     const float inv = want_dw ? a.inv_count[0] : 0.f;
-    load(blockIdx.x);
+    if ((int32_t)blockIdx.x < blocks) load(blockIdx.x);
     __syncthreads();
     bf16x8 fh[2][PL];
 #pragma unroll
@@ -962,7 +963,7 @@ __global__ void __launch_bounds__(256, 3) k_xent_few(const XentArgs a, const voi
             const int q = tid + 256 * u;
             if (q >= quads) break;
             const int c4 = q >> log;
-            const int64_t v = (int64_t)b * CB + 4 * c4;
+            const int64_t v = a.v0 + (int64_t)b * CB + 4 * c4;
             float p[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
@@ -1012,7 +1013,7 @@ __global__ void __launch_bounds__(256, 3) k_xent_few(const XentArgs a, const voi
                     for (int pl = 0; pl < PL; ++pl) g[pl] = across(sp[pl], std::integral_constant<int, 32>(), 32 * cb, kk);
                     acc = multiply(fh[kk], g, acc);
                 }
-                const int64_t v = (int64_t)b * CB + 32 * cb + lr, c = c0 + 32 * fb;
+                const int64_t v = a.v0 + (int64_t)b * CB + 32 * cb + lr, c = c0 + 32 * fb;
                 if constexpr (PL == 1) {
 #pragma unroll
                     for (int g = 0; g < 4; g += 2) {
@@ -1037,9 +1038,12 @@ __global__ void __launch_bounds__(256, 3) k_xent_few(const XentArgs a, const voi
     }
     if (want_dh && lr < a.few)
 #pragma unroll
-        for (int g = 0; g < 4; ++g)
-            *(f32x4x *)(part + (((int64_t)blockIdx.x * HALVES + half) * a.few + lr) * width + c0 + 32 * fb + 8 * g + 4 * h) =
-                f32x4x{dh[4 * g], dh[4 * g + 1], dh[4 * g + 2], dh[4 * g + 3]};
+        for (int g = 0; g < 4; ++g) {
+            f32x4x *at = (f32x4x *)(part + (((int64_t)blockIdx.x * HALVES + half) * a.few + lr) * width + c0 + 32 * fb + 8 * g + 4 * h);
+            f32x4x v = {dh[4 * g], dh[4 * g + 1], dh[4 * g + 2], dh[4 * g + 3]};
+            if (!a.first) v += *at;
+            *at = v;
+        }
 }
 
 // dh of few rows from its parts: 8 units of four columns a workgroup, the parts dealt to 32 threads of each.
@@ -1193,6 +1197,9 @@ __global__ void __launch_bounds__(256) k_xent_dh(const f32x4x *__restrict__ part
 namespace {
 
 constexpr int64_t kPBytes = int64_t(1) << 30;     // p of a piece, at most (or one tile of classes)
+// Kept logits of few rows, at most: past it (32 rows of 262,144 classes) the gradients score a piece again, which reads
+// w a third time.
+constexpr int64_t kFewBytes = int64_t(32) << 20;
 constexpr int64_t kLogits = int64_t(1) << 32;     // logits of a piece whose p is not kept, at most: its statistics are a 64th of their size
 constexpr int64_t kWBytes = int64_t(512) << 20;   // packed weights, at most (or one tile): of all pieces, else of one
 
@@ -1206,7 +1213,8 @@ struct XentPlan {
     int32_t strips, strip_tiles;    // k_xent_strip: strips of a piece, their tiles (0: the other kernels)
     int64_t piece, vt;              // classes of a piece, of a logit tile
     int32_t few;                    // rows of the kept logits, of the kernels for at most 32 rows (0: the other kernels)
-    int32_t few_blocks, few_splits; // k_xent_few: blocks of classes, workgroups along them
+    int32_t few_tile;               // k_xent_score: classes of a workgroup
+    int32_t few_splits;             // k_xent_few: workgroups along the classes of a piece
     bool whole;                     // the packed weights of all pieces are kept between the passes
     int32_t splits, split_steps;    // of dh's sum over a piece
     size_t z, h, w, p, part, stats, label_logit, lse, losses, inv, total;
@@ -1253,19 +1261,25 @@ struct XentPlan {
     void few_plan(int64_t n_classes, int64_t d, bool bf16, bool grads, bool dh) {
         const int64_t all = up(n_classes, kPiece), cw = few_columns(d, bf16);
         width = up(d, cw);
-        few_blocks = (int32_t)((n_classes + kFewClasses - 1) / kFewClasses);
+        // one workgroup of 8 wavefronts to 256 classes, of 4 to 128 where those are too few for the device (17 x 30,000 x 1,024
+        // bf16 66 -> 57 us in all)
+        few_tile = d > 64 && all / 256 < 512 ? 128 : 256;
+        piece = std::min(all, std::max<int64_t>(kPiece, kFewBytes / (few * 4) / kPiece * kPiece));
+        const int64_t pieces = (all + piece - 1) / piece;
+        piece = up((all + pieces - 1) / pieces, kPiece);
+        const int64_t blocks = piece / kFewClasses;
         // two workgroups a unit (three: 32 x 169,000 x 256 fp32 167 -> 172 us, 1 row 121 -> 126), of as many blocks each
-        const int64_t most = std::max<int64_t>(1, 512 / (width / cw)), each = (few_blocks + most - 1) / most;
-        few_splits = (int32_t)((few_blocks + each - 1) / each);
+        const int64_t most = std::max<int64_t>(1, 512 / (width / cw)), each = (blocks + most - 1) / most;
+        few_splits = (int32_t)((blocks + each - 1) / each);
         size_t at = 0;
         auto take = [&](int64_t bytes) {
             const size_t here = at;
             at += (size_t)up(bytes, 256);
             return here;
         };
-        z = take(grads ? all * few * 4 : 0);
+        z = take(grads ? piece * few * 4 : 0);
         part = take(dh ? few_splits * (128 / cw) * few * width * 4 : 0);
-        stats = take((1 + all / 128) * rows * 8);
+        stats = take((1 + all / few_tile) * rows * 8);
         label_logit = take(rows * 4);
         lse = take(rows * 4);
         losses = take(rows * 4);
@@ -1284,8 +1298,7 @@ struct XentPlan {
         // (fp32, 57 x 25,820 x 602: 158 us with 128 rows of which half are none, 115 with 64)
         few = 1;
         while (few < m) few *= 2;
-        // kept logits past the limit of p (32 rows of 8 million classes): the tiles, in pieces
-        if (m > 32 || (grads && up(n_classes, kPiece) * few * 4 > kPBytes)) few = 0;
+        if (m > 32) few = 0;
         ln = few > 0 ? 32 : !bf16 && m <= 64 ? 64 : 128;
         rn = big ? 256 : ln;
         bm = big ? 256 : d <= 64 && rn >= 64 ? 64 : 128;
@@ -1430,22 +1443,24 @@ void xent_few(const XentPlan &p, const LinearXentArgs &x, hipStream_t s) {
     a.inv_count = inv;
     a.ignore = x.ignore;
     a.few = p.few;
-    a.z = x.dh || x.dw ? (f32x4x *)(ws + p.z) : nullptr;
     a.dw = x.dw;
     a.ld_dw = x.ld_dw;
-    int64_t entries;
-    {
+    f32x4x *z = (f32x4x *)(ws + p.z);
+    const bool grads = x.dh || x.dw;
+    const int64_t all = up(x.n_classes, kPiece), entries = all / p.few_tile;
+    const bool one = p.piece == all;   // otherwise the gradients score each piece again
+    auto score = [&](int64_t classes) {
         KernelTimer t("xent_stats", s);
-#define GNNAV_L(F)                                                                                                       \
-    do {                                                                                                                 \
-        entries = up(x.n_classes, kPiece) / (4 * 32 * F);                                                                \
-        hipLaunchKernelGGL((k_xent_score<PL, F>), dim3((unsigned)entries), dim3(256), 0, s, a, x.w, x.ld_w, x.h, x.ld_h, \
-                           x.ignore, (int32_t)x.d);                                                                      \
-    } while (0)
-        if (x.d <= 64) GNNAV_L(2);
-        else GNNAV_L(1);
+#define GNNAV_L(F, WAVES)                                                                                                \
+    hipLaunchKernelGGL((k_xent_score<PL, F, WAVES>), dim3((unsigned)(classes / p.few_tile)), dim3(64 * WAVES), 0, s, a,  \
+                       x.w, x.ld_w, x.h, x.ld_h, x.ignore, (int32_t)x.d)
+        if (x.d <= 64) GNNAV_L(2, 4);
+        else if (p.few_tile == 128) GNNAV_L(1, 4);
+        else GNNAV_L(1, 8);
 #undef GNNAV_L
-    }
+    };
+    a.z = grads && one ? z : nullptr;
+    score(all);
     {
         KernelTimer t("xent_rows", s);
 #define GNNAV_L(ROWS)                                                                                                    \
@@ -1455,19 +1470,32 @@ void xent_few(const XentPlan &p, const LinearXentArgs &x, hipStream_t s) {
         else GNNAV_L(32);
 #undef GNNAV_L
     }
-    if (x.dh || x.dw) {
+    if (!grads) {
+        GNNAV_HIP(hipGetLastError());
+        return;
+    }
+    float *part = x.dh ? (float *)(ws + p.part) : nullptr;
+    const int cw = p.few_columns(x.d, BF);
+    a.z = z;
+    a.stats = nullptr;
+    for (int64_t v0 = 0; v0 < all; v0 += p.piece) {
+        const int64_t vp = std::min(p.piece, all - v0);
+        a.v0 = v0;
+        a.first = v0 == 0;
+        if (!one) score(vp);
         KernelTimer t("xent_grads", s);
-        float *part = x.dh ? (float *)(ws + p.part) : nullptr;
-        const int cw = p.few_columns(x.d, BF);
         const dim3 grid((unsigned)p.few_splits, (unsigned)(p.width / cw));
+        const int32_t blocks = (int32_t)(vp / kFewClasses);
         if constexpr (BF)
             if (cw == 128)
-                hipLaunchKernelGGL((k_xent_few<PL, 128, kFewClasses>), grid, dim3(256), 0, s, a, x.w, x.ld_w, x.h, x.ld_h, p.few_blocks, part, p.width);
+                hipLaunchKernelGGL((k_xent_few<PL, 128, kFewClasses>), grid, dim3(256), 0, s, a, x.w, x.ld_w, x.h, x.ld_h, blocks, part, p.width);
         if (cw == 64)
-            hipLaunchKernelGGL((k_xent_few<PL, 64, kFewClasses>), grid, dim3(256), 0, s, a, x.w, x.ld_w, x.h, x.ld_h, p.few_blocks, part, p.width);
-        if (x.dh && x.m > 0)
-            hipLaunchKernelGGL(k_xent_few_dh, dim3((unsigned)(p.width / 32), (unsigned)x.m), dim3(256), 0, s, (const f32x4x *)part,
-                               p.few_splits * (128 / cw), p.few, p.width, x.d, lse, inv, x.dh, x.ld_dh, BF);
+            hipLaunchKernelGGL((k_xent_few<PL, 64, kFewClasses>), grid, dim3(256), 0, s, a, x.w, x.ld_w, x.h, x.ld_h, blocks, part, p.width);
+    }
+    if (x.dh && x.m > 0) {
+        KernelTimer t("xent_dh_join", s);
+        hipLaunchKernelGGL(k_xent_few_dh, dim3((unsigned)(p.width / 32), (unsigned)x.m), dim3(256), 0, s, (const f32x4x *)part,
+                           p.few_splits * (128 / cw), p.few, p.width, x.d, lse, inv, x.dh, x.ld_dh, BF);
     }
     GNNAV_HIP(hipGetLastError());
 }

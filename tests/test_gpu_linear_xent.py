@@ -308,7 +308,7 @@ def test_argument_types(G):
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("m,v,d", [(1, 20_001, 96), (2, 129, 200), (4, 40_000, 373), (9, 1_000, 64), (16, 70_003, 33),
-                                   (17, 5_000, 1_030), (32, 60_001, 128)])
+                                   (17, 5_000, 1_030), (32, 60_001, 128), (32, 300_001, 16), (20, 524_289, 72)])
 def test_few_rows(G, m, v, d, dtype):
     """At most 32 rows: several blocks of classes a workgroup, columns that end inside a block's."""
     say("xent few rows", m, v, d, dtype)
