@@ -38,7 +38,7 @@ struct ClipTable {
     int32_t first[kClipTensors + 1];   // first chunk of each tensor
     int32_t n;
 };
-static_assert(sizeof(ClipTable) < 3072 + 4, "kernel arguments");
+static_assert(sizeof(ClipTable) <= 2704, "kernel arguments");
 
 enum { kNorm, kClip, kStep };
 

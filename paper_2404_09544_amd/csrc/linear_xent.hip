@@ -1157,14 +1157,20 @@ __global__ void __launch_bounds__(1024) k_xent_loss(const float *__restrict__ lo
 
 // dh from the splits' parts, in the order the products kept them in (each lane's registers side by side, so that
 // parts are written, added to and read in whole lines).
-template <int WMF, int WNF, int WGM, int WGN>
+// SLICES > 1: a workgroup has 256 / SLICES units and deals the splits to as many threads of each (few units: 57 x 137,653 x
+// 200 bf16 8 -> 5 us).
+template <int WMF, int WNF, int WGM, int WGN, int SLICES>
 __global__ void __launch_bounds__(256) k_xent_dh(const f32x4x *__restrict__ part, int64_t total, int32_t splits,
                                                  int64_t split_stride, int32_t m_tiles, int64_t m, int64_t d,
                                                  const float *__restrict__ lse, const float *__restrict__ inv_count,
                                                  void *__restrict__ dh, int64_t ld, bool bf16) {
+    constexpr int UNITS = 256 / SLICES;
+    __shared__ f32x4x sums[SLICES][UNITS];
     const float inv = inv_count[0];
-    const int64_t stride = (int64_t)gridDim.x * 256;
-    for (int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x; at < total; at += stride) {
+    const int64_t stride = (int64_t)gridDim.x * UNITS;
+    const int unit = threadIdx.x % UNITS, slice = threadIdx.x / UNITS;
+    for (int64_t base = (int64_t)blockIdx.x * UNITS; base < total; base += stride) {
+        const int64_t at = base + unit;
         int64_t x = at;
         const int lane = x & 63;
         x >>= 6;
@@ -1179,11 +1185,21 @@ __global__ void __launch_bounds__(256) k_xent_dh(const f32x4x *__restrict__ part
         const int64_t c = (x % m_tiles) * (32 * WMF * WGM) + (wid / WGN) * (32 * WMF) + 32 * i + 8 * g + 4 * (lane >> 5);
         const int64_t n = (x / m_tiles) * (32 * WNF * WGN) + (wid % WGN) * (32 * WNF) + 32 * j + (lane & 31);
         const int64_t width = bf16 ? (d + 7) / 8 * 8 : (d + 3) / 4 * 4;
-        if (n >= m || c >= width) continue;
+        const bool live = at < total && n < m && c < width;
         f32x4x v = {0.f, 0.f, 0.f, 0.f};
-        if (row_counts(lse[n]))
+        if (live && row_counts(lse[n]))
 #pragma unroll 8
-            for (int32_t s = 0; s < splits; ++s) v += part[s * split_stride + at];
+            for (int32_t s = slice; s < splits; s += SLICES) v += part[s * split_stride + at];
+        if constexpr (SLICES > 1) {
+            sums[slice][unit] = v;
+            __syncthreads();
+            if (slice == 0)
+#pragma unroll
+                for (int k = 1; k < SLICES; ++k) v += sums[k][unit];
+            __syncthreads();
+            if (slice > 0) continue;
+        }
+        if (!live) continue;
 #pragma unroll
         for (int e = 0; e < 4; ++e) v[e] = c + e < d ? v[e] * inv : 0.f;
         if (bf16)
@@ -1301,7 +1317,9 @@ struct XentPlan {
         if (m > 32) few = 0;
         ln = few > 0 ? 32 : !bf16 && m <= 64 ? 64 : 128;
         rn = big ? 256 : ln;
-        bm = big ? 256 : d <= 64 && rn >= 64 ? 64 : 128;
+        // 64 features where d has no more, and where dw, whose sum is not cut, has too few tiles of 128: 3,590 x 6,349 x 128
+        // fp32 (50) 264 -> 221 us, 8,000 x 5,000 x 128 bf16 (40) 145 -> 135; 2,000 x 6,000 x 602 fp32 (235) 345, 372 with 64
+        bm = big ? 256 : (d <= 64 || up(d, 128) / 128 * (up(n_classes, 128) / 128) < 128) && rn >= 64 ? 64 : 128;
         if (bf16 && few == 0 && d <= 256) ln = m > 128 ? 256 : 128;   // held in registers
         rows = up(std::max<int64_t>(m, 1), grads ? std::max(rn, ln) : ln);
         width = up(d, grads ? bm : 64);
@@ -1606,10 +1624,17 @@ void xent(const XentPlan &p, const LinearXentArgs &x, hipStream_t s) {
             const int64_t total = p.rows * p.width / 4;
             const f32x4x *part = (const f32x4x *)(ws + p.part);
             const int32_t mt = (int32_t)(p.width / p.bm);
-            const unsigned grid = grid_for(total, 256, 4096);
-#define GNNAV_L(A, B, C, D)                                                                                          \
-    hipLaunchKernelGGL((k_xent_dh<A, B, C, D>), dim3(grid), dim3(256), 0, s, part, total, p.splits, total, mt, x.m,   \
-                       x.d, lse, inv, x.dh, x.ld_dh, BF)
+            const bool slices = total < 256 * 256;   // fewer workgroups than compute units
+            const unsigned grid = grid_for(total, slices ? 32 : 256, 4096);
+#define GNNAV_L(A, B, C, D)                                                                                               \
+    do {                                                                                                                  \
+        if (slices)                                                                                                       \
+            hipLaunchKernelGGL((k_xent_dh<A, B, C, D, 8>), dim3(grid), dim3(256), 0, s, part, total, p.splits, total, mt, \
+                               x.m, x.d, lse, inv, x.dh, x.ld_dh, BF);                                                    \
+        else                                                                                                              \
+            hipLaunchKernelGGL((k_xent_dh<A, B, C, D, 1>), dim3(grid), dim3(256), 0, s, part, total, p.splits, total, mt, \
+                               x.m, x.d, lse, inv, x.dh, x.ld_dh, BF);                                                    \
+    } while (0)
             if (p.rn == 256) GNNAV_L(4, 2, 2, 4);
             else if (p.rn == 64 && p.bm == 128) GNNAV_L(2, 1, 2, 2);
             else if (p.rn == 64) GNNAV_L(1, 1, 2, 2);
