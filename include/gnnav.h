@@ -530,7 +530,7 @@ gnnav_status gnnav_embedding_backward(const void *dout_dev, int64_t ld_dout, con
  * gnnav_linear_xent_workspace bytes (grads: whether dh or dw is asked for; -1
  * for bad arguments; host only) on a 256-byte boundary.  It holds h and one
  * piece of the classes: some multiples of m x d, and less than 2 GiB for the
- * piece, however many classes there are (m <= 32: n_classes bytes more).  No call allocates.
+ * piece, however many classes there are (m <= 64: 2 * n_classes bytes more).  No call allocates.
  * Outputs must not overlap inputs or each other.
  * Errors: E_INVALID (null pointers, sizes, strides, alignment, workspace),
  * E_CAPACITY (a size beyond int32, d beyond 2^20), E_DEVICE.  Asynchronous. */

@@ -184,7 +184,7 @@ struct XentArgs {
     float *loss;
     // few rows: the logits of four classes at a time, [class / 4][few] (nullable)
     f32x4x *z;
-    int32_t few;               // rows of z, a power of two
+    int32_t few;               // rows of z, a power of two of at most 64
 };
 
 // Wave grid WGM x WGN, each wavefront WMF x WNF MFMA blocks of 32 x 32; BK summed
@@ -771,54 +771,67 @@ __global__ void __launch_bounds__(256, 2) k_xent_strip(const XentArgs a) {
     }
 }
 
-// The statistics for at most 32 rows: bound by reading w once, so w and h are read as they lie (row-major, into the
+// The statistics for at most 32 NR rows: bound by reading w once, so w and h are read as they lie (row-major, into the
 // fragments), without the packing that the tiles above need.  A wavefront takes F x 32 classes: two blocks where its rows
 // are short (30 x 200,000 x 64 bf16 24 -> 18 us), else one, so that there are more of them (1 x 169,000 x 256 31 -> 27;
 // with the columns dealt to the four wavefronts of a workgroup 32).  169,000 x 256 bf16, one row: 19 us, 4.6 TB/s.
-template <int PL, int F, int WAVES>
+template <int PL>
+__device__ __forceinline__ f32x16x product(const bf16x8 (&p)[PL], const bf16x8 (&q)[PL], f32x16x c) {
+    if constexpr (PL == 1) return __builtin_amdgcn_mfma_f32_32x32x16_bf16(p[0], q[0], c, 0, 0, 0);
+    else return mfma_split6(p[0], p[PL - 2], p[PL - 1], q[0], q[PL - 2], q[PL - 1], c);
+}
+
+template <int PL, int NR, int F, int WAVES>
 __global__ void __launch_bounds__(64 * WAVES) k_xent_score(const XentArgs a, const void *__restrict__ W, int64_t ld_w,
                                                     const void *__restrict__ H, int64_t ld_h, int32_t ignore,
                                                     int32_t d) {
     constexpr int X = PL == 1 ? 1 : 2;                 // 16-byte units of 8 columns
     constexpr int U = 4;                 // steps of 16 columns in flight
     constexpr int TILE = 32 * F * WAVES;   // classes of a workgroup
-    __shared__ float2 red[WAVES * 32];
+    __shared__ float2 red[WAVES * 32 * NR];
     const int lane = threadIdx.x & 63, wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5, lr = lane & 31;
     const int elt = PL == 1 ? 2 : 4;
-    const char *src[F + 1];   // this lane's rows of w, and of h
+    const char *src[F + NR];   // this lane's rows of w, and of h
 #pragma unroll
     for (int f = 0; f < F; ++f) {
         const int64_t v = std::min<int64_t>(a.v0 + (int64_t)blockIdx.x * TILE + 32 * (F * wid + f) + lr, a.n_classes - 1);
         src[f] = (const char *)W + v * ld_w * elt;
     }
-    const int32_t y = lr < a.m ? a.labels[lr] : -1;
-    const bool live = lr < a.m && y != ignore && y >= 0 && y < a.n_classes;
-    src[F] = (const char *)H + (live ? lr : 0) * ld_h * elt;
-    f32x16x acc[F][1];
+    bool live[NR];
+#pragma unroll
+    for (int j = 0; j < NR; ++j) {
+        const int n = 32 * j + lr;
+        const int32_t y = n < a.m ? a.labels[n] : -1;
+        live[j] = n < a.m && y != ignore && y >= 0 && y < a.n_classes;
+        src[F + j] = (const char *)H + (live[j] ? n : 0) * ld_h * elt;
+    }
+    f32x16x acc[F][NR];
 #pragma unroll
     for (int f = 0; f < F; ++f)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) acc[f][0][r] = 0.f;
+        for (int j = 0; j < NR; ++j)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) acc[f][j][r] = 0.f;
     // 16 columns a step, 8 of them this lane's; past the end they count as zeros
     for (int32_t k0 = 0; k0 < d; k0 += 16 * U) {
-        u32x4x x[U][F + 1][X];
+        u32x4x x[U][F + NR][X];
 #pragma unroll
         for (int u = 0; u < U; ++u)
 #pragma unroll
-            for (int f = 0; f <= F; ++f)
+            for (int f = 0; f < F + NR; ++f)
 #pragma unroll
                 for (int q = 0; q < X; ++q) {
                     const int32_t k = k0 + 16 * u + 8 * h + q * 4;
                     x[u][f][q] = u32x4x{0, 0, 0, 0};
-                    if (k < d && (f < F || live)) x[u][f][q] = *(const u32x4x *)(src[f] + k * elt);
+                    if (k < d && (f < F || live[f < F ? 0 : f - F])) x[u][f][q] = *(const u32x4x *)(src[f] + k * elt);
                 }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int32_t left = d - (k0 + 16 * u + 8 * h);
-            bf16x8 p[F + 1][PL];
+            bf16x8 p[F + NR][PL];
             if (left < 8)
 #pragma unroll
-                for (int f = 0; f <= F; ++f)
+                for (int f = 0; f < F + NR; ++f)
 #pragma unroll
                     for (int q = 0; q < 4 * X; ++q) {
                         const uint32_t unit = x[u][f][q / 4][q % 4];
@@ -826,7 +839,7 @@ __global__ void __launch_bounds__(64 * WAVES) k_xent_score(const XentArgs a, con
                         else x[u][f][q / 4][q % 4] = q >= left ? 0u : unit;
                     }
 #pragma unroll
-            for (int f = 0; f <= F; ++f) {
+            for (int f = 0; f < F + NR; ++f) {
                 if constexpr (PL == 1) {
                     p[f][0] = __builtin_bit_cast(bf16x8, x[u][f][0]);
                 } else {
@@ -837,37 +850,40 @@ __global__ void __launch_bounds__(64 * WAVES) k_xent_score(const XentArgs a, con
                 }
             }
 #pragma unroll
-            for (int f = 0; f < F; ++f) {
-                if constexpr (PL == 1) acc[f][0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(p[f][0], p[F][0], acc[f][0], 0, 0, 0);
-                else acc[f][0] = mfma_split6(p[f][0], p[f][PL - 2], p[f][PL - 1], p[F][0], p[F][PL - 2], p[F][PL - 1], acc[f][0]);
-            }
+            for (int f = 0; f < F; ++f)
+#pragma unroll
+                for (int j = 0; j < NR; ++j) acc[f][j] = product<PL>(p[f], p[F + j], acc[f][j]);
         }
     }
-    if (a.z && lr < a.few)
+    if (a.z)
 #pragma unroll
         for (int f = 0; f < F; ++f)
 #pragma unroll
-            for (int g = 0; g < 4; ++g)
-                a.z[((int64_t)blockIdx.x * (TILE / 4) + 8 * (F * wid + f) + 2 * g + h) * a.few + lr] =
-                    f32x4x{acc[f][0][4 * g], acc[f][0][4 * g + 1], acc[f][0][4 * g + 2], acc[f][0][4 * g + 3]};
-    if (a.stats) stats_of<PL, F, 1, WAVES, 1>(a, acc, blockIdx.x, 0, red);
+            for (int j = 0; j < NR; ++j)
+#pragma unroll
+                for (int g = 0; g < 4; ++g)
+                    if (32 * j + lr < a.few)
+                        a.z[((int64_t)blockIdx.x * (TILE / 4) + 8 * (F * wid + f) + 2 * g + h) * a.few + 32 * j + lr] =
+                            f32x4x{acc[f][j][4 * g], acc[f][j][4 * g + 1], acc[f][j][4 * g + 2], acc[f][j][4 * g + 3]};
+    if (a.stats) stats_of<PL, F, NR, WAVES, 1>(a, acc, blockIdx.x, 0, red);
 }
 
-// The gradients of at most 32 rows: bound by reading w and writing dw once, so they too take w and h as they lie, and the
+// The gradients of at most 32 NR rows: bound by reading w and writing dw once, so they too take w and h as they lie, and the
 // logits that the statistics kept (4 bytes a class and row, where a second product would read all of w again).
 // A workgroup takes CW columns of every splits-th block of CB classes: w's block goes through LDS, where both its
 // classes (dh) and, of p, the rows (dw) can be summed over; the next block's loads are in flight meanwhile.  One row x
-// 169,000 x 256 bf16, in all: 61 us, through packed operands and the tiles 126; 4 x 39,124 x 373 fp32 138 -> 58.  Blocks
+// 169,000 x 256 bf16, in all: 61 us, through packed operands and the tiles 126; 4 x 39,124 x 373 fp32 138 -> 58, 64 x
+// 1,000,000 x 128 bf16 486 -> 348, 57 x 25,820 x 602 fp32 157 -> 104.  Blocks
 // of 128 classes need more registers than three workgroups leave (2 x 244,200 x 100 bf16 36 us against 20).
 constexpr int kFewClasses = 64;
 
-template <int PL, int CW, int CB>
-__global__ void __launch_bounds__(256, 3) k_xent_few(const XentArgs a, const void *__restrict__ W, int64_t ld_w,
+template <int PL, int NR, int CW, int CB>
+__global__ void __launch_bounds__(256, NR == 1 ? 3 : 2) k_xent_few(const XentArgs a, const void *__restrict__ W, int64_t ld_w,
                                                      const void *__restrict__ H, int64_t ld_h, int32_t blocks,
                                                      float *__restrict__ part, int64_t width) {
     constexpr int FB = CW / 32, HALVES = 4 / FB;       // wavefronts along the columns, along the classes
-    constexpr int C8 = CW / 8, UW = CB * C8 / 256, X = PL == 1 ? 1 : 2, ZN = CB / 4 * 32 / 256;
-    __shared__ u32x4x sw[PL][C8 * CB], sp[PL][CB / 8 * 32], sh[PL][C8 * 32];
+    constexpr int C8 = CW / 8, UW = CB * C8 / 256, X = PL == 1 ? 1 : 2, RB = 32 * NR, ZN = CB / 4 * RB / 256;
+    __shared__ u32x4x sw[PL][C8 * CB], sp[PL][CB / 8 * RB], sh[PL][C8 * RB];
     const int tid = threadIdx.x, lane = tid & 63, wid = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5, lr = lane & 31;
     const int fb = wid % FB, half = wid / FB, elt = PL == 1 ? 2 : 4;
     const int64_t c0 = (int64_t)blockIdx.y * CW;
@@ -899,14 +915,14 @@ __global__ void __launch_bounds__(256, 3) k_xent_few(const XentArgs a, const voi
             for (int pl = 0; pl < PL; ++pl) to[pl * plane] = __builtin_bit_cast(u32x4x, p[pl]);
         }
     };
-    for (int q = tid; q < C8 * 32; q += 256) {
+    for (int q = tid; q < C8 * RB; q += 256) {
         const int lc = q % C8, r = q / C8;
         const int32_t y = r < a.m ? a.labels[r] : -1;
         u32x4x x[X];
         fetch(x, H, r, ld_h, c0 + 8 * lc, r < a.m && y != a.ignore && y >= 0 && y < a.n_classes);
-        put(x, c0 + 8 * lc, &sh[0][lc * 32 + (r ^ ((lc & 3) * 4))], C8 * 32);
+        put(x, c0 + 8 * lc, &sh[0][lc * RB + (r ^ ((lc & 3) * 4))], C8 * RB);
     }
-    for (int q = tid; q < PL * (CB / 8) * 32; q += 256) (&sp[0][0])[q] = u32x4x{0, 0, 0, 0};
+    for (int q = tid; q < PL * (CB / 8) * RB; q += 256) (&sp[0][0])[q] = u32x4x{0, 0, 0, 0};
     // p of four classes of a row, per thread and entry: the row is the same for all of a thread's entries
     const int quads = CB / 4 * a.few, row = tid & (a.few - 1), log = __builtin_ctz(a.few);
     const float lse = row < a.m ? a.lse[row] : INFINITY;
@@ -936,21 +952,19 @@ __global__ void __launch_bounds__(256, 3) k_xent_few(const XentArgs a, const voi
         typedef short s16x8 __attribute__((ext_vector_type(8)));
         return __builtin_bit_cast(bf16x8, s16x8{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]});
     };
-    auto multiply = [&](const bf16x8 (&p)[PL], const bf16x8 (&q)[PL], f32x16x c) -> f32x16x {
-        if constexpr (PL == 1) return __builtin_amdgcn_mfma_f32_32x32x16_bf16(p[0], q[0], c, 0, 0, 0);
-        else return mfma_split6(p[0], p[PL - 2], p[PL - 1], q[0], q[PL - 2], q[PL - 1], c);
-    };
-    f32x16x dh;
+    f32x16x dh[NR];
 #pragma unroll
-    for (int r = 0; r < 16; ++r) dh[r] = 0.f;
+    for (int j = 0; j < NR; ++j)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) dh[j][r] = 0.f;
     const float inv = want_dw ? a.inv_count[0] : 0.f;
     if ((int32_t)blockIdx.x < blocks) load(blockIdx.x);
     __syncthreads();
-    bf16x8 fh[2][PL];
+    bf16x8 fh[2 * NR][PL];
 #pragma unroll
-    for (int kk = 0; kk < 2; ++kk)
+    for (int kk = 0; kk < 2 * NR; ++kk)
 #pragma unroll
-        for (int pl = 0; pl < PL; ++pl) fh[kk][pl] = across(sh[pl], std::integral_constant<int, 32>(), 32 * fb, kk);
+        for (int pl = 0; pl < PL; ++pl) fh[kk][pl] = across(sh[pl], std::integral_constant<int, RB>(), 32 * fb, kk);
     for (int32_t b = blockIdx.x; b < blocks; b += gridDim.x) {
         if (want_dh)
 #pragma unroll
@@ -972,7 +986,7 @@ __global__ void __launch_bounds__(256, 3) k_xent_few(const XentArgs a, const voi
                 if (label == v + e) p[e] -= 1.f;
                 if (lse == INFINITY || v + e >= a.n_classes) p[e] = 0.f;
             }
-            const int at = c4 / 2 * 32 + (row ^ ((c4 / 2 & 3) * 4));
+            const int at = c4 / 2 * RB + (row ^ ((c4 / 2 & 3) * 4));
             if constexpr (PL == 1) {   // (rounded as in the tiles above)
                 ((u32x2x *)&sp[0][at])[c4 & 1] = u32x2x{bf16_pair(p[0], p[1]), bf16_pair(p[2], p[3])};
             } else {
@@ -993,11 +1007,14 @@ __global__ void __launch_bounds__(256, 3) k_xent_few(const XentArgs a, const voi
                 const int kk = half * (CB / 16 / HALVES) + k, c8 = 2 * kk + h;
                 bf16x8 f[PL], g[PL];
 #pragma unroll
-                for (int pl = 0; pl < PL; ++pl) {
-                    f[pl] = across(sw[pl], std::integral_constant<int, CB>(), 32 * fb, kk);
-                    g[pl] = __builtin_bit_cast(bf16x8, sp[pl][c8 * 32 + (lr ^ ((c8 & 3) * 4))]);
+                for (int pl = 0; pl < PL; ++pl) f[pl] = across(sw[pl], std::integral_constant<int, CB>(), 32 * fb, kk);
+#pragma unroll
+                for (int j = 0; j < NR; ++j) {
+#pragma unroll
+                    for (int pl = 0; pl < PL; ++pl)
+                        g[pl] = __builtin_bit_cast(bf16x8, sp[pl][c8 * RB + ((32 * j + lr) ^ ((c8 & 3) * 4))]);
+                    dh[j] = product<PL>(f, g, dh[j]);
                 }
-                dh = multiply(f, g, dh);
             }
         if (want_dw)
 #pragma unroll
@@ -1007,11 +1024,11 @@ __global__ void __launch_bounds__(256, 3) k_xent_few(const XentArgs a, const voi
 #pragma unroll
                 for (int r = 0; r < 16; ++r) acc[r] = 0.f;
 #pragma unroll
-                for (int kk = 0; kk < 2; ++kk) {
+                for (int kk = 0; kk < 2 * NR; ++kk) {
                     bf16x8 g[PL];
 #pragma unroll
-                    for (int pl = 0; pl < PL; ++pl) g[pl] = across(sp[pl], std::integral_constant<int, 32>(), 32 * cb, kk);
-                    acc = multiply(fh[kk], g, acc);
+                    for (int pl = 0; pl < PL; ++pl) g[pl] = across(sp[pl], std::integral_constant<int, RB>(), 32 * cb, kk);
+                    acc = product<PL>(fh[kk], g, acc);
                 }
                 const int64_t v = a.v0 + (int64_t)b * CB + 32 * cb + lr, c = c0 + 32 * fb;
                 if constexpr (PL == 1) {
@@ -1036,14 +1053,18 @@ __global__ void __launch_bounds__(256, 3) k_xent_few(const XentArgs a, const voi
             }
         __syncthreads();
     }
-    if (want_dh && lr < a.few)
+    if (want_dh)
 #pragma unroll
-        for (int g = 0; g < 4; ++g) {
-            f32x4x *at = (f32x4x *)(part + (((int64_t)blockIdx.x * HALVES + half) * a.few + lr) * width + c0 + 32 * fb + 8 * g + 4 * h);
-            f32x4x v = {dh[4 * g], dh[4 * g + 1], dh[4 * g + 2], dh[4 * g + 3]};
-            if (!a.first) v += *at;
-            *at = v;
-        }
+        for (int j = 0; j < NR; ++j)
+#pragma unroll
+            for (int g = 0; g < 4; ++g)
+                if (32 * j + lr < a.few) {
+                    f32x4x *at = (f32x4x *)(part + (((int64_t)blockIdx.x * HALVES + half) * a.few + 32 * j + lr) * width + c0 +
+                                            32 * fb + 8 * g + 4 * h);
+                    f32x4x v = {dh[j][4 * g], dh[j][4 * g + 1], dh[j][4 * g + 2], dh[j][4 * g + 3]};
+                    if (!a.first) v += *at;
+                    *at = v;
+                }
 }
 
 // dh of few rows from its parts: 8 units of four columns a workgroup, the parts dealt to 32 threads of each.
@@ -1216,6 +1237,7 @@ constexpr int64_t kPBytes = int64_t(1) << 30;     // p of a piece, at most (or o
 // Kept logits of few rows, at most: past it (32 rows of 262,144 classes) the gradients score a piece again, which reads
 // w a third time.
 constexpr int64_t kFewBytes = int64_t(32) << 20;
+constexpr int64_t kFewMore = int64_t(1) << 20;   // classes for which 33 to 64 rows count as few, at most (256 MiB of logits)
 constexpr int64_t kLogits = int64_t(1) << 32;     // logits of a piece whose p is not kept, at most: its statistics are a 64th of their size
 constexpr int64_t kWBytes = int64_t(512) << 20;   // packed weights, at most (or one tile): of all pieces, else of one
 
@@ -1228,7 +1250,7 @@ struct XentPlan {
     int64_t bm, width, chunks;      // features of a gradient tile, packed columns, their chunks
     int32_t strips, strip_tiles;    // k_xent_strip: strips of a piece, their tiles (0: the other kernels)
     int64_t piece, vt;              // classes of a piece, of a logit tile
-    int32_t few;                    // rows of the kept logits, of the kernels for at most 32 rows (0: the other kernels)
+    int32_t few;                    // rows of the kept logits, of the kernels for at most 64 rows (0: the other kernels)
     int32_t few_tile;               // k_xent_score: classes of a workgroup
     int32_t few_splits;             // k_xent_few: workgroups along the classes of a piece
     bool whole;                     // the packed weights of all pieces are kept between the passes
@@ -1280,7 +1302,7 @@ struct XentPlan {
         // one workgroup of 8 wavefronts to 256 classes, of 4 to 128 where those are too few for the device (17 x 30,000 x 1,024
         // bf16 66 -> 57 us in all)
         few_tile = d > 64 && all / 256 < 512 ? 128 : 256;
-        piece = std::min(all, std::max<int64_t>(kPiece, kFewBytes / (few * 4) / kPiece * kPiece));
+        piece = few > 32 ? all : std::min(all, std::max<int64_t>(kPiece, kFewBytes / (few * 4) / kPiece * kPiece));
         const int64_t pieces = (all + piece - 1) / piece;
         piece = up((all + pieces - 1) / pieces, kPiece);
         const int64_t blocks = piece / kFewClasses;
@@ -1311,15 +1333,14 @@ struct XentPlan {
         // 1,000 x 40,000 x 256 (157) 120 us, 128 x 128 126; 1,000 x 20,000 (79) 93 and 86.
         const bool big = bf16 && m > 128 && d > 128 && up(d, 256) * 10 <= up(d, 128) * 11 &&
                          up(d, 256) / 256 * (up(n_classes, 256) / 256) >= 128;
-        // (fp32, 57 x 25,820 x 602: 158 us with 128 rows of which half are none, 115 with 64)
-        few = 1;
-        while (few < m) few *= 2;
-        if (m > 32) few = 0;
-        ln = few > 0 ? 32 : !bf16 && m <= 64 ? 64 : 128;
+        few = 0;
+        if (m <= 32 || (m <= 64 && n_classes <= kFewMore))
+            for (few = 1; few < m;) few *= 2;
+        ln = few > 32 ? 64 : few > 0 ? 32 : 128;
         rn = big ? 256 : ln;
         // 64 features where d has no more, and where dw, whose sum is not cut, has too few tiles of 128: 3,590 x 6,349 x 128
         // fp32 (50) 264 -> 221 us, 8,000 x 5,000 x 128 bf16 (40) 145 -> 135; 2,000 x 6,000 x 602 fp32 (235) 345, 372 with 64
-        bm = big ? 256 : (d <= 64 || up(d, 128) / 128 * (up(n_classes, 128) / 128) < 128) && rn >= 64 ? 64 : 128;
+        bm = big ? 256 : (d <= 64 || up(d, 128) / 128 * (up(n_classes, 128) / 128) < 128) && rn == 128 ? 64 : 128;
         if (bf16 && few == 0 && d <= 256) ln = m > 128 ? 256 : 128;   // held in registers
         rows = up(std::max<int64_t>(m, 1), grads ? std::max(rn, ln) : ln);
         width = up(d, grads ? bm : 64);
@@ -1339,7 +1360,7 @@ struct XentPlan {
         piece = up((all + pieces - 1) / pieces, kPiece);   // equal ones
         // fp32 with fewer 128 x 128 tiles than places for them: 64 x 64 (256 x 10,000 x 64 47 -> 41 us, 128 x 5,000 x 256 59 ->
         // 44; bf16 tiles are too short for it to matter)
-        vt = !bf16 && (ln == 64 || (ln == 128 && piece / 128 * (rows / 128) < 512)) ? 64 : 128;
+        vt = !bf16 && piece / 128 * (rows / 128) < 512 ? 64 : 128;
         strips = strip_tiles = 0;
         if (bf16 && d <= 256) {   // two workgroups a unit
             const int64_t t = piece / kStrip, s = std::min(t, std::max<int64_t>(1, 512 / (rows / ln)));
@@ -1420,7 +1441,7 @@ void run_logits(XentArgs &a, const XentPlan &plan, int64_t d, int64_t vdim, bool
     hipLaunchKernelGGL((k_xent_logits<PL, 2, 2, 2, 2, EPI>), dim3(grid), dim3(256), 0, s, a);
 }
 
-// Gradient tiles: bm features x 128 classes for dw, bm x rn rows for dh (rn = 256: 256 x 256 both; 64: fp32 only).  Either product
+// Gradient tiles: bm features x 128 classes for dw, bm x rn rows for dh (rn = 256: 256 x 256 both).  Either product
 // may be absent (no tiles).
 template <int PL>
 void run_grads(const XentArgs &w, const XentArgs &h, int64_t bm, int64_t rn, hipStream_t s) {
@@ -1431,11 +1452,6 @@ void run_grads(const XentArgs &w, const XentArgs &h, int64_t bm, int64_t rn, hip
                        dim3(64 * WGM * WGN), 0, s, w, h, (int32_t)nh)
     if (rn == 256) {
         if constexpr (PL == 1) GNNAV_L(4, 2, 2, 2, 4, 2, 4);
-    } else if (rn == 64) {
-        if constexpr (PL == 3) {
-            if (bm == 128) GNNAV_L(2, 2, 1, 2, 2, 2, 2);
-            else GNNAV_L(1, 2, 1, 2, 2, 2, 1);
-        }
     } else if (bm == 128) {
         GNNAV_L(2, 2, 2, 2, 2, 2, 2);
     } else {
@@ -1444,7 +1460,7 @@ void run_grads(const XentArgs &w, const XentArgs &h, int64_t bm, int64_t rn, hip
 #undef GNNAV_L
 }
 
-template <int PL>
+template <int PL, int NR>
 void xent_few(const XentPlan &p, const LinearXentArgs &x, hipStream_t s) {
     constexpr bool BF = PL == 1;
     char *ws = (char *)x.workspace;
@@ -1470,7 +1486,7 @@ void xent_few(const XentPlan &p, const LinearXentArgs &x, hipStream_t s) {
     auto score = [&](int64_t classes) {
         KernelTimer t("xent_stats", s);
 #define GNNAV_L(F, WAVES)                                                                                                \
-    hipLaunchKernelGGL((k_xent_score<PL, F, WAVES>), dim3((unsigned)(classes / p.few_tile)), dim3(64 * WAVES), 0, s, a,  \
+    hipLaunchKernelGGL((k_xent_score<PL, NR, F, WAVES>), dim3((unsigned)(classes / p.few_tile)), dim3(64 * WAVES), 0, s, a,  \
                        x.w, x.ld_w, x.h, x.ld_h, x.ignore, (int32_t)x.d)
         if (x.d <= 64) GNNAV_L(2, 4);
         else if (p.few_tile == 128) GNNAV_L(1, 4);
@@ -1482,10 +1498,10 @@ void xent_few(const XentPlan &p, const LinearXentArgs &x, hipStream_t s) {
     {
         KernelTimer t("xent_rows", s);
 #define GNNAV_L(ROWS)                                                                                                    \
-    hipLaunchKernelGGL((k_xent_rows<ROWS, 1024 / ROWS, kLoss>), dim3(1), dim3(1024), 0, s, a.stats, (int64_t)1, entries, p.rows, \
+    hipLaunchKernelGGL((k_xent_rows<ROWS, 1024 / (ROWS), kLoss>), dim3(1), dim3(1024), 0, s, a.stats, (int64_t)1, entries, p.rows, \
                        x.m, x.labels, x.ignore, x.n_classes, a.label_logit, lse, losses, x.row_loss, x.loss, inv)
-        if (p.few <= 4) GNNAV_L(4);
-        else GNNAV_L(32);
+        if (NR == 1 && p.few <= 4) GNNAV_L(4);
+        else GNNAV_L(32 * NR);
 #undef GNNAV_L
     }
     if (!grads) {
@@ -1506,9 +1522,9 @@ void xent_few(const XentPlan &p, const LinearXentArgs &x, hipStream_t s) {
         const int32_t blocks = (int32_t)(vp / kFewClasses);
         if constexpr (BF)
             if (cw == 128)
-                hipLaunchKernelGGL((k_xent_few<PL, 128, kFewClasses>), grid, dim3(256), 0, s, a, x.w, x.ld_w, x.h, x.ld_h, blocks, part, p.width);
+                hipLaunchKernelGGL((k_xent_few<PL, NR, 128, kFewClasses>), grid, dim3(256), 0, s, a, x.w, x.ld_w, x.h, x.ld_h, blocks, part, p.width);
         if (cw == 64)
-            hipLaunchKernelGGL((k_xent_few<PL, 64, kFewClasses>), grid, dim3(256), 0, s, a, x.w, x.ld_w, x.h, x.ld_h, blocks, part, p.width);
+            hipLaunchKernelGGL((k_xent_few<PL, NR, 64, kFewClasses>), grid, dim3(256), 0, s, a, x.w, x.ld_w, x.h, x.ld_h, blocks, part, p.width);
     }
     if (x.dh && x.m > 0) {
         KernelTimer t("xent_dh_join", s);
@@ -1520,7 +1536,8 @@ void xent_few(const XentPlan &p, const LinearXentArgs &x, hipStream_t s) {
 
 template <int PL>
 void xent(const XentPlan &p, const LinearXentArgs &x, hipStream_t s) {
-    if (p.few > 0) return xent_few<PL>(p, x, s);
+    if (p.few > 32) return xent_few<PL, 2>(p, x, s);
+    if (p.few > 0) return xent_few<PL, 1>(p, x, s);
     constexpr bool BF = PL == 1;
     char *ws = (char *)x.workspace;
     u32x4x *H = (u32x4x *)(ws + p.h), *W = (u32x4x *)(ws + p.w), *Pb = (u32x4x *)(ws + p.p);
@@ -1636,8 +1653,6 @@ void xent(const XentPlan &p, const LinearXentArgs &x, hipStream_t s) {
                                x.m, x.d, lse, inv, x.dh, x.ld_dh, BF);                                                    \
     } while (0)
             if (p.rn == 256) GNNAV_L(4, 2, 2, 4);
-            else if (p.rn == 64 && p.bm == 128) GNNAV_L(2, 1, 2, 2);
-            else if (p.rn == 64) GNNAV_L(1, 1, 2, 2);
             else if (p.bm == 128) GNNAV_L(2, 2, 2, 2);
             else GNNAV_L(1, 2, 2, 2);
 #undef GNNAV_L

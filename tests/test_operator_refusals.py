@@ -158,3 +158,12 @@ def test_binding_refuses_host_tensors():
                  lambda: G.linear_xent(t, t, ids, one), lambda: G.TensorList([t]), lambda: G.grad_norm([t], one)):
         with pytest.raises(ValueError):
             call()
+
+
+def test_workspace_of_the_largest_sizes():
+    """Up to the limits of the sizes the query answers, or says that it cannot."""
+    top = 2 ** 31 - 1
+    for m, v, d in [(top, 10, 8), (2 ** 30 + 1, 300, 64), (1, top, 8), (64, top, 1), (top, top, 1), (5, 7, 2 ** 20)]:
+        for dt in (0, 1):
+            for grads in (0, 1):
+                assert lib.gnnav_linear_xent_workspace(m, v, d, dt, grads) > 0, (m, v, d, dt, grads)
