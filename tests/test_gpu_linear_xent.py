@@ -328,3 +328,23 @@ def test_few_rows_of_very_many_classes(G, m, v):
     d = 8
     h, w = matrix(m, d, "bf16", 1, extra=1), matrix(v, d, "bf16", 2, extra=1)
     check(G, h, w, np.arange(m) * (v // m - 1), "bf16", what=("row", "dh", "dw"))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("m,v,d", [(20, 140_000, 40), (50, 70_000, 130), (130, 1300, 100), (290, 40_000, 200)])
+def test_garbage_in_the_workspace(G, m, v, d, dtype):
+    """NaN in every byte of a workspace of the size asked for, and canaries behind it: the same bits as with zeros."""
+    import torch
+    say("xent garbage", m, v, d, dtype)
+    h, w = matrix(m, d, dtype, 1), matrix(v, d, dtype, 2)
+    y = (torch.arange(m, dtype=torch.int32, device="cuda") * 17) % v
+    need = G.linear_xent_workspace(m, v, d, dtype, True)
+    res = []
+    for fill in (0, 0xFF):
+        ws = torch.full((need + 4096,), 0x5A, dtype=torch.uint8, device="cuda")
+        ws[:need] = fill
+        loss, row, dh, dw = torch.zeros(1, device="cuda"), torch.zeros(m, device="cuda"), matrix(m, d, dtype, 3), matrix(v, d, dtype, 3)
+        G.linear_xent(h, w, y, loss, row_loss=row, dh=dh, dw=dw, workspace=ws[:need])
+        assert (ws[need:] == 0x5A).all()
+        res.append((loss, row, dh, dw))
+    assert all(torch.equal(a, b) and torch.isfinite(b).all() for a, b in zip(*res))
