@@ -1239,7 +1239,7 @@ constexpr int64_t kPBytes = int64_t(1) << 30;     // p of a piece, at most (or o
 constexpr int64_t kFewBytes = int64_t(32) << 20;
 constexpr int64_t kFewMore = int64_t(1) << 20;   // classes for which 33 to 64 rows count as few, at most (256 MiB of logits)
 constexpr int64_t kLogits = int64_t(1) << 32;     // logits of a piece whose p is not kept, at most: its statistics are a 64th of their size
-constexpr int64_t kWBytes = int64_t(512) << 20;   // packed weights, at most (or one tile): of all pieces, else of one
+constexpr int64_t kWBytes = int64_t(896) << 20;   // packed weights, at most (or one tile): of all pieces, else of one
 
 int64_t up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
 
