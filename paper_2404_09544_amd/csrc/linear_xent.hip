@@ -1095,15 +1095,12 @@ __global__ void __launch_bounds__(256) k_xent_few_dh(const f32x4x *__restrict__ 
 }
 
 // A piece's dh and dw in one launch: the workgroups of dh (the first `dh_ids`), then those of dw, fill
-// the units together.  dw's tiles are 32 x WMF x WGM by 32 x WNW x WGN, dh's 32 x WMF x WGM by 32 x WNH x WGN.
-template <int PL, int WMF, int WNW, int WNH, int WGM, int WGN, int WGMH, int WMFH>
+// the units together.  Both take the same tiles.
+template <int PL, int WMF, int WNF, int WGM, int WGN>
 __global__ void __launch_bounds__(64 * WGM * WGN, 2) k_xent_grads(const XentArgs w, const XentArgs h, int32_t dh_ids) {
-    constexpr int WGNH = WGM * WGN / WGMH;
-    using CW = Tile<PL, WMF, WNW, WGM, WGN>;
-    using CH = Tile<PL, WMFH, WNH, WGMH, WGNH>;
-    __shared__ u32x4x S[CW::LDS > CH::LDS ? CW::LDS : CH::LDS];
-    if ((int32_t)blockIdx.x < dh_ids) xent_tile<PL, WMFH, WNH, WGMH, WGNH, true, false, kDh>(h, blockIdx.x, S, nullptr);
-    else xent_tile<PL, WMF, WNW, WGM, WGN, true, true, kDw>(w, blockIdx.x - dh_ids, S, nullptr);
+    __shared__ u32x4x S[Tile<PL, WMF, WNF, WGM, WGN>::LDS];
+    if ((int32_t)blockIdx.x < dh_ids) xent_tile<PL, WMF, WNF, WGM, WGN, true, false, kDh>(h, blockIdx.x, S, nullptr);
+    else xent_tile<PL, WMF, WNF, WGM, WGN, true, true, kDw>(w, blockIdx.x - dh_ids, S, nullptr);
 }
 
 // ------------------------------------------------------------- rows and loss
@@ -1247,7 +1244,7 @@ struct XentPlan {
     int pl;                         // planes
     int64_t rows, bk;               // packed rows of h, summed elements per step
     int64_t dw_rows;                // rows that dw sums over: whole steps of those that there are (150 x 30,000 x 256 fp32 131 -> 112 us)
-    int64_t ln, rn;                 // rows of a logit tile, of a dh tile (and classes of a dw tile, at least 128)
+    int64_t ln, rn;                 // rows of a logit tile, of a dh tile (and classes of a dw tile)
     int64_t bm, width, chunks;      // features of a gradient tile, packed columns, their chunks
     int32_t strips, strip_tiles;    // k_xent_strip: strips of a piece, their tiles (0: the other kernels)
     int64_t piece, vt;              // classes of a piece, of a logit tile
@@ -1265,7 +1262,7 @@ struct XentPlan {
     int32_t dh_splits(int64_t tiles, int64_t steps, int64_t dw, int64_t dw_steps, int64_t part_bytes) const {
         const int64_t places = rn == 256 ? 256 : 512;   // a 256 x 256 tile has a unit to itself
         // seconds of a step of one workgroup at the rate that the products reach
-        const double step = 2.0 * bm * std::max<int64_t>(rn, 128) * bk * (pl == 3 ? 6 : 1) * places / 1.1e15;
+        const double step = 2.0 * bm * rn * bk * (pl == 3 ? 6 : 1) * places / 1.1e15;
         double best = 0;
         int32_t best_s = 0;
         for (int64_t s = 1; s <= 128 && s <= std::max<int64_t>(1, steps / 8); s += s < 16 ? 1 : s < 32 ? 2 : 8) {
@@ -1372,7 +1369,7 @@ struct XentPlan {
         splits = 1;
         split_steps = 0;
         if (dh) {
-            const int64_t steps = piece / bk, dw = width / bm * (piece / std::max<int64_t>(rn, 128));
+            const int64_t steps = piece / bk, dw = width / bm * (piece / rn);
             // (dw with the steps of all packed rows: the ones that it leaves out about pay for its stores; 520 x 50,000 x 512
             // bf16 195 us so, 203 with its own)
             splits = dh_splits(width / bm * (rows / rn), steps, dw, rows / bk, rows * width * 4 * (pieces + 1));
@@ -1446,21 +1443,19 @@ void run_logits(XentArgs &a, const XentPlan &plan, int64_t d, int64_t vdim, bool
     hipLaunchKernelGGL((k_xent_logits<PL, 2, 2, 2, 2, EPI>), dim3(grid), dim3(256), 0, s, a);
 }
 
-// Gradient tiles: bm features x 128 classes for dw, bm x rn rows for dh (rn = 256: 256 x 256 both).  Either product
-// may be absent (no tiles).
+// Gradient tiles: bm features x rn classes for dw, x rn rows for dh.  Either product may be absent (no tiles).
 template <int PL>
 void run_grads(const XentArgs &w, const XentArgs &h, int64_t bm, int64_t rn, hipStream_t s) {
     KernelTimer t("xent_grads", s);
     const unsigned nw = w.m_tiles > 0 ? ids_of(w) : 0, nh = h.m_tiles > 0 ? ids_of(h) : 0;
-#define GNNAV_L(WMF, WNW, WNH, WGM, WGN, WGMH, WMFH)                                                                  \
-    hipLaunchKernelGGL((k_xent_grads<PL, WMF, WNW, WNH, WGM, WGN, WGMH, WMFH>), dim3(nw + nh),                        \
-                       dim3(64 * WGM * WGN), 0, s, w, h, (int32_t)nh)
+#define GNNAV_L(WMF, WNF, WGM, WGN)                                                                                   \
+    hipLaunchKernelGGL((k_xent_grads<PL, WMF, WNF, WGM, WGN>), dim3(nw + nh), dim3(64 * WGM * WGN), 0, s, w, h, (int32_t)nh)
     if (rn == 256) {
-        if constexpr (PL == 1) GNNAV_L(4, 2, 2, 2, 4, 2, 4);
+        if constexpr (PL == 1) GNNAV_L(4, 2, 2, 4);
     } else if (bm == 128) {
-        GNNAV_L(2, 2, 2, 2, 2, 2, 2);
+        GNNAV_L(2, 2, 2, 2);
     } else {
-        GNNAV_L(1, 2, 2, 2, 2, 2, 1);
+        GNNAV_L(1, 2, 2, 2);
     }
 #undef GNNAV_L
 }
