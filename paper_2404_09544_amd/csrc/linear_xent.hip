@@ -464,7 +464,6 @@ __device__ __forceinline__ void xent_tile(const XentArgs &a, int32_t id, u32x4x 
     if constexpr (EPI == kStats) {
         stats_of<PL, WMF, WNF, WGM, WGN>(a, acc, mt, n0, red);
     } else if constexpr (EPI == kProb) {
-        // (a row that does not count has the lse +inf, so its p is 0 where its logits, those of zeros, are finite)
         const bool tail = a.v0 + m0 + BM > a.n_classes;
         const int live = live_classes<WMF>(a, mw, h);
 #pragma unroll
@@ -480,15 +479,21 @@ __device__ __forceinline__ void xent_tile(const XentArgs &a, int32_t id, u32x4x 
                     else acc[i][j][r] = expf(acc[i][j][r] - lse);
                 }
             if (__any(y > -64) || tail) {   // labels here, or classes that are none
-                const float one = lse == INFINITY ? 0.f : 1.f;
 #pragma unroll
                 for (int i = 0; i < WMF; ++i)
 #pragma unroll
                     for (int r = 0; r < 16; ++r) {
-                        if (y == place(i, r)) acc[i][j][r] -= one;
+                        if (y == place(i, r)) acc[i][j][r] -= 1.f;
                         if (place(i, r) >= live) acc[i][j][r] = 0.f;
                     }
             }
+            // a row that does not count was packed as zeros: its logits are NaN where w is infinite, and so would its p be
+            const bool out = lse == INFINITY;
+            if (__any(out))
+#pragma unroll
+                for (int i = 0; i < WMF; ++i)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) acc[i][j][r] = out ? 0.f : acc[i][j][r];
 #pragma unroll
             for (int i = 0; i < WMF; ++i) {
 #pragma unroll
@@ -738,15 +743,20 @@ __global__ void __launch_bounds__(256, 2) k_xent_strip(const XentArgs a) {
                         for (int r = 0; r < 16; ++r) acc[i][j][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(acc[i][j][r], kLog2e, shift));
                 }
                 if (__any(at > -64) || tail) {
-                    const float one = lse[j] == INFINITY ? 0.f : 1.f;
 #pragma unroll
                     for (int i = 0; i < 2; ++i)
 #pragma unroll
                         for (int r = 0; r < 16; ++r) {
-                            if (at == place(i, r)) acc[i][j][r] -= one;
+                            if (at == place(i, r)) acc[i][j][r] -= 1.f;
                             if (place(i, r) >= live) acc[i][j][r] = 0.f;
                         }
                 }
+                const bool out = lse[j] == INFINITY;   // (as in the tiles above)
+                if (__any(out))
+#pragma unroll
+                    for (int i = 0; i < 2; ++i)
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) acc[i][j][r] = out ? 0.f : acc[i][j][r];
 #pragma unroll
                 for (int i = 0; i < 2; ++i)
 #pragma unroll
