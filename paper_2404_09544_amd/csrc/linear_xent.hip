@@ -7,7 +7,10 @@
 //
 // The classes are taken in pieces.  A first pass over the pieces multiplies and
 // keeps, per row and tile of classes, the largest logit and the sum of
-// exponentials (the logits stay in registers); one launch joins them to lse.  A
+// exponentials (the logits stay in registers); one launch joins them to lse, which
+// is kept as two numbers, the largest logit and the log of the sum: their sum in
+// fp32 would be off by a step of the logits' size, and every p of the row by as
+// much of itself (900 equal logits of -1e30: p = 1 instead of 1 / 900).  A
 // second pass multiplies a piece again, writes its p, in the matrix cores' 16-bit
 // type, to a buffer the size of a piece, and two products take the piece's dw and
 // its part of dh from that buffer.
@@ -49,9 +52,10 @@ typedef short s16x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kPiece = 256;    // pieces of the classes are multiples of this, a whole number of any product's tiles
 constexpr float kLog2e = 1.44269504088896340736f;
-// exp2(x log2e - r log2e) as one multiply-add errs by the rounding of r log2e, less than that of a logit of r's size;
-// past this the error would leave the exponent's range, and the difference is taken first.
-constexpr float kFmaRange = 65536.f;
+// exp2(x log2e - r log2e) as one multiply-add errs by the rounding of r log2e: below this 2^-17.5 of the result at most
+// (with the log of a sum of up to 2^31 beside r).  Past it the difference is taken first, by each row for itself: what
+// other rows hold changes no bit of a row's.
+constexpr float kFmaRange = 128.f;
 
 // Two values rounded to bf16, nearest even.
 __device__ __forceinline__ uint32_t bf16_pair(float lo, float hi) {
@@ -68,9 +72,9 @@ __device__ __forceinline__ u32x4x join_chunk(uint32_t a0, uint32_t a1, uint32_t 
     return u32x4x{lo[0], hi[0], lo[1], hi[1]};
 }
 
-// What a row does: counted rows carry their lse, the others +inf, which makes
-// every p of theirs zero.
-__device__ __forceinline__ bool row_counts(float lse) { return lse < INFINITY || lse != lse; }
+// What a row does: counted rows carry their largest logit and the log of their sum, the others 0 and +inf (a sum of at
+// most 2^31 ones has no such log).
+__device__ __forceinline__ bool row_counts(float2 lse) { return lse.y < INFINITY || lse.y != lse.y; }
 
 }  // namespace
 
@@ -165,7 +169,7 @@ struct XentArgs {
     int64_t m;                 // rows of h
     float2 *stats;             // [1 + tile or strip of the piece's classes][rows]; the first: of earlier pieces (k_xent_score: nullable)
     float *label_logit;        // [rows]
-    const float *lse;          // [rows]
+    const float2 *lse;         // [rows]: the largest logit, the log of the sum of exponentials less it
     u32x4x *p;                 // planes [class chunk][rows]
     int64_t p_plane;
     // kDh
@@ -469,14 +473,15 @@ __device__ __forceinline__ void xent_tile(const XentArgs &a, int32_t id, u32x4x 
 #pragma unroll
         for (int j = 0; j < WNF; ++j) {
             const int64_t n = nw + 32 * j + lr;
-            const float lse = a.lse[n];
+            const float2 lse = a.lse[n];
+            const float shift = -lse.y * kLog2e;
             const int y = label_place<WMF>(a, n, mw, h);
 #pragma unroll
             for (int i = 0; i < WMF; ++i)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
-                    if constexpr (PL == 1) acc[i][j][r] = __builtin_amdgcn_exp2f((acc[i][j][r] - lse) * kLog2e);
-                    else acc[i][j][r] = expf(acc[i][j][r] - lse);
+                    if constexpr (PL == 1) acc[i][j][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(acc[i][j][r] - lse.x, kLog2e, shift));
+                    else acc[i][j][r] = expf((acc[i][j][r] - lse.x) - lse.y);
                 }
             if (__any(y > -64) || tail) {   // labels here, or classes that are none
 #pragma unroll
@@ -488,7 +493,7 @@ __device__ __forceinline__ void xent_tile(const XentArgs &a, int32_t id, u32x4x 
                     }
             }
             // a row that does not count was packed as zeros: its logits are NaN where w is infinite, and so would its p be
-            const bool out = lse == INFINITY;
+            const bool out = lse.y == INFINITY;
             if (__any(out))
 #pragma unroll
                 for (int i = 0; i < WMF; ++i)
@@ -639,7 +644,8 @@ __global__ void __launch_bounds__(256, 2) k_xent_strip(const XentArgs a) {
         for (int u = 0; u < IN; ++u) issue(0, u);
     src += kStrip * 16;
     bf16x8 b[KS][WNF];
-    float lse[WNF], mx[WNF], sum[WNF];
+    float2 lse[WNF];
+    float mx[WNF], sum[WNF];
     int32_t y[WNF];   // the label's place in the piece (negative or past it: elsewhere)
 #pragma unroll
     for (int j = 0; j < WNF; ++j) {
@@ -647,7 +653,7 @@ __global__ void __launch_bounds__(256, 2) k_xent_strip(const XentArgs a) {
 #pragma unroll
         for (int k = 0; k < KS; ++k) b[k][j] = __builtin_bit_cast(bf16x8, a.B[(2 * k + h) * a.b_rows + n]);
         y[j] = n < a.m && a.labels[n] >= 0 ? a.labels[n] - (int32_t)a.v0 : -1;
-        lse[j] = EPI == kProb ? a.lse[n] : 0.f;
+        lse[j] = EPI == kProb ? a.lse[n] : make_float2(0.f, 0.f);
         mx[j] = -INFINITY;
         sum[j] = 0.f;
     }
@@ -714,13 +720,17 @@ __global__ void __launch_bounds__(256, 2) k_xent_strip(const XentArgs a) {
                     for (int r = 0; r < 16; ++r) top = fmaxf(top, acc[i][j][r]);
                 const float ref = top == -INFINITY ? 0.f : top;
                 float part[2] = {sum[j] * __builtin_amdgcn_exp2f((mx[j] - ref) * kLog2e), 0.f};
-                if (__any(!(fabsf(ref) < kFmaRange))) {
+                const bool far = !(fabsf(ref) < kFmaRange);
+                const float shift = -ref * kLog2e;
+                if (__any(far)) {
 #pragma unroll
                     for (int i = 0; i < 2; ++i)
 #pragma unroll
-                        for (int r = 0; r < 16; ++r) part[i] += __builtin_amdgcn_exp2f((acc[i][j][r] - ref) * kLog2e);
+                        for (int r = 0; r < 16; ++r) {
+                            const float x = acc[i][j][r];
+                            part[i] += __builtin_amdgcn_exp2f(far ? (x - ref) * kLog2e : __builtin_fmaf(x, kLog2e, shift));
+                        }
                 } else {
-                    const float shift = -ref * kLog2e;
 #pragma unroll
                     for (int i = 0; i < 2; ++i)
 #pragma unroll
@@ -730,13 +740,17 @@ __global__ void __launch_bounds__(256, 2) k_xent_strip(const XentArgs a) {
                 sum[j] = part[0] + part[1];
                 mx[j] = top;
             } else {
-                if (__any(!(fabsf(lse[j]) < kFmaRange || lse[j] == INFINITY))) {
+                const bool far = !(fabsf(lse[j].x) < kFmaRange);
+                const float sum2 = -lse[j].y * kLog2e, shift = __builtin_fmaf(-lse[j].x, kLog2e, sum2);
+                if (__any(far)) {
 #pragma unroll
                     for (int i = 0; i < 2; ++i)
 #pragma unroll
-                        for (int r = 0; r < 16; ++r) acc[i][j][r] = __builtin_amdgcn_exp2f((acc[i][j][r] - lse[j]) * kLog2e);
+                        for (int r = 0; r < 16; ++r) {
+                            const float x = acc[i][j][r];
+                            acc[i][j][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(far ? x - lse[j].x : x, kLog2e, far ? sum2 : shift));
+                        }
                 } else {
-                    const float shift = -lse[j] * kLog2e;
 #pragma unroll
                     for (int i = 0; i < 2; ++i)
 #pragma unroll
@@ -751,7 +765,7 @@ __global__ void __launch_bounds__(256, 2) k_xent_strip(const XentArgs a) {
                             if (place(i, r) >= live) acc[i][j][r] = 0.f;
                         }
                 }
-                const bool out = lse[j] == INFINITY;   // (as in the tiles above)
+                const bool out = lse[j].y == INFINITY;   // (as in the tiles above)
                 if (__any(out))
 #pragma unroll
                     for (int i = 0; i < 2; ++i)
@@ -935,7 +949,7 @@ __global__ void __launch_bounds__(256, NR == 1 ? 3 : 2) k_xent_few(const XentArg
     for (int q = tid; q < PL * (CB / 8) * RB; q += 256) (&sp[0][0])[q] = u32x4x{0, 0, 0, 0};
     // p of four classes of a row, per thread and entry: the row is the same for all of a thread's entries
     const int quads = CB / 4 * a.few, row = tid & (a.few - 1), log = __builtin_ctz(a.few);
-    const float lse = row < a.m ? a.lse[row] : INFINITY;
+    const float2 lse = row < a.m ? a.lse[row] : make_float2(0.f, INFINITY);
     const int32_t label = row < a.m ? a.labels[row] : -1;
     u32x4x x[UW][X];
     f32x4x z[ZN];
@@ -991,10 +1005,10 @@ __global__ void __launch_bounds__(256, NR == 1 ? 3 : 2) k_xent_few(const XentArg
             float p[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                if constexpr (PL == 1) p[e] = __builtin_amdgcn_exp2f((z[u][e] - lse) * kLog2e);
-                else p[e] = expf(z[u][e] - lse);
+                if constexpr (PL == 1) p[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[u][e] - lse.x, kLog2e, -lse.y * kLog2e));
+                else p[e] = expf((z[u][e] - lse.x) - lse.y);
                 if (label == v + e) p[e] -= 1.f;
-                if (lse == INFINITY || v + e >= a.n_classes) p[e] = 0.f;
+                if (lse.y == INFINITY || v + e >= a.n_classes) p[e] = 0.f;
             }
             const int at = c4 / 2 * RB + (row ^ ((c4 / 2 & 3) * 4));
             if constexpr (PL == 1) {   // (rounded as in the tiles above)
@@ -1079,7 +1093,7 @@ __global__ void __launch_bounds__(256, NR == 1 ? 3 : 2) k_xent_few(const XentArg
 
 // dh of few rows from its parts: 8 units of four columns a workgroup, the parts dealt to 32 threads of each.
 __global__ void __launch_bounds__(256) k_xent_few_dh(const f32x4x *__restrict__ part, int32_t parts, int32_t few,
-                                                     int64_t width, int64_t d, const float *__restrict__ lse,
+                                                     int64_t width, int64_t d, const float2 *__restrict__ lse,
                                                      const float *__restrict__ inv_count, void *__restrict__ dh, int64_t ld,
                                                      bool bf16) {
     __shared__ f32x4x sums[4][8];
@@ -1114,7 +1128,7 @@ __global__ void __launch_bounds__(64 * WGM * WGN, 2) k_xent_grads(const XentArgs
 }
 
 // ------------------------------------------------------------- rows and loss
-// Joins a row's entries [from, tiles]: before the last piece to entry 0 (kFold), then to lse (+inf for a row that
+// Joins a row's entries [from, tiles]: before the last piece to entry 0 (kFold), then to lse (0 and +inf for a row that
 // does not count) and the row's loss.  ROWS rows a workgroup, the entries dealt to SLICES threads of each.
 // kLoss: there is one workgroup, which takes the mean too.
 enum { kFold, kLse, kLoss };
@@ -1123,7 +1137,7 @@ __global__ void __launch_bounds__(ROWS * SLICES) k_xent_rows(float2 *stats, int6
                                                              int64_t m, const int32_t *__restrict__ labels,
                                                              int32_t ignore, int64_t n_classes,
                                                              const float *__restrict__ label_logit,
-                                                             float *__restrict__ lse, float *losses,
+                                                             float2 *__restrict__ lse, float *losses,
                                                              float *__restrict__ row_loss, float *loss,
                                                              float *inv_count) {
     __shared__ float2 part[SLICES][ROWS];
@@ -1166,7 +1180,7 @@ __global__ void __launch_bounds__(ROWS * SLICES) k_xent_rows(float2 *stats, int6
     if (k == 0) {
         const int32_t y = n < m ? labels[n] : ignore;
         const bool out = n >= m || y == ignore, bad = !out && (y < 0 || y >= n_classes);
-        lse[n] = out || bad ? INFINITY : mx + logf(s);
+        lse[n] = out || bad ? make_float2(0.f, INFINITY) : make_float2(mx, logf(s));
         const float one = out ? 0.f : bad ? NAN : logf(s) + (mx - label_logit[n]);
         losses[n] = one;
         if (row_loss && n < m) row_loss[n] = one;
@@ -1190,7 +1204,7 @@ __global__ void __launch_bounds__(1024) k_xent_loss(const float *__restrict__ lo
 template <int WMF, int WNF, int WGM, int WGN, int SLICES>
 __global__ void __launch_bounds__(256) k_xent_dh(const f32x4x *__restrict__ part, int64_t total, int32_t splits,
                                                  int64_t split_stride, int32_t m_tiles, int64_t m, int64_t d,
-                                                 const float *__restrict__ lse, const float *__restrict__ inv_count,
+                                                 const float2 *__restrict__ lse, const float *__restrict__ inv_count,
                                                  void *__restrict__ dh, int64_t ld, bool bf16) {
     constexpr int UNITS = 256 / SLICES;
     __shared__ f32x4x sums[SLICES][UNITS];
@@ -1327,7 +1341,7 @@ struct XentPlan {
         part = take(dh ? few_splits * (128 / cw) * few * width * 4 : 0);
         stats = take((1 + all / few_tile) * rows * 8);
         label_logit = take(rows * 4);
-        lse = take(rows * 4);
+        lse = take(rows * 8);
         losses = take(rows * 4);
         inv = take(4);
         total = at;
@@ -1399,7 +1413,7 @@ struct XentPlan {
         part = take(dh ? splits * rows * width * 4 : 0);
         stats = take((1 + (strips > 0 ? strips : piece / vt)) * rows * 8);
         label_logit = take(rows * 4);
-        lse = take(rows * 4);
+        lse = take(rows * 8);
         losses = take(rows * 4);
         inv = take(4);
         total = at;
@@ -1474,7 +1488,8 @@ template <int PL, int NR>
 void xent_few(const XentPlan &p, const LinearXentArgs &x, hipStream_t s) {
     constexpr bool BF = PL == 1;
     char *ws = (char *)x.workspace;
-    float *lse = (float *)(ws + p.lse), *inv = (float *)(ws + p.inv), *losses = (float *)(ws + p.losses);
+    float2 *lse = (float2 *)(ws + p.lse);
+    float *inv = (float *)(ws + p.inv), *losses = (float *)(ws + p.losses);
     XentArgs a = {};
     a.n_classes = x.n_classes;
     a.rows = p.rows;
@@ -1551,7 +1566,8 @@ void xent(const XentPlan &p, const LinearXentArgs &x, hipStream_t s) {
     constexpr bool BF = PL == 1;
     char *ws = (char *)x.workspace;
     u32x4x *H = (u32x4x *)(ws + p.h), *W = (u32x4x *)(ws + p.w), *Pb = (u32x4x *)(ws + p.p);
-    float *lse = (float *)(ws + p.lse), *inv = (float *)(ws + p.inv), *losses = (float *)(ws + p.losses);
+    float2 *lse = (float2 *)(ws + p.lse);
+    float *inv = (float *)(ws + p.inv), *losses = (float *)(ws + p.losses);
     const int64_t esize = BF ? 2 : 4, k1 = up(x.d, p.bk);
     // h, with the first piece of w that is packed
     bool h_packed = false;

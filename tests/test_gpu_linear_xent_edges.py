@@ -64,3 +64,68 @@ def test_no_row_counts_and_classes_are_infinite(G, m, d, dtype):
         loss, row, dh, dw = outputs(m, v, d, dtype)
         G.linear_xent(h, w, torch.full((m,), -1, dtype=torch.int32, device="cuda"), loss, row_loss=row, dh=dh, dw=dw)
         assert all((t == 0).all() for t in (loss, row, dh, dw))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("m,d", PATHS)
+def test_rows_of_nan_and_infinity(G, m, d, dtype):
+    """A counted row of NaN or infinities spoils its own loss and dh, and dw, but no other row's loss or dh."""
+    import torch
+    say("xent nan rows", m, d, dtype)
+    v = 700
+    for value in (float("nan"), float("inf")):
+        h, w = matrix(m, d, dtype, 1), matrix(v, d, dtype, 2)
+        y = torch.arange(m, dtype=torch.int32, device="cuda")
+        clean, spoilt = outputs(m, v, d, dtype), outputs(m, v, d, dtype)
+        G.linear_xent(h, w, y, clean[0], row_loss=clean[1], dh=clean[2], dw=clean[3])
+        h[m - 3, 3] = value
+        G.linear_xent(h, w, y, spoilt[0], row_loss=spoilt[1], dh=spoilt[2], dw=spoilt[3])
+        others = [i for i in range(m) if i != m - 3]
+        assert torch.isnan(spoilt[1][m - 3]) and torch.isnan(spoilt[0]).all() and torch.isnan(spoilt[2][m - 3]).all()
+        assert torch.equal(spoilt[1][others], clean[1][others]) and torch.equal(spoilt[2][others], clean[2][others])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("m,d", PATHS)
+@pytest.mark.parametrize("base", [0.0, 2.0 ** 8, 2.0 ** 14, 2.0 ** 20, -2.0 ** 20, 2.0 ** 100], ids=str)
+def test_logits_far_from_zero(G, m, d, dtype, base):
+    """Adding the same number to all of a row's logits changes no p.
+
+    h holds |base|^(1/2) and 1, w +-|base|^(1/2) and -k, k = 0 .. 3 (0 at 2^100): the logits base - k are exact in fp32, so p is off by its own arithmetic alone: 2^-15 and 2^-22 (1 + |z - lse|) of it, as
+    test_gpu_linear_xent.py derives, its rounding (bf16), and the sums over 1 to m rows and the result's rounding.
+    """
+    import torch
+    say("xent far logits", m, d, dtype, base)
+    v = 900
+    t = dict(dtype=torch_type(dtype), device="cuda")
+    h, w = torch.zeros((m, (d + 7) // 8 * 8), **t)[:, :d], torch.zeros((v, (d + 7) // 8 * 8), **t)[:, :d]
+    k = np.arange(v) % (4 if abs(base) < 2.0 ** 30 else 1)
+    h[:, 0], h[:, 1] = abs(base) ** 0.5, 1.0
+    w[:, 0] = float(np.copysign(abs(base) ** 0.5, base))
+    w[:, 1] = -torch.from_numpy(k.astype(np.float32)).cuda().to(t["dtype"])
+    y = np.arange(m) * 5 % v
+    y[1] = -1
+    loss, row, dh, dw = outputs(m, v, d, dtype)
+    G.linear_xent(h, w, torch.from_numpy(y.astype(np.int32)).cuda(), loss, row_loss=row, dh=dh, dw=dw)
+    z = -k.astype(float)
+    lse = np.log(np.exp(z).sum())
+    live, p = y >= 0, np.exp(z - lse)
+    n = live.sum()
+    want = np.where(live, lse - z[np.where(live, y, 0)], 0.0)
+    assert (np.abs(f64(row) - want) <= 2.0 ** -15 + 2.0 ** -20).all()
+    assert abs(loss.item() - want.sum() / n) <= 2.0 ** -15 + 2.0 ** -20
+    # column 1 of h is 1: dw there is the sum of p - [v = y] over the rows that count, divided by their number
+    hits = np.bincount(y[live], minlength=v)
+    got = f64(dw)[:, 1]
+    exact = p - hits / n
+    ep = p * (2.0 ** -15 + 2.0 ** -22 * (1 + np.abs(z - lse)))
+    ep = ep + (HALF_STEP["bf16"] if dtype == "bf16" else 2.0 ** -22) * (p + hits / n) + 2.0 ** -24 * hits / n
+    tol = ep + (2 * m * 2.0 ** -23 + 2.0 ** -20) * (p + hits / n) + (HALF_STEP[dtype] + 2.0 ** -22) * np.abs(exact)
+    worst = (np.abs(got - exact) / tol).max()
+    assert worst <= 1.0
+    # dh's column 1: sum_v p_v (-k_v) + k_y, of one row
+    x = np.where(live, (-p * k).sum() + k[np.where(live, y, 0)], 0.0) / n
+    size = (p * k).sum() + k[np.where(live, y, 0)]
+    rel = 2.0 ** -15 + 2.0 ** -19 + (HALF_STEP["bf16"] if dtype == "bf16" else 2.0 ** -22) + 2 * v * 2.0 ** -23 + 2.0 ** -20
+    worst = (np.abs(f64(dh)[:, 1] - x) / (rel * size / n + (HALF_STEP[dtype] + 2.0 ** -22) * np.abs(x) + 1e-30)).max()
+    assert worst <= 1.0
