@@ -620,6 +620,8 @@ __global__ void __launch_bounds__(64 * WGM * WGN, 2) k_xent_logits(const XentArg
 // A lane's running maximum and sum stay in registers over the strip.  4,096 x 84,736 x 256: statistics 230 us
 // with the tiles above, 167 so (1,063 TFLOP/s); probabilities 345 and 210 (the 694 MB of p go out at 3.3 TB/s).
 constexpr int kStrip = 64;   // classes of a tile
+// Tiles of a strip, at most: the running sums round once a tile, 384 2^-24 of a sum in a strip.
+constexpr int64_t kStripTiles = 384;
 
 template <int KS, int WNF, int EPI>
 __global__ void __launch_bounds__(256, 2) k_xent_strip(const XentArgs a) {
@@ -719,7 +721,7 @@ __global__ void __launch_bounds__(256, 2) k_xent_strip(const XentArgs a) {
 #pragma unroll
                     for (int r = 0; r < 16; ++r) top = fmaxf(top, acc[i][j][r]);
                 const float ref = top == -INFINITY ? 0.f : top;
-                float part[2] = {sum[j] * __builtin_amdgcn_exp2f((mx[j] - ref) * kLog2e), 0.f};
+                float part[2] = {0.f, 0.f};
                 const bool far = !(fabsf(ref) < kFmaRange);
                 const float shift = -ref * kLog2e;
                 if (__any(far)) {
@@ -737,7 +739,8 @@ __global__ void __launch_bounds__(256, 2) k_xent_strip(const XentArgs a) {
                         for (int r = 0; r < 16; ++r)
                             part[i] += __builtin_amdgcn_exp2f(__builtin_fmaf(acc[i][j][r], kLog2e, shift));
                 }
-                sum[j] = part[0] + part[1];
+                // (a tile's 32 terms to each other first: one rounding of the running sum a tile)
+                sum[j] = __builtin_fmaf(sum[j], __builtin_amdgcn_exp2f((mx[j] - ref) * kLog2e), part[0] + part[1]);
                 mx[j] = top;
             } else {
                 const bool far = !(fabsf(lse[j].x) < kFmaRange);
@@ -1386,7 +1389,8 @@ struct XentPlan {
         vt = !bf16 && piece / 128 * (rows / 128) < 512 ? 64 : 128;
         strips = strip_tiles = 0;
         if (bf16 && d <= 256) {   // two workgroups a unit
-            const int64_t t = piece / kStrip, s = std::min(t, std::max<int64_t>(1, 512 / (rows / ln)));
+            const int64_t t = piece / kStrip, round = std::max<int64_t>(1, 512 / (rows / ln));
+            const int64_t s = std::min(t, (t + round * kStripTiles - 1) / (round * kStripTiles) * round);
             strip_tiles = (int32_t)((t + s - 1) / s);
             strips = (int32_t)((t + strip_tiles - 1) / strip_tiles);
         }

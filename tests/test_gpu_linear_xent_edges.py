@@ -129,3 +129,30 @@ def test_logits_far_from_zero(G, m, d, dtype, base):
     rel = 2.0 ** -15 + 2.0 ** -19 + (HALF_STEP["bf16"] if dtype == "bf16" else 2.0 ** -22) + 2 * v * 2.0 ** -23 + 2.0 ** -20
     worst = (np.abs(f64(dh)[:, 1] - x) / (rel * size / n + (HALF_STEP[dtype] + 2.0 ** -22) * np.abs(x) + 1e-30)).max()
     assert worst <= 1.0
+
+
+def test_sums_of_many_equal_terms(G):
+    """bf16, a million classes, no gradients: logits 0 at two classes of each 512 (one for each half of a wavefront), all
+    others ln t with t = 0.45 of a step above a multiple of 2^-10, which a sum past 8,192 that takes them one by one loses
+    each time.  A row's sum may round 384 times along a wavefront's run of tiles, 17 times in a tile and 128 times where
+    runs are joined: (384 + 17 + 128) 2^-24 of it; exp2's argument and result are off by 2^-22 (1 + |z|); a few roundings
+    of the result."""
+    import torch
+    m, v, d = 4096, (1 << 20) - 300, 16
+    say("xent long sums", m, v, d)
+    t = (717 + 0.45) * 2.0 ** -10
+    hi = torch.tensor(np.log(t), dtype=torch.float64).bfloat16()
+    lo = torch.tensor(np.log(t) - hi.item(), dtype=torch.float64).bfloat16()
+    h, w = torch.zeros((m, d), dtype=torch.bfloat16, device="cuda"), torch.zeros((v, d), dtype=torch.bfloat16, device="cuda")
+    h[:, :2] = 1.0
+    w[:, 0], w[:, 1] = hi.item(), lo.item()
+    w[::512] = 0.0
+    w[4::512] = 0.0
+    zeros = len(range(0, v, 512)) + len(range(4, v, 512))
+    loss, row = torch.zeros(1, device="cuda"), torch.zeros(m, device="cuda")
+    G.linear_xent(h, w, torch.zeros(m, dtype=torch.int32, device="cuda"), loss, row_loss=row)
+    want = np.log(zeros + (v - zeros) * np.exp(hi.double().item() + lo.double().item()))
+    tol = (384 + 17 + 128) * 2.0 ** -24 + 2.0 ** -22 * (2 + abs(np.log(t))) + 2.0 ** -22 * want
+    off = np.abs(f64(row) - want).max()
+    say("off by", off, "of", tol)
+    assert off <= tol
