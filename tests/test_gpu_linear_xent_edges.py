@@ -68,6 +68,17 @@ def test_no_row_counts_and_classes_are_infinite(G, m, d, dtype):
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("m,d", PATHS)
+def test_labels_outside_the_classes(G, m, d, dtype):
+    say("xent bad labels", m, d, dtype)
+    h, w = matrix(m, d, dtype, 1), matrix(300, d, dtype, 2)
+    y = np.arange(m) * 7 % 300
+    y[3], y[m - 1], y[20], y[21] = 300, -2, 2 ** 31 - 1, -1
+    loss, row, dh, dw = check(G, h, w, y, dtype)
+    assert np.isnan(loss.item()) and (dh[[3, m - 1, 20, 21]] == 0).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("m,d", PATHS)
 def test_rows_of_nan_and_infinity(G, m, d, dtype):
     """A counted row of NaN or infinities spoils its own loss and dh, and dw, but no other row's loss or dh."""
     import torch
@@ -131,6 +142,19 @@ def test_logits_far_from_zero(G, m, d, dtype, base):
     assert worst <= 1.0
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("m,d", PATHS)
+def test_large_logits(G, m, d, dtype):
+    """Logits of several hundred and thousand, confident rows: no overflow."""
+    say("xent large logits", m, d, dtype)
+    for scale in (16.0, 256.0):
+        h, w = matrix(m, d, dtype, 1), matrix(900, d, dtype, 2)
+        h.mul_(scale)
+        y = np.arange(m)
+        y[::5] = -1
+        check(G, h, w, y, dtype)
+
+
 def test_sums_of_many_equal_terms(G):
     """bf16, a million classes, no gradients: logits 0 at two classes of each 512 (one for each half of a wavefront), all
     others ln t with t = 0.45 of a step above a multiple of 2^-10, which a sum past 8,192 that takes them one by one loses
@@ -156,3 +180,48 @@ def test_sums_of_many_equal_terms(G):
     off = np.abs(f64(row) - want).max()
     say("off by", off, "of", tol)
     assert off <= tol
+
+
+@pytest.mark.parametrize("dtype,m,v,d", [("f32", 70, 157_300, 1_000), ("bf16", 70, 230_001, 2_050)])
+def test_weights_packed_twice(G, dtype, m, v, d):
+    """Packed weights of more than 896 MiB are not kept between the passes: each packs its pieces, the last one ragged.
+    In a workspace of the size asked for, every byte NaN; against 64 bits on the device.  Bounds as of
+    test_several_pieces_of_classes: ez by the largest sum of |h w|, gradients by the norm."""
+    import torch
+    say("xent packed twice", dtype, m, v, d)
+    gen = torch.Generator(device="cuda").manual_seed(5)
+    ld = (d + 7) // 8 * 8
+    t = dict(dtype=torch_type(dtype), device="cuda")
+    h = torch.randn((m, ld), generator=gen, device="cuda").to(t["dtype"])[:, :d]
+    w = (torch.randn((v, ld), generator=gen, device="cuda") / d ** 0.5).to(t["dtype"])[:, :d]
+    y = (torch.arange(m, device="cuda") * 2_237) % v
+    y[-1], y[::7] = v - 1, -1
+    loss, row, dh, dw = outputs(m, v, d, dtype)
+    need = G.linear_xent_workspace(m, v, d, dtype, True)
+    ws = torch.full((need + 4096,), 0xFF, dtype=torch.uint8, device="cuda")
+    G.linear_xent(h, w, y.int(), loss, row_loss=row, dh=dh, dw=dw, workspace=ws[:need])
+    assert (ws[need:] == 0xFF).all()
+    keep = y >= 0
+    x = h.double() * keep[:, None]
+    z, biggest, step = torch.empty((m, v), dtype=torch.float64, device="cuda"), 0.0, 16_384
+    for a in range(0, v, step):
+        piece = w[a:a + step].double()
+        z[:, a:a + step] = x @ piece.t().contiguous()
+        biggest = max(biggest, (x.abs() @ piece.abs().t().contiguous()).max().item())
+    lse = torch.logsumexp(z, 1)
+    at = torch.arange(m, device="cuda")
+    want = torch.where(keep, lse - z[at, y.clamp(min=0)], 0.0)
+    ez = (2 * d * 2.0 ** -23 + (2.0 ** -20 if dtype == "f32" else 0.0)) * biggest
+    assert (row.double() - want).abs().max().item() <= 2 * ez + 2.0 ** -15 + 2.0 ** -18
+    assert abs(loss.item() - want.sum().item() / keep.sum().item()) <= 2 * ez + 2.0 ** -15 + 2.0 ** -18
+    p = torch.exp(z - lse[:, None])
+    p[at, y.clamp(min=0)] -= 1
+    p *= keep[:, None] / keep.sum()
+    want_dh = torch.zeros((m, d), dtype=torch.float64, device="cuda")
+    bound = 2.0 ** -7 if dtype == "bf16" else 2.0 ** -9
+    for a in range(0, v, step):
+        q = p[:, a:a + step].contiguous()
+        want_dh += q @ w[a:a + step].double()
+        ref = q.t().contiguous() @ x
+        assert torch.linalg.norm(dw[a:a + step].double() - ref).item() <= bound * torch.linalg.norm(ref).item(), a
+    assert torch.linalg.norm(dh.double() - want_dh).item() <= bound * torch.linalg.norm(want_dh).item()
