@@ -522,7 +522,8 @@ gnnav_status gnnav_embedding_backward(const void *dout_dev, int64_t ld_dout, con
  * dt = F32: fp32-accurate products (six bf16 part products; an infinite entry
  * of a row that counts or of w makes its logits NaN).  dt = BF16: bf16
  * operands, fp32 accumulation and statistics; p - [v = y] is rounded to bf16
- * before the gradients' products, the gradients once to bf16.  exp of less than
+ * before the gradients' products (up to 32 rows, and up to 64 rows of at most
+ * 2^20 classes, it keeps 16 bits), the gradients once to bf16.  exp of less than
  * 2^-126 counts as 0.  row_loss_dev,
  * dh_dev, dw_dev may be NULL; dh and dw are of type dt, every row written, the
  * columns from d up to the next 16-byte boundary with zeros.  Results do not

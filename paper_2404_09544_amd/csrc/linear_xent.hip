@@ -902,7 +902,18 @@ __global__ void __launch_bounds__(64 * WAVES) k_xent_score(const XentArgs a, con
 // 169,000 x 256 bf16, in all: 61 us, through packed operands and the tiles 126; 4 x 39,124 x 373 fp32 138 -> 58, 64 x
 // 1,000,000 x 128 bf16 486 -> 348, 57 x 25,820 x 602 fp32 157 -> 104.  Blocks
 // of 128 classes need more registers than three workgroups leave (2 x 244,200 x 100 bf16 36 us against 20).
+// p of bf16 rows is multiplied in two parts, its rounded value and the rest, 2^-16 of it off at most: sums of so few
+// rows would show one rounding.  The second product costs little beside the loads: 1 x 169,000 x 256 60.1 -> 60.8 us, 64 x
+// 1,000,000 x 128 346 -> 349, 57 x 137,653 x 200 83.6 -> 86.5.
 constexpr int kFewClasses = 64;
+
+template <int PL>
+__device__ __forceinline__ f32x16x product_p(const bf16x8 (&x)[PL], const bf16x8 (&p)[PL == 1 ? 2 : PL], f32x16x c) {
+    if constexpr (PL == 1)
+        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[0], p[0], __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[0], p[1], c, 0, 0, 0),
+                                                       0, 0, 0);
+    else return product<PL>(x, p, c);
+}
 
 template <int PL, int NR, int CW, int CB>
 __global__ void __launch_bounds__(256, NR == 1 ? 3 : 2) k_xent_few(const XentArgs a, const void *__restrict__ W, int64_t ld_w,
@@ -910,7 +921,8 @@ __global__ void __launch_bounds__(256, NR == 1 ? 3 : 2) k_xent_few(const XentArg
                                                      float *__restrict__ part, int64_t width) {
     constexpr int FB = CW / 32, HALVES = 4 / FB;       // wavefronts along the columns, along the classes
     constexpr int C8 = CW / 8, UW = CB * C8 / 256, X = PL == 1 ? 1 : 2, RB = 32 * NR, ZN = CB / 4 * RB / 256;
-    __shared__ u32x4x sw[PL][C8 * CB], sp[PL][CB / 8 * RB], sh[PL][C8 * RB];
+    constexpr int PP = PL == 1 ? 2 : PL;               // parts of p
+    __shared__ u32x4x sw[PL][C8 * CB], sp[PP][CB / 8 * RB], sh[PL][C8 * RB];
     const int tid = threadIdx.x, lane = tid & 63, wid = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5, lr = lane & 31;
     const int fb = wid % FB, half = wid / FB, elt = PL == 1 ? 2 : 4;
     const int64_t c0 = (int64_t)blockIdx.y * CW;
@@ -949,7 +961,7 @@ __global__ void __launch_bounds__(256, NR == 1 ? 3 : 2) k_xent_few(const XentArg
         fetch(x, H, r, ld_h, c0 + 8 * lc, r < a.m && y != a.ignore && y >= 0 && y < a.n_classes);
         put(x, c0 + 8 * lc, &sh[0][lc * RB + (r ^ ((lc & 3) * 4))], C8 * RB);
     }
-    for (int q = tid; q < PL * (CB / 8) * RB; q += 256) (&sp[0][0])[q] = u32x4x{0, 0, 0, 0};
+    for (int q = tid; q < PP * (CB / 8) * RB; q += 256) (&sp[0][0])[q] = u32x4x{0, 0, 0, 0};
     // p of four classes of a row, per thread and entry: the row is the same for all of a thread's entries
     const int quads = CB / 4 * a.few, row = tid & (a.few - 1), log = __builtin_ctz(a.few);
     const float2 lse = row < a.m ? a.lse[row] : make_float2(0.f, INFINITY);
@@ -1014,8 +1026,14 @@ __global__ void __launch_bounds__(256, NR == 1 ? 3 : 2) k_xent_few(const XentArg
                 if (lse.y == INFINITY || v + e >= a.n_classes) p[e] = 0.f;
             }
             const int at = c4 / 2 * RB + (row ^ ((c4 / 2 & 3) * 4));
-            if constexpr (PL == 1) {   // (rounded as in the tiles above)
-                ((u32x2x *)&sp[0][at])[c4 & 1] = u32x2x{bf16_pair(p[0], p[1]), bf16_pair(p[2], p[3])};
+            if constexpr (PL == 1) {   // the value rounded, and what that leaves
+#pragma unroll
+                for (int pl = 0; pl < PP; ++pl) {
+                    const u32x2x w = {bf16_pair(p[0], p[1]), bf16_pair(p[2], p[3])};
+                    ((u32x2x *)&sp[pl][at])[c4 & 1] = w;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) p[e] -= __uint_as_float(e & 1 ? w[e / 2] & 0xffff0000u : w[e / 2] << 16);
+                }
             } else {
                 uint16_t s[4][3];
 #pragma unroll
@@ -1032,15 +1050,15 @@ __global__ void __launch_bounds__(256, NR == 1 ? 3 : 2) k_xent_few(const XentArg
 #pragma unroll
             for (int k = 0; k < CB / 16 / HALVES; ++k) {
                 const int kk = half * (CB / 16 / HALVES) + k, c8 = 2 * kk + h;
-                bf16x8 f[PL], g[PL];
+                bf16x8 f[PL], g[PP];
 #pragma unroll
                 for (int pl = 0; pl < PL; ++pl) f[pl] = across(sw[pl], std::integral_constant<int, CB>(), 32 * fb, kk);
 #pragma unroll
                 for (int j = 0; j < NR; ++j) {
 #pragma unroll
-                    for (int pl = 0; pl < PL; ++pl)
+                    for (int pl = 0; pl < PP; ++pl)
                         g[pl] = __builtin_bit_cast(bf16x8, sp[pl][c8 * RB + ((32 * j + lr) ^ ((c8 & 3) * 4))]);
-                    dh[j] = product<PL>(f, g, dh[j]);
+                    dh[j] = product_p<PL>(f, g, dh[j]);
                 }
             }
         if (want_dw)
@@ -1052,10 +1070,10 @@ __global__ void __launch_bounds__(256, NR == 1 ? 3 : 2) k_xent_few(const XentArg
                 for (int r = 0; r < 16; ++r) acc[r] = 0.f;
 #pragma unroll
                 for (int kk = 0; kk < 2 * NR; ++kk) {
-                    bf16x8 g[PL];
+                    bf16x8 g[PP];
 #pragma unroll
-                    for (int pl = 0; pl < PL; ++pl) g[pl] = across(sp[pl], std::integral_constant<int, RB>(), 32 * cb, kk);
-                    acc = product<PL>(fh[kk], g, acc);
+                    for (int pl = 0; pl < PP; ++pl) g[pl] = across(sp[pl], std::integral_constant<int, RB>(), 32 * cb, kk);
+                    acc = product_p<PL>(fh[kk], g, acc);
                 }
                 const int64_t v = a.v0 + (int64_t)b * CB + 32 * cb + lr, c = c0 + 32 * fb;
                 if constexpr (PL == 1) {

@@ -225,3 +225,35 @@ def test_weights_packed_twice(G, dtype, m, v, d):
         ref = q.t().contiguous() @ x
         assert torch.linalg.norm(dw[a:a + step].double() - ref).item() <= bound * torch.linalg.norm(ref).item(), a
     assert torch.linalg.norm(dh.double() - want_dh).item() <= bound * torch.linalg.norm(want_dh).item()
+
+
+@pytest.mark.parametrize("m,v,d", [(1, 20_001, 96), (1, 300, 24), (3, 9_000, 200), (30, 5_000, 300), (64, 3_001, 130), (17, 600_001, 40)])
+def test_gradients_of_few_bf16_rows_are_rounded_once(G, m, v, d):
+    """Up to 64 rows, p - [v = y] is multiplied in two bf16 parts, 2^-8 of 2^-8 off at most: sums this short would show one
+    of 2^-8.  What is left is p's own error (as test_gpu_linear_xent.py derives), the sums' and the result's."""
+    say("xent few rows, rounding", m, v, d)
+    rng = np.random.default_rng(m + v + d)
+    h, w = matrix(m, d, "bf16", m + 1), matrix(v, d, "bf16", v + 2)
+    y = rng.integers(0, v, m)
+    if m > 2:
+        y[1] = -1
+    import torch
+    loss, row, dh, dw = outputs(m, v, d, "bf16")
+    G.linear_xent(h, w, torch.from_numpy(y.astype(np.int32)).cuda(), loss, row_loss=row, dh=dh, dw=dw)
+    x, ww, live, rows = f64(h), f64(w), y >= 0, np.arange(m)
+    x[~live] = 0
+    z, s = x @ ww.T, np.abs(x) @ np.abs(ww).T
+    lse = np.log(np.exp(z - z.max(axis=1, keepdims=True)).sum(axis=1)) + z.max(axis=1)
+    ez = (2 * d * 2.0 ** -23 * s).max(axis=1)
+    p = np.exp(z - lse[:, None]) * live[:, None]
+    ep = p * ((2 * ez + 2.0 ** -15)[:, None] + 2.0 ** -22 * (1 + np.abs(z - lse[:, None])))
+    p[rows[live], y[live]] -= 1
+    ep += 2.0 ** -16 * np.abs(p) + 2.0 ** -24 * (p < 0) + 2.0 ** -126
+    n = live.sum()
+
+    def worst(got, a, ea, b):
+        want = a @ b / n
+        tol = (ea @ np.abs(b) + 2 * a.shape[1] * 2.0 ** -23 * (np.abs(a) @ np.abs(b))) / n
+        return (np.abs(f64(got) - want) / (tol * (1 + 2.0 ** -20) + (HALF_STEP["bf16"] + 2.0 ** -22) * np.abs(want) + 1e-38)).max()
+    assert worst(dw, p.T, ep.T, x) <= 1.0
+    assert worst(dh, p, ep, ww) <= 1.0
