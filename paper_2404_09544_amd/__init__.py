@@ -526,6 +526,13 @@ def _vector(t, what: str, device: int, dtype, n: int = 0):
     return t.data_ptr()
 
 
+def _torch_stream(stream):
+    """A stream that is given as a torch stream or as an address, as a torch stream."""
+    if hasattr(stream, "cuda_stream"):
+        return stream
+    return torch.cuda.ExternalStream(_stream(stream)) if _stream(stream) else torch.cuda.default_stream()
+
+
 def _workspace(given, need: int, device: int, stream):
     """(address, bytes, tensor that holds them) of a call's workspace; one that is not given comes
     from torch's allocator, in the pool of the stream that the call runs on."""
@@ -536,10 +543,7 @@ def _workspace(given, need: int, device: int, stream):
     if stream is None:
         t = torch.empty(need, dtype=torch.uint8, device="cuda")
     else:
-        address = _stream(stream)
-        st = (stream if hasattr(stream, "cuda_stream") else
-              torch.cuda.ExternalStream(address) if address else torch.cuda.default_stream())
-        with torch.cuda.stream(st):
+        with torch.cuda.stream(_torch_stream(stream)):
             t = torch.empty(need, dtype=torch.uint8, device="cuda")
     return t.data_ptr(), need, t
 

@@ -33,8 +33,8 @@ import atexit
 import numpy as np
 import torch
 
-from . import (Blocks, Cache, Graph, clip_workspace, gather, gather_n, sage_forward, sage_train_step, sample,
-               sample_async, sample_biased, sgd_clip_step, stream_create, stream_destroy, sync)
+from . import (Blocks, Cache, Graph, _torch_stream, clip_workspace, gather, gather_n, sage_forward, sage_train_step,
+               sample, sample_async, sample_biased, sgd_clip_step, stream_create, stream_destroy, sync)
 
 
 def to_device_weights(ws, dtype: str):
@@ -144,9 +144,9 @@ class MiniBatchStep:
                             grads, st)
             return
         if self._clip is None:
-            self._clip = ([torch.empty_like(w) for w in self.weights],
-                          torch.empty(clip_workspace(self.weights), dtype=torch.uint8, device="cuda"))
-            torch.cuda.current_stream().synchronize()      # the buffers are used on other streams too
+            with torch.cuda.stream(_torch_stream(st)):     # memory whose earlier work is this stream's: nothing to wait for
+                self._clip = ([torch.empty_like(w) for w in self.weights],
+                              torch.empty(clip_workspace(self.weights), dtype=torch.uint8, device="cuda"))
         own, ws = self._clip
         grads = own if grads is None else grads
         sage_train_step(self.blocks, self.h0, self.weights, self.dims, labels_dev, 0.0, self.logits, self.loss, grads, st)
