@@ -12,7 +12,7 @@
 // as a kernel argument, kClipTensors tensors a launch.
 //
 // Bound by HBM, read twice and written once: 400 million bf16 gradients 2.4 GB in
-// 500 us, 4.8 TB/s; two small tensors by their two launches, 9 us.
+// 471 us, 5.1 TB/s; two small tensors by their two launches, 9 us.
 #include <algorithm>
 
 #include "common.hpp"
@@ -28,7 +28,8 @@ constexpr int kClipTensors = 96;       // of a launch: the table stays below 4 K
 constexpr int64_t kClipChunk = 16384;  // elements a workgroup takes at a time
 constexpr int64_t kClipParts = 4096;   // part sums, at most (or one per launch)
 // Results larger than this are stored past the caches, which then hold more of the gradients for the second
-// pass: 400 million bf16 gradients over and over 493 us, 461 so; over three sets of buffers in turn 506 and 500.
+// pass: 400 million bf16 gradients, three sets of buffers in turn, 502 us, 471 so; 84 million 100.5 and 85.0.  (A kernel has
+// one kind of store: of two in the branches of an `if` the compiler makes one, of the ordinary kind.)
 constexpr int64_t kStreamBytes = int64_t(128) << 20;
 
 struct ClipTable {
@@ -73,10 +74,9 @@ __device__ __forceinline__ double norm_of(const double *parts, int32_t n_parts, 
 }
 
 // OP kNorm: one part sum per workgroup to parts[blockIdx.x].  kClip, kStep: the second pass.
-template <class T, int OP>
+template <class T, int OP, bool STREAMED>
 __global__ void __launch_bounds__(256) k_clip(const ClipTable t, double *__restrict__ parts, int32_t n_parts,
-                                              double max_norm, float lr, float *__restrict__ norm, bool in_place,
-                                              bool streamed) {
+                                              double max_norm, float lr, float *__restrict__ norm, bool in_place) {
     constexpr int N = 16 / sizeof(T);
     __shared__ double scratch[4];
     const int tid = threadIdx.x;
@@ -138,7 +138,7 @@ __global__ void __launch_bounds__(256) k_clip(const ClipTable t, double *__restr
                     if constexpr (N == 4) r[q] = __float_as_uint(y[q]);
                     else r[q] = (uint32_t)bf16_rne(y[2 * q]) | ((uint32_t)bf16_rne(y[2 * q + 1]) << 16);
                 }
-                if (streamed) __builtin_nontemporal_store(r, &ov[u]);
+                if constexpr (STREAMED) __builtin_nontemporal_store(r, &ov[u]);
                 else ov[u] = r;
             }
         };
@@ -214,11 +214,11 @@ void launch_clip(int32_t n_tensors, const void *const *grads, const int64_t *cou
         KernelTimer timer("grad_norm", s);
         const unsigned grid = (unsigned)std::min<int64_t>(chunks, most);
         if (bf16)
-            hipLaunchKernelGGL((k_clip<uint16_t, kNorm>), dim3(grid), dim3(256), 0, s, t, parts + n_parts, 0, 0.0, 0.f,
-                               nullptr, false, false);
+            hipLaunchKernelGGL((k_clip<uint16_t, kNorm, false>), dim3(grid), dim3(256), 0, s, t, parts + n_parts, 0, 0.0, 0.f,
+                               nullptr, false);
         else
-            hipLaunchKernelGGL((k_clip<float, kNorm>), dim3(grid), dim3(256), 0, s, t, parts + n_parts, 0, 0.0, 0.f,
-                               nullptr, false, false);
+            hipLaunchKernelGGL((k_clip<float, kNorm, false>), dim3(grid), dim3(256), 0, s, t, parts + n_parts, 0, 0.0, 0.f,
+                               nullptr, false);
         n_parts += (int32_t)grid;
     });
     if (!out || n_parts == 0) {
@@ -230,8 +230,14 @@ void launch_clip(int32_t n_tensors, const void *const *grads, const int64_t *cou
             KernelTimer timer(step ? "sgd_clip_step" : "clip_grads", s);
             const unsigned grid = (unsigned)std::min<int64_t>(chunks, 1024);
 #define GNNAV_L(T, OP)                                                                                                \
-    hipLaunchKernelGGL((k_clip<T, OP>), dim3(grid), dim3(256), 0, s, t, parts, n_parts, max_norm, lr, norm, in_place,   \
-                       streamed)
+    do {                                                                                                              \
+        if (streamed)                                                                                                 \
+            hipLaunchKernelGGL((k_clip<T, OP, true>), dim3(grid), dim3(256), 0, s, t, parts, n_parts, max_norm, lr,   \
+                               norm, in_place);                                                                       \
+        else                                                                                                          \
+            hipLaunchKernelGGL((k_clip<T, OP, false>), dim3(grid), dim3(256), 0, s, t, parts, n_parts, max_norm, lr,  \
+                               norm, in_place);                                                                       \
+    } while (0)
             if (step) {
                 if (bf16) GNNAV_L(uint16_t, kStep);
                 else GNNAV_L(float, kStep);

@@ -14,6 +14,7 @@
 //              zeros by the same launch.  A few ids need no sort: each
 //              position looks for its id among the others itself.
 #include <algorithm>
+#include <type_traits>
 
 #include "common.hpp"
 
@@ -68,11 +69,23 @@ struct Unit {
 };
 
 // Results larger than this are stored past the caches, which the tables and gradients being read then have for
-// themselves: 800,000 rows of 256 bytes 89 us, 79 so; the gradient of 524,288 skewed ids x 256 bf16 159 and 145.
+// themselves (smaller ones stay there for what reads them next): 800,000 rows of 256 bytes 89.3 us, 84.2 so; the gradient
+// of 524,288 skewed ids x 256 bf16 148.7 and 145.5, of 260,003 x 602 fp32 326.4 and 317.3; 67 MB of rows 31.7 and 26.1.
+// A kernel has one kind of store: of two in the branches of an `if` the compiler makes one, of the ordinary kind.
 constexpr int64_t kStreamBytes = int64_t(64) << 20;
-__device__ __forceinline__ void store(u32x4e *to, u32x4e v, bool streamed) {
-    if (streamed) __builtin_nontemporal_store(v, to);
+template <bool STREAMED>
+__device__ __forceinline__ void store(u32x4e *to, u32x4e v) {
+    if constexpr (STREAMED) __builtin_nontemporal_store(v, to);
     else *to = v;
+}
+
+// launch(g, bf16, streamed) with the last two as constants
+template <class F, class GV>
+void by_type(F &&launch, GV g, bool bf16, bool streamed) {
+    const std::true_type yes{};
+    const std::false_type no{};
+    if (bf16) streamed ? launch(g, yes, yes) : launch(g, yes, no);
+    else streamed ? launch(g, no, yes) : launch(g, no, no);
 }
 
 int lane_group(int64_t units) {   // lanes per row: the power of two that covers it, at most a wavefront
@@ -86,12 +99,12 @@ int lane_group(int64_t units) {   // lanes per row: the power of two that covers
 // ---------------------------------------------------------------- lookup
 // G lanes per row, R rows of a lane group in flight: their units are loaded
 // before any is stored; longer rows loop over slabs of G units.  Bound by HBM: 800,000 random rows of
-// 256 bytes 81 us, 5.0 TB/s; few rows by the launch.
-template <int G, int R, bool BF>
+// 256 bytes 84 us, 4.9 TB/s; few rows by the launch.
+template <int G, int R, bool BF, bool STREAMED>
 __global__ void __launch_bounds__(256) k_embedding(const u32x4e *__restrict__ table, int64_t n_rows, int64_t ld16,
                                                    int32_t units, int64_t d, const int32_t *__restrict__ ids,
                                                    const int32_t *__restrict__ n_dev, int64_t n, float scale,
-                                                   u32x4e *__restrict__ out, int64_t out_ld16, bool streamed) {
+                                                   u32x4e *__restrict__ out, int64_t out_ld16) {
     constexpr int RPW = kWave / G;
     const int lane = lane_id(), sub = lane / G, c0 = lane % G;
     if (n_dev) n = std::min<int64_t>(n, std::max<int32_t>(*n_dev, 0));
@@ -116,7 +129,7 @@ __global__ void __launch_bounds__(256) k_embedding(const u32x4e *__restrict__ ta
 #pragma unroll
                 for (int e = 0; e < Unit<BF>::N; ++e) v.v[e] *= scale;
                 if (id[r] < 0 || id[r] >= n_rows) v.zero();
-                store(&out[(i0 + r * groups) * out_ld16 + c], v.to((int64_t)c * Unit<BF>::N, d), streamed);
+                store<STREAMED>(&out[(i0 + r * groups) * out_ld16 + c], v.to((int64_t)c * Unit<BF>::N, d));
             }
         }
     }
@@ -130,17 +143,13 @@ void launch_embedding(const void *table, int64_t n_rows, int64_t ld_bytes, int64
     KernelTimer t("embedding", s);
     const unsigned grid = grid_for(n, 256 / g * 4, 4096);
     const bool streamed = n * units * 16 > kStreamBytes;
+    auto launch = [&](auto g_, auto bf_, auto st_) {
+        hipLaunchKernelGGL((k_embedding<decltype(g_)::value, 4, decltype(bf_)::value, decltype(st_)::value>), dim3(grid), dim3(256),
+                           0, s, (const u32x4e *)table, n_rows, ld_bytes / 16, units, d, ids, n_dev, n, scale, (u32x4e *)out,
+                           out_ld_bytes / 16);
+    };
 #define GNNAV_L(GV)                                                                                                 \
-    case GV:                                                                                                        \
-        if (bf16)                                                                                                   \
-            hipLaunchKernelGGL((k_embedding<GV, 4, true>), dim3(grid), dim3(256), 0, s, (const u32x4e *)table,      \
-                               n_rows, ld_bytes / 16, units, d, ids, n_dev, n, scale, (u32x4e *)out,                \
-                               out_ld_bytes / 16, streamed);                                                        \
-        else                                                                                                        \
-            hipLaunchKernelGGL((k_embedding<GV, 4, false>), dim3(grid), dim3(256), 0, s, (const u32x4e *)table,     \
-                               n_rows, ld_bytes / 16, units, d, ids, n_dev, n, scale, (u32x4e *)out,                \
-                               out_ld_bytes / 16, streamed);                                                        \
-        break
+    case GV: by_type(launch, std::integral_constant<int, GV>{}, bf16, streamed); break
     switch (g) {
         GNNAV_L(1);
         GNNAV_L(2);
@@ -478,14 +487,14 @@ int stretch_of(int64_t n, int32_t units) {
 }
 }  // namespace
 
-template <int G, int Q, bool BF>
+template <int G, int Q, bool BF, bool STREAMED>
 __global__ void __launch_bounds__(256) k_embedding_grad(const u32x4e *__restrict__ dout, int64_t ld16, int32_t units,
                                                         int64_t d, const int2 *__restrict__ pairs,
                                                         const int32_t *__restrict__ n_dev, int64_t n, float scale,
                                                         bool accumulate, u32x4e *__restrict__ dtable, int64_t n_rows,
                                                         int64_t table_ld16, float *__restrict__ part,
-                                                        const uint8_t *__restrict__ flags, int64_t blocks, int32_t stretch,
-                                                        bool streamed) {
+                                                        const uint8_t *__restrict__ flags, int64_t blocks,
+                                                        int32_t stretch) {
     constexpr int RPW = kWave / G, N = Unit<BF>::N;
     const int lane = lane_id(), sub = lane / G, cl = lane % G;
     if (n_dev) n = std::min<int64_t>(n, std::max<int32_t>(*n_dev, 0));
@@ -509,7 +518,7 @@ __global__ void __launch_bounds__(256) k_embedding_grad(const u32x4e *__restrict
                 if (row >= 0)
 #pragma unroll
                     for (int q = 0; q < Q; ++q)
-                        if (c0 + q * G < units) store(&dtable[(r0 + row) * table_ld16 + c0 + q * G], u32x4e{0, 0, 0, 0}, streamed);
+                        if (c0 + q * G < units) store<STREAMED>(&dtable[(r0 + row) * table_ld16 + c0 + q * G], u32x4e{0, 0, 0, 0});
             }
         }
         return;
@@ -534,7 +543,7 @@ __global__ void __launch_bounds__(256) k_embedding_grad(const u32x4e *__restrict
                 if (accumulate) o.from(*to);
 #pragma unroll
                 for (int x = 0; x < N; ++x) o.v[x] += scale * acc[q].v[x];
-                store(to, o.to((int64_t)c * N, d), streamed);
+                store<STREAMED>(to, o.to((int64_t)c * N, d));
             }
         } else {
             float *to = part + (2 * st + (began ? 1 : 0)) * padded;
@@ -799,17 +808,13 @@ void launch_embedding_backward(const void *dout, int64_t ld_bytes, const int32_t
         const bool streamed = n_rows * units * 16 > kStreamBytes;
         const unsigned slabs = (unsigned)((units + 3 * kWave - 1) / (3 * kWave));
         const int q = (int)((units + g * slabs - 1) / (g * slabs));
-#define GNNAV_L(GV, QV)                                                                                               \
-    do {                                                                                                              \
-        if (bf16)                                                                                                     \
-            hipLaunchKernelGGL((k_embedding_grad<GV, QV, true>), dim3((unsigned)blocks + zeros, slabs), dim3(256), 0, \
-                               s, in, ld16, units, d, pairs, n_dev, n, scale, accumulate, out, n_rows, tld16,      \
-                               part, flags, blocks, stretch, streamed);                                                                  \
-        else                                                                                                          \
-            hipLaunchKernelGGL((k_embedding_grad<GV, QV, false>), dim3((unsigned)blocks + zeros, slabs), dim3(256),   \
-                               0, s, in, ld16, units, d, pairs, n_dev, n, scale, accumulate, out, n_rows, tld16,   \
-                               part, flags, blocks, stretch, streamed);                                                                  \
-    } while (0)
+        auto launch = [&](auto gq_, auto bf_, auto st_) {
+            constexpr int GV = decltype(gq_)::value / 4, QV = decltype(gq_)::value % 4;
+            hipLaunchKernelGGL((k_embedding_grad<GV, QV, decltype(bf_)::value, decltype(st_)::value>),
+                               dim3((unsigned)blocks + zeros, slabs), dim3(256), 0, s, in, ld16, units, d, pairs, n_dev, n, scale,
+                               accumulate, out, n_rows, tld16, part, flags, blocks, stretch);
+        };
+#define GNNAV_L(GV, QV) by_type(launch, std::integral_constant<int, 4 * GV + QV>{}, bf16, streamed)
         switch (g) {
             case 1: GNNAV_L(1, 1); break;
             case 2: GNNAV_L(2, 1); break;
