@@ -485,10 +485,11 @@ gnnav_status gnnav_weight_grad(const float *self_dev, int64_t ld_self, const flo
  *
  * gnnav_embedding_backward: dtable row v = scale * sum over the i with
  * ids_dev[i] = v of dout row i, summed in fp32 in a fixed order that depends on
- * the ids alone (no floating-point atomics: repeated calls give identical bits)
- * and rounded once.  accumulate = 0: every row of dtable is written, with zeros
+ * the ids, n_ids, d and dt alone (no floating-point atomics: repeated calls give
+ * identical bits) and rounded once.  accumulate = 0: every row of dtable is written, with zeros
  * where no id names it; otherwise the sums are added to dtable's rows and the rows
- * that no id names stay as they are.  Ids outside [0, n_rows) are left out.
+ * that no id names stay as they are.  In the rows that it writes, the columns from d up
+ * to the next 16-byte boundary are written with zeros.  Ids outside [0, n_rows) are left out.
  * n_ids_dev as above.  workspace_dev: device memory of at least
  * gnnav_embedding_backward_workspace bytes (0 for few ids; -1 for bad
  * arguments; host only) on a 256-byte boundary, used until the work has run; its
@@ -514,6 +515,7 @@ gnnav_status gnnav_embedding_backward(const void *dout_dev, int64_t ld_dout, con
  *   loss_dev[0] = mean of row_loss over the rows that count;
  *   dh_i = (1/N) (sum_v p_iv w_v - w_y),  dw_v = (1/N) sum_i (p_iv - [v = y_i]) h_i,
  *   p_iv = exp(z_iv - lse_i), N = the rows that count.
+ * A class whose logit is -inf has p = 0.
  * Rows whose label is ignore_label do not count: row_loss 0, zero gradients, and
  * their h is not used (it may hold anything).  No rows that count: loss 0,
  * zero gradients.  Any other label outside [0, n_classes) makes its row's
@@ -529,9 +531,13 @@ gnnav_status gnnav_embedding_backward(const void *dout_dev, int64_t ld_dout, con
  * columns from d up to the next 16-byte boundary with zeros.  Results do not
  * depend on the run (no atomics).  workspace_dev: at least
  * gnnav_linear_xent_workspace bytes (grads: whether dh or dw is asked for; -1
- * for bad arguments; host only) on a 256-byte boundary.  It holds h and one
- * piece of the classes: some multiples of m x d, and less than 2 GiB for the
- * piece, however many classes there are (m <= 64: 2 * n_classes bytes more).  No call allocates.
+ * for bad arguments; host only) on a 256-byte boundary.  It holds h, dh in up to
+ * 128 parts of 4 bytes an entry, and a piece of the classes: their rows, at most
+ * 896 MiB or 256 classes, their p, at most 1 GiB or 256 classes (512 bytes a row
+ * of h in bf16, 1,536 in fp32), and their statistics, at most 64 MiB (512 without
+ * gradients) or 56 bytes a row of h.  Up to 64 rows (of at most 2^20 classes from 33
+ * on) it holds at most 4 bytes a class, logits, 32 MiB of them at most (256 MiB from
+ * 33 rows on), and dh in up to 1,024 parts, 33 MiB or 2 of them.  No call allocates.
  * Outputs must not overlap inputs or each other.
  * Errors: E_INVALID (null pointers, sizes, strides, alignment, workspace),
  * E_CAPACITY (a size beyond int32, d beyond 2^20), E_DEVICE.  Asynchronous. */

@@ -574,7 +574,10 @@ def embedding(table, ids, out, scale: float = 1.0, n_ids=None, n_ids_dev=None, s
     """gnnav_embedding: out[i] = scale * table[ids[i]] in the table's type (fp32 or
     bf16); an id outside the table gives a zero row.  ids: device int32 tensor,
     or the address of n_ids of them (a frontier's Blocks.nodes_ptr());
-    n_ids_dev: device int32 (tensor or address) with the count of ids to take."""
+    n_ids_dev: device int32 (tensor or address) with the count of ids to take.
+    Here and in the calls below rows start on 16-byte boundaries (GnnavError
+    otherwise), and a row that is written is written up to the next boundary, with
+    zeros behind its columns."""
     dev, dt = _here(), table.dtype
     rows, d, ld = _rows(table, "table", dev)
     n_out, _, ld_out = _rows(out, "out", dev, d, dt)

@@ -10,9 +10,11 @@
 //              stretches are joined in order afterwards.  Every lane group
 //              reads the same number of rows however popular an id is, and
 //              there are no floating-point atomics, so the bits are the same
-//              on every run.  Rows of ids that do not occur are filled with
+//              on every run (the stretches' length goes by the size of the list,
+//              and so does the order of the sums).  Rows of ids that do not occur are filled with
 //              zeros by the same launch.  A few ids need no sort: each
-//              position looks for its id among the others itself.
+//              position looks for its id among the others itself, and a popular
+//              id's rows are added up by one workgroup.
 #include <algorithm>
 #include <type_traits>
 
@@ -471,7 +473,7 @@ __global__ void __launch_bounds__(kIdThreads) k_id_scatter(const void *__restric
 // began earlier goes to part[2 * stretch], of one that begins here and goes on to
 // part[2 * stretch + 1].  Workgroups past the stretches fill the rows of ids that
 // do not occur.  Q units of a row per lane, wider rows in slabs (blockIdx.y).  Bound by HBM: 260,003 rows of
-// 602 fp32 into 233,000, 277 us, 4.3 TB/s; 524,288 skewed ones of 256 bf16 91 us, 3.9 TB/s.  Stretches of 32 ids join
+// 602 fp32 into 233,000, 273 us, 4.6 TB/s by the counters; 524,288 skewed ones of 256 bf16 79 us, 4.7 TB/s.  Stretches of 32 ids join
 // more parts (skewed 151 -> 158 us in all), of 128 leave units idle (168).  Where stretches of 64 are fewer than
 // kFullWaves wavefronts their loads are too few to hide each other: they are halved, to 8 at the least (7,124 ids of
 // 272 bf16 73 -> 37 us in all, 43,847 skewed ones of 100 83 -> 51; kFullWaves of 4,096: 218,815 skewed ones of 584 fp32

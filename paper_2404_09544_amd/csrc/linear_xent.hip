@@ -30,9 +30,9 @@
 // two, for the statistics and for the gradients (k_xent_score, k_xent_few).
 //
 // Operations: 2 m V d for each of the two logit passes, dh and dw: 8 m V d, where
-// kept logits would take 6.  8,192 x 65,536 x 1,024 bf16: 4.06 ms, 1,083 TFLOP/s of the
-// 1,307 that a library product of 8,192^3 reaches; 4,093 x 169,000 x 256 bf16 1.53 ms
-// (925); 1,024 x 169,000 x 256 fp32 2.05 ms (1,037 of bf16 part products).
+// kept logits would take 6.  8,192 x 65,536 x 1,024 bf16: 4.05 to 4.35 ms on one card and another, 1,010 to
+// 1,085 TFLOP/s of the 1,307 that a library product of 8,192^3 reaches; 4,093 x 169,000 x 256 bf16 1.51 to 1.58 ms
+// (895 to 940); 1,024 x 169,000 x 256 fp32 2.02 to 2.15 ms (990 to 1,050 of bf16 part products).
 #include <algorithm>
 #include <cmath>
 
@@ -304,8 +304,9 @@ __device__ __forceinline__ void stats_of(const XentArgs &a, f32x16x (&acc)[WMF][
 }
 
 // One tile of a product, from packed operands by way of LDS, and what becomes of it.  Bound by the matrix cores at the clock
-// that their power leaves (the same launch on zeros is 1.3 times as fast): 128 x 128 x 1,024 logit tiles 1,037
-// TFLOP/s, 256 x 256 gradient tiles 1,120-1,210, a library product of the same shapes 1,140-1,265.  Fragments that
+// that their power leaves (the same launch on zeros is 1.3 times as fast; 1.4 to 2.0 GHz by the counters, where the
+// kernels that wait for memory run at 2.4): 128 x 128 x 1,024 logit tiles 1,035 TFLOP/s, 256 x 256 gradient tiles 1,100 to
+// 1,120 of 1,024 columns and 880 to 1,020 of 256, a library product of the larger shapes 1,150 to 1,300.  Fragments that
 // are read and copies that are issued in one burst behind the barrier: 10% slower; higher priority for the
 // products, a fourth stage, 128 x 128 blocks per wavefront, groups of 4 or 16 tiles: nothing or slower.
 // AT, BT: the operand's rows are summed over.
@@ -613,12 +614,13 @@ __global__ void __launch_bounds__(64 * WGM * WGN, 2) k_xent_logits(const XentArg
 }
 
 // The logits of bf16 rows of at most 256 columns.  The tiles above copy 128 KB to LDS per 128 x 128 of them, and
-// those copies' rate (some 25 bytes a clock and unit) is their bound at so few columns: here a wavefront keeps its 32 WNF
+// those copies' rate (2.8 GB in 230 us below, some 25 bytes a clock and unit) is their bound at so few columns: here a wavefront keeps its 32 WNF
 // rows of h in registers for good (KS steps of 16 columns) and only the classes stream through LDS, 64 at a
 // time, two buffers and one barrier a tile.  A workgroup's four wavefronts hold 128 WNF rows and take a strip
 // of the piece's classes; two workgroups a unit, so that one's exponentials run beside the other's products.
 // A lane's running maximum and sum stay in registers over the strip.  4,096 x 84,736 x 256: statistics 230 us
-// with the tiles above, 167 so (1,063 TFLOP/s); probabilities 345 and 210 (the 694 MB of p go out at 3.3 TB/s).
+// with the tiles above, 157 to 186 so (955 to 1,130 TFLOP/s); probabilities 345, and 212 to 230 (the 694 MB of p go out at
+// 3.0 to 3.3 TB/s).
 constexpr int kStrip = 64;   // classes of a tile
 // Tiles of a strip, at most: the running sums round once a tile, 384 2^-24 of a sum in a strip.
 constexpr int64_t kStripTiles = 384;
