@@ -548,6 +548,91 @@ gnnav_status gnnav_linear_xent(const void *h_dev, int64_t ld_h, int64_t m, const
                                int64_t ld_dh, void *dw_dev, int64_t ld_dw, void *workspace_dev,
                                int64_t workspace_bytes, void *stream);
 
+/* ----------------------------------------------- gated feed-forward blocks ---
+ * A block that answers from a row alone, for m rows x of d columns:
+ *   a = x Wg,  b = x Wu,  h = act(a) * b (entry by entry),  y = h Wd,
+ * Wg and Wu d x f, Wd f x d_out, all row-major with strides.  act: GNNAV_ACT_SILU
+ * a / (1 + exp(-a)), GNNAV_ACT_GELU a (1 + erf(a / sqrt 2)) / 2, GNNAV_ACT_RELU.
+ * dt = F32: fp32-accurate products (six bf16 part products; an infinite entry makes
+ * its products NaN).  dt = BF16: bf16 operands, fp32 accumulation; a and b stay in
+ * fp32, h is rounded to bf16 for its product, y once.  The columns of an output
+ * row from its last to the next 16-byte boundary are written with zeros; whatever
+ * inputs hold there is not used.  m = 0 is allowed.
+ *
+ * saved_dev: NULL, or device memory of at least gnnav_gated_ffn_saved bytes (16-byte aligned)
+ * that receives a, b and h for the backward pass, in an order of the library's own.
+ *
+ * gnnav_gated_ffn_backward: from dy (m x d_out) and the saved_dev of the forward
+ * pass with the same x, weights, sizes and act:
+ *   dh = dy Wd^T,  da = dh * b * act'(a),  db = dh * act(a),
+ *   dx = da Wg^T + db Wu^T,  dWg = x^T da,  dWu = x^T db,  dWd = h^T dy.
+ * ReLU's slope at 0 is 0.  dx, dwg, dwu and dwd may each be NULL.  BF16: da and db
+ * are rounded to bf16 for their products, the gradients once.  Every row of a gradient is
+ * written (m = 0: zeros).
+ * workspace_dev: at least gnnav_gated_ffn_workspace or
+ * gnnav_gated_ffn_backward_workspace bytes (-1 for bad arguments; host only) on a
+ * 256-byte boundary, used until the work has run; its contents do not matter.  No call
+ * allocates or waits; sums run in a fixed order (no atomics: repeated calls give
+ * identical bits).  Outputs must not overlap inputs or each other.
+ * Errors: E_INVALID (null pointers, sizes, strides, alignment, act, workspace),
+ * E_CAPACITY (m beyond 2^28, d, f or d_out beyond 2^20), E_DEVICE.  Asynchronous.  */
+enum { GNNAV_ACT_SILU = 0, GNNAV_ACT_GELU = 1, GNNAV_ACT_RELU = 2 };
+int64_t gnnav_gated_ffn_workspace(int64_t m, int64_t d, int64_t f, int64_t d_out, gnnav_dtype dt);
+int64_t gnnav_gated_ffn_backward_workspace(int64_t m, int64_t d, int64_t f, int64_t d_out, gnnav_dtype dt);
+int64_t gnnav_gated_ffn_saved(int64_t m, int64_t f, gnnav_dtype dt);
+gnnav_status gnnav_gated_ffn(const void *x_dev, int64_t ld_x, int64_t m, int64_t d, const void *wg_dev, int64_t ld_wg,
+                             const void *wu_dev, int64_t ld_wu, int64_t f, const void *wd_dev, int64_t ld_wd,
+                             int64_t d_out, gnnav_dtype dt, int32_t act, void *y_dev, int64_t ld_y, void *saved_dev,
+                             int64_t saved_bytes, void *workspace_dev, int64_t workspace_bytes, void *stream);
+gnnav_status gnnav_gated_ffn_backward(const void *x_dev, int64_t ld_x, int64_t m, int64_t d, const void *wg_dev,
+                                      int64_t ld_wg, const void *wu_dev, int64_t ld_wu, int64_t f, const void *wd_dev,
+                                      int64_t ld_wd, int64_t d_out, gnnav_dtype dt, int32_t act, const void *dy_dev,
+                                      int64_t ld_dy, const void *saved_dev, int64_t saved_bytes, void *dx_dev,
+                                      int64_t ld_dx, void *dwg_dev, int64_t ld_dwg, void *dwu_dev, int64_t ld_dwu,
+                                      void *dwd_dev, int64_t ld_dwd, void *workspace_dev, int64_t workspace_bytes,
+                                      void *stream);
+
+/* ------------------------------------------------------ top logits, distillation ---
+ * gnnav_top_logits: the k largest of each of m rows of n_classes logits, in falling
+ * order, equal ones (and zeros of either sign) by rising class: values_dev (fp32) and
+ * ids_dev (int32), both [m][k] contiguous.  NaN counts as larger than any number.
+ * Places past n_classes hold -inf and -1.  1 <= k <= 256.
+ *
+ * gnnav_distill: a student's logits z (m x n_classes, dt F32 or BF16) against
+ * the k logits t that a teacher kept of each row, for the classes ids (fp32 and int32
+ * [m][k] contiguous, as gnnav_top_logits writes them), temperature T > 0:
+ *   q_j = softmax over the row's entries of t_j / T,  p = softmax(z / T),
+ *   kd_i = T^2 sum_j q_j (log q_j - log p_id(j)),
+ *   ce_i = -log softmax(z)_y, y = labels_dev[i],
+ *   loss_dev[0] = alpha loss_dev[1] + (1 - alpha) loss_dev[2], loss_dev[1] the mean
+ *   of kd over its rows, loss_dev[2] that of ce over its rows,
+ *   row_loss_dev[i] = alpha kd_i + (1 - alpha) ce_i (may be NULL),
+ *   dlogits = the gradient of loss_dev[0] (type dt; may be NULL; may be the logits themselves).
+ * An entry with a negative id or a teacher's logit of -inf is not there; a class that is
+ * named more than once has the sum of its shares.  A row without entries has no kd, a
+ * row whose label is ignore_label no ce: that part of its loss and gradient is 0, it does not
+ * count in the mean, and the logits of a row with neither are not used (they may hold
+ * anything).  An id of n_classes or more makes the row's kd NaN, a label outside
+ * [0, n_classes) its ce, with a gradient of zero for that part; they count.  A
+ * class whose logit is -inf has p = 0; a row of -inf alone gives NaN.  alpha in [0, 1]: with
+ * alpha = 0 teacher_dev and ids_dev are not used (k may be 0), with alpha = 1 or
+ * labels_dev NULL there is no ce.  Otherwise 1 <= k <= 256.  fp32 statistics; no atomics, repeated
+ * calls give identical bits.
+ * dlogits rows are written to the next 16-byte boundary, with zeros.
+ * Both: logits on 16-byte boundaries; m = 0 is allowed (losses of 0).  workspace_dev as above
+ * (gnnav_top_logits_workspace, gnnav_distill_workspace).  No call allocates or waits.
+ * Errors: E_INVALID (null pointers, sizes, strides, alignment, k, temperature, alpha,
+ * workspace), E_CAPACITY (sizes beyond int32), E_DEVICE.  Asynchronous.     */
+int64_t gnnav_top_logits_workspace(int64_t m, int64_t n_classes, int32_t k, gnnav_dtype dt);
+gnnav_status gnnav_top_logits(const void *logits_dev, int64_t ld, int64_t m, int64_t n_classes, gnnav_dtype dt, int32_t k,
+                              float *values_dev, int32_t *ids_dev, void *workspace_dev, int64_t workspace_bytes,
+                              void *stream);
+int64_t gnnav_distill_workspace(int64_t m, int64_t n_classes, int32_t k, gnnav_dtype dt);
+gnnav_status gnnav_distill(const void *logits_dev, int64_t ld, int64_t m, int64_t n_classes, gnnav_dtype dt,
+                           const int32_t *ids_dev, const float *teacher_dev, int32_t k, float temperature, float alpha,
+                           const int32_t *labels_dev, int32_t ignore_label, float *loss_dev, float *row_loss_dev,
+                           void *dlogits_dev, int64_t ld_d, void *workspace_dev, int64_t workspace_bytes, void *stream);
+
 /* ------------------------------------------------------ gradient clipping ---
  * Over n_tensors device tensors of one type (host arrays of device pointers and
  * element counts, read before the call returns; contiguous, aligned to their

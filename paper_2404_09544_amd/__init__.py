@@ -46,6 +46,8 @@ EXPORTS = [
     "gnnav_stream_create", "gnnav_stream_destroy",
     "gnnav_embedding", "gnnav_embedding_backward", "gnnav_embedding_backward_workspace",
     "gnnav_linear_xent", "gnnav_linear_xent_workspace",
+    "gnnav_gated_ffn", "gnnav_gated_ffn_backward", "gnnav_gated_ffn_workspace", "gnnav_gated_ffn_backward_workspace",
+    "gnnav_gated_ffn_saved", "gnnav_top_logits", "gnnav_top_logits_workspace", "gnnav_distill", "gnnav_distill_workspace",
     "gnnav_grad_norm", "gnnav_clip_grads", "gnnav_sgd_clip_step", "gnnav_clip_workspace",
 ]
 
@@ -113,6 +115,16 @@ _sig = {
     "gnnav_embedding_backward_workspace": ([i64, i64, i64, i32], i64),
     "gnnav_linear_xent": ([P, i64, i64, P, i64, i64, i64, i32, P, i32, P, P, P, i64, P, i64, P, i64, P], i32),
     "gnnav_linear_xent_workspace": ([i64, i64, i64, i32, i32], i64),
+    "gnnav_gated_ffn_workspace": ([i64, i64, i64, i64, i32], i64),
+    "gnnav_gated_ffn_backward_workspace": ([i64, i64, i64, i64, i32], i64),
+    "gnnav_gated_ffn_saved": ([i64, i64, i32], i64),
+    "gnnav_gated_ffn": ([P, i64, i64, i64, P, i64, P, i64, i64, P, i64, i64, i32, i32, P, i64, P, i64, P, i64, P], i32),
+    "gnnav_gated_ffn_backward": ([P, i64, i64, i64, P, i64, P, i64, i64, P, i64, i64, i32, i32, P, i64, P, i64, P, i64, P, i64,
+                                  P, i64, P, i64, P, i64, P], i32),
+    "gnnav_top_logits_workspace": ([i64, i64, i32, i32], i64),
+    "gnnav_top_logits": ([P, i64, i64, i64, i32, i32, P, P, P, i64, P], i32),
+    "gnnav_distill_workspace": ([i64, i64, i32, i32], i64),
+    "gnnav_distill": ([P, i64, i64, i64, i32, P, P, i32, C.c_float, C.c_float, P, i32, P, P, P, i64, P, i64, P], i32),
     "gnnav_grad_norm": ([i32, P, P, i32, P, P, i64, P], i32),
     "gnnav_clip_grads": ([i32, P, P, i32, C.c_float, P, P, P, i64, P], i32),
     "gnnav_sgd_clip_step": ([i32, P, P, P, i32, C.c_float, C.c_float, P, P, i64, P], i32),
@@ -645,6 +657,143 @@ def linear_xent(h, w, labels, loss, row_loss=None, dh=None, dw=None, ignore_labe
     ws, ws_bytes, _hold = _workspace(workspace, need, dev, stream)
     _check(_lib.gnnav_linear_xent(h.data_ptr(), ld_h, m, w.data_ptr(), ld_w, v, d, code, labels_ptr, ignore_label,
                                   loss_ptr, row_ptr, dh_ptr, ld_dh, dw_ptr, ld_dw, ws, ws_bytes, _on(stream, dev)))
+
+
+# ------------------------------------------ gated blocks, distillation
+ACTS = {"silu": 0, "gelu": 1, "relu": 2}
+
+
+def _act(act: str) -> int:
+    if act not in ACTS:
+        raise ValueError(f"act must be one of {', '.join(ACTS)}")
+    return ACTS[act]
+
+
+def gated_ffn_workspace(m: int, d: int, f: int, d_out: int, dtype: str) -> int:
+    """Bytes of workspace that gated_ffn needs."""
+    return _workspace_bytes(_lib.gnnav_gated_ffn_workspace(int(m), int(d), int(f), int(d_out), dtype_code(dtype)))
+
+
+def gated_ffn_backward_workspace(m: int, d: int, f: int, d_out: int, dtype: str) -> int:
+    """Bytes of workspace that gated_ffn_backward needs."""
+    return _workspace_bytes(_lib.gnnav_gated_ffn_backward_workspace(int(m), int(d), int(f), int(d_out), dtype_code(dtype)))
+
+
+def gated_ffn_saved(m: int, f: int, dtype: str) -> int:
+    """Bytes of what gated_ffn keeps for gated_ffn_backward (a uint8 tensor of at least as many)."""
+    return _workspace_bytes(_lib.gnnav_gated_ffn_saved(int(m), int(f), dtype_code(dtype)))
+
+
+def _gated(x, wg, wu, wd, dev: int):
+    """Checks a block's rows and weights; its arguments up to d_out, and (m, d, f, d_out, type)."""
+    dt = x.dtype
+    m, d, ld_x = _rows(x, "x", dev)
+    n, f, ld_wg = _rows(wg, "wg", dev, None, dt)
+    n_u, _, ld_wu = _rows(wu, "wu", dev, f, dt)
+    n_d, d_out, ld_wd = _rows(wd, "wd", dev, None, dt)
+    if n != d or n_u != d or n_d != f:
+        raise ValueError("wg and wu must be [columns of x, f], wd [f, d_out]")
+    return ((x.data_ptr(), ld_x, m, d, wg.data_ptr(), ld_wg, wu.data_ptr(), ld_wu, f, wd.data_ptr(), ld_wd, d_out),
+            (m, d, f, d_out, dt))
+
+
+def _grad(t, what: str, device: int, rows: int, cols: int, dtype):
+    """(address, stride) of a gradient that may be left out."""
+    if t is None:
+        return None, 0
+    n, _, ld = _rows(t, what, device, cols, dtype)
+    if n < rows:
+        raise ValueError(f"{what} must have {rows} rows")
+    return t.data_ptr(), ld
+
+
+def gated_ffn(x, wg, wu, wd, y, act: str = "silu", saved=None, workspace=None, stream=None):
+    """gnnav_gated_ffn: y = (act(x wg) * (x wu)) wd for x [m, d], wg and wu [d, f], wd [f, d_out],
+    fp32 or bf16; act: silu, gelu or relu.  saved: a uint8 tensor of gated_ffn_saved bytes
+    that receives what gated_ffn_backward needs."""
+    dev = _here()
+    args, (m, d, f, d_out, dt) = _gated(x, wg, wu, wd, dev)
+    n, _, ld_y = _rows(y, "y", dev, d_out, dt)
+    if n < m:
+        raise ValueError("y has fewer rows than x")
+    code, kind = _TORCH_CODE[dt], _act(act)
+    saved_ptr, saved_bytes = (None, 0) if saved is None else (_vector(saved, "saved", dev, torch.uint8), saved.numel())
+    need = 0 if workspace is not None else _workspace_bytes(_lib.gnnav_gated_ffn_workspace(m, d, f, d_out, code))
+    ws, ws_bytes, _hold = _workspace(workspace, need, dev, stream)
+    _check(_lib.gnnav_gated_ffn(*args, code, kind, y.data_ptr(), ld_y, saved_ptr, saved_bytes, ws, ws_bytes, _on(stream, dev)))
+
+
+def gated_ffn_backward(x, wg, wu, wd, dy, saved, dx=None, dwg=None, dwu=None, dwd=None, act: str = "silu", workspace=None,
+                       stream=None):
+    """gnnav_gated_ffn_backward: the gradients that are given, from dy [m, d_out] and what gated_ffn saved
+    with the same x, weights and act."""
+    dev = _here()
+    args, (m, d, f, d_out, dt) = _gated(x, wg, wu, wd, dev)
+    n, _, ld_dy = _rows(dy, "dy", dev, d_out, dt)
+    if n < m:
+        raise ValueError("dy has fewer rows than x")
+    code, kind = _TORCH_CODE[dt], _act(act)
+    saved_ptr = _vector(saved, "saved", dev, torch.uint8)
+    grads = (*_grad(dx, "dx", dev, m, d, dt), *_grad(dwg, "dwg", dev, d, f, dt), *_grad(dwu, "dwu", dev, d, f, dt),
+             *_grad(dwd, "dwd", dev, f, d_out, dt))
+    need = 0 if workspace is not None else _workspace_bytes(_lib.gnnav_gated_ffn_backward_workspace(m, d, f, d_out, code))
+    ws, ws_bytes, _hold = _workspace(workspace, need, dev, stream)
+    _check(_lib.gnnav_gated_ffn_backward(*args, code, kind, dy.data_ptr(), ld_dy, saved_ptr, saved.numel(), *grads, ws, ws_bytes,
+                                         _on(stream, dev)))
+
+
+def _kept(ids, values, what: str, device: int, m: int):
+    """Checks [m, k] class ids (int32) and logits (float32); their addresses and k."""
+    for t, name, dtype in ((ids, "ids", torch.int32), (values, what, torch.float32)):
+        if t.dim() != 2 or t.shape != ids.shape or t.shape[0] != m:
+            raise ValueError(f"ids and {what} must be [rows of logits, k]")
+        _vector(t, name, device, dtype)
+    return ids.data_ptr(), values.data_ptr(), ids.shape[1]
+
+
+def top_logits_workspace(m: int, n_classes: int, k: int, dtype: str) -> int:
+    """Bytes of workspace that top_logits needs."""
+    return _workspace_bytes(_lib.gnnav_top_logits_workspace(int(m), int(n_classes), int(k), dtype_code(dtype)))
+
+
+def top_logits(logits, values, ids, workspace=None, stream=None):
+    """gnnav_top_logits: the k largest of each row of logits [m, n_classes], in falling order, equal ones
+    by class: values (float32) and ids (int32), both [m, k].  k up to 256; places past n_classes
+    hold -inf and -1."""
+    dev = _here()
+    m, v, ld = _rows(logits, "logits", dev)
+    ids_ptr, values_ptr, k = _kept(ids, values, "values", dev, m)
+    code = _TORCH_CODE[logits.dtype]
+    need = 0
+    if workspace is None and m > 0:
+        need = _workspace_bytes(_lib.gnnav_top_logits_workspace(m, v, k, code))
+    ws, ws_bytes, _hold = _workspace(workspace, need, dev, stream)
+    _check(_lib.gnnav_top_logits(logits.data_ptr(), ld, m, v, code, k, values_ptr, ids_ptr, ws, ws_bytes, _on(stream, dev)))
+
+
+def distill_workspace(m: int, n_classes: int, k: int, dtype: str) -> int:
+    """Bytes of workspace that distill needs."""
+    return _workspace_bytes(_lib.gnnav_distill_workspace(int(m), int(n_classes), int(k), dtype_code(dtype)))
+
+
+def distill(logits, ids, teacher, loss, temperature: float = 1.0, alpha: float = 1.0, labels=None, ignore_label: int = -1,
+            row_loss=None, dlogits=None, workspace=None, stream=None):
+    """gnnav_distill: a student's logits [m, n_classes] against the teacher's logits [m, k] (float32) of
+    the classes ids [m, k] (int32; as top_logits writes them, -1 for none) at a temperature, weighed alpha, and the
+    cross entropy with labels (int32[m]), weighed 1 - alpha.  loss (float32[3]): the sum, and the
+    means of both parts; row_loss (float32[m]) and dlogits (may be logits itself) are written where given."""
+    dev, dt = _here(), logits.dtype
+    m, v, ld = _rows(logits, "logits", dev)
+    ids_ptr, teacher_ptr, k = (None, None, 0) if ids is None else _kept(ids, teacher, "teacher", dev, m)
+    labels_ptr = None if labels is None else _vector(labels, "labels", dev, torch.int32, m)
+    loss_ptr = _vector(loss, "loss", dev, torch.float32, 3)
+    row_ptr = None if row_loss is None else _vector(row_loss, "row_loss", dev, torch.float32, m)
+    d_ptr, ld_d = _grad(dlogits, "dlogits", dev, m, v, dt)
+    code = _TORCH_CODE[dt]
+    need = 0 if workspace is not None else _workspace_bytes(_lib.gnnav_distill_workspace(m, v, k, code))
+    ws, ws_bytes, _hold = _workspace(workspace, need, dev, stream)
+    _check(_lib.gnnav_distill(logits.data_ptr(), ld, m, v, code, ids_ptr, teacher_ptr, k, temperature, alpha, labels_ptr,
+                              ignore_label, loss_ptr, row_ptr, d_ptr, ld_d, ws, ws_bytes, _on(stream, dev)))
 
 
 class TensorList:

@@ -1675,6 +1675,174 @@ extern "C" gnnav_status gnnav_linear_xent(const void *h_dev, int64_t ld_h, int64
     });
 }
 
+// ------------------------------------------------ gated feed-forward blocks
+static GatedArgs gated_sizes(int64_t m, int64_t d, int64_t f, int64_t d_out, gnnav_dtype dt) {
+    GatedArgs a = {};
+    a.m = m;
+    a.d = d;
+    a.f = f;
+    a.d_out = d_out;
+    a.bf16 = dt == GNNAV_BF16;
+    return a;
+}
+static bool gated_sizes_ok(int64_t m, int64_t d, int64_t f, int64_t d_out) { return m >= 0 && d > 0 && f > 0 && d_out > 0; }
+static bool gated_sizes_fit(int64_t m, int64_t d, int64_t f, int64_t d_out) {
+    return m <= (int64_t(1) << 28) && d <= kMaxWidth && f <= kMaxWidth && d_out <= kMaxWidth;
+}
+
+extern "C" int64_t gnnav_gated_ffn_workspace(int64_t m, int64_t d, int64_t f, int64_t d_out, gnnav_dtype dt) {
+    if (!dtype_ok(dt) || !gated_sizes_ok(m, d, f, d_out) || !gated_sizes_fit(m, d, f, d_out)) return -1;
+    return (int64_t)gated_workspace(gated_sizes(m, d, f, d_out, dt), false);
+}
+extern "C" int64_t gnnav_gated_ffn_backward_workspace(int64_t m, int64_t d, int64_t f, int64_t d_out, gnnav_dtype dt) {
+    if (!dtype_ok(dt) || !gated_sizes_ok(m, d, f, d_out) || !gated_sizes_fit(m, d, f, d_out)) return -1;
+    return (int64_t)gated_workspace(gated_sizes(m, d, f, d_out, dt), true);
+}
+extern "C" int64_t gnnav_gated_ffn_saved(int64_t m, int64_t f, gnnav_dtype dt) {
+    if (!dtype_ok(dt) || !gated_sizes_ok(m, 1, f, 1) || !gated_sizes_fit(m, 1, f, 1)) return -1;
+    return (int64_t)gated_saved(m, f, dt == GNNAV_BF16);
+}
+
+// what the forward and the backward pass have in common
+static GatedArgs gated_args(const void *x, int64_t ld_x, int64_t m, int64_t d, const void *wg, int64_t ld_wg, const void *wu,
+                            int64_t ld_wu, int64_t f, const void *wd, int64_t ld_wd, int64_t d_out, gnnav_dtype dt, int32_t act) {
+    GNNAV_CHECK(dtype_ok(dt), GNNAV_E_INVALID, "bad dtype");
+    GNNAV_CHECK(act >= GNNAV_ACT_SILU && act <= GNNAV_ACT_RELU, GNNAV_E_INVALID, "bad act");
+    GNNAV_CHECK(gated_sizes_ok(m, d, f, d_out), GNNAV_E_INVALID, "m < 0, or d, f or d_out <= 0");
+    GNNAV_CHECK(gated_sizes_fit(m, d, f, d_out), GNNAV_E_CAPACITY, "m beyond 2^28, or rows wider than 2^20");
+    const int64_t elt = dt == GNNAV_BF16 ? 2 : 4;
+    if (m > 0) check_rows(x, ld_x, d, elt, "x");
+    check_rows(wg, ld_wg, f, elt, "wg");
+    check_rows(wu, ld_wu, f, elt, "wu");
+    check_rows(wd, ld_wd, d_out, elt, "wd");
+    GatedArgs a = gated_sizes(m, d, f, d_out, dt);
+    a.x = x;
+    a.ld_x = ld_x;
+    a.wg = wg;
+    a.ld_wg = ld_wg;
+    a.wu = wu;
+    a.ld_wu = ld_wu;
+    a.wd = wd;
+    a.ld_wd = ld_wd;
+    a.act = act;
+    return a;
+}
+static void check_saved(const void *saved, int64_t bytes, const GatedArgs &a) {
+    const int64_t need = (int64_t)gated_saved(a.m, a.f, a.bf16);
+    GNNAV_CHECK(bytes >= need, GNNAV_E_INVALID, "saved of " + std::to_string(bytes) + " bytes, " + std::to_string(need) + " needed");
+    GNNAV_CHECK(need == 0 || (saved && aligned16(saved)), GNNAV_E_INVALID, "saved must be on a 16-byte boundary");
+}
+
+extern "C" gnnav_status gnnav_gated_ffn(const void *x_dev, int64_t ld_x, int64_t m, int64_t d, const void *wg_dev, int64_t ld_wg,
+                                        const void *wu_dev, int64_t ld_wu, int64_t f, const void *wd_dev, int64_t ld_wd,
+                                        int64_t d_out, gnnav_dtype dt, int32_t act, void *y_dev, int64_t ld_y, void *saved_dev,
+                                        int64_t saved_bytes, void *workspace_dev, int64_t workspace_bytes, void *stream) {
+    return guarded([&] {
+        GatedArgs a = gated_args(x_dev, ld_x, m, d, wg_dev, ld_wg, wu_dev, ld_wu, f, wd_dev, ld_wd, d_out, dt, act);
+        if (m == 0) return;
+        check_rows(y_dev, ld_y, d_out, a.bf16 ? 2 : 4, "y");
+        if (saved_dev) check_saved(saved_dev, saved_bytes, a);
+        check_workspace(workspace_dev, workspace_bytes, gated_workspace(a, false));
+        a.y = y_dev;
+        a.ld_y = ld_y;
+        a.saved = saved_dev;
+        a.workspace = workspace_dev;
+        launch_gated(a, false, (hipStream_t)stream);
+    });
+}
+
+extern "C" gnnav_status gnnav_gated_ffn_backward(const void *x_dev, int64_t ld_x, int64_t m, int64_t d, const void *wg_dev,
+                                                 int64_t ld_wg, const void *wu_dev, int64_t ld_wu, int64_t f, const void *wd_dev,
+                                                 int64_t ld_wd, int64_t d_out, gnnav_dtype dt, int32_t act, const void *dy_dev,
+                                                 int64_t ld_dy, const void *saved_dev, int64_t saved_bytes, void *dx_dev,
+                                                 int64_t ld_dx, void *dwg_dev, int64_t ld_dwg, void *dwu_dev, int64_t ld_dwu,
+                                                 void *dwd_dev, int64_t ld_dwd, void *workspace_dev, int64_t workspace_bytes,
+                                                 void *stream) {
+    return guarded([&] {
+        GatedArgs a = gated_args(x_dev, ld_x, m, d, wg_dev, ld_wg, wu_dev, ld_wu, f, wd_dev, ld_wd, d_out, dt, act);
+        const int64_t elt = a.bf16 ? 2 : 4;
+        if (m > 0) check_rows(dy_dev, ld_dy, d_out, elt, "dy");
+        check_saved(saved_dev, saved_bytes, a);
+        if (dx_dev && m > 0) check_rows(dx_dev, ld_dx, d, elt, "dx");
+        if (dwg_dev) check_rows(dwg_dev, ld_dwg, f, elt, "dwg");
+        if (dwu_dev) check_rows(dwu_dev, ld_dwu, f, elt, "dwu");
+        if (dwd_dev) check_rows(dwd_dev, ld_dwd, d_out, elt, "dwd");
+        check_workspace(workspace_dev, workspace_bytes, gated_workspace(a, true));
+        a.dy = dy_dev;
+        a.ld_dy = ld_dy;
+        a.saved = const_cast<void *>(saved_dev);
+        a.dx = dx_dev;
+        a.ld_dx = ld_dx;
+        a.dwg = dwg_dev;
+        a.ld_dwg = ld_dwg;
+        a.dwu = dwu_dev;
+        a.ld_dwu = ld_dwu;
+        a.dwd = dwd_dev;
+        a.ld_dwd = ld_dwd;
+        a.workspace = workspace_dev;
+        launch_gated(a, true, (hipStream_t)stream);
+    });
+}
+
+// ------------------------------------------------ top logits, distillation
+static constexpr int32_t kMaxTop = 256;
+
+extern "C" int64_t gnnav_top_logits_workspace(int64_t m, int64_t n_classes, int32_t k, gnnav_dtype dt) {
+    if (!dtype_ok(dt) || m < 0 || n_classes <= 0 || m > INT32_MAX || n_classes > INT32_MAX || k < 1 || k > kMaxTop) return -1;
+    return (int64_t)top_logits_workspace(m, n_classes, k);
+}
+extern "C" gnnav_status gnnav_top_logits(const void *logits_dev, int64_t ld, int64_t m, int64_t n_classes, gnnav_dtype dt,
+                                         int32_t k, float *values_dev, int32_t *ids_dev, void *workspace_dev,
+                                         int64_t workspace_bytes, void *stream) {
+    return guarded([&] {
+        GNNAV_CHECK(dtype_ok(dt), GNNAV_E_INVALID, "bad dtype");
+        GNNAV_CHECK(m >= 0 && n_classes > 0, GNNAV_E_INVALID, "m < 0 or n_classes <= 0");
+        GNNAV_CHECK(k >= 1 && k <= kMaxTop, GNNAV_E_INVALID, "k outside [1, 256]");
+        GNNAV_CHECK(m <= INT32_MAX && n_classes <= INT32_MAX, GNNAV_E_CAPACITY, "sizes beyond int32");
+        if (m == 0) return;
+        check_rows(logits_dev, ld, n_classes, dt == GNNAV_BF16 ? 2 : 4, "logits");
+        GNNAV_CHECK(values_dev && ids_dev, GNNAV_E_INVALID, "NULL values or ids");
+        check_workspace(workspace_dev, workspace_bytes, top_logits_workspace(m, n_classes, k));
+        launch_top_logits(logits_dev, ld, m, n_classes, dt == GNNAV_BF16, k, values_dev, ids_dev, workspace_dev,
+                          (hipStream_t)stream);
+    });
+}
+
+extern "C" int64_t gnnav_distill_workspace(int64_t m, int64_t n_classes, int32_t k, gnnav_dtype dt) {
+    if (!dtype_ok(dt) || m < 0 || n_classes <= 0 || m > INT32_MAX || n_classes > INT32_MAX || k < 0 || k > kMaxTop) return -1;
+    return (int64_t)distill_workspace(m);
+}
+extern "C" gnnav_status gnnav_distill(const void *logits_dev, int64_t ld, int64_t m, int64_t n_classes, gnnav_dtype dt,
+                                      const int32_t *ids_dev, const float *teacher_dev, int32_t k, float temperature,
+                                      float alpha, const int32_t *labels_dev, int32_t ignore_label, float *loss_dev,
+                                      float *row_loss_dev, void *dlogits_dev, int64_t ld_d, void *workspace_dev,
+                                      int64_t workspace_bytes, void *stream) {
+    return guarded([&] {
+        GNNAV_CHECK(dtype_ok(dt), GNNAV_E_INVALID, "bad dtype");
+        GNNAV_CHECK(m >= 0 && n_classes > 0, GNNAV_E_INVALID, "m < 0 or n_classes <= 0");
+        GNNAV_CHECK(m <= INT32_MAX && n_classes <= INT32_MAX, GNNAV_E_CAPACITY, "sizes beyond int32");
+        GNNAV_CHECK(alpha >= 0.f && alpha <= 1.f, GNNAV_E_INVALID, "alpha outside [0, 1]");
+        GNNAV_CHECK(temperature > 0.f && std::isfinite(temperature) && std::isfinite(1.f / temperature), GNNAV_E_INVALID,
+                    "temperature is not positive and finite");
+        GNNAV_CHECK(alpha == 0.f ? k >= 0 && k <= kMaxTop : k >= 1 && k <= kMaxTop, GNNAV_E_INVALID, "k outside [1, 256]");
+        GNNAV_CHECK(loss_dev, GNNAV_E_INVALID, "NULL loss");
+        const int64_t elt = dt == GNNAV_BF16 ? 2 : 4;
+        if (m > 0) {
+            check_rows(logits_dev, ld, n_classes, elt, "logits");
+            GNNAV_CHECK(alpha == 0.f || (ids_dev && teacher_dev), GNNAV_E_INVALID, "NULL ids or teacher");
+            if (dlogits_dev) {
+                check_rows(dlogits_dev, ld_d, n_classes, elt, "dlogits");
+                GNNAV_CHECK(dlogits_dev != logits_dev || ld_d == ld, GNNAV_E_INVALID, "dlogits in place needs the logits' stride");
+            }
+        }
+        check_workspace(workspace_dev, workspace_bytes, distill_workspace(m));
+        DistillArgs x = {logits_dev, ld, m, n_classes, dt == GNNAV_BF16, ids_dev, teacher_dev, k, temperature, alpha,
+                         alpha < 1.f ? labels_dev : nullptr, ignore_label, loss_dev, row_loss_dev, dlogits_dev, ld_d,
+                         workspace_dev};
+        launch_distill(x, (hipStream_t)stream);
+    });
+}
+
 extern "C" int64_t gnnav_clip_workspace(int32_t n_tensors) {
     return n_tensors < 0 ? -1 : (int64_t)clip_workspace(n_tensors);
 }

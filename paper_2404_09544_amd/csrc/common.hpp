@@ -368,6 +368,56 @@ struct LinearXentArgs {
 size_t linear_xent_workspace(int64_t m, int64_t n_classes, int64_t d, bool bf16, bool grads);
 void launch_linear_xent(const LinearXentArgs &x, hipStream_t s);
 
+// gated.hip: gated feed-forward blocks and their backward pass
+struct GatedArgs {
+    const void *x;
+    int64_t ld_x, m, d;
+    const void *wg;
+    int64_t ld_wg;
+    const void *wu;
+    int64_t ld_wu, f;
+    const void *wd;
+    int64_t ld_wd, d_out;
+    bool bf16;
+    int32_t act;
+    void *y;                  // forward
+    int64_t ld_y;
+    const void *dy;           // backward
+    int64_t ld_dy;
+    void *dx, *dwg, *dwu, *dwd;   // nullable
+    int64_t ld_dx, ld_dwg, ld_dwu, ld_dwd;
+    void *saved;              // forward: nullable
+    void *workspace;
+};
+size_t gated_workspace(const GatedArgs &a, bool backward);   // of its sizes
+size_t gated_saved(int64_t m, int64_t f, bool bf16);
+void launch_gated(const GatedArgs &x, bool backward, hipStream_t s);
+
+// top_logits.hip: the k largest logits of each row
+size_t top_logits_workspace(int64_t m, int64_t n_classes, int64_t k);
+void launch_top_logits(const void *logits, int64_t ld, int64_t m, int64_t n_classes, bool bf16, int32_t k, float *values,
+                       int32_t *ids, void *ws, hipStream_t s);
+
+// distill.hip: divergence from a teacher's top logits, with the labels' cross entropy
+struct DistillArgs {
+    const void *logits;
+    int64_t ld, m, n_classes;
+    bool bf16;
+    const int32_t *ids;       // [m][k]
+    const float *teacher;     // [m][k]
+    int32_t k;
+    float temperature, alpha;
+    const int32_t *labels;    // nullable
+    int32_t ignore;
+    float *loss;              // [3]
+    float *row_loss;          // nullable
+    void *dlogits;            // nullable
+    int64_t ld_d;
+    void *workspace;
+};
+size_t distill_workspace(int64_t m);
+void launch_distill(const DistillArgs &x, hipStream_t s);
+
 // clip.hip: out nullptr: the norm alone; step: out holds weights, which take
 // -lr * c * g; otherwise out = c * g
 size_t clip_workspace(int64_t n_tensors);
