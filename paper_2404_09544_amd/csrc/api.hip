@@ -1810,7 +1810,7 @@ extern "C" gnnav_status gnnav_top_logits(const void *logits_dev, int64_t ld, int
 
 extern "C" int64_t gnnav_distill_workspace(int64_t m, int64_t n_classes, int32_t k, gnnav_dtype dt) {
     if (!dtype_ok(dt) || m < 0 || n_classes <= 0 || m > INT32_MAX || n_classes > INT32_MAX || k < 0 || k > kMaxTop) return -1;
-    return (int64_t)distill_workspace(m);
+    return (int64_t)distill_workspace(m, n_classes, k, dt == GNNAV_BF16);
 }
 extern "C" gnnav_status gnnav_distill(const void *logits_dev, int64_t ld, int64_t m, int64_t n_classes, gnnav_dtype dt,
                                       const int32_t *ids_dev, const float *teacher_dev, int32_t k, float temperature,
@@ -1835,7 +1835,7 @@ extern "C" gnnav_status gnnav_distill(const void *logits_dev, int64_t ld, int64_
                 GNNAV_CHECK(dlogits_dev != logits_dev || ld_d == ld, GNNAV_E_INVALID, "dlogits in place needs the logits' stride");
             }
         }
-        check_workspace(workspace_dev, workspace_bytes, distill_workspace(m));
+        check_workspace(workspace_dev, workspace_bytes, distill_workspace(m, n_classes, k, dt == GNNAV_BF16));
         DistillArgs x = {logits_dev, ld, m, n_classes, dt == GNNAV_BF16, ids_dev, teacher_dev, k, temperature, alpha,
                          alpha < 1.f ? labels_dev : nullptr, ignore_label, loss_dev, row_loss_dev, dlogits_dev, ld_d,
                          workspace_dev};

@@ -415,7 +415,7 @@ struct DistillArgs {
     int64_t ld_d;
     void *workspace;
 };
-size_t distill_workspace(int64_t m);
+size_t distill_workspace(int64_t m, int64_t n_classes, int64_t k, bool bf16);
 void launch_distill(const DistillArgs &x, hipStream_t s);
 
 // clip.hip: out nullptr: the norm alone; step: out holds weights, which take

@@ -5,36 +5,38 @@
 //   kd_i = T^2 sum_j q_j (log q_j - (z_j - M) / T + log s(T)),   ce_i = log s(1) - (z_y - M)
 //   dz_v = alpha T / A (p_v(T) - sum_{j: id_j = v} q_j) + (1 - alpha) / B (p_v(1) - [v = y_i])
 //
-// A the rows with entries, B those with a label that counts.  Bound by memory: the logits are read once where a row's fit the
-// registers, and the gradient written once.
+// A the rows with entries, B those with a label that counts.  Bound by memory: a row is read once, into the registers of a
+// team of 16 lanes to four wavefronts, and its gradient written from them.  Rows of more classes are cut into strips, whose
+// sums take a launch of their own, by groups of rows that the memory-side cache still holds when the gradient reads them again.
 #include <algorithm>
 #include <cmath>
 
 #include "common.hpp"
+#include "lanes.hpp"
 
 namespace gnnav {
 
 namespace {
 
 typedef uint32_t u32x4x __attribute__((ext_vector_type(4)));
-typedef uint32_t u32x2x __attribute__((ext_vector_type(2)));
-constexpr float kLog2e = 1.44269504088896340736f;
-constexpr int kParts = 256;   // counts of rows, at most
+constexpr double kLog2e = 1.44269504088896340736;
+constexpr int kParts = 1024;   // counts of rows, at most
 constexpr int kMost = 256;    // entries of a row, at most
+constexpr int kSplitVectors = 4;   // 16-byte vectors of a thread in a strip
+constexpr int kBlocks = 2048;      // workgroups that take whole rows, at most
 
 struct Args {
     DistillArgs x;
     int2 *counts;        // [parts]: rows with entries, with labels
-    int32_t parts;
-    float *kd, *ce;      // [m]
+    int32_t parts;       // 0: every workgroup counts for itself
+    double2 *losses;     // [n_losses]: sums of both parts of the loss
+    int32_t n_losses;
+    int64_t first;       // strips > 0: first row of the group
+    float scale, inv_t;  // log2(e) times what the logits are divided by (1 / T, or 1 where there is no teacher's part); 1 / T
+    int32_t strips, width;
+    float4 *sums;        // strips > 0: [m][strips] largest logit, sums at T and at 1
+    float *own;          // ... and [m][k + 1] logits of the entries' classes and of the label
 };
-
-// exp(x c): fp32 logits by expf, bf16 ones, whose own rounding is coarser, by the hardware's exp2
-template <bool BF>
-__device__ __forceinline__ float exp_of(float x, float inv_t) {
-    if constexpr (BF) return __builtin_amdgcn_exp2f(x * (inv_t * kLog2e));
-    else return expf(x * inv_t);
-}
 
 __device__ __forceinline__ bool entry_there(int32_t id, float t) { return id >= 0 && t != -INFINITY; }
 
@@ -44,93 +46,164 @@ __device__ __forceinline__ uint32_t bf16_pair(float lo, float hi) {
     return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{lo, hi}, bf16x2));
 }
 
-// Max, or sum, over a workgroup of NT threads; scratch: NT / 64 values of LDS.
-template <int NT, bool MAX>
-__device__ __forceinline__ float reduce(float x, float *scratch) {
-#pragma unroll
-    for (int o = 1; o < kWave; o <<= 1) {
-        const float y = __shfl_xor(x, o, kWave);
-        x = MAX ? fmaxf(x, y) : x + y;
-    }
-    if (NT == kWave) return x;
-    if (lane_id() == 0) scratch[threadIdx.x / kWave] = x;
-    __syncthreads();
-    x = scratch[0];
-#pragma unroll
-    for (int w = 1; w < NT / kWave; ++w) x = MAX ? fmaxf(x, scratch[w]) : x + scratch[w];
-    __syncthreads();
-    return x;
+template <bool BF>
+__device__ __forceinline__ float element(const u32x4x &v, int e) {
+    if constexpr (BF) return __uint_as_float(e & 1 ? v[e / 2] & 0xffff0000u : v[e / 2] << 16);
+    else return __uint_as_float(v[e]);
 }
+template <bool BF>
+__device__ __forceinline__ float logit(const char *row, int64_t c) {
+    if constexpr (BF) return bf16_to_f32(((const uint16_t *)row)[c]);
+    else return ((const float *)row)[c];
+}
+
+// 16 bytes of a row from class c on, -inf past the last class.
+template <bool BF>
+__device__ __forceinline__ u32x4x load(const char *row, int64_t c, int64_t end) {
+    constexpr int PER = BF ? 8 : 4;
+    constexpr uint32_t NONE = BF ? 0xff80ff80u : 0xff800000u;
+    u32x4x v = {NONE, NONE, NONE, NONE};
+    if (c < end) v = *(const u32x4x *)(row + c * (BF ? 2 : 4));
+    if (c < end && c + PER > end)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            if constexpr (BF) {
+                if (c + 2 * e + 1 >= end) v[e] = (v[e] & 0xffffu) | (NONE & 0xffff0000u);
+                if (c + 2 * e >= end) v[e] = NONE;
+            } else if (c + e >= end) {
+                v[e] = NONE;
+            }
+        }
+    return v;
+}
+
+// What the T threads of a row's team have in common.  Round r of its reductions has a place of its own in LDS, so that one
+// barrier does for each.
+template <int T>
+struct Team {
+    static constexpr int W = T > 64 ? T / 64 : 1;
+    float (*scratch)[W];   // [places][W]
+    __device__ __forceinline__ void sync() const {
+        if constexpr (T > 64) {
+            __syncthreads();
+        } else {
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+        }
+    }
+    template <bool MAX>
+    __device__ __forceinline__ float within(float x, int place) const {
+        x = lanes_reduce<(T < 64 ? T : 64), MAX>(x);
+        if constexpr (T > 64)
+            if (lane_id() == 0) scratch[place][threadIdx.x / 64] = x;
+        return x;
+    }
+    template <bool MAX>
+    __device__ __forceinline__ float across(float x, int place) const {
+        if constexpr (T > 64) {
+            x = scratch[place][0];
+#pragma unroll
+            for (int w = 1; w < W; ++w) x = MAX ? fmaxf(x, scratch[place][w]) : x + scratch[place][w];
+        }
+        return x;
+    }
+};
+
+// Rows with entries and rows with labels that count, of those that this thread looks at: most rows show by their first entry.
+__device__ __forceinline__ int2 count_rows(const DistillArgs &x, int64_t first, int64_t step) {
+    int32_t n = 0, l = 0;
+#pragma unroll 4
+    for (int64_t i = first; i < x.m; i += step) {
+        bool any = x.k > 0 && entry_there(x.ids[i * x.k], x.teacher[i * x.k]);
+        if (!any)
+            for (int32_t j = 1; j < x.k && !any; ++j) any = entry_there(x.ids[i * x.k + j], x.teacher[i * x.k + j]);
+        n += any;
+        if (x.labels) l += x.labels[i] != x.ignore;
+    }
+    return make_int2(n, l);
+}
+// ... and their sum over a workgroup of NT threads, in every thread; s: LDS.
+template <int NT>
+__device__ __forceinline__ int2 sum_counts(int2 c, int2 *s) {
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        c.x += __shfl_xor(c.x, o, 64);
+        c.y += __shfl_xor(c.y, o, 64);
+    }
+    if (lane_id() == 0) s[threadIdx.x / 64] = c;
+    __syncthreads();
+    c = s[0];
+#pragma unroll
+    for (int w = 1; w < NT / 64; ++w) {
+        c.x += s[w].x;
+        c.y += s[w].y;
+    }
+    return c;
+}
+
+// A running largest logit, the sums of exponentials less it.
+struct Sums {
+    float top = -INFINITY, st = 0.f, s1 = 0.f;
+};
+__device__ __forceinline__ float exp_of(float x, float scale) { return __builtin_amdgcn_exp2f(x * scale); }
 
 }  // namespace
 
-// Rows with entries and rows with labels that count, by parts.
+// Rows with entries and rows with labels that count, by parts: 16 lanes a row.
 __global__ void __launch_bounds__(256) k_distill_count(const Args a) {
-    const DistillArgs &x = a.x;
-    int32_t n = 0, l = 0;
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < x.m; i += (int64_t)gridDim.x * 256) {
-        if (x.alpha > 0.f) {
-            bool any = false;
-            for (int32_t j = 0; j < x.k && !any; ++j) any = entry_there(x.ids[i * x.k + j], x.teacher[i * x.k + j]);
-            n += any;
-        }
-        if (x.labels) l += x.labels[i] != x.ignore;
-    }
-#pragma unroll
-    for (int o = 1; o < kWave; o <<= 1) {
-        n += __shfl_xor(n, o, kWave);
-        l += __shfl_xor(l, o, kWave);
-    }
     __shared__ int2 s[4];
-    if (lane_id() == 0) s[threadIdx.x / kWave] = make_int2(n, l);
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        for (int w = 1; w < 4; ++w) {
-            n += s[w].x;
-            l += s[w].y;
+    const DistillArgs &x = a.x;
+    const int lane = threadIdx.x % 16, shift = lane_id() & 48;
+    int32_t n = 0, l = 0;
+    for (int64_t first = (int64_t)blockIdx.x * 16; first < x.m; first += (int64_t)gridDim.x * 16) {
+        const int64_t i = first + threadIdx.x / 16;
+        bool any = false;
+        for (int32_t j = lane; i < x.m && j < x.k; j += 16) any |= entry_there(x.ids[i * x.k + j], x.teacher[i * x.k + j]);
+        const bool row = (__ballot(any) >> shift & 0xffff) != 0;
+        if (lane == 0 && i < x.m) {
+            n += row;
+            if (x.labels) l += x.labels[i] != x.ignore;
         }
-        a.counts[blockIdx.x] = make_int2(n, l);
     }
+    const int2 c = sum_counts<256>(make_int2(n, l), s);
+    if (threadIdx.x == 0) a.counts[blockIdx.x] = c;
 }
 
 // The losses' means, in 64 bits and a fixed order.
-__global__ void __launch_bounds__(1024) k_distill_mean(const Args a) {
+__global__ void __launch_bounds__(256) k_distill_mean(const Args a) {
     const DistillArgs &x = a.x;
+    __shared__ double sd[4][2];
+    __shared__ int2 si[4];
     double kd = 0.0, ce = 0.0;
-    int64_t n = 0, l = 0;
-    for (int64_t i = threadIdx.x; i < x.m; i += 1024) {
-        kd += (double)a.kd[i];
-        ce += (double)a.ce[i];
+#pragma unroll 8
+    for (int32_t i = threadIdx.x; i < a.n_losses; i += 256) {
+        const double2 p = a.losses[i];
+        kd += p.x;
+        ce += p.y;
     }
-    if ((int)threadIdx.x < a.parts) {
-        n = a.counts[threadIdx.x].x;
-        l = a.counts[threadIdx.x].y;
+    int2 c = make_int2(0, 0);
+    for (int32_t i = threadIdx.x; i < std::max(a.parts, 1); i += 256) {
+        const int2 p = a.counts[i];
+        c.x += p.x;
+        c.y += p.y;
     }
 #pragma unroll
-    for (int o = 1; o < kWave; o <<= 1) {
-        kd += __shfl_xor(kd, o, kWave);
-        ce += __shfl_xor(ce, o, kWave);
-        n += __shfl_xor(n, o, kWave);
-        l += __shfl_xor(l, o, kWave);
+    for (int o = 1; o < 64; o <<= 1) {
+        kd += __shfl_xor(kd, o, 64);
+        ce += __shfl_xor(ce, o, 64);
     }
-    __shared__ double sd[16][2];
-    __shared__ int64_t si[16][2];
     if (lane_id() == 0) {
-        sd[threadIdx.x / kWave][0] = kd;
-        sd[threadIdx.x / kWave][1] = ce;
-        si[threadIdx.x / kWave][0] = n;
-        si[threadIdx.x / kWave][1] = l;
+        sd[threadIdx.x / 64][0] = kd;
+        sd[threadIdx.x / 64][1] = ce;
     }
-    __syncthreads();
+    c = sum_counts<256>(c, si);
     if (threadIdx.x == 0) {
-        for (int w = 1; w < 16; ++w) {
+        for (int w = 1; w < 4; ++w) {
             kd += sd[w][0];
             ce += sd[w][1];
-            n += si[w][0];
-            l += si[w][1];
         }
-        kd = n ? kd / (double)n : 0.0;
-        ce = l ? ce / (double)l : 0.0;
+        kd = c.x ? kd / (double)c.x : 0.0;
+        ce = c.y ? ce / (double)c.y : 0.0;
         const double first = x.alpha > 0.f ? (double)x.alpha * kd : 0.0, second = x.alpha < 1.f ? (1.0 - (double)x.alpha) * ce : 0.0;
         x.loss[0] = (float)(first + second);
         x.loss[1] = (float)kd;
@@ -138,262 +211,376 @@ __global__ void __launch_bounds__(1024) k_distill_mean(const Args a) {
     }
 }
 
-namespace {
-
-template <bool BF>
-__device__ __forceinline__ float element(const u32x4x &v, int e) {
-    if constexpr (BF) return __uint_as_float(e & 1 ? v[e / 2] & 0xffff0000u : v[e / 2] << 16);
-    else return __uint_as_float(v[e]);
-}
-
-// A running largest logit and the sums of exponentials less it.
-struct Sums {
-    float top = -INFINITY, st = 0.f, s1 = 0.f;
-};
-
-template <bool BF>
-__device__ __forceinline__ void add(Sums &s, const float *z, int n, float inv_t, bool both) {
-    float mx = s.top;
+// The sums of one strip of a row, and the logits that are needed by themselves (the gradient may take their place).
+template <bool BF, bool BOTH>
+__global__ void __launch_bounds__(256) k_distill_sums(const Args a) {
+    constexpr int PER = BF ? 8 : 4;
+    __shared__ float scratch[3][4];
+    const DistillArgs &x = a.x;
+    const Team<256> team = {scratch};
+    const int tid = threadIdx.x;
+    const int64_t row = a.first + blockIdx.y, begin = (int64_t)blockIdx.x * a.width, end = std::min(x.n_classes, begin + a.width);
+    const char *src = (const char *)x.logits + row * x.ld * (BF ? 2 : 4);
+    u32x4x v[kSplitVectors];
 #pragma unroll
-    for (int e = 0; e < n; ++e) mx = fmaxf(mx, z[e]);
-    if (mx > s.top) {
-        s.st *= exp_of<BF>(s.top - mx, inv_t);
-        if (both) s.s1 *= exp_of<BF>(s.top - mx, 1.f);
-        s.top = mx;
-    }
+    for (int i = 0; i < kSplitVectors; ++i) v[i] = load<BF>(src, begin + (i * 256 + tid) * PER, end);
+    Sums s;
+#pragma unroll
+    for (int i = 0; i < kSplitVectors; ++i)
+#pragma unroll
+        for (int e = 0; e < PER; ++e) s.top = fmaxf(s.top, element<BF>(v[i], e));
     const float ref = s.top == -INFINITY ? 0.f : s.top;
 #pragma unroll
-    for (int e = 0; e < n; ++e) {
-        s.st += exp_of<BF>(z[e] - ref, inv_t);
-        if (both) s.s1 += exp_of<BF>(z[e] - ref, 1.f);
+    for (int i = 0; i < kSplitVectors; ++i)
+#pragma unroll
+        for (int e = 0; e < PER; ++e) {
+            s.st += exp_of(element<BF>(v[i], e) - ref, a.scale);
+            if constexpr (BOTH) s.s1 += exp_of(element<BF>(v[i], e) - ref, (float)kLog2e);
+        }
+    const float top = team.across<true>((team.within<true>(s.top, 0), team.sync(), 0.f), 0);
+    const float ft = s.top == -INFINITY ? 1.f : exp_of(s.top - top, a.scale), f1 = s.top == -INFINITY ? 1.f : exp_of(s.top - top, (float)kLog2e);
+    team.within<false>(s.st * ft, 1);
+    if constexpr (BOTH) team.within<false>(s.s1 * f1, 2);
+    team.sync();
+    if (tid == 0) {
+        const float st = team.across<false>(0.f, 1);
+        a.sums[row * a.strips + blockIdx.x] = make_float4(top, st, BOTH ? team.across<false>(0.f, 2) : st, 0.f);
+    }
+    for (int32_t j = tid; j <= x.k; j += 256) {
+        const int32_t id = j < x.k ? (x.alpha > 0.f ? x.ids[row * x.k + j] : -1) : x.labels ? x.labels[row] : -1;
+        if (id >= begin && id < end) a.own[row * (x.k + 1) + j] = logit<BF>(src, id);
     }
 }
 
-}  // namespace
-
-// One row a workgroup of NT threads.  Its first NV vectors of 16 bytes a thread stay in registers; what is beyond them
-// is read again for the gradient.
-template <bool BF, int NT, int NV>
-__device__ __forceinline__ void distill_row(const Args &a, int64_t row) {
-    constexpr int PER = BF ? 8 : 4;
+// One row, by the team of T threads that calls it.  VEC: 16-byte loads (otherwise a class a lane); NV of them a thread stay
+// in registers.  SPLIT: the sums are there, and strip `strip` of the gradient is written.
+template <bool BF, int T, int NV, bool VEC, bool BOTH, bool SPLIT>
+__device__ __forceinline__ void distill_row(const Args &a, int64_t row, int32_t strip, bool live, int2 counted_rows, const Team<T> &team, int32_t *ids,
+                                            float *share, double2 &loss) {
+    constexpr int PER = !VEC ? 1 : BF ? 8 : 4, ELT = BF ? 2 : 4;
+    constexpr bool EXPS = VEC && !BF && !BOTH && !SPLIT;   // the kept logits give way to their exponentials
     const DistillArgs &x = a.x;
-    __shared__ float scratch[NT / kWave];
-    __shared__ int32_t ids[kMost];
-    __shared__ float share[kMost];
-    __shared__ int32_t flags[4];
-    const int tid = threadIdx.x;
-    const int32_t C = (int32_t)x.n_classes;
-    const char *src = (const char *)x.logits + row * x.ld * (BF ? 2 : 4);
+    const int tid = threadIdx.x % T;
+    const int64_t C = x.n_classes, begin = SPLIT ? (int64_t)strip * a.width : 0, end = SPLIT ? std::min(C, begin + a.width) : C;
+    const char *src = (const char *)x.logits + row * x.ld * ELT;
+    char *out = x.dlogits ? (char *)x.dlogits + row * x.ld_d * ELT : nullptr;
 
-    // what there is to do (the row before may still be looked up in ids and share)
-    __syncthreads();
-    if (tid < 4) flags[tid] = 0;
-    __syncthreads();
+    // the row, and what there is to do
+    u32x4x keep[VEC ? NV : 1];
+    float one[VEC ? 1 : NV];
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+        const int64_t c = begin + (int64_t)(v * T + tid) * PER;
+        if constexpr (VEC) keep[v] = live ? load<BF>(src, c, end) : u32x4x{0, 0, 0, 0};
+        else one[v] = live && c < C ? logit<BF>(src, c) : -INFINITY;
+    }
     int32_t id = -1;
     float t = -INFINITY;
-    if (x.alpha > 0.f && tid < x.k) {
+    if (live && x.alpha > 0.f && tid < x.k) {
         id = x.ids[row * x.k + tid];
         t = x.teacher[row * x.k + tid];
         if (!entry_there(id, t)) id = -1;
-        ids[tid] = id;
-        if (id >= 0) flags[0] = 1;
-        if (id >= C) flags[1] = 1;
     }
-    if (tid < kWave) {
-        int32_t n = 0, l = 0;
-        for (int i = tid; i < a.parts; i += kWave) {
-            n += a.counts[i].x;
-            l += a.counts[i].y;
-        }
-#pragma unroll
-        for (int o = 1; o < kWave; o <<= 1) {
-            n += __shfl_xor(n, o, kWave);
-            l += __shfl_xor(l, o, kWave);
-        }
-        if (tid == 0) {
-            flags[2] = n;
-            flags[3] = l;
-        }
-    }
-    __syncthreads();
-    const bool has = flags[0], wrong = flags[1];
-    const int32_t y = x.labels ? x.labels[row] : x.ignore;
-    const bool counted = x.labels && y != x.ignore, off = counted && (y < 0 || y >= C);
-    const bool do_kd = has && !wrong, do_ce = counted && !off;
-    const float wk = do_kd ? (float)((double)x.alpha * x.temperature / flags[2]) : 0.f;
-    const float wc = do_ce ? (float)((1.0 - (double)x.alpha) / flags[3]) : 0.f;
-    const bool both = do_ce && !(do_kd && x.temperature == 1.f);
-    const float inv_t = 1.f / x.temperature;
+    if (tid < (x.k + 3) / 4 * 4) ids[tid] = id;
+    const int32_t y = live && x.labels ? x.labels[row] : x.ignore;
+    const bool counts = live && x.labels && y != x.ignore, off = counts && (y < 0 || y >= C);
 
-    u32x4x keep[NV];
-    float top = 0.f, rt = 0.f, r1 = 0.f, kd = 0.f, ce = 0.f, zj = 0.f, zy = 0.f, q = 0.f;
-    if (do_kd || do_ce) {
-        Sums s;
+    // largest logit, largest of the teacher's, whether there are entries and wrong ones
+    Sums s;
+    float kept = 0.f;   // what the kept exponentials are less
+    if constexpr (SPLIT) {
+        for (int i = tid; i < a.strips; i += T) s.top = fmaxf(s.top, a.sums[row * a.strips + i].x);
+    } else {
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
-            const int32_t c = (v * NT + tid) * PER;
-            keep[v] = u32x4x{0, 0, 0, 0};
-            if (c < C) keep[v] = *(const u32x4x *)(src + (int64_t)c * (BF ? 2 : 4));
-        }
+            if ((int64_t)v * T * PER >= C) break;
 #pragma unroll
-        for (int v = 0; v < NV; ++v) {
-            const int32_t c = (v * NT + tid) * PER;
-#pragma unroll
-            for (int e = 0; e < PER; ++e)
-                if (c + e < C) s.top = fmaxf(s.top, element<BF>(keep[v], e));
+            for (int e = 0; e < PER; ++e) {
+                if constexpr (VEC) s.top = fmaxf(s.top, element<BF>(keep[v], e));
+                else s.top = fmaxf(s.top, one[v]);
+            }
         }
         const float ref = s.top == -INFINITY ? 0.f : s.top;
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
-            const int32_t c = (v * NT + tid) * PER;
+            if ((int64_t)v * T * PER >= C) break;
 #pragma unroll
-            for (int e = 0; e < PER; ++e)
-                if (c + e < C) {
-                    s.st += exp_of<BF>(element<BF>(keep[v], e) - ref, inv_t);
-                    if (both) s.s1 += exp_of<BF>(element<BF>(keep[v], e) - ref, 1.f);
-                }
-        }
-        for (int64_t c = (int64_t)(NV * NT + tid) * PER; c < C; c += NT * PER) {
-            const u32x4x v = *(const u32x4x *)(src + c * (BF ? 2 : 4));
-            float z[PER];
-#pragma unroll
-            for (int e = 0; e < PER; ++e) z[e] = c + e < C ? element<BF>(v, e) : -INFINITY;
-            add<BF>(s, z, PER, inv_t, both);
-        }
-        top = reduce<NT, true>(s.top, scratch);
-        // (a thread without logits has no part; a row of -inf alone has no distribution)
-        const float st = reduce<NT, false>(s.top == -INFINITY ? s.st : s.st * exp_of<BF>(s.top - top, inv_t), scratch);
-        float s1 = st;
-        if (both) s1 = reduce<NT, false>(s.top == -INFINITY ? s.s1 : s.s1 * exp_of<BF>(s.top - top, 1.f), scratch);
-        const float nan = __builtin_nanf("");
-        rt = top == -INFINITY ? nan : 1.f / st;
-        r1 = top == -INFINITY ? nan : 1.f / s1;
-        if (do_kd) {
-            const float most = reduce<NT, true>(t, scratch);
-            const float u = id >= 0 ? (t - most) * inv_t : 0.f, w = id >= 0 ? expf(u) : 0.f;
-            const float sum = reduce<NT, false>(w, scratch);
-            q = w / sum;
-            if (id >= 0) {
-                if constexpr (BF) zj = bf16_to_f32(((const uint16_t *)src)[id]);
-                else zj = ((const float *)src)[id];
+            for (int e = 0; e < PER; ++e) {
+                float z;
+                if constexpr (VEC) z = element<BF>(keep[v], e);
+                else z = one[v];
+                const float p = exp_of(z - ref, a.scale);
+                s.st += p;
+                if constexpr (BOTH) s.s1 += exp_of(z - ref, (float)kLog2e);
+                if constexpr (EXPS) keep[v][e] = __float_as_uint(p);
             }
-            // an entry whose q is zero has no part, whatever the student's logit
-            const float term = q == 0.f ? 0.f : q * ((u - logf(sum)) - ((zj - top) * inv_t - logf(st)));
-            kd = reduce<NT, false>(term, scratch) * (x.temperature * x.temperature);
-            if (top == -INFINITY) kd = nan;
-            if (tid < x.k) share[tid] = q;
         }
-        if (do_ce) {
-            if constexpr (BF) zy = bf16_to_f32(((const uint16_t *)src)[y]);
-            else zy = ((const float *)src)[y];
-            ce = top == -INFINITY ? nan : logf(s1) - (zy - top);
-        }
-        // every logit that is needed by itself has been read: the gradient may take the logits' place
-        __syncthreads();
+        kept = ref;
     }
-    if (tid == 0) {
-        const float nan = __builtin_nanf("");
-        if (has && wrong) kd = nan;
-        if (off) ce = nan;
-        a.kd[row] = kd;
-        a.ce[row] = ce;
+    float top = team.template within<true>(s.top, 0), most = team.template within<true>(id >= 0 ? t : -INFINITY, 1);
+    float has_f = team.template within<true>(id >= 0 ? 1.f : 0.f, 2), wrong_f = team.template within<true>(id >= C ? 1.f : 0.f, 3);
+    float listed_f = team.template within<true>(id >= 0 && id == y ? 1.f : 0.f, 8);
+    team.sync();
+    top = team.template across<true>(top, 0);
+    most = team.template across<true>(most, 1);
+    const bool has = team.template across<true>(has_f, 2) > 0.f, wrong = team.template across<true>(wrong_f, 3) > 0.f;
+    const bool listed = team.template across<true>(listed_f, 8) > 0.f;   // whether the label is an entry's class
+    const bool do_kd = has && !wrong, do_ce = counts && !off, some = do_kd || do_ce;
+
+    // sums of exponentials (a thread without logits has no part)
+    float st, s1;
+    if constexpr (SPLIT) {
+        st = s1 = 0.f;
+        for (int i = tid; i < a.strips; i += T) {
+            const float4 p = a.sums[row * a.strips + i];
+            st += p.x == -INFINITY ? p.y : p.y * exp_of(p.x - top, a.scale);
+            if constexpr (BOTH) s1 += p.x == -INFINITY ? p.z : p.z * exp_of(p.x - top, (float)kLog2e);
+        }
+    } else {
+        st = s.top == -INFINITY ? s.st : s.st * exp_of(s.top - top, a.scale);
+        s1 = 0.f;
+        if constexpr (BOTH) s1 = s.top == -INFINITY ? s.s1 : s.s1 * exp_of(s.top - top, (float)kLog2e);
+    }
+    const float u = id >= 0 ? (t - most) * a.inv_t : 0.f, w = id >= 0 ? expf(u) : 0.f;
+    st = team.template within<false>(st, 4);
+    if constexpr (BOTH) s1 = team.template within<false>(s1, 5);
+    float sum = team.template within<false>(w, 6);
+    float zj = 0.f, zy = 0.f;   // every logit that is needed by itself is read before the gradient may take its place
+    if (do_kd && id >= 0) zj = SPLIT ? a.own[row * (x.k + 1) + tid] : logit<BF>(src, id);
+    if (do_ce) zy = SPLIT ? a.own[row * (x.k + 1) + x.k] : logit<BF>(src, y);
+    team.sync();
+    st = team.template across<false>(st, 4);
+    s1 = BOTH ? team.template across<false>(s1, 5) : st;
+    sum = team.template across<false>(sum, 6);
+    const float nan = __builtin_nanf("");
+    const bool none = top == -INFINITY;   // a row of -inf alone has no distribution
+    const float q = do_kd ? w / sum : 0.f;
+    // an entry whose q is zero has no part, whatever the student's logit
+    const float term = q == 0.f ? 0.f : q * ((u - logf(sum)) - ((zj - top) * a.inv_t - logf(st)));
+    float kd = team.template within<false>(term, 7);
+    if (tid < x.k) share[tid] = q;
+    asm volatile("" ::"v"(zj), "v"(zy));   // (both have arrived when the row is written)
+    team.sync();
+    kd = team.template across<false>(kd, 7) * (x.temperature * x.temperature);
+    if (!live) return;
+    if (strip == 0 && tid == 0) {
+        kd = has && wrong ? nan : !do_kd ? 0.f : none ? nan : kd;
+        const float ce = off ? nan : !do_ce ? 0.f : none ? nan : logf(s1) - (zy - top);
+        loss.x += (double)kd;
+        loss.y += (double)ce;
         if (x.row_loss) x.row_loss[row] = (x.alpha > 0.f ? x.alpha * kd : 0.f) + (x.alpha < 1.f ? (1.f - x.alpha) * ce : 0.f);
     }
-    if (!x.dlogits) return;
+    if (!out) return;
 
-    char *out = (char *)x.dlogits + row * x.ld_d * (BF ? 2 : 4);
+    // the gradient: coefficients of the exponentials at T and at 1
+    const float wk = do_kd ? (float)((double)x.alpha * x.temperature / counted_rows.x) : 0.f;
+    const float wc = do_ce ? (float)((1.0 - (double)x.alpha) / counted_rows.y) : 0.f;
+    const float ct = do_kd ? (none ? nan : wk / st) : 0.f, c1 = do_ce ? (none ? nan : wc / s1) : 0.f;
+    const float ref = some ? top : 0.f;
     auto grad = [&](float z) {
-        float g = 0.f;
-        if (do_kd) g = wk * (exp_of<BF>(z - top, inv_t) * rt);
-        if (do_ce) g += wc * ((both ? exp_of<BF>(z - top, 1.f) : exp_of<BF>(z - top, inv_t)) * r1);
-        return g;
+        if constexpr (BOTH) return ct * exp_of(z - ref, a.scale) + c1 * exp_of(z - ref, (float)kLog2e);
+        else return (ct + c1) * exp_of(z - ref, a.scale);
     };
-    auto write = [&](const u32x4x &v, int64_t c) {
+    auto write = [&](const u32x4x &v, int64_t c, auto exps_, float factor) {   // of logits, or of their exponentials
         float g[PER];
 #pragma unroll
-        for (int e = 0; e < PER; ++e) g[e] = c + e < C ? grad(element<BF>(v, e)) : 0.f;
+        for (int e = 0; e < PER; ++e) {
+            if constexpr (decltype(exps_)::value) g[e] = factor * element<BF>(v, e);
+            else g[e] = grad(element<BF>(v, e));
+        }
+        if (c + PER > C)
+#pragma unroll
+            for (int e = 0; e < PER; ++e)
+                if (c + e >= C) g[e] = 0.f;
         u32x4x o;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            if constexpr (BF) o[e] = bf16_pair(g[2 * e], g[2 * e + 1]);
-            else o[e] = __float_as_uint(g[e]);
+            if constexpr (BF) o[e] = bf16_pair(g[2 * e % PER], g[(2 * e + 1) % PER]);
+            else o[e] = __float_as_uint(g[e % PER]);
         }
-        *(u32x4x *)(out + c * (BF ? 2 : 4)) = o;
+        *(u32x4x *)(out + c * ELT) = o;
     };
-#pragma unroll
-    for (int v = 0; v < NV; ++v) {
-        const int64_t c = (int64_t)(v * NT + tid) * PER;
-        if (c < C) write(keep[v], c);
-    }
-    for (int64_t c = (int64_t)(NV * NT + tid) * PER; c < C; c += NT * PER) {
-        u32x4x v = {0, 0, 0, 0};
-        if (do_kd || do_ce) v = *(const u32x4x *)(src + c * (BF ? 2 : 4));
-        write(v, c);
-    }
-    if (!do_kd && !do_ce) return;
-    // the classes that have a share of the target, once each, over what was written
-    __syncthreads();
-    auto put = [&](int32_t c, float g) {
+    auto put = [&](int64_t c, float g) {
         if constexpr (BF) ((uint16_t *)out)[c] = bf16_rne(g);
         else ((float *)out)[c] = g;
     };
-    if (do_kd && id >= 0) {
-        float sum = 0.f;
+    const u32x4x zeros = {0, 0, 0, 0};
+    const float factor = EXPS ? (ct + c1) * exp_of(kept - ref, a.scale) : 0.f;
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+        const int64_t c = begin + (int64_t)(v * T + tid) * PER;
+        if (begin + (int64_t)v * T * PER >= end) break;
+        if constexpr (VEC) {
+            if (c < end) write(some ? keep[v] : zeros, c, std::integral_constant<bool, EXPS>(), factor);
+        } else if (c < (C * ELT + 15) / 16 * 16 / ELT) {
+            put(c, c < C ? grad(some ? one[v] : 0.f) : 0.f);
+        }
+    }
+    // the classes that have a share of the target, once each, over what was written
+    team.sync();
+    if (do_kd && id >= begin && id < end) {
+        bool twice = false;
+        for (int32_t j = 0; j < x.k; j += 4) {
+            const int4 other = *(const int4 *)(ids + j);
+            twice = twice || (other.x == id && j != tid) || (other.y == id && j + 1 != tid) || (other.z == id && j + 2 != tid) ||
+                    (other.w == id && j + 3 != tid);
+        }
+        float all = q;
         bool first = true;
-        for (int32_t j = 0; j < x.k; ++j)
-            if (ids[j] == id) {
-                first = first && j >= tid;
-                sum += share[j];
-            }
-        if (first) {
-            float g = wk * (exp_of<BF>(zj - top, inv_t) * rt - sum);
-            if (do_ce) g += wc * ((both ? exp_of<BF>(zj - top, 1.f) : exp_of<BF>(zj - top, inv_t)) * r1 - (id == y ? 1.f : 0.f));
-            put(id, g);
+        if (twice) {
+            all = 0.f;
+            for (int32_t j = 0; j < x.k; ++j)
+                if (ids[j] == id) {
+                    first = first && j >= tid;
+                    all += share[j];
+                }
         }
+        if (first) put(id, grad(zj) - wk * all - (do_ce && id == y ? wc : 0.f));
     }
-    if (do_ce && tid == 0) {
-        bool listed = false;
-        if (do_kd)
-            for (int32_t j = 0; j < x.k; ++j) listed = listed || ids[j] == y;
-        if (!listed) {
-            float g = wc * ((both ? exp_of<BF>(zy - top, 1.f) : exp_of<BF>(zy - top, inv_t)) * r1 - 1.f);
-            if (do_kd) g += wk * (exp_of<BF>(zy - top, inv_t) * rt);
-            put(y, g);
-        }
-    }
+    if (do_ce && tid == 0 && y >= begin && y < end && !(do_kd && listed)) put(y, grad(zy) - wc);
 }
 
-template <bool BF, int NT, int NV>
-__global__ void __launch_bounds__(NT) k_distill_row(const Args a) {
-    for (int64_t row = blockIdx.x; row < a.x.m; row += gridDim.x) distill_row<BF, NT, NV>(a, row);
+template <bool BF, int T, int NV, bool VEC, bool BOTH, bool SPLIT>
+__global__ void __launch_bounds__(256) k_distill_row(const Args a) {
+    constexpr int NT = 256, ROWS = NT / T, ENTRIES = T;
+    __shared__ float scratch[9][Team<T>::W];
+    __shared__ __align__(16) int32_t ids[ROWS][ENTRIES];
+    __shared__ float share[ROWS][ENTRIES];
+    __shared__ int2 counts[NT / 64];
+    int2 c = make_int2(0, 0);
+    if (a.parts == 0) c = count_rows(a.x, threadIdx.x, NT);
+    else
+        for (int32_t i = threadIdx.x; i < a.parts; i += NT) {
+            const int2 p = a.counts[i];
+            c.x += p.x;
+            c.y += p.y;
+        }
+    c = sum_counts<NT>(c, counts);
+    if (a.parts == 0 && threadIdx.x == 0 && blockIdx.x == 0 && blockIdx.y == 0) a.counts[0] = c;   // for the means
+    const Team<T> team = {scratch};
+    const int at = threadIdx.x / T;
+    double2 loss = make_double2(0.0, 0.0);
+    if constexpr (SPLIT) {
+        // (the last rows first: the memory-side cache still holds them from the sums' launch)
+        const int64_t row = a.first + (gridDim.y - 1 - blockIdx.y);
+        distill_row<BF, T, NV, VEC, BOTH, SPLIT>(a, row, blockIdx.x, true, c, team, ids[0], share[0], loss);
+        if (threadIdx.x == 0 && blockIdx.x == 0) a.losses[row] = loss;
+    } else {
+        // (whole teams of a wavefront past the last row go along with the others)
+        for (int64_t row = (int64_t)blockIdx.x * ROWS; row < a.x.m; row += (int64_t)gridDim.x * ROWS) {
+            distill_row<BF, T, NV, VEC, BOTH, SPLIT>(a, std::min(row + at, a.x.m - 1), 0, row + at < a.x.m, c, team, ids[at], share[at], loss);
+            team.sync();   // (the next row takes the same LDS)
+        }
+        __shared__ double2 losses[ROWS];
+        if (threadIdx.x % T == 0) losses[at] = loss;
+        __syncthreads();
+        if (threadIdx.x == 0) {
+#pragma unroll
+            for (int r = 1; r < ROWS; ++r) {
+                loss.x += losses[r].x;
+                loss.y += losses[r].y;
+            }
+            a.losses[blockIdx.x] = loss;
+        }
+    }
 }
 
 namespace {
 int64_t up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
+
+// Strips of a row: 0 where a row is taken whole.
+int32_t strips_for(int64_t m, int64_t n_classes, bool bf16) {
+    const int64_t per = bf16 ? 8 : 4, width = 256 * kSplitVectors * per;
+    return n_classes > 2048 * per || (m <= 128 && n_classes > 2 * width) ? (int32_t)((n_classes + width - 1) / width) : 0;
+}
+
+struct Plan {
+    int32_t strips, n_losses;
+    size_t losses, sums, own, total;
+    Plan(int64_t m, int64_t n_classes, int64_t k, bool bf16) {
+        strips = strips_for(m, n_classes, bf16);
+        n_losses = strips > 0 ? (int32_t)m : (int32_t)std::min<int64_t>(m, kBlocks);
+        size_t at = kParts * sizeof(int2);
+        auto take = [&](int64_t bytes) {
+            const size_t here = at;
+            at += (size_t)up(bytes, 256);
+            return here;
+        };
+        losses = take((int64_t)n_losses * 16);
+        sums = take(m * strips * 16);
+        own = take(strips > 0 ? m * (k + 1) * 4 : 0);
+        total = at;
+    }
+};
+
+template <bool BF, bool BOTH>
+void rows(Args &a, hipStream_t s) {
+    const int64_t m = a.x.m, C = a.x.n_classes, k = a.x.alpha > 0.f ? a.x.k : 0;
+    constexpr int PER = BF ? 8 : 4;
+    if (a.strips > 0) {
+        for (int64_t first = 0; first < m; first += 65535) {
+            Args g = a;
+            g.first = first;
+            const dim3 grid((unsigned)a.strips, (unsigned)std::min<int64_t>(65535, m - first));
+            {
+                KernelTimer t("distill_sums", s);
+                hipLaunchKernelGGL((k_distill_sums<BF, BOTH>), grid, dim3(256), 0, s, g);
+            }
+            KernelTimer t("distill_row", s);
+            hipLaunchKernelGGL((k_distill_row<BF, 256, kSplitVectors, true, BOTH, true>), grid, dim3(256), 0, s, g);
+        }
+        return;
+    }
+    KernelTimer t("distill_row", s);
+#define GNNAV_L(T, NV, VEC)                                                                                                \
+    do {                                                                                                                   \
+        a.n_losses = (int32_t)grid_for(m, 256 / T, kBlocks);                                                 \
+        hipLaunchKernelGGL((k_distill_row<BF, T, NV, VEC, BOTH, false>), dim3((unsigned)a.n_losses), dim3(256), 0, s, a);  \
+    } while (0)
+    const bool many = m >= 2048;   // enough rows for a wavefront each
+    if (C <= 64 && k <= 16) GNNAV_L(16, 4, false);
+    else if (C <= 128 && k <= 32) GNNAV_L(32, 4, false);
+    else if (C <= 64 * PER && k <= 64) GNNAV_L(64, 1, true);
+    else if (C <= 128 * PER && k <= 64) GNNAV_L(64, 2, true);
+    else if (C <= 256 * PER && k <= 64 && many) GNNAV_L(64, 4, true);
+    else if (C <= 512 * PER && k <= 64 && many) GNNAV_L(64, 8, true);
+    else if (C <= 512 * PER) GNNAV_L(256, 2, true);
+    else if (C <= 1024 * PER) GNNAV_L(256, 4, true);
+    else GNNAV_L(256, 8, true);
+#undef GNNAV_L
+}
 }  // namespace
 
-size_t distill_workspace(int64_t m) { return (size_t)(kParts * 8 + 2 * up(m * 4, 256)); }
+size_t distill_workspace(int64_t m, int64_t n_classes, int64_t k, bool bf16) { return Plan(m, n_classes, k, bf16).total; }
 
 void launch_distill(const DistillArgs &x, hipStream_t s) {
     Args a = {};
     a.x = x;
+    if (x.alpha == 0.f) a.x.k = 0;
+    const Plan p(x.m, x.n_classes, x.k, x.bf16);
     char *ws = (char *)x.workspace;
     a.counts = (int2 *)ws;
-    a.parts = (int32_t)grid_for(x.m, 256, kParts);
-    a.kd = (float *)(ws + kParts * 8);
-    a.ce = a.kd + up(x.m * 4, 256) / 4;
-    {
+    a.losses = (double2 *)(ws + p.losses);
+    a.n_losses = p.n_losses;
+    a.sums = (float4 *)(ws + p.sums);
+    a.own = (float *)(ws + p.own);
+    a.inv_t = 1.f / x.temperature;
+    a.scale = (float)(x.alpha > 0.f ? kLog2e / x.temperature : kLog2e);
+    a.strips = p.strips;
+    a.width = 256 * kSplitVectors * (x.bf16 ? 8 : 4);
+    a.parts = x.m <= 1024 && a.x.k <= 16 ? 0 : (int32_t)grid_for(x.m, 16, kParts);
+    if (a.parts > 0) {
         KernelTimer t("distill_count", s);
         hipLaunchKernelGGL(k_distill_count, dim3((unsigned)a.parts), dim3(256), 0, s, a);
     }
     if (x.m > 0) {
-        KernelTimer t("distill_row", s);
-        if (x.bf16) hipLaunchKernelGGL((k_distill_row<true, 256, 4>), dim3(grid_for(x.m, 1, 1 << 20)), dim3(256), 0, s, a);
-        else hipLaunchKernelGGL((k_distill_row<false, 256, 4>), dim3(grid_for(x.m, 1, 1 << 20)), dim3(256), 0, s, a);
+        const bool both = x.alpha > 0.f && x.labels && x.temperature != 1.f;
+        if (x.bf16) both ? rows<true, true>(a, s) : rows<true, false>(a, s);
+        else both ? rows<false, true>(a, s) : rows<false, false>(a, s);
     }
     {
         KernelTimer t("distill_mean", s);
-        hipLaunchKernelGGL(k_distill_mean, dim3(1), dim3(1024), 0, s, a);
+        hipLaunchKernelGGL(k_distill_mean, dim3(1), dim3(256), 0, s, a);
     }
     GNNAV_HIP(hipGetLastError());
 }
