@@ -560,7 +560,9 @@ gnnav_status gnnav_linear_xent(const void *h_dev, int64_t ld_h, int64_t m, const
  * inputs hold there is not used.  m = 0 is allowed.
  *
  * saved_dev: NULL, or device memory of at least gnnav_gated_ffn_saved bytes (16-byte aligned)
- * that receives a, b and h for the backward pass, in an order of the library's own.
+ * that receives what the backward pass takes from the forward one, in an order of the
+ * library's own: h (BF16: 2 bytes an entry; the backward pass forms a and b again), and a
+ * and b (F32: 14 bytes an entry in all).
  *
  * gnnav_gated_ffn_backward: from dy (m x d_out) and the saved_dev of the forward
  * pass with the same x, weights, sizes and act:

@@ -13,8 +13,10 @@
 //
 // fp32 operands are split into three bf16 planes and multiplied with the six part products of bf16split.hpp.
 //
-// Rounding: a and b stay in fp32, also where they are kept for the backward pass (bf16 ones would cost da and db a second
-// rounding of the results' own size); h, da and db are rounded once to the operands' type for the products that read them.
+// Rounding: a and b stay in fp32 (bf16 ones would cost da and db a second rounding of the results' own size): fp32 keeps them
+// for the backward pass, bf16 multiplies x with Wg and Wu again in the tiles of dh, which is less time than 16 bytes an entry
+// until d is some 900, and five times less memory at any d.  h, da and db are rounded once to the operands' type for the
+// products that read them; where a product's output has few entries, so that it costs nothing, to two bf16 parts.
 #include <algorithm>
 #include <cmath>
 
@@ -142,27 +144,32 @@ __global__ void __launch_bounds__(256) k_gated_pack(const PackJobs jobs) {
 // ------------------------------------------------------------------ products
 // out[n][m] = sum over k of A(m, k) B(n, k).  The tile's M index is the output's column, N its row: a lane then holds four
 // consecutive columns of a row.
+// (no arrays: what is indexed at run time would be copied to memory)
 struct Operand {
-    const char *p[2];            // two matrices: side by side along M (kGate), or one after the other along the sum
-    int64_t row[2];              // bytes from a row of each to the next
+    const char *p0, *p1, *p2, *p3;   // matrices side by side along M (both projections: two), or one after the other along the sum
+    int64_t row0, row1;          // bytes from a row to the next, of either side (one after the other along the sum: row0)
     int64_t chunk, plane;        // from a chunk, from a plane
     int32_t rows, chunks;        // what there is of each
 };
-
-enum { kGate, kDgate, kOut };
+// A sum: `segments` matrices one after the other, of `steps` steps each; the last step of each takes `tail` of its BK.
+struct Sum {
+    Operand A, B;
+    int32_t segments, steps, tail;
+};
 
 struct Product {
-    Operand A, B;
+    Sum s;
     int32_t m_tiles, n_tiles, splits, split_steps;
-    int32_t segments, steps;     // matrices one after the other; steps of each
-    int32_t tail;                // what the last step of a segment sums over (its BK where that is whole)
     int32_t n;                   // rows of the output
-    // kGate, kDgate: columns, 4-float groups [group][row] of a and b (kGate: nullable), chunks of h, or of da and db
+    // h, da and db: columns, 4-float groups [group][row] of a and b (nullable for h), chunks of h, or of da and db
     int32_t f;
     f32x4x *a, *b;
     u32x4x *h;
     int64_t h_plane, second;     // chunks of a plane; from da to db
-    // kOut: columns of one output, where the second one starts (INT_MAX: there is none)
+    int64_t low;                 // bf16: from the values to their second parts (0: none are kept)
+    u32x4x *h2;                  // da and db, bf16: h in two parts (nullable)
+    int64_t h2_low;
+    // y and the gradients: columns of one output, where the second one starts (INT_MAX: there is none)
     int32_t cols, half;
     void *out[2];
     int64_t ld[2];
@@ -213,7 +220,7 @@ __device__ __forceinline__ void store4(const Product &a, int64_t n, int32_t c, c
 
 // 16 values of a lane (four groups of 4 columns, c + 8 g + 4 h) of row n as chunks of the operands' type.
 template <int PL>
-__device__ __forceinline__ void store_chunks(u32x4x *to, int64_t plane, int64_t rows, int64_t chunk, int64_t chunks, int64_t n,
+__device__ __forceinline__ void store_chunks(u32x4x *to, int64_t plane, int64_t rows, int32_t chunk, int32_t chunks, int64_t n,
                                              int h, const float (&x)[16]) {
 #pragma unroll
     for (int pl = 0; pl < PL; ++pl)
@@ -235,89 +242,167 @@ __device__ __forceinline__ void store_chunks(u32x4x *to, int64_t plane, int64_t 
                     }
                 }
             const u32x4x v = join_chunk(w[0][0], w[0][1], w[1][0], w[1][1]);
-            if (n < rows && chunk + g + h < chunks) to[pl * plane + (chunk + g + h) * rows + n] = v;
+            if (n < rows && chunk + g + h < chunks) to[pl * plane + (int64_t)(chunk + g + h) * rows + n] = v;
         }
 }
 
-// One tile of a product, from operands in memory by way of LDS, and what becomes of it.
-// AT, BT: the operand's rows are summed over.  In LDS an operand whose columns are summed over lies row by row, its BK / 8
-// chunks exchanged by the row (16 rows read 256 bytes of distinct banks); one whose rows are lies in blocks of 8 of them,
-// chunk by chunk, the two halves of a block exchanged by the chunk (32 lanes of a transposing read take 256 bytes of distinct
-// banks).  Both copy whole runs from row-major and from chunk-major memory.
-template <int PL, int WMF, int WNF, int WGM, int WGN, bool AT, bool BT, int EPI, int ACT>
-__device__ __forceinline__ void gated_tile(const Product &a, int32_t id, u32x4x *S) {
-    using C = Tile<PL, WMF, WNF, WGM, WGN>;
-    constexpr int BK = C::BK, ST = C::ST, NW = C::NW, BM = C::BM, BN = C::BN, APC = C::APC, BPC = C::BPC;
-    constexpr int STAGE = C::STAGE, INSTR = STAGE / 64, IN = (INSTR + NW - 1) / NW, CK = BK / 8;
-    constexpr bool DUAL = EPI == kGate;
-    static_assert(!DUAL || (AT && WMF % 2 == 0), "both projections in one tile");
-    constexpr int AM = DUAL ? BM / 2 : BM, WA = DUAL ? WMF / 2 : WMF;   // columns of one matrix in the tile, blocks of a wavefront
-    const int tid = threadIdx.x, lane = tid & 63, wid = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int wm = wid / WGN, wn = wid % WGN, h = lane >> 5, lr = lane & 31;
-    int32_t split, mt, nt;
-    if (!tile_of(a, id, split, mt, nt)) return;
-    const int64_t m0 = (int64_t)mt * AM, n0 = (int64_t)nt * BN;
-    const int32_t all = a.segments * a.steps, s0 = EPI == kOut ? split * a.split_steps : 0;
-    const int32_t T = EPI == kOut ? std::max(0, std::min(a.split_steps, all - s0)) : all;
+// ... and what bf16 leaves of the values, in bf16.
+__device__ __forceinline__ void store_low(u32x4x *to, int64_t rows, int32_t chunk, int32_t chunks, int64_t n, int h, const float (&x)[16]) {
+    float low[16];
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+        // (an infinite value leaves nothing)
+        const float high = bf16_to_f32(bf16_rne(x[e]));
+        low[e] = fabsf(high) < INFINITY ? x[e] - high : 0.f;
+    }
+    store_chunks<1>(to, 0, rows, chunk, chunks, n, h, low);
+}
 
-    // This wavefront's copies of a stage: source of the next step, its advance, whether the lane's is part of a last step.
-    const char *src[IN];
-    int64_t inc[IN];
-    int dst[IN];
-    uint32_t in_tail = 0;
-    auto aim = [&](int32_t segment, int32_t step) {
+// A wavefront's copies of a sum's stages to LDS.  DUAL: A's two matrices side by side.  AT, BT: the operand's rows are summed
+// over.  In LDS an operand whose columns are summed over lies row by row, its BK / 8 chunks exchanged by the row (16 rows read
+// 256 bytes of distinct banks); one whose rows are lies in blocks of 8 of them, chunk by chunk, the two halves of a block
+// exchanged by the chunk (32 lanes of a transposing read take 256 bytes of distinct banks).  Both copy whole runs from
+// row-major and from chunk-major memory.  STRIDE: chunks from a stage to the next.
+template <int PL_, int WMF_, int WNF_, int WGM_, int WGN_, bool AT_, bool BT_, bool DUAL_, int STRIDE_ = Tile<PL_, WMF_, WNF_, WGM_, WGN_>::STAGE>
+struct Feed {
+    using C = Tile<PL_, WMF_, WNF_, WGM_, WGN_>;
+    static constexpr int PL = PL_, WMF = WMF_, WNF = WNF_, WGM = WGM_, WGN = WGN_, STRIDE = STRIDE_;
+    static constexpr bool AT = AT_, BT = BT_, DUAL = DUAL_;
+    static constexpr int BK = C::BK, CK = BK / 8, APC = C::APC, BPC = C::BPC, BN = C::BN, INSTR = C::STAGE / 64, IN = (INSTR + C::NW - 1) / C::NW;
+    static constexpr int AM = DUAL ? C::BM / 2 : C::BM, WA = DUAL ? WMF / 2 : WMF;   // columns of one matrix in the tile, blocks of a wavefront
+    static_assert(!DUAL || WMF % 2 == 0, "both projections in one tile");
+    int64_t m0, n0;
+    const char *src[IN];   // source of the next step
+    int64_t inc[IN];       // its advance
+    int dst[IN];           // place in the stage
+    uint32_t in_tail;      // whether the lane's is part of a last step
+    int32_t segment, local;
+    bool tail;             // of the step that is copied: it is such a one
+
+    __device__ __forceinline__ int slot(int u) const {   // (the last wavefront may repeat the last copy)
+        return std::min((int)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * IN + u, INSTR - 1) * 64;
+    }
+    __device__ __forceinline__ void aim(const Sum &a, int32_t step) {
+        // (every field is read, then chosen among: a choice of addresses would put the arguments into memory)
+        const char *const a0 = a.A.p0, *const a1 = a.A.p1, *const a2 = a.A.p2, *const a3 = a.A.p3;
+        const char *const b0 = a.B.p0, *const b1 = a.B.p1, *const b2 = a.B.p2, *const b3 = a.B.p3;
+        const int64_t a_row0 = a.A.row0, a_row1 = a.A.row1, b_row = a.B.row0, a_chunk = a.A.chunk, b_chunk = a.B.chunk, a_plane = a.A.plane, b_plane = a.B.plane;
+        const int32_t a_rows = a.A.rows, b_rows = a.B.rows, a_chunks = a.A.chunks, b_chunks = a.B.chunks;
+        const char *const a_at = segment < 2 ? (segment < 1 ? a0 : a1) : (segment < 3 ? a2 : a3), *const b_at = segment < 2 ? (segment < 1 ? b0 : b1) : (segment < 3 ? b2 : b3);
+        in_tail = 0;
 #pragma unroll
         for (int u = 0; u < IN; ++u) {
-            const int q = std::min(wid * IN + u, INSTR - 1);   // the last wavefront may repeat the last copy
-            const int slot = q * 64;
-            const bool isB = slot >= PL * APC;
-            const int rel = slot - (isB ? PL * APC : 0), pc = isB ? BPC : APC;
+            const int at = dst[u] = slot(u);
+            const bool isB = at >= PL * APC;
+            const int rel = at - (isB ? PL * APC : 0), pc = isB ? BPC : APC;
             const int plane = rel / pc;
-            int s = rel % pc + lane;
-            const Operand &o = isB ? a.B : a.A;
-            int32_t matrix = segment;
+            int s = rel % pc + (threadIdx.x & 63);
+            bool side = false;   // the second of two matrices side by side
             if (DUAL && !isB) {
-                matrix = s / (APC / 2);
-                s -= matrix * (APC / 2);
+                side = rel % pc >= APC / 2;
+                s -= side ? APC / 2 : 0;
             }
             const int64_t x0 = isB ? n0 : m0;
-            const char *base = o.p[matrix] + plane * o.plane;
-            const int64_t row = o.row[matrix];
+            const char *base = isB ? b_at + plane * b_plane : (DUAL ? (side ? a1 : a0) : a_at) + plane * a_plane;
+            const int64_t row = isB ? b_row : DUAL && side ? a_row1 : a_row0, chunk = isB ? b_chunk : a_chunk;
+            const int32_t rows = isB ? b_rows : a_rows, chunks = isB ? b_chunks : a_chunks;
             int k;
             if (isB ? BT : AT) {
                 const int mcs = (isB ? BN : AM) / 8, mc = (s / 8) % mcs;
                 k = s / (8 * mcs) * 8 + ((s % 8) ^ ((mc & 2) * 2));
-                src[u] = base + ((int64_t)step * BK + k) * row + std::min<int64_t>(x0 / 8 + mc, o.chunks - 1) * o.chunk;
+                src[u] = base + ((int64_t)step * BK + k) * row + std::min<int64_t>(x0 / 8 + mc, chunks - 1) * chunk;
                 inc[u] = BK * row;
             } else {
                 const int r = s / CK, c = (s % CK) ^ (CK == 4 ? (r >> 2) & 3 : (r >> 3) & 1);
                 k = c * 8;
-                src[u] = base + std::min<int64_t>(x0 + r, o.rows - 1) * row + ((int64_t)step * CK + c) * o.chunk;
-                inc[u] = CK * o.chunk;
+                src[u] = base + std::min<int64_t>(x0 + r, rows - 1) * row + ((int64_t)step * CK + c) * chunk;
+                inc[u] = CK * chunk;
             }
-            dst[u] = slot;
-            in_tail = (in_tail & ~(1u << u)) | (uint32_t)(k < a.tail) << u;
+            in_tail |= (uint32_t)(k < a.tail) << u;
         }
-    };
-    auto issue = [&](int stage, int u) {
-        dma16(src[u], &S[stage * STAGE + dst[u]]);
-        src[u] += inc[u];
-    };
-    int32_t segment = s0 / std::max(a.steps, 1), local = s0 - segment * a.steps;   // of the step that is copied next
-    // before the copies of the next step: the second matrices, or the end of a sum
-    auto prepare = [&]() {
+    }
+    // from step s0 on of the tile at m0, n0
+    __device__ __forceinline__ void start(const Sum &a, int64_t m, int64_t n, int32_t s0) {
+        m0 = m;
+        n0 = n;
+        segment = s0 / std::max(a.steps, 1);
+        local = s0 - segment * a.steps;
+        aim(a, local);
+    }
+    // before the copies of the next step: the next matrices, which lie as the ones before them, or the end of a sum
+    __device__ __forceinline__ void prepare(const Sum &a) {
         if (local == a.steps) {
             local = 0;
-            aim(++segment, 0);
-        }
-        if (++local == a.steps && a.tail < BK) {
+            const char *const a0 = a.A.p0, *const a1 = a.A.p1, *const a2 = a.A.p2, *const a3 = a.A.p3;
+            const char *const b0 = a.B.p0, *const b1 = a.B.p1, *const b2 = a.B.p2, *const b3 = a.B.p3;
+            const int64_t a_on = segment < 1 ? a1 - a0 : segment < 2 ? a2 - a1 : a3 - a2, b_on = segment < 1 ? b1 - b0 : segment < 2 ? b2 - b1 : b3 - b2;
 #pragma unroll
-            for (int u = 0; u < IN; ++u)
-                if (!(in_tail >> u & 1)) src[u] = (const char *)&kZeros;
+            for (int u = 0; u < IN; ++u) src[u] += (dst[u] >= PL * APC ? b_on : a_on) - a.steps * inc[u];
+            ++segment;
+        }
+        tail = ++local == a.steps && a.tail < BK;
+    }
+    __device__ __forceinline__ void issue(u32x4x *S, int stage, int u) {
+        const char *from = src[u];
+        if (tail) from = in_tail >> u & 1 ? from : (const char *)&kZeros;
+        dma16(from, &S[stage * STRIDE + dst[u]]);
+        src[u] += inc[u];
+    }
+};
+
+// The sum that follows one: its first two stages are copied over the end of the one before it.
+template <class F>
+struct Next {
+    static constexpr int IN = F::IN;
+    int64_t m0, n0;
+    int32_t stages;   // 2, 1 where it has no more, 0 where nothing follows
+};
+struct Nothing {
+    static constexpr int IN = 0;
+    static constexpr int32_t stages = 0;
+};
+
+// The sum of one tile, T steps of `feed`, from operands in memory by way of LDS.  `ready`: the stage that holds its first step, and
+// after it the next sum's; `primed`: stages that are on their way; stored: stores may have been issued behind their copies.
+template <class F, class N, class G>
+__device__ __forceinline__ void tile_sum(F &feed, const Sum &sum, int32_t T, u32x4x *S, f32x16x (&acc)[F::WMF][F::WNF], int &ready, int primed, bool stored, const N &follow,
+                                         G &after, const Sum &after_sum) {
+    constexpr int PL = F::PL, WMF = F::WMF, WNF = F::WNF, WGN = F::WGN, BK = F::BK, CK = F::CK, APC = F::APC, BPC = F::BPC, BN = F::BN;
+    constexpr int AM = F::AM, WA = F::WA, IN = F::IN, NIN = N::IN, ST = F::C::ST;
+    const int lane = threadIdx.x & 63, wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wm = wid / WGN, wn = wid % WGN, h = lane >> 5, lr = lane & 31;
+    // stage i of this sum, or i - T of the next one
+    enum { kIdle, kOwn, kNext };
+    auto whose = [&](int32_t i) __attribute__((always_inline)) { return i < T ? kOwn : i - T < follow.stages ? kNext : kIdle; };
+    auto prepare = [&](int32_t i) __attribute__((always_inline)) {
+        if (i < T) {
+            feed.prepare(sum);
+        } else if constexpr (NIN > 0) {
+            if (i - T < follow.stages) {
+                if (i == T) after.start(after_sum, follow.m0, follow.n0, 0);
+                after.prepare(after_sum);
+            }
         }
     };
+    auto issue = [&](int mode, int stage, int u, bool last) __attribute__((always_inline)) {
+        if (NIN == 0 || mode == kOwn) feed.issue(S, stage, u);
+        if constexpr (NIN > 0) {
+            if (mode == kNext) {
+                if (u < NIN) after.issue(S, stage, u);
+                if (last)
+#pragma unroll
+                    for (int more = IN; more < NIN; ++more) after.issue(S, stage, more);
+            }
+        }
+        (void)last;
+    };
+    auto issue_all = [&](int32_t i, int stage, int from, int to) __attribute__((always_inline)) {
+        const int mode = whose(i);
+        if (mode != kIdle)
+#pragma unroll
+            for (int u = from; u < to; ++u) issue(mode, stage, u, u == IN - 1);
+    };
 
-    f32x16x acc[WMF][WNF];
 #pragma unroll
     for (int i = 0; i < WMF; ++i)
 #pragma unroll
@@ -329,7 +414,7 @@ __device__ __forceinline__ void gated_tile(const Product &a, int32_t id, u32x4x 
     const int tr_mc = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
     const int tr_at = tr_mc * 8 + (((lane & 15) >> 2) ^ ((tr_mc & 2) * 2));
     const int n_swz = CK == 4 ? (lr >> 2) & 3 : (lr >> 3) & 1;
-    auto frag = [&](const u32x4x *plane, auto tr_, int tile, int x, int kk) -> bf16x8 {
+    auto frag = [&](const u32x4x *plane, auto tr_, int tile, int x, int kk) __attribute__((always_inline)) -> bf16x8 {
         if constexpr (decltype(tr_)::value) {
             typedef __attribute__((address_space(3))) s16x4 lds4;
             const u32x4x *p = plane + ((2 * kk + h) * (tile / 8) + x / 8) * 8;
@@ -346,20 +431,20 @@ __device__ __forceinline__ void gated_tile(const Product &a, int32_t id, u32x4x 
     };
     // fragment k of a step: B's, then A's, as the products need them
     constexpr int NF = (WMF + WNF) * PL;
-    auto read = [&](Frags &f, int stage, int kk, int k) {
-        const u32x4x *sa = &S[stage * STAGE], *sb = sa + PL * APC;
+    auto read = [&](Frags &f, int stage, int kk, int k) __attribute__((always_inline)) {
+        const u32x4x *sa = &S[stage * F::STRIDE], *sb = sa + PL * APC;
         const int x = k / PL, p = k % PL;
         if (x < WNF) {
-            f.b[x][p] = frag(sb + p * BPC, std::integral_constant<bool, BT>(), BN, wn * (32 * WNF) + 32 * x, kk);
+            f.b[x][p] = frag(sb + p * BPC, std::integral_constant<bool, F::BT>(), BN, wn * (32 * WNF) + 32 * x, kk);
         } else {
             const int i = x - WNF, matrix = i / WA;
-            f.a[i][p] = frag(sa + p * APC + matrix * (APC / 2), std::integral_constant<bool, AT>(), AM, wm * (32 * WA) + 32 * (i % WA), kk);
+            f.a[i][p] = frag(sa + p * APC + matrix * (APC / 2), std::integral_constant<bool, F::AT>(), AM, wm * (32 * WA) + 32 * (i % WA), kk);
         }
     };
     // The products of one fragment set.  Between them go, one at a time, the reads of the next set (first half) and
     // copies [c0, c1) of a stage to come (second half): in one burst behind the barrier they queue
     // up, and the wavefront's products wait with them.  Past the last stage the reads are idle ones.
-    auto multiply = [&](const Frags &f, Frags &nxt, int from, int kk, bool more, int into, auto c0_, auto c1_) {
+    auto multiply = [&](const Frags &f, Frags &nxt, int from, int kk, int mode, int into, auto c0_, auto c1_) __attribute__((always_inline)) {
         constexpr int SLOTS = WMF * WNF, HALF = (SLOTS + 1) / 2, C0 = decltype(c0_)::value, C1 = decltype(c1_)::value;
         constexpr int REST = SLOTS > HALF ? SLOTS - HALF : 1, CUT = SLOTS > HALF ? HALF : 0;
 #pragma unroll
@@ -374,15 +459,17 @@ __device__ __forceinline__ void gated_tile(const Product &a, int32_t id, u32x4x 
             if (k < HALF)
 #pragma unroll
                 for (int q = NF * k / HALF; q < NF * (k + 1) / HALF; ++q) read(nxt, from, kk, q);
-            if (k >= CUT && more)
+            if (k >= CUT && mode != kIdle)
 #pragma unroll
-                for (int q = C0 + (C1 - C0) * (k - CUT) / REST; q < C0 + (C1 - C0) * (k - CUT + 1) / REST; ++q) issue(into, q);
+                for (int q = C0 + (C1 - C0) * (k - CUT) / REST; q < C0 + (C1 - C0) * (k - CUT + 1) / REST; ++q) issue(mode, into, q, q == IN - 1);
             __builtin_amdgcn_sched_barrier(0);
         }
     };
     // Makes stage t readable: its copies are done, everywhere; those of the stage after it may not be.
-    auto advance = [&](int32_t t) {
-        if (t + 1 < T) wait_vm<IN *(ST - 2)>();
+    auto advance = [&](int32_t t) __attribute__((always_inline)) {
+        const int then = whose(t + 1);
+        if (then == kOwn) wait_vm<IN *(ST - 2)>();
+        else if (NIN > 0 && then == kNext) wait_vm<NIN *(ST - 2)>();
         else wait_vm<0>();
         lds_barrier();
     };
@@ -395,123 +482,263 @@ __device__ __forceinline__ void gated_tile(const Product &a, int32_t id, u32x4x 
     constexpr std::integral_constant<int, FIRST> kMiddle{};
     constexpr std::integral_constant<int, IN> kEnd{};
     Frags f0, f1;
-    int ready = 0, fill = BK == 32 ? ST - 1 : 0;
+    int fill = ready;
     if (T > 0) {
-        aim(segment, local);
 #pragma unroll
-        for (int k = 0; k < ST - 1; ++k)
-            if (k < T) {
-                prepare();
-#pragma unroll
-                for (int u = 0; u < IN; ++u) issue(k, u);
+        for (int k = 0; k < ST - 1; ++k) {
+            if (k >= primed) {
+                prepare(k);
+                issue_all(k, fill, 0, IN);
             }
-        advance(0);
-        if (ST - 1 < T) {
-            prepare();
-#pragma unroll
-            for (int u = 0; u < FIRST; ++u) issue(ST - 1, u);
+            fill = next(fill);
         }
+        if (primed > 0 && stored) {
+            wait_vm<0>();
+            lds_barrier();
+        } else {
+            advance(0);
+        }
+        prepare(ST - 1);
+        issue_all(ST - 1, fill, 0, FIRST);
+        if constexpr (BK == 16) fill = next(fill);
 #pragma unroll
-        for (int q = 0; q < NF; ++q) read(f0, 0, 0, q);
+        for (int q = 0; q < NF; ++q) read(f0, ready, 0, q);
     }
-    for (int32_t t = 0; t < T;) {
+    // (while every copy is this sum's own, without asking)
+    auto round = [&](int32_t &t, auto own_) __attribute__((always_inline)) {
+        constexpr bool OWN = decltype(own_)::value;
+        auto mode = [&](int32_t i) __attribute__((always_inline)) -> int { return OWN ? (int)kOwn : (int)whose(i); };
+        auto go_on = [&](int32_t to) __attribute__((always_inline)) {
+            if constexpr (OWN) {
+                wait_vm<IN *(ST - 2)>();
+                lds_barrier();
+                feed.prepare(sum);
+            } else if (to < T) {
+                advance(to);
+                prepare(to + ST - 1);
+            }
+        };
         if constexpr (BK == 32) {
-            multiply(f0, f1, ready, 1, t + ST - 1 < T, fill, kMiddle, kEnd);
+            multiply(f0, f1, ready, 1, mode(t + ST - 1), fill, kMiddle, kEnd);
             fill = next(fill);
             ready = next(ready);
-            if (++t < T) advance(t);
-            if (t + ST - 1 < T) prepare();
-            multiply(f1, f0, ready, 0, t + ST - 1 < T, fill, kBegin, kMiddle);
+            go_on(++t);
+            multiply(f1, f0, ready, 0, OWN || t < T ? mode(t + ST - 1) : kIdle, fill, kBegin, kMiddle);
         } else {
-#pragma unroll
-            for (int half = 0; half < 2; ++half) {
-                // (its copies of the first stages were issued above: ST - 1 whole ones and this one)
-                ready = next(ready);
-                if (++t < T) advance(t);
-                if (t + ST - 1 < T) prepare();
-                if (half == 0) multiply(f0, f1, ready, 0, t + ST - 1 < T, fill, kBegin, kEnd);
-                else multiply(f1, f0, ready, 0, t + ST - 1 < T, fill, kBegin, kEnd);
-                fill = next(fill);
-                if (t >= T) break;
-            }
+            ready = next(ready);
+            go_on(++t);
+            multiply(f0, f1, ready, 0, OWN || t < T ? mode(t + ST - 1) : kIdle, fill, kBegin, kEnd);
+            fill = next(fill);
+            if (!OWN && t >= T) return;
+            ready = next(ready);
+            go_on(++t);
+            multiply(f1, f0, ready, 0, OWN || t < T ? mode(t + ST - 1) : kIdle, fill, kBegin, kEnd);
+            fill = next(fill);
         }
-    }
+    };
+    int32_t t = 0;
+    while (t + (BK == 32 ? ST : ST + 1) < T) round(t, std::true_type());
+    while (t < T) round(t, std::false_type());
+}
 
-    const int64_t mw = m0 + wm * (32 * WA), nw = n0 + wn * (32 * WNF);
-    if constexpr (EPI == kGate || EPI == kDgate) {
-        const int32_t chunks = (a.f + 7) / 8;
+// h = act(x Wg) * (x Wu) for one tile from both sums, kept for the product with Wd, and a and b where they are kept.  WA: blocks
+// of a wavefront along f.
+template <int PL, int WA, int WNF, int WGM, int WGN, int ACT>
+__device__ __forceinline__ void gate_store(const Product &a, int64_t m0, int64_t n0, const f32x16x (&acc)[2 * WA][WNF]) {
+    const int lane = threadIdx.x & 63, wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5, lr = lane & 31;
+    const int32_t mw = (int32_t)m0 + wid / WGN * (32 * WA);
+    const int64_t nw = n0 + wid % WGN * (32 * WNF);
+    const int32_t chunks = (a.f + 7) / 8;
+    const bool whole = m0 + 32 * WA * WGM <= a.f;   // no column past the last
 #pragma unroll
-        for (int j = 0; j < WNF; ++j) {
-            const int64_t n = nw + 32 * j + lr;
+    for (int j = 0; j < WNF; ++j) {
+        const int64_t n = nw + 32 * j + lr;
 #pragma unroll
-            for (int i = 0; i < WA; ++i) {
-                float x[16], z[16];
+        for (int i = 0; i < WA; ++i) {
+            float x[16];
 #pragma unroll
-                for (int g = 0; g < 4; ++g) {
-                    const int64_t c = mw + 32 * i + 8 * g + 4 * h;
-                    const bool here = n < a.n && c < chunks * 8;
-                    f32x4x va = {0.f, 0.f, 0.f, 0.f}, vb = va;
-                    if constexpr (EPI == kGate) {
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            va[e] = acc[i][j][4 * g + e];
-                            vb[e] = acc[i + WA][j][4 * g + e];
-                        }
-                        if (here && a.a) {
-                            a.a[c / 4 * a.n + n] = va;
-                            a.b[c / 4 * a.n + n] = vb;
-                        }
-                    } else if (here) {
-                        va = a.a[c / 4 * a.n + n];
-                        vb = a.b[c / 4 * a.n + n];
-                    }
+            for (int g = 0; g < 4; ++g) {
+                const int32_t c = mw + 32 * i + 8 * g + 4 * h;
+                if (PL == 3 && a.a && n < a.n && c < chunks * 8) {
+                    f32x4x va, vb;
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        float value, slope;
-                        activate<ACT, PL == 3>(va[e], value, slope);
-                        const bool live = c + e < a.f;
-                        if constexpr (EPI == kGate) {
-                            x[4 * g + e] = live ? value * vb[e] : 0.f;
-                        } else {
-                            x[4 * g + e] = live ? acc[i][j][4 * g + e] * vb[e] * slope : 0.f;
-                            z[4 * g + e] = live ? acc[i][j][4 * g + e] * value : 0.f;
-                        }
+                        va[e] = acc[i][j][4 * g + e];
+                        vb[e] = acc[i + WA][j][4 * g + e];
                     }
+                    a.a[(int64_t)(c / 4) * a.n + n] = va;
+                    a.b[(int64_t)(c / 4) * a.n + n] = vb;
                 }
-                store_chunks<PL>(a.h, a.h_plane, a.n, (mw + 32 * i) / 8, chunks, n, h, x);
-                if constexpr (EPI == kDgate) store_chunks<PL>(a.h + a.second, a.h_plane, a.n, (mw + 32 * i) / 8, chunks, n, h, z);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    float value, slope;
+                    activate<ACT, PL == 3>(acc[i][j][4 * g + e], value, slope);
+                    x[4 * g + e] = value * acc[i + WA][j][4 * g + e];
+                }
             }
+            if (!whole)
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    if (mw + 32 * i + 8 * (r / 4) + 4 * h + r % 4 >= a.f) x[r] = 0.f;
+            store_chunks<PL>(a.h, a.h_plane, a.n, (mw + 32 * i) / 8, chunks, n, h, x);
+            if (PL == 1 && a.low) store_low(a.h + a.low, a.n, (mw + 32 * i) / 8, chunks, n, h, x);
         }
-    } else {
-        f32x4x *part = a.part;
-        if (part) part += split * a.split_stride + ((int64_t)(nt * a.m_tiles + mt) * NW + wid) * (WMF * WNF * 4 * 64) + lane;
-#pragma unroll
-        for (int j = 0; j < WNF; ++j)
-#pragma unroll
-            for (int i = 0; i < WMF; ++i)
-#pragma unroll
-                for (int g = 0; g < 4; ++g) {
-                    const f32x4x v = {acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]};
-                    if (part) part[((i * WNF + j) * 4 + g) * 64] = v;
-                    else store4(a, nw + 32 * j + lr, (int32_t)(mw + 32 * i + 8 * g + 4 * h), v);
-                }
     }
 }
 
+// da and db of one tile from dh = dy Wd^T; a and b are read (fp32) or were multiplied again (bf16).
+template <int PL, int WA, int WNF, int WGM, int WGN, int ACT>
+__device__ __forceinline__ void dgate_store(const Product &a, int64_t m0, int64_t n0, const f32x16x (&ab)[PL == 1 ? 2 * WA : 1][PL == 1 ? WNF : 1],
+                                            const f32x16x (&acc)[WA][WNF]) {
+    const int lane = threadIdx.x & 63, wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5, lr = lane & 31;
+    const int32_t mw = (int32_t)m0 + wid / WGN * (32 * WA);
+    const int64_t nw = n0 + wid % WGN * (32 * WNF);
+    const int32_t chunks = (a.f + 7) / 8;
+    const bool whole = m0 + 32 * WA * WGM <= a.f;
+#pragma unroll
+    for (int j = 0; j < WNF; ++j) {
+        const int64_t n = nw + 32 * j + lr;
+#pragma unroll
+        for (int i = 0; i < WA; ++i) {
+            float x[16], z[16], v[16];
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const int32_t c = mw + 32 * i + 8 * g + 4 * h;
+                f32x4x va = {0.f, 0.f, 0.f, 0.f}, vb = va;
+                if constexpr (PL == 1) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        va[e] = ab[i][j][4 * g + e];
+                        vb[e] = ab[i + WA][j][4 * g + e];
+                    }
+                } else if (n < a.n && c < chunks * 8) {
+                    va = a.a[(int64_t)(c / 4) * a.n + n];
+                    vb = a.b[(int64_t)(c / 4) * a.n + n];
+                }
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    float value, slope;
+                    activate<ACT, PL == 3>(va[e], value, slope);
+                    const float dh = acc[i][j][4 * g + e];
+                    x[4 * g + e] = dh * vb[e] * slope;
+                    z[4 * g + e] = dh * value;
+                    v[4 * g + e] = value * vb[e];
+                }
+            }
+            if (!whole)
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    if (mw + 32 * i + 8 * (r / 4) + 4 * h + r % 4 >= a.f) x[r] = z[r] = v[r] = 0.f;
+            const int32_t chunk = (mw + 32 * i) / 8;
+            store_chunks<PL>(a.h, a.h_plane, a.n, chunk, chunks, n, h, x);
+            store_chunks<PL>(a.h + a.second, a.h_plane, a.n, chunk, chunks, n, h, z);
+            if (PL == 1 && a.low) {
+                store_low(a.h + a.low, a.n, chunk, chunks, n, h, x);
+                store_low(a.h + a.second + a.low, a.n, chunk, chunks, n, h, z);
+            }
+            if (PL == 1 && a.h2) {
+                store_chunks<1>(a.h2, 0, a.n, chunk, chunks, n, h, v);
+                store_low(a.h2 + a.h2_low, a.n, chunk, chunks, n, h, v);
+            }
+        }
+    }
+}
+
+// Tile `id` of a product that goes to the caller, or to parts.
+template <int PL, int WMF, int WNF, int WGM, int WGN, bool AT, bool BT>
+__device__ __forceinline__ void out_tile(const Product &a, int32_t id, u32x4x *S) {
+    const int lane = threadIdx.x & 63, wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5, lr = lane & 31;
+    int32_t split, mt, nt;
+    if (!tile_of(a, id, split, mt, nt)) return;
+    const int64_t m0 = (int64_t)mt * (32 * WMF * WGM), n0 = (int64_t)nt * (32 * WNF * WGN);
+    const int32_t s0 = split * a.split_steps, T = std::max(0, std::min(a.split_steps, a.s.segments * a.s.steps - s0));
+    f32x16x acc[WMF][WNF];
+    Feed<PL, WMF, WNF, WGM, WGN, AT, BT, false> feed;
+    int ready = 0;
+    Nothing nothing;
+    if (T > 0) feed.start(a.s, m0, n0, s0);
+    tile_sum(feed, a.s, T, S, acc, ready, 0, false, nothing, feed, a.s);
+    const int64_t mw = m0 + wid / WGN * (32 * WMF), nw = n0 + wid % WGN * (32 * WNF);
+    f32x4x *part = a.part;
+    if (part) part += split * a.split_stride + ((int64_t)(nt * a.m_tiles + mt) * (WGM * WGN) + wid) * (WMF * WNF * 4 * 64) + lane;
+#pragma unroll
+    for (int j = 0; j < WNF; ++j)
+#pragma unroll
+        for (int i = 0; i < WMF; ++i)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const f32x4x v = {acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]};
+                if (part) part[((i * WNF + j) * 4 + g) * 64] = v;
+                else store4(a, nw + 32 * j + lr, (int32_t)(mw + 32 * i + 8 * g + 4 * h), v);
+            }
+}
+
+// A workgroup takes tile after tile, the next one's first copies under way while one's results are formed and stored.
 template <int PL, int WMF, int WNF, int WGM, int WGN, int ACT>
-__global__ void __launch_bounds__(64 * WGM * WGN, 2) k_gated_gate(const Product a) {
+__global__ void __launch_bounds__(64 * WGM * WGN, 2) k_gated_gate(const Product a, int32_t ids) {
+    constexpr int WA = WMF / 2;
+    constexpr int64_t AM = 32 * WA * WGM, BN = 32 * WNF * WGN;
     __shared__ u32x4x S[Tile<PL, WMF, WNF, WGM, WGN>::LDS];
-    gated_tile<PL, WMF, WNF, WGM, WGN, true, false, kGate, ACT>(a, blockIdx.x, S);
+    int32_t split, mt, nt, id = blockIdx.x;
+    if (!tile_of(a, id, split, mt, nt)) return;
+    using F = Feed<PL, WMF, WNF, WGM, WGN, true, false, true>;
+    F feed;
+    feed.start(a.s, mt * AM, nt * BN, 0);
+    f32x16x acc[WMF][WNF];
+    int ready = 0, primed = 0;
+    while (true) {
+        int32_t m2 = 0, n2 = 0;
+        id += gridDim.x;
+        const bool more = id < ids && tile_of(a, id, split, m2, n2);
+        const Next<F> next = {m2 * AM, n2 * BN, more ? std::min(a.s.steps, 2) : 0};
+        tile_sum(feed, a.s, a.s.steps, S, acc, ready, primed, true, next, feed, a.s);
+        gate_store<PL, WA, WNF, WGM, WGN, ACT>(a, mt * AM, nt * BN, acc);
+        if (!more) break;
+        primed = next.stages;
+        mt = m2;
+        nt = n2;
+    }
 }
 template <int PL, int WMF, int WNF, int WGM, int WGN>
 __global__ void __launch_bounds__(64 * WGM * WGN, 2) k_gated_down(const Product a) {
     __shared__ u32x4x S[Tile<PL, WMF, WNF, WGM, WGN>::LDS];
-    gated_tile<PL, WMF, WNF, WGM, WGN, true, false, kOut, 0>(a, blockIdx.x, S);
+    out_tile<PL, WMF, WNF, WGM, WGN, true, false>(a, blockIdx.x, S);
 }
-template <int PL, int WMF, int WNF, int WGM, int WGN, int ACT>
-__global__ void __launch_bounds__(64 * WGM * WGN, 2) k_gated_dgate(const Product a) {
-    __shared__ u32x4x S[Tile<PL, WMF, WNF, WGM, WGN>::LDS];
-    gated_tile<PL, WMF, WNF, WGM, WGN, false, false, kDgate, ACT>(a, blockIdx.x, S);
+template <int PL, int WA, int WNF, int WGM, int WGN, int ACT>
+__global__ void __launch_bounds__(64 * WGM * WGN, 2) k_gated_dgate(const Product a, const Sum again, int32_t ids) {
+    constexpr int64_t AM = 32 * WA * WGM, BN = 32 * WNF * WGN;
+    using C = Tile<PL, PL == 1 ? 2 * WA : WA, WNF, WGM, WGN>;
+    __shared__ u32x4x S[C::LDS];
+    int32_t split, mt, nt, id = blockIdx.x;
+    if (!tile_of(a, id, split, mt, nt)) return;
+    using F = Feed<PL, WA, WNF, WGM, WGN, false, false, false, C::STAGE>;
+    using A = Feed<PL, PL == 1 ? 2 * WA : WA, WNF, WGM, WGN, true, false, PL == 1>;
+    F feed;
+    A first;
+    f32x16x ab[PL == 1 ? 2 * WA : 1][PL == 1 ? WNF : 1], acc[WA][WNF];
+    int ready = 0, primed = 0;
+    if constexpr (PL == 1) first.start(again, mt * AM, nt * BN, 0);
+    else feed.start(a.s, mt * AM, nt * BN, 0);
+    while (true) {
+        int32_t m2 = 0, n2 = 0;
+        id += gridDim.x;
+        const bool more = id < ids && tile_of(a, id, split, m2, n2);
+        if constexpr (PL == 1) {
+            const Next<F> dh = {mt * AM, nt * BN, std::min(a.s.steps, 2)};
+            tile_sum(first, again, again.steps, S, ab, ready, primed, true, dh, feed, a.s);
+            const Next<A> next = {m2 * AM, n2 * BN, more ? std::min(again.steps, 2) : 0};
+            tile_sum(feed, a.s, a.s.steps, S, acc, ready, dh.stages, false, next, first, again);
+            primed = next.stages;
+        } else {
+            const Next<F> next = {m2 * AM, n2 * BN, more ? std::min(a.s.steps, 2) : 0};
+            tile_sum(feed, a.s, a.s.steps, S, acc, ready, primed, true, next, feed, a.s);
+            primed = next.stages;
+        }
+        dgate_store<PL, WA, WNF, WGM, WGN, ACT>(a, mt * AM, nt * BN, ab, acc);
+        if (!more) break;
+        mt = m2;
+        nt = n2;
+    }
 }
 // dx and the weights' gradients in one launch: workgroups below `w_at` take dx's tiles, below `d_at` those of dWg and dWu.
 template <int PL, int WMF, int WNF, int WGM, int WGN>
@@ -519,9 +746,9 @@ __global__ void __launch_bounds__(64 * WGM * WGN, 2) k_gated_grads(const Product
                                                                    int32_t d_at) {
     __shared__ u32x4x S[Tile<PL, WMF, WNF, WGM, WGN>::LDS];
     const int32_t id = blockIdx.x;
-    if (id < w_at) gated_tile<PL, WMF, WNF, WGM, WGN, false, false, kOut, 0>(x, id, S);
-    else if (id < d_at) gated_tile<PL, WMF, WNF, WGM, WGN, true, true, kOut, 0>(w, id - w_at, S);
-    else gated_tile<PL, WMF, WNF, WGM, WGN, true, true, kOut, 0>(d, id - d_at, S);
+    if (id < w_at) out_tile<PL, WMF, WNF, WGM, WGN, false, false>(x, id, S);
+    else if (id < d_at) out_tile<PL, WMF, WNF, WGM, WGN, true, true>(w, id - w_at, S);
+    else out_tile<PL, WMF, WNF, WGM, WGN, true, true>(d, id - d_at, S);
 }
 
 // The sum of the splits' parts, in their order.  A launch takes up to three products.
@@ -556,29 +783,114 @@ __global__ void __launch_bounds__(256) k_gated_join(const JoinJobs jobs) {
 int64_t up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
 
 enum { kTile64, kTile128, kTile256 };
+int64_t edge_of(int tile) { return tile == kTile256 ? 256 : tile == kTile128 ? 128 : 64; }
+int64_t tiles(int64_t rows, int64_t cols, int64_t edge) { return up(rows, edge) / edge * (up(cols, edge) / edge); }
 
 // Tile of the launches over m rows and these columns: the largest that gives every compute unit something to do.
 int tile_for(int64_t rows, int64_t cols, bool bf16) {
-    if (bf16 && up(rows, 256) / 256 * (up(cols, 256) / 256) >= 192) return kTile256;
-    return up(rows, 128) / 128 * (up(cols, 128) / 128) >= 192 ? kTile128 : kTile64;
+    if (bf16 && tiles(rows, cols, 256) >= 192) return kTile256;
+    return tiles(rows, cols, 128) >= 192 ? kTile128 : kTile64;
 }
-int64_t edge_of(int tile) { return tile == kTile256 ? 256 : tile == kTile128 ? 128 : 64; }
 
-// Splits of a sum of `steps` steps whose product has `tiles` tiles: two workgroups a unit, 8 steps each at least.
-int32_t splits_for(int64_t tiles, int64_t steps) {
-    const int64_t want = std::max<int64_t>(1, 512 / std::max<int64_t>(tiles, 1));
-    return (int32_t)std::max<int64_t>(1, std::min<int64_t>({want, steps / 8, 64}));
+// A product's part in a launch: tiles, steps of each, entries of the output.
+struct Job {
+    int64_t tiles, steps, entries;
+    int32_t splits = 1;
+};
+// Steps until a launch's last workgroup ends, its jobs' workgroups going to `slots` places in their order.
+int64_t makespan(const Job *jobs, int n, int64_t slots) {
+    // times at which places become free, with how many do: few distinct ones
+    int64_t at[64], count[64];
+    int k = 1;
+    at[0] = 0;
+    count[0] = slots;
+    int64_t last = 0;
+    for (int j = 0; j < n; ++j) {
+        int64_t left = jobs[j].tiles * jobs[j].splits;
+        const int64_t each = (jobs[j].steps + jobs[j].splits - 1) / std::max<int64_t>(jobs[j].splits, 1);
+        if (left > 16 * slots) return INT64_MAX;   // (long anyway)
+        while (left > 0) {
+            int first = 0;
+            for (int i = 1; i < k; ++i)
+                if (at[i] < at[first]) first = i;
+            const int64_t take = std::min(left, count[first]), end = at[first] + each;
+            left -= take;
+            last = std::max(last, end);
+            count[first] -= take;
+            if (count[first] == 0) {
+                at[first] = at[k - 1];
+                count[first] = count[k - 1];
+                --k;
+            }
+            int same = 0;
+            while (same < k && at[same] != end) ++same;
+            if (same < k) {
+                count[same] += take;
+            } else if (k < 64) {
+                at[k] = end;
+                count[k++] = take;
+            } else {
+                return INT64_MAX;
+            }
+        }
+    }
+    return last;
+}
+// Splits of the jobs' sums, so that the launch ends early: the steps of its longest place and what the parts' way to
+// memory and back takes (in steps of `step_us`).  Parts have 32 steps at least.
+void split(Job *jobs, int n, int64_t slots, double step_us) {
+    int64_t total = 0, longest = 0;
+    for (int j = 0; j < n; ++j) {
+        jobs[j].splits = 1;
+        total += jobs[j].tiles * jobs[j].steps;
+        longest = std::max(longest, jobs[j].tiles > 0 ? jobs[j].steps : 0);
+    }
+    if (longest < 64) return;
+    Job best[3], now[3];
+    auto cost = [&](const Job *x) {
+        const int64_t m = makespan(x, n, slots);
+        if (m == INT64_MAX) return 1e18;
+        double bytes = 0;
+        for (int j = 0; j < n; ++j)
+            if (x[j].splits > 1) bytes += x[j].entries * 8.0 * x[j].splits;
+        return m * step_us + (bytes > 0 ? 4.0 + bytes / 4.5e6 : 0.0);
+    };
+    for (int j = 0; j < n; ++j) best[j] = jobs[j];
+    double least = cost(best);
+    const int64_t even = std::max<int64_t>(1, total / slots);
+    for (int r = 1; r <= 6; ++r)                   // parts of about this share of an even load
+        for (int from = n - 1; from >= 0; --from) {   // the jobs from this one on
+            const int64_t length = std::max<int64_t>(32, (even + r - 1) / r);
+            for (int j = 0; j < n; ++j) {
+                now[j] = jobs[j];
+                if (j >= from && jobs[j].tiles > 0) {
+                    int64_t s = std::max<int64_t>(1, std::min<int64_t>(jobs[j].steps / 32, (jobs[j].steps + length - 1) / length));
+                    const int64_t each = (jobs[j].steps + s - 1) / s;
+                    now[j].splits = (int32_t)((jobs[j].steps + each - 1) / each);   // without empty ones
+                }
+            }
+            const double c = cost(now);
+            if (c < least) {
+                least = c;
+                for (int j = 0; j < n; ++j) best[j] = now[j];
+            }
+        }
+    for (int j = 0; j < n; ++j) jobs[j] = best[j];
 }
 
 unsigned ids_of(const Product &a) {   // workgroups of a product, whole rounds over the XCDs
     return (unsigned)up((int64_t)a.m_tiles * a.n_tiles * a.splits, 8);
 }
 
+// Outputs of fewer entries take h, da and db in two bf16 parts.
+constexpr int64_t kFew = 8192;
+
 // Where everything lies in the workspace, and how the products are cut.
 struct Plan {
     int64_t m, d, f, o;
     int pl, bk;
     bool bf16, pack_x, pack_w, pack_wd, pack_dy;
+    bool low_y, low_dx, low_dw, low_dd;
     int gate, down, dgate, grads;
     int32_t down_splits = 1, dx_splits = 1, dw_splits = 1, dd_splits = 1;
     size_t x = 0, wg = 0, wu = 0, wd = 0, dy = 0, h = 0, D = 0, part = 0, part2 = 0, part3 = 0, total = 0;
@@ -592,45 +904,57 @@ struct Plan {
     static int64_t parts(int64_t rows, int64_t cols, int64_t edge, int32_t splits) {
         return splits > 1 ? splits * up(rows, edge) * up(cols, edge) * 4 : 0;
     }
+    // places of a launch's tiles on the device (two or three workgroups of the smaller ones a unit), and us a step
+    static int64_t slots(int tile) { return tile == kTile256 ? 256 : tile == kTile128 ? 512 : 1024; }
+    double step_us(int tile) const { return (tile == kTile256 ? 1.1 : tile == kTile128 ? 0.6 : 0.4) * (bf16 ? 1.0 : 3.0); }
     Plan(const GatedArgs &a, bool backward) : m(a.m), d(a.d), f(a.f), o(a.d_out), bf16(a.bf16) {
         pl = bf16 ? 1 : 3;
         bk = bf16 ? 32 : 16;
+        low_y = bf16 && m * o < kFew;
+        low_dx = bf16 && m * d < kFew;
+        low_dw = bf16 && d * f < kFew;
+        low_dd = bf16 && f * o < kFew;
         // (where the columns are summed over, the last chunk has to end in zeros)
-        pack_x = !bf16 || (!backward && d % 8);
+        pack_x = !bf16 || d % 8;
         pack_wd = !bf16 || (backward && o % 8);
         pack_dy = !bf16 || o % 8;
-        pack_w = !bf16 || (backward && f % 8);
+        pack_w = !bf16 || (backward && (f % 8 || a.ld_wg != a.ld_wu));   // (a sum's matrices lie alike)
         if (pack_x) x = packed(m, d);
-        if (pack_w) {
+        if (pack_w || backward) {   // (whether their strides differ is not known to who asks for the size)
             wg = packed(d, f);
             wu = packed(d, f);
         }
         if (pack_wd) wd = packed(f, o);
         if (!backward) {
-            h = take(fp() * m * 2 * pl);
+            h = take(fp() * m * 2 * (low_y ? 2 : pl));
             gate = tile_for(m, 2 * f, bf16);
             down = tile_for(m, o, bf16);
-            const int64_t e = edge_of(down), steps = (f + bk - 1) / bk;
-            down_splits = cut(splits_for(up(m, e) / e * (up(o, e) / e), steps), steps);
+            const int64_t e = edge_of(down), steps = (f + bk - 1) / bk * (low_y ? 2 : 1);
+            Job y = {tiles(m, o, e), steps, m * o};
+            split(&y, 1, slots(down), step_us(down));
+            down_splits = y.splits;
             part = take(parts(m, o, e, down_splits));
         } else {
             if (pack_dy) dy = packed(m, o);
-            D = take(2 * fp() * m * 2 * pl);
-            dgate = tile_for(m, f, bf16);
-            grads = std::min(tile_for(m + d, 2 * f, bf16), tile_for(std::max(m, d), std::max(d, f), bf16));
-            const int64_t e = edge_of(grads), ks = (fp() + bk - 1) / bk * 2, ms = (m + bk - 1) / bk;
-            const int64_t tx = up(m, e) / e * (up(d, e) / e), tw = up(d, e) / e * (up(2 * fp(), e) / e), td = up(f, e) / e * (up(o, e) / e);
-            dx_splits = cut(splits_for(tx, ks), ks);
-            dw_splits = cut(splits_for(tw, ms), ms);
-            dd_splits = cut(splits_for(td, ms), ms);
+            D = take(2 * fp() * m * 2 * (low_dx || low_dw ? 2 : pl));
+            if (low_dd) h = take(fp() * m * 4);
+            dgate = bf16 ? (up(m, 256) / 256 * (up(f, 128) / 128) >= 192 ? kTile256 : up(m, 128) / 128 * (up(f, 64) / 64) >= 384 ? kTile128 : kTile64)
+                         : tile_for(m, f, false);
+            // (the larger tiles where the sums can be cut into enough parts)
+            const int64_t ks = (fp() + bk - 1) / bk * (low_dx ? 4 : 2), ms = (m + bk - 1) / bk;
+            auto work = [&](int64_t e) { return tiles(m, d, e) * ks + (tiles(d, 2 * fp(), e) + tiles(f, o, e)) * ms; };
+            grads = bf16 && work(256) >= 192 * 32 ? kTile256 : work(128) >= 192 * 32 ? kTile128 : kTile64;
+            const int64_t e = edge_of(grads);
+            Job j[3] = {{tiles(m, d, e), ks, m * d}, {tiles(d, 2 * fp(), e), ms * (low_dw ? 2 : 1), 2 * d * fp()},
+                        {tiles(f, o, e), ms * (low_dd ? 2 : 1), f * o}};
+            split(j, 3, slots(grads), step_us(grads));
+            dx_splits = j[0].splits;
+            dw_splits = j[1].splits;
+            dd_splits = j[2].splits;
             part = take(parts(m, d, e, dx_splits));
             part2 = take(parts(d, 2 * fp(), e, dw_splits));
             part3 = take(parts(f, o, e, dd_splits));
         }
-    }
-    static int32_t cut(int32_t splits, int64_t steps) {   // without empty ones
-        const int64_t each = std::max<int64_t>(1, (steps + splits - 1) / splits);
-        return (int32_t)std::max<int64_t>(1, (steps + each - 1) / each);
     }
 };
 
@@ -639,32 +963,26 @@ Operand operand(const void *p, int64_t ld, int64_t rows, int64_t cols, const cha
     Operand o = {};
     o.rows = (int32_t)rows;
     o.chunks = (int32_t)(up(cols, 8) / 8);
-    if (packed_at) {
-        o.p[0] = o.p[1] = packed_at;
-        o.row[0] = o.row[1] = 16;
-        o.chunk = rows * 16;
-        o.plane = o.chunk * o.chunks;
-    } else {
-        o.p[0] = o.p[1] = (const char *)p;
-        o.row[0] = o.row[1] = ld * 2;
-        o.chunk = 16;
-        o.plane = 0;
-    }
+    o.chunk = packed_at ? rows * 16 : 16;
+    o.plane = packed_at ? o.chunk * o.chunks : 0;
+    o.p0 = o.p1 = o.p2 = o.p3 = packed_at ? packed_at : (const char *)p;
+    o.row0 = o.row1 = packed_at ? 16 : ld * 2;
     return o;
 }
-
-// ... and a second matrix of the same sizes
+// ... and a second matrix of the same sizes (and so on, in turn)
 void second(Operand &o, const void *p, int64_t ld, const char *packed_at) {
-    o.p[1] = packed_at ? packed_at : (const char *)p;
-    o.row[1] = packed_at ? 16 : ld * 2;
+    o.p1 = o.p3 = packed_at ? packed_at : (const char *)p;
+    o.row1 = packed_at ? 16 : ld * 2;
 }
 
-void sum_over(Product &p, int64_t k, int bk, int32_t segments, int32_t splits) {
+void sum_over(Sum &p, int64_t k, int bk, int32_t segments) {
     p.segments = segments;
     p.steps = (int32_t)((k + bk - 1) / bk);
     p.tail = (int32_t)(k - (int64_t)(p.steps - 1) * bk);
+}
+void cut(Product &p, int32_t splits) {
     p.splits = splits;
-    p.split_steps = (int32_t)((segments * (int64_t)p.steps + splits - 1) / splits);
+    p.split_steps = (int32_t)((p.s.segments * (int64_t)p.s.steps + splits - 1) / splits);
 }
 void tiles_of(Product &p, int64_t rows, int64_t cols, int64_t bn, int64_t bm) {
     p.n = (int32_t)rows;
@@ -715,18 +1033,32 @@ struct Packer {
         else L(PL, 2, 1, 1, 2);                        \
     } while (0)
 
+// Workgroups of a launch that takes tile after tile: `each` a unit, whole rounds over the XCDs.
+unsigned places_of(const Product &a, int each, hipStream_t s) {
+    return std::min<unsigned>(ids_of(a), (unsigned)up((int64_t)stream_units(s) * each, 8));
+}
 template <int PL, int ACT>
 void run_gate(const Product &p, int tile, hipStream_t s) {
     KernelTimer t("gated_gate", s);
-#define GNNAV_L(P, A, B, C, D) hipLaunchKernelGGL((k_gated_gate<P, A, B, C, D, ACT>), dim3(ids_of(p)), dim3(64 * C * D), 0, s, p)
+#define GNNAV_L(P, A, B, C, D)                                                                                          \
+    hipLaunchKernelGGL((k_gated_gate<P, A, B, C, D, ACT>), dim3(places_of(p, tile == kTile256 ? 1 : 3, s)), dim3(64 * C * D), 0, s, p, \
+                       (int32_t)ids_of(p))
     GNNAV_TILES(PL, tile, GNNAV_L);
 #undef GNNAV_L
 }
 template <int PL, int ACT>
-void run_dgate(const Product &p, int tile, hipStream_t s) {
+void run_dgate(const Product &p, const Sum &again, int tile, hipStream_t s) {
     KernelTimer t("gated_dgate", s);
-#define GNNAV_L(P, A, B, C, D) hipLaunchKernelGGL((k_gated_dgate<P, A, B, C, D, ACT>), dim3(ids_of(p)), dim3(64 * C * D), 0, s, p)
-    GNNAV_TILES(PL, tile, GNNAV_L);
+#define GNNAV_L(A, B, C, D, EACH)                                                                                       \
+    hipLaunchKernelGGL((k_gated_dgate<PL, A, B, C, D, ACT>), dim3(places_of(p, EACH, s)), dim3(64 * C * D), 0, s, p, again, (int32_t)ids_of(p))
+    if constexpr (PL == 1) {
+        if (tile == kTile256) GNNAV_L(2, 2, 2, 4, 1);
+        else if (tile == kTile128) GNNAV_L(1, 2, 2, 2, 3);
+        else GNNAV_L(1, 1, 2, 2, 4);
+    } else {
+        if (tile == kTile128) GNNAV_L(2, 2, 2, 2, 2);
+        else GNNAV_L(1, 1, 2, 2, 4);
+    }
 #undef GNNAV_L
 }
 template <int PL>
@@ -766,15 +1098,17 @@ void run_grads(const Product &x, const Product &w, const Product &d, int tile, h
     run_join<PL>(x, w, d, tile, s);
 }
 
-// where a, b and h lie in what is kept for the backward pass
+// where a, b (fp32) and h lie in what is kept for the backward pass
 struct Saved {
-    f32x4x *a, *b;
+    f32x4x *a = nullptr, *b = nullptr;
     u32x4x *h;
-    Saved(void *p, int64_t m, int64_t f) {
+    Saved(void *p, int64_t m, int64_t f, bool bf16) {
         const int64_t fp = up(f, 8);
-        a = (f32x4x *)p;
-        b = a + fp / 4 * m;
-        h = (u32x4x *)(b + fp / 4 * m);
+        if (!bf16 && p) {
+            a = (f32x4x *)p;
+            b = a + fp / 4 * m;
+        }
+        h = bf16 ? (u32x4x *)p : (u32x4x *)((char *)p + fp * m * 8);
     }
 };
 
@@ -791,28 +1125,34 @@ void forward(const GatedArgs &x, hipStream_t s) {
     }
     if (p.pack_wd) pack.add(x.wd, x.ld_wd, x.f, x.d_out, ws + p.wd);
     pack.run(x.bf16, s);
-    const Saved saved(x.saved, x.m, x.f);
+    const Saved saved(x.saved, x.m, x.f, x.bf16);
     u32x4x *h = x.saved ? saved.h : (u32x4x *)(ws + p.h);
-    const int64_t fp = p.fp();
+    const int64_t plane = p.fp() / 8 * x.m;   // chunks of h
 
     Product g = {};
-    g.A = operand(x.wg, x.ld_wg, x.d, x.f, at(p.pack_w, p.wg));
-    second(g.A, x.wu, x.ld_wu, at(p.pack_w, p.wu));
-    g.B = operand(x.x, x.ld_x, x.m, x.d, at(p.pack_x, p.x));
-    sum_over(g, x.d, p.bk, 1, 1);
+    g.s.A = operand(x.wg, x.ld_wg, x.d, x.f, at(p.pack_w, p.wg));
+    second(g.s.A, x.wu, x.ld_wu, at(p.pack_w, p.wu));
+    g.s.B = operand(x.x, x.ld_x, x.m, x.d, at(p.pack_x, p.x));
+    sum_over(g.s, x.d, p.bk, 1);
+    cut(g, 1);
     const int64_t e = edge_of(p.gate);
     tiles_of(g, x.m, x.f, e, e / 2);
     g.f = (int32_t)x.f;
-    g.a = x.saved ? saved.a : nullptr;
-    g.b = x.saved ? saved.b : nullptr;
+    g.a = saved.a;
+    g.b = saved.b;
     g.h = h;
-    g.h_plane = fp / 8 * x.m;
+    g.h_plane = plane;
+    // (second parts always go to the workspace, behind the place that h has there)
+    u32x4x *low = (u32x4x *)(ws + p.h) + plane;
+    g.low = p.low_y ? low - h : 0;
     run_gate<PL, ACT>(g, p.gate, s);
 
     Product y = {};
-    y.A = operand(x.wd, x.ld_wd, x.f, x.d_out, at(p.pack_wd, p.wd));
-    y.B = operand(nullptr, 0, x.m, x.f, (const char *)h);
-    sum_over(y, x.f, p.bk, 1, p.down_splits);
+    y.s.A = operand(x.wd, x.ld_wd, x.f, x.d_out, at(p.pack_wd, p.wd));
+    y.s.B = operand(nullptr, 0, x.m, x.f, (const char *)h);
+    y.s.B.p1 = (const char *)low;
+    sum_over(y.s, x.f, p.bk, p.low_y ? 2 : 1);
+    cut(y, p.down_splits);
     tiles_of(y, x.m, x.d_out, edge_of(p.down), edge_of(p.down));
     writes(y, x.y, x.ld_y, x.d_out, x.bf16);
     parts_at(y, ws + p.part, edge_of(p.down));
@@ -825,50 +1165,67 @@ void backward(const GatedArgs &x, hipStream_t s) {
     const Plan p(x, true);
     char *ws = (char *)x.workspace;
     auto at = [&](bool packed, size_t offset) { return packed ? ws + offset : nullptr; };
+    const bool dgate = x.m > 0 && (x.dx || x.dwg || x.dwu || (x.dwd && p.low_dd));
     Packer pack;
-    if (p.pack_x && (x.dwg || x.dwu)) pack.add(x.x, x.ld_x, x.m, x.d, ws + p.x);
+    if (p.pack_x && (x.dwg || x.dwu || (PL == 1 && dgate))) pack.add(x.x, x.ld_x, x.m, x.d, ws + p.x);
     if (p.pack_w && x.dx) {
         pack.add(x.wg, x.ld_wg, x.d, x.f, ws + p.wg);
         pack.add(x.wu, x.ld_wu, x.d, x.f, ws + p.wu);
     }
-    if (p.pack_wd) pack.add(x.wd, x.ld_wd, x.f, x.d_out, ws + p.wd);
+    if (p.pack_wd && dgate) pack.add(x.wd, x.ld_wd, x.f, x.d_out, ws + p.wd);
     if (p.pack_dy) pack.add(x.dy, x.ld_dy, x.m, x.d_out, ws + p.dy);
     if (x.m > 0) pack.run(x.bf16, s);
-    const Saved saved(const_cast<void *>(x.saved), x.m, x.f);
-    u32x4x *D = (u32x4x *)(ws + p.D);
-    const int64_t fp = p.fp(), e = edge_of(p.grads);
+    const Saved saved(x.saved, x.m, x.f, x.bf16);
+    u32x4x *D = (u32x4x *)(ws + p.D), *h = (u32x4x *)(ws + p.h);
+    const int64_t fp = p.fp(), e = edge_of(p.grads), plane = fp / 8 * x.m;   // chunks of da, of db, of h
+    const Operand wg = operand(x.wg, x.ld_wg, x.d, x.f, at(p.pack_w, p.wg)), rows = operand(x.x, x.ld_x, x.m, x.d, at(p.pack_x, p.x)),
+                  dy = operand(x.dy, x.ld_dy, x.m, x.d_out, at(p.pack_dy, p.dy));
 
-    if (x.m > 0 && (x.dx || x.dwg || x.dwu)) {
+    if (dgate) {
         Product g = {};
-        g.A = operand(x.wd, x.ld_wd, x.f, x.d_out, at(p.pack_wd, p.wd));
-        g.B = operand(x.dy, x.ld_dy, x.m, x.d_out, at(p.pack_dy, p.dy));
-        sum_over(g, x.d_out, p.bk, 1, 1);
-        tiles_of(g, x.m, x.f, edge_of(p.dgate), edge_of(p.dgate));
+        g.s.A = operand(x.wd, x.ld_wd, x.f, x.d_out, at(p.pack_wd, p.wd));
+        g.s.B = dy;
+        sum_over(g.s, x.d_out, p.bk, 1);
+        cut(g, 1);
+        tiles_of(g, x.m, x.f, edge_of(p.dgate), edge_of(p.dgate) / (PL == 1 && p.dgate != kTile64 ? 2 : 1));
         g.f = (int32_t)x.f;
         g.a = saved.a;
         g.b = saved.b;
         g.h = D;
-        g.h_plane = 2 * fp / 8 * x.m;
-        g.second = fp / 8 * x.m;
-        run_dgate<PL, ACT>(g, p.dgate, s);
+        g.h_plane = 2 * plane;
+        g.second = plane;
+        g.low = p.low_dx || p.low_dw ? 2 * plane : 0;
+        g.h2 = p.low_dd ? h : nullptr;
+        g.h2_low = plane;
+        Sum again = {};   // (the weights' rows are summed over: as they lie)
+        again.A = operand(x.wg, x.ld_wg, x.d, x.f, nullptr);
+        second(again.A, x.wu, x.ld_wu, nullptr);
+        again.B = rows;
+        sum_over(again, x.d, p.bk, 1);
+        run_dgate<PL, ACT>(g, again, p.dgate, s);
     }
 
     Product dx = {}, w = {}, d = {};
     if (x.dx && x.m > 0) {
-        dx.A = operand(x.wg, x.ld_wg, x.d, x.f, at(p.pack_w, p.wg));
-        second(dx.A, x.wu, x.ld_wu, at(p.pack_w, p.wu));
-        dx.B = operand(nullptr, 0, x.m, x.f, (const char *)D);
-        dx.B.p[1] += fp / 8 * x.m * 16;
-        dx.B.plane *= 2;
-        sum_over(dx, fp, p.bk, 2, p.dx_splits);
+        dx.s.A = wg;
+        second(dx.s.A, x.wu, x.ld_wu, at(p.pack_w, p.wu));
+        dx.s.B = operand(nullptr, 0, x.m, x.f, (const char *)D);
+        dx.s.B.p1 += plane * 16;   // da, db, their second parts
+        dx.s.B.p2 += 2 * plane * 16;
+        dx.s.B.p3 += 3 * plane * 16;
+        dx.s.B.plane = 2 * plane * 16;
+        sum_over(dx.s, fp, p.bk, p.low_dx ? 4 : 2);
+        cut(dx, p.dx_splits);
         tiles_of(dx, x.m, x.d, e, e);
         writes(dx, x.dx, x.ld_dx, x.d, x.bf16);
         parts_at(dx, ws + p.part, e);
     }
     if (x.dwg || x.dwu) {
-        w.A = operand(nullptr, 0, x.m, 2 * fp, (const char *)D);
-        w.B = operand(x.x, x.ld_x, x.m, x.d, at(p.pack_x, p.x));
-        sum_over(w, x.m, p.bk, 1, p.dw_splits);
+        w.s.A = operand(nullptr, 0, x.m, 2 * fp, (const char *)D);
+        w.s.A.p1 += 2 * plane * 16;
+        w.s.B = rows;
+        sum_over(w.s, x.m, p.bk, p.low_dw ? 2 : 1);
+        cut(w, p.dw_splits);
         tiles_of(w, x.d, 2 * fp, e, e);
         writes(w, x.dwg, x.ld_dwg, x.f, x.bf16);
         w.out[1] = x.dwu;
@@ -877,9 +1234,11 @@ void backward(const GatedArgs &x, hipStream_t s) {
         parts_at(w, ws + p.part2, e);
     }
     if (x.dwd) {
-        d.A = operand(x.dy, x.ld_dy, x.m, x.d_out, at(p.pack_dy, p.dy));
-        d.B = operand(nullptr, 0, x.m, x.f, (const char *)saved.h);
-        sum_over(d, x.m, p.bk, 1, p.dd_splits);
+        d.s.A = dy;
+        d.s.B = operand(nullptr, 0, x.m, x.f, (const char *)(p.low_dd ? h : saved.h));
+        d.s.B.p1 = (const char *)(h + plane);
+        sum_over(d.s, x.m, p.bk, p.low_dd ? 2 : 1);
+        cut(d, p.dd_splits);
         tiles_of(d, x.f, x.d_out, e, e);
         writes(d, x.dwd, x.ld_dwd, x.d_out, x.bf16);
         parts_at(d, ws + p.part3, e);
@@ -900,7 +1259,7 @@ void by_act(const GatedArgs &x, bool back, hipStream_t s) {
 }  // namespace
 
 size_t gated_workspace(const GatedArgs &a, bool backward) { return Plan(a, backward).total; }
-size_t gated_saved(int64_t m, int64_t f, bool bf16) { return (size_t)(m * up(f, 8) * (8 + (bf16 ? 2 : 6))); }
+size_t gated_saved(int64_t m, int64_t f, bool bf16) { return (size_t)(m * up(f, 8) * (bf16 ? 2 : 14)); }
 
 void launch_gated(const GatedArgs &x, bool backward, hipStream_t s) {
     if (x.m == 0 && !backward) return;

@@ -106,7 +106,7 @@ def test_workspace_sizes():
         for m, d, f, o in [(0, 1, 1, 1), (1 << 28, 8, 8, 8), (1, 1 << 20, 1 << 20, 1 << 20), (1 << 28, 1 << 20, 1 << 20, 1 << 20)]:
             for query in (lib.gnnav_gated_ffn_workspace, lib.gnnav_gated_ffn_backward_workspace):
                 assert 0 <= query(m, d, f, o, dt) < 1 << 62
-            assert lib.gnnav_gated_ffn_saved(m, f, dt) == m * ((f + 7) // 8 * 8) * (10 if dt else 14)
+            assert lib.gnnav_gated_ffn_saved(m, f, dt) == m * ((f + 7) // 8 * 8) * (2 if dt else 14)
         for m, c in [(0, 1), (top, 41), (1, top), (top, top), (64, top)]:
             assert lib.gnnav_top_logits_workspace(m, c, 256, dt) >= 0 and lib.gnnav_distill_workspace(m, c, 256, dt) > 0
 
