@@ -704,6 +704,8 @@ __global__ void __launch_bounds__(64 * WGM * WGN, 2) k_gated_down(const Product 
     __shared__ u32x4x S[Tile<PL, WMF, WNF, WGM, WGN>::LDS];
     out_tile<PL, WMF, WNF, WGM, WGN, true, false>(a, blockIdx.x, S);
 }
+// fp32 takes tile after tile too; bf16, whose three sums leave no registers for the next tile's copies, one: the copies of dh's sum
+// follow those of a and b.
 template <int PL, int WA, int WNF, int WGM, int WGN, int ACT>
 __global__ void __launch_bounds__(64 * WGM * WGN, 2) k_gated_dgate(const Product a, const Sum again, int32_t ids) {
     constexpr int64_t AM = 32 * WA * WGM, BN = 32 * WNF * WGN;
@@ -712,32 +714,32 @@ __global__ void __launch_bounds__(64 * WGM * WGN, 2) k_gated_dgate(const Product
     int32_t split, mt, nt, id = blockIdx.x;
     if (!tile_of(a, id, split, mt, nt)) return;
     using F = Feed<PL, WA, WNF, WGM, WGN, false, false, false, C::STAGE>;
-    using A = Feed<PL, PL == 1 ? 2 * WA : WA, WNF, WGM, WGN, true, false, PL == 1>;
     F feed;
-    A first;
     f32x16x ab[PL == 1 ? 2 * WA : 1][PL == 1 ? WNF : 1], acc[WA][WNF];
     int ready = 0, primed = 0;
-    if constexpr (PL == 1) first.start(again, mt * AM, nt * BN, 0);
-    else feed.start(a.s, mt * AM, nt * BN, 0);
-    while (true) {
-        int32_t m2 = 0, n2 = 0;
-        id += gridDim.x;
-        const bool more = id < ids && tile_of(a, id, split, m2, n2);
-        if constexpr (PL == 1) {
-            const Next<F> dh = {mt * AM, nt * BN, std::min(a.s.steps, 2)};
-            tile_sum(first, again, again.steps, S, ab, ready, primed, true, dh, feed, a.s);
-            const Next<A> next = {m2 * AM, n2 * BN, more ? std::min(again.steps, 2) : 0};
-            tile_sum(feed, a.s, a.s.steps, S, acc, ready, dh.stages, false, next, first, again);
-            primed = next.stages;
-        } else {
+    if constexpr (PL == 1) {
+        using A = Feed<PL, 2 * WA, WNF, WGM, WGN, true, false, true>;
+        A first;
+        first.start(again, mt * AM, nt * BN, 0);
+        const Next<F> dh = {mt * AM, nt * BN, std::min(a.s.steps, 2)};
+        tile_sum(first, again, again.steps, S, ab, ready, 0, false, dh, feed, a.s);
+        const Nothing nothing;
+        tile_sum(feed, a.s, a.s.steps, S, acc, ready, dh.stages, false, nothing, feed, a.s);
+        dgate_store<PL, WA, WNF, WGM, WGN, ACT>(a, mt * AM, nt * BN, ab, acc);
+    } else {
+        feed.start(a.s, mt * AM, nt * BN, 0);
+        while (true) {
+            int32_t m2 = 0, n2 = 0;
+            id += gridDim.x;
+            const bool more = id < ids && tile_of(a, id, split, m2, n2);
             const Next<F> next = {m2 * AM, n2 * BN, more ? std::min(a.s.steps, 2) : 0};
             tile_sum(feed, a.s, a.s.steps, S, acc, ready, primed, true, next, feed, a.s);
             primed = next.stages;
+            dgate_store<PL, WA, WNF, WGM, WGN, ACT>(a, mt * AM, nt * BN, ab, acc);
+            if (!more) break;
+            mt = m2;
+            nt = n2;
         }
-        dgate_store<PL, WA, WNF, WGM, WGN, ACT>(a, mt * AM, nt * BN, ab, acc);
-        if (!more) break;
-        mt = m2;
-        nt = n2;
     }
 }
 // dx and the weights' gradients in one launch: workgroups below `w_at` take dx's tiles, below `d_at` those of dWg and dWu.
@@ -1050,7 +1052,8 @@ template <int PL, int ACT>
 void run_dgate(const Product &p, const Sum &again, int tile, hipStream_t s) {
     KernelTimer t("gated_dgate", s);
 #define GNNAV_L(A, B, C, D, EACH)                                                                                       \
-    hipLaunchKernelGGL((k_gated_dgate<PL, A, B, C, D, ACT>), dim3(places_of(p, EACH, s)), dim3(64 * C * D), 0, s, p, again, (int32_t)ids_of(p))
+    hipLaunchKernelGGL((k_gated_dgate<PL, A, B, C, D, ACT>), dim3(PL == 1 ? ids_of(p) : places_of(p, EACH, s)), dim3(64 * C * D), 0, s, p, again, \
+                       (int32_t)ids_of(p))
     if constexpr (PL == 1) {
         if (tile == kTile256) GNNAV_L(2, 2, 2, 4, 1);
         else if (tile == kTile128) GNNAV_L(1, 2, 2, 2, 3);
