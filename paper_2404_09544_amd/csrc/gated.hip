@@ -761,38 +761,57 @@ struct JoinJobs {
 template <int WMF, int WNF, int WGM, int WGN>
 __global__ void __launch_bounds__(256) k_gated_join(const JoinJobs jobs) {
     constexpr int NW = WGM * WGN, BM = 32 * WMF * WGM, BN = 32 * WNF * WGN;
-    for (int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x; at < jobs.end[2]; at += (int64_t)gridDim.x * 256) {
+    // 256 threads take a block of 32 x 32: 8 consecutive ones four columns each of one row
+    const int row = threadIdx.x / 8, group = threadIdx.x % 8;
+    for (int64_t at = (int64_t)blockIdx.x * 256; at < jobs.end[2]; at += (int64_t)gridDim.x * 256) {
         const int k = at < jobs.end[0] ? 0 : at < jobs.end[1] ? 1 : 2;
         const Product &a = jobs.p[k];
-        const int64_t i = at - (k ? jobs.end[k - 1] : 0);
-        f32x4x v = a.part[i];
-        for (int32_t s = 1; s < a.splits; ++s) v += a.part[s * a.split_stride + i];
-        const int lane = (int)(i & 63);
-        int64_t r = i >> 6;
-        const int g = (int)(r & 3);
-        r >>= 2;
+        int64_t r = at - (k ? jobs.end[k - 1] : 0);
+        const f32x4x *part = a.part + r + group * 32 + row;   // (register group g, half h of the lanes: 64 g + 32 h)
+        f32x4x v = {0.f, 0.f, 0.f, 0.f};
+        int32_t s = 0;
+        for (; s + 8 <= a.splits; s += 8) {
+            f32x4x x[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = part[(s + i) * a.split_stride];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v += x[i];
+        }
+        for (; s < a.splits; ++s) v += part[s * a.split_stride];
+        r >>= 8;
         const int fj = (int)(r % WNF), fi = (int)(r / WNF % WMF);
         r /= WNF * WMF;
         const int wid = (int)(r % NW);
         r /= NW;
         const int32_t mt = (int32_t)(r % a.m_tiles), nt = (int32_t)(r / a.m_tiles);
-        store4(a, (int64_t)nt * BN + wid % WGN * (32 * WNF) + 32 * fj + (lane & 31),
-               mt * BM + wid / WGN * (32 * WMF) + 32 * fi + 8 * g + 4 * (lane >> 5), v);
+        store4(a, (int64_t)nt * BN + wid % WGN * (32 * WNF) + 32 * fj + row, mt * BM + wid / WGN * (32 * WMF) + 32 * fi + 4 * group, v);
     }
 }
 
 // ------------------------------------------------------------------ host
 int64_t up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
 
-enum { kTile64, kTile128, kTile256 };
-int64_t edge_of(int tile) { return tile == kTile256 ? 256 : tile == kTile128 ? 128 : 64; }
-int64_t tiles(int64_t rows, int64_t cols, int64_t edge) { return up(rows, edge) / edge * (up(cols, edge) / edge); }
+int64_t tiles(int64_t rows, int64_t cols, int64_t bn, int64_t bm) { return up(rows, bn) / bn * (up(cols, bm) / bm); }
 
-// Tile of the launches over m rows and these columns: the largest that gives every compute unit something to do.
-int tile_for(int64_t rows, int64_t cols, bool bf16) {
-    if (bf16 && tiles(rows, cols, 256) >= 192) return kTile256;
-    return tiles(rows, cols, 128) >= 192 ? kTile128 : kTile64;
-}
+// A tile: columns and rows of the output, workgroups that a unit holds at once, and what a step takes: a unit's workgroups
+// `share` us each, and none less than `alone`.  Measured: 8,192 x 1,024 outputs of 4,096 summed bf16 columns 126 us in tiles of
+// 256 x 256, 104 of 128 x 256, 175 of 64 x 128, 256 of 64 x 64; 4,000 x 512 of 1,024 columns 42, 31, 19, 22.
+struct Shape {
+    int bm, bn, each;
+    double share, alone;
+};
+constexpr int kUnits = 256;
+enum { kLarge, kWide, kMedium, kSmall, kShapes };
+const Shape kOutBf16[kShapes] = {{256, 256, 1, 1.05, 1.05}, {128, 256, 2, 0.52, 0.81}, {64, 128, 4, 0.33, 0.47}, {64, 64, 8, 0.25, 0.40}};
+const Shape kOutF32[kShapes] = {{0, 0, 0, 0, 0}, {128, 128, 2, 0.80, 1.0}, {64, 128, 2, 0.45, 0.70}, {64, 64, 4, 0.25, 0.5}};
+// the gradients, whose operands' rows are summed over
+const Shape kGradsBf16[kShapes] = {{256, 256, 1, 0.95, 0.95}, {128, 256, 2, 0.72, 0.90}, {64, 128, 4, 0.36, 0.50}, {64, 64, 8, 0.27, 0.42}};
+// h: columns of one projection
+const Shape kGateBf16[kShapes] = {{128, 256, 1, 1.05, 1.05}, {0, 0, 0, 0, 0}, {64, 128, 3, 0.33, 0.50}, {32, 64, 6, 0.22, 0.40}};
+const Shape kGateF32[kShapes] = {{0, 0, 0, 0, 0}, {64, 128, 2, 0.80, 1.0}, {0, 0, 0, 0, 0}, {32, 64, 4, 0.25, 0.5}};
+// da and db: a step of one product
+const Shape kDgateBf16[kShapes] = {{128, 256, 1, 0.56, 0.60}, {0, 0, 0, 0, 0}, {64, 128, 3, 0.18, 0.30}, {64, 64, 4, 0.12, 0.25}};
+const Shape kDgateF32[kShapes] = {{0, 0, 0, 0, 0}, {128, 128, 2, 0.80, 1.0}, {0, 0, 0, 0, 0}, {64, 64, 4, 0.25, 0.5}};
 
 // A product's part in a launch: tiles, steps of each, entries of the output.
 struct Job {
@@ -838,46 +857,80 @@ int64_t makespan(const Job *jobs, int n, int64_t slots) {
     }
     return last;
 }
-// Splits of the jobs' sums, so that the launch ends early: the steps of its longest place and what the parts' way to
-// memory and back takes (in steps of `step_us`).  Parts have 32 steps at least.
-void split(Job *jobs, int n, int64_t slots, double step_us) {
+// us that a launch of these jobs takes, their parts' way to memory and back in a launch of its own among them.
+double cost(const Job *jobs, int n, const Shape &shape) {
+    const int64_t m = makespan(jobs, n, (int64_t)kUnits * shape.each);
+    if (m == INT64_MAX) return 1e18;
+    int64_t groups = 0;
+    double bytes = 0;
+    for (int j = 0; j < n; ++j) {
+        groups += jobs[j].tiles * jobs[j].splits;
+        if (jobs[j].splits > 1) bytes += jobs[j].entries * 8.0 * jobs[j].splits;
+    }
+    const int64_t held = std::min<int64_t>(shape.each, (groups + kUnits - 1) / kUnits);
+    return m * std::max(shape.alone, held * shape.share) + (bytes > 0 ? 5.0 + bytes / 2.5e6 : 0.0);
+}
+// Splits of the jobs' sums that make it least.  Parts have 16 steps at least.
+double split(Job *jobs, int n, const Shape &shape) {
     int64_t total = 0, longest = 0;
     for (int j = 0; j < n; ++j) {
         jobs[j].splits = 1;
         total += jobs[j].tiles * jobs[j].steps;
         longest = std::max(longest, jobs[j].tiles > 0 ? jobs[j].steps : 0);
     }
-    if (longest < 64) return;
+    double least = cost(jobs, n, shape);
+    if (least > 1e17) {   // (more rounds than are followed)
+        least = total * shape.share / kUnits;
+        return least;
+    }
+    if (longest < 48) return least;
     Job best[3], now[3];
-    auto cost = [&](const Job *x) {
-        const int64_t m = makespan(x, n, slots);
-        if (m == INT64_MAX) return 1e18;
-        double bytes = 0;
-        for (int j = 0; j < n; ++j)
-            if (x[j].splits > 1) bytes += x[j].entries * 8.0 * x[j].splits;
-        return m * step_us + (bytes > 0 ? 4.0 + bytes / 4.5e6 : 0.0);
-    };
     for (int j = 0; j < n; ++j) best[j] = jobs[j];
-    double least = cost(best);
-    const int64_t even = std::max<int64_t>(1, total / slots);
+    const int64_t even = std::max<int64_t>(1, total / ((int64_t)kUnits * shape.each));
     for (int r = 1; r <= 6; ++r)                   // parts of about this share of an even load
         for (int from = n - 1; from >= 0; --from) {   // the jobs from this one on
-            const int64_t length = std::max<int64_t>(32, (even + r - 1) / r);
+            const int64_t length = std::max<int64_t>(16, (even + r - 1) / r);
             for (int j = 0; j < n; ++j) {
                 now[j] = jobs[j];
                 if (j >= from && jobs[j].tiles > 0) {
-                    int64_t s = std::max<int64_t>(1, std::min<int64_t>(jobs[j].steps / 32, (jobs[j].steps + length - 1) / length));
+                    const int64_t s = std::max<int64_t>(1, std::min<int64_t>({jobs[j].steps / 16, (jobs[j].steps + length - 1) / length, 64}));
                     const int64_t each = (jobs[j].steps + s - 1) / s;
                     now[j].splits = (int32_t)((jobs[j].steps + each - 1) / each);   // without empty ones
                 }
             }
-            const double c = cost(now);
+            const double c = cost(now, n, shape);
             if (c < least) {
                 least = c;
                 for (int j = 0; j < n; ++j) best[j] = now[j];
             }
         }
     for (int j = 0; j < n; ++j) jobs[j] = best[j];
+    return least;
+}
+// The shape, of those that there are, whose launch takes least: `jobs_of` fills the jobs of a shape.
+template <class F>
+int choose(const Shape *shapes, Job *jobs, int n, bool may_split, F &&jobs_of) {
+    int which = -1;
+    double least = 0;
+    Job best[3];
+    for (int k = 0; k < kShapes; ++k) {
+        if (shapes[k].bm == 0) continue;
+        jobs_of(shapes[k], jobs);
+        double c;
+        if (may_split) {
+            c = split(jobs, n, shapes[k]);
+        } else {
+            c = cost(jobs, n, shapes[k]);
+            if (c > 1e17) c = jobs[0].tiles * jobs[0].steps * shapes[k].share / kUnits;
+        }
+        if (which < 0 || c < least) {
+            which = k;
+            least = c;
+            for (int j = 0; j < n; ++j) best[j] = jobs[j];
+        }
+    }
+    for (int j = 0; j < n; ++j) jobs[j] = best[j];
+    return which;
 }
 
 unsigned ids_of(const Product &a) {   // workgroups of a product, whole rounds over the XCDs
@@ -903,12 +956,10 @@ struct Plan {
         return here;
     }
     size_t packed(int64_t rows, int64_t cols) { return take(rows * up(cols, 8) * 2 * pl); }
-    static int64_t parts(int64_t rows, int64_t cols, int64_t edge, int32_t splits) {
-        return splits > 1 ? splits * up(rows, edge) * up(cols, edge) * 4 : 0;
+    static int64_t parts(int64_t rows, int64_t cols, const Shape &e, int32_t splits) {
+        return splits > 1 ? splits * up(rows, e.bn) * up(cols, e.bm) * 4 : 0;
     }
-    // places of a launch's tiles on the device (two or three workgroups of the smaller ones a unit), and us a step
-    static int64_t slots(int tile) { return tile == kTile256 ? 256 : tile == kTile128 ? 512 : 1024; }
-    double step_us(int tile) const { return (tile == kTile256 ? 1.1 : tile == kTile128 ? 0.6 : 0.4) * (bf16 ? 1.0 : 3.0); }
+    const Shape &out(int which) const { return (bf16 ? kOutBf16 : kOutF32)[which]; }   // (kGradsBf16's have the same sizes)
     Plan(const GatedArgs &a, bool backward) : m(a.m), d(a.d), f(a.f), o(a.d_out), bf16(a.bf16) {
         pl = bf16 ? 1 : 3;
         bk = bf16 ? 32 : 16;
@@ -929,27 +980,27 @@ struct Plan {
         if (pack_wd) wd = packed(f, o);
         if (!backward) {
             h = take(fp() * m * 2 * (low_y ? 2 : pl));
-            gate = tile_for(m, 2 * f, bf16);
-            down = tile_for(m, o, bf16);
-            const int64_t e = edge_of(down), steps = (f + bk - 1) / bk * (low_y ? 2 : 1);
-            Job y = {tiles(m, o, e), steps, m * o};
-            split(&y, 1, slots(down), step_us(down));
-            down_splits = y.splits;
-            part = take(parts(m, o, e, down_splits));
+            Job j;
+            gate = choose(bf16 ? kGateBf16 : kGateF32, &j, 1, false, [&](const Shape &e, Job *x) { *x = {tiles(m, f, e.bn, e.bm), (d + bk - 1) / bk, 0}; });
+            down = choose(bf16 ? kOutBf16 : kOutF32, &j, 1, true,
+                          [&](const Shape &e, Job *x) { *x = {tiles(m, o, e.bn, e.bm), (f + bk - 1) / bk * (low_y ? 2 : 1), m * o}; });
+            down_splits = j.splits;
+            part = take(parts(m, o, out(down), down_splits));
         } else {
             if (pack_dy) dy = packed(m, o);
             D = take(2 * fp() * m * 2 * (low_dx || low_dw ? 2 : pl));
             if (low_dd) h = take(fp() * m * 4);
-            dgate = bf16 ? (up(m, 256) / 256 * (up(f, 128) / 128) >= 192 ? kTile256 : up(m, 128) / 128 * (up(f, 64) / 64) >= 384 ? kTile128 : kTile64)
-                         : tile_for(m, f, false);
-            // (the larger tiles where the sums can be cut into enough parts)
+            Job j[3];
+            dgate = choose(bf16 ? kDgateBf16 : kDgateF32, j, 1, false, [&](const Shape &e, Job *x) {
+                *x = {tiles(m, f, e.bn, e.bm), (o + bk - 1) / bk + (bf16 ? (d + bk - 1) / bk * 2 : 0), 0};
+            });
             const int64_t ks = (fp() + bk - 1) / bk * (low_dx ? 4 : 2), ms = (m + bk - 1) / bk;
-            auto work = [&](int64_t e) { return tiles(m, d, e) * ks + (tiles(d, 2 * fp(), e) + tiles(f, o, e)) * ms; };
-            grads = bf16 && work(256) >= 192 * 32 ? kTile256 : work(128) >= 192 * 32 ? kTile128 : kTile64;
-            const int64_t e = edge_of(grads);
-            Job j[3] = {{tiles(m, d, e), ks, m * d}, {tiles(d, 2 * fp(), e), ms * (low_dw ? 2 : 1), 2 * d * fp()},
-                        {tiles(f, o, e), ms * (low_dd ? 2 : 1), f * o}};
-            split(j, 3, slots(grads), step_us(grads));
+            grads = choose(bf16 ? kGradsBf16 : kOutF32, j, 3, true, [&](const Shape &e, Job *x) {
+                x[0] = {tiles(m, d, e.bn, e.bm), ks, m * d};
+                x[1] = {tiles(d, 2 * fp(), e.bn, e.bm), ms * (low_dw ? 2 : 1), 2 * d * fp()};
+                x[2] = {tiles(f, o, e.bn, e.bm), ms * (low_dd ? 2 : 1), f * o};
+            });
+            const Shape &e = out(grads);
             dx_splits = j[0].splits;
             dw_splits = j[1].splits;
             dd_splits = j[2].splits;
@@ -986,10 +1037,10 @@ void cut(Product &p, int32_t splits) {
     p.splits = splits;
     p.split_steps = (int32_t)((p.s.segments * (int64_t)p.s.steps + splits - 1) / splits);
 }
-void tiles_of(Product &p, int64_t rows, int64_t cols, int64_t bn, int64_t bm) {
+void tiles_of(Product &p, int64_t rows, int64_t cols, const Shape &e) {
     p.n = (int32_t)rows;
-    p.n_tiles = (int32_t)(up(rows, bn) / bn);
-    p.m_tiles = (int32_t)(up(cols, bm) / bm);
+    p.n_tiles = (int32_t)(up(rows, e.bn) / e.bn);
+    p.m_tiles = (int32_t)(up(cols, e.bm) / e.bm);
 }
 void writes(Product &p, void *out, int64_t ld, int64_t cols, bool bf16) {
     p.out[0] = out;
@@ -999,8 +1050,8 @@ void writes(Product &p, void *out, int64_t ld, int64_t cols, bool bf16) {
     p.cols = (int32_t)cols;
     p.bf16 = bf16;
 }
-void parts_at(Product &p, char *at, int64_t edge) {
-    p.split_stride = (int64_t)p.n_tiles * p.m_tiles * edge * edge / 4;
+void parts_at(Product &p, char *at, const Shape &e) {
+    p.split_stride = (int64_t)p.n_tiles * p.m_tiles * e.bn * e.bm / 4;
     p.part = p.splits > 1 ? (f32x4x *)at : nullptr;
 }
 
@@ -1028,11 +1079,18 @@ struct Packer {
     }
 };
 
-#define GNNAV_TILES(PL, TILE, L)                       \
-    do {                                               \
-        if (PL == 1 && TILE == kTile256) L(1, 4, 2, 2, 4); \
-        else if (TILE >= kTile128) L(PL, 2, 2, 2, 2);  \
-        else L(PL, 2, 1, 1, 2);                        \
+#define GNNAV_TILES(PL, WHICH, L)                        \
+    do {                                                 \
+        if constexpr (PL == 1) {                         \
+            if (WHICH == kLarge) L(1, 4, 2, 2, 4);       \
+            else if (WHICH == kWide) L(1, 2, 2, 2, 4);   \
+            else if (WHICH == kMedium) L(1, 1, 2, 2, 2); \
+            else L(1, 2, 1, 1, 2);                       \
+        } else {                                         \
+            if (WHICH == kWide) L(3, 2, 2, 2, 2);        \
+            else if (WHICH == kMedium) L(3, 1, 2, 2, 2); \
+            else L(3, 2, 1, 1, 2);                       \
+        }                                                \
     } while (0)
 
 // Workgroups of a launch that takes tile after tile: `each` a unit, whole rounds over the XCDs.
@@ -1040,26 +1098,32 @@ unsigned places_of(const Product &a, int each, hipStream_t s) {
     return std::min<unsigned>(ids_of(a), (unsigned)up((int64_t)stream_units(s) * each, 8));
 }
 template <int PL, int ACT>
-void run_gate(const Product &p, int tile, hipStream_t s) {
+void run_gate(const Product &p, int which, hipStream_t s) {
     KernelTimer t("gated_gate", s);
-#define GNNAV_L(P, A, B, C, D)                                                                                          \
-    hipLaunchKernelGGL((k_gated_gate<P, A, B, C, D, ACT>), dim3(places_of(p, tile == kTile256 ? 1 : 3, s)), dim3(64 * C * D), 0, s, p, \
-                       (int32_t)ids_of(p))
-    GNNAV_TILES(PL, tile, GNNAV_L);
+#define GNNAV_L(A, B, C, D, EACH)                                                                                       \
+    hipLaunchKernelGGL((k_gated_gate<PL, A, B, C, D, ACT>), dim3(places_of(p, EACH, s)), dim3(64 * C * D), 0, s, p, (int32_t)ids_of(p))
+    if constexpr (PL == 1) {
+        if (which == kLarge) GNNAV_L(4, 2, 2, 4, 1);
+        else if (which == kMedium) GNNAV_L(2, 2, 2, 2, 3);
+        else GNNAV_L(2, 1, 1, 2, 6);
+    } else {
+        if (which == kWide) GNNAV_L(2, 2, 2, 2, 2);
+        else GNNAV_L(2, 1, 1, 2, 4);
+    }
 #undef GNNAV_L
 }
 template <int PL, int ACT>
-void run_dgate(const Product &p, const Sum &again, int tile, hipStream_t s) {
+void run_dgate(const Product &p, const Sum &again, int which, hipStream_t s) {
     KernelTimer t("gated_dgate", s);
 #define GNNAV_L(A, B, C, D, EACH)                                                                                       \
     hipLaunchKernelGGL((k_gated_dgate<PL, A, B, C, D, ACT>), dim3(PL == 1 ? ids_of(p) : places_of(p, EACH, s)), dim3(64 * C * D), 0, s, p, again, \
                        (int32_t)ids_of(p))
     if constexpr (PL == 1) {
-        if (tile == kTile256) GNNAV_L(2, 2, 2, 4, 1);
-        else if (tile == kTile128) GNNAV_L(1, 2, 2, 2, 3);
+        if (which == kLarge) GNNAV_L(2, 2, 2, 4, 1);
+        else if (which == kMedium) GNNAV_L(1, 2, 2, 2, 3);
         else GNNAV_L(1, 1, 2, 2, 4);
     } else {
-        if (tile == kTile128) GNNAV_L(2, 2, 2, 2, 2);
+        if (which == kWide) GNNAV_L(2, 2, 2, 2, 2);
         else GNNAV_L(1, 1, 2, 2, 4);
     }
 #undef GNNAV_L
@@ -1138,8 +1202,7 @@ void forward(const GatedArgs &x, hipStream_t s) {
     g.s.B = operand(x.x, x.ld_x, x.m, x.d, at(p.pack_x, p.x));
     sum_over(g.s, x.d, p.bk, 1);
     cut(g, 1);
-    const int64_t e = edge_of(p.gate);
-    tiles_of(g, x.m, x.f, e, e / 2);
+    tiles_of(g, x.m, x.f, (PL == 1 ? kGateBf16 : kGateF32)[p.gate]);
     g.f = (int32_t)x.f;
     g.a = saved.a;
     g.b = saved.b;
@@ -1156,9 +1219,9 @@ void forward(const GatedArgs &x, hipStream_t s) {
     y.s.B.p1 = (const char *)low;
     sum_over(y.s, x.f, p.bk, p.low_y ? 2 : 1);
     cut(y, p.down_splits);
-    tiles_of(y, x.m, x.d_out, edge_of(p.down), edge_of(p.down));
+    tiles_of(y, x.m, x.d_out, p.out(p.down));
     writes(y, x.y, x.ld_y, x.d_out, x.bf16);
-    parts_at(y, ws + p.part, edge_of(p.down));
+    parts_at(y, ws + p.part, p.out(p.down));
     run_down<PL>(y, p.down, s);
     GNNAV_HIP(hipGetLastError());
 }
@@ -1180,7 +1243,8 @@ void backward(const GatedArgs &x, hipStream_t s) {
     if (x.m > 0) pack.run(x.bf16, s);
     const Saved saved(x.saved, x.m, x.f, x.bf16);
     u32x4x *D = (u32x4x *)(ws + p.D), *h = (u32x4x *)(ws + p.h);
-    const int64_t fp = p.fp(), e = edge_of(p.grads), plane = fp / 8 * x.m;   // chunks of da, of db, of h
+    const int64_t fp = p.fp(), plane = fp / 8 * x.m;   // chunks of da, of db, of h
+    const Shape &e = p.out(p.grads);
     const Operand wg = operand(x.wg, x.ld_wg, x.d, x.f, at(p.pack_w, p.wg)), rows = operand(x.x, x.ld_x, x.m, x.d, at(p.pack_x, p.x)),
                   dy = operand(x.dy, x.ld_dy, x.m, x.d_out, at(p.pack_dy, p.dy));
 
@@ -1190,7 +1254,7 @@ void backward(const GatedArgs &x, hipStream_t s) {
         g.s.B = dy;
         sum_over(g.s, x.d_out, p.bk, 1);
         cut(g, 1);
-        tiles_of(g, x.m, x.f, edge_of(p.dgate), edge_of(p.dgate) / (PL == 1 && p.dgate != kTile64 ? 2 : 1));
+        tiles_of(g, x.m, x.f, (PL == 1 ? kDgateBf16 : kDgateF32)[p.dgate]);
         g.f = (int32_t)x.f;
         g.a = saved.a;
         g.b = saved.b;
@@ -1219,7 +1283,7 @@ void backward(const GatedArgs &x, hipStream_t s) {
         dx.s.B.plane = 2 * plane * 16;
         sum_over(dx.s, fp, p.bk, p.low_dx ? 4 : 2);
         cut(dx, p.dx_splits);
-        tiles_of(dx, x.m, x.d, e, e);
+        tiles_of(dx, x.m, x.d, e);
         writes(dx, x.dx, x.ld_dx, x.d, x.bf16);
         parts_at(dx, ws + p.part, e);
     }
@@ -1229,7 +1293,7 @@ void backward(const GatedArgs &x, hipStream_t s) {
         w.s.B = rows;
         sum_over(w.s, x.m, p.bk, p.low_dw ? 2 : 1);
         cut(w, p.dw_splits);
-        tiles_of(w, x.d, 2 * fp, e, e);
+        tiles_of(w, x.d, 2 * fp, e);
         writes(w, x.dwg, x.ld_dwg, x.f, x.bf16);
         w.out[1] = x.dwu;
         w.ld[1] = x.ld_dwu;
@@ -1242,7 +1306,7 @@ void backward(const GatedArgs &x, hipStream_t s) {
         d.s.B.p1 = (const char *)(h + plane);
         sum_over(d.s, x.m, p.bk, p.low_dd ? 2 : 1);
         cut(d, p.dd_splits);
-        tiles_of(d, x.f, x.d_out, e, e);
+        tiles_of(d, x.f, x.d_out, e);
         writes(d, x.dwd, x.ld_dwd, x.d_out, x.bf16);
         parts_at(d, ws + p.part3, e);
     }
