@@ -23,6 +23,7 @@
 #include "bf16split.hpp"
 #include "common.hpp"
 #include "dma.hpp"
+#include "lanes.hpp"
 
 namespace gnnav {
 
@@ -788,6 +789,126 @@ __global__ void __launch_bounds__(256) k_gated_join(const JoinJobs jobs) {
     }
 }
 
+// ------------------------------------------------------------------ few rows
+// At most 8 rows, nothing kept: the weights are read once as they lie and multiplied in fp32; h stays in fp32.  A workgroup
+// takes 32 columns, its lanes 16 bytes of a row each, the wavefronts different rows; the sums over the rows are joined in
+// registers and then in LDS.  Two launches: h, from both projections (MATS = 2), and y.
+// 1 x 1,024 x 4,096 x 1,024 bf16: 11.9 us, of which the weights' way at 4.72 TB/s is 5.3; 27 with the tiles.
+struct FewArgs {
+    const void *x;             // rows that are multiplied: of the operands' type, or h in fp32
+    int64_t ld_x;
+    const void *w, *w2;
+    int64_t ld_w, ld_w2;
+    int32_t m, k, cols;
+    float *h;                  // [m][cols]
+    void *y;
+    int64_t ld_y;
+};
+constexpr int kFewRows = 8, kFewColumns = 32, kFewChunk = 1024;   // summed rows that are staged at a time
+
+template <bool BF, bool XF, int MR, int MATS, int ACT>
+__global__ void __launch_bounds__(MATS == 2 ? 512 : 1024) k_gated_few(const FewArgs a) {
+    constexpr int NW = MATS == 2 ? 8 : 16, PER = BF ? 8 : 4, CL = kFewColumns / PER, RW = 64 / CL, ROUND = NW * RW, ROUNDS = kFewChunk / ROUND;
+    __shared__ float X[MR][kFewChunk];
+    __shared__ float red[NW][MATS][MR][kFewColumns];
+    const int tid = threadIdx.x, lane = tid & 63, wid = tid >> 6, cl = lane % CL, rl = lane / CL;
+    // workgroups go to the eight XCDs in turn: each takes neighbouring columns, whose lines its L2 shares
+    const int groups = gridDim.x, per = groups / 8, extra = groups % 8, xcd = blockIdx.x % 8;
+    const int group = xcd * per + std::min(xcd, extra) + blockIdx.x / 8;
+    const int32_t c = group * kFewColumns + cl * PER;
+    const bool here = c < a.cols;
+    float acc[MATS][MR][PER];
+#pragma unroll
+    for (int q = 0; q < MATS; ++q)
+#pragma unroll
+        for (int r = 0; r < MR; ++r)
+#pragma unroll
+            for (int e = 0; e < PER; ++e) acc[q][r][e] = 0.f;
+    for (int32_t k0 = 0; k0 < a.k; k0 += kFewChunk) {
+        u32x4x w[MATS][ROUNDS];
+#pragma unroll
+        for (int i = 0; i < ROUNDS; ++i) {
+            const int64_t k = k0 + i * ROUND + wid * RW + rl;
+#pragma unroll
+            for (int q = 0; q < MATS; ++q) {
+                w[q][i] = u32x4x{0, 0, 0, 0};
+                if (here && k < a.k) {
+                    const char *at = (const char *)(q ? a.w2 : a.w) + (k * (q ? a.ld_w2 : a.ld_w) + c) * (BF ? 2 : 4);
+                    w[q][i] = *(const u32x4x *)at;
+                }
+            }
+        }
+        if (k0 > 0) __syncthreads();
+#pragma unroll
+        for (int r = 0; r < MR; ++r)
+            for (int i = tid; i < kFewChunk; i += 64 * NW) {
+                float v = 0.f;
+                if (r < a.m && k0 + i < a.k) {
+                    if constexpr (XF) v = ((const float *)a.x)[r * a.ld_x + k0 + i];
+                    else v = bf16_to_f32(((const uint16_t *)a.x)[r * a.ld_x + k0 + i]);
+                }
+                X[r][i] = v;
+            }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < ROUNDS; ++i) {
+            const int at = i * ROUND + wid * RW + rl;
+            if (k0 + at >= a.k) continue;   // (past the end the staged zeros would meet what is not the weights')
+#pragma unroll
+            for (int q = 0; q < MATS; ++q) {
+                float v[PER];
+#pragma unroll
+                for (int e = 0; e < PER; ++e) {
+                    if constexpr (BF) v[e] = __uint_as_float(e & 1 ? w[q][i][e / 2] & 0xffff0000u : w[q][i][e / 2] << 16);
+                    else v[e] = __uint_as_float(w[q][i][e]);
+                }
+#pragma unroll
+                for (int r = 0; r < MR; ++r)
+#pragma unroll
+                    for (int e = 0; e < PER; ++e) acc[q][r][e] = __builtin_fmaf(v[e], X[r][at], acc[q][r][e]);
+            }
+        }
+    }
+#pragma unroll
+    for (int q = 0; q < MATS; ++q)
+#pragma unroll
+        for (int r = 0; r < MR; ++r)
+#pragma unroll
+            for (int e = 0; e < PER; ++e) {
+                float v = acc[q][r][e];
+                auto f = [](uint32_t u) { return __uint_as_float(u); };
+                if constexpr (CL <= 4) v += f(lane_xor<4>(__float_as_uint(v)));
+                v += f(lane_xor<8>(__float_as_uint(v)));
+                const LanePair p = lane_pair<16>(__float_as_uint(v));
+                v = f(p.low) + f(p.high);
+                const LanePair z = lane_pair<32>(__float_as_uint(v));
+                v = f(z.low) + f(z.high);
+                if (rl == 0) red[wid][q][r][cl * PER + e] = v;
+            }
+    __syncthreads();
+    for (int i = tid; i < MR * kFewColumns; i += 64 * NW) {
+        const int r = i / kFewColumns, at = i % kFewColumns;
+        const int64_t col = (int64_t)group * kFewColumns + at;
+        if (r >= a.m) break;
+        float v[MATS];
+#pragma unroll
+        for (int q = 0; q < MATS; ++q) {
+            v[q] = red[0][q][r][at];
+#pragma unroll
+            for (int w = 1; w < NW; ++w) v[q] += red[w][q][r][at];
+        }
+        if constexpr (MATS == 2) {
+            float value, slope;
+            activate<ACT, true>(v[0], value, slope);
+            if (col < a.cols) a.h[r * (int64_t)a.cols + col] = value * v[MATS - 1];
+        } else if (col < (a.cols + 16 / (BF ? 2 : 4) - 1) / (16 / (BF ? 2 : 4)) * (16 / (BF ? 2 : 4))) {
+            const float out = col < a.cols ? v[0] : 0.f;   // (zeros to the next 16-byte boundary)
+            if constexpr (BF) ((uint16_t *)a.y)[r * a.ld_y + col] = bf16_rne(out);
+            else ((float *)a.y)[r * a.ld_y + col] = out;
+        }
+    }
+}
+
 // ------------------------------------------------------------------ host
 int64_t up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
 
@@ -979,7 +1100,7 @@ struct Plan {
         }
         if (pack_wd) wd = packed(f, o);
         if (!backward) {
-            h = take(fp() * m * 2 * (low_y ? 2 : pl));
+            h = take(std::max(fp() * m * 2 * (low_y ? 2 : pl), m <= kFewRows ? m * f * 4 : 0));
             Job j;
             gate = choose(bf16 ? kGateBf16 : kGateF32, &j, 1, false, [&](const Shape &e, Job *x) { *x = {tiles(m, f, e.bn, e.bm), (d + bk - 1) / bk, 0}; });
             down = choose(bf16 ? kOutBf16 : kOutF32, &j, 1, true,
@@ -1179,8 +1300,35 @@ struct Saved {
     }
 };
 
+// Few rows that keep nothing; longer sums than these would have too few workgroups for themselves.  x 1,024 x 4,096 x 1,024 in
+// bf16: 1 row 12 us, 4 23, 8 37, in tiles 24; in fp32, whose tiles need the weights in planes: 22, 28, 37 and 65.
+bool few_rows(const GatedArgs &x) { return x.m <= (x.bf16 ? 4 : kFewRows) && !x.saved && x.d <= 16384 && x.f <= 16384; }
+
+template <int PL, int MR, int ACT>
+void forward_few(const GatedArgs &x, hipStream_t s) {
+    constexpr bool BF = PL == 1;
+    float *h = (float *)x.workspace;
+    {
+        KernelTimer t("gated_few", s);
+        const FewArgs a = {x.x, x.ld_x, x.wg, x.wu, x.ld_wg, x.ld_wu, (int32_t)x.m, (int32_t)x.d, (int32_t)x.f, h, nullptr, 0};
+        hipLaunchKernelGGL((k_gated_few<BF, !BF, MR, 2, ACT>), dim3((unsigned)(up(x.f, kFewColumns) / kFewColumns)), dim3(512), 0, s, a);
+    }
+    {
+        KernelTimer t("gated_few_down", s);
+        const FewArgs a = {h, x.f, x.wd, nullptr, x.ld_wd, 0, (int32_t)x.m, (int32_t)x.f, (int32_t)x.d_out, nullptr, x.y, x.ld_y};
+        hipLaunchKernelGGL((k_gated_few<BF, true, MR, 1, 0>), dim3((unsigned)(up(x.d_out, kFewColumns) / kFewColumns)), dim3(1024), 0, s, a);
+    }
+    GNNAV_HIP(hipGetLastError());
+}
+
 template <int PL, int ACT>
 void forward(const GatedArgs &x, hipStream_t s) {
+    if (few_rows(x)) {
+        if (x.m == 1) return forward_few<PL, 1, ACT>(x, s);
+        if (x.m == 2) return forward_few<PL, 2, ACT>(x, s);
+        if (x.m <= 4) return forward_few<PL, 4, ACT>(x, s);
+        if constexpr (PL == 3) return forward_few<PL, kFewRows, ACT>(x, s);
+    }
     const Plan p(x, false);
     char *ws = (char *)x.workspace;
     auto at = [&](bool packed, size_t offset) { return packed ? ws + offset : nullptr; };

@@ -120,7 +120,8 @@ def check(G, x, wg, wu, wd, dy, act, dtype, grads=("dx", "dwg", "dwu", "dwd"), r
 
 
 SHAPES = [(1, 1, 1, 1), (1, 8, 16, 8), (2, 5, 3, 7), (3, 40, 72, 41), (7, 64, 130, 16), (17, 100, 33, 9), (33, 31, 96, 64),
-          (64, 128, 128, 128), (65, 72, 200, 5), (130, 602, 257, 41), (200, 33, 64, 300), (257, 16, 520, 129), (1000, 24, 40, 8)]
+          (64, 128, 128, 128), (65, 72, 200, 5), (130, 602, 257, 41), (200, 33, 64, 300), (257, 16, 520, 129), (1000, 24, 40, 8),
+          (1, 1100, 2300, 70), (4, 2050, 1025, 33), (5, 64, 96, 24), (8, 40, 1030, 9), (9, 1024, 70, 16)]
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
@@ -149,6 +150,16 @@ def test_large_tiles(G, m, d, f, o, dtype):
     """Enough rows and columns for the larger tiles and for sums that are cut; ragged ones among them."""
     say("gated large", m, d, f, o, dtype)
     check(G, *block(m, d, f, o, dtype, 11), "silu", dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_strides_of_the_weights(G, dtype):
+    """Every matrix has a stride of its own, Wg and Wu too; rows and outputs in views of wider buffers."""
+    say("gated strides", dtype)
+    for m in (2, 70, 600):
+        x, wg, wu, wd, dy = block(m, 72, 136, 40, dtype, 3, extra=2)
+        assert wg.stride(0) != wu.stride(0) != wd.stride(0)
+        check(G, x, wg, wu, wd, dy, "silu", dtype)
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
