@@ -69,6 +69,19 @@ __device__ __forceinline__ void activate(float a, float &value, float &slope) {
     }
 }
 
+// The three bf16 parts of fp32 values, each rounded to nearest (bf16split.hpp's are cut): the second is then below 2^-9 of the
+// value and the third below 2^-18, and what six products leave out below 2^-26 of theirs.  A value that would round to
+// infinity is cut.
+__device__ __forceinline__ void parts_of(float x0, float x1, uint32_t (&q)[3]) {
+    q[0] = bf16_pair(x0, x1);
+    const uint32_t u0 = __float_as_uint(x0), u1 = __float_as_uint(x1);
+    if ((u0 & 0x7fffffffu) >= 0x7f7f8000u) q[0] = (q[0] & 0xffff0000u) | (u0 >> 16);
+    if ((u1 & 0x7fffffffu) >= 0x7f7f8000u) q[0] = (q[0] & 0xffffu) | (u1 & 0xffff0000u);
+    const float r0 = x0 - __uint_as_float(q[0] << 16), r1 = x1 - __uint_as_float(q[0] & 0xffff0000u);
+    q[1] = bf16_pair(r0, r1);
+    q[2] = bf16_pair(r0 - __uint_as_float(q[1] << 16), r1 - __uint_as_float(q[1] & 0xffff0000u));
+}
+
 // What copies read past the end of a sum.
 __device__ const u32x4x kZeros = {0, 0, 0, 0};
 
@@ -127,11 +140,16 @@ __global__ void __launch_bounds__(256) k_gated_pack(const PackJobs jobs) {
                     x[4 + e] = col + 4 + e < d ? hi[e] : 0.f;
                 }
             }
-            bf16x8 p1, p2, p3;
-            split3(x, p1, p2, p3);
-            tile[0][lc][lr] = __builtin_bit_cast(u32x4x, p1);
-            tile[PL - 2][lc][lr] = __builtin_bit_cast(u32x4x, p2);
-            tile[PL - 1][lc][lr] = __builtin_bit_cast(u32x4x, p3);
+            u32x4x part[3];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                uint32_t q[3];
+                parts_of(x[2 * e], x[2 * e + 1], q);
+#pragma unroll
+                for (int i = 0; i < 3; ++i) part[i][e] = q[i];
+            }
+#pragma unroll
+            for (int i = 0; i < PL; ++i) tile[i][lc][lr] = part[i];
         }
     }
     __syncthreads();
@@ -166,6 +184,9 @@ struct Product {
     int32_t f;
     f32x4x *a, *b;
     u32x4x *h;
+    const float *x, *wg;         // fp32's ReLU that keeps a: the operands of a, their strides and columns
+    int64_t ld_x, ld_wg;
+    int32_t d;
     int64_t h_plane, second;     // chunks of a plane; from da to db
     int64_t low;                 // bf16: from the values to their second parts (0: none are kept)
     u32x4x *h2;                  // da and db, bf16: h in two parts (nullable)
@@ -179,14 +200,15 @@ struct Product {
     int64_t split_stride;        // float4s
 };
 
-// Wave grid WGM x WGN, each wavefront WMF x WNF MFMA blocks of 32 x 32; BK summed elements per stage, three stages in LDS.
-template <int PL, int WMF, int WNF, int WGM, int WGN>
+// Wave grid WGM x WGN, each wavefront WMF x WNF MFMA blocks of 32 x 32; BK summed elements per stage, ST stages in LDS (small
+// tiles, whose steps are shorter than a copy's way, take more).
+template <int PL, int WMF, int WNF, int WGM, int WGN, int ST_ = 3>
 struct Tile {
     static constexpr int BK = PL == 1 ? 32 : 16;
     static constexpr int NW = WGM * WGN, BM = 32 * WMF * WGM, BN = 32 * WNF * WGN;
     static constexpr int APC = BM * BK / 8, BPC = BN * BK / 8;   // chunks of a plane of a stage
     static constexpr int STAGE = PL * (APC + BPC);
-    static constexpr int ST = 3, LDS = ST * STAGE;
+    static constexpr int ST = ST_, LDS = ST * STAGE;
     static_assert(APC % 64 == 0 && BPC % 64 == 0, "whole wavefront copies");
 };
 
@@ -224,27 +246,22 @@ template <int PL>
 __device__ __forceinline__ void store_chunks(u32x4x *to, int64_t plane, int64_t rows, int32_t chunk, int32_t chunks, int64_t n,
                                              int h, const float (&x)[16]) {
 #pragma unroll
-    for (int pl = 0; pl < PL; ++pl)
+    for (int g = 0; g < 4; g += 2) {
+        uint32_t w[2][2][3];
 #pragma unroll
-        for (int g = 0; g < 4; g += 2) {
-            uint32_t w[2][2];
+        for (int i = 0; i < 2; ++i)
 #pragma unroll
-            for (int i = 0; i < 2; ++i)
+            for (int j = 0; j < 2; ++j) {
+                const float f0 = x[4 * (g + i) + 2 * j], f1 = x[4 * (g + i) + 2 * j + 1];
+                if constexpr (PL == 1) w[i][j][0] = bf16_pair(f0, f1);
+                else parts_of(f0, f1, w[i][j]);
+            }
 #pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    const float f0 = x[4 * (g + i) + 2 * j], f1 = x[4 * (g + i) + 2 * j + 1];
-                    if constexpr (PL == 1) {
-                        w[i][j] = bf16_pair(f0, f1);
-                    } else {
-                        uint16_t q0[3], q1[3];
-                        split3_bits(f0, q0[0], q0[1], q0[2]);
-                        split3_bits(f1, q1[0], q1[1], q1[2]);
-                        w[i][j] = (uint32_t)q0[pl] | ((uint32_t)q1[pl] << 16);
-                    }
-                }
-            const u32x4x v = join_chunk(w[0][0], w[0][1], w[1][0], w[1][1]);
+        for (int pl = 0; pl < PL; ++pl) {
+            const u32x4x v = join_chunk(w[0][0][pl], w[0][1][pl], w[1][0][pl], w[1][1][pl]);
             if (n < rows && chunk + g + h < chunks) to[pl * plane + (int64_t)(chunk + g + h) * rows + n] = v;
         }
+    }
 }
 
 // ... and what bf16 leaves of the values, in bf16.
@@ -264,9 +281,9 @@ __device__ __forceinline__ void store_low(u32x4x *to, int64_t rows, int32_t chun
 // 256 bytes of distinct banks); one whose rows are lies in blocks of 8 of them, chunk by chunk, the two halves of a block
 // exchanged by the chunk (32 lanes of a transposing read take 256 bytes of distinct banks).  Both copy whole runs from
 // row-major and from chunk-major memory.  STRIDE: chunks from a stage to the next.
-template <int PL_, int WMF_, int WNF_, int WGM_, int WGN_, bool AT_, bool BT_, bool DUAL_, int STRIDE_ = Tile<PL_, WMF_, WNF_, WGM_, WGN_>::STAGE>
+template <int PL_, int WMF_, int WNF_, int WGM_, int WGN_, int ST_, bool AT_, bool BT_, bool DUAL_, int STRIDE_ = Tile<PL_, WMF_, WNF_, WGM_, WGN_>::STAGE>
 struct Feed {
-    using C = Tile<PL_, WMF_, WNF_, WGM_, WGN_>;
+    using C = Tile<PL_, WMF_, WNF_, WGM_, WGN_, ST_>;
     static constexpr int PL = PL_, WMF = WMF_, WNF = WNF_, WGM = WGM_, WGN = WGN_, STRIDE = STRIDE_;
     static constexpr bool AT = AT_, BT = BT_, DUAL = DUAL_;
     static constexpr int BK = C::BK, CK = BK / 8, APC = C::APC, BPC = C::BPC, BN = C::BN, INSTR = C::STAGE / 64, IN = (INSTR + C::NW - 1) / C::NW;
@@ -468,13 +485,22 @@ __device__ __forceinline__ void tile_sum(F &feed, const Sum &sum, int32_t T, u32
     };
     // Makes stage t readable: its copies are done, everywhere; those of the stage after it may not be.
     auto advance = [&](int32_t t) __attribute__((always_inline)) {
-        const int then = whose(t + 1);
-        if (then == kOwn) wait_vm<IN *(ST - 2)>();
-        else if (NIN > 0 && then == kNext) wait_vm<NIN *(ST - 2)>();
-        else wait_vm<0>();
+        if constexpr (ST == 3) {
+            const int then = whose(t + 1);
+            if (then == kOwn) wait_vm<IN>();
+            else if (NIN > 0 && then == kNext) wait_vm<NIN>();
+            else wait_vm<0>();
+        } else {
+            const int32_t behind = T - 1 - t;   // stages that may be on their way
+            if (behind >= ST - 2) wait_vm<IN *(ST - 2)>();
+            else if (ST > 5 && behind == 3) wait_vm<IN * 3>();
+            else if (ST > 4 && behind == 2) wait_vm<IN * 2>();
+            else if (behind == 1) wait_vm<IN>();
+            else wait_vm<0>();
+        }
         lds_barrier();
     };
-    static_assert(ST == 3 && (BK == 16 || BK == 32), "loop below");
+    static_assert(ST >= 3 && ST <= 6 && (ST == 3 || NIN == 0) && IN * (ST - 2) < 64 && (BK == 16 || BK == 32), "the waits and the loop below");
     auto next = [](int stage) { return stage + 1 == ST ? 0 : stage + 1; };
     // One fragment set is multiplied while the next one is read, across the barrier between two stages.  Once
     // stage t is readable, stage t + ST - 1 is copied into the one read before it, over the products up to the next barrier.
@@ -542,10 +568,55 @@ __device__ __forceinline__ void tile_sum(F &feed, const Sum &sum, int32_t T, u32
     while (t < T) round(t, std::false_type());
 }
 
+// ReLU's slope jumps at 0: where the rounding of a sum in fp32 decides which side a is on, da is 0 instead of a whole term, or the
+// other way round.  Values within 2^-17 of the largest of the lane's (all of one row of x) are summed again in 64 bits by the
+// whole wavefront, some 1 in 10^5 of them; the errors of a are below 2^-19 of it up to some 10,000 columns.  A 0 is one of them,
+// unless it comes from zeros: the row's values are all 0, or the column's are in 8 or more rows and no other.  Without it 1 of 5.6 million signs of a 1,362 x 333 x 4,096 block is wrong, which is 6e-4 of
+// dWg's norm; a 3,000 x 1,024 x 2,048 block's h takes 180 us with it, SiLU's 173.
+template <int WA, int WNF>
+__device__ __forceinline__ void sure_signs(const Product &a, int32_t c0, int64_t n, int j, int h, f32x16x (&acc)[2 * WA][WNF]) {
+    float most = 0.f;
+#pragma unroll
+    for (int i = 0; i < WA; ++i)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) most = fmaxf(most, fabsf(acc[i][j][r]));
+    most *= 0x1p-17f;
+#pragma unroll
+    for (int i = 0; i < WA; ++i) {
+        uint32_t near = 0;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            const float v = fabsf(acc[i][j][r]);
+            const bool live = n < a.n && c0 + 32 * i + 8 * (r / 4) + 4 * h + r % 4 < a.f;
+            bool close = live && v < most;
+            if (__ballot(close && v == 0.f)) {
+                const uint64_t other = __ballot(live && !(v == 0.f)), zero = __ballot(live && v == 0.f);
+                const uint32_t others = (uint32_t)(other >> (32 * h)), zeros = (uint32_t)(zero >> (32 * h));   // of the column
+                close = close && (v > 0.f || others || __builtin_popcount(zeros) < 8);
+            }
+            near |= (uint32_t)close << r;
+        }
+        uint64_t lanes;
+        while ((lanes = __ballot(near != 0)) != 0) {
+            const int from = __builtin_ctzll(lanes), r = __builtin_ctz(__builtin_amdgcn_readlane(near, from));
+            const int64_t row = n - (threadIdx.x & 31) + (from & 31);
+            const float *const x = a.x + row * a.ld_x, *const w = a.wg + c0 + 32 * i + 8 * (r / 4) + 4 * (from >> 5) + r % 4;
+            double sum = 0;
+            for (int32_t k = threadIdx.x & 63; k < a.d; k += 64) sum = fma((double)x[k], (double)w[k * a.ld_wg], sum);
+#pragma unroll
+            for (int q = 32; q > 0; q /= 2) sum += __shfl_xor(sum, q);
+            const bool mine = (int)(threadIdx.x & 63) == from;
+#pragma unroll
+            for (int q = 0; q < 16; ++q) acc[i][j][q] = mine && q == r ? (float)sum : acc[i][j][q];
+            near &= mine ? near - 1 : ~0u;
+        }
+    }
+}
+
 // h = act(x Wg) * (x Wu) for one tile from both sums, kept for the product with Wd, and a and b where they are kept.  WA: blocks
 // of a wavefront along f.
 template <int PL, int WA, int WNF, int WGM, int WGN, int ACT>
-__device__ __forceinline__ void gate_store(const Product &a, int64_t m0, int64_t n0, const f32x16x (&acc)[2 * WA][WNF]) {
+__device__ __forceinline__ void gate_store(const Product &a, int64_t m0, int64_t n0, f32x16x (&acc)[2 * WA][WNF]) {
     const int lane = threadIdx.x & 63, wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5, lr = lane & 31;
     const int32_t mw = (int32_t)m0 + wid / WGN * (32 * WA);
     const int64_t nw = n0 + wid % WGN * (32 * WNF);
@@ -554,6 +625,8 @@ __device__ __forceinline__ void gate_store(const Product &a, int64_t m0, int64_t
 #pragma unroll
     for (int j = 0; j < WNF; ++j) {
         const int64_t n = nw + 32 * j + lr;
+        if constexpr (PL == 3 && ACT == GNNAV_ACT_RELU)
+            if (a.a) sure_signs<WA, WNF>(a, mw, n, j, h, acc);
 #pragma unroll
         for (int i = 0; i < WA; ++i) {
             float x[16];
@@ -646,7 +719,7 @@ __device__ __forceinline__ void dgate_store(const Product &a, int64_t m0, int64_
 }
 
 // Tile `id` of a product that goes to the caller, or to parts.
-template <int PL, int WMF, int WNF, int WGM, int WGN, bool AT, bool BT>
+template <int PL, int WMF, int WNF, int WGM, int WGN, int ST, bool AT, bool BT>
 __device__ __forceinline__ void out_tile(const Product &a, int32_t id, u32x4x *S) {
     const int lane = threadIdx.x & 63, wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5, lr = lane & 31;
     int32_t split, mt, nt;
@@ -654,7 +727,7 @@ __device__ __forceinline__ void out_tile(const Product &a, int32_t id, u32x4x *S
     const int64_t m0 = (int64_t)mt * (32 * WMF * WGM), n0 = (int64_t)nt * (32 * WNF * WGN);
     const int32_t s0 = split * a.split_steps, T = std::max(0, std::min(a.split_steps, a.s.segments * a.s.steps - s0));
     f32x16x acc[WMF][WNF];
-    Feed<PL, WMF, WNF, WGM, WGN, AT, BT, false> feed;
+    Feed<PL, WMF, WNF, WGM, WGN, ST, AT, BT, false> feed;
     int ready = 0;
     Nothing nothing;
     if (T > 0) feed.start(a.s, m0, n0, s0);
@@ -675,57 +748,75 @@ __device__ __forceinline__ void out_tile(const Product &a, int32_t id, u32x4x *S
 }
 
 // A workgroup takes tile after tile, the next one's first copies under way while one's results are formed and stored.
-template <int PL, int WMF, int WNF, int WGM, int WGN, int ACT>
+// (Tiles of more than three stages are for launches that have one a workgroup.)
+template <int PL, int WMF, int WNF, int WGM, int WGN, int ST, int ACT>
 __global__ void __launch_bounds__(64 * WGM * WGN, 2) k_gated_gate(const Product a, int32_t ids) {
     constexpr int WA = WMF / 2;
     constexpr int64_t AM = 32 * WA * WGM, BN = 32 * WNF * WGN;
-    __shared__ u32x4x S[Tile<PL, WMF, WNF, WGM, WGN>::LDS];
+    __shared__ u32x4x S[Tile<PL, WMF, WNF, WGM, WGN, ST>::LDS];
     int32_t split, mt, nt, id = blockIdx.x;
     if (!tile_of(a, id, split, mt, nt)) return;
-    using F = Feed<PL, WMF, WNF, WGM, WGN, true, false, true>;
+    using F = Feed<PL, WMF, WNF, WGM, WGN, ST, true, false, true>;
     F feed;
     feed.start(a.s, mt * AM, nt * BN, 0);
     f32x16x acc[WMF][WNF];
     int ready = 0, primed = 0;
-    while (true) {
-        int32_t m2 = 0, n2 = 0;
-        id += gridDim.x;
-        const bool more = id < ids && tile_of(a, id, split, m2, n2);
-        const Next<F> next = {m2 * AM, n2 * BN, more ? std::min(a.s.steps, 2) : 0};
-        tile_sum(feed, a.s, a.s.steps, S, acc, ready, primed, true, next, feed, a.s);
+    if constexpr (ST > 3) {
+        const Nothing nothing;
+        tile_sum(feed, a.s, a.s.steps, S, acc, ready, 0, false, nothing, feed, a.s);
         gate_store<PL, WA, WNF, WGM, WGN, ACT>(a, mt * AM, nt * BN, acc);
-        if (!more) break;
-        primed = next.stages;
-        mt = m2;
-        nt = n2;
+    } else {
+        while (true) {
+            int32_t m2 = 0, n2 = 0;
+            id += gridDim.x;
+            const bool more = id < ids && tile_of(a, id, split, m2, n2);
+            const Next<F> next = {m2 * AM, n2 * BN, more ? std::min(a.s.steps, 2) : 0};
+            tile_sum(feed, a.s, a.s.steps, S, acc, ready, primed, true, next, feed, a.s);
+            gate_store<PL, WA, WNF, WGM, WGN, ACT>(a, mt * AM, nt * BN, acc);
+            if (!more) break;
+            primed = next.stages;
+            mt = m2;
+            nt = n2;
+        }
     }
 }
-template <int PL, int WMF, int WNF, int WGM, int WGN>
+template <int PL, int WMF, int WNF, int WGM, int WGN, int ST>
 __global__ void __launch_bounds__(64 * WGM * WGN, 2) k_gated_down(const Product a) {
-    __shared__ u32x4x S[Tile<PL, WMF, WNF, WGM, WGN>::LDS];
-    out_tile<PL, WMF, WNF, WGM, WGN, true, false>(a, blockIdx.x, S);
+    __shared__ u32x4x S[Tile<PL, WMF, WNF, WGM, WGN, ST>::LDS];
+    out_tile<PL, WMF, WNF, WGM, WGN, ST, true, false>(a, blockIdx.x, S);
 }
 // fp32 takes tile after tile too; bf16, whose three sums leave no registers for the next tile's copies, one: the copies of dh's sum
 // follow those of a and b.
-template <int PL, int WA, int WNF, int WGM, int WGN, int ACT>
+template <int PL, int WA, int WNF, int WGM, int WGN, int ST, int ACT>
 __global__ void __launch_bounds__(64 * WGM * WGN, 2) k_gated_dgate(const Product a, const Sum again, int32_t ids) {
     constexpr int64_t AM = 32 * WA * WGM, BN = 32 * WNF * WGN;
-    using C = Tile<PL, PL == 1 ? 2 * WA : WA, WNF, WGM, WGN>;
+    using C = Tile<PL, PL == 1 ? 2 * WA : WA, WNF, WGM, WGN, ST>;
     __shared__ u32x4x S[C::LDS];
     int32_t split, mt, nt, id = blockIdx.x;
     if (!tile_of(a, id, split, mt, nt)) return;
-    using F = Feed<PL, WA, WNF, WGM, WGN, false, false, false, C::STAGE>;
+    using F = Feed<PL, WA, WNF, WGM, WGN, ST, false, false, false, C::STAGE>;
     F feed;
     f32x16x ab[PL == 1 ? 2 * WA : 1][PL == 1 ? WNF : 1], acc[WA][WNF];
     int ready = 0, primed = 0;
+    const Nothing nothing;
     if constexpr (PL == 1) {
-        using A = Feed<PL, 2 * WA, WNF, WGM, WGN, true, false, true>;
+        using A = Feed<PL, 2 * WA, WNF, WGM, WGN, ST, true, false, true>;
         A first;
         first.start(again, mt * AM, nt * BN, 0);
-        const Next<F> dh = {mt * AM, nt * BN, std::min(a.s.steps, 2)};
-        tile_sum(first, again, again.steps, S, ab, ready, 0, false, dh, feed, a.s);
-        const Nothing nothing;
-        tile_sum(feed, a.s, a.s.steps, S, acc, ready, dh.stages, false, nothing, feed, a.s);
+        if constexpr (ST == 3) {
+            const Next<F> dh = {mt * AM, nt * BN, std::min(a.s.steps, 2)};
+            tile_sum(first, again, again.steps, S, ab, ready, 0, false, dh, feed, a.s);
+            primed = dh.stages;
+        } else {
+            tile_sum(first, again, again.steps, S, ab, ready, 0, false, nothing, first, again);
+            lds_barrier();   // (the last fragments are read)
+            feed.start(a.s, mt * AM, nt * BN, 0);
+        }
+        tile_sum(feed, a.s, a.s.steps, S, acc, ready, primed, false, nothing, feed, a.s);
+        dgate_store<PL, WA, WNF, WGM, WGN, ACT>(a, mt * AM, nt * BN, ab, acc);
+    } else if constexpr (ST > 3) {
+        feed.start(a.s, mt * AM, nt * BN, 0);
+        tile_sum(feed, a.s, a.s.steps, S, acc, ready, 0, false, nothing, feed, a.s);
         dgate_store<PL, WA, WNF, WGM, WGN, ACT>(a, mt * AM, nt * BN, ab, acc);
     } else {
         feed.start(a.s, mt * AM, nt * BN, 0);
@@ -744,14 +835,14 @@ __global__ void __launch_bounds__(64 * WGM * WGN, 2) k_gated_dgate(const Product
     }
 }
 // dx and the weights' gradients in one launch: workgroups below `w_at` take dx's tiles, below `d_at` those of dWg and dWu.
-template <int PL, int WMF, int WNF, int WGM, int WGN>
+template <int PL, int WMF, int WNF, int WGM, int WGN, int ST>
 __global__ void __launch_bounds__(64 * WGM * WGN, 2) k_gated_grads(const Product x, const Product w, const Product d, int32_t w_at,
                                                                    int32_t d_at) {
-    __shared__ u32x4x S[Tile<PL, WMF, WNF, WGM, WGN>::LDS];
+    __shared__ u32x4x S[Tile<PL, WMF, WNF, WGM, WGN, ST>::LDS];
     const int32_t id = blockIdx.x;
-    if (id < w_at) out_tile<PL, WMF, WNF, WGM, WGN, false, false>(x, id, S);
-    else if (id < d_at) out_tile<PL, WMF, WNF, WGM, WGN, true, true>(w, id - w_at, S);
-    else out_tile<PL, WMF, WNF, WGM, WGN, true, true>(d, id - d_at, S);
+    if (id < w_at) out_tile<PL, WMF, WNF, WGM, WGN, ST, false, false>(x, id, S);
+    else if (id < d_at) out_tile<PL, WMF, WNF, WGM, WGN, ST, true, true>(w, id - w_at, S);
+    else out_tile<PL, WMF, WNF, WGM, WGN, ST, true, true>(d, id - d_at, S);
 }
 
 // The sum of the splits' parts, in their order.  A launch takes up to three products.
@@ -1200,18 +1291,18 @@ struct Packer {
     }
 };
 
-#define GNNAV_TILES(PL, WHICH, L)                        \
-    do {                                                 \
-        if constexpr (PL == 1) {                         \
-            if (WHICH == kLarge) L(1, 4, 2, 2, 4);       \
-            else if (WHICH == kWide) L(1, 2, 2, 2, 4);   \
-            else if (WHICH == kMedium) L(1, 1, 2, 2, 2); \
-            else L(1, 2, 1, 1, 2);                       \
-        } else {                                         \
-            if (WHICH == kWide) L(3, 2, 2, 2, 2);        \
-            else if (WHICH == kMedium) L(3, 1, 2, 2, 2); \
-            else L(3, 2, 1, 1, 2);                       \
-        }                                                \
+#define GNNAV_TILES(PL, WHICH, L)                           \
+    do {                                                    \
+        if constexpr (PL == 1) {                            \
+            if (WHICH == kLarge) L(1, 4, 2, 2, 4, 3);       \
+            else if (WHICH == kWide) L(1, 2, 2, 2, 4, 3);   \
+            else if (WHICH == kMedium) L(1, 1, 2, 2, 2, 4); \
+            else L(1, 2, 1, 1, 2, 6);                       \
+        } else {                                            \
+            if (WHICH == kWide) L(3, 2, 2, 2, 2, 3);        \
+            else if (WHICH == kMedium) L(3, 1, 2, 2, 2, 4); \
+            else L(3, 2, 1, 1, 2, 6);                       \
+        }                                                   \
     } while (0)
 
 // Workgroups of a launch that takes tile after tile: `each` a unit, whole rounds over the XCDs.
@@ -1221,31 +1312,32 @@ unsigned places_of(const Product &a, int each, hipStream_t s) {
 template <int PL, int ACT>
 void run_gate(const Product &p, int which, hipStream_t s) {
     KernelTimer t("gated_gate", s);
-#define GNNAV_L(A, B, C, D, EACH)                                                                                       \
-    hipLaunchKernelGGL((k_gated_gate<PL, A, B, C, D, ACT>), dim3(places_of(p, EACH, s)), dim3(64 * C * D), 0, s, p, (int32_t)ids_of(p))
+#define GNNAV_L(A, B, C, D, ST, EACH)                                                                                   \
+    hipLaunchKernelGGL((k_gated_gate<PL, A, B, C, D, ST, ACT>), dim3(ST == 3 ? places_of(p, EACH, s) : ids_of(p)), dim3(64 * C * D), 0, s, p, \
+                       (int32_t)ids_of(p))
     if constexpr (PL == 1) {
-        if (which == kLarge) GNNAV_L(4, 2, 2, 4, 1);
-        else if (which == kMedium) GNNAV_L(2, 2, 2, 2, 3);
-        else GNNAV_L(2, 1, 1, 2, 6);
+        if (which == kLarge) GNNAV_L(4, 2, 2, 4, 3, 1);
+        else if (which == kMedium) GNNAV_L(2, 2, 2, 2, 3, 3);
+        else GNNAV_L(2, 1, 1, 2, 6, 0);
     } else {
-        if (which == kWide) GNNAV_L(2, 2, 2, 2, 2);
-        else GNNAV_L(2, 1, 1, 2, 4);
+        if (which == kWide) GNNAV_L(2, 2, 2, 2, 3, 2);
+        else GNNAV_L(2, 1, 1, 2, 6, 0);
     }
 #undef GNNAV_L
 }
 template <int PL, int ACT>
 void run_dgate(const Product &p, const Sum &again, int which, hipStream_t s) {
     KernelTimer t("gated_dgate", s);
-#define GNNAV_L(A, B, C, D, EACH)                                                                                       \
-    hipLaunchKernelGGL((k_gated_dgate<PL, A, B, C, D, ACT>), dim3(PL == 1 ? ids_of(p) : places_of(p, EACH, s)), dim3(64 * C * D), 0, s, p, again, \
-                       (int32_t)ids_of(p))
+#define GNNAV_L(A, B, C, D, ST)                                                                                         \
+    hipLaunchKernelGGL((k_gated_dgate<PL, A, B, C, D, ST, ACT>), dim3(PL == 1 || ST > 3 ? ids_of(p) : places_of(p, 2, s)), dim3(64 * C * D), 0, s, p, \
+                       again, (int32_t)ids_of(p))
     if constexpr (PL == 1) {
-        if (which == kLarge) GNNAV_L(2, 2, 2, 4, 1);
+        if (which == kLarge) GNNAV_L(2, 2, 2, 4, 3);
         else if (which == kMedium) GNNAV_L(1, 2, 2, 2, 3);
-        else GNNAV_L(1, 1, 2, 2, 4);
+        else GNNAV_L(1, 1, 2, 2, 6);
     } else {
-        if (which == kWide) GNNAV_L(2, 2, 2, 2, 2);
-        else GNNAV_L(1, 1, 2, 2, 4);
+        if (which == kWide) GNNAV_L(2, 2, 2, 2, 3);
+        else GNNAV_L(1, 1, 2, 2, 6);
     }
 #undef GNNAV_L
 }
@@ -1257,7 +1349,7 @@ void run_join(const Product &p, const Product &q, const Product &r, int tile, hi
     if (at == 0) return;
     KernelTimer t("gated_join", s);
     const unsigned grid = grid_for(at, 256, 4096);
-#define GNNAV_L(P, A, B, C, D) hipLaunchKernelGGL((k_gated_join<A, B, C, D>), dim3(grid), dim3(256), 0, s, j)
+#define GNNAV_L(P, A, B, C, D, ST) hipLaunchKernelGGL((k_gated_join<A, B, C, D>), dim3(grid), dim3(256), 0, s, j)
     GNNAV_TILES(PL, tile, GNNAV_L);
 #undef GNNAV_L
 }
@@ -1265,7 +1357,7 @@ template <int PL>
 void run_down(const Product &p, int tile, hipStream_t s) {
     {
         KernelTimer t("gated_down", s);
-#define GNNAV_L(P, A, B, C, D) hipLaunchKernelGGL((k_gated_down<P, A, B, C, D>), dim3(ids_of(p)), dim3(64 * C * D), 0, s, p)
+#define GNNAV_L(P, A, B, C, D, ST) hipLaunchKernelGGL((k_gated_down<P, A, B, C, D, ST>), dim3(ids_of(p)), dim3(64 * C * D), 0, s, p)
         GNNAV_TILES(PL, tile, GNNAV_L);
 #undef GNNAV_L
     }
@@ -1277,8 +1369,8 @@ void run_grads(const Product &x, const Product &w, const Product &d, int tile, h
     if (nx + nw + nd == 0) return;
     {
         KernelTimer t("gated_grads", s);
-#define GNNAV_L(P, A, B, C, D)                                                                                        \
-    hipLaunchKernelGGL((k_gated_grads<P, A, B, C, D>), dim3(nx + nw + nd), dim3(64 * C * D), 0, s, x, w, d, (int32_t)nx, \
+#define GNNAV_L(P, A, B, C, D, ST)                                                                                    \
+    hipLaunchKernelGGL((k_gated_grads<P, A, B, C, D, ST>), dim3(nx + nw + nd), dim3(64 * C * D), 0, s, x, w, d, (int32_t)nx, \
                        (int32_t)(nx + nw))
         GNNAV_TILES(PL, tile, GNNAV_L);
 #undef GNNAV_L
@@ -1354,6 +1446,11 @@ void forward(const GatedArgs &x, hipStream_t s) {
     g.f = (int32_t)x.f;
     g.a = saved.a;
     g.b = saved.b;
+    g.x = (const float *)x.x;
+    g.wg = (const float *)x.wg;
+    g.ld_x = x.ld_x;
+    g.ld_wg = x.ld_wg;
+    g.d = (int32_t)x.d;
     g.h = h;
     g.h_plane = plane;
     // (second parts always go to the workspace, behind the place that h has there)

@@ -41,8 +41,8 @@ def product(x, ex, w, ew, e):
     return x @ w, off
 
 
-def reference(x, wg, wu, wd, dy, act, dtype):
-    """{name: (value, tolerance)} of y, dx, dwg, dwu, dwd."""
+def reference(x, wg, wu, wd, dy, act, dtype, sides=False):
+    """{name: (value, tolerance)} of y, dx, dwg, dwu, dwd; `sides`: ReLU's slope is right however near a is to 0."""
     e = 2.0 ** -20 if dtype == "f32" else 0.0
     mid = HALF_STEP["bf16"] if dtype == "bf16" else 0.0
     a, ea = product(x, None, wg, None, e)
@@ -50,7 +50,7 @@ def reference(x, wg, wu, wd, dy, act, dtype):
     v, s = activation(a, act)
     near = 2.0 ** -20 * (np.abs(a) + 1)
     ev = 1.13 * ea + near
-    es = 0.8 * ea + near if act != "relu" else (np.abs(a) <= ea) * 1.0
+    es = 0.8 * ea + near if act != "relu" else (np.abs(a) <= (0.0 if sides else ea)) * 1.0
     h = v * b
     eh = np.abs(v) * eb + np.abs(b) * ev + (mid + U) * np.abs(h)
     out = {}
@@ -89,8 +89,8 @@ def saved_for(G, m, f, dtype):
     return torch.full((G.gated_ffn_saved(m, f, dtype),), 0xFF, dtype=torch.uint8, device="cuda")
 
 
-def check(G, x, wg, wu, wd, dy, act, dtype, grads=("dx", "dwg", "dwu", "dwd"), rows=None):
-    """Runs both passes and compares every output; `rows`: those of x and dy that are compared in y and dx."""
+def check(G, x, wg, wu, wd, dy, act, dtype, grads=("dx", "dwg", "dwu", "dwd"), sides=False):
+    """Runs both passes and compares every output."""
     m, d = x.shape
     f, o = wd.shape
     got = dict(y=empty(m, o, dtype))
@@ -106,7 +106,7 @@ def check(G, x, wg, wu, wd, dy, act, dtype, grads=("dx", "dwg", "dwu", "dwd"), r
         got["y"].copy_(alone)
         wide(got["y"]).copy_(wide(alone))
     G.sync()
-    want = reference(f64(x), f64(wg), f64(wu), f64(wd), f64(dy) if grads else None, act, dtype)
+    want = reference(f64(x), f64(wg), f64(wu), f64(wd), f64(dy) if grads else None, act, dtype, sides)
     got["alone"], want["alone"] = alone, want["y"]
     for n, t in got.items():
         value, tol = want[n]
@@ -130,6 +130,22 @@ def test_both_passes(G, m, d, f, o, dtype):
     act = ("silu", "gelu", "relu")[(m + f) % 3]
     say("gated", m, d, f, o, dtype, act)
     check(G, *block(m, d, f, o, dtype, m + d + f), act, dtype)
+
+
+@pytest.mark.parametrize("m,d,f,o", [(40, 64, 700, 24), (300, 333, 1000, 41), (3000, 130, 520, 70)])
+def test_relu_is_on_the_right_side_of_zero(G, m, d, f, o):
+    """Every hidden column has a row whose a nearly cancels, to less than what a sum in fp32 is off by; none is 0."""
+    import torch
+    x, wg, wu, wd, dy = block(m, d, f, o, "f32", 60)
+    at = np.arange(f) * 7 % m
+    x[:, d - 1] = 1.0 + x[:, d - 1].abs()
+    full = f64(x)
+    rest = np.einsum("cd,dc->c", full[at, :-1], f64(wg)[:-1])
+    wg[d - 1] = torch.from_numpy(-rest / full[at, -1]).to(wg)
+    a = np.einsum("cd,dc->c", full[at], f64(wg))
+    assert (a != 0).all() and (np.abs(a) < 2.0 ** -22 * np.abs(full[at]).max()).all()
+    say("gated relu sides", m, d, f, o)
+    check(G, x, wg, wu, wd, dy, "relu", "f32", sides=True)
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
