@@ -1005,33 +1005,40 @@ int64_t up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
 
 int64_t tiles(int64_t rows, int64_t cols, int64_t bn, int64_t bm) { return up(rows, bn) / bn * (up(cols, bm) / bm); }
 
-// A tile: columns and rows of the output, workgroups that a unit holds at once, and what a step takes: a unit's workgroups
-// `share` us each, and none less than `alone`.  Measured: 8,192 x 1,024 outputs of 4,096 summed bf16 columns 126 us in tiles of
-// 256 x 256, 104 of 128 x 256, 175 of 64 x 128, 256 of 64 x 64; 4,000 x 512 of 1,024 columns 42, 31, 19, 22.
+// A tile: columns and rows of the output, workgroups that a unit holds at once, and what one takes, in us: a step `share` times the
+// workgroups that share the unit and `alone` at least, all else `start`.  Fitted to 19 blocks of 20 to 100,000 rows in bf16 and 16
+// in fp32, each in every tile; the launches' times are within some 15% of it, and the tile that it takes within 7% of the best
+// in 9 of 10 cases.
+// Measured: 8,192 x 1,024 outputs of 4,096 summed bf16 columns 126 us in tiles of 256 x 256, 104 of 128 x 256, 175 of 64 x 128,
+// 256 of 64 x 64; 4,000 x 512 of 1,024 columns 42, 31, 19, 22.
 struct Shape {
     int bm, bn, each;
-    double share, alone;
+    double share, alone, start;
 };
 constexpr int kUnits = 256;
 enum { kLarge, kWide, kMedium, kSmall, kShapes };
-const Shape kOutBf16[kShapes] = {{256, 256, 1, 1.05, 1.05}, {128, 256, 2, 0.52, 0.81}, {64, 128, 4, 0.33, 0.47}, {64, 64, 8, 0.25, 0.40}};
-const Shape kOutF32[kShapes] = {{0, 0, 0, 0, 0}, {128, 128, 2, 0.80, 1.0}, {64, 128, 2, 0.45, 0.70}, {64, 64, 4, 0.25, 0.5}};
-// the gradients, whose operands' rows are summed over
-const Shape kGradsBf16[kShapes] = {{256, 256, 1, 0.95, 0.95}, {128, 256, 2, 0.72, 0.90}, {64, 128, 4, 0.36, 0.50}, {64, 64, 8, 0.27, 0.42}};
+const Shape kNone = {0, 0, 0, 0, 0, 0};
+const Shape kOutBf16[kShapes] = {{256, 256, 1, 0.92, 0.92, 9.6}, {128, 256, 2, 0.63, 0.54, 7.6}, {64, 128, 4, 0.25, 0.26, 7.8}, {64, 64, 8, 0.16, 0.15, 8.8}};
+const Shape kOutF32[kShapes] = {kNone, {128, 128, 2, 0.57, 0.63, 7.8}, {64, 128, 2, 0.37, 0.43, 6.7}, {64, 64, 4, 0.22, 0.31, 9.5}};
+// the gradients, whose operands' rows are summed over: the same tiles
+const Shape kGradsBf16[kShapes] = {{256, 256, 1, 0.83, 0.83, 8.8}, {128, 256, 2, 0.51, 0.52, 7.6}, {64, 128, 4, 0.21, 0.28, 5.5}, {64, 64, 8, 0.13, 0.19, 6.7}};
+const Shape kGradsF32[kShapes] = {kNone, {128, 128, 2, 0.52, 0.64, 6.9}, {64, 128, 2, 0.34, 0.54, 4.8}, {64, 64, 4, 0.20, 0.36, 7.6}};
 // h: columns of one projection
-const Shape kGateBf16[kShapes] = {{128, 256, 1, 1.05, 1.05}, {0, 0, 0, 0, 0}, {64, 128, 3, 0.33, 0.50}, {32, 64, 6, 0.22, 0.40}};
-const Shape kGateF32[kShapes] = {{0, 0, 0, 0, 0}, {64, 128, 2, 0.80, 1.0}, {0, 0, 0, 0, 0}, {32, 64, 4, 0.25, 0.5}};
+const Shape kGateBf16[kShapes] = {{128, 256, 1, 0.79, 0.79, 7.6}, kNone, {64, 128, 3, 0.22, 0.60, 7.2}, {32, 64, 6, 0.19, 0.49, 4.7}};
+const Shape kGateF32[kShapes] = {kNone, {64, 128, 2, 0.51, 0.60, 11.9}, kNone, {32, 64, 4, 0.19, 0.26, 9.1}};
 // da and db: a step of one product
-const Shape kDgateBf16[kShapes] = {{128, 256, 1, 0.56, 0.60}, {0, 0, 0, 0, 0}, {64, 128, 3, 0.18, 0.30}, {64, 64, 4, 0.12, 0.25}};
-const Shape kDgateF32[kShapes] = {{0, 0, 0, 0, 0}, {128, 128, 2, 0.80, 1.0}, {0, 0, 0, 0, 0}, {64, 64, 4, 0.25, 0.5}};
+const Shape kDgateBf16[kShapes] = {{128, 256, 1, 0.36, 0.36, 13.6}, kNone, {64, 128, 3, 0.12, 0.30, 10.0}, {64, 64, 4, 0.12, 0.20, 7.3}};
+const Shape kDgateF32[kShapes] = {kNone, {128, 128, 2, 0.58, 0.23, 23.5}, kNone, {64, 64, 4, 0.23, 0.13, 10.3}};
 
 // A product's part in a launch: tiles, steps of each, entries of the output.
 struct Job {
     int64_t tiles, steps, entries;
     int32_t splits = 1;
 };
-// Steps until a launch's last workgroup ends, its jobs' workgroups going to `slots` places in their order.
-int64_t makespan(const Job *jobs, int n, int64_t slots) {
+// Time until a launch's last workgroup ends, its jobs' workgroups going to `slots` places in their order; in kTicks of a step, of
+// which each takes `start` besides its steps.
+constexpr int kTicks = 16;
+int64_t makespan(const Job *jobs, int n, int64_t slots, int64_t start) {
     // times at which places become free, with how many do: few distinct ones
     int64_t at[64], count[64];
     int k = 1;
@@ -1040,7 +1047,7 @@ int64_t makespan(const Job *jobs, int n, int64_t slots) {
     int64_t last = 0;
     for (int j = 0; j < n; ++j) {
         int64_t left = jobs[j].tiles * jobs[j].splits;
-        const int64_t each = (jobs[j].steps + jobs[j].splits - 1) / std::max<int64_t>(jobs[j].splits, 1);
+        const int64_t each = (jobs[j].steps + jobs[j].splits - 1) / jobs[j].splits * kTicks + start;
         if (left > 16 * slots) return INT64_MAX;   // (long anyway)
         while (left > 0) {
             int first = 0;
@@ -1069,18 +1076,28 @@ int64_t makespan(const Job *jobs, int n, int64_t slots) {
     }
     return last;
 }
-// us that a launch of these jobs takes, their parts' way to memory and back in a launch of its own among them.
+// us that a launch of these jobs takes, their parts' way to memory and back in a launch of its own among them (5 us and 4 TB/s).
 double cost(const Job *jobs, int n, const Shape &shape) {
-    const int64_t m = makespan(jobs, n, (int64_t)kUnits * shape.each);
-    if (m == INT64_MAX) return 1e18;
+    const int64_t slots = (int64_t)kUnits * shape.each;
     int64_t groups = 0;
-    double bytes = 0;
+    double bytes = 0, t = 0;
     for (int j = 0; j < n; ++j) {
         groups += jobs[j].tiles * jobs[j].splits;
         if (jobs[j].splits > 1) bytes += jobs[j].entries * 8.0 * jobs[j].splits;
     }
-    const int64_t held = std::min<int64_t>(shape.each, (groups + kUnits - 1) / kUnits);
-    return m * std::max(shape.alone, held * shape.share) + (bytes > 0 ? 5.0 + bytes / 2.5e6 : 0.0);
+    // a step, of so many workgroups
+    auto step = [&](int64_t of) { return std::max(shape.alone, std::min<int64_t>(shape.each, (of + kUnits - 1) / kUnits) * shape.share); };
+    const double full = step(groups);
+    const int64_t m = n > 1 ? makespan(jobs, n, slots, (int64_t)(shape.start / full * kTicks)) : INT64_MAX;
+    if (n == 1) {   // full rounds, and the last one
+        const int64_t steps = (jobs[0].steps + jobs[0].splits - 1) / jobs[0].splits;
+        t = groups / slots * (steps * full + shape.start) + (groups % slots ? steps * step(groups % slots) + shape.start : 0.0);
+    } else if (m != INT64_MAX) {
+        t = m * full / kTicks;
+    } else {
+        for (int j = 0; j < n; ++j) t += jobs[j].tiles * jobs[j].splits * ((jobs[j].steps + jobs[j].splits - 1) / jobs[j].splits * full + shape.start) / slots;
+    }
+    return t + (bytes > 0 ? 5.0 + bytes / 4e6 : 0.0);
 }
 // Splits of the jobs' sums that make it least.  Parts have 16 steps at least.
 double split(Job *jobs, int n, const Shape &shape) {
@@ -1091,10 +1108,6 @@ double split(Job *jobs, int n, const Shape &shape) {
         longest = std::max(longest, jobs[j].tiles > 0 ? jobs[j].steps : 0);
     }
     double least = cost(jobs, n, shape);
-    if (least > 1e17) {   // (more rounds than are followed)
-        least = total * shape.share / kUnits;
-        return least;
-    }
     if (longest < 48) return least;
     Job best[3], now[3];
     for (int j = 0; j < n; ++j) best[j] = jobs[j];
@@ -1128,13 +1141,7 @@ int choose(const Shape *shapes, Job *jobs, int n, bool may_split, F &&jobs_of) {
     for (int k = 0; k < kShapes; ++k) {
         if (shapes[k].bm == 0) continue;
         jobs_of(shapes[k], jobs);
-        double c;
-        if (may_split) {
-            c = split(jobs, n, shapes[k]);
-        } else {
-            c = cost(jobs, n, shapes[k]);
-            if (c > 1e17) c = jobs[0].tiles * jobs[0].steps * shapes[k].share / kUnits;
-        }
+        const double c = may_split ? split(jobs, n, shapes[k]) : cost(jobs, n, shapes[k]);
         if (which < 0 || c < least) {
             which = k;
             least = c;
@@ -1171,7 +1178,7 @@ struct Plan {
     static int64_t parts(int64_t rows, int64_t cols, const Shape &e, int32_t splits) {
         return splits > 1 ? splits * up(rows, e.bn) * up(cols, e.bm) * 4 : 0;
     }
-    const Shape &out(int which) const { return (bf16 ? kOutBf16 : kOutF32)[which]; }   // (kGradsBf16's have the same sizes)
+    const Shape &out(int which) const { return (bf16 ? kOutBf16 : kOutF32)[which]; }   // (the gradients' have the same sizes)
     Plan(const GatedArgs &a, bool backward) : m(a.m), d(a.d), f(a.f), o(a.d_out), bf16(a.bf16) {
         pl = bf16 ? 1 : 3;
         bk = bf16 ? 32 : 16;
@@ -1207,7 +1214,7 @@ struct Plan {
                 *x = {tiles(m, f, e.bn, e.bm), (o + bk - 1) / bk + (bf16 ? (d + bk - 1) / bk * 2 : 0), 0};
             });
             const int64_t ks = (fp() + bk - 1) / bk * (low_dx ? 4 : 2), ms = (m + bk - 1) / bk;
-            grads = choose(bf16 ? kGradsBf16 : kOutF32, j, 3, true, [&](const Shape &e, Job *x) {
+            grads = choose(bf16 ? kGradsBf16 : kGradsF32, j, 3, true, [&](const Shape &e, Job *x) {
                 x[0] = {tiles(m, d, e.bn, e.bm), ks, m * d};
                 x[1] = {tiles(d, 2 * fp(), e.bn, e.bm), ms * (low_dw ? 2 : 1), 2 * d * fp()};
                 x[2] = {tiles(f, o, e.bn, e.bm), ms * (low_dd ? 2 : 1), f * o};
