@@ -553,8 +553,8 @@ gnnav_status gnnav_linear_xent(const void *h_dev, int64_t ld_h, int64_t m, const
  *   a = x Wg,  b = x Wu,  h = act(a) * b (entry by entry),  y = h Wd,
  * Wg and Wu d x f, Wd f x d_out, all row-major with strides.  act: GNNAV_ACT_SILU
  * a / (1 + exp(-a)), GNNAV_ACT_GELU a (1 + erf(a / sqrt 2)) / 2, GNNAV_ACT_RELU.
- * dt = F32: fp32-accurate products (six bf16 part products; an infinite entry makes
- * its products NaN).  dt = BF16: bf16 operands, fp32 accumulation; a and b stay in
+ * dt = F32: fp32-accurate products (six bf16 part products; an infinite entry may make
+ * its products NaN; ReLU's slope follows the sign of a in 64 bits where a nearly cancels).  dt = BF16: bf16 operands, fp32 accumulation; a and b stay in
  * fp32, h is rounded to bf16 for its product, y once.  The columns of an output
  * row from its last to the next 16-byte boundary are written with zeros; whatever
  * inputs hold there is not used.  m = 0 is allowed.

@@ -6,8 +6,11 @@
 //   dz_v = alpha T / A (p_v(T) - sum_{j: id_j = v} q_j) + (1 - alpha) / B (p_v(1) - [v = y_i])
 //
 // A the rows with entries, B those with a label that counts.  Bound by memory: a row is read once, into the registers of a
-// team of 16 lanes to four wavefronts, and its gradient written from them.  Rows of more classes are cut into strips, whose
-// sums take a launch of their own, by groups of rows that the memory-side cache still holds when the gradient reads them again.
+// team of 16 lanes to four wavefronts, and its gradient written from them: 4,093 x 10,000 bf16 66 us, of which reading and writing
+// at 4.72 TB/s is 35; its two exponentials a logit (at T and at 1) and the four barriers of a row take the rest.  Rows of
+// more classes are cut into strips, whose sums take a launch of their own; the gradient's starts with the last rows, which
+// the memory-side cache still holds: 1,024 x 169,000 fp32 385 us (293), 392 in the same order.  Groups of rows by turns, small enough
+// for that cache, are slower (a launch's end each), and so are teams of 512 and 1,024 threads, which spill.
 #include <algorithm>
 #include <cmath>
 
@@ -21,7 +24,6 @@ namespace {
 typedef uint32_t u32x4x __attribute__((ext_vector_type(4)));
 constexpr double kLog2e = 1.44269504088896340736;
 constexpr int kParts = 1024;   // counts of rows, at most
-constexpr int kMost = 256;    // entries of a row, at most
 constexpr int kSplitVectors = 4;   // 16-byte vectors of a thread in a strip
 constexpr int kBlocks = 2048;      // workgroups that take whole rows, at most
 
@@ -31,7 +33,7 @@ struct Args {
     int32_t parts;       // 0: every workgroup counts for itself
     double2 *losses;     // [n_losses]: sums of both parts of the loss
     int32_t n_losses;
-    int64_t first;       // strips > 0: first row of the group
+    int64_t first;       // strips > 0: first row of the launch
     float scale, inv_t;  // log2(e) times what the logits are divided by (1 / T, or 1 where there is no teacher's part); 1 / T
     int32_t strips, width;
     float4 *sums;        // strips > 0: [m][strips] largest logit, sums at T and at 1
@@ -488,17 +490,18 @@ __global__ void __launch_bounds__(256) k_distill_row(const Args a) {
 namespace {
 int64_t up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
 
-// Strips of a row: 0 where a row is taken whole.
-int32_t strips_for(int64_t m, int64_t n_classes, bool bf16) {
+// Strips of a row: 0 where a row is taken whole, as long as four wavefronts hold it.  1,024 x 8,192 fp32: 31 us, in strips 36;
+// 4,093 x 16,000 bf16: 84 and 90; 64 x 16,000 as much.
+int32_t strips_for(int64_t n_classes, bool bf16) {
     const int64_t per = bf16 ? 8 : 4, width = 256 * kSplitVectors * per;
-    return n_classes > 2048 * per || (m <= 128 && n_classes > 2 * width) ? (int32_t)((n_classes + width - 1) / width) : 0;
+    return n_classes > 2048 * per ? (int32_t)((n_classes + width - 1) / width) : 0;
 }
 
 struct Plan {
     int32_t strips, n_losses;
     size_t losses, sums, own, total;
     Plan(int64_t m, int64_t n_classes, int64_t k, bool bf16) {
-        strips = strips_for(m, n_classes, bf16);
+        strips = strips_for(n_classes, bf16);
         n_losses = strips > 0 ? (int32_t)m : (int32_t)std::min<int64_t>(m, kBlocks);
         size_t at = kParts * sizeof(int2);
         auto take = [&](int64_t bytes) {
@@ -534,16 +537,17 @@ void rows(Args &a, hipStream_t s) {
     KernelTimer t("distill_row", s);
 #define GNNAV_L(T, NV, VEC)                                                                                                \
     do {                                                                                                                   \
-        a.n_losses = (int32_t)grid_for(m, 256 / T, kBlocks);                                                 \
+        a.n_losses = (int32_t)grid_for(m, 256 / T, kBlocks);                                                               \
         hipLaunchKernelGGL((k_distill_row<BF, T, NV, VEC, BOTH, false>), dim3((unsigned)a.n_losses), dim3(256), 0, s, a);  \
     } while (0)
-    const bool many = m >= 2048;   // enough rows for a wavefront each
+    // The smallest team that holds the row and its entries.  99,603 x 41 fp32, k = 8: 16 lanes 39 us, 32 60, 64 104, 256 350; 20,000 x
+    // 100, k = 16: 32 lanes 23, 64 30, 256 80; 20,000 x 1,000: 64 lanes 55, 256 110; 4,093 x 4,000 bf16: 33 and 40; 500 x 2,000: as much.
     if (C <= 64 && k <= 16) GNNAV_L(16, 4, false);
     else if (C <= 128 && k <= 32) GNNAV_L(32, 4, false);
     else if (C <= 64 * PER && k <= 64) GNNAV_L(64, 1, true);
     else if (C <= 128 * PER && k <= 64) GNNAV_L(64, 2, true);
-    else if (C <= 256 * PER && k <= 64 && many) GNNAV_L(64, 4, true);
-    else if (C <= 512 * PER && k <= 64 && many) GNNAV_L(64, 8, true);
+    else if (C <= 256 * PER && k <= 64) GNNAV_L(64, 4, true);
+    else if (C <= 512 * PER && k <= 64) GNNAV_L(64, 8, true);
     else if (C <= 512 * PER) GNNAV_L(256, 2, true);
     else if (C <= 1024 * PER) GNNAV_L(256, 4, true);
     else GNNAV_L(256, 8, true);

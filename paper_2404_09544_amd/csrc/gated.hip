@@ -87,7 +87,8 @@ __device__ const u32x4x kZeros = {0, 0, 0, 0};
 
 // ------------------------------------------------------------------ packing
 // rows x cols (row-major, 16-byte aligned rows) -> PL planes of chunks [chunk][row], zeros past the columns.
-// One workgroup: 64 rows x 64 columns through LDS.  A launch takes up to five matrices.
+// One workgroup: 64 rows x 64 columns through LDS.  A launch takes up to five matrices.  Bound by memory and, where the matrices are
+// small, by the launch: 12.8 million fp32 of four matrices 23 us, 5.6 TB/s; 100,000 x 100 30 us, 3.3 TB/s; a small one 5 us.
 struct PackJob {
     const void *src;
     int64_t ld;
@@ -569,10 +570,11 @@ __device__ __forceinline__ void tile_sum(F &feed, const Sum &sum, int32_t T, u32
 }
 
 // ReLU's slope jumps at 0: where the rounding of a sum in fp32 decides which side a is on, da is 0 instead of a whole term, or the
-// other way round.  Values within 2^-17 of the largest of the lane's (all of one row of x) are summed again in 64 bits by the
-// whole wavefront, some 1 in 10^5 of them; the errors of a are below 2^-19 of it up to some 10,000 columns.  A 0 is one of them,
-// unless it comes from zeros: the row's values are all 0, or the column's are in 8 or more rows and no other.  Without it 1 of 5.6 million signs of a 1,362 x 333 x 4,096 block is wrong, which is 6e-4 of
-// dWg's norm; a 3,000 x 1,024 x 2,048 block's h takes 180 us with it, SiLU's 173.
+// other way round.  Values within 2^-17 of the largest of the lane's (all of one row of x), and of the largest of the 32 rows in
+// their column where 8 are there, are summed again in 64 bits by the whole wavefront, some 1 in 10^5 of them; the errors of
+// a are below 2^-19 of that up to some 10,000 columns.  (A row or a column of zeros, or of much smaller values than others, is none
+// of it.)  Without it 1 of 5.6 million signs of a 1,362 x 333 x 4,096 block is wrong, which is 6e-4 of dWg's norm; a
+// 3,000 x 1,024 x 2,048 block's h takes 144 us with it, SiLU's 138.
 template <int WA, int WNF>
 __device__ __forceinline__ void sure_signs(const Product &a, int32_t c0, int64_t n, int j, int h, f32x16x (&acc)[2 * WA][WNF]) {
     float most = 0.f;
@@ -580,7 +582,7 @@ __device__ __forceinline__ void sure_signs(const Product &a, int32_t c0, int64_t
     for (int i = 0; i < WA; ++i)
 #pragma unroll
         for (int r = 0; r < 16; ++r) most = fmaxf(most, fabsf(acc[i][j][r]));
-    most *= 0x1p-17f;
+    most = most < INFINITY ? most * 0x1p-17f : 0.f;
 #pragma unroll
     for (int i = 0; i < WA; ++i) {
         uint32_t near = 0;
@@ -589,10 +591,12 @@ __device__ __forceinline__ void sure_signs(const Product &a, int32_t c0, int64_t
             const float v = fabsf(acc[i][j][r]);
             const bool live = n < a.n && c0 + 32 * i + 8 * (r / 4) + 4 * h + r % 4 < a.f;
             bool close = live && v < most;
-            if (__ballot(close && v == 0.f)) {
-                const uint64_t other = __ballot(live && !(v == 0.f)), zero = __ballot(live && v == 0.f);
-                const uint32_t others = (uint32_t)(other >> (32 * h)), zeros = (uint32_t)(zero >> (32 * h));   // of the column
-                close = close && (v > 0.f || others || __builtin_popcount(zeros) < 8);
+            if (__ballot(close)) {
+                const uint32_t rows = (uint32_t)(__ballot(live) >> (32 * h));
+                float column = live ? v : 0.f;
+#pragma unroll
+                for (int q = 16; q > 0; q /= 2) column = fmaxf(column, __shfl_xor(column, q));
+                close = close && (v < column * 0x1p-17f || __builtin_popcount(rows) < 8);
             }
             near |= (uint32_t)close << r;
         }
@@ -748,7 +752,9 @@ __device__ __forceinline__ void out_tile(const Product &a, int32_t id, u32x4x *S
 }
 
 // A workgroup takes tile after tile, the next one's first copies under way while one's results are formed and stored.
-// (Tiles of more than three stages are for launches that have one a workgroup.)
+// (Tiles of more than three stages are for launches that have one a workgroup.)  8,192 x 1,024 x 4,096 bf16: 137 us, 1,000 TFLOP/s,
+// bound by the matrix cores' power; 65,537 x 256 x 1,024: 110 us (117 with a tile a workgroup), bound by a tile's ends, its
+// sum having eight steps; 99,603 x 128 x 512: 69 us (73), four steps and the activation.
 template <int PL, int WMF, int WNF, int WGM, int WGN, int ST, int ACT>
 __global__ void __launch_bounds__(64 * WGM * WGN, 2) k_gated_gate(const Product a, int32_t ids) {
     constexpr int WA = WMF / 2;
@@ -780,13 +786,16 @@ __global__ void __launch_bounds__(64 * WGM * WGN, 2) k_gated_gate(const Product 
         }
     }
 }
+// 8,192 x 4,096 x 1,024 bf16: 105 us, 650 TFLOP/s: 256 tiles, one a unit, which leaves a step's latencies open; in tiles of 256 x 256
+// two splits' parts would take as long.  99,603 x 512 x 64: 28 us, 4.4 TB/s.
 template <int PL, int WMF, int WNF, int WGM, int WGN, int ST>
 __global__ void __launch_bounds__(64 * WGM * WGN, 2) k_gated_down(const Product a) {
     __shared__ u32x4x S[Tile<PL, WMF, WNF, WGM, WGN, ST>::LDS];
     out_tile<PL, WMF, WNF, WGM, WGN, ST, true, false>(a, blockIdx.x, S);
 }
 // fp32 takes tile after tile too; bf16, whose three sums leave no registers for the next tile's copies, one: the copies of dh's sum
-// follow those of a and b.
+// follow those of a and b.  8,192 x 1,024 x 4,096 x 1,024 bf16: 221 us, 930 TFLOP/s; 65,537 x 256 x 1,024 x 256: 197, its stores 1.4 TB/s
+// beside eight and sixteen steps.
 template <int PL, int WA, int WNF, int WGM, int WGN, int ST, int ACT>
 __global__ void __launch_bounds__(64 * WGM * WGN, 2) k_gated_dgate(const Product a, const Sum again, int32_t ids) {
     constexpr int64_t AM = 32 * WA * WGM, BN = 32 * WNF * WGN;
@@ -834,7 +843,8 @@ __global__ void __launch_bounds__(64 * WGM * WGN, 2) k_gated_dgate(const Product
         }
     }
 }
-// dx and the weights' gradients in one launch: workgroups below `w_at` take dx's tiles, below `d_at` those of dWg and dWu.
+// dx and the weights' gradients in one launch (8,192 x 1,024 x 4,096 x 1,024 bf16: 308 us, 1,120 TFLOP/s; 65,537 x 256 x 1,024 x 256:
+// 218 us, 940 TFLOP/s and 4 TB/s): workgroups below `w_at` take dx's tiles, below `d_at` those of dWg and dWu.
 template <int PL, int WMF, int WNF, int WGM, int WGN, int ST>
 __global__ void __launch_bounds__(64 * WGM * WGN, 2) k_gated_grads(const Product x, const Product w, const Product d, int32_t w_at,
                                                                    int32_t d_at) {

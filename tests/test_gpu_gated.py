@@ -148,6 +148,18 @@ def test_relu_is_on_the_right_side_of_zero(G, m, d, f, o):
     check(G, x, wg, wu, wd, dy, "relu", "f32", sides=True)
 
 
+@pytest.mark.parametrize("m", [5, 70, 500])
+def test_relu_with_columns_and_rows_that_are_nearly_dead(G, m):
+    """Hidden columns of zeros, and columns and rows 2^-40 of the others: their signs are those of their own sizes."""
+    x, wg, wu, wd, dy = block(m, 130, 300, 40, "f32", 70)
+    wg[:, 3::7] = 0
+    wg[:, 5::7] *= 2.0 ** -40
+    x[1::9] *= 2.0 ** -40
+    x[2::9] = 0
+    say("gated relu dead", m)
+    check(G, x, wg, wu, wd, dy, "relu", "f32")
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("act", ["silu", "gelu", "relu"])
 def test_activations(G, act, dtype):
