@@ -6,8 +6,8 @@
 //   dz_v = alpha T / A (p_v(T) - sum_{j: id_j = v} q_j) + (1 - alpha) / B (p_v(1) - [v = y_i])
 //
 // A the rows with entries, B those with a label that counts.  Bound by memory: a row is read once, into the registers of a
-// team of 16 lanes to four wavefronts, and its gradient written from them: 4,093 x 10,000 bf16 66 us, of which reading and writing
-// at 4.72 TB/s is 35; its two exponentials a logit (at T and at 1) and the four barriers of a row take the rest.  Rows of
+// team of 16 lanes to four wavefronts, and its gradient written from them: 4,093 x 10,000 bf16 64 us, of which reading and writing
+// at 4.72 TB/s is 35; the exponentials (one a logit and pass at least) and the four barriers of a row take the rest.  Rows of
 // more classes are cut into strips, whose sums take a launch of their own; the gradient's starts with the last rows, which
 // the memory-side cache still holds: 1,024 x 169,000 fp32 385 us (293), 392 in the same order.  Groups of rows by turns, small enough
 // for that cache, are slower (a launch's end each), and so are teams of 512 and 1,024 threads, which spill.
@@ -149,6 +149,16 @@ struct Sums {
 };
 __device__ __forceinline__ float exp_of(float x, float scale) { return __builtin_amdgcn_exp2f(x * scale); }
 
+// Whether the exponentials at 1 are needed beside those at T, and how they are had: from those at T = 2 or 4 by one or two
+// products, as exact (an exponent's rounding counts T times either way).  4,093 x 10,000 bf16 at T = 4: 64 us, 67 with two.
+enum { kOne, kBoth, kSquare, kFourth };
+template <int WAY>
+__device__ __forceinline__ float exp_at_one(float x, float at_t) {
+    if constexpr (WAY == kSquare) return at_t * at_t;
+    else if constexpr (WAY == kFourth) return (at_t * at_t) * (at_t * at_t);
+    else return exp_of(x, (float)kLog2e);
+}
+
 }  // namespace
 
 // Rows with entries and rows with labels that count, by parts: 16 lanes a row.
@@ -214,7 +224,7 @@ __global__ void __launch_bounds__(256) k_distill_mean(const Args a) {
 }
 
 // The sums of one strip of a row, and the logits that are needed by themselves (the gradient may take their place).
-template <bool BF, bool BOTH>
+template <bool BF, int BOTH>
 __global__ void __launch_bounds__(256) k_distill_sums(const Args a) {
     constexpr int PER = BF ? 8 : 4;
     __shared__ float scratch[3][4];
@@ -236,8 +246,9 @@ __global__ void __launch_bounds__(256) k_distill_sums(const Args a) {
     for (int i = 0; i < kSplitVectors; ++i)
 #pragma unroll
         for (int e = 0; e < PER; ++e) {
-            s.st += exp_of(element<BF>(v[i], e) - ref, a.scale);
-            if constexpr (BOTH) s.s1 += exp_of(element<BF>(v[i], e) - ref, (float)kLog2e);
+            const float z = element<BF>(v[i], e) - ref, p = exp_of(z, a.scale);
+            s.st += p;
+            if constexpr (BOTH) s.s1 += exp_at_one<BOTH>(z, p);
         }
     const float top = team.across<true>((team.within<true>(s.top, 0), team.sync(), 0.f), 0);
     const float ft = s.top == -INFINITY ? 1.f : exp_of(s.top - top, a.scale), f1 = s.top == -INFINITY ? 1.f : exp_of(s.top - top, (float)kLog2e);
@@ -256,7 +267,7 @@ __global__ void __launch_bounds__(256) k_distill_sums(const Args a) {
 
 // One row, by the team of T threads that calls it.  VEC: 16-byte loads (otherwise a class a lane); NV of them a thread stay
 // in registers.  SPLIT: the sums are there, and strip `strip` of the gradient is written.
-template <bool BF, int T, int NV, bool VEC, bool BOTH, bool SPLIT>
+template <bool BF, int T, int NV, bool VEC, int BOTH, bool SPLIT>
 __device__ __forceinline__ void distill_row(const Args &a, int64_t row, int32_t strip, bool live, int2 counted_rows, const Team<T> &team, int32_t *ids,
                                             float *share, double2 &loss) {
     constexpr int PER = !VEC ? 1 : BF ? 8 : 4, ELT = BF ? 2 : 4;
@@ -313,7 +324,7 @@ __device__ __forceinline__ void distill_row(const Args &a, int64_t row, int32_t 
                 else z = one[v];
                 const float p = exp_of(z - ref, a.scale);
                 s.st += p;
-                if constexpr (BOTH) s.s1 += exp_of(z - ref, (float)kLog2e);
+                if constexpr (BOTH) s.s1 += exp_at_one<BOTH>(z - ref, p);
                 if constexpr (EXPS) keep[v][e] = __float_as_uint(p);
             }
         }
@@ -380,8 +391,9 @@ __device__ __forceinline__ void distill_row(const Args &a, int64_t row, int32_t 
     const float ct = do_kd ? (none ? nan : wk / st) : 0.f, c1 = do_ce ? (none ? nan : wc / s1) : 0.f;
     const float ref = some ? top : 0.f;
     auto grad = [&](float z) {
-        if constexpr (BOTH) return ct * exp_of(z - ref, a.scale) + c1 * exp_of(z - ref, (float)kLog2e);
-        else return (ct + c1) * exp_of(z - ref, a.scale);
+        const float p = exp_of(z - ref, a.scale);
+        if constexpr (BOTH) return ct * p + c1 * exp_at_one<BOTH>(z - ref, p);
+        else return (ct + c1) * p;
     };
     auto write = [&](const u32x4x &v, int64_t c, auto exps_, float factor) {   // of logits, or of their exponentials
         float g[PER];
@@ -442,7 +454,7 @@ __device__ __forceinline__ void distill_row(const Args &a, int64_t row, int32_t 
     if (do_ce && tid == 0 && y >= begin && y < end && !(do_kd && listed)) put(y, grad(zy) - wc);
 }
 
-template <bool BF, int T, int NV, bool VEC, bool BOTH, bool SPLIT>
+template <bool BF, int T, int NV, bool VEC, int BOTH, bool SPLIT>
 __global__ void __launch_bounds__(256) k_distill_row(const Args a) {
     constexpr int NT = 256, ROWS = NT / T, ENTRIES = T;
     __shared__ float scratch[9][Team<T>::W];
@@ -516,7 +528,7 @@ struct Plan {
     }
 };
 
-template <bool BF, bool BOTH>
+template <bool BF, int BOTH>
 void rows(Args &a, hipStream_t s) {
     const int64_t m = a.x.m, C = a.x.n_classes, k = a.x.alpha > 0.f ? a.x.k : 0;
     constexpr int PER = BF ? 8 : 4;
@@ -553,6 +565,15 @@ void rows(Args &a, hipStream_t s) {
     else GNNAV_L(256, 8, true);
 #undef GNNAV_L
 }
+template <bool BF>
+void by_way(Args &a, int way, hipStream_t s) {
+    switch (way) {
+    case kOne: return rows<BF, kOne>(a, s);
+    case kSquare: return rows<BF, kSquare>(a, s);
+    case kFourth: return rows<BF, kFourth>(a, s);
+    default: return rows<BF, kBoth>(a, s);
+    }
+}
 }  // namespace
 
 size_t distill_workspace(int64_t m, int64_t n_classes, int64_t k, bool bf16) { return Plan(m, n_classes, k, bf16).total; }
@@ -579,8 +600,9 @@ void launch_distill(const DistillArgs &x, hipStream_t s) {
     }
     if (x.m > 0) {
         const bool both = x.alpha > 0.f && x.labels && x.temperature != 1.f;
-        if (x.bf16) both ? rows<true, true>(a, s) : rows<true, false>(a, s);
-        else both ? rows<false, true>(a, s) : rows<false, false>(a, s);
+        const int way = !both ? kOne : x.temperature == 2.f ? kSquare : x.temperature == 4.f ? kFourth : kBoth;
+        if (x.bf16) by_way<true>(a, way, s);
+        else by_way<false>(a, way, s);
     }
     {
         KernelTimer t("distill_mean", s);

@@ -149,6 +149,19 @@ def test_loss_and_gradient(G, m, c, k, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("c", [41, 1_000, 40_000])
+@pytest.mark.parametrize("temp", [4.0, 3.0, 0.25])
+def test_temperatures_beside_labels(G, c, temp, dtype):
+    """Exponentials at the temperature and at 1, from one another or each by itself."""
+    m, k = 30, 12
+    z = matrix(m, c, dtype, 80).mul_(4.0)
+    ids, t = teacher(m, c, k, 81)
+    labels = np.random.default_rng(82).integers(0, c, m).astype(np.int32)
+    say("distill temperatures", c, temp, dtype)
+    check(G, z, ids, t, temp=temp, alpha=0.4, labels=labels)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("c", [41, 3_000, 40_000])
 def test_what_is_asked_for_and_in_place(G, c, dtype):
     say("distill outputs", c, dtype)
