@@ -744,6 +744,8 @@ def gated_ffn_backward(x, wg, wu, wd, dy, saved, dx=None, dwg=None, dwu=None, dw
 
 def _kept(ids, values, what: str, device: int, m: int):
     """Checks [m, k] class ids (int32) and logits (float32); their addresses and k."""
+    if values is None:
+        raise ValueError(f"ids need {what}")
     for t, name, dtype in ((ids, "ids", torch.int32), (values, what, torch.float32)):
         if t.dim() != 2 or t.shape != ids.shape or t.shape[0] != m:
             raise ValueError(f"ids and {what} must be [rows of logits, k]")

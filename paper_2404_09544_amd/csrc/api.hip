@@ -1733,6 +1733,17 @@ static void check_saved(const void *saved, int64_t bytes, const GatedArgs &a) {
     GNNAV_CHECK(need == 0 || (saved && aligned16(saved)), GNNAV_E_INVALID, "saved must be on a 16-byte boundary");
 }
 
+// outputs that take the place of an input, or of each other, which other workgroups still read or write
+static void check_apart(std::initializer_list<const void *> outputs, std::initializer_list<const void *> inputs) {
+    for (const void *const *o = outputs.begin(); o != outputs.end(); ++o) {
+        if (!*o) continue;
+        bool same = false;
+        for (const void *i : inputs) same = same || i == *o;
+        for (const void *const *other = outputs.begin(); other != o; ++other) same = same || *other == *o;
+        GNNAV_CHECK(!same, GNNAV_E_INVALID, "an output in the place of an input or of another output");
+    }
+}
+
 extern "C" gnnav_status gnnav_gated_ffn(const void *x_dev, int64_t ld_x, int64_t m, int64_t d, const void *wg_dev, int64_t ld_wg,
                                         const void *wu_dev, int64_t ld_wu, int64_t f, const void *wd_dev, int64_t ld_wd,
                                         int64_t d_out, gnnav_dtype dt, int32_t act, void *y_dev, int64_t ld_y, void *saved_dev,
@@ -1743,6 +1754,7 @@ extern "C" gnnav_status gnnav_gated_ffn(const void *x_dev, int64_t ld_x, int64_t
         check_rows(y_dev, ld_y, d_out, a.bf16 ? 2 : 4, "y");
         if (saved_dev) check_saved(saved_dev, saved_bytes, a);
         check_workspace(workspace_dev, workspace_bytes, gated_workspace(a, false));
+        check_apart({y_dev}, {x_dev, wg_dev, wu_dev, wd_dev});
         a.y = y_dev;
         a.ld_y = ld_y;
         a.saved = saved_dev;
@@ -1768,6 +1780,7 @@ extern "C" gnnav_status gnnav_gated_ffn_backward(const void *x_dev, int64_t ld_x
         if (dwu_dev) check_rows(dwu_dev, ld_dwu, f, elt, "dwu");
         if (dwd_dev) check_rows(dwd_dev, ld_dwd, d_out, elt, "dwd");
         check_workspace(workspace_dev, workspace_bytes, gated_workspace(a, true));
+        check_apart({m > 0 ? dx_dev : nullptr, dwg_dev, dwu_dev, dwd_dev}, {x_dev, wg_dev, wu_dev, wd_dev, dy_dev});
         a.dy = dy_dev;
         a.ld_dy = ld_dy;
         a.saved = const_cast<void *>(saved_dev);

@@ -52,6 +52,23 @@ def test_gated_backward_refusals(change, want, text):
                                          a["dwd"], 8, a["ws"], a["ws_bytes"], None), want, text)
 
 
+P = {n: A * (i + 1) for i, n in enumerate(("x", "wg", "wu", "wd", "y", "saved", "ws", "dx", "dwg", "dwu", "dwd"))}
+
+
+@pytest.mark.parametrize("out,other", [("y", "x"), ("y", "wd"), ("y", "wg")])
+def test_gated_refuses_an_output_in_the_place_of_an_input(out, other):
+    a = dict(FFN, **dict(P, **{out: P[other]}))
+    refused(lib.gnnav_gated_ffn(a["x"], 8, 4, 8, a["wg"], 16, a["wu"], 16, 16, a["wd"], 8, 8, G.F32, 0, a["y"], 8, a["saved"], HUGE, a["ws"], HUGE, None),
+            INVALID, b"in the place")
+
+
+@pytest.mark.parametrize("out,other", [("dx", "y"), ("dx", "x"), ("dwg", "wg"), ("dwu", "wu"), ("dwd", "wd"), ("dwu", "dwg"), ("dwd", "dx")])
+def test_gated_backward_refuses_an_output_in_the_place_of_another_operand(out, other):
+    a = dict(FFN, **dict(P, **{out: P[other]}))
+    refused(lib.gnnav_gated_ffn_backward(a["x"], 8, 4, 8, a["wg"], 16, a["wu"], 16, 16, a["wd"], 8, 8, G.F32, 0, a["y"], 8, a["saved"], HUGE, a["dx"], 8,
+                                         a["dwg"], 16, a["dwu"], 16, a["dwd"], 8, a["ws"], HUGE, None), INVALID, b"in the place")
+
+
 TOP = dict(z=A, ld=8, m=3, c=8, dt=G.F32, k=2, values=A, ids=A, ws=A, ws_bytes=HUGE)
 
 
@@ -124,3 +141,9 @@ def test_binding_refuses_host_tensors():
                  lambda: G.distill(t, ids, t[:, :2], loss)):
         with pytest.raises(ValueError):
             call()
+
+
+def test_binding_refuses_ids_without_logits():
+    import torch
+    with pytest.raises(ValueError):
+        G._kept(torch.zeros(8, 2, dtype=torch.int32), None, "teacher", 0, 8)
