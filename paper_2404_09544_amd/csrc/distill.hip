@@ -419,8 +419,10 @@ __device__ __forceinline__ void distill_row(const Args &a, int64_t row, int32_t 
         else ((float *)out)[c] = g;
     };
     const u32x4x zeros = {0, 0, 0, 0};
-    // (a row that does not count may hold what makes the exponential infinite)
-    const float factor = EXPS && some ? (ct + c1) * exp_of(kept - ref, a.scale) : 0.f;
+    // (a row that does not count may hold what makes the exponential infinite; a thread of -inf alone kept zeros, with no scale of
+    // their own)
+    const float down = s.top == -INFINITY ? 0.f : exp_of(kept - ref, a.scale);
+    const float factor = EXPS && some ? (ct + c1) * down : 0.f;
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
         const int64_t c = begin + (int64_t)(v * T + tid) * PER;

@@ -55,3 +55,33 @@ def test_rows_that_do_not_count_hold_anything(G, c, dtype, temp, alpha, with_lab
     z[3] = 1e4
     loss, row, dz = call(G, z, ids, t, temp, alpha, labels, ignore=-100)
     assert torch.isnan(loss[0]) and torch.isnan(row[3]) and (dz[3] == 0).all() and torch.isfinite(dz).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("c", CLASSES)
+@pytest.mark.parametrize("temp,alpha,with_labels", WAYS)
+def test_masked_classes_beside_low_logits(G, c, dtype, temp, alpha, with_labels):
+    """Long runs of classes of -inf have p = 0 however low the others are; a row of -inf alone and one with a NaN are NaN everywhere."""
+    import torch
+    say("distill masked runs", c, dtype, temp, alpha, with_labels)
+    m, k = 9, 4
+    ids, t = teacher(m, c, k, 2)
+    ids[:] = np.arange(k)
+    labels = np.zeros(m, int) if with_labels else None
+    z = matrix(m, c, dtype, 1)
+    for row, low in enumerate((50.0, 100.0, 200.0, 1e3, 1e6 if dtype == "f32" else 4096.0)):
+        z[row].sub_(low)
+        z[row, k:] = -float("inf")
+    z[5].sub_(300.0)
+    z[5, c // 2:] = -float("inf")
+    z[6].sub_(300.0)
+    z[6, k + 1:] = torch.finfo(z.dtype).min
+    z[6, c // 2:] = -float("inf")
+    z[7].sub_(500.0)
+    z[7, k + 4:c - 2] = -float("inf")
+    dz = check(G, z, ids, t, temp, alpha, labels)[2]
+    assert (dz[:5, k:] == 0).all() and (dz[5:7, c // 2:] == 0).all()
+    z[0] = -float("inf")
+    z[1, c - 1] = float("nan")
+    again = call(G, z, ids, t, temp, alpha, labels)[2]
+    assert torch.isnan(again[:2]).all() and torch.isfinite(again[2:]).all()
