@@ -575,7 +575,8 @@ gnnav_status gnnav_linear_xent(const void *h_dev, int64_t ld_h, int64_t m, const
  * gnnav_gated_ffn_backward_workspace bytes (-1 for bad arguments; host only) on a
  * 256-byte boundary, used until the work has run; its contents do not matter.  No call
  * allocates or waits; sums run in a fixed order (no atomics: repeated calls give
- * identical bits).  Outputs must not overlap inputs or each other (the same address is refused).
+ * identical bits).  Outputs must not overlap inputs or each other, saved_dev among them (the same
+ * address is refused).
  * Errors: E_INVALID (null pointers, sizes, strides, alignment, act, workspace),
  * E_CAPACITY (m beyond 2^28, d, f or d_out beyond 2^20), E_DEVICE.  Asynchronous.  */
 enum { GNNAV_ACT_SILU = 0, GNNAV_ACT_GELU = 1, GNNAV_ACT_RELU = 2 };

@@ -1754,7 +1754,7 @@ extern "C" gnnav_status gnnav_gated_ffn(const void *x_dev, int64_t ld_x, int64_t
         check_rows(y_dev, ld_y, d_out, a.bf16 ? 2 : 4, "y");
         if (saved_dev) check_saved(saved_dev, saved_bytes, a);
         check_workspace(workspace_dev, workspace_bytes, gated_workspace(a, false));
-        check_apart({y_dev}, {x_dev, wg_dev, wu_dev, wd_dev});
+        check_apart({y_dev, saved_dev}, {x_dev, wg_dev, wu_dev, wd_dev});
         a.y = y_dev;
         a.ld_y = ld_y;
         a.saved = saved_dev;
@@ -1780,7 +1780,7 @@ extern "C" gnnav_status gnnav_gated_ffn_backward(const void *x_dev, int64_t ld_x
         if (dwu_dev) check_rows(dwu_dev, ld_dwu, f, elt, "dwu");
         if (dwd_dev) check_rows(dwd_dev, ld_dwd, d_out, elt, "dwd");
         check_workspace(workspace_dev, workspace_bytes, gated_workspace(a, true));
-        check_apart({m > 0 ? dx_dev : nullptr, dwg_dev, dwu_dev, dwd_dev}, {x_dev, wg_dev, wu_dev, wd_dev, dy_dev});
+        check_apart({m > 0 ? dx_dev : nullptr, dwg_dev, dwu_dev, dwd_dev}, {x_dev, wg_dev, wu_dev, wd_dev, dy_dev, m > 0 ? saved_dev : nullptr});
         a.dy = dy_dev;
         a.ld_dy = ld_dy;
         a.saved = const_cast<void *>(saved_dev);

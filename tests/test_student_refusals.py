@@ -69,6 +69,21 @@ def test_gated_backward_refuses_an_output_in_the_place_of_another_operand(out, o
                                          a["dwg"], 16, a["dwu"], 16, a["dwd"], 8, a["ws"], HUGE, None), INVALID, b"in the place")
 
 
+
+@pytest.mark.parametrize("saved", ["x", "wg", "wu", "wd", "y"])
+def test_gated_refuses_what_is_saved_in_the_place_of_an_operand(saved):
+    a = dict(FFN, **dict(P, saved=P[saved]))
+    refused(lib.gnnav_gated_ffn(a["x"], 8, 4, 8, a["wg"], 16, a["wu"], 16, 16, a["wd"], 8, 8, G.F32, 0, a["y"], 8, a["saved"], HUGE, a["ws"], HUGE, None),
+            INVALID, b"in the place")
+
+
+@pytest.mark.parametrize("out", ["dx", "dwg", "dwu", "dwd"])
+def test_gated_backward_refuses_an_output_in_the_place_of_what_was_saved(out):
+    a = dict(FFN, **dict(P, **{out: P["saved"]}))
+    refused(lib.gnnav_gated_ffn_backward(a["x"], 8, 4, 8, a["wg"], 16, a["wu"], 16, 16, a["wd"], 8, 8, G.F32, 0, a["y"], 8, a["saved"], HUGE, a["dx"], 8,
+                                         a["dwg"], 16, a["dwu"], 16, a["dwd"], 8, a["ws"], HUGE, None), INVALID, b"in the place")
+
+
 TOP = dict(z=A, ld=8, m=3, c=8, dt=G.F32, k=2, values=A, ids=A, ws=A, ws_bytes=HUGE)
 
 
