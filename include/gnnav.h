@@ -603,7 +603,8 @@ gnnav_status gnnav_gated_ffn_backward(const void *x_dev, int64_t ld_x, int64_t m
  *
  * gnnav_distill: a student's logits z (m x n_classes, dt F32 or BF16) against
  * the k logits t that a teacher kept of each row, for the classes ids (fp32 and int32
- * [m][k] contiguous, as gnnav_top_logits writes them), temperature T > 0:
+ * [m][k] contiguous, as gnnav_top_logits writes them), temperature T from
+ * 1.1e-19 to 1.8e19 (T^2 is a normal fp32 number; kd is T^2 times a sum that is rounded in fp32):
  *   q_j = softmax over the row's entries of t_j / T,  p = softmax(z / T),
  *   kd_i = T^2 sum_j q_j (log q_j - log p_id(j)),
  *   ce_i = -log softmax(z)_y, y = labels_dev[i],

@@ -1835,8 +1835,8 @@ extern "C" gnnav_status gnnav_distill(const void *logits_dev, int64_t ld, int64_
         GNNAV_CHECK(m >= 0 && n_classes > 0, GNNAV_E_INVALID, "m < 0 or n_classes <= 0");
         GNNAV_CHECK(m <= INT32_MAX && n_classes <= INT32_MAX, GNNAV_E_CAPACITY, "sizes beyond int32");
         GNNAV_CHECK(alpha >= 0.f && alpha <= 1.f, GNNAV_E_INVALID, "alpha outside [0, 1]");
-        GNNAV_CHECK(temperature > 0.f && std::isfinite(temperature) && std::isfinite(1.f / temperature), GNNAV_E_INVALID,
-                    "temperature is not positive and finite");
+        // (T^2 has to be a normal number: zeros meet an infinite one, and infinite logits / T one that is 0)
+        GNNAV_CHECK(temperature > 0.f && std::isnormal(temperature * temperature), GNNAV_E_INVALID, "temperature^2 is not a normal positive number");
         GNNAV_CHECK(alpha == 0.f ? k >= 0 && k <= kMaxTop : k >= 1 && k <= kMaxTop, GNNAV_E_INVALID, "k outside [1, 256]");
         GNNAV_CHECK(loss_dev, GNNAV_E_INVALID, "NULL loss");
         const int64_t elt = dt == GNNAV_BF16 ? 2 : 4;

@@ -119,6 +119,14 @@ def test_distill_refusals(change, want, text):
                               a["dz"], a["ld_d"], a["ws"], a["ws_bytes"], None), want, text)
 
 
+@pytest.mark.parametrize("temp", [3.5e-39, 4.2e-39, 1e-30, 1e-19, 2e19, 3e38])
+def test_distill_refuses_temperatures_past_fp32(temp):
+    """log2(e) / T or T^2 is infinite, which zeros would meet, or T^2 is none, which infinite logits / T would."""
+    a = dict(DISTILL, temp=temp, dz=A + 4096)
+    refused(lib.gnnav_distill(a["z"], a["ld"], a["m"], a["c"], a["dt"], a["ids"], a["t"], a["k"], a["temp"], a["alpha"], a["labels"], -1, a["loss"], None,
+                              a["dz"], a["ld_d"], a["ws"], a["ws_bytes"], None), INVALID, b"temperature")
+
+
 def test_workspace_sizes():
     """Host only: -1 for bad arguments, an answer for every size that a call takes."""
     for bad in [(-1, 8, 8, 8, 0), (4, 0, 8, 8, 0), (4, 8, 0, 8, 0), (4, 8, 8, 0, 0), (4, 8, 8, 8, 2), ((1 << 28) + 1, 8, 8, 8, 0), (4, 8, (1 << 20) + 1, 8, 0)]:
