@@ -95,17 +95,76 @@ struct PackJob {
     int32_t rows, cols, col_tiles, end;   // end: workgroups of the jobs so far
     u32x4x *out;
 };
+// Norms of x's rows, times `scale`, and of wg's columns (`blocks` workgroups: `row_blocks`, and one for 16 columns).
+struct NormJob {
+    const float *x, *wg;
+    int64_t ld_x, ld_wg, m;
+    int32_t d, f, row_blocks, blocks;
+    float scale, *rows, *columns;
+};
 struct PackJobs {
     PackJob job[5];
+    NormJob norms;
 };
+// Sums in 64 bits, in which any fp32 entry's square is a number.  Rows of up to 256 columns take 16 lanes, longer ones a wavefront;
+// 16 threads share a column.
+__device__ __forceinline__ void norms_of(const NormJob &a, double *part) {   // part: 16 x 16 sums in LDS
+    const int tid = threadIdx.x;
+    if ((int32_t)blockIdx.x < a.row_blocks) {
+        const int lanes = a.d <= 256 ? 16 : 64, at = tid % lanes, each = 256 / lanes;
+        for (int64_t first = (int64_t)blockIdx.x * each; first < a.m; first += (int64_t)a.row_blocks * each) {
+            const int64_t r = first + tid / lanes;
+            double sum = 0;
+            if (r < a.m) {
+#pragma unroll 4
+                for (int32_t c = at * 4; c < a.d; c += lanes * 4) {
+                    const f32x4x v = *(const f32x4x *)(a.x + r * a.ld_x + c);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const double w = c + e < a.d ? v[e] : 0.f;
+                        sum = fma(w, w, sum);
+                    }
+                }
+            }
+#pragma unroll
+            for (int q = 8; q > 0; q /= 2) sum += __shfl_xor(sum, q);
+            if (lanes == 64) {
+                sum += __shfl_xor(sum, 16);
+                sum += __shfl_xor(sum, 32);
+            }
+            if (at == 0 && r < a.m) a.rows[r] = (float)(sqrt(sum) * a.scale);
+        }
+        return;
+    }
+    const int at = tid % 16, from = tid / 16;
+    const int32_t c = ((int32_t)blockIdx.x - a.row_blocks) * 16 + at;
+    double sum = 0;
+    if (c < a.f) {
+#pragma unroll 8
+        for (int32_t r = from; r < a.d; r += 16) {
+            const double v = a.wg[r * a.ld_wg + c];
+            sum = fma(v, v, sum);
+        }
+    }
+    part[from * 16 + at] = sum;
+    __syncthreads();
+    if (from == 0 && c < a.f) {
+#pragma unroll
+        for (int q = 1; q < 16; ++q) sum += part[q * 16 + at];
+        a.columns[c] = (float)sqrt(sum);
+    }
+}
 template <bool BF>
 __global__ void __launch_bounds__(256) k_gated_pack(const PackJobs jobs) {
-    int32_t k = 0, base = 0;
-    while ((int32_t)blockIdx.x >= jobs.job[k].end) base = jobs.job[k++].end;
-    const PackJob &a = jobs.job[k];
-    const int32_t t = (int32_t)blockIdx.x - base, rows = a.rows, d = a.cols, chunks = (d + 7) / 8;
     constexpr int PL = BF ? 1 : 3;
     __shared__ u32x4x tile[PL][8][65];
+    if constexpr (!BF)
+        if ((int32_t)blockIdx.x < jobs.norms.blocks) return norms_of(jobs.norms, (double *)tile);
+    const int32_t id = (int32_t)blockIdx.x - (BF ? 0 : jobs.norms.blocks);
+    int32_t k = 0, base = 0;
+    while (id >= jobs.job[k].end) base = jobs.job[k++].end;
+    const PackJob &a = jobs.job[k];
+    const int32_t t = id - base, rows = a.rows, d = a.cols, chunks = (d + 7) / 8;
     const int tid = threadIdx.x;
     const int64_t r0 = (int64_t)(t / a.col_tiles) * 64;
     const int32_t c0 = (t % a.col_tiles) * 8;
@@ -185,7 +244,8 @@ struct Product {
     int32_t f;
     f32x4x *a, *b;
     u32x4x *h;
-    const float *x, *wg;         // fp32's ReLU that keeps a: the operands of a, their strides and columns
+    const float *x, *wg;         // fp32's ReLU that keeps a: the operands of a, their strides and columns, the norms of x's rows,
+    const float *row_norms, *column_norms;   // times what a norm's part may be off by, and of wg's columns
     int64_t ld_x, ld_wg;
     int32_t d;
     int64_t h_plane, second;     // chunks of a plane; from da to db
@@ -570,35 +630,30 @@ __device__ __forceinline__ void tile_sum(F &feed, const Sum &sum, int32_t T, u32
 }
 
 // ReLU's slope jumps at 0: where the rounding of a sum in fp32 decides which side a is on, da is 0 instead of a whole term, or the
-// other way round.  Values within 2^-17 of the largest of the lane's (all of one row of x), and of the largest of the 32 rows in
-// their column where 8 are there, are summed again in 64 bits by the whole wavefront, some 1 in 10^5 of them; the errors of
-// a are below 2^-19 of that up to some 10,000 columns.  (A row or a column of zeros, or of much smaller values than others, is none
-// of it.)  Without it 1 of 5.6 million signs of a 1,362 x 333 x 4,096 block is wrong, which is 6e-4 of dWg's norm; a
-// 3,000 x 1,024 x 2,048 block's h takes 144 us with it, SiLU's 138.
+// other way round.  Values below sure_below |x's row| |wg's column| are summed again in 64 bits by the whole wavefront.  A sum's terms
+// are together at most that product of norms, its running sum at most half of it where they cancel in the worst order, and
+// each of some 6 d / 16 additions rounds it by a part of 2^-24: errors grow with sqrt(d).  Measured over 2 million
+// entries each, in sqrt(d) 2^-24 of the norms: terms that rise to their largest sum and fall again 0.10 as a spread, 0.6 at the
+// most at 40 columns, 0.08 and 0.4 at 1,024; in random order some 0.25 2^-24 at any d, 4 2^-24 at the most.
+// Random entries are summed again at d x 5 10^-8 of them, and at d x 5 10^-5 where features lie 1,000 spreads from zero and columns sum
+// to nothing.  A 3,000 x 1,024 x 2,048 block's h takes 153 us (SiLU's 138) and its packing 3 more; with features 10, 100 and 1,000
+// spreads from zero 183, 340 and 1,490.  Without it 1 of 5.6 million signs of a random 1,362 x 333 x 4,096 block is wrong, which
+// is 6e-4 of dWg's norm, and 1 in 100 of a 33 x 4,096 x 64 one whose terms cancel.
+constexpr float sure_below(float root_d) { return std::max(root_d, 8.f) * 0x1p-24f; }
 template <int WA, int WNF>
 __device__ __forceinline__ void sure_signs(const Product &a, int32_t c0, int64_t n, int j, int h, f32x16x (&acc)[2 * WA][WNF]) {
-    float most = 0.f;
-#pragma unroll
-    for (int i = 0; i < WA; ++i)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) most = fmaxf(most, fabsf(acc[i][j][r]));
-    most = most < INFINITY ? most * 0x1p-17f : 0.f;
+    const float row = n < a.n ? a.row_norms[n] : 0.f;
 #pragma unroll
     for (int i = 0; i < WA; ++i) {
         uint32_t near = 0;
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-            const float v = fabsf(acc[i][j][r]);
-            const bool live = n < a.n && c0 + 32 * i + 8 * (r / 4) + 4 * h + r % 4 < a.f;
-            bool close = live && v < most;
-            if (__ballot(close)) {
-                const uint32_t rows = (uint32_t)(__ballot(live) >> (32 * h));
-                float column = live ? v : 0.f;
+        for (int g = 0; g < 4; ++g) {
+            const int32_t c = c0 + 32 * i + 8 * g + 4 * h;
+            f32x4x column = {0.f, 0.f, 0.f, 0.f};
+            if (c < a.f) column = *(const f32x4x *)(a.column_norms + c);
 #pragma unroll
-                for (int q = 16; q > 0; q /= 2) column = fmaxf(column, __shfl_xor(column, q));
-                close = close && (v < column * 0x1p-17f || __builtin_popcount(rows) < 8);
-            }
-            near |= (uint32_t)close << r;
+            for (int e = 0; e < 4; ++e)
+                near |= (uint32_t)(c + e < a.f && fabsf(acc[i][j][4 * g + e]) < row * column[e]) << (4 * g + e);
         }
         uint64_t lanes;
         while ((lanes = __ballot(near != 0)) != 0) {
@@ -1177,7 +1232,7 @@ struct Plan {
     bool low_y, low_dx, low_dw, low_dd;
     int gate, down, dgate, grads;
     int32_t down_splits = 1, dx_splits = 1, dw_splits = 1, dd_splits = 1;
-    size_t x = 0, wg = 0, wu = 0, wd = 0, dy = 0, h = 0, D = 0, part = 0, part2 = 0, part3 = 0, total = 0;
+    size_t x = 0, wg = 0, wu = 0, wd = 0, dy = 0, h = 0, D = 0, part = 0, part2 = 0, part3 = 0, row_norms = 0, column_norms = 0, total = 0;
     int64_t fp() const { return up(f, 8); }
     size_t take(int64_t bytes) {
         const size_t here = total;
@@ -1215,6 +1270,10 @@ struct Plan {
                           [&](const Shape &e, Job *x) { *x = {tiles(m, o, e.bn, e.bm), (f + bk - 1) / bk * (low_y ? 2 : 1), m * o}; });
             down_splits = j.splits;
             part = take(parts(m, o, out(down), down_splits));
+            if (!bf16) {   // (which activation it is, and whether a is kept, is not known to who asks for the size)
+                row_norms = take(m * 4);
+                column_norms = take(fp() * 4);
+            }
         } else {
             if (pack_dy) dy = packed(m, o);
             D = take(2 * fp() * m * 2 * (low_dx || low_dw ? 2 : pl));
@@ -1300,11 +1359,16 @@ struct Packer {
         j.end = blocks;
         j.out = (u32x4x *)out;
     }
+    void add_norms(const GatedArgs &x, float scale, float *rows, float *columns) {
+        const int32_t row_blocks = (int32_t)grid_for(x.m, x.d <= 256 ? 16 : 4, 4096);
+        jobs.norms = {(const float *)x.x, (const float *)x.wg, x.ld_x, x.ld_wg, x.m, (int32_t)x.d, (int32_t)x.f, row_blocks,
+                      row_blocks + (int32_t)(up(x.f, 16) / 16), scale, rows, columns};
+    }
     void run(bool bf16, hipStream_t s) {
         if (blocks == 0) return;
         KernelTimer t("gated_pack", s);
         if (bf16) hipLaunchKernelGGL(k_gated_pack<true>, dim3((unsigned)blocks), dim3(256), 0, s, jobs);
-        else hipLaunchKernelGGL(k_gated_pack<false>, dim3((unsigned)blocks), dim3(256), 0, s, jobs);
+        else hipLaunchKernelGGL(k_gated_pack<false>, dim3((unsigned)(blocks + jobs.norms.blocks)), dim3(256), 0, s, jobs);
     }
 };
 
@@ -1448,6 +1512,8 @@ void forward(const GatedArgs &x, hipStream_t s) {
         pack.add(x.wu, x.ld_wu, x.d, x.f, ws + p.wu);
     }
     if (p.pack_wd) pack.add(x.wd, x.ld_wd, x.f, x.d_out, ws + p.wd);
+    float *const row_norms = (float *)(ws + p.row_norms), *const column_norms = (float *)(ws + p.column_norms);
+    if (PL == 3 && ACT == GNNAV_ACT_RELU && x.saved) pack.add_norms(x, sure_below(std::sqrt((float)x.d)), row_norms, column_norms);
     pack.run(x.bf16, s);
     const Saved saved(x.saved, x.m, x.f, x.bf16);
     u32x4x *h = x.saved ? saved.h : (u32x4x *)(ws + p.h);
@@ -1468,6 +1534,8 @@ void forward(const GatedArgs &x, hipStream_t s) {
     g.ld_x = x.ld_x;
     g.ld_wg = x.ld_wg;
     g.d = (int32_t)x.d;
+    g.row_norms = row_norms;
+    g.column_norms = column_norms;
     g.h = h;
     g.h_plane = plane;
     // (second parts always go to the workspace, behind the place that h has there)
