@@ -521,6 +521,38 @@ gnnav_status gnnav_embedding_backward(const void *dout_dev, int64_t ld_dout, con
  * zero gradients.  Any other label outside [0, n_classes) makes its row's
  * loss NaN (so the mean is NaN) and its gradients zero; it counts.  n_classes
  * may be anything from 1; m = 0 is allowed.
+ * dt = F32: fp32-accurate products (six bf16 part products; an infinite entry
+ * of a row that counts or of w makes its logits NaN).  dt = BF16: bf16
+ * operands, fp32 accumulation and statistics; p - [v = y] is rounded to bf16
+ * before the gradients' products (up to 32 rows, and up to 64 rows of at most
+ * 2^20 classes, it keeps 16 bits), the gradients once to bf16.  exp of less than
+ * 2^-126 counts as 0.  row_loss_dev,
+ * dh_dev, dw_dev may be NULL; dh and dw are of type dt, every row written, the
+ * columns from d up to the next 16-byte boundary with zeros.  Results do not
+ * depend on the run (no atomics).  workspace_dev: at least
+ * gnnav_linear_xent_workspace bytes (grads: whether dh or dw is asked for; -1
+ * for bad arguments; host only) on a 256-byte boundary.  It holds h, dh in up to
+ * 128 parts of 4 bytes an entry, and a piece of the classes: their rows, at most
+ * 896 MiB or 256 classes, their p, at most 1 GiB or 256 classes (512 bytes a row
+ * of h in bf16, 1,536 in fp32), and their statistics, at most 64 MiB (512 without
+ * gradients) or 56 bytes a row of h.  Up to 64 rows (of at most 2^20 classes from 33
+ * on) it holds at most 4 bytes a class, logits, 32 MiB of them at most (256 MiB from
+ * 33 rows on), and dh in up to 1,024 parts, 33 MiB or 2 of them.  No call allocates.
+ * Outputs must not overlap inputs or each other.
+ * Errors: E_INVALID (null pointers, sizes, strides, alignment, workspace),
+ * E_CAPACITY (a size beyond int32, d beyond 2^20), E_DEVICE.  Asynchronous. */
+int64_t gnnav_linear_xent_workspace(int64_t m, int64_t n_classes, int64_t d, gnnav_dtype dt, int32_t grads);
+gnnav_status gnnav_linear_xent(const void *h_dev, int64_t ld_h, int64_t m, const void *w_dev, int64_t ld_w,
+                               int64_t n_classes, int64_t d, gnnav_dtype dt, const int32_t *labels_dev,
+                               int32_t ignore_label, float *loss_dev, float *row_loss_dev, void *dh_dev,
+                               int64_t ld_dh, void *dw_dev, int64_t ld_dw, void *workspace_dev,
+                               int64_t workspace_bytes, void *stream);
+
+/* ----------------------------------------------- gated feed-forward blocks ---
+ * A block that answers from a row alone, for m rows x of d columns:
+ *   a = x Wg,  b = x Wu,  h = act(a) * b (entry by entry),  y = h Wd,
+ * Wg and Wu d x f, Wd f x d_out, all row-major with strides.  act: GNNAV_ACT_SILU
+ * a / (1 + exp(-a)), GNNAV_ACT_GELU a (1 + erf(a / sqrt 2)) / 2, GNNAV_ACT_RELU.
  * dt = F32: fp32-accurate products (six bf16 part products; an infinite entry may
  * make its products NaN; where saved_dev is given, ReLU's slope follows the sign of a
  * in 64 bits: entries of a within sqrt(d) 2^-24, or 2^-21, of the product of the norms of
