@@ -42,17 +42,6 @@ struct Args {
 
 __device__ __forceinline__ bool entry_there(int32_t id, float t) { return id >= 0 && t != -INFINITY; }
 
-__device__ __forceinline__ uint32_t bf16_pair(float lo, float hi) {
-    typedef float f32x2 __attribute__((ext_vector_type(2)));
-    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-    return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{lo, hi}, bf16x2));
-}
-
-template <bool BF>
-__device__ __forceinline__ float element(const u32x4x &v, int e) {
-    if constexpr (BF) return __uint_as_float(e & 1 ? v[e / 2] & 0xffff0000u : v[e / 2] << 16);
-    else return __uint_as_float(v[e]);
-}
 template <bool BF>
 __device__ __forceinline__ float logit(const char *row, int64_t c) {
     if constexpr (BF) return bf16_to_f32(((const uint16_t *)row)[c]);

@@ -36,13 +36,6 @@ typedef uint32_t u32x4x __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2x __attribute__((ext_vector_type(2)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 
-// Two values rounded to bf16, nearest even.
-__device__ __forceinline__ uint32_t bf16_pair(float lo, float hi) {
-    typedef float f32x2 __attribute__((ext_vector_type(2)));
-    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-    return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{lo, hi}, bf16x2));
-}
-
 // Two groups of 4 values (as bf16 pairs) of a lane, of its row's columns c .. c + 3 and c + 8 .. c + 11, with those of
 // lane ^ 32, c + 4 .. and c + 12 ..: the chunk of 8 from c for the lower lanes, from c + 8 for the upper ones.
 __device__ __forceinline__ u32x4x join_chunk(uint32_t a0, uint32_t a1, uint32_t b0, uint32_t b1) {

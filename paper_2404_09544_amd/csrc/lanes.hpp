@@ -1,4 +1,4 @@
-// A lane's value from another lane of its wavefront, without LDS.
+// A lane's values: from another lane of its wavefront, without LDS, and in and out of its words.
 #pragma once
 #include <hip/hip_runtime.h>
 #include <cstdint>
@@ -50,6 +50,19 @@ __device__ __forceinline__ float lanes_reduce(float x) {
         x = join(f(p.low), f(p.high));
     }
     return x;
+}
+
+// Two values in one conversion: the bits of bf16_rne.
+__device__ __forceinline__ uint32_t bf16_pair(float lo, float hi) {
+    typedef float f32x2 __attribute__((ext_vector_type(2)));
+    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{lo, hi}, bf16x2));
+}
+// Entry e of a vector of 32-bit words that hold fp32 values, or pairs of bf16 ones.
+template <bool BF, class V>
+__device__ __forceinline__ float element(const V &v, int e) {
+    if constexpr (BF) return __uint_as_float(e & 1 ? v[e / 2] & 0xffff0000u : v[e / 2] << 16);
+    else return __uint_as_float(v[e]);
 }
 
 }  // namespace gnnav

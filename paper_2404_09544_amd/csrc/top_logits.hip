@@ -31,12 +31,6 @@ __device__ __forceinline__ float logit_of(uint32_t order) {
     return __uint_as_float(order & 0x80000000u ? (order == 0xffffffffu ? 0x7fc00000u : order & 0x7fffffffu) : ~order);
 }
 
-template <bool BF>
-__device__ __forceinline__ float element(const u32x4x &v, int e) {
-    if constexpr (BF) return __uint_as_float(e & 1 ? v[e / 2] & 0xffff0000u : v[e / 2] << 16);
-    else return __uint_as_float(v[e]);
-}
-
 // The lanes of register r that keep the larger number of their pair in one step of a bitonic network over places
 // r * 64 + lane: falling where (place & block) == 0, rising elsewhere, and the other way round if `rising`.
 constexpr uint64_t larger_lanes(int r, int stride, int block, bool rising) {
