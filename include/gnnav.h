@@ -562,10 +562,10 @@ gnnav_status gnnav_linear_xent(const void *h_dev, int64_t ld_h, int64_t m, const
  * row from its last to the next 16-byte boundary are written with zeros; whatever
  * inputs hold there is not used.  m = 0 is allowed.
  *
- * saved_dev: NULL, or device memory of at least gnnav_gated_ffn_saved bytes (16-byte aligned)
- * that receives what the backward pass takes from the forward one, in an order of the
- * library's own: h (BF16: 2 bytes an entry; the backward pass forms a and b again), and a
- * and b (F32: 14 bytes an entry in all).
+ * saved_dev: NULL, or device memory of at least gnnav_gated_ffn_saved bytes (16-byte
+ * aligned) that receives what the backward pass takes from the forward one, in an
+ * order of the library's own: h (BF16: 2 bytes an entry; the backward pass forms a and
+ * b again), and a and b (F32: 14 bytes an entry in all).
  *
  * gnnav_gated_ffn_backward: from dy (m x d_out) and the saved_dev of the forward
  * pass with the same x, weights, sizes and act:
@@ -578,8 +578,8 @@ gnnav_status gnnav_linear_xent(const void *h_dev, int64_t ld_h, int64_t m, const
  * gnnav_gated_ffn_backward_workspace bytes (-1 for bad arguments; host only) on a
  * 256-byte boundary, used until the work has run; its contents do not matter.  No call
  * allocates or waits; sums run in a fixed order (no atomics: repeated calls give
- * identical bits).  Outputs must not overlap inputs or each other, saved_dev among them (the same
- * address is refused).
+ * identical bits).  Outputs must not overlap inputs or each other, saved_dev among
+ * them (the same address is refused).
  * Errors: E_INVALID (null pointers, sizes, strides, alignment, act, workspace),
  * E_CAPACITY (m beyond 2^28, d, f or d_out beyond 2^20), E_DEVICE.  Asynchronous.  */
 enum { GNNAV_ACT_SILU = 0, GNNAV_ACT_GELU = 1, GNNAV_ACT_RELU = 2 };
@@ -607,7 +607,8 @@ gnnav_status gnnav_gated_ffn_backward(const void *x_dev, int64_t ld_x, int64_t m
  * gnnav_distill: a student's logits z (m x n_classes, dt F32 or BF16) against
  * the k logits t that a teacher kept of each row, for the classes ids (fp32 and int32
  * [m][k] contiguous, as gnnav_top_logits writes them), temperature T from
- * 1.1e-19 to 1.8e19 (T^2 is a normal fp32 number; kd is T^2 times a sum that is rounded in fp32):
+ * 1.1e-19 to 1.8e19 (T^2 is a normal fp32 number; kd is T^2 times a sum that is
+ * rounded in fp32):
  *   q_j = softmax over the row's entries of t_j / T,  p = softmax(z / T),
  *   kd_i = T^2 sum_j q_j (log q_j - log p_id(j)),
  *   ce_i = -log softmax(z)_y, y = labels_dev[i],

@@ -139,7 +139,8 @@ struct Sums {
 __device__ __forceinline__ float exp_of(float x, float scale) { return __builtin_amdgcn_exp2f(x * scale); }
 
 // Whether the exponentials at 1 are needed beside those at T, and how they are had: from those at T = 2 or 4 by one or two
-// products, as exact (an exponent's rounding counts T times either way).  4,093 x 10,000 bf16 at T = 4: 64 us, 67 with two.
+// products.  The argument's rounding counts as much either way; exp2's own (2^-23) counts T times, and the products round
+// log2(T) times: at T = 4 within 2^-20 of the value.  4,093 x 10,000 bf16 at T = 4: 64 us, 67 with two.
 enum { kOne, kBoth, kSquare, kFourth };
 template <int WAY>
 __device__ __forceinline__ float exp_at_one(float x, float at_t) {

@@ -15,8 +15,9 @@
 //
 // Rounding: a and b stay in fp32 (bf16 ones would cost da and db a second rounding of the results' own size): fp32 keeps them
 // for the backward pass, bf16 multiplies x with Wg and Wu again in the tiles of dh, which is less time than 16 bytes an entry
-// until d is some 900, and five times less memory at any d.  h, da and db are rounded once to the operands' type for the
-// products that read them; where a product's output has few entries, so that it costs nothing, to two bf16 parts.
+// until d is some 900 and more past that (137 of 756 GFLOP at 8,192 x 1,024 x 4,096 x 1,024), and five times less memory at any d.  h, da
+// and db are rounded once to the operands' type for the products that read them, or to two bf16 parts where a product's
+// output has few entries.
 #include <algorithm>
 #include <cmath>
 
@@ -801,9 +802,10 @@ __device__ __forceinline__ void out_tile(const Product &a, int32_t id, u32x4x *S
 }
 
 // A workgroup takes tile after tile, the next one's first copies under way while one's results are formed and stored.
-// (Tiles of more than three stages are for launches that have one a workgroup.)  8,192 x 1,024 x 4,096 bf16: 137 us, 1,000 TFLOP/s,
-// bound by the matrix cores' power; 65,537 x 256 x 1,024: 110 us (117 with a tile a workgroup), bound by a tile's ends, its
-// sum having eight steps; 99,603 x 128 x 512: 69 us (73), four steps and the activation.
+// (Tiles of more than three stages are for launches that have one a workgroup.)  8,192 x 1,024 x 4,096 bf16: 137 to 163 us, 840 to 1,000
+// TFLOP/s, bound by the matrix cores' power; 65,537 x 256 x 1,024: 110 to 130 us (110 and 117 with a tile a workgroup on one
+// card), bound by a tile's ends, its sum having eight steps; 99,603 x 128 x 512: 66 to 69 us (73), four steps and SiLU; with
+// GELU, in fp32's accuracy, the block's two launches take 149 us instead of 88.
 template <int PL, int WMF, int WNF, int WGM, int WGN, int ST, int ACT>
 __global__ void __launch_bounds__(64 * WGM * WGN, 2) k_gated_gate(const Product a, int32_t ids) {
     constexpr int WA = WMF / 2;
@@ -835,16 +837,16 @@ __global__ void __launch_bounds__(64 * WGM * WGN, 2) k_gated_gate(const Product 
         }
     }
 }
-// 8,192 x 4,096 x 1,024 bf16: 105 us, 650 TFLOP/s: 256 tiles, one a unit, which leaves a step's latencies open; in tiles of 256 x 256
-// two splits' parts would take as long.  99,603 x 512 x 64: 28 us, 4.4 TB/s.
+// 8,192 x 4,096 x 1,024 bf16: 105 to 134 us, 510 to 650 TFLOP/s: 256 tiles, one a unit, which leaves a step's latencies open; in tiles of 256 x 256
+// two splits' parts would take as long.  99,603 x 512 x 64: 26 us, 4.4 TB/s.
 template <int PL, int WMF, int WNF, int WGM, int WGN, int ST>
 __global__ void __launch_bounds__(64 * WGM * WGN, 2) k_gated_down(const Product a) {
     __shared__ u32x4x S[Tile<PL, WMF, WNF, WGM, WGN, ST>::LDS];
     out_tile<PL, WMF, WNF, WGM, WGN, ST, true, false>(a, blockIdx.x, S);
 }
 // fp32 takes tile after tile too; bf16, whose three sums leave no registers for the next tile's copies, one: the copies of dh's sum
-// follow those of a and b.  8,192 x 1,024 x 4,096 x 1,024 bf16: 221 us, 930 TFLOP/s; 65,537 x 256 x 1,024 x 256: 197, its stores 1.4 TB/s
-// beside eight and sixteen steps.
+// follow those of a and b.  8,192 x 1,024 x 4,096 x 1,024 bf16: 221 to 264 us, 780 to 930 TFLOP/s; 65,537 x 256 x 1,024 x 256: 196 to 222, its
+// stores 1.4 TB/s beside eight and sixteen steps.
 template <int PL, int WA, int WNF, int WGM, int WGN, int ST, int ACT>
 __global__ void __launch_bounds__(64 * WGM * WGN, 2) k_gated_dgate(const Product a, const Sum again, int32_t ids) {
     constexpr int64_t AM = 32 * WA * WGM, BN = 32 * WNF * WGN;
@@ -892,8 +894,8 @@ __global__ void __launch_bounds__(64 * WGM * WGN, 2) k_gated_dgate(const Product
         }
     }
 }
-// dx and the weights' gradients in one launch (8,192 x 1,024 x 4,096 x 1,024 bf16: 308 us, 1,120 TFLOP/s; 65,537 x 256 x 1,024 x 256:
-// 218 us, 940 TFLOP/s and 4 TB/s): workgroups below `w_at` take dx's tiles, below `d_at` those of dWg and dWu.
+// dx and the weights' gradients in one launch (8,192 x 1,024 x 4,096 x 1,024 bf16: 307 to 352 us, 980 to 1,120 TFLOP/s; 65,537 x 256 x
+// 1,024 x 256: 218 to 233 us, 880 to 940 TFLOP/s and 4 TB/s): workgroups below `w_at` take dx's tiles, below `d_at` those of dWg and dWu.
 template <int PL, int WMF, int WNF, int WGM, int WGN, int ST>
 __global__ void __launch_bounds__(64 * WGM * WGN, 2) k_gated_grads(const Product x, const Product w, const Product d, int32_t w_at,
                                                                    int32_t d_at) {
@@ -943,7 +945,9 @@ __global__ void __launch_bounds__(256) k_gated_join(const JoinJobs jobs) {
 // At most 8 rows, nothing kept: the weights are read once as they lie and multiplied in fp32; h stays in fp32.  A workgroup
 // takes 32 columns, its lanes 16 bytes of a row each, the wavefronts different rows; the sums over the rows are joined in
 // registers and then in LDS.  Two launches: h, from both projections (MATS = 2), and y.
-// 1 x 1,024 x 4,096 x 1,024 bf16: 11.9 us, of which the weights' way at 4.72 TB/s is 5.3; 27 with the tiles.
+// 1 x 1,024 x 4,096 x 1,024 bf16: 12 us over the same weights again, 19 over four sets of them in turn, 30 over 24 sets, which no cache
+// holds (24, 24 and 26 with the tiles); the weights' way at 4.72 TB/s is 5.3.  The columns / 32 workgroups, 128 and 32 here, leave most of
+// the 256 units idle, and a round of 1,024 summed rows is not on its way while the one before it is multiplied.
 struct FewArgs {
     const void *x;             // rows that are multiplied: of the operands' type, or h in fp32
     int64_t ld_x;
@@ -1239,7 +1243,9 @@ struct Saved {
 };
 
 // Few rows that keep nothing; longer sums than these would have too few workgroups for themselves.  x 1,024 x 4,096 x 1,024 in
-// bf16: 1 row 12 us, 4 23, 8 37, in tiles 24; in fp32, whose tiles need the weights in planes: 22, 28, 37 and 65.
+// bf16 over the same weights again: 1 row 12 us, 4 23, 8 37, in tiles 24; over four sets of weights in turn 19, 28 for 4 rows, in tiles
+// 24; over 24 sets 30 and 38, in tiles 26.  In fp32, whose tiles need the weights in planes: 22, 28, 37 and 64 in tiles; 33, 39, 47
+// and 71 over 24 sets.
 bool few_rows(const GatedArgs &x) { return x.m <= (x.bf16 ? 4 : kFewRows) && !x.saved && x.d <= 16384 && x.f <= 16384; }
 
 template <int PL, int MR, int ACT>

@@ -162,7 +162,9 @@ int choose(const Shape *shapes, Job *jobs, int n, bool may_split, F &&jobs_of) {
     return which;
 }
 
-// Outputs of fewer entries take h, da and db in two bf16 parts.
+// Outputs of fewer entries take h, da and db in two bf16 parts: bf16's roundings average out over many entries and show in few.
+// Those outputs are then off by their own rounding, 0.0016 by norm, and not by 0.0023; steps of 1,024 x 602 x 1,024 x 7 take
+// 76 us (68 without), of 65,537 x 64 x 128 x 41, whose h of two parts costs more than elsewhere, 98 (86).
 constexpr int64_t kFew = 8192;
 
 // Where everything lies in the workspace, and how the products are cut.

@@ -7,7 +7,9 @@
 //                above the k-th of them goes to a buffer in LDS; a full buffer is sorted over the lanes and joined to the
 //                list (the larger of a falling and a rising list, place by place, is a bitonic one).  The k-th largest of the
 //                lanes' largest of the first logits is where it starts from: k logits are not below it.  On random logits
-//                some k log(n / k) of n are ever appended, so a logit costs a comparison and the row is read once.
+//                some k log(n / k) of n are ever appended, so a logit costs a comparison and the row is read once; of a
+//                rising row all are, and every block is sorted: 1,024 x 169,000 fp32, k = 32, 989 us instead of 142 (bf16 742 and
+//                88), one such row, in strips, 22 instead of 16.
 //   k_top_join   joins the strips' lists where long rows of few are cut.
 //   k_top_rows   many short rows and small k: a lane a row, its list in registers.
 #include <algorithm>
