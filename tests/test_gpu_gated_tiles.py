@@ -47,3 +47,47 @@ def test_both_passes(G, dtype, m, d, f, o, act, plan):
         whole = v.as_strided((v.shape[0], v.stride(0)), (v.stride(0), 1)).float()
         end = unit_end(c, dtype)
         assert (whole[:r, c:end] == 0).all() and (whole[:, end:] == -7).all() and (whole[r:] == -7).all(), n
+
+
+@pytest.mark.parametrize("dtype,m,d,f,o,act", [("bf16", 50_001, 256, 1_024, 256, "silu"), ("bf16", 8_193, 602, 1_024, 41, "relu"),
+                                               ("f32", 30_001, 200, 700, 100, "relu"), ("f32", 2_459, 21, 5_499, 105, "gelu")])
+def test_captured_and_on_a_share_of_the_units(G, dtype, m, d, f, o, act):
+    """Workgroups that take tiles in turn: on a quarter of the units, captured and replayed between eager calls on other rows, the same bits."""
+    import torch
+    say("gated turns", dtype, m, d, f, o, act)
+    gen = torch.Generator(device="cuda").manual_seed(7)
+    x, dy, wg, wu, wd = (rows(*s, dtype, gen, c) for s, c in (((m, d), 1.0), ((m, o), 1.0), ((d, f), d ** -0.5), ((d, f), d ** -0.5), ((f, o), f ** -0.5)))
+    others = rows(m, d, dtype, gen)
+    need = max(G.gated_ffn_workspace(m, d, f, o, dtype), G.gated_ffn_backward_workspace(m, d, f, o, dtype))
+
+    def state():
+        out = dict(y=rows(m, o, dtype), dx=rows(m, d, dtype), dwg=rows(d, f, dtype), dwu=rows(d, f, dtype), dwd=rows(f, o, dtype))
+        return out, saved_for(G, m, f, dtype), torch.full((need,), 0xFF, dtype=torch.uint8, device="cuda")
+
+    def step(s, xx, stream=None):
+        out, saved, ws = s
+        G.gated_ffn(xx, wg, wu, wd, out["y"], act=act, saved=saved, workspace=ws, stream=stream)
+        G.gated_ffn_backward(xx, wg, wu, wd, dy, saved, act=act, workspace=ws, stream=stream, **{n: v for n, v in out.items() if n != "y"})
+    eager, other, quarter, captured = (state() for _ in range(4))
+    step(eager, x)
+    share = G.stream_create(1, 4)
+    torch.cuda.synchronize()
+    step(quarter, x, share)
+    torch.cuda.synchronize()
+    G.stream_destroy(share)
+    graph, inner = torch.cuda.CUDAGraph(), x.clone()
+    xin = rows(m, d, dtype, gen)
+    xin.copy_(inner)
+    with torch.cuda.graph(graph):
+        step(captured, xin)
+    for it in range(3):
+        for v in captured[0].values():
+            v.fill_(3.0)
+        graph.replay()
+        step(other, others)
+        torch.cuda.synchronize()
+        for n, v in eager[0].items():
+            r = v.shape[0] - 1
+            assert torch.equal(v[:r], captured[0][n][:r]), (it, n)
+    for n, v in eager[0].items():
+        assert torch.equal(v, quarter[0][n]), n
